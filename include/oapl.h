@@ -65,7 +65,8 @@ typedef enum {
   OAPL_ERR_WORKSPACE = 7,   /* workspace NULL, misaligned or too small */
   OAPL_ERR_HIP = 8,         /* a HIP launch or runtime call failed */
   OAPL_ERR_TOKEN_RANGE = 9, /* device: sampled token outside [0, V) */
-  OAPL_ERR_SCRATCH_LIMIT = 10 /* oapl_loss_fwd_bwd_noalloc: the sizes need more than the static scratch */
+  OAPL_ERR_SCRATCH_LIMIT = 10, /* oapl_loss_fwd_bwd_noalloc: the sizes need more than the static scratch */
+  OAPL_ERR_ALIGN = 11       /* a pointer or stride of heads is not a multiple of 16 bytes */
 } oapl_status;
 
 typedef enum {
@@ -355,6 +356,124 @@ int32_t oapl_read_path_taken(const void* workspace, void* stream, int32_t* two_p
  */
 int32_t oapl_timing_enable(int32_t enable);
 int32_t oapl_timing_read(int32_t kernel, double* total_ms, int64_t* launches);
+
+/*
+ * The policy's attention, on the same packed rollouts: what lies below the loss
+ * head in the transformer's forward and backward pass.
+ *
+ * An operand of heads is [tokens][heads][head_dim] with head_dim channels side
+ * by side and any distance between tokens and between heads, so that the
+ * queries, keys and values that one projection writes side by side are read
+ * where they lie, and gradients are written where the projection's backward
+ * pass wants them.  Strides are in elements; inputs may have strides of 0
+ * (broadcast), rows that are written must not overlap.  Data and strides are
+ * multiples of 16 bytes (OAPL_ERR_ALIGN; the stride of a single token or head is not looked at), a token
+ * stride is at most 16 MiB (OAPL_ERR_SHAPE).
+ *   head_dim    8 .. 128, a multiple of 8
+ *   dtype       of every operand of heads and of the gains
+ * Sizes that are not served: OAPL_ERR_SHAPE.
+ */
+typedef struct {
+  void* data;
+  int64_t token_stride, head_stride;
+} oapl_heads;
+
+/*
+ * Norm of every query and key head, then the position rotation, in one pass:
+ *
+ *     y = R(pos_t) (gain o x / sqrt(mean_c x_c^2 + eps))
+ *
+ * R turns the channel pairs (i, i + rot_dim / 2), i < rot_dim / 2, by the angle
+ * whose cosine and sine are cos_sin[pos][i] and cos_sin[pos][rot_dim / 2 + i];
+ * channels from rot_dim on stay.  Sums and products in 32 bits, one rounding.
+ *   positions  [T] int32 in [0, n_positions); a token outside gets NaN
+ *   cos_sin    [n_positions][rot_dim] float, 16-byte aligned
+ *   q_gain, k_gain  [head_dim] in dtype, 16-byte aligned; both NULL: no norm
+ *   rot_dim    0 .. head_dim, a multiple of 8
+ *   rows       NULL, or [T] int64: token t's key (and value) goes to row rows[t]
+ *              of k_out (v_out), which have n_rows rows: a cache.  A row outside
+ *              [0, n_rows) is not written.  Rows must differ.
+ *   v, v_out   both NULL, or values to copy along with the keys
+ *   q_out may be q and k_out k (same strides, rows NULL).  Needs no workspace.
+ *   eps >= 0 and finite (else OAPL_ERR_BETA)
+ */
+int32_t oapl_qk_norm_rope_fwd(const oapl_heads* q, const oapl_heads* k, const oapl_heads* v,
+                              const int32_t* positions, const float* cos_sin,
+                              const void* q_gain, const void* k_gain, const int64_t* rows,
+                              int64_t T, int32_t n_q_heads, int32_t n_k_heads, int32_t head_dim,
+                              int32_t rot_dim, int64_t n_positions, int64_t n_rows, int32_t dtype, float eps,
+                              const oapl_heads* q_out, const oapl_heads* k_out, const oapl_heads* v_out,
+                              void* stream);
+
+/* Bytes of workspace of the next call; 0 for invalid sizes. */
+size_t oapl_qk_norm_rope_workspace_bytes(int64_t T, int32_t n_q_heads, int32_t n_k_heads, int32_t head_dim);
+
+/*
+ * Its gradients.  q, k: the inputs of the forward call; dq_out, dk_out:
+ * gradients of its outputs; dq, dk: gradients of its inputs (may be dq_out, dk_out).
+ *   dq_gain, dk_gain  [head_dim] float, summed over tokens and heads in a fixed
+ *                     order; not looked at without gains (nor is the workspace)
+ */
+int32_t oapl_qk_norm_rope_bwd(const oapl_heads* q, const oapl_heads* k,
+                              const oapl_heads* dq_out, const oapl_heads* dk_out,
+                              const int32_t* positions, const float* cos_sin,
+                              const void* q_gain, const void* k_gain,
+                              int64_t T, int32_t n_q_heads, int32_t n_k_heads, int32_t head_dim,
+                              int32_t rot_dim, int64_t n_positions, int32_t dtype, float eps,
+                              const oapl_heads* dq, const oapl_heads* dk, float* dq_gain, float* dk_gain,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace of the attention calls for these sizes (with_backward: of
+ * oapl_attention_bwd, otherwise of oapl_attention_fwd); 0 for invalid sizes. */
+size_t oapl_attention_workspace_bytes(int64_t Tq, int64_t Tk, int32_t n_seq, int32_t n_q_heads, int32_t n_k_heads,
+                                      int32_t head_dim, int32_t dtype, int32_t with_backward);
+
+/*
+ * Soft-max attention of packed sequences.  Sequence s has the queries
+ * [q_offsets[s], q_offsets[s+1]) and the keys [k_offsets[s], k_offsets[s+1]), or,
+ * with k_used, the first k_used[s] of them (a cache with room for more; what lies
+ * behind is not read).  With n_q queries and n_k keys, query i sees key j if
+ * causal is 0 or j <= i + n_k - n_q: the last query sees every key.
+ *
+ *     lse_i = ln sum_j exp(scale q_i . k_j),   out_i = sum_j exp(scale q_i . k_j - lse_i) v_j
+ *
+ * over the keys that i sees; where there are none, out_i = 0 and lse_i = -infinity.
+ * Query head h attends to key head h / (n_q_heads / n_k_heads).  Sums and the
+ * soft-max in 32 bits; OAPL_BF16 rounds the probabilities (before they are
+ * normalised) once for the product with the values.
+ * A NaN or infinity among the keys or values of a sequence may reach any row of that sequence,
+ * also rows that do not see it; it reaches no other sequence.
+ *   q_offsets, k_offsets  [n_seq + 1] int64 from 0 to Tq and Tk, non-decreasing
+ *                         (may be the same array; sequences may be empty)
+ *   k_used      NULL, or [n_seq] int64
+ *   lse         [Tq][n_q_heads] float, or NULL if not wanted
+ * Malformed offsets or k_used: OAPL_ERR_OFFSETS in the workspace's status, NaN in every output.
+ *   scale finite (else OAPL_ERR_BETA)
+ */
+int32_t oapl_attention_fwd(const oapl_heads* q, const oapl_heads* k, const oapl_heads* v,
+                           const int64_t* q_offsets, const int64_t* k_offsets, const int64_t* k_used,
+                           int64_t Tq, int64_t Tk, int32_t n_seq, int32_t n_q_heads, int32_t n_k_heads,
+                           int32_t head_dim, int32_t dtype, int32_t causal, float scale,
+                           const oapl_heads* out, float* lse,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its gradients, from the output and the log-sum-exp; the probabilities are
+ * computed again.  With P_ij = exp(scale q_i . k_j - lse_i) and D_i = dout_i . out_i:
+ *
+ *     dS_ij = P_ij (dout_i . v_j - D_i)
+ *     dq_i = scale sum_j dS_ij k_j,   dk_j = scale sum_i dS_ij q_i,   dv_j = sum_i P_ij dout_i
+ *
+ * dk and dv sum over the queries of all heads that share the key head, in a
+ * fixed order.  OAPL_BF16 rounds P and dS once for these products.
+ */
+int32_t oapl_attention_bwd(const oapl_heads* q, const oapl_heads* k, const oapl_heads* v,
+                           const oapl_heads* out, const float* lse, const oapl_heads* dout,
+                           const int64_t* q_offsets, const int64_t* k_offsets,
+                           int64_t Tq, int64_t Tk, int32_t n_seq, int32_t n_q_heads, int32_t n_k_heads,
+                           int32_t head_dim, int32_t dtype, int32_t causal, float scale,
+                           const oapl_heads* dq, const oapl_heads* dk, const oapl_heads* dv,
+                           void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,278 @@
+// C ABI of the policy's attention: argument checks, workspace plans, launches.  Part of the translation unit of oapl_api.hip.
+#pragma once
+
+#include "attention.hip.h"
+#include "norm_rope.hip.h"
+
+namespace oapl {
+
+constexpr int64_t kMaxRowBytes = (int64_t)1 << 24;   // between tokens: 64 of them stay within 32-bit offsets
+constexpr int64_t kMaxTileRows = ((int64_t)1 << 31) - 1024;
+
+static inline size_t esize(int dtype) { return dtype == OAPL_BF16 ? 2 : 4; }
+
+// A heads argument of n tokens and `heads` heads: 16-byte rows that an offset of 32 bits spans 64 of.  `written` rows must not overlap.
+static int check_heads(const oapl_heads* x, int64_t n, int heads, int D, int dtype, bool written) {
+  if (!x) return OAPL_ERR_NULL;
+  if (n == 0) return OAPL_OK;
+  if (!x->data) return OAPL_ERR_NULL;
+  const int64_t size = (int64_t)esize(dtype), least = written ? D : 0;
+  if (n > 1 && (x->token_stride < least || x->token_stride > kMaxRowBytes / size)) return OAPL_ERR_SHAPE;
+  if (heads > 1 && (x->head_stride < least || x->head_stride > ((int64_t)1 << 48))) return OAPL_ERR_SHAPE;
+  if ((uintptr_t)x->data % 16 || (n > 1 && x->token_stride * size % 16) || (heads > 1 && x->head_stride * size % 16))
+    return OAPL_ERR_ALIGN;
+  return OAPL_OK;
+}
+
+static Heads heads_of(const oapl_heads* x, int dtype) {
+  if (!x) return Heads{nullptr, 0, 0};
+  const int64_t size = (int64_t)esize(dtype);
+  return Heads{(char*)x->data, x->token_stride * size, x->head_stride * size};
+}
+
+static bool head_counts_ok(int hq, int hk, int D) {
+  return hk >= 1 && hq >= hk && hq % hk == 0 && hq <= 65536 && D >= 8 && D <= kMaxHeadDim && D % 8 == 0;
+}
+
+static bool workspace_ok(const void* ws, size_t have, size_t need) { return ws && (uintptr_t)ws % 256 == 0 && have >= need; }
+
+// ---------------------------------------------------------------------------------------------------------------- norm, rotation
+// Wavefronts that share a token: as many as its heads occupy (four at a time) while tokens alone do not fill the chip.
+static int rope_parts(int64_t T, int heads) {
+  int64_t parts = 4096 / (T > 0 ? T : 1);
+  const int most = (heads + 3) / 4;
+  return (int)(parts < 1 ? 1 : parts > most ? most : parts);
+}
+
+static unsigned rope_bwd_grid(int64_t T, int heads) {
+  const int64_t n = (T * rope_parts(T, heads) + 3) / 4;
+  return (unsigned)(n < 1024 ? n : 1024);
+}
+
+static int rope_args(NormRopeArgs& a, const oapl_heads* q, const oapl_heads* k, const int32_t* positions, const float* cos_sin,
+                     const void* q_gain, const void* k_gain, int64_t T, int hq, int hk, int D, int rot, int64_t n_pos, int dtype,
+                     float eps) {
+  if (dtype != OAPL_F32 && dtype != OAPL_BF16) return OAPL_ERR_DTYPE;
+  if (T < 0 || T > kMaxTileRows || hq < 1 || hk < 1 || hq > 65536 || hk > 65536 || D < 8 || D > kMaxHeadDim || D % 8 || rot < 0 ||
+      rot > D || rot % 8 || n_pos < 0)
+    return OAPL_ERR_SHAPE;
+  if (!(eps >= 0.f) || !isfinite(eps)) return OAPL_ERR_BETA;
+  if ((q_gain == nullptr) != (k_gain == nullptr)) return OAPL_ERR_NULL;
+  if (T > 0 && (!positions || (rot > 0 && n_pos > 0 && !cos_sin))) return OAPL_ERR_NULL;
+  if (int rc = check_heads(q, T, hq, D, dtype, false)) return rc;
+  if (int rc = check_heads(k, T, hk, D, dtype, false)) return rc;
+  if ((uintptr_t)cos_sin % 16 || (uintptr_t)q_gain % 16 || (uintptr_t)k_gain % 16) return OAPL_ERR_ALIGN;
+  a = NormRopeArgs{};
+  a.q = heads_of(q, dtype), a.k = heads_of(k, dtype);
+  a.positions = positions, a.cos_sin = cos_sin, a.q_gain = q_gain, a.k_gain = k_gain;
+  a.T = T, a.n_pos = n_pos, a.hq = hq, a.hk = hk, a.D = D, a.rot = rot, a.eps = eps;
+  return OAPL_OK;
+}
+
+// ---------------------------------------------------------------------------------------------------------------- attention
+struct AttnPlan {
+  size_t off_delta = 0, total = 0;
+};
+
+static bool attn_plan(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int hq, int hk, int D, int dtype, bool bwd) {
+  if (dtype != OAPL_F32 && dtype != OAPL_BF16) return false;
+  if (!head_counts_ok(hq, hk, D) || Tq < 0 || Tk < 0 || n_seq < 0 || (n_seq == 0 && (Tq || Tk)) || Tk > kMaxTileRows ||
+      Tq > kMaxTileRows / hq || n_seq > (1 << 24))
+    return false;
+  // every grid in 31 bits
+  if ((tile_ids<32>(Tq * (hq / hk), n_seq) + tile_ids<32>(Tk, n_seq)) * hk > kMaxTileRows) return false;
+  size_t at = kStatusWords * sizeof(int);
+  p.off_delta = at;
+  if (bwd) at += (size_t)round_up(Tq * hq * (int64_t)sizeof(float), 256);
+  p.total = at;
+  return true;
+}
+
+static int attn_args(AttnArgs& a, const oapl_heads* q, const oapl_heads* k, const oapl_heads* v, const int64_t* q_offsets,
+                     const int64_t* k_offsets, int64_t Tq, int64_t Tk, int n_seq, int hq, int hk, int D, int dtype, int causal,
+                     float scale) {
+  if (!isfinite(scale)) return OAPL_ERR_BETA;
+  if (n_seq > 0 && (!q_offsets || !k_offsets)) return OAPL_ERR_NULL;
+  if (int rc = check_heads(q, Tq, hq, D, dtype, false)) return rc;
+  if (int rc = check_heads(k, Tk, hk, D, dtype, false)) return rc;
+  if (int rc = check_heads(v, Tk, hk, D, dtype, false)) return rc;
+  a = AttnArgs{};
+  a.q = heads_of(q, dtype), a.k = heads_of(k, dtype), a.v = heads_of(v, dtype);
+  a.q_offsets = q_offsets, a.k_offsets = k_offsets;
+  a.Tq = Tq, a.Tk = Tk, a.n_seq = n_seq, a.hq = hq, a.hk = hk, a.g = hq / hk, a.D = D, a.causal = causal != 0, a.scale = scale;
+  return OAPL_OK;
+}
+
+// Head widths up to 64 and up to 128 have kernels of their own; channels behind D are zeros.
+template <class F>
+static int by_type(int dtype, int D, F&& launch) {
+  if (dtype == OAPL_BF16) return D <= 64 ? launch((bf16_t*)nullptr, std::integral_constant<int, 64>{}) : launch((bf16_t*)nullptr, std::integral_constant<int, 128>{});
+  return D <= 64 ? launch((float*)nullptr, std::integral_constant<int, 64>{}) : launch((float*)nullptr, std::integral_constant<int, 128>{});
+}
+
+template <class T, int DP>
+static int launch_attn_fwd(const AttnArgs& a, hipStream_t st) {
+  constexpr int lds = 2 * kKeys * Tile<T, DP>::kPitch;
+  if (!allow_big_lds(k_attn_fwd<T, DP>, lds)) return OAPL_ERR_HIP;
+  k_attn_fwd<T, DP><<<(unsigned)(tile_ids<128>(a.Tq * a.g, a.n_seq) * a.hk), 256, lds, st>>>(a);
+  OAPL_LAUNCH_CHECK();
+  return OAPL_OK;
+}
+
+template <class T, int DP>
+static int launch_attn_bwd(const AttnArgs& a, hipStream_t st) {
+  constexpr int lds = 2 * kKeys * Tile<T, DP>::kPitch, lds2 = 2 * 32 * Tile<T, DP>::kPitch + 32 * 12;
+  if (!allow_big_lds(k_attn_dq<T, DP>, lds)) return OAPL_ERR_HIP;
+  k_attn_dq<T, DP><<<(unsigned)(tile_ids<128>(a.Tq * a.g, a.n_seq) * a.hk), 256, lds, st>>>(a);
+  OAPL_LAUNCH_CHECK();
+  k_attn_dkdv<T, DP><<<(unsigned)(tile_ids<128>(a.Tk, a.n_seq) * a.hk), 256, lds2, st>>>(a);
+  OAPL_LAUNCH_CHECK();
+  return OAPL_OK;
+}
+
+}  // namespace oapl
+
+using namespace oapl;
+
+extern "C" {
+
+int32_t oapl_qk_norm_rope_fwd(const oapl_heads* q, const oapl_heads* k, const oapl_heads* v, const int32_t* positions,
+                              const float* cos_sin, const void* q_gain, const void* k_gain, const int64_t* rows, int64_t T,
+                              int32_t n_q_heads, int32_t n_k_heads, int32_t head_dim, int32_t rot_dim, int64_t n_positions,
+                              int64_t n_rows, int32_t dtype, float eps, const oapl_heads* q_out, const oapl_heads* k_out,
+                              const oapl_heads* v_out, void* stream) {
+  NormRopeArgs a;
+  if (int rc = rope_args(a, q, k, positions, cos_sin, q_gain, k_gain, T, n_q_heads, n_k_heads, head_dim, rot_dim, n_positions,
+                         dtype, eps))
+    return rc;
+  if (rows && n_rows < 0) return OAPL_ERR_SHAPE;
+  if ((v == nullptr) != (v_out == nullptr)) return OAPL_ERR_NULL;
+  const int64_t out_rows = rows ? n_rows : T;
+  if (int rc = check_heads(q_out, T, n_q_heads, head_dim, dtype, true)) return rc;
+  if (int rc = check_heads(k_out, out_rows, n_k_heads, head_dim, dtype, true)) return rc;
+  if (v) {
+    if (int rc = check_heads(v, T, n_k_heads, head_dim, dtype, false)) return rc;
+    if (int rc = check_heads(v_out, out_rows, n_k_heads, head_dim, dtype, true)) return rc;
+  }
+  if (T == 0) return OAPL_OK;
+  a.v = heads_of(v, dtype);
+  a.q_out = heads_of(q_out, dtype), a.k_out = heads_of(k_out, dtype), a.v_out = heads_of(v_out, dtype);
+  a.rows = rows, a.n_rows = n_rows;
+  a.parts = rope_parts(T, n_q_heads + n_k_heads * (v ? 2 : 1));
+  const unsigned grid = (unsigned)((T * a.parts + 3) / 4);
+  if (dtype == OAPL_BF16) k_qk_norm_rope_fwd<bf16_t><<<grid, 256, 0, (hipStream_t)stream>>>(a);
+  else k_qk_norm_rope_fwd<float><<<grid, 256, 0, (hipStream_t)stream>>>(a);
+  OAPL_LAUNCH_CHECK();
+  return OAPL_OK;
+}
+
+size_t oapl_qk_norm_rope_workspace_bytes(int64_t T, int32_t n_q_heads, int32_t n_k_heads, int32_t head_dim) {
+  if (T < 0 || T > kMaxTileRows || n_q_heads < 1 || n_k_heads < 1 || n_q_heads > 65536 || n_k_heads > 65536 || head_dim < 8 ||
+      head_dim > kMaxHeadDim || head_dim % 8)
+    return 0;
+  return (size_t)round_up((int64_t)rope_bwd_grid(T, n_q_heads + n_k_heads) * 2 * head_dim * (int64_t)sizeof(float) + 1, 256);
+}
+
+int32_t oapl_qk_norm_rope_bwd(const oapl_heads* q, const oapl_heads* k, const oapl_heads* dq_out, const oapl_heads* dk_out,
+                              const int32_t* positions, const float* cos_sin, const void* q_gain, const void* k_gain, int64_t T,
+                              int32_t n_q_heads, int32_t n_k_heads, int32_t head_dim, int32_t rot_dim, int64_t n_positions,
+                              int32_t dtype, float eps, const oapl_heads* dq, const oapl_heads* dk, float* dq_gain, float* dk_gain,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  NormRopeArgs a;
+  if (int rc = rope_args(a, q, k, positions, cos_sin, q_gain, k_gain, T, n_q_heads, n_k_heads, head_dim, rot_dim, n_positions,
+                         dtype, eps))
+    return rc;
+  if (int rc = check_heads(dq_out, T, n_q_heads, head_dim, dtype, false)) return rc;
+  if (int rc = check_heads(dk_out, T, n_k_heads, head_dim, dtype, false)) return rc;
+  if (int rc = check_heads(dq, T, n_q_heads, head_dim, dtype, true)) return rc;
+  if (int rc = check_heads(dk, T, n_k_heads, head_dim, dtype, true)) return rc;
+  if (q_gain && (!dq_gain || !dk_gain)) return OAPL_ERR_NULL;
+  if (q_gain &&
+      !workspace_ok(workspace, workspace_bytes, oapl_qk_norm_rope_workspace_bytes(T, n_q_heads, n_k_heads, head_dim)))
+    return OAPL_ERR_WORKSPACE;
+  a.q_out = heads_of(dq_out, dtype), a.k_out = heads_of(dk_out, dtype);
+  a.dq = heads_of(dq, dtype), a.dk = heads_of(dk, dtype);
+  a.partials = q_gain ? (float*)workspace : nullptr;
+  a.parts = rope_parts(T, n_q_heads + n_k_heads);
+  const unsigned grid = rope_bwd_grid(T, n_q_heads + n_k_heads);
+  hipStream_t st = (hipStream_t)stream;
+  if (T > 0) {
+    if (dtype == OAPL_BF16) k_qk_norm_rope_bwd<bf16_t><<<grid, 256, 0, st>>>(a);
+    else k_qk_norm_rope_bwd<float><<<grid, 256, 0, st>>>(a);
+    OAPL_LAUNCH_CHECK();
+  }
+  if (q_gain) {
+    k_gain_grads<<<2 * head_dim, 64, 0, st>>>(a.partials, (int)grid, head_dim, dq_gain, dk_gain);
+    OAPL_LAUNCH_CHECK();
+  }
+  return OAPL_OK;
+}
+
+size_t oapl_attention_workspace_bytes(int64_t Tq, int64_t Tk, int32_t n_seq, int32_t n_q_heads, int32_t n_k_heads,
+                                      int32_t head_dim, int32_t dtype, int32_t with_backward) {
+  AttnPlan p;
+  return attn_plan(p, Tq, Tk, n_seq, n_q_heads, n_k_heads, head_dim, dtype, with_backward != 0) ? p.total : 0;
+}
+
+int32_t oapl_attention_fwd(const oapl_heads* q, const oapl_heads* k, const oapl_heads* v, const int64_t* q_offsets,
+                           const int64_t* k_offsets, const int64_t* k_used, int64_t Tq, int64_t Tk, int32_t n_seq,
+                           int32_t n_q_heads, int32_t n_k_heads, int32_t head_dim, int32_t dtype, int32_t causal, float scale,
+                           const oapl_heads* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  if (dtype != OAPL_F32 && dtype != OAPL_BF16) return OAPL_ERR_DTYPE;
+  AttnPlan p;
+  if (!attn_plan(p, Tq, Tk, n_seq, n_q_heads, n_k_heads, head_dim, dtype, false)) return OAPL_ERR_SHAPE;
+  AttnArgs a;
+  if (int rc = attn_args(a, q, k, v, q_offsets, k_offsets, Tq, Tk, n_seq, n_q_heads, n_k_heads, head_dim, dtype, causal, scale))
+    return rc;
+  if (int rc = check_heads(out, Tq, n_q_heads, head_dim, dtype, true)) return rc;
+  if (!workspace_ok(workspace, workspace_bytes, p.total)) return OAPL_ERR_WORKSPACE;
+  hipStream_t st = (hipStream_t)stream;
+  a.o = heads_of(out, dtype);
+  a.lse = lse;
+  a.k_used = k_used;
+  a.status = (int*)workspace;
+  if (n_seq == 0) {
+    k_fill_i32<<<1, 64, 0, st>>>(a.status, kStatusWords, 0);
+    OAPL_LAUNCH_CHECK();
+    return OAPL_OK;
+  }
+  return by_type(dtype, head_dim, [&](auto* t, auto dp) {
+    return launch_attn_fwd<std::remove_pointer_t<decltype(t)>, decltype(dp)::value>(a, st);
+  });
+}
+
+int32_t oapl_attention_bwd(const oapl_heads* q, const oapl_heads* k, const oapl_heads* v, const oapl_heads* out, const float* lse,
+                           const oapl_heads* dout, const int64_t* q_offsets, const int64_t* k_offsets, int64_t Tq, int64_t Tk,
+                           int32_t n_seq, int32_t n_q_heads, int32_t n_k_heads, int32_t head_dim, int32_t dtype, int32_t causal,
+                           float scale, const oapl_heads* dq, const oapl_heads* dk, const oapl_heads* dv, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  if (dtype != OAPL_F32 && dtype != OAPL_BF16) return OAPL_ERR_DTYPE;
+  AttnPlan p;
+  if (!attn_plan(p, Tq, Tk, n_seq, n_q_heads, n_k_heads, head_dim, dtype, true)) return OAPL_ERR_SHAPE;
+  AttnArgs a;
+  if (int rc = attn_args(a, q, k, v, q_offsets, k_offsets, Tq, Tk, n_seq, n_q_heads, n_k_heads, head_dim, dtype, causal, scale))
+    return rc;
+  if (Tq > 0 && !lse) return OAPL_ERR_NULL;
+  if (int rc = check_heads(out, Tq, n_q_heads, head_dim, dtype, false)) return rc;
+  if (int rc = check_heads(dout, Tq, n_q_heads, head_dim, dtype, false)) return rc;
+  if (int rc = check_heads(dq, Tq, n_q_heads, head_dim, dtype, true)) return rc;
+  if (int rc = check_heads(dk, Tk, n_k_heads, head_dim, dtype, true)) return rc;
+  if (int rc = check_heads(dv, Tk, n_k_heads, head_dim, dtype, true)) return rc;
+  if (!workspace_ok(workspace, workspace_bytes, p.total)) return OAPL_ERR_WORKSPACE;
+  hipStream_t st = (hipStream_t)stream;
+  a.o = heads_of(out, dtype), a.dout = heads_of(dout, dtype);
+  a.dq = heads_of(dq, dtype), a.dk = heads_of(dk, dtype), a.dv = heads_of(dv, dtype);
+  a.lse = const_cast<float*>(lse);
+  a.delta = (float*)((char*)workspace + p.off_delta);
+  a.status = (int*)workspace;
+  if (n_seq == 0) {
+    k_fill_i32<<<1, 64, 0, st>>>(a.status, kStatusWords, 0);
+    OAPL_LAUNCH_CHECK();
+    return OAPL_OK;
+  }
+  return by_type(dtype, head_dim, [&](auto* t, auto dp) {
+    return launch_attn_bwd<std::remove_pointer_t<decltype(t)>, decltype(dp)::value>(a, st);
+  });
+}
+
+}  // extern "C"

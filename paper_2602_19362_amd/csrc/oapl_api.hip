@@ -5,6 +5,7 @@
 
 #include <math.h>
 #include <mutex>
+#include <type_traits>
 #include <utility>
 #include <vector>
 
@@ -1611,6 +1612,7 @@ const char* oapl_status_string(int32_t status) {
     case OAPL_ERR_HIP: return "HIP launch or runtime call failed";
     case OAPL_ERR_TOKEN_RANGE: return "sampled token outside [0, V)";
     case OAPL_ERR_SCRATCH_LIMIT: return "sizes need more than the library's 64 MiB static scratch";
+    case OAPL_ERR_ALIGN: return "a pointer or stride is not a multiple of 16 bytes";
     default: return "unknown status";
   }
 }
@@ -1831,3 +1833,5 @@ int32_t oapl_read_device_status(const void* workspace, void* stream, int32_t* st
 }
 
 }  // extern "C"
+
+#include "attention_api.hip.h"

@@ -23,11 +23,20 @@ OAPL_FLAG_TWO_PASS = 1
 STATUS_NAMES = {
     0: "OAPL_OK", 1: "OAPL_ERR_NULL", 2: "OAPL_ERR_SHAPE", 3: "OAPL_ERR_DTYPE", 4: "OAPL_ERR_OFFSETS",
     5: "OAPL_ERR_GROUP", 6: "OAPL_ERR_BETA", 7: "OAPL_ERR_WORKSPACE", 8: "OAPL_ERR_HIP", 9: "OAPL_ERR_TOKEN_RANGE",
-    10: "OAPL_ERR_SCRATCH_LIMIT",
+    10: "OAPL_ERR_SCRATCH_LIMIT", 11: "OAPL_ERR_ALIGN",
 }
 
 # Every symbol include/oapl.h declares, with its ctypes signature.
 _c = ctypes
+
+
+class Heads(ctypes.Structure):
+    """oapl_heads: an operand [tokens][heads][channels], strides in elements."""
+
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+_H = ctypes.POINTER(Heads)
 _SIGNATURES = {
     "oapl_status_string": (_c.c_char_p, [_c.c_int32]),
     "oapl_workspace_bytes": (_c.c_size_t, [_c.c_int64, _c.c_int32, _c.c_int32, _c.c_int32, _c.c_int32, _c.c_int32,
@@ -50,6 +59,16 @@ _SIGNATURES = {
     "oapl_grpo_loss_fwd_bwd": (_c.c_int32, [_c.c_void_p] * 8 + [_c.c_int64] + [_c.c_int32] * 5 + [_c.c_float] * 3 +
                                [_c.c_uint32] + [_c.c_void_p] * 6 + [_c.c_size_t, _c.c_void_p]),
     "oapl_segmented_sum_f32": (_c.c_int32, [_c.c_void_p, _c.c_void_p, _c.c_int32, _c.c_void_p, _c.c_void_p]),
+    "oapl_qk_norm_rope_fwd": (_c.c_int32, [_H] * 3 + [_c.c_void_p] * 5 + [_c.c_int64] + [_c.c_int32] * 4 + [_c.c_int64] * 2 +
+                              [_c.c_int32, _c.c_float] + [_H] * 3 + [_c.c_void_p]),
+    "oapl_qk_norm_rope_workspace_bytes": (_c.c_size_t, [_c.c_int64] + [_c.c_int32] * 3),
+    "oapl_qk_norm_rope_bwd": (_c.c_int32, [_H] * 4 + [_c.c_void_p] * 4 + [_c.c_int64] + [_c.c_int32] * 4 + [_c.c_int64] +
+                              [_c.c_int32, _c.c_float] + [_H] * 2 + [_c.c_void_p] * 3 + [_c.c_size_t, _c.c_void_p]),
+    "oapl_attention_workspace_bytes": (_c.c_size_t, [_c.c_int64] * 2 + [_c.c_int32] * 6),
+    "oapl_attention_fwd": (_c.c_int32, [_H] * 3 + [_c.c_void_p] * 3 + [_c.c_int64] * 2 + [_c.c_int32] * 6 +
+                           [_c.c_float, _H] + [_c.c_void_p] * 2 + [_c.c_size_t, _c.c_void_p]),
+    "oapl_attention_bwd": (_c.c_int32, [_H] * 4 + [_c.c_void_p, _H] + [_c.c_void_p] * 2 + [_c.c_int64] * 2 + [_c.c_int32] * 6 +
+                           [_c.c_float] + [_H] * 3 + [_c.c_void_p, _c.c_size_t, _c.c_void_p]),
     "oapl_read_device_status": (_c.c_int32, [_c.c_void_p, _c.c_void_p, _c.POINTER(_c.c_int32)]),
     "oapl_read_path_taken": (_c.c_int32, [_c.c_void_p, _c.c_void_p, _c.POINTER(_c.c_int32)]),
     "oapl_timing_enable": (_c.c_int32, [_c.c_int32]),
@@ -375,6 +394,183 @@ def grpo_loss_fwd_bwd(H, W, tokens, logq, logp_old, seq_offsets, rewards, group_
     if rc != 0:
         raise OaplError(rc, "oapl_grpo_loss_fwd_bwd")
     return GrpoResult(loss, logprob, adv, dH, dW, ws)
+
+
+def _heads(t: torch.Tensor, name: str, shape, like: torch.Tensor) -> Heads:
+    """The oapl_heads of a tensor [tokens, heads, channels] whose channels lie side by side."""
+    if t.device != like.device:
+        raise ValueError(f"{name} must live on {like.device}")
+    if t.dtype != like.dtype:
+        raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
+    if t.dim() != 3 or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.stride(2) != 1 and t.numel() > 0:
+        raise ValueError(f"the channels of {name} must lie side by side")
+    return Heads(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _qk_shapes(q: torch.Tensor, k: torch.Tensor):
+    _check_device(q)
+    _dtype_code(q)
+    if q.dim() != 3 or k.dim() != 3 or q.shape[2] != k.shape[2]:
+        raise ValueError("q and k must be [tokens, heads, channels] with the same channels")
+
+
+class NormRopeResult(NamedTuple):
+    q: torch.Tensor               # [T, n_q_heads, D]
+    k: torch.Tensor               # [T, n_k_heads, D], or the cache it was written to
+    v: Optional[torch.Tensor]     # the value cache
+
+
+def qk_norm_rope_fwd(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, cos_sin: torch.Tensor,
+                     q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None, *, eps: float = 1e-6,
+                     v: Optional[torch.Tensor] = None, rows: Optional[torch.Tensor] = None,
+                     q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                     v_out: Optional[torch.Tensor] = None) -> NormRopeResult:
+    """oapl_qk_norm_rope_fwd: norm of every query and key head and the position rotation, in one pass.
+
+    q, k (and v) may be views into one projection's output.  With `rows`, keys (and values) go to those rows of the caches
+    k_out (and v_out); without, k_out defaults to a new tensor.
+    """
+    _qk_shapes(q, k)
+    (T, hq, D), hk, dev = q.shape, k.shape[1], q.device
+    if positions.shape != (T,) or cos_sin.dim() != 2 or (rows is not None and rows.shape != (T,)):
+        raise ValueError("shape mismatch between q, positions, cos_sin and rows")
+    if (q_gain is None) != (k_gain is None) or (q_gain is not None and (q_gain.shape != (D,) or k_gain.shape != (D,))):
+        raise ValueError("q_gain and k_gain come as a pair, one value a channel")
+    if (v is None) != (v_out is None) or (rows is not None and k_out is None):
+        raise ValueError("rows need a cache k_out, values a cache v_out")
+    q_out = torch.empty((T, hq, D), dtype=q.dtype, device=dev) if q_out is None else q_out
+    k_out = torch.empty((T, hk, D), dtype=q.dtype, device=dev) if k_out is None else k_out
+    n_rows = T if rows is None else k_out.shape[0]
+    rc = lib().oapl_qk_norm_rope_fwd(
+        _heads(q, "q", (T, hq, D), q), _heads(k, "k", (T, hk, D), q), None if v is None else _heads(v, "v", (T, hk, D), q),
+        _dev(positions, torch.int32, "positions", dev), _dev(cos_sin, torch.float32, "cos_sin", dev),
+        _dev(q_gain, q.dtype, "q_gain", dev), _dev(k_gain, q.dtype, "k_gain", dev), _dev(rows, torch.int64, "rows", dev),
+        T, hq, hk, D, cos_sin.shape[1], cos_sin.shape[0], n_rows, _dtype_code(q), float(eps),
+        _heads(q_out, "q_out", (T, hq, D), q), _heads(k_out, "k_out", (n_rows, hk, D), q),
+        None if v is None else _heads(v_out, "v_out", (n_rows, hk, D), q), _stream(dev))
+    if rc != 0:
+        raise OaplError(rc, "oapl_qk_norm_rope_fwd")
+    return NormRopeResult(q_out, k_out, v_out)
+
+
+class NormRopeGrads(NamedTuple):
+    dq: torch.Tensor
+    dk: torch.Tensor
+    dq_gain: Optional[torch.Tensor]   # [D] float32
+    dk_gain: Optional[torch.Tensor]
+    workspace: Optional[torch.Tensor]
+
+
+def qk_norm_rope_bwd(q: torch.Tensor, k: torch.Tensor, dq_out: torch.Tensor, dk_out: torch.Tensor, positions: torch.Tensor,
+                     cos_sin: torch.Tensor, q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None, *,
+                     eps: float = 1e-6, dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None) -> NormRopeGrads:
+    """oapl_qk_norm_rope_bwd: gradients of the inputs (q, k) and of the gains, from those of the outputs."""
+    _qk_shapes(q, k)
+    (T, hq, D), hk, dev = q.shape, k.shape[1], q.device
+    if positions.shape != (T,) or cos_sin.dim() != 2:
+        raise ValueError("shape mismatch between q, positions and cos_sin")
+    if (q_gain is None) != (k_gain is None) or (q_gain is not None and (q_gain.shape != (D,) or k_gain.shape != (D,))):
+        raise ValueError("q_gain and k_gain come as a pair, one value a channel")
+    dq = torch.empty((T, hq, D), dtype=q.dtype, device=dev) if dq is None else dq
+    dk = torch.empty((T, hk, D), dtype=q.dtype, device=dev) if dk is None else dk
+    gains = ws = None
+    if q_gain is not None:
+        nbytes = lib().oapl_qk_norm_rope_workspace_bytes(T, hq, hk, D)
+        if nbytes == 0:
+            raise OaplError(2, "oapl_qk_norm_rope_workspace_bytes")
+        ws = _workspace(nbytes, dev, workspace)
+        gains = torch.empty((2, D), dtype=torch.float32, device=dev)
+    rc = lib().oapl_qk_norm_rope_bwd(
+        _heads(q, "q", (T, hq, D), q), _heads(k, "k", (T, hk, D), q), _heads(dq_out, "dq_out", (T, hq, D), q),
+        _heads(dk_out, "dk_out", (T, hk, D), q), _dev(positions, torch.int32, "positions", dev),
+        _dev(cos_sin, torch.float32, "cos_sin", dev), _dev(q_gain, q.dtype, "q_gain", dev), _dev(k_gain, q.dtype, "k_gain", dev),
+        T, hq, hk, D, cos_sin.shape[1], cos_sin.shape[0], _dtype_code(q), float(eps), _heads(dq, "dq", (T, hq, D), q),
+        _heads(dk, "dk", (T, hk, D), q), None if gains is None else gains[0].data_ptr(),
+        None if gains is None else gains[1].data_ptr(), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
+        _stream(dev))
+    if rc != 0:
+        raise OaplError(rc, "oapl_qk_norm_rope_bwd")
+    return NormRopeGrads(dq, dk, None if gains is None else gains[0], None if gains is None else gains[1], ws)
+
+
+def attention_workspace_bytes(Tq: int, Tk: int, n_seq: int, n_q_heads: int, n_k_heads: int, head_dim: int, dtype: int,
+                              with_backward: bool) -> int:
+    """oapl_attention_workspace_bytes."""
+    return int(lib().oapl_attention_workspace_bytes(Tq, Tk, n_seq, n_q_heads, n_k_heads, head_dim, dtype,
+                                                    1 if with_backward else 0))
+
+
+def _attention_setup(q, k, v, q_offsets, k_offsets, scale, with_backward, workspace):
+    _qk_shapes(q, k)
+    (Tq, hq, D), (Tk, hk, _) = q.shape, k.shape
+    k_offsets = q_offsets if k_offsets is None else k_offsets
+    if q_offsets.dim() != 1 or q_offsets.shape[0] < 1 or k_offsets.shape != q_offsets.shape:
+        raise ValueError("q_offsets and k_offsets must have one entry more than there are sequences")
+    n_seq = q_offsets.shape[0] - 1
+    nbytes = attention_workspace_bytes(Tq, Tk, n_seq, hq, hk, D, _dtype_code(q), with_backward)
+    if nbytes == 0:
+        raise OaplError(2, "oapl_attention_workspace_bytes")
+    ws = _workspace(nbytes, q.device, workspace)
+    heads = [_heads(q, "q", (Tq, hq, D), q), _heads(k, "k", (Tk, hk, D), q), _heads(v, "v", (Tk, hk, D), q)]
+    offsets = [_dev(q_offsets, torch.int64, "q_offsets", q.device), _dev(k_offsets, torch.int64, "k_offsets", q.device)]
+    sizes = [Tq, Tk, n_seq, hq, hk, D, _dtype_code(q)]
+    return heads, offsets, sizes, float(D ** -0.5 if scale is None else scale), ws
+
+
+class AttentionResult(NamedTuple):
+    out: torch.Tensor             # [Tq, n_q_heads, D]
+    lse: Optional[torch.Tensor]   # [Tq, n_q_heads] float32
+    workspace: torch.Tensor
+
+
+def attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor,
+                  k_offsets: Optional[torch.Tensor] = None, *, causal: bool = True, scale: Optional[float] = None,
+                  k_used: Optional[torch.Tensor] = None, want_lse: bool = True, out: Optional[torch.Tensor] = None,
+                  workspace: Optional[torch.Tensor] = None) -> AttentionResult:
+    """oapl_attention_fwd: soft-max attention of packed sequences, or of a few new tokens over a cache (k_used).
+
+    k_offsets defaults to q_offsets, scale to 1 / sqrt(D).
+    """
+    heads, offsets, sizes, scale, ws = _attention_setup(q, k, v, q_offsets, k_offsets, scale, False, workspace)
+    if k_used is not None and k_used.shape != (sizes[2],):
+        raise ValueError("k_used must have one entry a sequence")
+    out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
+    rc = lib().oapl_attention_fwd(*heads, *offsets, _dev(k_used, torch.int64, "k_used", q.device), *sizes, 1 if causal else 0,
+                                  scale, _heads(out, "out", q.shape, q), None if lse is None else lse.data_ptr(), ws.data_ptr(),
+                                  ws.numel(), _stream(q.device))
+    if rc != 0:
+        raise OaplError(rc, "oapl_attention_fwd")
+    return AttentionResult(out, lse, ws)
+
+
+class AttentionGrads(NamedTuple):
+    dq: torch.Tensor
+    dk: torch.Tensor
+    dv: torch.Tensor
+    workspace: torch.Tensor
+
+
+def attention_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor, dout: torch.Tensor,
+                  q_offsets: torch.Tensor, k_offsets: Optional[torch.Tensor] = None, *, causal: bool = True,
+                  scale: Optional[float] = None, dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
+                  dv: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> AttentionGrads:
+    """oapl_attention_bwd: gradients of q, k and v from attention_fwd's output and log-sum-exp and the output's gradient."""
+    heads, offsets, sizes, scale, ws = _attention_setup(q, k, v, q_offsets, k_offsets, scale, True, workspace)
+    dq, dk, dv = (torch.empty(x.shape, dtype=x.dtype, device=x.device) if g is None else g
+                  for x, g in ((q, dq), (k, dk), (v, dv)))
+    if lse.shape != q.shape[:2]:
+        raise ValueError("lse must be [tokens, heads] of q")
+    rc = lib().oapl_attention_bwd(*heads, _heads(out, "out", q.shape, q), _dev(lse, torch.float32, "lse", q.device),
+                                  _heads(dout, "dout", q.shape, q), *offsets, *sizes, 1 if causal else 0, scale,
+                                  _heads(dq, "dq", q.shape, q), _heads(dk, "dk", k.shape, q), _heads(dv, "dv", k.shape, q),
+                                  ws.data_ptr(), ws.numel(), _stream(q.device))
+    if rc != 0:
+        raise OaplError(rc, "oapl_attention_bwd")
+    return AttentionGrads(dq, dk, dv, ws)
 
 
 def segmented_sum_f32(x: torch.Tensor, seq_offsets: torch.Tensor) -> torch.Tensor:
