@@ -466,6 +466,7 @@ int32_t oapl_attention_fwd(const oapl_heads* q, const oapl_heads* k, const oapl_
  *
  * dk and dv sum over the queries of all heads that share the key head, in a
  * fixed order.  OAPL_BF16 rounds P and dS once for these products.
+ *   q, dout: the heads that share a key head lie within 1 GiB of each other (OAPL_ERR_SHAPE)
  */
 int32_t oapl_attention_bwd(const oapl_heads* q, const oapl_heads* k, const oapl_heads* v,
                            const oapl_heads* out, const float* lse, const oapl_heads* dout,

@@ -15,6 +15,7 @@
 // the lane holds them, and the soft-max needs one exchange between the two halves of a wavefront.
 #pragma once
 
+#include "gemm_bf16.hip.h"   // vmcnt_imm, lds_read_transposed
 #include "heads.hip.h"
 
 namespace oapl {
@@ -24,11 +25,13 @@ constexpr float kLn2f = 0.69314718055994531f;
 struct AttnArgs {
   Heads q, k, v, o, dout, dq, dk, dv;   // o: written forward, read backward
   float* lse;                           // [Tq][hq]; read backward; nullptr: not wanted (forward)
-  float* delta;                         // [Tq][hq] D_i, between the two backward kernels
+  float *lse2, *delta;                  // [Tq][hq] log-sum-exp in base 2 and D_i, between the two backward kernels
   const int64_t *q_offsets, *k_offsets, *k_used;
   int* status;
   int64_t Tq, Tk;
   int n_seq, hq, hk, g, D, causal;
+  uint32_t g_mul;                       // quotients by g, see by_group
+  int g_shift;
   float scale;
 };
 
@@ -99,22 +102,22 @@ template <class T> struct FragOf;
 template <> struct FragOf<bf16_t> { typedef bf16x8 type; };
 template <> struct FragOf<float> { typedef FragF32 type; };
 
-__device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ f32x16 mma(const FragF32& a, const FragF32& b, f32x16 c) {
+__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma(const FragF32& a, const FragF32& b, f32x4 c) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x[j >> 2][j & 3], b.x[j >> 2][j & 3], c, 0, 0, 0);
+  for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[j >> 2][j & 3], b.x[j >> 2][j & 3], c, 0, 0, 0);
   return c;
 }
-
-// Rows (keys) 8 (i / 4) + 4 half + i % 4 of a 32 x 32 result are in accumulator i; eight of them in a row, as an operand.
-__device__ __forceinline__ void pack(const f32x16& c, int chunk, bf16x8& f) {
+__device__ __forceinline__ void pack(f32x4 a, f32x4 b, bf16x8& f) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) f[j] = (bf16_t)c[chunk * 8 + j];
+  for (int j = 0; j < 4; ++j) f[j] = (bf16_t)a[j], f[j + 4] = (bf16_t)b[j];
 }
-__device__ __forceinline__ void pack(const f32x16& c, int chunk, FragF32& f) {
+__device__ __forceinline__ void pack_half(f32x4 a, int half, bf16x8& f) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) f.x[j >> 2][j & 3] = c[chunk * 8 + j];
+  for (int j = 0; j < 4; ++j) f[half * 4 + j] = (bf16_t)a[j];
 }
+__device__ __forceinline__ void pack_half(f32x4 a, int half, FragF32& f) { f.x[half] = a; }
+__device__ __forceinline__ void pack(f32x4 a, f32x4 b, FragF32& f) { f.x[0] = a, f.x[1] = b; }
 
 // A row's channels of one k-step from memory (nullptr: zeros).
 __device__ __forceinline__ void load_frag(const char* row, int c, int D, bf16x8& f) {
@@ -138,13 +141,19 @@ __device__ __forceinline__ float dot(const FragF32& a, const FragF32& b) {
   return s;
 }
 
+// A value that the compiler computes with where it stands, and not ahead of a loop.
+__device__ __forceinline__ int fresh(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // A tile of R rows of DP channels in LDS.  16-byte chunk c of row r lies at chunk c ^ swizzle(r): fetches of one chunk of many
 // rows, and transposing fetches of four rows of one column range, both touch every bank once.
 template <class T, int DP>
 struct Tile {
   static constexpr int kPitch = DP * (int)sizeof(T), kChunks = kPitch / 16;
   __device__ static __forceinline__ int swizzle(int r) {
-    return kChunks >= 16 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
+    return kChunks >= 16 ? (r & 3) << 2 | (r >> 2 & 1) << 1 | (r >> 3 & 1) : (r >> 1 & 1) << 2 | (r >> 2 & 1) << 1 | (r >> 3 & 1);
   }
   __device__ static __forceinline__ int at(int r, int c) { return r * kPitch + ((c ^ swizzle(r)) << 4); }
 
@@ -160,52 +169,85 @@ struct Tile {
     }
   }
 
-  // Operand of rows r0 + lane % 32, contracted over the 16 channels of step kk.
-  __device__ static __forceinline__ void rows(lds_char_ptr lds, int r0, int kk, bf16x8& f) {
+  // Operands come out of a tile at `lds` (a multiple of 256 bytes) from places that differ in a few bits of the chunk: a lane keeps
+  // one place for each kind, and the step's bits are put in where the operand is fetched (kept apart they would be a dozen registers).
+
+  // Rows r0 + lane % 16, contracted over the 32 channels of step kk.
+  __device__ static __forceinline__ int rows_place() {
     const int lane = threadIdx.x & 63;
-    f = *(__attribute__((address_space(3))) bf16x8*)(lds + at(r0 + (lane & 31), kk * 2 + (lane >> 5)));
+    return (lane & 15) * kPitch + (((lane >> 4) * ((int)sizeof(T) / 2) ^ swizzle(lane & 15)) << 4);
   }
-  __device__ static __forceinline__ void rows(lds_char_ptr lds, int r0, int kk, FragF32& f) {
-    const int lane = threadIdx.x & 63;
+  __device__ static __forceinline__ void rows(lds_char_ptr lds, int place, int r0, int kk, bf16x8& f) {
+    f = *(__attribute__((address_space(3))) bf16x8*)(lds + (fresh(place) ^ kk << 6) + r0 * kPitch);
+  }
+  __device__ static __forceinline__ void rows(lds_char_ptr lds, int place, int r0, int kk, FragF32& f) {
 #pragma unroll
     for (int x = 0; x < 2; ++x)
-      f.x[x] = *(__attribute__((address_space(3))) f32x4*)(lds + at(r0 + (lane & 31), kk * 4 + (lane >> 5) * 2 + x));
+      f.x[x] = *(__attribute__((address_space(3))) f32x4*)(lds + (place ^ (kk * 8 + x) << 4) + r0 * kPitch);
   }
 
-  // Operand of channels c0 + lane % 32, contracted over rows r0 .. r0 + 15 in the order of a result's accumulators.
-  // bf16: of the 16 lanes of a group, lane 4e + a points at four channels of row e, and lane i receives channel i of four rows.
-  __device__ static __forceinline__ void columns(lds_char_ptr lds, int r0, int c0, bf16x8& f) {
-    typedef __attribute__((address_space(3))) bf16x4* ptr;
+  // Channels 16 d + lane % 16, contracted over rows r0 .. r0 + 31 in the order in which the results of two blocks of 16 rows hold
+  // them.  bf16: of the 16 lanes of a group, lane 4e + a points at four channels of row e, and lane i receives channel i of four
+  // rows.
+  __device__ static __forceinline__ int columns_place() {
     const int lane = threadIdx.x & 63;
-    const int r = r0 + (lane >> 5) * 4 + (lane >> 2 & 3), c = c0 + (lane >> 4 & 1) * 16 + (lane & 3) * 4;
-    const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((ptr)(lds + at(r, c >> 3) + (c & 4) * 2));
-    const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((ptr)(lds + at(r + 8, c >> 3) + (c & 4) * 2));
+    if (sizeof(T) == 2) {
+      const int r = (lane >> 4) * 4 + (lane >> 2 & 3);
+      return r * kPitch + (((lane >> 1 & 1) ^ swizzle(r)) << 4) + ((lane & 1) << 3);
+    }
+    return (lane >> 4) * 4 * kPitch + (((lane >> 2 & 3) ^ swizzle((lane >> 4) * 4)) << 4) + ((lane & 3) << 2);
+  }
+  __device__ static __forceinline__ void columns(lds_char_ptr lds, int place, int r0, int d, bf16x8& f) {
+    const lds_char_ptr at = lds + (fresh(place) ^ d << 5) + r0 * kPitch;
+    const bf16x4 x = lds_read_transposed(at), y = lds_read_transposed(at + 16 * kPitch);
     f = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
   }
-  __device__ static __forceinline__ void columns(lds_char_ptr lds, int r0, int c0, FragF32& f) {
-    const int lane = threadIdx.x & 63, c = c0 + (lane & 31);
+  __device__ static __forceinline__ void columns(lds_char_ptr lds, int place, int r0, int d, FragF32& f) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int r = r0 + (lane >> 5) * 4 + (j & 3) + (j >> 2) * 8;
-      f.x[j >> 2][j & 3] = *(__attribute__((address_space(3))) float*)(lds + at(r, c >> 2) + (c & 3) * 4);
+    for (int j = 0; j < 8; ++j)
+      f.x[j >> 2][j & 3] = *(__attribute__((address_space(3))) float*)(lds + (place ^ (d ^ (j & 3)) << 6) +
+                                                                        (r0 + (j & 3) + (j >> 2) * 16) * kPitch);
+  }
+};
+
+// Rows of one tile of R rows of DP channels on their way from memory to LDS without passing through registers: 16 bytes a lane, whole
+// LDS rows a wavefront.  What lies behind the last row or channel is behind the buffer's range and reads as zeros.
+template <class T, int DP, int R>
+struct Stager {
+  typedef Tile<T, DP> Lds;
+  static constexpr int kRows = 64 / Lds::kChunks;          // that a wavefront's load covers
+  static constexpr int kLoads = R / (4 * kRows);           // of each of four wavefronts
+  static constexpr uint32_t kOutside = 0x80000000u;        // rows of a tile span 2^30 bytes at most
+  const char* base;
+  int64_t stride;
+  int row, wave;
+  uint32_t column;
+  __device__ __forceinline__ Stager(const char* p, int64_t token_stride, int D) : base(p), stride(token_stride) {
+    const int lane = threadIdx.x & 63;
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    row = wave * kRows + lane / Lds::kChunks;
+    const int c = (lane % Lds::kChunks) ^ Lds::swizzle(row);
+    column = c * 16 < D * (int)sizeof(T) ? c * 16 : kOutside;
+  }
+  // Starts the loads of rows [first, first + R), of which those from `n` on (counted from the base) do not exist.
+  __device__ __forceinline__ void start(lds_char_ptr lds, int first, int n) const {
+    const __amdgpu_buffer_rsrc_t r =
+        __builtin_amdgcn_make_buffer_rsrc((void*)(base + first * stride), 0, kOutside, 0x00020000);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int at = row + j * 4 * kRows;
+      // rows 16 apart are swizzled alike; a wavefront of two rows comes back to them with every other load
+      const uint32_t flip = 4 * kRows % 16 ? (uint32_t)(j & 1) << 4 : 0;
+      const uint32_t v = first + at < n ? (uint32_t)(at * (int)stride) + (column ^ flip) : kOutside;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_ptr)(lds + (j * 4 + wave) * 1024), 16, v, 0, 0, 0);
     }
   }
 };
 
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
-
-// Four consecutive channels a lane: a result whose columns are rows (keys) of `row`.
-template <class T, int DB>
-__device__ __forceinline__ void store_columns(char* row, const f32x16 (&acc)[DB], float factor, int D) {
-  if (!row) return;
-  const int half = threadIdx.x >> 5 & 1;
-#pragma unroll
-  for (int b = 0; b < DB; ++b)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int c = b * 32 + i * 8 + half * 4;
-      if (c < D) store4((T*)row + c, f32x4{acc[b][i * 4], acc[b][i * 4 + 1], acc[b][i * 4 + 2], acc[b][i * 4 + 3]} * factor);
-    }
+// Everything that this wavefront started has arrived, and so has what the others of the workgroup started.
+__device__ __forceinline__ void staged_barrier() {
+  __builtin_amdgcn_s_waitcnt(vmcnt_imm(0) & ~0x0F00);      // vmcnt(0) lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
 }
 
 // What a lane of the forward and dq kernels knows of its row.
@@ -235,14 +277,61 @@ __device__ __forceinline__ int tile_sees(const AttnArgs& p, const SeqTile& t) {
 constexpr int kKeys = 64;   // keys staged at a time
 
 // ---------------------------------------------------------------------------------------------------------------- forward
-// A workgroup: 128 rows, 32 a wavefront, over all keys that they see.
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+
+__device__ __forceinline__ void negate(bf16x8& f) {
+  u32x4 x;
+  __builtin_memcpy(&x, &f, 16);
+  x ^= 0x80008000u;
+  __builtin_memcpy(&f, &x, 16);
+}
+__device__ __forceinline__ void negate(FragF32& f) { f.x[0] = -f.x[0], f.x[1] = -f.x[1]; }
+
+template <class T, int DB>
+__device__ __forceinline__ void store_columns(char* row, const f32x4 (&acc)[DB], float factor, int D) {
+  const int group = threadIdx.x >> 4 & 3;
+#pragma unroll
+  for (int b = 0; b < DB; ++b) {
+    const int c = b * 16 + group * 4;
+    if (c < D) store4((T*)row + c, acc[b] * factor);
+  }
+}
+
+// Over the four lanes that hold a row, in all of them.
+template <class F>
+__device__ __forceinline__ float over_row(float v, F f) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float row_max(float v) { return over_row(v, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float row_sum(float v) { return over_row(v, [](float a, float b) { return a + b; }); }
+
+// The order in which a group of products wants its operands out of LDS: a few fetches ahead, then one for every `N`
+// multiplications.  Left alone the compiler fetches two and waits for them.
+template <int FETCHES, int N>
+__device__ __forceinline__ void feed_products() {
+  constexpr int AHEAD = 4;
+  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+  for (int i = 0; i < FETCHES - AHEAD; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x8, N, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x8, AHEAD * N, 0);
+}
+
+// A workgroup: 128 rows, 32 a wavefront, over all keys that they see, 64 at a time.
 template <class T, int DP>
-__global__ __launch_bounds__(256) void k_attn_fwd(const AttnArgs p) {
+__global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs p) {
   typedef typename FragOf<T>::type Frag;
   typedef Tile<T, DP> Lds;
-  constexpr int B = 128, KS = DP / 16, DB = DP / 32;
+  typedef Stager<T, DP, kKeys> Stage;
+  constexpr int B = 128, KS = DP / 32, DB = DP / 16, KB = kKeys / 16, SIZE = kKeys * Lds::kPitch;
   extern __shared__ char smem[];
-  const lds_char_ptr ks = (lds_char_ptr)smem, vs = ks + kKeys * Lds::kPitch;
+  const lds_char_ptr lds = (lds_char_ptr)smem;     // two slots of keys and values
+  const int rp = Lds::rows_place(), cp = Lds::columns_place();
   const bool ok = sequences_ok(p);
   if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = ok ? 0 : kErrOffsets;
   if (!ok) {
@@ -253,152 +342,287 @@ __global__ __launch_bounds__(256) void k_attn_fwd(const AttnArgs p) {
   const int kh = blockIdx.x % p.hk;
   const SeqTile t = find_tile<B>(p, p.q_offsets, p.g, tile_ids<B>(p.Tq * p.g, p.n_seq) - 1 - blockIdx.x / p.hk);
   if (t.first >= t.nq * p.g) return;
-  const int lane = threadIdx.x & 63, half = lane >> 5;
-  const Row row(p, t, t.first + (threadIdx.x >> 6) * 32 + (lane & 31));
-  const int head = kh * p.g + row.head;
-  Frag q[KS];
-#pragma unroll
-  for (int kk = 0; kk < KS; ++kk) load_frag(row.exists ? p.q.row(t.q0 + row.token, head) : nullptr, kk * 16 + half * 8, p.D, q[kk]);
-  f32x16 o[DB] = {};
-  float m = kNegHuge, l = 0.f;     // l: this half's keys
-  const float scale2 = p.scale * kLog2e;
   const int sees = tile_sees<B>(p, t);
-  for (int j0 = 0; j0 < sees; j0 += kKeys) {
-    __syncthreads();
-    Lds::template fill<kKeys>(ks, p.k.row(t.k0 + j0, kh), p.k.token, t.nk - j0, p.D);
-    Lds::template fill<kKeys>(vs, p.v.row(t.k0 + j0, kh), p.v.token, t.nk - j0, p.D);
-    __syncthreads();
-    f32x16 s[2] = {};
+  const Stage ks(p.k.row(t.k0, kh), p.k.token, p.D), vs(p.v.row(t.k0, kh), p.v.token, p.D);
+  if (sees > 0) ks.start(lds, 0, t.nk), vs.start(lds + SIZE, 0, t.nk);
+  const int group = threadIdx.x >> 4 & 3, row0 = t.first + (threadIdx.x >> 6) * 32 + (threadIdx.x & 15);
+  const bool flip = p.scale < 0.f;                 // then products are taken with -q, and with zeros if it is 0
+  const float scale2 = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;
+  int row_sees[2];
+  Frag q[2][KS];
+  f32x4 o[2][DB] = {};
+  float m[2], l[2];                                // m: the running maximum before scaling; l: this lane's keys
+  int all_see = t.nk;                              // keys that every row of this wavefront sees
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const Row row(p, t, row0 + n * 16);
+    const char* x = row.exists && p.scale != 0.f ? p.q.row(t.q0 + row.token, kh * p.g + row.head) : nullptr;
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) {
+      load_frag(x, kk * 32 + group * 8, p.D, q[n][kk]);
+      if (flip) negate(q[n][kk]);
+    }
+    row_sees[n] = row.sees;
+    all_see = row.sees < all_see ? row.sees : all_see;
+    m[n] = kNegHuge;
+    l[n] = 0.f;
+  }
+#pragma unroll
+  for (int x = 8; x > 0; x >>= 1) {
+    const int y = __shfl_xor(all_see, x, 64);
+    all_see = y < all_see ? y : all_see;
+  }
+  all_see = __builtin_amdgcn_readfirstlane(all_see);
+  int slot = 0;
+  for (int j0 = 0; j0 < sees; j0 += kKeys, slot ^= 2 * SIZE) {
+    staged_barrier();
+    if (j0 + kKeys < sees) {
+      ks.start(lds + (slot ^ 2 * SIZE), j0 + kKeys, t.nk);
+      vs.start(lds + (slot ^ 2 * SIZE) + SIZE, j0 + kKeys, t.nk);
+    }
+    const lds_char_ptr kt = lds + slot, vt = kt + SIZE;
+    f32x4 s[2][KB] = {};
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk)
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int b = 0; b < KB; ++b) {
         Frag f;
-        Lds::rows(ks, b * 32, kk, f);
-        s[b] = mma(f, q[kk], s[b]);
+        Lds::rows(kt, rp, b * 16, kk, f);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) s[n][b] = mma(f, q[n][kk], s[n][b]);
       }
-    float top = kNegHuge;
+    feed_products<KS * KB, 2>();
+    if (j0 + kKeys > all_see) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+      for (int n = 0; n < 2; ++n)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int key = j0 + b * 32 + (i >> 2) * 8 + half * 4 + (i & 3);
-        s[b][i] = key < row.sees ? s[b][i] * scale2 : -__builtin_inff();
-        top = fmaxf(top, s[b][i]);
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (j0 + b * 16 + group * 4 + i >= row_sees[n]) s[n][b][i] = -__builtin_inff();
+    }
+    float top[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      top[n] = m[n];
+#pragma unroll
+      for (int b = 0; b < KB; ++b) top[n] = max3(max3(top[n], s[n][b][0], s[n][b][1]), s[n][b][2], s[n][b][3]);
+      top[n] = row_max(top[n]);
+    }
+    if (__any(fmaxf(top[0] - m[0], top[1] - m[1]) * scale2 > 8.f)) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const float old = __builtin_amdgcn_exp2f((m[n] - top[n]) * scale2);
+        m[n] = top[n];
+        l[n] *= old;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[n][d] *= old;
       }
-    top = fmaxf(m, fmaxf(top, other_half(top)));
-    const float old = __builtin_amdgcn_exp2f(m - top);
-    m = top;
-    l *= old;
+    }
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int n = 0; n < 2; ++n) {
+      const float m2 = m[n] * scale2;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[b][i] = __builtin_amdgcn_exp2f(s[b][i] - m);
-        l += s[b][i];
-      }
+      for (int b = 0; b < KB; ++b)
 #pragma unroll
-    for (int d = 0; d < DB; ++d) o[d] *= old;
+        for (int i = 0; i < 4; ++i) {
+          s[n][b][i] = __builtin_amdgcn_exp2f(fmaf(s[n][b][i], scale2, -m2));
+          l[n] += s[n][b][i];
+        }
+    }
 #pragma unroll
-    for (int c = 0; c < kKeys / 16; ++c) {
-      Frag f, w;
-      pack(s[c >> 1], c & 1, w);
+    for (int c = 0; c < KB / 2; ++c) {
+      Frag f, w[2];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) pack(s[n][c * 2], s[n][c * 2 + 1], w[n]);
 #pragma unroll
       for (int d = 0; d < DB; ++d) {
-        Lds::columns(vs, c * 16, d * 32, f);
-        o[d] = mma(f, w, o[d]);
+        Lds::columns(vt, cp, c * 32, d, f);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) o[n][d] = mma(f, w[n], o[n][d]);
       }
     }
   }
-  l += other_half(l);
-  if (!row.exists) return;
-  store_columns<T>(p.o.row(t.q0 + row.token, head), o, l > 0.f ? 1.f / l : l == 0.f ? 0.f : l, p.D);
-  if (p.lse && half == 0)
-    p.lse[(t.q0 + row.token) * p.hq + head] = l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2f;
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const Row row(p, t, row0 + n * 16);
+    l[n] = row_sum(l[n]);
+    if (!row.exists) continue;
+    const int head = kh * p.g + row.head;
+    store_columns<T>(p.o.row(t.q0 + row.token, head), o[n], l[n] > 0.f ? 1.f / l[n] : l[n] == 0.f ? 0.f : l[n], p.D);
+    if (p.lse && group == 0)
+      p.lse[(t.q0 + row.token) * p.hq + head] =
+          l[n] == 0.f ? -__builtin_inff() : fmaf(m[n], scale2, __builtin_amdgcn_logf(l[n])) * kLn2f;
+  }
 }
 
 // ---------------------------------------------------------------------------------------------------------------- backward
-// D_i and dq: a workgroup has 128 rows, as forward.
+// dq, and what the other kernel needs of a row: its log-sum-exp in base 2 and D_i.  A workgroup has 128 rows, as forward.
 template <class T, int DP>
-__global__ __launch_bounds__(256) void k_attn_dq(const AttnArgs p) {
+__global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
   typedef typename FragOf<T>::type Frag;
   typedef Tile<T, DP> Lds;
-  constexpr int B = 128, KS = DP / 16, DB = DP / 32;
+  typedef Stager<T, DP, kKeys> Stage;
+  constexpr int B = 128, KS = DP / 32, DB = DP / 16, SIZE = kKeys * Lds::kPitch;
   extern __shared__ char smem[];
-  const lds_char_ptr ks = (lds_char_ptr)smem, vs = ks + kKeys * Lds::kPitch;
+  const lds_char_ptr lds = (lds_char_ptr)smem;
+  const int rp = Lds::rows_place(), cp = Lds::columns_place();
   const bool ok = sequences_ok(p);
   if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = ok ? 0 : kErrOffsets;
   if (!ok) return poison<T>(p.dq, p.Tq, p.hq, p.D);
   const int kh = blockIdx.x % p.hk;
   const SeqTile t = find_tile<B>(p, p.q_offsets, p.g, tile_ids<B>(p.Tq * p.g, p.n_seq) - 1 - blockIdx.x / p.hk);
   if (t.first >= t.nq * p.g) return;
-  const int lane = threadIdx.x & 63, half = lane >> 5;
-  const Row row(p, t, t.first + (threadIdx.x >> 6) * 32 + (lane & 31));
-  const int head = kh * p.g + row.head;
-  const int64_t token = t.q0 + row.token;
-  Frag q[KS], dout[KS];
-  float delta = 0.f;
-#pragma unroll
-  for (int kk = 0; kk < KS; ++kk) {
-    Frag o;
-    load_frag(row.exists ? p.q.row(token, head) : nullptr, kk * 16 + half * 8, p.D, q[kk]);
-    load_frag(row.exists ? p.dout.row(token, head) : nullptr, kk * 16 + half * 8, p.D, dout[kk]);
-    load_frag(row.exists ? p.o.row(token, head) : nullptr, kk * 16 + half * 8, p.D, o);
-    delta += dot(o, dout[kk]);
-  }
-  delta += other_half(delta);
-  if (row.exists && half == 0) p.delta[token * p.hq + head] = delta;
-  const float scale2 = p.scale * kLog2e, lse2 = row.exists ? p.lse[token * p.hq + head] * kLog2e : 0.f;
-  f32x16 dq[DB] = {};
   const int sees = tile_sees<B>(p, t);
-  for (int j0 = 0; j0 < sees; j0 += kKeys) {
-    __syncthreads();
-    Lds::template fill<kKeys>(ks, p.k.row(t.k0 + j0, kh), p.k.token, t.nk - j0, p.D);
-    Lds::template fill<kKeys>(vs, p.v.row(t.k0 + j0, kh), p.v.token, t.nk - j0, p.D);
-    __syncthreads();
+  const Stage ks(p.k.row(t.k0, kh), p.k.token, p.D), vs(p.v.row(t.k0, kh), p.v.token, p.D);
+  if (sees > 0) ks.start(lds, 0, t.nk), vs.start(lds + SIZE, 0, t.nk);
+  const int group = threadIdx.x >> 4 & 3, row0 = t.first + (threadIdx.x >> 6) * 32 + (threadIdx.x & 15);
+  const float scale2 = p.scale * kLog2e;
+  int row_sees[2];
+  Frag q[2][KS], dout[2][KS];
+  float lse2[2], delta[2];
+  f32x4 dq[2][DB] = {};
+  int all_see = t.nk;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      f32x16 s = {}, dp = {};
+  for (int n = 0; n < 2; ++n) {
+    const Row row(p, t, row0 + n * 16);
+    const int64_t token = t.q0 + row.token;
+    const int head = kh * p.g + row.head;
+    delta[n] = 0.f;
 #pragma unroll
-      for (int kk = 0; kk < KS; ++kk) {
-        Frag f;
-        Lds::rows(ks, b * 32, kk, f);
-        s = mma(f, q[kk], s);
-        Lds::rows(vs, b * 32, kk, f);
-        dp = mma(f, dout[kk], dp);
-      }
+    for (int kk = 0; kk < KS; ++kk) {
+      Frag o;
+      load_frag(row.exists ? p.q.row(token, head) : nullptr, kk * 32 + group * 8, p.D, q[n][kk]);
+      load_frag(row.exists ? p.dout.row(token, head) : nullptr, kk * 32 + group * 8, p.D, dout[n][kk]);
+      load_frag(row.exists ? p.o.row(token, head) : nullptr, kk * 32 + group * 8, p.D, o);
+      delta[n] += dot(o, dout[n][kk]);
+    }
+    delta[n] = row_sum(delta[n]);
+    lse2[n] = row.exists ? p.lse[token * p.hq + head] * kLog2e : 0.f;
+    if (row.exists && group == 0) {
+      p.delta[token * p.hq + head] = delta[n];
+      // of a row that sees nothing: every probability comes out as 0
+      p.lse2[token * p.hq + head] = lse2[n] == -__builtin_inff() ? __builtin_inff() : lse2[n];
+    }
+    row_sees[n] = row.sees;
+    all_see = row.sees < all_see ? row.sees : all_see;
+  }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int key = j0 + b * 32 + (i >> 2) * 8 + half * 4 + (i & 3);
-        s[i] = key < row.sees ? __builtin_amdgcn_exp2f(s[i] * scale2 - lse2) * (dp[i] - delta) : 0.f;
-      }
+  for (int x = 8; x > 0; x >>= 1) {
+    const int y = __shfl_xor(all_see, x, 64);
+    all_see = y < all_see ? y : all_see;
+  }
+  all_see = __builtin_amdgcn_readfirstlane(all_see);
+  int slot = 0;
+  for (int j0 = 0; j0 < sees; j0 += kKeys, slot ^= 2 * SIZE) {
+    staged_barrier();
+    if (j0 + kKeys < sees) {
+      ks.start(lds + (slot ^ 2 * SIZE), j0 + kKeys, t.nk);
+      vs.start(lds + (slot ^ 2 * SIZE) + SIZE, j0 + kKeys, t.nk);
+    }
+    const lds_char_ptr kt = lds + slot, vt = kt + SIZE;
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        Frag f, w;
-        pack(s, c, w);
+    for (int c = 0; c < kKeys / 32; ++c) {
+      f32x4 s[2][2] = {}, dp[2][2] = {};
 #pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          Lds::columns(ks, b * 32 + c * 16, d * 32, f);
-          dq[d] = mma(f, w, dq[d]);
+      for (int kk = 0; kk < KS; ++kk)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          Frag f, g;
+          Lds::rows(kt, rp, c * 32 + b * 16, kk, f);
+          Lds::rows(vt, rp, c * 32 + b * 16, kk, g);
+#pragma unroll
+          for (int n = 0; n < 2; ++n) s[n][b] = mma(f, q[n][kk], s[n][b]);
+#pragma unroll
+          for (int n = 0; n < 2; ++n) dp[n][b] = mma(g, dout[n][kk], dp[n][b]);
         }
+      feed_products<KS * 4, 2>();
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            s[n][b][i] = __builtin_amdgcn_exp2f(fmaf(s[n][b][i], scale2, -lse2[n])) * (dp[n][b][i] - delta[n]);
+      if (j0 + c * 32 + 32 > all_see) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (j0 + c * 32 + b * 16 + group * 4 + i >= row_sees[n]) s[n][b][i] = 0.f;
+      }
+      Frag f, w[2];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) pack(s[n][0], s[n][1], w[n]);
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        Lds::columns(kt, cp, c * 32, d, f);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) dq[n][d] = mma(f, w[n], dq[n][d]);
       }
     }
   }
-  if (row.exists) store_columns<T>(p.dq.row(token, head), dq, p.scale, p.D);
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const Row row(p, t, row0 + n * 16);
+    if (row.exists) store_columns<T>(p.dq.row(t.q0 + row.token, kh * p.g + row.head), dq[n], p.scale, p.D);
+  }
 }
 
-// dk and dv: a workgroup has 128 keys, 32 a wavefront, over all rows that see any of them.
+// Quotients by the group size of numbers below 2^31: (x * mul) >> shift.
+__device__ __forceinline__ int by_group(const AttnArgs& p, int x) { return (int)((uint64_t)(uint32_t)x * p.g_mul >> p.g_shift); }
+
+constexpr int kRows = 64;    // rows staged at a time
+
+// Rows of two operands (queries and the output's gradient) and the rows' two numbers on their way to LDS, as Stager; what lies
+// behind the sequence's last row or channel D reads as zeros.
 template <class T, int DP>
-__global__ __launch_bounds__(256) void k_attn_dkdv(const AttnArgs p) {
+struct RowStager {
+  typedef Tile<T, DP> Lds;
+  static constexpr int kRowsPerLoad = 64 / Lds::kChunks, kLoads = kRows / (4 * kRowsPerLoad), SIZE = kRows * Lds::kPitch;
+  static constexpr int kBytes = 2 * SIZE + 2 * kRows * 4;
+  static constexpr uint32_t kOutside = 0x80000000u;
+  __device__ static __forceinline__ void start(const AttnArgs& p, const SeqTile& t, int kh, lds_char_ptr lds, int first) {
+    // nothing of the addresses is kept from one tile to the next: the registers are needed elsewhere
+    const int lane = fresh(threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rows = t.nq * p.g, token0 = by_group(p, first);
+    const __amdgpu_buffer_rsrc_t q =
+        __builtin_amdgcn_make_buffer_rsrc((void*)p.q.row(t.q0 + token0, kh * p.g), 0, kOutside, 0x00020000);
+    const __amdgpu_buffer_rsrc_t d =
+        __builtin_amdgcn_make_buffer_rsrc((void*)p.dout.row(t.q0 + token0, kh * p.g), 0, kOutside, 0x00020000);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int r = (j * 4 + wave) * kRowsPerLoad + lane / Lds::kChunks, x = first + r;
+      const int c = ((lane % Lds::kChunks) ^ Lds::swizzle(r)) * 16;
+      const int token = by_group(p, x), head = x - token * p.g;
+      const bool any = x < rows && c < p.D * (int)sizeof(T);
+      const uint32_t vq = any ? (uint32_t)((token - token0) * (int)p.q.token + head * (int)p.q.head + c) : kOutside;
+      const uint32_t vd = any ? (uint32_t)((token - token0) * (int)p.dout.token + head * (int)p.dout.head + c) : kOutside;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(q, (lds_void_ptr)(lds + (j * 4 + wave) * 1024), 16, vq, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(d, (lds_void_ptr)(lds + SIZE + (j * 4 + wave) * 1024), 16, vd, 0, 0, 0);
+    }
+    if (wave < 2) {
+      const int x = first + lane, token = by_group(p, x);
+      const __amdgpu_buffer_rsrc_t n = __builtin_amdgcn_make_buffer_rsrc(
+          (void*)((wave ? p.delta : p.lse2) + (t.q0 + token0) * p.hq + kh * p.g), 0, kOutside, 0x00020000);
+      const uint32_t v = x < rows ? (uint32_t)((token - token0) * p.hq + x - token * p.g) * 4 : kOutside;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(n, (lds_void_ptr)(lds + 2 * SIZE + wave * kRows * 4), 4, v, 0, 0, 0);
+    }
+  }
+};
+
+// dk and dv: a workgroup has 128 keys, 32 a wavefront, over all rows that see any of them, 64 at a time.
+template <class T, int DP>
+__global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   typedef typename FragOf<T>::type Frag;
   typedef Tile<T, DP> Lds;
-  constexpr int B = 128, KS = DP / 16, DB = DP / 32, R = 32;
+  typedef RowStager<T, DP> Stage;
+  constexpr int B = 128, KS = DP / 32, DB = DP / 16;
   extern __shared__ char smem[];
-  const lds_char_ptr qs = (lds_char_ptr)smem, ds = qs + R * Lds::kPitch;
-  typedef __attribute__((address_space(3))) float* lds_f32;
-  typedef __attribute__((address_space(3))) int* lds_i32;
-  const lds_f32 lse2s = (lds_f32)(ds + R * Lds::kPitch), deltas = lse2s + R;
-  const lds_i32 seess = (lds_i32)(deltas + R);
+  const lds_char_ptr lds = (lds_char_ptr)smem;
+  const int rp = Lds::rows_place(), cp = Lds::columns_place();
   if (!sequences_ok(p)) {
     poison<T>(p.dk, p.Tk, p.hk, p.D);
     return poison<T>(p.dv, p.Tk, p.hk, p.D);
@@ -406,76 +630,95 @@ __global__ __launch_bounds__(256) void k_attn_dkdv(const AttnArgs p) {
   const int kh = blockIdx.x % p.hk;
   const SeqTile t = find_tile<B>(p, p.k_offsets, 1, blockIdx.x / p.hk);
   if (t.first >= t.nk) return;
-  const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int key = t.first + (threadIdx.x >> 6) * 32 + (lane & 31);
-  const bool exists = key < t.nk;
-  Frag k[KS], v[KS];
+  const int rows = t.nq * p.g, ahead = t.nk - t.nq;
+  // the first row that sees the tile's first key, and whole tiles of rows
+  const int from = p.causal && t.first > ahead ? (t.first - ahead) * p.g / kRows * kRows : 0;
+  if (from < rows) Stage::start(p, t, kh, lds, from);
+  const int group = threadIdx.x >> 4 & 3, key0 = t.first + (threadIdx.x >> 6) * 32 + (threadIdx.x & 15);
+  Frag k[2][KS], v[2][KS];
+  f32x4 dk[2][DB] = {}, dv[2][DB] = {};
+  int first_row[2], all_from = 0;     // rows from here on see the key; from all_from on every key of the wavefront
 #pragma unroll
-  for (int kk = 0; kk < KS; ++kk) {
-    load_frag(exists ? p.k.row(t.k0 + key, kh) : nullptr, kk * 16 + half * 8, p.D, k[kk]);
-    load_frag(exists ? p.v.row(t.k0 + key, kh) : nullptr, kk * 16 + half * 8, p.D, v[kk]);
-  }
-  f32x16 dk[DB] = {}, dv[DB] = {};
-  const float scale2 = p.scale * kLog2e;
-  const int rows = t.nq * p.g;
-  // the first token that sees the tile's first key
-  const int from = p.causal && t.first > t.nk - t.nq ? t.first - (t.nk - t.nq) : 0;
-  for (int r0 = from * p.g / R * R; r0 < rows; r0 += R) {
-    __syncthreads();
-#pragma unroll 4
-    for (int i = threadIdx.x; i < R * Lds::kChunks; i += 256) {
-      const int r = i / Lds::kChunks, c = i % Lds::kChunks, x = r0 + r;
-      u32x4 a = {}, b = {};
-      if (x < rows && c * 16 < p.D * (int)sizeof(T)) {
-        a = *(const u32x4*)(p.q.row(t.q0 + x / p.g, kh * p.g + x % p.g) + c * 16);
-        b = *(const u32x4*)(p.dout.row(t.q0 + x / p.g, kh * p.g + x % p.g) + c * 16);
-      }
-      *(__attribute__((address_space(3))) u32x4*)(qs + Lds::at(r, c)) = a;
-      *(__attribute__((address_space(3))) u32x4*)(ds + Lds::at(r, c)) = b;
-    }
-    if (threadIdx.x < R) {
-      const Row row(p, t, r0 + threadIdx.x);
-      const int64_t i = (t.q0 + row.token) * p.hq + kh * p.g + row.head;
-      lse2s[threadIdx.x] = row.exists ? p.lse[i] * kLog2e : 0.f;
-      deltas[threadIdx.x] = row.exists ? p.delta[i] : 0.f;
-      seess[threadIdx.x] = row.sees;
-    }
-    __syncthreads();
-    f32x16 s = {}, dp = {};
+  for (int n = 0; n < 2; ++n) {
+    const int key = key0 + n * 16;
+    const bool exists = key < t.nk;
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) {
-      Frag f;
-      Lds::rows(qs, 0, kk, f);
-      s = mma(f, k[kk], s);
-      Lds::rows(ds, 0, kk, f);
-      dp = mma(f, v[kk], dp);
+      load_frag(exists ? p.k.row(t.k0 + key, kh) : nullptr, kk * 32 + group * 8, p.D, k[n][kk]);
+      load_frag(exists ? p.v.row(t.k0 + key, kh) : nullptr, kk * 32 + group * 8, p.D, v[n][kk]);
     }
+    first_row[n] = p.causal && exists && key > ahead ? (key - ahead) * p.g : 0;
+    all_from = first_row[n] > all_from ? first_row[n] : all_from;
+  }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int r = (i >> 2) * 8 + half * 4 + (i & 3);
-      s[i] = key < seess[r] ? __builtin_amdgcn_exp2f(s[i] * scale2 - lse2s[r]) : 0.f;
-      dp[i] = key < seess[r] ? s[i] * (dp[i] - deltas[r]) : 0.f;
-    }
+  for (int x = 8; x > 0; x >>= 1) {
+    const int y = __shfl_xor(all_from, x, 64);
+    all_from = y > all_from ? y : all_from;
+  }
+  all_from = __builtin_amdgcn_readfirstlane(all_from);
+  const float scale2 = p.scale * kLog2e;
+  int slot = 0;
+  for (int r0 = from; r0 < rows; r0 += kRows, slot ^= 1) {
+    staged_barrier();
+    if (r0 + kRows < rows) Stage::start(p, t, kh, lds + (slot ^ 1) * Stage::kBytes, r0 + kRows);
+    const lds_char_ptr qt = lds + slot * Stage::kBytes, dt = qt + Stage::SIZE, numbers = dt + Stage::SIZE;
+#pragma unroll 1
+    for (int c = 0; c < kRows / 32; ++c) {
+      typedef __attribute__((address_space(3))) f32x4* ptr;
+      Frag f, w[2], wd[2];      // probabilities and dS of 32 rows, keys in columns
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      Frag f, w;
-      pack(s, c, w);
+      for (int b = 0; b < 2; ++b) {
+        f32x4 s[2] = {}, dp[2] = {};
 #pragma unroll
-      for (int d = 0; d < DB; ++d) {
-        Lds::columns(ds, c * 16, d * 32, f);
-        dv[d] = mma(f, w, dv[d]);
+        for (int kk = 0; kk < KS; ++kk) {
+          Frag g;
+          Lds::rows(qt, rp, c * 32 + b * 16, kk, f);
+          Lds::rows(dt, rp, c * 32 + b * 16, kk, g);
+#pragma unroll
+          for (int n = 0; n < 2; ++n) s[n] = mma(f, k[n][kk], s[n]);
+#pragma unroll
+          for (int n = 0; n < 2; ++n) dp[n] = mma(g, v[n][kk], dp[n]);
+        }
+        const f32x4 lse2 = *(ptr)(numbers + (c * 32 + b * 16 + group * 4) * 4);
+        const f32x4 delta = *(ptr)(numbers + kRows * 4 + (c * 32 + b * 16 + group * 4) * 4);
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], scale2, -lse2[i]));
+            dp[n][i] = s[n][i] * (dp[n][i] - delta[i]);
+          }
+        if (r0 + c * 32 < all_from) {
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (r0 + c * 32 + b * 16 + group * 4 + i < first_row[n]) s[n][i] = dp[n][i] = 0.f;
+        }
+#pragma unroll
+        for (int n = 0; n < 2; ++n) pack_half(s[n], b, w[n]), pack_half(dp[n], b, wd[n]);
       }
-      pack(dp, c, w);
 #pragma unroll
       for (int d = 0; d < DB; ++d) {
-        Lds::columns(qs, c * 16, d * 32, f);
-        dk[d] = mma(f, w, dk[d]);
+        Lds::columns(dt, cp, c * 32, d, f);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) dv[n][d] = mma(f, w[n], dv[n][d]);
+      }
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        Lds::columns(qt, cp, c * 32, d, f);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) dk[n][d] = mma(f, wd[n], dk[n][d]);
       }
     }
   }
-  if (!exists) return;
-  store_columns<T>(p.dk.row(t.k0 + key, kh), dk, p.scale, p.D);
-  store_columns<T>(p.dv.row(t.k0 + key, kh), dv, 1.f, p.D);
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const int key = key0 + n * 16;
+    if (key >= t.nk) continue;
+    store_columns<T>(p.dk.row(t.k0 + key, kh), dk[n], p.scale, p.D);
+    store_columns<T>(p.dv.row(t.k0 + key, kh), dv[n], 1.f, p.D);
+  }
 }
 
 }  // namespace oapl

@@ -71,7 +71,7 @@ static int rope_args(NormRopeArgs& a, const oapl_heads* q, const oapl_heads* k, 
 
 // ---------------------------------------------------------------------------------------------------------------- attention
 struct AttnPlan {
-  size_t off_delta = 0, total = 0;
+  size_t off_lse2 = 0, off_delta = 0, total = 0;
 };
 
 static bool attn_plan(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int hq, int hk, int D, int dtype, bool bwd) {
@@ -82,8 +82,9 @@ static bool attn_plan(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int hq, in
   // every grid in 31 bits
   if ((tile_ids<32>(Tq * (hq / hk), n_seq) + tile_ids<32>(Tk, n_seq)) * hk > kMaxTileRows) return false;
   size_t at = kStatusWords * sizeof(int);
-  p.off_delta = at;
-  if (bwd) at += (size_t)round_up(Tq * hq * (int64_t)sizeof(float), 256);
+  const size_t numbers = bwd ? (size_t)round_up(Tq * hq * (int64_t)sizeof(float), 256) : 0;
+  p.off_lse2 = at, at += numbers;
+  p.off_delta = at, at += numbers;
   p.total = at;
   return true;
 }
@@ -100,6 +101,11 @@ static int attn_args(AttnArgs& a, const oapl_heads* q, const oapl_heads* k, cons
   a.q = heads_of(q, dtype), a.k = heads_of(k, dtype), a.v = heads_of(v, dtype);
   a.q_offsets = q_offsets, a.k_offsets = k_offsets;
   a.Tq = Tq, a.Tk = Tk, a.n_seq = n_seq, a.hq = hq, a.hk = hk, a.g = hq / hk, a.D = D, a.causal = causal != 0, a.scale = scale;
+  // floor(2^(31 + s) / g) + 1 with 2^s >= g: exact for numbers below 2^31
+  int s = 0;
+  while ((1 << s) < a.g) ++s;
+  a.g_shift = 31 + s;
+  a.g_mul = (uint32_t)((((uint64_t)1 << a.g_shift) / (uint64_t)a.g) + 1);
   return OAPL_OK;
 }
 
@@ -110,24 +116,24 @@ static int by_type(int dtype, int D, F&& launch) {
   return D <= 64 ? launch((float*)nullptr, std::integral_constant<int, 64>{}) : launch((float*)nullptr, std::integral_constant<int, 128>{});
 }
 
-template <class T, int DP>
-static int launch_attn_fwd(const AttnArgs& a, hipStream_t st) {
-  constexpr int lds = 2 * kKeys * Tile<T, DP>::kPitch;
-  if (!allow_big_lds(k_attn_fwd<T, DP>, lds)) return OAPL_ERR_HIP;
-  k_attn_fwd<T, DP><<<(unsigned)(tile_ids<128>(a.Tq * a.g, a.n_seq) * a.hk), 256, lds, st>>>(a);
+template <class K>
+static int launch_attn(K kernel, int64_t workgroups, int lds, const AttnArgs& a, hipStream_t st) {
+  if (!allow_big_lds(kernel, lds)) return OAPL_ERR_HIP;
+  kernel<<<(unsigned)workgroups, 256, lds, st>>>(a);
   OAPL_LAUNCH_CHECK();
   return OAPL_OK;
 }
 
 template <class T, int DP>
+static int launch_attn_fwd(const AttnArgs& a, hipStream_t st) {
+  return launch_attn(k_attn_fwd<T, DP>, tile_ids<128>(a.Tq * a.g, a.n_seq) * a.hk, 4 * kKeys * Tile<T, DP>::kPitch, a, st);
+}
+
+template <class T, int DP>
 static int launch_attn_bwd(const AttnArgs& a, hipStream_t st) {
-  constexpr int lds = 2 * kKeys * Tile<T, DP>::kPitch, lds2 = 2 * 32 * Tile<T, DP>::kPitch + 32 * 12;
-  if (!allow_big_lds(k_attn_dq<T, DP>, lds)) return OAPL_ERR_HIP;
-  k_attn_dq<T, DP><<<(unsigned)(tile_ids<128>(a.Tq * a.g, a.n_seq) * a.hk), 256, lds, st>>>(a);
-  OAPL_LAUNCH_CHECK();
-  k_attn_dkdv<T, DP><<<(unsigned)(tile_ids<128>(a.Tk, a.n_seq) * a.hk), 256, lds2, st>>>(a);
-  OAPL_LAUNCH_CHECK();
-  return OAPL_OK;
+  if (int rc = launch_attn(k_attn_dq<T, DP>, tile_ids<128>(a.Tq * a.g, a.n_seq) * a.hk, 4 * kKeys * Tile<T, DP>::kPitch, a, st))
+    return rc;
+  return launch_attn(k_attn_dkdv<T, DP>, tile_ids<128>(a.Tk, a.n_seq) * a.hk, 2 * RowStager<T, DP>::kBytes, a, st);
 }
 
 }  // namespace oapl
@@ -261,8 +267,11 @@ int32_t oapl_attention_bwd(const oapl_heads* q, const oapl_heads* k, const oapl_
   if (!workspace_ok(workspace, workspace_bytes, p.total)) return OAPL_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)stream;
   a.o = heads_of(out, dtype), a.dout = heads_of(dout, dtype);
+  // RowStager's offsets: 64 tokens and the heads of a group within 31 bits
+  if ((a.g - 1) * std::max(a.q.head, a.dout.head) > ((int64_t)1 << 30)) return OAPL_ERR_SHAPE;
   a.dq = heads_of(dq, dtype), a.dk = heads_of(dk, dtype), a.dv = heads_of(dv, dtype);
   a.lse = const_cast<float*>(lse);
+  a.lse2 = (float*)((char*)workspace + p.off_lse2);
   a.delta = (float*)((char*)workspace + p.off_delta);
   a.status = (int*)workspace;
   if (n_seq == 0) {

@@ -3,6 +3,7 @@
 // computes on the host and nothing falls back to a CPU path.
 #include "oapl.h"
 
+#include <algorithm>
 #include <math.h>
 #include <mutex>
 #include <type_traits>

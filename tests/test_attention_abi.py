@@ -27,8 +27,8 @@ def fwd(Tq=4, Tk=4, n=1, hq=2, hk=1, D=64, dtype=1, scale=0.1, q=H(), k=H(), v=H
     return oapl.lib().oapl_attention_fwd(q, k, v, qo, ko, None, Tq, Tk, n, hq, hk, D, dtype, 1, scale, out, None, ws, have, None)
 
 
-def bwd(lse=AT, dq=H(), dk=H(), dv=H(), dout=H(), D=64, have=1 << 24):
-    return oapl.lib().oapl_attention_bwd(H(), H(), H(), H(), lse, dout, AT, AT, 4, 4, 1, 2, 1, D, 1, 1, 0.1, dq, dk, dv, AT, have, None)
+def bwd(lse=AT, dq=H(), dk=H(), dv=H(), dout=H(), D=64, have=1 << 24, q=H()):
+    return oapl.lib().oapl_attention_bwd(q, H(), H(), H(), lse, dout, AT, AT, 4, 4, 1, 2, 1, D, 1, 1, 0.1, dq, dk, dv, AT, have, None)
 
 
 @pytest.mark.parametrize("kw, want", [
@@ -69,7 +69,7 @@ def test_attention_refuses(kw, want):
 
 @pytest.mark.parametrize("kw, want", [
     ({"lse": None}, NULL), ({"dq": None}, NULL), ({"dk": None}, NULL), ({"dv": H(None)}, NULL), ({"dout": H(AT + 4)}, ALIGN),
-    ({"dv": H(AT, 0)}, SHAPE), ({"D": 4}, SHAPE), ({"have": 256}, WORKSPACE),
+    ({"dv": H(AT, 0)}, SHAPE), ({"D": 4}, SHAPE), ({"have": 256}, WORKSPACE), ({"q": H(AT, 128, 1 << 30)}, SHAPE),
 ])
 def test_attention_gradients_refuse(kw, want):
     assert bwd(**kw) == want
