@@ -59,6 +59,12 @@ __device__ __forceinline__ bool sequences_ok(const AttnArgs& p) {
   return __ballot(bad) == 0;
 }
 
+// A number that all lanes hold alike, for the scalar unit.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return (int64_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
+}
+
 // Whose tile `id` is, by a search over the first ids of the sequences, 64 at a time; `off` and `per` say what tiles are cut from
 // (rows: query offsets times heads in a group; keys: key offsets).  Only after sequences_ok.
 template <int B>
@@ -72,13 +78,15 @@ __device__ __forceinline__ SeqTile find_tile(const AttnArgs& p, const int64_t* _
     lo += k * step;
     n = n - k * step < step ? n - k * step : step;
   }
+  lo = uniform(lo);
+  const int64_t q0 = uniform(p.q_offsets[lo]), k0 = uniform(p.k_offsets[lo]), from = uniform(off[lo]);
   SeqTile t;
-  t.q0 = p.q_offsets[lo];
-  t.k0 = p.k_offsets[lo];
-  t.nq = (int)(p.q_offsets[lo + 1] - t.q0);
-  t.nk = (int)(p.k_used ? p.k_used[lo] : p.k_offsets[lo + 1] - t.k0);
-  const int64_t first = (id - (off[lo] * per / B + lo)) * B, rows = (off[lo + 1] - off[lo]) * per;
-  t.first = (int)(first < rows ? first : rows);
+  t.q0 = q0;
+  t.k0 = k0;
+  t.nq = uniform((int)(p.q_offsets[lo + 1] - q0));
+  t.nk = uniform((int)(p.k_used ? p.k_used[lo] : p.k_offsets[lo + 1] - k0));
+  const int64_t first = (id - (from * per / B + lo)) * B, rows = (uniform(off[lo + 1]) - from) * per;
+  t.first = uniform((int)(first < rows ? first : rows));
   return t;
 }
 
@@ -102,21 +110,53 @@ template <class T> struct FragOf;
 template <> struct FragOf<bf16_t> { typedef bf16x8 type; };
 template <> struct FragOf<float> { typedef FragF32 type; };
 
-__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ f32x4 mma(const FragF32& a, const FragF32& b, f32x4 c) {
+// Inline assembly, so that an accumulator stays where it is: given the builtin the compiler moves results about in the middle of a
+// sum.  What it then does not keep are the wait states around an MFMA: results are looked at behind settle(), and operands that
+// vector instructions made go through ready().
+__device__ __forceinline__ void mma(f32x4& c, bf16x8 a, bf16x8 b) { asm("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b)); }
+__device__ __forceinline__ void mma(f32x4& c, const FragF32& a, const FragF32& b) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[j >> 2][j & 3], b.x[j >> 2][j & 3], c, 0, 0, 0);
-  return c;
+  for (int j = 0; j < 8; ++j) asm("v_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+v"(c) : "v"(a.x[j >> 2][j & 3]), "v"(b.x[j >> 2][j & 3]));
 }
+// ... the first of a sum.
+__device__ __forceinline__ void mma0(f32x4& c, bf16x8 a, bf16x8 b) { asm("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=&v"(c) : "v"(a), "v"(b)); }
+__device__ __forceinline__ void mma0(f32x4& c, const FragF32& a, const FragF32& b) {
+  asm("v_mfma_f32_16x16x4_f32 %0, %1, %2, 0" : "=&v"(c) : "v"(a.x[0][0]), "v"(b.x[0][0]));
+#pragma unroll
+  for (int j = 1; j < 8; ++j) asm("v_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+v"(c) : "v"(a.x[j >> 2][j & 3]), "v"(b.x[j >> 2][j & 3]));
+}
+// The wait states of the slower of the two shapes: one statement that all results go into and come out of.
+template <int N>
+__device__ __forceinline__ void settle(f32x4 (&x)[2][N]) {
+  static_assert(N == 2 || N == 4 || N == 8, "operands are listed");
+  __builtin_amdgcn_sched_barrier(0);
+  if constexpr (N == 2)
+    asm volatile("s_nop 7\n\ts_nop 7" : "+v"(x[0][0]), "+v"(x[0][1]), "+v"(x[1][0]), "+v"(x[1][1]));
+  else if constexpr (N == 4)
+    asm volatile("s_nop 7\n\ts_nop 7" : "+v"(x[0][0]), "+v"(x[0][1]), "+v"(x[0][2]), "+v"(x[0][3]), "+v"(x[1][0]), "+v"(x[1][1]),
+                 "+v"(x[1][2]), "+v"(x[1][3]));
+  else
+    asm volatile("s_nop 7\n\ts_nop 7" : "+v"(x[0][0]), "+v"(x[0][1]), "+v"(x[0][2]), "+v"(x[0][3]), "+v"(x[0][4]), "+v"(x[0][5]),
+                 "+v"(x[0][6]), "+v"(x[0][7]), "+v"(x[1][0]), "+v"(x[1][1]), "+v"(x[1][2]), "+v"(x[1][3]), "+v"(x[1][4]),
+                 "+v"(x[1][5]), "+v"(x[1][6]), "+v"(x[1][7]));
+}
+__device__ __forceinline__ void settle(f32x4 (&x)[2], f32x4 (&y)[2]) {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 7\n\ts_nop 7" : "+v"(x[0]), "+v"(x[1]), "+v"(y[0]), "+v"(y[1]));
+}
+__device__ __forceinline__ void ready(bf16x8 (&f)[2]) { asm volatile("s_nop 1" : "+v"(f[0]), "+v"(f[1])); }
+__device__ __forceinline__ void ready(FragF32 (&f)[2]) {
+  asm volatile("s_nop 1" : "+v"(f[0].x[0]), "+v"(f[0].x[1]), "+v"(f[1].x[0]), "+v"(f[1].x[1]));
+}
+__device__ __forceinline__ void zero(f32x4& c) {
+  c = f32x4{0.f, 0.f, 0.f, 0.f};
+  asm volatile("" : "+v"(c));     // here, and not in front of the multiplication that adds to it
+}
+
 __device__ __forceinline__ void pack(f32x4 a, f32x4 b, bf16x8& f) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) f[j] = (bf16_t)a[j], f[j + 4] = (bf16_t)b[j];
 }
-__device__ __forceinline__ void pack_half(f32x4 a, int half, bf16x8& f) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) f[half * 4 + j] = (bf16_t)a[j];
-}
-__device__ __forceinline__ void pack_half(f32x4 a, int half, FragF32& f) { f.x[half] = a; }
 __device__ __forceinline__ void pack(f32x4 a, f32x4 b, FragF32& f) { f.x[0] = a, f.x[1] = b; }
 
 // A row's channels of one k-step from memory (nullptr: zeros).
@@ -153,7 +193,7 @@ template <class T, int DP>
 struct Tile {
   static constexpr int kPitch = DP * (int)sizeof(T), kChunks = kPitch / 16;
   __device__ static __forceinline__ int swizzle(int r) {
-    return kChunks >= 16 ? (r & 3) << 2 | (r >> 2 & 1) << 1 | (r >> 3 & 1) : (r >> 1 & 1) << 2 | (r >> 2 & 1) << 1 | (r >> 3 & 1);
+    return (kChunks >= 16 ? (r & 3) << 2 : (r >> 1 & 1) << 2) | (-(r >> 2) & 3);
   }
   __device__ static __forceinline__ int at(int r, int c) { return r * kPitch + ((c ^ swizzle(r)) << 4); }
 
@@ -221,13 +261,13 @@ struct Stager {
   const char* base;
   int64_t stride;
   int row, wave;
-  uint32_t column;
+  uint32_t column, columns;
   __device__ __forceinline__ Stager(const char* p, int64_t token_stride, int D) : base(p), stride(token_stride) {
     const int lane = threadIdx.x & 63;
     wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     row = wave * kRows + lane / Lds::kChunks;
-    const int c = (lane % Lds::kChunks) ^ Lds::swizzle(row);
-    column = c * 16 < D * (int)sizeof(T) ? c * 16 : kOutside;
+    column = ((lane % Lds::kChunks) ^ Lds::swizzle(row)) * 16;
+    columns = D * sizeof(T);
   }
   // Starts the loads of rows [first, first + R), of which those from `n` on (counted from the base) do not exist.
   __device__ __forceinline__ void start(lds_char_ptr lds, int first, int n) const {
@@ -237,8 +277,8 @@ struct Stager {
     for (int j = 0; j < kLoads; ++j) {
       const int at = row + j * 4 * kRows;
       // rows 16 apart are swizzled alike; a wavefront of two rows comes back to them with every other load
-      const uint32_t flip = 4 * kRows % 16 ? (uint32_t)(j & 1) << 4 : 0;
-      const uint32_t v = first + at < n ? (uint32_t)(at * (int)stride) + (column ^ flip) : kOutside;
+      const uint32_t flip = 4 * kRows % 16 ? (uint32_t)(j & 1) << 5 : 0;
+      const uint32_t v = first + at < n && (column ^ flip) < columns ? (uint32_t)(at * (int)stride) + (column ^ flip) : kOutside;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_ptr)(lds + (j * 4 + wave) * 1024), 16, v, 0, 0, 0);
     }
   }
@@ -308,18 +348,45 @@ __device__ __forceinline__ float over_row(float v, F f) {
 __device__ __forceinline__ float row_max(float v) { return over_row(v, [](float a, float b) { return fmaxf(a, b); }); }
 __device__ __forceinline__ float row_sum(float v) { return over_row(v, [](float a, float b) { return a + b; }); }
 
-// The order in which a group of products wants its operands out of LDS: a few fetches ahead, then one for every `N`
-// multiplications.  Left alone the compiler fetches two and waits for them.
-template <int FETCHES, int N>
-__device__ __forceinline__ void feed_products() {
-  constexpr int AHEAD = 4;
-  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+// Scores of two blocks of 16 rows of a tile in LDS (keys, or rows) with the wavefront's 32 rows (keys): s[n][b] is block r0 + 16 b
+// by the wavefront's block n.  Operands are fetched three ahead of their multiplications, and after each pair of these comes
+// between(i), i = 0 .. 2 KS - 1: other work for the vector unit while the matrix unit is busy.  The compiler left alone fetches two operands
+// and waits for them, and puts the other work behind.
+template <class Lds, int KS, int AHEAD = 3, class Frag, class F>
+__device__ __forceinline__ void scores(f32x4 (&s)[2][2], lds_char_ptr lds, int place, int r0, const Frag (&x)[2][KS], F&& between) {
+  constexpr int N = 2 * KS;
+  Frag f[N];
 #pragma unroll
-  for (int i = 0; i < FETCHES - AHEAD; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x8, N, 0);
-    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+  for (int i = 0; i < AHEAD; ++i) Lds::rows(lds, place, r0 + (i & 1) * 16, i >> 1, f[i]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_barrier(0);
+    if (i + AHEAD < N) Lds::rows(lds, place, r0 + ((i + AHEAD) & 1) * 16, (i + AHEAD) >> 1, f[i + AHEAD]);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      if (i < 2) mma0(s[n][i & 1], f[i], x[n][i >> 1]);
+      else mma(s[n][i & 1], f[i], x[n][i >> 1]);
+    }
+    between(i);
   }
-  __builtin_amdgcn_sched_group_barrier(0x8, AHEAD * N, 0);
+  settle(s);
+}
+
+// acc[n][d] += columns 16 d of 32 rows of a tile, contracted over those rows with w[n].
+template <class Lds, int DB, int AHEAD = 3, class Frag, class F>
+__device__ __forceinline__ void add_columns(f32x4 (&acc)[2][DB], lds_char_ptr lds, int place, int r0, const Frag (&w)[2], F&& between) {
+  Frag f[DB];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) Lds::columns(lds, place, r0, i, f[i]);
+#pragma unroll
+  for (int i = 0; i < DB; ++i) {
+    __builtin_amdgcn_sched_barrier(0);
+    if (i + AHEAD < DB) Lds::columns(lds, place, r0, i + AHEAD, f[i + AHEAD]);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) mma(acc[n][i], f[i], w[n]);
+    between(i);
+  }
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 // A workgroup: 128 rows, 32 a wavefront, over all keys that they see, 64 at a time.
@@ -328,7 +395,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs p) {
   typedef typename FragOf<T>::type Frag;
   typedef Tile<T, DP> Lds;
   typedef Stager<T, DP, kKeys> Stage;
-  constexpr int B = 128, KS = DP / 32, DB = DP / 16, KB = kKeys / 16, SIZE = kKeys * Lds::kPitch;
+  constexpr int B = 128, KS = DP / 32, DB = DP / 16, SIZE = kKeys * Lds::kPitch;
   extern __shared__ char smem[];
   const lds_char_ptr lds = (lds_char_ptr)smem;     // two slots of keys and values
   const int rp = Lds::rows_place(), cp = Lds::columns_place();
@@ -350,7 +417,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs p) {
   const float scale2 = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;
   int row_sees[2];
   Frag q[2][KS];
-  f32x4 o[2][DB] = {};
+  f32x4 o[2][DB];
   float m[2], l[2];                                // m: the running maximum before scaling; l: this lane's keys
   int all_see = t.nk;                              // keys that every row of this wavefront sees
 #pragma unroll
@@ -362,6 +429,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs p) {
       load_frag(x, kk * 32 + group * 8, p.D, q[n][kk]);
       if (flip) negate(q[n][kk]);
     }
+#pragma unroll
+    for (int d = 0; d < DB; ++d) zero(o[n][d]);
     row_sees[n] = row.sees;
     all_see = row.sees < all_see ? row.sees : all_see;
     m[n] = kNegHuge;
@@ -381,68 +450,71 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs p) {
       vs.start(lds + (slot ^ 2 * SIZE) + SIZE, j0 + kKeys, t.nk);
     }
     const lds_char_ptr kt = lds + slot, vt = kt + SIZE;
-    f32x4 s[2][KB] = {};
-#pragma unroll
-    for (int kk = 0; kk < KS; ++kk)
-#pragma unroll
-      for (int b = 0; b < KB; ++b) {
-        Frag f;
-        Lds::rows(kt, rp, b * 16, kk, f);
-#pragma unroll
-        for (int n = 0; n < 2; ++n) s[n][b] = mma(f, q[n][kk], s[n][b]);
-      }
-    feed_products<KS * KB, 2>();
-    if (j0 + kKeys > all_see) {
+    // Two halves of 32 keys, a step apart: the exponentials of the first run beside the scores of the second, those of the second
+    // beside the first one's product with the values.
+    f32x4 a[2][2], b[2][2];
+    Frag wa[2], wb[2];
+    const auto mask = [&](f32x4 (&s)[2][2], int first) {
+      if (first + 32 <= all_see) return;
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (j0 + b * 16 + group * 4 + i >= row_sees[n]) s[n][b][i] = -__builtin_inff();
-    }
-    float top[2];
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      top[n] = m[n];
-#pragma unroll
-      for (int b = 0; b < KB; ++b) top[n] = max3(max3(top[n], s[n][b][0], s[n][b][1]), s[n][b][2], s[n][b][3]);
-      top[n] = row_max(top[n]);
-    }
-    if (__any(fmaxf(top[0] - m[0], top[1] - m[1]) * scale2 > 8.f)) {
+        for (int x = 0; x < 8; ++x)
+          if (first + (x >> 2) * 16 + group * 4 + (x & 3) >= row_sees[n]) s[n][x >> 2][x & 3] = -__builtin_inff();
+    };
+    // The maximum that the exponentials are taken from follows only when it falls behind by 2^8: until then they stay below 2^8, and
+    // what is rounded is rounded as well as below 1.
+    const auto follow = [&](const f32x4 (&s)[2][2], bool second) {
+      float top[2];
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
-        const float old = __builtin_amdgcn_exp2f((m[n] - top[n]) * scale2);
-        m[n] = top[n];
-        l[n] *= old;
+        top[n] = m[n];
 #pragma unroll
-        for (int d = 0; d < DB; ++d) o[n][d] *= old;
+        for (int x = 0; x < 8; x += 2) top[n] = max3(top[n], s[n][x >> 2][x & 3], s[n][x >> 2][(x & 3) + 1]);
+        top[n] = row_max(top[n]);
       }
-    }
+      if (__any(fmaxf(top[0] - m[0], top[1] - m[1]) * scale2 > 8.f)) {
+        settle(o);
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      const float m2 = m[n] * scale2;
+        for (int n = 0; n < 2; ++n) {
+          const float old = __builtin_amdgcn_exp2f((m[n] - top[n]) * scale2);
+          m[n] = top[n];
+          l[n] *= old;
 #pragma unroll
-      for (int b = 0; b < KB; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s[n][b][i] = __builtin_amdgcn_exp2f(fmaf(s[n][b][i], scale2, -m2));
-          l[n] += s[n][b][i];
+          for (int d = 0; d < DB; ++d) o[n][d] *= old;
+          if (second) a[n][0] *= old, a[n][1] *= old;
         }
-    }
-#pragma unroll
-    for (int c = 0; c < KB / 2; ++c) {
-      Frag f, w[2];
-#pragma unroll
-      for (int n = 0; n < 2; ++n) pack(s[n][c * 2], s[n][c * 2 + 1], w[n]);
-#pragma unroll
-      for (int d = 0; d < DB; ++d) {
-        Lds::columns(vt, cp, c * 32, d, f);
-#pragma unroll
-        for (int n = 0; n < 2; ++n) o[n][d] = mma(f, w[n], o[n][d]);
       }
-    }
+    };
+    const auto exponential = [&](f32x4 (&s)[2][2], int i) {
+      const int n = i >> 3, x = i & 7;
+      const float e = __builtin_amdgcn_exp2f(fmaf(s[n][x >> 2][x & 3], scale2, -m[n] * scale2));
+      l[n] += e;
+      s[n][x >> 2][x & 3] = e;
+    };
+    constexpr int PER_S = 16 / (2 * KS), PER_C = 16 / DB;
+    scores<Lds, KS>(a, kt, rp, 0, q, [](int) {});
+    mask(a, j0);
+    follow(a, false);
+    scores<Lds, KS>(b, kt, rp, 32, q, [&](int i) {
+#pragma unroll
+      for (int x = 0; x < PER_S; ++x) exponential(a, i * PER_S + x);
+    });
+    mask(b, j0 + 32);
+    follow(b, true);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) pack(a[n][0], a[n][1], wa[n]);
+    ready(wa);
+    add_columns<Lds, DB>(o, vt, cp, 0, wa, [&](int i) {
+#pragma unroll
+      for (int x = 0; x < PER_C; ++x) exponential(b, i * PER_C + x);
+    });
+#pragma unroll
+    for (int n = 0; n < 2; ++n) pack(b[n][0], b[n][1], wb[n]);
+    ready(wb);
+    add_columns<Lds, DB>(o, vt, cp, 32, wb, [](int) {});
   }
+  settle(o);
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     const Row row(p, t, row0 + n * 16);
@@ -481,13 +553,15 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
   int row_sees[2];
   Frag q[2][KS], dout[2][KS];
   float lse2[2], delta[2];
-  f32x4 dq[2][DB] = {};
+  f32x4 dq[2][DB];
   int all_see = t.nk;
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     const Row row(p, t, row0 + n * 16);
     const int64_t token = t.q0 + row.token;
     const int head = kh * p.g + row.head;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) zero(dq[n][d]);
     delta[n] = 0.f;
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) {
@@ -521,49 +595,44 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
       vs.start(lds + (slot ^ 2 * SIZE) + SIZE, j0 + kKeys, t.nk);
     }
     const lds_char_ptr kt = lds + slot, vt = kt + SIZE;
-#pragma unroll
-    for (int c = 0; c < kKeys / 32; ++c) {
-      f32x4 s[2][2] = {}, dp[2][2] = {};
-#pragma unroll
-      for (int kk = 0; kk < KS; ++kk)
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          Frag f, g;
-          Lds::rows(kt, rp, c * 32 + b * 16, kk, f);
-          Lds::rows(vt, rp, c * 32 + b * 16, kk, g);
-#pragma unroll
-          for (int n = 0; n < 2; ++n) s[n][b] = mma(f, q[n][kk], s[n][b]);
-#pragma unroll
-          for (int n = 0; n < 2; ++n) dp[n][b] = mma(g, dout[n][kk], dp[n][b]);
-        }
-      feed_products<KS * 4, 2>();
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            s[n][b][i] = __builtin_amdgcn_exp2f(fmaf(s[n][b][i], scale2, -lse2[n])) * (dp[n][b][i] - delta[n]);
+    f32x4 s[2][2][2], dp[2][2][2];     // [half][rows][keys]
+    Frag w[2][2];
+    const auto finish = [&](int c, int i) {
+      const int n = i >> 3, x = i & 7;
+      s[c][n][x >> 2][x & 3] = __builtin_amdgcn_exp2f(fmaf(s[c][n][x >> 2][x & 3], scale2, -lse2[n])) * (dp[c][n][x >> 2][x & 3] - delta[n]);
+    };
+    const auto mask = [&](int c) {
       if (j0 + c * 32 + 32 > all_see) {
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
-          for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (j0 + c * 32 + b * 16 + group * 4 + i >= row_sees[n]) s[n][b][i] = 0.f;
+          for (int x = 0; x < 8; ++x)
+            if (j0 + c * 32 + (x >> 2) * 16 + group * 4 + (x & 3) >= row_sees[n]) s[c][n][x >> 2][x & 3] = 0.f;
       }
-      Frag f, w[2];
 #pragma unroll
-      for (int n = 0; n < 2; ++n) pack(s[n][0], s[n][1], w[n]);
+      for (int n = 0; n < 2; ++n) pack(s[c][n][0], s[c][n][1], w[c][n]);
+      ready(w[c]);
+    };
+    constexpr int PER_S = 8 / KS / 2, PER_C = 16 / DB;
+    scores<Lds, KS>(s[0], kt, rp, 0, q, [](int) {});
+    scores<Lds, KS>(dp[0], vt, rp, 0, dout, [](int) {});
+    scores<Lds, KS>(s[1], kt, rp, 32, q, [&](int i) {
 #pragma unroll
-      for (int d = 0; d < DB; ++d) {
-        Lds::columns(kt, cp, c * 32, d, f);
+      for (int x = 0; x < PER_S; ++x) finish(0, i * PER_S + x);
+    });
+    scores<Lds, KS>(dp[1], vt, rp, 32, dout, [&](int i) {
 #pragma unroll
-        for (int n = 0; n < 2; ++n) dq[n][d] = mma(f, w[n], dq[n][d]);
-      }
-    }
+      for (int x = 0; x < PER_S; ++x) finish(0, 8 + i * PER_S + x);
+    });
+    mask(0);
+    add_columns<Lds, DB>(dq, kt, cp, 0, w[0], [&](int i) {
+#pragma unroll
+      for (int x = 0; x < PER_C; ++x) finish(1, i * PER_C + x);
+    });
+    mask(1);
+    add_columns<Lds, DB>(dq, kt, cp, 32, w[1], [](int) {});
   }
+  settle(dq);
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     const Row row(p, t, row0 + n * 16);
@@ -634,21 +703,23 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   // the first row that sees the tile's first key, and whole tiles of rows
   const int from = p.causal && t.first > ahead ? (t.first - ahead) * p.g / kRows * kRows : 0;
   if (from < rows) Stage::start(p, t, kh, lds, from);
-  const int group = threadIdx.x >> 4 & 3, key0 = t.first + (threadIdx.x >> 6) * 32 + (threadIdx.x & 15);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Frag k[2][KS], v[2][KS];
-  f32x4 dk[2][DB] = {}, dv[2][DB] = {};
-  int first_row[2], all_from = 0;     // rows from here on see the key; from all_from on every key of the wavefront
+  f32x4 dk[2][DB], dv[2][DB];
+  const auto first_row = [&](int key) { return p.causal && key < t.nk && key > ahead ? (key - ahead) * p.g : 0; };   // that sees it
+  int all_from = 0;     // rows from here on see every key of the wavefront
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
-    const int key = key0 + n * 16;
+    const int key = t.first + wave * 32 + n * 16 + (threadIdx.x & 15), group = threadIdx.x >> 4 & 3;
     const bool exists = key < t.nk;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) zero(dk[n][d]), zero(dv[n][d]);
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) {
       load_frag(exists ? p.k.row(t.k0 + key, kh) : nullptr, kk * 32 + group * 8, p.D, k[n][kk]);
       load_frag(exists ? p.v.row(t.k0 + key, kh) : nullptr, kk * 32 + group * 8, p.D, v[n][kk]);
     }
-    first_row[n] = p.causal && exists && key > ahead ? (key - ahead) * p.g : 0;
-    all_from = first_row[n] > all_from ? first_row[n] : all_from;
+    all_from = first_row(key) > all_from ? first_row(key) : all_from;
   }
 #pragma unroll
   for (int x = 8; x > 0; x >>= 1) {
@@ -665,56 +736,44 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
 #pragma unroll 1
     for (int c = 0; c < kRows / 32; ++c) {
       typedef __attribute__((address_space(3))) f32x4* ptr;
-      Frag f, w[2], wd[2];      // probabilities and dS of 32 rows, keys in columns
+      Frag w[2], wd[2];      // probabilities and dS of 32 rows, keys in columns
+      f32x4 s[2][2], dp[2][2];     // [keys][rows]
+      scores<Lds, KS>(s, qt, rp, c * 32, k, [](int) {});
+      scores<Lds, KS>(dp, dt, rp, c * 32, v, [](int) {});
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        f32x4 s[2] = {}, dp[2] = {};
-#pragma unroll
-        for (int kk = 0; kk < KS; ++kk) {
-          Frag g;
-          Lds::rows(qt, rp, c * 32 + b * 16, kk, f);
-          Lds::rows(dt, rp, c * 32 + b * 16, kk, g);
-#pragma unroll
-          for (int n = 0; n < 2; ++n) s[n] = mma(f, k[n][kk], s[n]);
-#pragma unroll
-          for (int n = 0; n < 2; ++n) dp[n] = mma(g, v[n][kk], dp[n]);
-        }
-        const f32x4 lse2 = *(ptr)(numbers + (c * 32 + b * 16 + group * 4) * 4);
-        const f32x4 delta = *(ptr)(numbers + kRows * 4 + (c * 32 + b * 16 + group * 4) * 4);
+        const lds_char_ptr at = numbers + (fresh(threadIdx.x) >> 4 & 3) * 16 + (c * 32 + b * 16) * 4;
+        const f32x4 lse2 = *(ptr)at, delta = *(ptr)(at + kRows * 4);
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], scale2, -lse2[i]));
-            dp[n][i] = s[n][i] * (dp[n][i] - delta[i]);
+            s[n][b][i] = __builtin_amdgcn_exp2f(fmaf(s[n][b][i], scale2, -lse2[i]));
+            dp[n][b][i] = s[n][b][i] * (dp[n][b][i] - delta[i]);
           }
-        if (r0 + c * 32 < all_from) {
+      }
+      if (r0 + c * 32 < all_from) {
+        const int lane = fresh(threadIdx.x) & 63, key0 = t.first + wave * 32 + (lane & 15);
 #pragma unroll
-          for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (r0 + c * 32 + b * 16 + group * 4 + i < first_row[n]) s[n][i] = dp[n][i] = 0.f;
-        }
-#pragma unroll
-        for (int n = 0; n < 2; ++n) pack_half(s[n], b, w[n]), pack_half(dp[n], b, wd[n]);
+          for (int x = 0; x < 8; ++x)
+            if (r0 + c * 32 + (x >> 2) * 16 + (lane >> 4) * 4 + (x & 3) < first_row(key0 + n * 16))
+              s[n][x >> 2][x & 3] = dp[n][x >> 2][x & 3] = 0.f;
       }
 #pragma unroll
-      for (int d = 0; d < DB; ++d) {
-        Lds::columns(dt, cp, c * 32, d, f);
-#pragma unroll
-        for (int n = 0; n < 2; ++n) dv[n][d] = mma(f, w[n], dv[n][d]);
-      }
-#pragma unroll
-      for (int d = 0; d < DB; ++d) {
-        Lds::columns(qt, cp, c * 32, d, f);
-#pragma unroll
-        for (int n = 0; n < 2; ++n) dk[n][d] = mma(f, wd[n], dk[n][d]);
-      }
+      for (int n = 0; n < 2; ++n) pack(s[n][0], s[n][1], w[n]), pack(dp[n][0], dp[n][1], wd[n]);
+      ready(w);
+      ready(wd);
+      add_columns<Lds, DB>(dv, dt, cp, c * 32, w, [](int) {});
+      add_columns<Lds, DB>(dk, qt, cp, c * 32, wd, [](int) {});
     }
   }
+  settle(dk);
+  settle(dv);
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
-    const int key = key0 + n * 16;
+    const int key = t.first + wave * 32 + n * 16 + (threadIdx.x & 15);
     if (key >= t.nk) continue;
     store_columns<T>(p.dk.row(t.k0 + key, kh), dk[n], p.scale, p.D);
     store_columns<T>(p.dv.row(t.k0 + key, kh), dv[n], 1.f, p.D);
