@@ -25,7 +25,7 @@ constexpr float kLn2f = 0.69314718055994531f;
 struct AttnArgs {
   Heads q, k, v, o, dout, dq, dk, dv;   // o: written forward, read backward
   float* lse;                           // [Tq][hq]; read backward; nullptr: not wanted (forward)
-  float *lse2, *delta;                  // [Tq][hq] log-sum-exp in base 2 and D_i, between the two backward kernels
+  float *lse2, *delta;                  // [hk][Tq][g] log-sum-exp in base 2 and D_i, between the two backward kernels
   const int64_t *q_offsets, *k_offsets, *k_used;
   int* status;
   int64_t Tq, Tk;
@@ -187,6 +187,10 @@ __device__ __forceinline__ int fresh(int x) {
   return x;
 }
 
+// LDS addresses as numbers.
+__device__ __forceinline__ int lds_place(lds_char_ptr p) { return (int)(uintptr_t)p; }
+__device__ __forceinline__ lds_char_ptr lds_at(int place) { return (lds_char_ptr)(uintptr_t)(uint32_t)place; }
+
 // A tile of R rows of DP channels in LDS.  16-byte chunk c of row r lies at chunk c ^ swizzle(r): fetches of one chunk of many
 // rows, and transposing fetches of four rows of one column range, both touch every bank once.
 template <class T, int DP>
@@ -209,44 +213,53 @@ struct Tile {
     }
   }
 
-  // Operands come out of a tile at `lds` (a multiple of 256 bytes) from places that differ in a few bits of the chunk: a lane keeps
-  // one place for each kind, and the step's bits are put in where the operand is fetched (kept apart they would be a dozen registers).
+  // Operands come out of a tile (at a multiple of 256 bytes) from places that differ in a few bits of the chunk: a lane has one place
+  // for each kind, and the step's bits are put in where the operand is fetched: once for all fetches of a step or, with KEEP =
+  // false, each time anew, where a dozen places do not fit the registers.
 
-  // Rows r0 + lane % 16, contracted over the 32 channels of step kk.
-  __device__ static __forceinline__ int rows_place() {
+  // Fetches below take a place with the step's bits in it, and what is constant of an address beside it.
+  template <bool KEEP = true>
+  __device__ static __forceinline__ int flip(int place, int bits) {
+    if (KEEP) return place ^ bits;
+    int at;
+    asm volatile("v_xor_b32 %0, %1, %2" : "=v"(at) : "i"(bits), "v"(place));
+    return at;
+  }
+  static constexpr int kRowBits = 16 * 2 * (int)sizeof(T), kColumnBits = 16 * (int)sizeof(T);   // of a step of 32 (16) channels
+
+  // Rows lane % 16 of the 16 rows `off` bytes into the tile, contracted over 32 channels.
+  __device__ static __forceinline__ int rows_place(lds_char_ptr lds) {
     const int lane = threadIdx.x & 63;
-    return (lane & 15) * kPitch + (((lane >> 4) * ((int)sizeof(T) / 2) ^ swizzle(lane & 15)) << 4);
+    return lds_place(lds) + (lane & 15) * kPitch + (((lane >> 4) * ((int)sizeof(T) / 2) ^ swizzle(lane & 15)) << 4);
   }
-  __device__ static __forceinline__ void rows(lds_char_ptr lds, int place, int r0, int kk, bf16x8& f) {
-    f = *(__attribute__((address_space(3))) bf16x8*)(lds + (fresh(place) ^ kk << 6) + r0 * kPitch);
+  __device__ static __forceinline__ void rows(int place, int off, bf16x8& f) {
+    f = *(__attribute__((address_space(3))) bf16x8*)(lds_at(place) + off);
   }
-  __device__ static __forceinline__ void rows(lds_char_ptr lds, int place, int r0, int kk, FragF32& f) {
+  __device__ static __forceinline__ void rows(int place, int off, FragF32& f) {
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
-      f.x[x] = *(__attribute__((address_space(3))) f32x4*)(lds + (place ^ (kk * 8 + x) << 4) + r0 * kPitch);
+    for (int x = 0; x < 2; ++x) f.x[x] = *(__attribute__((address_space(3))) f32x4*)(lds_at(place ^ x << 4) + off);
   }
 
-  // Channels 16 d + lane % 16, contracted over rows r0 .. r0 + 31 in the order in which the results of two blocks of 16 rows hold
-  // them.  bf16: of the 16 lanes of a group, lane 4e + a points at four channels of row e, and lane i receives channel i of four
+  // Channels lane % 16 of 16, contracted over 32 rows in the order in which the results of two blocks of 16 rows hold them.  bf16: of the 16 lanes of a group, lane 4e + a points at four channels of row e, and lane i receives channel i of four
   // rows.
-  __device__ static __forceinline__ int columns_place() {
+  __device__ static __forceinline__ int columns_place(lds_char_ptr lds) {
     const int lane = threadIdx.x & 63;
     if (sizeof(T) == 2) {
       const int r = (lane >> 4) * 4 + (lane >> 2 & 3);
-      return r * kPitch + (((lane >> 1 & 1) ^ swizzle(r)) << 4) + ((lane & 1) << 3);
+      return lds_place(lds) + r * kPitch + (((lane >> 1 & 1) ^ swizzle(r)) << 4) + ((lane & 1) << 3);
     }
-    return (lane >> 4) * 4 * kPitch + (((lane >> 2 & 3) ^ swizzle((lane >> 4) * 4)) << 4) + ((lane & 3) << 2);
+    return lds_place(lds) + (lane >> 4) * 4 * kPitch + (((lane >> 2 & 3) ^ swizzle((lane >> 4) * 4)) << 4) + ((lane & 3) << 2);
   }
-  __device__ static __forceinline__ void columns(lds_char_ptr lds, int place, int r0, int d, bf16x8& f) {
-    const lds_char_ptr at = lds + (fresh(place) ^ d << 5) + r0 * kPitch;
+  __device__ static __forceinline__ void columns(int place, int off, bf16x8& f) {
+    const lds_char_ptr at = lds_at(place) + off;
     const bf16x4 x = lds_read_transposed(at), y = lds_read_transposed(at + 16 * kPitch);
     f = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
   }
-  __device__ static __forceinline__ void columns(lds_char_ptr lds, int place, int r0, int d, FragF32& f) {
+  __device__ static __forceinline__ void columns(int place, int off, FragF32& f) {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      f.x[j >> 2][j & 3] = *(__attribute__((address_space(3))) float*)(lds + (place ^ (d ^ (j & 3)) << 6) +
-                                                                        (r0 + (j & 3) + (j >> 2) * 16) * kPitch);
+      f.x[j >> 2][j & 3] = *(__attribute__((address_space(3))) float*)(lds_at(place ^ (j & 3) << 6) + off +
+                                                                        ((j & 3) + (j >> 2) * 16) * kPitch);
   }
 };
 
@@ -261,24 +274,32 @@ struct Stager {
   const char* base;
   int64_t stride;
   int row, wave;
-  uint32_t column, columns;
+  uint32_t column, columns, whole;
   __device__ __forceinline__ Stager(const char* p, int64_t token_stride, int D) : base(p), stride(token_stride) {
     const int lane = threadIdx.x & 63;
-    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    wave = uniform((int)threadIdx.x >> 6);
     row = wave * kRows + lane / Lds::kChunks;
     column = ((lane % Lds::kChunks) ^ Lds::swizzle(row)) * 16;
     columns = D * sizeof(T);
+    whole = column < columns ? (uint32_t)(row * (int)stride) + column : kOutside;
   }
   // Starts the loads of rows [first, first + R), of which those from `n` on (counted from the base) do not exist.
   __device__ __forceinline__ void start(lds_char_ptr lds, int first, int n) const {
     const __amdgpu_buffer_rsrc_t r =
         __builtin_amdgcn_make_buffer_rsrc((void*)(base + first * stride), 0, kOutside, 0x00020000);
+    // rows 16 apart are swizzled alike; a wavefront of two rows comes back to them with every other load
+    constexpr bool kAlike = 4 * kRows % 16 == 0;
+    if (kAlike && first + R <= n) {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_ptr)(lds + (j * 4 + wave) * 1024), 16, whole, j * 4 * kRows * (int)stride, 0, 0);
+      return;
+    }
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
       const int at = row + j * 4 * kRows;
-      // rows 16 apart are swizzled alike; a wavefront of two rows comes back to them with every other load
-      const uint32_t flip = 4 * kRows % 16 ? (uint32_t)(j & 1) << 5 : 0;
-      const uint32_t v = first + at < n && (column ^ flip) < columns ? (uint32_t)(at * (int)stride) + (column ^ flip) : kOutside;
+      const uint32_t c = column ^ (kAlike ? 0 : (uint32_t)(j & 1) << 5);
+      const uint32_t v = first + at < n && c < columns ? (uint32_t)(at * (int)stride) + c : kOutside;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_ptr)(lds + (j * 4 + wave) * 1024), 16, v, 0, 0, 0);
     }
   }
@@ -317,7 +338,11 @@ __device__ __forceinline__ int tile_sees(const AttnArgs& p, const SeqTile& t) {
 constexpr int kKeys = 64;   // keys staged at a time
 
 // ---------------------------------------------------------------------------------------------------------------- forward
-__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;      // fmaxf would first make quiet what may be a signalling NaN
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+  return d;
+}
 
 __device__ __forceinline__ void negate(bf16x8& f) {
   u32x4 x;
@@ -345,23 +370,24 @@ __device__ __forceinline__ float over_row(float v, F f) {
   const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
-__device__ __forceinline__ float row_max(float v) { return over_row(v, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float row_max(float v) { return over_row(v, [](float a, float b) { return max3(a, a, b); }); }
 __device__ __forceinline__ float row_sum(float v) { return over_row(v, [](float a, float b) { return a + b; }); }
 
-// Scores of two blocks of 16 rows of a tile in LDS (keys, or rows) with the wavefront's 32 rows (keys): s[n][b] is block r0 + 16 b
-// by the wavefront's block n.  Operands are fetched three ahead of their multiplications, and after each pair of these comes
-// between(i), i = 0 .. 2 KS - 1: other work for the vector unit while the matrix unit is busy.  The compiler left alone fetches two operands
-// and waits for them, and puts the other work behind.
-template <class Lds, int KS, int AHEAD = 3, class Frag, class F>
-__device__ __forceinline__ void scores(f32x4 (&s)[2][2], lds_char_ptr lds, int place, int r0, const Frag (&x)[2][KS], F&& between) {
-  constexpr int N = 2 * KS;
+// Scores of two blocks of 16 rows of a tile in LDS (keys, or rows) with the wavefront's 32 rows (keys): s[n][b] is the tile's block b,
+// `off` bytes into it, by the wavefront's block n.  Operands are fetched three ahead of their multiplications, and after each pair of
+// these comes between(i), i = 0 .. 2 KS - 1: other work for the vector unit while the matrix unit is busy.  The compiler left alone
+// fetches two operands and waits for them, and puts the other work behind.
+template <class Lds, int KS, class Frag, class F>
+__device__ __forceinline__ void scores(f32x4 (&s)[2][2], int place, int off, const Frag (&x)[2][KS], F&& between) {
+  constexpr int AHEAD = 3, N = 2 * KS;
   Frag f[N];
+  const auto fetch = [&](int i) { Lds::rows(Lds::flip(place, (i >> 1) * Lds::kRowBits), off + (i & 1) * 16 * Lds::kPitch, f[i]); };
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i) Lds::rows(lds, place, r0 + (i & 1) * 16, i >> 1, f[i]);
+  for (int i = 0; i < AHEAD; ++i) fetch(i);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     __builtin_amdgcn_sched_barrier(0);
-    if (i + AHEAD < N) Lds::rows(lds, place, r0 + ((i + AHEAD) & 1) * 16, (i + AHEAD) >> 1, f[i + AHEAD]);
+    if (i + AHEAD < N) fetch(i + AHEAD);
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       if (i < 2) mma0(s[n][i & 1], f[i], x[n][i >> 1]);
@@ -373,18 +399,69 @@ __device__ __forceinline__ void scores(f32x4 (&s)[2][2], lds_char_ptr lds, int p
 }
 
 // acc[n][d] += columns 16 d of 32 rows of a tile, contracted over those rows with w[n].
-template <class Lds, int DB, int AHEAD = 3, class Frag, class F>
-__device__ __forceinline__ void add_columns(f32x4 (&acc)[2][DB], lds_char_ptr lds, int place, int r0, const Frag (&w)[2], F&& between) {
+template <class Lds, int DB, class Frag, class F>
+__device__ __forceinline__ void add_columns(f32x4 (&acc)[2][DB], int place, int off, const Frag (&w)[2], F&& between) {
+  constexpr int AHEAD = 3;
   Frag f[DB];
+  const auto fetch = [&](int i) { Lds::columns(Lds::flip(place, i * Lds::kColumnBits), off, f[i]); };
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i) Lds::columns(lds, place, r0, i, f[i]);
+  for (int i = 0; i < AHEAD; ++i) fetch(i);
 #pragma unroll
   for (int i = 0; i < DB; ++i) {
     __builtin_amdgcn_sched_barrier(0);
-    if (i + AHEAD < DB) Lds::columns(lds, place, r0, i + AHEAD, f[i + AHEAD]);
+    if (i + AHEAD < DB) fetch(i + AHEAD);
 #pragma unroll
     for (int n = 0; n < 2; ++n) mma(acc[n][i], f[i], w[n]);
     between(i);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Both for a pair of tiles SIZE bytes apart, for where registers are short: places are made anew with every fetch, for both tiles.
+template <class Lds, int KS, int SIZE, class Frag>
+__device__ __forceinline__ void scores2(f32x4 (&s)[2][2], f32x4 (&t)[2][2], int place, const Frag (&x)[2][KS], const Frag (&y)[2][KS]) {
+  constexpr int AHEAD = 3, N = 4 * KS;      // fetch i: channels i / 4, tile (i / 2) % 2, block i % 2
+  Frag f[N];
+  int at = place;
+  const auto fetch = [&](int i) {
+    if ((i & 3) == 0) at = Lds::template flip<false>(place, (i >> 2) * Lds::kRowBits);
+    Lds::rows(at, (i >> 1 & 1) * SIZE + (i & 1) * 16 * Lds::kPitch, f[i]);
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) fetch(i);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_barrier(0);
+    if (i + AHEAD < N) fetch(i + AHEAD);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      f32x4& to = (i >> 1 & 1) ? t[n][i & 1] : s[n][i & 1];
+      const Frag& by = (i >> 1 & 1) ? y[n][i >> 2] : x[n][i >> 2];
+      if (i < 4) mma0(to, f[i], by);
+      else mma(to, f[i], by);
+    }
+  }
+  settle(s);
+  settle(t);
+}
+
+template <class Lds, int DB, int SIZE, class Frag>
+__device__ __forceinline__ void add_columns2(f32x4 (&a)[2][DB], f32x4 (&b)[2][DB], int place, const Frag (&w)[2], const Frag (&x)[2]) {
+  constexpr int AHEAD = 3, N = 2 * DB;      // fetch i: channels i / 2, tile i % 2
+  Frag f[N];
+  int at = place;
+  const auto fetch = [&](int i) {
+    if ((i & 1) == 0) at = Lds::template flip<false>(place, (i >> 1) * Lds::kColumnBits);
+    Lds::columns(at, (i & 1) * SIZE, f[i]);
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) fetch(i);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_barrier(0);
+    if (i + AHEAD < N) fetch(i + AHEAD);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) mma((i & 1) ? b[n][i >> 1] : a[n][i >> 1], f[i], (i & 1) ? x[n] : w[n]);
   }
   __builtin_amdgcn_sched_barrier(0);
 }
@@ -398,7 +475,6 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs p) {
   constexpr int B = 128, KS = DP / 32, DB = DP / 16, SIZE = kKeys * Lds::kPitch;
   extern __shared__ char smem[];
   const lds_char_ptr lds = (lds_char_ptr)smem;     // two slots of keys and values
-  const int rp = Lds::rows_place(), cp = Lds::columns_place();
   const bool ok = sequences_ok(p);
   if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = ok ? 0 : kErrOffsets;
   if (!ok) {
@@ -449,7 +525,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs p) {
       ks.start(lds + (slot ^ 2 * SIZE), j0 + kKeys, t.nk);
       vs.start(lds + (slot ^ 2 * SIZE) + SIZE, j0 + kKeys, t.nk);
     }
-    const lds_char_ptr kt = lds + slot, vt = kt + SIZE;
+    const int k_rows = Lds::rows_place(lds + slot), v_columns = Lds::columns_place(lds + slot + SIZE);
     // Two halves of 32 keys, a step apart: the exponentials of the first run beside the scores of the second, those of the second
     // beside the first one's product with the values.
     f32x4 a[2][2], b[2][2];
@@ -493,10 +569,10 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs p) {
       s[n][x >> 2][x & 3] = e;
     };
     constexpr int PER_S = 16 / (2 * KS), PER_C = 16 / DB;
-    scores<Lds, KS>(a, kt, rp, 0, q, [](int) {});
+    scores<Lds, KS>(a, k_rows, 0, q, [](int) {});
     mask(a, j0);
     follow(a, false);
-    scores<Lds, KS>(b, kt, rp, 32, q, [&](int i) {
+    scores<Lds, KS>(b, k_rows, 32 * Lds::kPitch, q, [&](int i) {
 #pragma unroll
       for (int x = 0; x < PER_S; ++x) exponential(a, i * PER_S + x);
     });
@@ -505,14 +581,14 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs p) {
 #pragma unroll
     for (int n = 0; n < 2; ++n) pack(a[n][0], a[n][1], wa[n]);
     ready(wa);
-    add_columns<Lds, DB>(o, vt, cp, 0, wa, [&](int i) {
+    add_columns<Lds, DB>(o, v_columns, 0, wa, [&](int i) {
 #pragma unroll
       for (int x = 0; x < PER_C; ++x) exponential(b, i * PER_C + x);
     });
 #pragma unroll
     for (int n = 0; n < 2; ++n) pack(b[n][0], b[n][1], wb[n]);
     ready(wb);
-    add_columns<Lds, DB>(o, vt, cp, 32, wb, [](int) {});
+    add_columns<Lds, DB>(o, v_columns, 32 * Lds::kPitch, wb, [](int) {});
   }
   settle(o);
 #pragma unroll
@@ -529,6 +605,11 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs p) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------- backward
+// Where lse2 and delta of a row lie: rows of a key head one after the other.
+__device__ __forceinline__ int64_t packed_row(const AttnArgs& p, const SeqTile& t, int kh, int row) {
+  return (kh * p.Tq + t.q0) * p.g + row;
+}
+
 // dq, and what the other kernel needs of a row: its log-sum-exp in base 2 and D_i.  A workgroup has 128 rows, as forward.
 template <class T, int DP>
 __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
@@ -538,7 +619,6 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
   constexpr int B = 128, KS = DP / 32, DB = DP / 16, SIZE = kKeys * Lds::kPitch;
   extern __shared__ char smem[];
   const lds_char_ptr lds = (lds_char_ptr)smem;
-  const int rp = Lds::rows_place(), cp = Lds::columns_place();
   const bool ok = sequences_ok(p);
   if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = ok ? 0 : kErrOffsets;
   if (!ok) return poison<T>(p.dq, p.Tq, p.hq, p.D);
@@ -574,9 +654,10 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
     delta[n] = row_sum(delta[n]);
     lse2[n] = row.exists ? p.lse[token * p.hq + head] * kLog2e : 0.f;
     if (row.exists && group == 0) {
-      p.delta[token * p.hq + head] = delta[n];
+      const int64_t at = packed_row(p, t, kh, row0 + n * 16);
+      p.delta[at] = delta[n];
       // of a row that sees nothing: every probability comes out as 0
-      p.lse2[token * p.hq + head] = lse2[n] == -__builtin_inff() ? __builtin_inff() : lse2[n];
+      p.lse2[at] = lse2[n] == -__builtin_inff() ? __builtin_inff() : lse2[n];
     }
     row_sees[n] = row.sees;
     all_see = row.sees < all_see ? row.sees : all_see;
@@ -594,7 +675,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
       ks.start(lds + (slot ^ 2 * SIZE), j0 + kKeys, t.nk);
       vs.start(lds + (slot ^ 2 * SIZE) + SIZE, j0 + kKeys, t.nk);
     }
-    const lds_char_ptr kt = lds + slot, vt = kt + SIZE;
+    const int k_rows = Lds::rows_place(lds + slot), k_columns = Lds::columns_place(lds + slot);
     f32x4 s[2][2][2], dp[2][2][2];     // [half][rows][keys]
     Frag w[2][2];
     const auto finish = [&](int c, int i) {
@@ -614,23 +695,23 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
       ready(w[c]);
     };
     constexpr int PER_S = 8 / KS / 2, PER_C = 16 / DB;
-    scores<Lds, KS>(s[0], kt, rp, 0, q, [](int) {});
-    scores<Lds, KS>(dp[0], vt, rp, 0, dout, [](int) {});
-    scores<Lds, KS>(s[1], kt, rp, 32, q, [&](int i) {
+    scores<Lds, KS>(s[0], k_rows, 0, q, [](int) {});
+    scores<Lds, KS>(dp[0], k_rows, SIZE, dout, [](int) {});
+    scores<Lds, KS>(s[1], k_rows, 32 * Lds::kPitch, q, [&](int i) {
 #pragma unroll
       for (int x = 0; x < PER_S; ++x) finish(0, i * PER_S + x);
     });
-    scores<Lds, KS>(dp[1], vt, rp, 32, dout, [&](int i) {
+    scores<Lds, KS>(dp[1], k_rows, SIZE + 32 * Lds::kPitch, dout, [&](int i) {
 #pragma unroll
       for (int x = 0; x < PER_S; ++x) finish(0, 8 + i * PER_S + x);
     });
     mask(0);
-    add_columns<Lds, DB>(dq, kt, cp, 0, w[0], [&](int i) {
+    add_columns<Lds, DB>(dq, k_columns, 0, w[0], [&](int i) {
 #pragma unroll
       for (int x = 0; x < PER_C; ++x) finish(1, i * PER_C + x);
     });
     mask(1);
-    add_columns<Lds, DB>(dq, kt, cp, 32, w[1], [](int) {});
+    add_columns<Lds, DB>(dq, k_columns, 32 * Lds::kPitch, w[1], [](int) {});
   }
   settle(dq);
 #pragma unroll
@@ -653,31 +734,54 @@ struct RowStager {
   static constexpr int kRowsPerLoad = 64 / Lds::kChunks, kLoads = kRows / (4 * kRowsPerLoad), SIZE = kRows * Lds::kPitch;
   static constexpr int kBytes = 2 * SIZE + 2 * kRows * 4;
   static constexpr uint32_t kOutside = 0x80000000u;
-  __device__ static __forceinline__ void start(const AttnArgs& p, const SeqTile& t, int kh, lds_char_ptr lds, int first) {
-    // nothing of the addresses is kept from one tile to the next: the registers are needed elsewhere
-    const int lane = fresh(threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int rows = t.nq * p.g, token0 = by_group(p, first);
+  // Where the heads in a group divide the rows that lie between two loads of a wavefront, a lane is at the same place of a token's heads
+  // with every load, and only the (scalar) token moves.
+  bool alike;
+  uint32_t whole_q, whole_d;
+  __device__ __forceinline__ RowStager(const AttnArgs& p) {
+    const int lane = threadIdx.x & 63, r = uniform((int)threadIdx.x >> 6) * kRowsPerLoad + lane / Lds::kChunks;
+    const int c = ((lane % Lds::kChunks) ^ Lds::swizzle(r)) * 16;
+    alike = 4 * kRowsPerLoad % 16 == 0 && 4 * kRowsPerLoad % p.g == 0;
+    const int token = by_group(p, r), head = r - token * p.g;
+    const bool any = c < p.D * (int)sizeof(T);
+    whole_q = any ? (uint32_t)(token * (int)p.q.token + head * (int)p.q.head + c) : kOutside;
+    whole_d = any ? (uint32_t)(token * (int)p.dout.token + head * (int)p.dout.head + c) : kOutside;
+  }
+  // Starts the loads of rows [first, first + 64); `first` is a multiple of 64.
+  __device__ __forceinline__ void start(const AttnArgs& p, const SeqTile& t, int kh, lds_char_ptr lds, int first) const {
+    const int wave = uniform((int)threadIdx.x >> 6), rows = t.nq * p.g, token0 = uniform(by_group(p, first));
     const __amdgpu_buffer_rsrc_t q =
         __builtin_amdgcn_make_buffer_rsrc((void*)p.q.row(t.q0 + token0, kh * p.g), 0, kOutside, 0x00020000);
     const __amdgpu_buffer_rsrc_t d =
         __builtin_amdgcn_make_buffer_rsrc((void*)p.dout.row(t.q0 + token0, kh * p.g), 0, kOutside, 0x00020000);
+    if (alike && first + kRows <= rows) {
+      const int tokens = by_group(p, 4 * kRowsPerLoad);
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-      const int r = (j * 4 + wave) * kRowsPerLoad + lane / Lds::kChunks, x = first + r;
-      const int c = ((lane % Lds::kChunks) ^ Lds::swizzle(r)) * 16;
-      const int token = by_group(p, x), head = x - token * p.g;
-      const bool any = x < rows && c < p.D * (int)sizeof(T);
-      const uint32_t vq = any ? (uint32_t)((token - token0) * (int)p.q.token + head * (int)p.q.head + c) : kOutside;
-      const uint32_t vd = any ? (uint32_t)((token - token0) * (int)p.dout.token + head * (int)p.dout.head + c) : kOutside;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(q, (lds_void_ptr)(lds + (j * 4 + wave) * 1024), 16, vq, 0, 0, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(d, (lds_void_ptr)(lds + SIZE + (j * 4 + wave) * 1024), 16, vd, 0, 0, 0);
+      for (int j = 0; j < kLoads; ++j) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(q, (lds_void_ptr)(lds + (j * 4 + wave) * 1024), 16, whole_q,
+                                                 j * tokens * (int)p.q.token, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(d, (lds_void_ptr)(lds + SIZE + (j * 4 + wave) * 1024), 16, whole_d,
+                                                 j * tokens * (int)p.dout.token, 0, 0);
+      }
+    } else {
+      const int lane = fresh(threadIdx.x) & 63;
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        const int r = (j * 4 + wave) * kRowsPerLoad + lane / Lds::kChunks, x = first + r;
+        const int c = ((lane % Lds::kChunks) ^ Lds::swizzle(r)) * 16;
+        const int token = by_group(p, x), head = x - token * p.g;
+        const bool any = x < rows && c < p.D * (int)sizeof(T);
+        const uint32_t vq = (uint32_t)((token - token0) * (int)p.q.token + head * (int)p.q.head + c);
+        const uint32_t vd = (uint32_t)((token - token0) * (int)p.dout.token + head * (int)p.dout.head + c);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(q, (lds_void_ptr)(lds + (j * 4 + wave) * 1024), 16, any ? vq : kOutside, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(d, (lds_void_ptr)(lds + SIZE + (j * 4 + wave) * 1024), 16, any ? vd : kOutside, 0, 0, 0);
+      }
     }
     if (wave < 2) {
-      const int x = first + lane, token = by_group(p, x);
-      const __amdgpu_buffer_rsrc_t n = __builtin_amdgcn_make_buffer_rsrc(
-          (void*)((wave ? p.delta : p.lse2) + (t.q0 + token0) * p.hq + kh * p.g), 0, kOutside, 0x00020000);
-      const uint32_t v = x < rows ? (uint32_t)((token - token0) * p.hq + x - token * p.g) * 4 : kOutside;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(n, (lds_void_ptr)(lds + 2 * SIZE + wave * kRows * 4), 4, v, 0, 0, 0);
+      const int left = rows - first < kRows ? rows - first : kRows;
+      const __amdgpu_buffer_rsrc_t n =
+          __builtin_amdgcn_make_buffer_rsrc((void*)((wave ? p.delta : p.lse2) + packed_row(p, t, kh, first)), 0, left * 4, 0x00020000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(n, (lds_void_ptr)(lds + 2 * SIZE + wave * kRows * 4), 4, (threadIdx.x & 63) * 4, 0, 0, 0);
     }
   }
 };
@@ -691,7 +795,6 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   constexpr int B = 128, KS = DP / 32, DB = DP / 16;
   extern __shared__ char smem[];
   const lds_char_ptr lds = (lds_char_ptr)smem;
-  const int rp = Lds::rows_place(), cp = Lds::columns_place();
   if (!sequences_ok(p)) {
     poison<T>(p.dk, p.Tk, p.hk, p.D);
     return poison<T>(p.dv, p.Tk, p.hk, p.D);
@@ -702,7 +805,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   const int rows = t.nq * p.g, ahead = t.nk - t.nq;
   // the first row that sees the tile's first key, and whole tiles of rows
   const int from = p.causal && t.first > ahead ? (t.first - ahead) * p.g / kRows * kRows : 0;
-  if (from < rows) Stage::start(p, t, kh, lds, from);
+  const Stage stage(p);
+  if (from < rows) stage.start(p, t, kh, lds, from);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Frag k[2][KS], v[2][KS];
   f32x4 dk[2][DB], dv[2][DB];
@@ -731,15 +835,15 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   int slot = 0;
   for (int r0 = from; r0 < rows; r0 += kRows, slot ^= 1) {
     staged_barrier();
-    if (r0 + kRows < rows) Stage::start(p, t, kh, lds + (slot ^ 1) * Stage::kBytes, r0 + kRows);
-    const lds_char_ptr qt = lds + slot * Stage::kBytes, dt = qt + Stage::SIZE, numbers = dt + Stage::SIZE;
+    if (r0 + kRows < rows) stage.start(p, t, kh, lds + (slot ^ 1) * Stage::kBytes, r0 + kRows);
+    const lds_char_ptr numbers = lds + slot * Stage::kBytes + 2 * Stage::SIZE;
+    const int places = Lds::rows_place(lds + slot * Stage::kBytes), column_places = Lds::columns_place(lds + slot * Stage::kBytes);
 #pragma unroll 1
     for (int c = 0; c < kRows / 32; ++c) {
       typedef __attribute__((address_space(3))) f32x4* ptr;
       Frag w[2], wd[2];      // probabilities and dS of 32 rows, keys in columns
       f32x4 s[2][2], dp[2][2];     // [keys][rows]
-      scores<Lds, KS>(s, qt, rp, c * 32, k, [](int) {});
-      scores<Lds, KS>(dp, dt, rp, c * 32, v, [](int) {});
+      scores2<Lds, KS, Stage::SIZE>(s, dp, places + c * 32 * Lds::kPitch, k, v);
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const lds_char_ptr at = numbers + (fresh(threadIdx.x) >> 4 & 3) * 16 + (c * 32 + b * 16) * 4;
@@ -765,8 +869,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
       for (int n = 0; n < 2; ++n) pack(s[n][0], s[n][1], w[n]), pack(dp[n][0], dp[n][1], wd[n]);
       ready(w);
       ready(wd);
-      add_columns<Lds, DB>(dv, dt, cp, c * 32, w, [](int) {});
-      add_columns<Lds, DB>(dk, qt, cp, c * 32, wd, [](int) {});
+      add_columns2<Lds, DB, Stage::SIZE>(dk, dv, column_places + c * 32 * Lds::kPitch, wd, w);
     }
   }
   settle(dk);
