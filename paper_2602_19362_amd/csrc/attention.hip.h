@@ -65,10 +65,25 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
   return (int64_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
 }
 
-// Whose tile `id` is, by a search over the first ids of the sequences, 64 at a time; `off` and `per` say what tiles are cut from
-// (rows: query offsets times heads in a group; keys: key offsets).  Only after sequences_ok.
+// Tiles of rows, or of keys.
+enum TileOf { kOfRows, kOfKeys };
+
+__device__ __forceinline__ SeqTile tile_of(const AttnArgs& p, int seq, TileOf what, int64_t first) {
+  SeqTile t;
+  t.q0 = uniform(p.q_offsets[seq]);
+  t.k0 = uniform(p.k_offsets[seq]);
+  t.nq = uniform((int)(p.q_offsets[seq + 1] - t.q0));
+  t.nk = uniform((int)(p.k_used ? p.k_used[seq] : p.k_offsets[seq + 1] - t.k0));
+  const int64_t end = what == kOfRows ? (int64_t)t.nq * p.g : t.nk;
+  t.first = uniform((int)(first < end ? first : end));
+  return t;
+}
+
+// The tile with this id, by a search over the first ids of the sequences, 64 at a time.  Only after sequences_ok.
 template <int B>
-__device__ __forceinline__ SeqTile find_tile(const AttnArgs& p, const int64_t* __restrict__ off, int per, int64_t id) {
+__device__ __forceinline__ SeqTile find_tile(const AttnArgs& p, TileOf what, int64_t id) {
+  const int64_t* __restrict__ off = what == kOfRows ? p.q_offsets : p.k_offsets;
+  const int per = what == kOfRows ? p.g : 1;
   int lo = 0, n = p.n_seq;                       // the last sequence in [lo, lo + n) whose first id is not above `id`
   const int lane = threadIdx.x & 63;
   while (n > 1) {
@@ -79,15 +94,64 @@ __device__ __forceinline__ SeqTile find_tile(const AttnArgs& p, const int64_t* _
     n = n - k * step < step ? n - k * step : step;
   }
   lo = uniform(lo);
-  const int64_t q0 = uniform(p.q_offsets[lo]), k0 = uniform(p.k_offsets[lo]), from = uniform(off[lo]);
-  SeqTile t;
-  t.q0 = q0;
-  t.k0 = k0;
-  t.nq = uniform((int)(p.q_offsets[lo + 1] - q0));
-  t.nk = uniform((int)(p.k_used ? p.k_used[lo] : p.k_offsets[lo + 1] - k0));
-  const int64_t first = (id - (from * per / B + lo)) * B, rows = (uniform(off[lo + 1]) - from) * per;
-  t.first = uniform((int)(first < rows ? first : rows));
-  return t;
+  return tile_of(p, lo, what, (id - (uniform(off[lo]) * per / B + lo)) * B);
+}
+
+// Sums over the lanes up to each one, and the largest of all.
+__device__ __forceinline__ int prefix_sum(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // from one, two, four, eight lanes below, in rows of 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // from the row before, from the half before
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+  return v;
+}
+__device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
+
+// The tile that stands `rank`-th when all are ordered by how far they reach, longest first (in 256 levels): what a tile of rows costs is
+// the keys that its last row sees, a tile of keys the queries that see its first key, and either is a closed form of the tile's
+// number, so that every workgroup finds its own by a search over levels.  Long tiles that start last are what the chip
+// waits for in the end.  False: there are not so many.  More than 64 sequences go in the order of their ids.
+template <int B>
+__device__ __forceinline__ bool pick_tile(const AttnArgs& p, TileOf what, int rank, SeqTile& t) {
+  if (p.n_seq > 64) {
+    const int64_t last = what == kOfRows ? tile_ids<B>(p.Tq * p.g, p.n_seq) - 1 : 0;
+    t = find_tile<B>(p, what, what == kOfRows ? last - rank : rank);
+    return t.first < (what == kOfRows ? t.nq * p.g : t.nk);
+  }
+  const int lane = threadIdx.x & 63;
+  int nq = 0, nk = 0;
+  if (lane < p.n_seq) {
+    nq = (int)(p.q_offsets[lane + 1] - p.q_offsets[lane]);
+    nk = (int)(p.k_used ? p.k_used[lane] : p.k_offsets[lane + 1] - p.k_offsets[lane]);
+  }
+  const int tiles = what == kOfRows ? (int)(((int64_t)nq * p.g + B - 1) / B) : (nk + B - 1) / B, reach = what == kOfRows ? nk : nq;
+  // the sequence's tiles that reach beyond x >= 0
+  const auto beyond = [&](int x) {
+    if (x >= reach) return 0;
+    if (!p.causal) return tiles;
+    if (what == kOfKeys) return min(tiles, (nk - x + B - 1) / B);
+    const int token = x - (nk - nq);       // the first that sees more than x
+    return tiles - (token > 0 ? (int)((int64_t)token * p.g / B) : 0);
+  };
+  int most = reach;
+#pragma unroll
+  for (int x = 32; x > 0; x >>= 1) most = max(most, __shfl_xor(most, x, 64));
+  const int unit = (uniform(most) + 255) / 256;
+  int lo = -1, hi = 256;      // all tiles reach beyond level -1, none beyond 256; lo: more than `rank` do, hi: not
+  while (hi - lo > 1) {
+    const int y = (lo + hi) / 2;
+    if (last_lane(prefix_sum(beyond(y * unit))) > rank) lo = y;
+    else hi = y;
+  }
+  const int above = beyond(hi * unit), mine = (lo < 0 ? tiles : beyond(lo * unit)) - above;
+  const int to = prefix_sum(mine), left = rank - last_lane(prefix_sum(above));
+  if (left >= last_lane(to)) return false;
+  const int seq = __ffsll((unsigned long long)__ballot(to > left)) - 1;
+  const int nth = __builtin_amdgcn_readlane(above + left - (to - mine), seq);    // among the sequence's, longest first
+  t = tile_of(p, seq, what, (int64_t)(what == kOfRows ? __builtin_amdgcn_readlane(tiles, seq) - 1 - nth : nth) * B);
+  return true;
 }
 
 // Malformed sequences: the outputs are NaN.  Workgroups share the tokens.
@@ -335,7 +399,7 @@ __device__ __forceinline__ int tile_sees(const AttnArgs& p, const SeqTile& t) {
   return n < 0 ? 0 : n < t.nk ? n : t.nk;
 }
 
-constexpr int kKeys = 64;   // keys staged at a time
+constexpr int kFwdKeys = 32, kKeys = 64;   // keys staged at a time: forward, for dq
 
 // ---------------------------------------------------------------------------------------------------------------- forward
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -466,13 +530,14 @@ __device__ __forceinline__ void add_columns2(f32x4 (&a)[2][DB], f32x4 (&b)[2][DB
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// A workgroup: 128 rows, 32 a wavefront, over all keys that they see, 64 at a time.
+// A workgroup: 128 rows, 32 a wavefront, over all keys that they see, 32 at a time.  Three wavefronts a
+// SIMD: one's exponentials run beside another's products.
 template <class T, int DP>
-__global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs p) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void k_attn_fwd(const AttnArgs p) {
   typedef typename FragOf<T>::type Frag;
   typedef Tile<T, DP> Lds;
-  typedef Stager<T, DP, kKeys> Stage;
-  constexpr int B = 128, KS = DP / 32, DB = DP / 16, SIZE = kKeys * Lds::kPitch;
+  typedef Stager<T, DP, kFwdKeys> Stage;
+  constexpr int B = 128, KS = DP / 32, DB = DP / 16, SIZE = kFwdKeys * Lds::kPitch;
   extern __shared__ char smem[];
   const lds_char_ptr lds = (lds_char_ptr)smem;     // two slots of keys and values
   const bool ok = sequences_ok(p);
@@ -483,8 +548,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs p) {
     return;
   }
   const int kh = blockIdx.x % p.hk;
-  const SeqTile t = find_tile<B>(p, p.q_offsets, p.g, tile_ids<B>(p.Tq * p.g, p.n_seq) - 1 - blockIdx.x / p.hk);
-  if (t.first >= t.nq * p.g) return;
+  SeqTile t;
+  if (!pick_tile<B>(p, kOfRows, blockIdx.x / p.hk, t)) return;
   const int sees = tile_sees<B>(p, t);
   const Stage ks(p.k.row(t.k0, kh), p.k.token, p.D), vs(p.v.row(t.k0, kh), p.v.token, p.D);
   if (sees > 0) ks.start(lds, 0, t.nk), vs.start(lds + SIZE, 0, t.nk);
@@ -519,76 +584,56 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs p) {
   }
   all_see = __builtin_amdgcn_readfirstlane(all_see);
   int slot = 0;
-  for (int j0 = 0; j0 < sees; j0 += kKeys, slot ^= 2 * SIZE) {
+  for (int j0 = 0; j0 < sees; j0 += kFwdKeys, slot ^= 2 * SIZE) {
     staged_barrier();
-    if (j0 + kKeys < sees) {
-      ks.start(lds + (slot ^ 2 * SIZE), j0 + kKeys, t.nk);
-      vs.start(lds + (slot ^ 2 * SIZE) + SIZE, j0 + kKeys, t.nk);
+    if (j0 + kFwdKeys < sees) {
+      ks.start(lds + (slot ^ 2 * SIZE), j0 + kFwdKeys, t.nk);
+      vs.start(lds + (slot ^ 2 * SIZE) + SIZE, j0 + kFwdKeys, t.nk);
     }
     const int k_rows = Lds::rows_place(lds + slot), v_columns = Lds::columns_place(lds + slot + SIZE);
-    // Two halves of 32 keys, a step apart: the exponentials of the first run beside the scores of the second, those of the second
-    // beside the first one's product with the values.
-    f32x4 a[2][2], b[2][2];
-    Frag wa[2], wb[2];
-    const auto mask = [&](f32x4 (&s)[2][2], int first) {
-      if (first + 32 <= all_see) return;
+    f32x4 s[2][2];     // [rows][keys]
+    scores<Lds, KS>(s, k_rows, 0, q, [](int) {});
+    if (j0 + kFwdKeys > all_see) {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int x = 0; x < 8; ++x)
-          if (first + (x >> 2) * 16 + group * 4 + (x & 3) >= row_sees[n]) s[n][x >> 2][x & 3] = -__builtin_inff();
-    };
+          if (j0 + (x >> 2) * 16 + group * 4 + (x & 3) >= row_sees[n]) s[n][x >> 2][x & 3] = -__builtin_inff();
+    }
     // The maximum that the exponentials are taken from follows only when it falls behind by 2^8: until then they stay below 2^8, and
     // what is rounded is rounded as well as below 1.
-    const auto follow = [&](const f32x4 (&s)[2][2], bool second) {
-      float top[2];
+    float top[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      top[n] = m[n];
+#pragma unroll
+      for (int x = 0; x < 8; x += 2) top[n] = max3(top[n], s[n][x >> 2][x & 3], s[n][x >> 2][(x & 3) + 1]);
+      top[n] = row_max(top[n]);
+    }
+    if (__any(fmaxf(top[0] - m[0], top[1] - m[1]) * scale2 > 8.f)) {
+      settle(o);
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
-        top[n] = m[n];
+        const float old = __builtin_amdgcn_exp2f((m[n] - top[n]) * scale2);
+        m[n] = top[n];
+        l[n] *= old;
 #pragma unroll
-        for (int x = 0; x < 8; x += 2) top[n] = max3(top[n], s[n][x >> 2][x & 3], s[n][x >> 2][(x & 3) + 1]);
-        top[n] = row_max(top[n]);
+        for (int d = 0; d < DB; ++d) o[n][d] *= old;
       }
-      if (__any(fmaxf(top[0] - m[0], top[1] - m[1]) * scale2 > 8.f)) {
-        settle(o);
+    }
+    Frag w[2];
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          const float old = __builtin_amdgcn_exp2f((m[n] - top[n]) * scale2);
-          m[n] = top[n];
-          l[n] *= old;
+    for (int n = 0; n < 2; ++n) {
 #pragma unroll
-          for (int d = 0; d < DB; ++d) o[n][d] *= old;
-          if (second) a[n][0] *= old, a[n][1] *= old;
-        }
+      for (int x = 0; x < 8; ++x) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(s[n][x >> 2][x & 3], scale2, -m[n] * scale2));
+        l[n] += e;
+        s[n][x >> 2][x & 3] = e;
       }
-    };
-    const auto exponential = [&](f32x4 (&s)[2][2], int i) {
-      const int n = i >> 3, x = i & 7;
-      const float e = __builtin_amdgcn_exp2f(fmaf(s[n][x >> 2][x & 3], scale2, -m[n] * scale2));
-      l[n] += e;
-      s[n][x >> 2][x & 3] = e;
-    };
-    constexpr int PER_S = 16 / (2 * KS), PER_C = 16 / DB;
-    scores<Lds, KS>(a, k_rows, 0, q, [](int) {});
-    mask(a, j0);
-    follow(a, false);
-    scores<Lds, KS>(b, k_rows, 32 * Lds::kPitch, q, [&](int i) {
-#pragma unroll
-      for (int x = 0; x < PER_S; ++x) exponential(a, i * PER_S + x);
-    });
-    mask(b, j0 + 32);
-    follow(b, true);
-#pragma unroll
-    for (int n = 0; n < 2; ++n) pack(a[n][0], a[n][1], wa[n]);
-    ready(wa);
-    add_columns<Lds, DB>(o, v_columns, 0, wa, [&](int i) {
-#pragma unroll
-      for (int x = 0; x < PER_C; ++x) exponential(b, i * PER_C + x);
-    });
-#pragma unroll
-    for (int n = 0; n < 2; ++n) pack(b[n][0], b[n][1], wb[n]);
-    ready(wb);
-    add_columns<Lds, DB>(o, v_columns, 32 * Lds::kPitch, wb, [](int) {});
+      pack(s[n][0], s[n][1], w[n]);
+    }
+    ready(w);
+    add_columns<Lds, DB>(o, v_columns, 0, w, [](int) {});
   }
   settle(o);
 #pragma unroll
@@ -623,8 +668,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
   if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = ok ? 0 : kErrOffsets;
   if (!ok) return poison<T>(p.dq, p.Tq, p.hq, p.D);
   const int kh = blockIdx.x % p.hk;
-  const SeqTile t = find_tile<B>(p, p.q_offsets, p.g, tile_ids<B>(p.Tq * p.g, p.n_seq) - 1 - blockIdx.x / p.hk);
-  if (t.first >= t.nq * p.g) return;
+  SeqTile t;
+  if (!pick_tile<B>(p, kOfRows, blockIdx.x / p.hk, t)) return;
   const int sees = tile_sees<B>(p, t);
   const Stage ks(p.k.row(t.k0, kh), p.k.token, p.D), vs(p.v.row(t.k0, kh), p.v.token, p.D);
   if (sees > 0) ks.start(lds, 0, t.nk), vs.start(lds + SIZE, 0, t.nk);
@@ -800,8 +845,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
     return poison<T>(p.dv, p.Tk, p.hk, p.D);
   }
   const int kh = blockIdx.x % p.hk;
-  const SeqTile t = find_tile<B>(p, p.k_offsets, 1, blockIdx.x / p.hk);
-  if (t.first >= t.nk) return;
+  SeqTile t;
+  if (!pick_tile<B>(p, kOfKeys, blockIdx.x / p.hk, t)) return;
   const int rows = t.nq * p.g, ahead = t.nk - t.nq;
   // the first row that sees the tile's first key, and whole tiles of rows
   const int from = p.causal && t.first > ahead ? (t.first - ahead) * p.g / kRows * kRows : 0;

@@ -126,7 +126,7 @@ static int launch_attn(K kernel, int64_t workgroups, int lds, const AttnArgs& a,
 
 template <class T, int DP>
 static int launch_attn_fwd(const AttnArgs& a, hipStream_t st) {
-  return launch_attn(k_attn_fwd<T, DP>, tile_ids<128>(a.Tq * a.g, a.n_seq) * a.hk, 4 * kKeys * Tile<T, DP>::kPitch, a, st);
+  return launch_attn(k_attn_fwd<T, DP>, tile_ids<128>(a.Tq * a.g, a.n_seq) * a.hk, 4 * kFwdKeys * Tile<T, DP>::kPitch, a, st);
 }
 
 template <class T, int DP>
