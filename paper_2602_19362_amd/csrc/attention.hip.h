@@ -29,7 +29,9 @@ struct AttnArgs {
   const int64_t *q_offsets, *k_offsets, *k_used;
   int* status;
   int64_t Tq, Tk;
+  float *partials, *part_sums;          // of splits
   int n_seq, hq, hk, g, D, causal;
+  int splits;                           // of the keys of a tile of rows (forward, dq), or of the rows of a tile of keys
   uint32_t g_mul;                       // quotients by g, see by_group
   int g_shift;
   float scale;
@@ -328,12 +330,12 @@ struct Tile {
 };
 
 // Rows of one tile of R rows of DP channels on their way from memory to LDS without passing through registers: 16 bytes a lane, whole
-// LDS rows a wavefront.  What lies behind the last row or channel is behind the buffer's range and reads as zeros.
-template <class T, int DP, int R>
+// LDS rows a wavefront, W wavefronts together.  What lies behind the last row or channel is behind the buffer's range and reads as zeros.
+template <class T, int DP, int R, int W>
 struct Stager {
   typedef Tile<T, DP> Lds;
   static constexpr int kRows = 64 / Lds::kChunks;          // that a wavefront's load covers
-  static constexpr int kLoads = R / (4 * kRows);           // of each of four wavefronts
+  static constexpr int kLoads = R / (W * kRows);           // of each wavefront
   static constexpr uint32_t kOutside = 0x80000000u;        // rows of a tile span 2^30 bytes at most
   const char* base;
   int64_t stride;
@@ -341,7 +343,7 @@ struct Stager {
   uint32_t column, columns, whole;
   __device__ __forceinline__ Stager(const char* p, int64_t token_stride, int D) : base(p), stride(token_stride) {
     const int lane = threadIdx.x & 63;
-    wave = uniform((int)threadIdx.x >> 6);
+    wave = W == 1 ? 0 : uniform((int)threadIdx.x >> 6);
     row = wave * kRows + lane / Lds::kChunks;
     column = ((lane % Lds::kChunks) ^ Lds::swizzle(row)) * 16;
     columns = D * sizeof(T);
@@ -351,27 +353,28 @@ struct Stager {
   __device__ __forceinline__ void start(lds_char_ptr lds, int first, int n) const {
     const __amdgpu_buffer_rsrc_t r =
         __builtin_amdgcn_make_buffer_rsrc((void*)(base + first * stride), 0, kOutside, 0x00020000);
-    // rows 16 apart are swizzled alike; a wavefront of two rows comes back to them with every other load
-    constexpr bool kAlike = 4 * kRows % 16 == 0;
-    if (kAlike && first + R <= n) {
+    // rows 16 apart are swizzled alike, and others by bits that do not depend on the lane
+    if (W * kRows % 16 == 0 && first + R <= n) {
 #pragma unroll
       for (int j = 0; j < kLoads; ++j)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_ptr)(lds + (j * 4 + wave) * 1024), 16, whole, j * 4 * kRows * (int)stride, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_ptr)(lds + (j * W + wave) * 1024), 16, whole, j * W * kRows * (int)stride, 0, 0);
       return;
     }
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
-      const int at = row + j * 4 * kRows;
-      const uint32_t c = column ^ (kAlike ? 0 : (uint32_t)(j & 1) << 5);
+      const int at = row + j * W * kRows;
+      const uint32_t c = column ^ (uint32_t)Lds::swizzle(j * W * kRows) << 4;
       const uint32_t v = first + at < n && c < columns ? (uint32_t)(at * (int)stride) + c : kOutside;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_ptr)(lds + (j * 4 + wave) * 1024), 16, v, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_ptr)(lds + (j * W + wave) * 1024), 16, v, 0, 0, 0);
     }
   }
 };
 
-// Everything that this wavefront started has arrived, and so has what the others of the workgroup started.
+// Everything that this wavefront started has arrived ...
+__device__ __forceinline__ void staged() { __builtin_amdgcn_s_waitcnt(vmcnt_imm(0) & ~0x0F00); }      // vmcnt(0) lgkmcnt(0)
+// ... and so has what the others of the workgroup started.
 __device__ __forceinline__ void staged_barrier() {
-  __builtin_amdgcn_s_waitcnt(vmcnt_imm(0) & ~0x0F00);      // vmcnt(0) lgkmcnt(0)
+  staged();
   __builtin_amdgcn_s_barrier();
 }
 
@@ -530,18 +533,54 @@ __device__ __forceinline__ void add_columns2(f32x4 (&a)[2][DB], f32x4 (&b)[2][DB
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// A workgroup: 128 rows, 32 a wavefront, over all keys that they see, 32 at a time.  Three wavefronts a
-// SIMD: one's exponentials run beside another's products.
-template <class T, int DP>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void k_attn_fwd(const AttnArgs p) {
+// Where a row's numbers lie in workspaces: rows of a key head one after the other.
+__device__ __forceinline__ int64_t packed_row(const AttnArgs& p, const SeqTile& t, int kh, int row) {
+  return (kh * p.Tq + t.q0) * p.g + row;
+}
+
+// LDS of a forward workgroup: slots of a tile of keys and one of values, and (WK = 4) the same for every wavefront, later its results.
+template <class T, int DP, int WK>
+struct FwdLds {
+  static constexpr int kTile = kFwdKeys * Tile<T, DP>::kPitch, kSlots = WK == 4 && sizeof(T) == 4 ? 1 : 2;
+  static constexpr int kStages = 2 * kSlots * kTile, kResults = 32 * (DP * 4 + 16);
+  static constexpr int kWave = WK == 1 || kStages > kResults ? kStages : (kResults + 511) / 512 * 512;
+  static constexpr int kBytes = WK * kWave;
+  static_assert(kBytes <= 160 * 1024, "LDS of one CU");
+};
+
+// Keys [begin, end) of split `split` of the n that a tile sees, in whole steps.
+struct Part {
+  int begin, end;
+  __device__ __forceinline__ Part(int n, int splits, int split, int step) {
+    const int64_t each = ((int64_t)n + (int64_t)splits * step - 1) / ((int64_t)splits * step) * step, from = split * each;
+    begin = (int)(from < n ? from : n);
+    end = (int)(from + each < n ? from + each : n);
+  }
+};
+
+// A result of one split, unnormalised: partial[split][packed row][D], and its maximum (in base 2) and sum.
+__device__ __forceinline__ void store_sums(const AttnArgs& p, int64_t row, float m2, float l) {
+  *(float2*)(p.part_sums + (blockIdx.y * p.Tq * p.hq + row) * 2) = make_float2(m2, l);
+}
+__device__ __forceinline__ float* partial_row(const AttnArgs& p, int64_t rows, int64_t row) {
+  return p.partials + (blockIdx.y * rows + row) * p.D;
+}
+
+// WK = 1: a workgroup has 128 rows, 32 a wavefront, over all keys that they see, 32 at a time.  Three wavefronts a SIMD: one's exponentials
+// run beside another's products.
+// WK = 4, for few rows: the wavefronts have the same 32 rows and take the steps of 32 keys in turn, each through LDS of its own, and
+// join at the end.  That is bound by reading the keys and values.
+// Where tiles are few, their keys are split over workgroups (blockIdx.y) whose results k_attn_join puts together.
+template <class T, int DP, int WK>
+__global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k_attn_fwd(const AttnArgs p) {
   typedef typename FragOf<T>::type Frag;
   typedef Tile<T, DP> Lds;
-  typedef Stager<T, DP, kFwdKeys> Stage;
-  constexpr int B = 128, KS = DP / 32, DB = DP / 16, SIZE = kFwdKeys * Lds::kPitch;
+  typedef Stager<T, DP, kFwdKeys, 4 / WK> Stage;
+  typedef FwdLds<T, DP, WK> Size;
+  constexpr int B = 128 / WK, KS = DP / 32, DB = DP / 16, SIZE = Size::kTile;
   extern __shared__ char smem[];
-  const lds_char_ptr lds = (lds_char_ptr)smem;     // two slots of keys and values
   const bool ok = sequences_ok(p);
-  if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = ok ? 0 : kErrOffsets;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = ok ? 0 : kErrOffsets;
   if (!ok) {
     poison<T>(p.o, p.Tq, p.hq, p.D);
     if (p.lse) poison(p.lse, p.Tq * p.hq);
@@ -550,10 +589,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void k_attn_fwd(const 
   const int kh = blockIdx.x % p.hk;
   SeqTile t;
   if (!pick_tile<B>(p, kOfRows, blockIdx.x / p.hk, t)) return;
-  const int sees = tile_sees<B>(p, t);
+  const int wave = uniform((int)threadIdx.x >> 6);
+  const lds_char_ptr lds = (lds_char_ptr)smem + (WK == 1 ? 0 : wave * Size::kWave);     // slots of keys and values
+  const Part part(tile_sees<B>(p, t), p.splits, blockIdx.y, kFwdKeys * WK);
   const Stage ks(p.k.row(t.k0, kh), p.k.token, p.D), vs(p.v.row(t.k0, kh), p.v.token, p.D);
-  if (sees > 0) ks.start(lds, 0, t.nk), vs.start(lds + SIZE, 0, t.nk);
-  const int group = threadIdx.x >> 4 & 3, row0 = t.first + (threadIdx.x >> 6) * 32 + (threadIdx.x & 15);
+  int j0 = part.begin + (WK == 1 ? 0 : wave * kFwdKeys), slot = 0;
+  const auto stage = [&](int at, int first) {
+    ks.start(lds + at, first, t.nk);
+    vs.start(lds + at + SIZE, first, t.nk);
+  };
+  if (Size::kSlots == 2 && j0 < part.end) stage(0, j0);
+  const int group = threadIdx.x >> 4 & 3, row0 = t.first + (WK == 1 ? wave * 32 : 0) + (threadIdx.x & 15);
   const bool flip = p.scale < 0.f;                 // then products are taken with -q, and with zeros if it is 0
   const float scale2 = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;
   int row_sees[2];
@@ -573,7 +619,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void k_attn_fwd(const 
 #pragma unroll
     for (int d = 0; d < DB; ++d) zero(o[n][d]);
     row_sees[n] = row.sees;
-    all_see = row.sees < all_see ? row.sees : all_see;
+    if (row.exists || WK == 1) all_see = row.sees < all_see ? row.sees : all_see;
     m[n] = kNegHuge;
     l[n] = 0.f;
   }
@@ -583,13 +629,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void k_attn_fwd(const 
     all_see = y < all_see ? y : all_see;
   }
   all_see = __builtin_amdgcn_readfirstlane(all_see);
-  int slot = 0;
-  for (int j0 = 0; j0 < sees; j0 += kFwdKeys, slot ^= 2 * SIZE) {
-    staged_barrier();
-    if (j0 + kFwdKeys < sees) {
-      ks.start(lds + (slot ^ 2 * SIZE), j0 + kFwdKeys, t.nk);
-      vs.start(lds + (slot ^ 2 * SIZE) + SIZE, j0 + kFwdKeys, t.nk);
-    }
+  for (; j0 < part.end; j0 += kFwdKeys * WK, slot ^= Size::kSlots == 2 ? 2 * SIZE : 0) {
+    if (Size::kSlots == 1) stage(0, j0);
+    if (WK == 1) staged_barrier();
+    else staged();
+    if (Size::kSlots == 2 && j0 + kFwdKeys * WK < part.end) stage(slot ^ 2 * SIZE, j0 + kFwdKeys * WK);
     const int k_rows = Lds::rows_place(lds + slot), v_columns = Lds::columns_place(lds + slot + SIZE);
     f32x4 s[2][2];     // [rows][keys]
     scores<Lds, KS>(s, k_rows, 0, q, [](int) {});
@@ -636,43 +680,131 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void k_attn_fwd(const 
     add_columns<Lds, DB>(o, v_columns, 0, w, [](int) {});
   }
   settle(o);
+  const auto finish = [&](float m2, float l) { return l == 0.f ? -__builtin_inff() : (m2 + __builtin_amdgcn_logf(l)) * kLn2f; };
+  const auto inverse = [&](float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : l; };
+  if constexpr (WK == 1) {
 #pragma unroll
-  for (int n = 0; n < 2; ++n) {
-    const Row row(p, t, row0 + n * 16);
-    l[n] = row_sum(l[n]);
-    if (!row.exists) continue;
+    for (int n = 0; n < 2; ++n) {
+      const Row row(p, t, row0 + n * 16);
+      l[n] = row_sum(l[n]);
+      if (!row.exists) continue;
+      const int head = kh * p.g + row.head;
+      if (p.splits > 1) {
+        const int64_t at = packed_row(p, t, kh, row0 + n * 16);
+        store_columns<float>((char*)partial_row(p, p.Tq * p.hq, at), o[n], 1.f, p.D);
+        if (group == 0) store_sums(p, at, m[n] * scale2, l[n]);
+        continue;
+      }
+      store_columns<T>(p.o.row(t.q0 + row.token, head), o[n], inverse(l[n]), p.D);
+      if (p.lse && group == 0) p.lse[(t.q0 + row.token) * p.hq + head] = finish(m[n] * scale2, l[n]);
+    }
+  } else {
+    // The wavefronts' results in LDS, then eight threads a row.
+    constexpr int PITCH = DP * 4 + 16;
+    typedef __attribute__((address_space(3))) float* lds_f32;
+    typedef __attribute__((address_space(3))) f32x4* lds_f32x4;
+    __syncthreads();      // everybody has read its last tile
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      l[n] = row_sum(l[n]);
+      const lds_char_ptr to = lds + (n * 16 + (threadIdx.x & 15)) * PITCH;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) *(lds_f32x4)(to + d * 64 + group * 16) = o[n][d];
+      if (group == 0) {
+        *(lds_f32)(to + DP * 4) = m[n] * scale2;
+        *(lds_f32)(to + DP * 4 + 4) = l[n];
+      }
+    }
+    __syncthreads();
+    const int r = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * (DP / 8);
+    const Row row(p, t, t.first + r);
+    const lds_char_ptr from = (lds_char_ptr)smem + r * PITCH;
+    float top = kNegHuge, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, *(lds_f32)(from + w * Size::kWave + DP * 4));
+    f32x4 x[DP / 32] = {};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float by = __builtin_amdgcn_exp2f(*(lds_f32)(from + w * Size::kWave + DP * 4) - top);
+      sum = fmaf(*(lds_f32)(from + w * Size::kWave + DP * 4 + 4), by, sum);
+#pragma unroll
+      for (int c = 0; c < DP / 32; ++c) x[c] += *(lds_f32x4)(from + w * Size::kWave + (c0 + c * 4) * 4) * by;
+    }
+    if (!row.exists) return;
     const int head = kh * p.g + row.head;
-    store_columns<T>(p.o.row(t.q0 + row.token, head), o[n], l[n] > 0.f ? 1.f / l[n] : l[n] == 0.f ? 0.f : l[n], p.D);
-    if (p.lse && group == 0)
-      p.lse[(t.q0 + row.token) * p.hq + head] =
-          l[n] == 0.f ? -__builtin_inff() : fmaf(m[n], scale2, __builtin_amdgcn_logf(l[n])) * kLn2f;
+    if (p.splits > 1) {
+      const int64_t at = packed_row(p, t, kh, t.first + r);
+#pragma unroll
+      for (int c = 0; c < DP / 32; ++c)
+        if (c0 + c * 4 < p.D) store4(partial_row(p, p.Tq * p.hq, at) + c0 + c * 4, x[c]);
+      if (c0 == 0) store_sums(p, at, top, sum);
+      return;
+    }
+    T* to = (T*)p.o.row(t.q0 + row.token, head);
+#pragma unroll
+    for (int c = 0; c < DP / 32; ++c)
+      if (c0 + c * 4 < p.D) store4(to + c0 + c * 4, x[c] * inverse(sum));
+    if (p.lse && c0 == 0) p.lse[(t.q0 + row.token) * p.hq + head] = finish(top, sum);
   }
 }
 
-// ---------------------------------------------------------------------------------------------------------------- backward
-// Where lse2 and delta of a row lie: rows of a key head one after the other.
-__device__ __forceinline__ int64_t packed_row(const AttnArgs& p, const SeqTile& t, int kh, int row) {
-  return (kh * p.Tq + t.q0) * p.g + row;
+// Puts the splits of a row together: 32 lanes a row, four channels each.
+template <class T>
+__global__ __launch_bounds__(256) void k_attn_join(const AttnArgs p) {
+  if (*p.status != 0) return;      // the outputs are NaN already
+  const int64_t rows = p.Tq * p.hq, row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (row >= rows) return;
+  const int c = (threadIdx.x & 31) * 4, h = (int)(row % p.g), kh = (int)(row / (p.Tq * p.g));
+  const int64_t token = row / p.g - kh * p.Tq;
+  const float2* sums = (const float2*)p.part_sums + row;
+  float top = kNegHuge, sum = 0.f;
+  for (int s = 0; s < p.splits; ++s) top = fmaxf(top, sums[s * rows].x);
+  f32x4 x = {};
+  for (int s = 0; s < p.splits; ++s) {
+    const float2 y = sums[s * rows];
+    const float by = __builtin_amdgcn_exp2f(y.x - top);
+    sum = fmaf(y.y, by, sum);
+    if (c < p.D) x += load4(p.partials + (s * rows + row) * p.D + c) * by;
+  }
+  const int head = kh * p.g + h;
+  if (c < p.D) store4((T*)p.o.row(token, head) + c, x * (sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum));
+  if (p.lse && c == 0) p.lse[token * p.hq + head] = sum == 0.f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * kLn2f;
 }
 
+// The sum of gradients' splits times a factor, in their order: out[token][head] from partial[split][head][token][group].
+template <class T>
+__global__ __launch_bounds__(256) void k_attn_add(const AttnArgs p, const float* __restrict__ partials, int64_t stride, Heads out, int64_t tokens,
+                                                  int heads, int g, int splits, float factor) {
+  if (*p.status != 0) return;
+  const int64_t rows = tokens * heads * g, row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int c = (threadIdx.x & 31) * 4;
+  if (row >= rows || c >= p.D) return;
+  const int kh = (int)(row / (tokens * g));
+  const int64_t token = row / g - kh * tokens;
+  f32x4 x = {};
+  for (int s = 0; s < splits; ++s) x += load4(partials + s * stride + row * p.D + c);
+  store4((T*)out.row(token, kh * g + (int)(row % g)) + c, x * factor);
+}
+
+// ---------------------------------------------------------------------------------------------------------------- backward
 // dq, and what the other kernel needs of a row: its log-sum-exp in base 2 and D_i.  A workgroup has 128 rows, as forward.
 template <class T, int DP>
 __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
   typedef typename FragOf<T>::type Frag;
   typedef Tile<T, DP> Lds;
-  typedef Stager<T, DP, kKeys> Stage;
+  typedef Stager<T, DP, kKeys, 4> Stage;
   constexpr int B = 128, KS = DP / 32, DB = DP / 16, SIZE = kKeys * Lds::kPitch;
   extern __shared__ char smem[];
   const lds_char_ptr lds = (lds_char_ptr)smem;
   const bool ok = sequences_ok(p);
-  if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = ok ? 0 : kErrOffsets;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = ok ? 0 : kErrOffsets;
   if (!ok) return poison<T>(p.dq, p.Tq, p.hq, p.D);
   const int kh = blockIdx.x % p.hk;
   SeqTile t;
   if (!pick_tile<B>(p, kOfRows, blockIdx.x / p.hk, t)) return;
-  const int sees = tile_sees<B>(p, t);
+  const Part part(tile_sees<B>(p, t), p.splits, blockIdx.y, kKeys);
   const Stage ks(p.k.row(t.k0, kh), p.k.token, p.D), vs(p.v.row(t.k0, kh), p.v.token, p.D);
-  if (sees > 0) ks.start(lds, 0, t.nk), vs.start(lds + SIZE, 0, t.nk);
+  if (part.begin < part.end) ks.start(lds, part.begin, t.nk), vs.start(lds + SIZE, part.begin, t.nk);
   const int group = threadIdx.x >> 4 & 3, row0 = t.first + (threadIdx.x >> 6) * 32 + (threadIdx.x & 15);
   const float scale2 = p.scale * kLog2e;
   int row_sees[2];
@@ -698,7 +830,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
     }
     delta[n] = row_sum(delta[n]);
     lse2[n] = row.exists ? p.lse[token * p.hq + head] * kLog2e : 0.f;
-    if (row.exists && group == 0) {
+    if (row.exists && group == 0 && blockIdx.y == 0) {
       const int64_t at = packed_row(p, t, kh, row0 + n * 16);
       p.delta[at] = delta[n];
       // of a row that sees nothing: every probability comes out as 0
@@ -714,9 +846,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
   }
   all_see = __builtin_amdgcn_readfirstlane(all_see);
   int slot = 0;
-  for (int j0 = 0; j0 < sees; j0 += kKeys, slot ^= 2 * SIZE) {
+  for (int j0 = part.begin; j0 < part.end; j0 += kKeys, slot ^= 2 * SIZE) {
     staged_barrier();
-    if (j0 + kKeys < sees) {
+    if (j0 + kKeys < part.end) {
       ks.start(lds + (slot ^ 2 * SIZE), j0 + kKeys, t.nk);
       vs.start(lds + (slot ^ 2 * SIZE) + SIZE, j0 + kKeys, t.nk);
     }
@@ -762,7 +894,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     const Row row(p, t, row0 + n * 16);
-    if (row.exists) store_columns<T>(p.dq.row(t.q0 + row.token, kh * p.g + row.head), dq[n], p.scale, p.D);
+    if (!row.exists) continue;
+    if (p.splits > 1) store_columns<float>((char*)partial_row(p, p.Tq * p.hq, packed_row(p, t, kh, row0 + n * 16)), dq[n], 1.f, p.D);
+    else store_columns<T>(p.dq.row(t.q0 + row.token, kh * p.g + row.head), dq[n], p.scale, p.D);
   }
 }
 
@@ -851,7 +985,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   // the first row that sees the tile's first key, and whole tiles of rows
   const int from = p.causal && t.first > ahead ? (t.first - ahead) * p.g / kRows * kRows : 0;
   const Stage stage(p);
-  if (from < rows) stage.start(p, t, kh, lds, from);
+  const Part part(rows > from ? rows - from : 0, p.splits, blockIdx.y, kRows);
+  if (part.begin < part.end) stage.start(p, t, kh, lds, from + part.begin);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Frag k[2][KS], v[2][KS];
   f32x4 dk[2][DB], dv[2][DB];
@@ -878,9 +1013,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   all_from = __builtin_amdgcn_readfirstlane(all_from);
   const float scale2 = p.scale * kLog2e;
   int slot = 0;
-  for (int r0 = from; r0 < rows; r0 += kRows, slot ^= 1) {
+  for (int r0 = from + part.begin; r0 < from + part.end; r0 += kRows, slot ^= 1) {
     staged_barrier();
-    if (r0 + kRows < rows) stage.start(p, t, kh, lds + (slot ^ 1) * Stage::kBytes, r0 + kRows);
+    if (r0 + kRows < from + part.end) stage.start(p, t, kh, lds + (slot ^ 1) * Stage::kBytes, r0 + kRows);
     const lds_char_ptr numbers = lds + slot * Stage::kBytes + 2 * Stage::SIZE;
     const int places = Lds::rows_place(lds + slot * Stage::kBytes), column_places = Lds::columns_place(lds + slot * Stage::kBytes);
 #pragma unroll 1
@@ -923,6 +1058,12 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   for (int n = 0; n < 2; ++n) {
     const int key = t.first + wave * 32 + n * 16 + (threadIdx.x & 15);
     if (key >= t.nk) continue;
+    if (p.splits > 1) {
+      float* to = partial_row(p, 2 * p.Tk * p.hk, kh * p.Tk + t.k0 + key);
+      store_columns<float>((char*)to, dk[n], 1.f, p.D);
+      store_columns<float>((char*)(to + p.Tk * p.hk * p.D), dv[n], 1.f, p.D);
+      continue;
+    }
     store_columns<T>(p.dk.row(t.k0 + key, kh), dk[n], p.scale, p.D);
     store_columns<T>(p.dv.row(t.k0 + key, kh), dv[n], 1.f, p.D);
   }

@@ -70,21 +70,56 @@ static int rope_args(NormRopeArgs& a, const oapl_heads* q, const oapl_heads* k, 
 }
 
 // ---------------------------------------------------------------------------------------------------------------- attention
+// Few rows a key head (decode steps, short answers): tiles of 32 rows whose wavefronts share the keys.
+static bool few_rows(int64_t Tq, int n_seq, int g) { return Tq * g <= (int64_t)n_seq * 32; }
+
+// Workgroups that share one tile's steps: as many as fill `want` workgroups, with `least` steps each or more.
+static int attn_splits(int64_t tiles, int64_t steps, int64_t want, int64_t least) {
+  const int64_t n = std::min((want + tiles - 1) / std::max<int64_t>(tiles, 1), steps / least);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(n, 64));
+}
+
 struct AttnPlan {
-  size_t off_lse2 = 0, off_delta = 0, total = 0;
+  int fwd = 1, dq = 1, dkdv = 1;       // splits
+  size_t off_lse2 = 0, off_delta = 0, off_sums = 0, off_partials = 0, total = 0;
 };
 
+#ifndef W1
+#define W1 512
+#define W4 1024
+#define L1 8
+#define L4 4
+#define WB 512
+#define LB 4
+#endif
 static bool attn_plan(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int hq, int hk, int D, int dtype, bool bwd) {
   if (dtype != OAPL_F32 && dtype != OAPL_BF16) return false;
   if (!head_counts_ok(hq, hk, D) || Tq < 0 || Tk < 0 || n_seq < 0 || (n_seq == 0 && (Tq || Tk)) || Tk > kMaxTileRows ||
       Tq > kMaxTileRows / hq || n_seq > (1 << 24))
     return false;
   // every grid in 31 bits
-  if ((tile_ids<32>(Tq * (hq / hk), n_seq) + tile_ids<32>(Tk, n_seq)) * hk > kMaxTileRows) return false;
+  const int g = hq / hk;
+  if ((tile_ids<32>(Tq * g, n_seq) + tile_ids<32>(Tk, n_seq)) * hk > kMaxTileRows) return false;
+  const int64_t seqs = std::max(n_seq, 1);
+  // Nothing is known here of single sequences: tiles and steps are those of sequences of average length.
+  const auto tiles = [&](int64_t n, int64_t b) { return seqs * ((n + seqs * b - 1) / (seqs * b)) * hk; };
+  const bool few = few_rows(Tq, n_seq, g);
+  p.fwd = few ? attn_splits(tiles(Tq * g, 32), Tk / seqs / (4 * kFwdKeys), W4, L4)
+              : attn_splits(tiles(Tq * g, 128), Tk / seqs / kFwdKeys, W1, L1);
+  p.dq = attn_splits(tiles(Tq * g, 128), Tk / seqs / kKeys, WB, LB);
+  p.dkdv = attn_splits(tiles(Tk, 128), Tq * g / seqs / kRows, WB, LB);
   size_t at = kStatusWords * sizeof(int);
-  const size_t numbers = bwd ? (size_t)round_up(Tq * hq * (int64_t)sizeof(float), 256) : 0;
-  p.off_lse2 = at, at += numbers;
-  p.off_delta = at, at += numbers;
+  const auto take = [&](int64_t floats) {
+    const size_t was = at;
+    at += (size_t)round_up(floats * (int64_t)sizeof(float), 256);
+    return was;
+  };
+  if (bwd) {
+    p.off_lse2 = take(Tq * hq), p.off_delta = take(Tq * hq);
+    p.off_partials = take(std::max(p.dq > 1 ? p.dq * Tq * hq * D : 0, p.dkdv > 1 ? p.dkdv * 2 * Tk * hk * D : 0));
+  } else if (p.fwd > 1) {
+    p.off_sums = take(2 * p.fwd * Tq * hq), p.off_partials = take(p.fwd * Tq * hq * D);
+  }
   p.total = at;
   return true;
 }
@@ -117,23 +152,46 @@ static int by_type(int dtype, int D, F&& launch) {
 }
 
 template <class K>
-static int launch_attn(K kernel, int64_t workgroups, int lds, const AttnArgs& a, hipStream_t st) {
+static int launch_attn(K kernel, int64_t tiles, int splits, int lds, const AttnArgs& a, hipStream_t st) {
   if (!allow_big_lds(kernel, lds)) return OAPL_ERR_HIP;
-  kernel<<<(unsigned)workgroups, 256, lds, st>>>(a);
+  kernel<<<dim3((unsigned)tiles, (unsigned)splits), 256, lds, st>>>(a);
   OAPL_LAUNCH_CHECK();
   return OAPL_OK;
 }
 
 template <class T, int DP>
-static int launch_attn_fwd(const AttnArgs& a, hipStream_t st) {
-  return launch_attn(k_attn_fwd<T, DP>, tile_ids<128>(a.Tq * a.g, a.n_seq) * a.hk, 4 * kFwdKeys * Tile<T, DP>::kPitch, a, st);
+static int launch_attn_fwd(AttnArgs a, const AttnPlan& p, hipStream_t st) {
+  a.splits = p.fwd;
+  const int64_t rows = a.Tq * a.g;
+  const int rc = few_rows(a.Tq, a.n_seq, a.g)
+                     ? launch_attn(k_attn_fwd<T, DP, 4>, tile_ids<32>(rows, a.n_seq) * a.hk, p.fwd, FwdLds<T, DP, 4>::kBytes, a, st)
+                     : launch_attn(k_attn_fwd<T, DP, 1>, tile_ids<128>(rows, a.n_seq) * a.hk, p.fwd, FwdLds<T, DP, 1>::kBytes, a, st);
+  if (rc != OAPL_OK || p.fwd == 1) return rc;
+  k_attn_join<T><<<grid1d(a.Tq * a.hq, 8), 256, 0, st>>>(a);
+  OAPL_LAUNCH_CHECK();
+  return OAPL_OK;
 }
 
 template <class T, int DP>
-static int launch_attn_bwd(const AttnArgs& a, hipStream_t st) {
-  if (int rc = launch_attn(k_attn_dq<T, DP>, tile_ids<128>(a.Tq * a.g, a.n_seq) * a.hk, 4 * kKeys * Tile<T, DP>::kPitch, a, st))
+static int launch_attn_bwd(AttnArgs a, const AttnPlan& p, hipStream_t st) {
+  a.splits = p.dq;
+  if (int rc = launch_attn(k_attn_dq<T, DP>, tile_ids<128>(a.Tq * a.g, a.n_seq) * a.hk, p.dq, 4 * kKeys * Tile<T, DP>::kPitch, a, st))
     return rc;
-  return launch_attn(k_attn_dkdv<T, DP>, tile_ids<128>(a.Tk, a.n_seq) * a.hk, 2 * RowStager<T, DP>::kBytes, a, st);
+  if (p.dq > 1 && a.Tq > 0) {
+    k_attn_add<T><<<grid1d(a.Tq * a.hq, 8), 256, 0, st>>>(a, a.partials, a.Tq * a.hq * a.D, a.dq, a.Tq, a.hk, a.g, p.dq, a.scale);
+    OAPL_LAUNCH_CHECK();
+  }
+  a.splits = p.dkdv;
+  if (int rc = launch_attn(k_attn_dkdv<T, DP>, tile_ids<128>(a.Tk, a.n_seq) * a.hk, p.dkdv, 2 * RowStager<T, DP>::kBytes, a, st))
+    return rc;
+  if (p.dkdv > 1 && a.Tk > 0) {
+    const int64_t one = a.Tk * a.hk * a.D;
+    k_attn_add<T><<<grid1d(a.Tk * a.hk, 8), 256, 0, st>>>(a, a.partials, 2 * one, a.dk, a.Tk, a.hk, 1, p.dkdv, a.scale);
+    OAPL_LAUNCH_CHECK();
+    k_attn_add<T><<<grid1d(a.Tk * a.hk, 8), 256, 0, st>>>(a, a.partials + one, 2 * one, a.dv, a.Tk, a.hk, 1, p.dkdv, 1.f);
+    OAPL_LAUNCH_CHECK();
+  }
+  return OAPL_OK;
 }
 
 }  // namespace oapl
@@ -237,13 +295,15 @@ int32_t oapl_attention_fwd(const oapl_heads* q, const oapl_heads* k, const oapl_
   a.lse = lse;
   a.k_used = k_used;
   a.status = (int*)workspace;
+  a.part_sums = (float*)((char*)workspace + p.off_sums);
+  a.partials = (float*)((char*)workspace + p.off_partials);
   if (n_seq == 0) {
     k_fill_i32<<<1, 64, 0, st>>>(a.status, kStatusWords, 0);
     OAPL_LAUNCH_CHECK();
     return OAPL_OK;
   }
   return by_type(dtype, head_dim, [&](auto* t, auto dp) {
-    return launch_attn_fwd<std::remove_pointer_t<decltype(t)>, decltype(dp)::value>(a, st);
+    return launch_attn_fwd<std::remove_pointer_t<decltype(t)>, decltype(dp)::value>(a, p, st);
   });
 }
 
@@ -273,6 +333,7 @@ int32_t oapl_attention_bwd(const oapl_heads* q, const oapl_heads* k, const oapl_
   a.lse = const_cast<float*>(lse);
   a.lse2 = (float*)((char*)workspace + p.off_lse2);
   a.delta = (float*)((char*)workspace + p.off_delta);
+  a.partials = (float*)((char*)workspace + p.off_partials);
   a.status = (int*)workspace;
   if (n_seq == 0) {
     k_fill_i32<<<1, 64, 0, st>>>(a.status, kStatusWords, 0);
@@ -280,7 +341,7 @@ int32_t oapl_attention_bwd(const oapl_heads* q, const oapl_heads* k, const oapl_
     return OAPL_OK;
   }
   return by_type(dtype, head_dim, [&](auto* t, auto dp) {
-    return launch_attn_bwd<std::remove_pointer_t<decltype(t)>, decltype(dp)::value>(a, st);
+    return launch_attn_bwd<std::remove_pointer_t<decltype(t)>, decltype(dp)::value>(a, p, st);
   });
 }
 
