@@ -194,13 +194,16 @@ __device__ __forceinline__ void mma0(f32x4& c, const FragF32& a, const FragF32& 
 // The wait states of the slower of the two shapes: one statement that all results go into and come out of.
 template <int N>
 __device__ __forceinline__ void settle(f32x4 (&x)[2][N]) {
-  static_assert(N == 2 || N == 4 || N == 8, "operands are listed");
+  static_assert(N == 2 || N == 4 || N == 6 || N == 8, "operands are listed");
   __builtin_amdgcn_sched_barrier(0);
   if constexpr (N == 2)
     asm volatile("s_nop 7\n\ts_nop 7" : "+v"(x[0][0]), "+v"(x[0][1]), "+v"(x[1][0]), "+v"(x[1][1]));
   else if constexpr (N == 4)
     asm volatile("s_nop 7\n\ts_nop 7" : "+v"(x[0][0]), "+v"(x[0][1]), "+v"(x[0][2]), "+v"(x[0][3]), "+v"(x[1][0]), "+v"(x[1][1]),
                  "+v"(x[1][2]), "+v"(x[1][3]));
+  else if constexpr (N == 6)
+    asm volatile("s_nop 7\n\ts_nop 7" : "+v"(x[0][0]), "+v"(x[0][1]), "+v"(x[0][2]), "+v"(x[0][3]), "+v"(x[0][4]), "+v"(x[0][5]),
+                 "+v"(x[1][0]), "+v"(x[1][1]), "+v"(x[1][2]), "+v"(x[1][3]), "+v"(x[1][4]), "+v"(x[1][5]));
   else
     asm volatile("s_nop 7\n\ts_nop 7" : "+v"(x[0][0]), "+v"(x[0][1]), "+v"(x[0][2]), "+v"(x[0][3]), "+v"(x[0][4]), "+v"(x[0][5]),
                  "+v"(x[0][6]), "+v"(x[0][7]), "+v"(x[1][0]), "+v"(x[1][1]), "+v"(x[1][2]), "+v"(x[1][3]), "+v"(x[1][4]),
@@ -252,6 +255,9 @@ __device__ __forceinline__ int fresh(int x) {
   asm volatile("" : "+v"(x));
   return x;
 }
+
+// Heads of up to DW channels (32, 64, 96, 128) lie in LDS in rows of 64 or 128.
+constexpr int padded(int DW) { return DW <= 64 ? 64 : 128; }
 
 // LDS addresses as numbers.
 __device__ __forceinline__ int lds_place(lds_char_ptr p) { return (int)(uintptr_t)p; }
@@ -450,7 +456,7 @@ __device__ __forceinline__ void scores(f32x4 (&s)[2][2], int place, int off, con
   Frag f[N];
   const auto fetch = [&](int i) { Lds::rows(Lds::flip(place, (i >> 1) * Lds::kRowBits), off + (i & 1) * 16 * Lds::kPitch, f[i]); };
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i) fetch(i);
+  for (int i = 0; i < (AHEAD < N ? AHEAD : N); ++i) fetch(i);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     __builtin_amdgcn_sched_barrier(0);
@@ -468,11 +474,11 @@ __device__ __forceinline__ void scores(f32x4 (&s)[2][2], int place, int off, con
 // acc[n][d] += columns 16 d of 32 rows of a tile, contracted over those rows with w[n].
 template <class Lds, int DB, class Frag, class F>
 __device__ __forceinline__ void add_columns(f32x4 (&acc)[2][DB], int place, int off, const Frag (&w)[2], F&& between) {
-  constexpr int AHEAD = 3;
+  constexpr int AHEAD = 3, N = DB;
   Frag f[DB];
   const auto fetch = [&](int i) { Lds::columns(Lds::flip(place, i * Lds::kColumnBits), off, f[i]); };
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i) fetch(i);
+  for (int i = 0; i < (AHEAD < N ? AHEAD : N); ++i) fetch(i);
 #pragma unroll
   for (int i = 0; i < DB; ++i) {
     __builtin_amdgcn_sched_barrier(0);
@@ -495,7 +501,7 @@ __device__ __forceinline__ void scores2(f32x4 (&s)[2][2], f32x4 (&t)[2][2], int 
     Lds::rows(at, (i >> 1 & 1) * SIZE + (i & 1) * 16 * Lds::kPitch, f[i]);
   };
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i) fetch(i);
+  for (int i = 0; i < (AHEAD < N ? AHEAD : N); ++i) fetch(i);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     __builtin_amdgcn_sched_barrier(0);
@@ -522,7 +528,7 @@ __device__ __forceinline__ void add_columns2(f32x4 (&a)[2][DB], f32x4 (&b)[2][DB
     Lds::columns(at, (i & 1) * SIZE, f[i]);
   };
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i) fetch(i);
+  for (int i = 0; i < (AHEAD < N ? AHEAD : N); ++i) fetch(i);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     __builtin_amdgcn_sched_barrier(0);
@@ -571,13 +577,14 @@ __device__ __forceinline__ float* partial_row(const AttnArgs& p, int64_t rows, i
 // WK = 4, for few rows: the wavefronts have the same 32 rows and take the steps of 32 keys in turn, each through LDS of its own, and
 // join at the end.  That is bound by reading the keys and values.
 // Where tiles are few, their keys are split over workgroups (blockIdx.y) whose results k_attn_join puts together.
-template <class T, int DP, int WK>
+template <class T, int DW, int WK>
 __global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k_attn_fwd(const AttnArgs p) {
+  constexpr int DP = padded(DW);
   typedef typename FragOf<T>::type Frag;
   typedef Tile<T, DP> Lds;
   typedef Stager<T, DP, kFwdKeys, 4 / WK> Stage;
   typedef FwdLds<T, DP, WK> Size;
-  constexpr int B = 128 / WK, KS = DP / 32, DB = DP / 16, SIZE = Size::kTile;
+  constexpr int B = 128 / WK, KS = DW / 32, DB = DW / 16, SIZE = Size::kTile;
   extern __shared__ char smem[];
   const bool ok = sequences_ok(p);
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = ok ? 0 : kErrOffsets;
@@ -716,84 +723,110 @@ __global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k
       }
     }
     __syncthreads();
-    const int r = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * (DP / 8);
+    const int r = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * (DW / 8);
     const Row row(p, t, t.first + r);
     const lds_char_ptr from = (lds_char_ptr)smem + r * PITCH;
     float top = kNegHuge, sum = 0.f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) top = fmaxf(top, *(lds_f32)(from + w * Size::kWave + DP * 4));
-    f32x4 x[DP / 32] = {};
+    f32x4 x[DW / 32] = {};
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
       const float by = __builtin_amdgcn_exp2f(*(lds_f32)(from + w * Size::kWave + DP * 4) - top);
       sum = fmaf(*(lds_f32)(from + w * Size::kWave + DP * 4 + 4), by, sum);
 #pragma unroll
-      for (int c = 0; c < DP / 32; ++c) x[c] += *(lds_f32x4)(from + w * Size::kWave + (c0 + c * 4) * 4) * by;
+      for (int c = 0; c < DW / 32; ++c) x[c] += *(lds_f32x4)(from + w * Size::kWave + (c0 + c * 4) * 4) * by;
     }
     if (!row.exists) return;
     const int head = kh * p.g + row.head;
     if (p.splits > 1) {
       const int64_t at = packed_row(p, t, kh, t.first + r);
 #pragma unroll
-      for (int c = 0; c < DP / 32; ++c)
+      for (int c = 0; c < DW / 32; ++c)
         if (c0 + c * 4 < p.D) store4(partial_row(p, p.Tq * p.hq, at) + c0 + c * 4, x[c]);
       if (c0 == 0) store_sums(p, at, top, sum);
       return;
     }
     T* to = (T*)p.o.row(t.q0 + row.token, head);
 #pragma unroll
-    for (int c = 0; c < DP / 32; ++c)
+    for (int c = 0; c < DW / 32; ++c)
       if (c0 + c * 4 < p.D) store4(to + c0 + c * 4, x[c] * inverse(sum));
     if (p.lse && c0 == 0) p.lse[(t.q0 + row.token) * p.hq + head] = finish(top, sum);
   }
 }
 
-// Puts the splits of a row together: 32 lanes a row, four channels each.
+// Puts the splits of a row together: 32 lanes a row, a lane for each split's numbers (two from 33 splits on), then four channels a lane.
 template <class T>
 __global__ __launch_bounds__(256) void k_attn_join(const AttnArgs p) {
   if (*p.status != 0) return;      // the outputs are NaN already
   const int64_t rows = p.Tq * p.hq, row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (row >= rows) return;
-  const int c = (threadIdx.x & 31) * 4, h = (int)(row % p.g), kh = (int)(row / (p.Tq * p.g));
+  const int lane = threadIdx.x & 31, c = lane * 4, h = (int)(row % p.g), kh = (int)(row / (p.Tq * p.g));
   const int64_t token = row / p.g - kh * p.Tq;
-  const float2* sums = (const float2*)p.part_sums + row;
+  float2 sums[2];
   float top = kNegHuge, sum = 0.f;
-  for (int s = 0; s < p.splits; ++s) top = fmaxf(top, sums[s * rows].x);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int s = lane + i * 32;
+    sums[i] = s < p.splits ? *((const float2*)p.part_sums + s * rows + row) : make_float2(kNegHuge, 0.f);
+    top = fmaxf(top, sums[i].x);
+  }
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 32));
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    sums[i].x = __builtin_amdgcn_exp2f(sums[i].x - top);
+    sum = fmaf(sums[i].x, sums[i].y, sum);
+  }
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor(sum, x, 32);
   f32x4 x = {};
-  for (int s = 0; s < p.splits; ++s) {
-    const float2 y = sums[s * rows];
-    const float by = __builtin_amdgcn_exp2f(y.x - top);
-    sum = fmaf(y.y, by, sum);
-    if (c < p.D) x += load4(p.partials + (s * rows + row) * p.D + c) * by;
+  const float* part = p.partials + row * p.D + (c < p.D ? c : 0);
+  for (int s0 = 0; s0 < p.splits; s0 += 8) {      // eight requests at a time; behind the last split the factors are 0
+    f32x4 y[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) y[s] = load4(part + min(s0 + s, p.splits - 1) * rows * p.D);
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      const float by = __shfl(s0 < 32 ? sums[0].x : sums[1].x, (s0 + s) & 31, 32);
+      x += y[s] * (s0 + s < p.splits ? by : 0.f);
+    }
   }
   const int head = kh * p.g + h;
   if (c < p.D) store4((T*)p.o.row(token, head) + c, x * (sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum));
   if (p.lse && c == 0) p.lse[token * p.hq + head] = sum == 0.f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * kLn2f;
 }
 
-// The sum of gradients' splits times a factor, in their order: out[token][head] from partial[split][head][token][group].
+// A gradient that comes in parts: out[token][head] = factor * sum over splits of partial[split][key head][token][in group], in their order.
+struct GradSum {
+  Heads out;
+  const float* partials;
+  float factor;
+};
 template <class T>
-__global__ __launch_bounds__(256) void k_attn_add(const AttnArgs p, const float* __restrict__ partials, int64_t stride, Heads out, int64_t tokens,
-                                                  int heads, int g, int splits, float factor) {
+__global__ __launch_bounds__(256) void k_attn_add(const AttnArgs p, GradSum first, GradSum second, int64_t stride, int64_t tokens, int g) {
   if (*p.status != 0) return;
-  const int64_t rows = tokens * heads * g, row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const GradSum& grad = blockIdx.y ? second : first;
+  const int64_t rows = tokens * p.hk * g, row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   const int c = (threadIdx.x & 31) * 4;
   if (row >= rows || c >= p.D) return;
   const int kh = (int)(row / (tokens * g));
   const int64_t token = row / g - kh * tokens;
   f32x4 x = {};
-  for (int s = 0; s < splits; ++s) x += load4(partials + s * stride + row * p.D + c);
-  store4((T*)out.row(token, kh * g + (int)(row % g)) + c, x * factor);
+#pragma unroll 8
+  for (int s = 0; s < p.splits; ++s) x += load4(grad.partials + s * stride + row * p.D + c);
+  store4((T*)grad.out.row(token, kh * g + (int)(row % g)) + c, x * grad.factor);
 }
 
 // ---------------------------------------------------------------------------------------------------------------- backward
 // dq, and what the other kernel needs of a row: its log-sum-exp in base 2 and D_i.  A workgroup has 128 rows, as forward.
-template <class T, int DP>
+template <class T, int DW>
 __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
+  constexpr int DP = padded(DW);
   typedef typename FragOf<T>::type Frag;
   typedef Tile<T, DP> Lds;
   typedef Stager<T, DP, kKeys, 4> Stage;
-  constexpr int B = 128, KS = DP / 32, DB = DP / 16, SIZE = kKeys * Lds::kPitch;
+  constexpr int B = 128, KS = DW / 32, DB = DW / 16, SIZE = kKeys * Lds::kPitch;
   extern __shared__ char smem[];
   const lds_char_ptr lds = (lds_char_ptr)smem;
   const bool ok = sequences_ok(p);
@@ -871,22 +904,17 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
       for (int n = 0; n < 2; ++n) pack(s[c][n][0], s[c][n][1], w[c][n]);
       ready(w[c]);
     };
-    constexpr int PER_S = 8 / KS / 2, PER_C = 16 / DB;
+    // the elements [from, to) of half c that go with one of n pairs of multiplications
+    const auto share = [&](int c, int from, int to, int i, int n) {
+#pragma unroll
+      for (int x = from + (to - from) * i / n; x < from + (to - from) * (i + 1) / n; ++x) finish(c, x);
+    };
     scores<Lds, KS>(s[0], k_rows, 0, q, [](int) {});
     scores<Lds, KS>(dp[0], k_rows, SIZE, dout, [](int) {});
-    scores<Lds, KS>(s[1], k_rows, 32 * Lds::kPitch, q, [&](int i) {
-#pragma unroll
-      for (int x = 0; x < PER_S; ++x) finish(0, i * PER_S + x);
-    });
-    scores<Lds, KS>(dp[1], k_rows, SIZE + 32 * Lds::kPitch, dout, [&](int i) {
-#pragma unroll
-      for (int x = 0; x < PER_S; ++x) finish(0, 8 + i * PER_S + x);
-    });
+    scores<Lds, KS>(s[1], k_rows, 32 * Lds::kPitch, q, [&](int i) { share(0, 0, 8, i, 2 * KS); });
+    scores<Lds, KS>(dp[1], k_rows, SIZE + 32 * Lds::kPitch, dout, [&](int i) { share(0, 8, 16, i, 2 * KS); });
     mask(0);
-    add_columns<Lds, DB>(dq, k_columns, 0, w[0], [&](int i) {
-#pragma unroll
-      for (int x = 0; x < PER_C; ++x) finish(1, i * PER_C + x);
-    });
+    add_columns<Lds, DB>(dq, k_columns, 0, w[0], [&](int i) { share(1, 0, 16, i, DB); });
     mask(1);
     add_columns<Lds, DB>(dq, k_columns, 32 * Lds::kPitch, w[1], [](int) {});
   }
@@ -966,12 +994,13 @@ struct RowStager {
 };
 
 // dk and dv: a workgroup has 128 keys, 32 a wavefront, over all rows that see any of them, 64 at a time.
-template <class T, int DP>
+template <class T, int DW>
 __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
+  constexpr int DP = padded(DW);
   typedef typename FragOf<T>::type Frag;
   typedef Tile<T, DP> Lds;
   typedef RowStager<T, DP> Stage;
-  constexpr int B = 128, KS = DP / 32, DB = DP / 16;
+  constexpr int B = 128, KS = DW / 32, DB = DW / 16;
   extern __shared__ char smem[];
   const lds_char_ptr lds = (lds_char_ptr)smem;
   if (!sequences_ok(p)) {

@@ -70,28 +70,41 @@ static int rope_args(NormRopeArgs& a, const oapl_heads* q, const oapl_heads* k, 
 }
 
 // ---------------------------------------------------------------------------------------------------------------- attention
-// Few rows a key head (decode steps, short answers): tiles of 32 rows whose wavefronts share the keys.
-static bool few_rows(int64_t Tq, int n_seq, int g) { return Tq * g <= (int64_t)n_seq * 32; }
-
-// Workgroups that share one tile's steps: as many as fill `want` workgroups, with `least` steps each or more.
-static int attn_splits(int64_t tiles, int64_t steps, int64_t want, int64_t least) {
-  const int64_t n = std::min((want + tiles - 1) / std::max<int64_t>(tiles, 1), steps / least);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(n, 64));
-}
-
+// What a call of average sequences is cut into; nothing more is known here of them.  Microseconds below: bf16, 128 channels, equal lengths,
+// as replayed graphs on one MI355X.
 struct AttnPlan {
-  int fwd = 1, dq = 1, dkdv = 1;       // splits
+  bool few = false;                    // tiles of 32 rows whose wavefronts share the keys
+  int fwd = 1, dq = 1, dkdv = 1;       // workgroups that share a tile's steps
   size_t off_lse2 = 0, off_delta = 0, off_sums = 0, off_partials = 0, total = 0;
 };
 
-#ifndef W1
-#define W1 512
-#define W4 1024
-#define L1 8
-#define L4 4
-#define WB 512
-#define LB 4
-#endif
+// At most `want` workgroups in all, with at least `least` steps each.
+static int attn_splits(int64_t want, int64_t steps, int64_t least) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>({want, steps / least, 64}));
+}
+
+static void attn_cut(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int g, int hk) {
+  const int64_t seqs = std::max(n_seq, 1), rows = Tq * g;
+  const auto tiles = [&](int64_t n, int64_t b) { return std::max<int64_t>(1, (n + seqs * b - 1) / (seqs * b)) * seqs * hk; };
+  // Tiles of 32 rows: for few rows, and where they are one round of workgroups (160 KB of LDS: one a compute unit) however many.
+  // 32 rows / 128 rows a tile: 16 sequences of 64 rows over 2000 keys, 8 key heads (256 small tiles) 29 / 34 (at its best split), of 96 rows
+  // (384) 51 / 42; one sequence of 1000 tokens, 8 heads on one (250) 11 / 19, 6 on 6 (192) 11 / 17, 32 on 8 (1000) 42 / 35.
+  p.few = rows <= seqs * 32 || tiles(rows, 32) <= 256;
+  // ... their keys in parts that fill that round: one token over 4096 / 32768 keys, 8 key heads, in 1 part 33 / 216, 8 parts 14 / 38, 16
+  // parts 13 / 31; 8 over 32768, 1 part 388, 4 181, 8 185; 24 over 4096 (192 tiles), 1 part 85, 2 96.  Short parts cost more to
+  // put together than they save: 4 x 32 rows over 2000 keys, 4 parts 16, 8 parts (of two steps) 21.
+  // Tiles of 128 rows: where few tiles have long walks.  8000 tokens, 4 heads on one (250 tiles of 250 steps), 1 part 190, 4 110; 1000
+  // tokens, 32 on 8 (256 of 31), 1 part 35, 2 41.
+  p.fwd = p.few ? attn_splits(256 / tiles(rows, 32), Tk / seqs / (4 * kFwdKeys), 3)
+                : attn_splits(1024 / tiles(rows, 128), Tk / seqs / kFwdKeys, 32);
+  // dq: parts of keys are rarely worth their sums.  One sequence of 1000 tokens, 6 heads (48 tiles of 15 steps), 1 part 59, 3 50 with
+  // dk, dv; 300 tokens, 32 on 8 (80 of 4), 1 part 70, 2 74.
+  p.dq = attn_splits(192 / tiles(rows, 128), Tk / seqs / kKeys, 4);
+  // dk, dv: two workgroups a compute unit, walks over the rows of all heads of a group.  300 tokens, 32 on 8 (24 tiles of 18 steps), 1
+  // part 70, 4 50, 8 49; 2500 (160 of 156), 1 part 424, 4 231, 8 247; 4000, 8 on one (32 of 500), 1 part 1151, 8 261, 16 224.
+  p.dkdv = attn_splits((511 + tiles(Tk, 128)) / tiles(Tk, 128), rows / seqs / kRows, 4);
+}
+
 static bool attn_plan(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int hq, int hk, int D, int dtype, bool bwd) {
   if (dtype != OAPL_F32 && dtype != OAPL_BF16) return false;
   if (!head_counts_ok(hq, hk, D) || Tq < 0 || Tk < 0 || n_seq < 0 || (n_seq == 0 && (Tq || Tk)) || Tk > kMaxTileRows ||
@@ -100,14 +113,7 @@ static bool attn_plan(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int hq, in
   // every grid in 31 bits
   const int g = hq / hk;
   if ((tile_ids<32>(Tq * g, n_seq) + tile_ids<32>(Tk, n_seq)) * hk > kMaxTileRows) return false;
-  const int64_t seqs = std::max(n_seq, 1);
-  // Nothing is known here of single sequences: tiles and steps are those of sequences of average length.
-  const auto tiles = [&](int64_t n, int64_t b) { return seqs * ((n + seqs * b - 1) / (seqs * b)) * hk; };
-  const bool few = few_rows(Tq, n_seq, g);
-  p.fwd = few ? attn_splits(tiles(Tq * g, 32), Tk / seqs / (4 * kFwdKeys), W4, L4)
-              : attn_splits(tiles(Tq * g, 128), Tk / seqs / kFwdKeys, W1, L1);
-  p.dq = attn_splits(tiles(Tq * g, 128), Tk / seqs / kKeys, WB, LB);
-  p.dkdv = attn_splits(tiles(Tk, 128), Tq * g / seqs / kRows, WB, LB);
+  attn_cut(p, Tq, Tk, n_seq, g, hk);
   size_t at = kStatusWords * sizeof(int);
   const auto take = [&](int64_t floats) {
     const size_t was = at;
@@ -144,51 +150,58 @@ static int attn_args(AttnArgs& a, const oapl_heads* q, const oapl_heads* k, cons
   return OAPL_OK;
 }
 
-// Head widths up to 64 and up to 128 have kernels of their own; channels behind D are zeros.
+// Heads of up to 32, 64, 96 and 128 channels have kernels of their own; channels behind D are zeros.
+template <class T, class F>
+static int by_width(int D, F&& launch) {
+  if (D <= 32) return launch((T*)nullptr, std::integral_constant<int, 32>{});
+  if (D <= 64) return launch((T*)nullptr, std::integral_constant<int, 64>{});
+  if (D <= 96) return launch((T*)nullptr, std::integral_constant<int, 96>{});
+  return launch((T*)nullptr, std::integral_constant<int, 128>{});
+}
 template <class F>
 static int by_type(int dtype, int D, F&& launch) {
-  if (dtype == OAPL_BF16) return D <= 64 ? launch((bf16_t*)nullptr, std::integral_constant<int, 64>{}) : launch((bf16_t*)nullptr, std::integral_constant<int, 128>{});
-  return D <= 64 ? launch((float*)nullptr, std::integral_constant<int, 64>{}) : launch((float*)nullptr, std::integral_constant<int, 128>{});
+  return dtype == OAPL_BF16 ? by_width<bf16_t>(D, launch) : by_width<float>(D, launch);
 }
 
-template <class K>
-static int launch_attn(K kernel, int64_t tiles, int splits, int lds, const AttnArgs& a, hipStream_t st) {
-  if (!allow_big_lds(kernel, lds)) return OAPL_ERR_HIP;
+template <auto kernel, int lds>
+static int launch_attn(int64_t tiles, int splits, const AttnArgs& a, hipStream_t st) {
+  static const bool ready = allow_big_lds(kernel, lds);
+  if (!ready) return OAPL_ERR_HIP;
   kernel<<<dim3((unsigned)tiles, (unsigned)splits), 256, lds, st>>>(a);
   OAPL_LAUNCH_CHECK();
   return OAPL_OK;
 }
 
-template <class T, int DP>
+template <class T, int DW>
 static int launch_attn_fwd(AttnArgs a, const AttnPlan& p, hipStream_t st) {
   a.splits = p.fwd;
   const int64_t rows = a.Tq * a.g;
-  const int rc = few_rows(a.Tq, a.n_seq, a.g)
-                     ? launch_attn(k_attn_fwd<T, DP, 4>, tile_ids<32>(rows, a.n_seq) * a.hk, p.fwd, FwdLds<T, DP, 4>::kBytes, a, st)
-                     : launch_attn(k_attn_fwd<T, DP, 1>, tile_ids<128>(rows, a.n_seq) * a.hk, p.fwd, FwdLds<T, DP, 1>::kBytes, a, st);
-  if (rc != OAPL_OK || p.fwd == 1) return rc;
+  constexpr int DP = padded(DW);
+  const int rc = p.few ? launch_attn<k_attn_fwd<T, DW, 4>, FwdLds<T, DP, 4>::kBytes>(tile_ids<32>(rows, a.n_seq) * a.hk, p.fwd, a, st)
+                       : launch_attn<k_attn_fwd<T, DW, 1>, FwdLds<T, DP, 1>::kBytes>(tile_ids<128>(rows, a.n_seq) * a.hk, p.fwd, a, st);
+  if (rc != OAPL_OK || p.fwd == 1 || a.Tq == 0) return rc;
   k_attn_join<T><<<grid1d(a.Tq * a.hq, 8), 256, 0, st>>>(a);
   OAPL_LAUNCH_CHECK();
   return OAPL_OK;
 }
 
-template <class T, int DP>
+template <class T, int DW>
 static int launch_attn_bwd(AttnArgs a, const AttnPlan& p, hipStream_t st) {
+  constexpr int DP = padded(DW);
   a.splits = p.dq;
-  if (int rc = launch_attn(k_attn_dq<T, DP>, tile_ids<128>(a.Tq * a.g, a.n_seq) * a.hk, p.dq, 4 * kKeys * Tile<T, DP>::kPitch, a, st))
+  if (int rc = launch_attn<k_attn_dq<T, DW>, 4 * kKeys * Tile<T, DP>::kPitch>(tile_ids<128>(a.Tq * a.g, a.n_seq) * a.hk, p.dq, a, st))
     return rc;
   if (p.dq > 1 && a.Tq > 0) {
-    k_attn_add<T><<<grid1d(a.Tq * a.hq, 8), 256, 0, st>>>(a, a.partials, a.Tq * a.hq * a.D, a.dq, a.Tq, a.hk, a.g, p.dq, a.scale);
+    const GradSum dq{a.dq, a.partials, a.scale};
+    k_attn_add<T><<<grid1d(a.Tq * a.hq, 8), 256, 0, st>>>(a, dq, dq, a.Tq * a.hq * a.D, a.Tq, a.g);
     OAPL_LAUNCH_CHECK();
   }
   a.splits = p.dkdv;
-  if (int rc = launch_attn(k_attn_dkdv<T, DP>, tile_ids<128>(a.Tk, a.n_seq) * a.hk, p.dkdv, 2 * RowStager<T, DP>::kBytes, a, st))
-    return rc;
+  if (int rc = launch_attn<k_attn_dkdv<T, DW>, 2 * RowStager<T, DP>::kBytes>(tile_ids<128>(a.Tk, a.n_seq) * a.hk, p.dkdv, a, st)) return rc;
   if (p.dkdv > 1 && a.Tk > 0) {
     const int64_t one = a.Tk * a.hk * a.D;
-    k_attn_add<T><<<grid1d(a.Tk * a.hk, 8), 256, 0, st>>>(a, a.partials, 2 * one, a.dk, a.Tk, a.hk, 1, p.dkdv, a.scale);
-    OAPL_LAUNCH_CHECK();
-    k_attn_add<T><<<grid1d(a.Tk * a.hk, 8), 256, 0, st>>>(a, a.partials + one, 2 * one, a.dv, a.Tk, a.hk, 1, p.dkdv, 1.f);
+    const GradSum dk{a.dk, a.partials, a.scale}, dv{a.dv, a.partials + one, 1.f};
+    k_attn_add<T><<<dim3(grid1d(a.Tk * a.hk, 8), 2), 256, 0, st>>>(a, dk, dv, 2 * one, a.Tk, 1);
     OAPL_LAUNCH_CHECK();
   }
   return OAPL_OK;

@@ -136,6 +136,10 @@ def _stream(device) -> int:
     return torch.cuda.current_stream(device).cuda_stream
 
 
+# The same number without a stream object around it, where this torch has it (2 us less on calls that take 10).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: _stream(torch.device("cuda", index)))
+
+
 def workspace_bytes(T: int, d: int, V: int, n_seq: int, n_groups: int, dtype: int, with_backward: bool,
                     max_panel_rows: Optional[int] = None, max_rollout_len: Optional[int] = None) -> int:
     """oapl_workspace_bytes, or oapl_workspace_bytes_for when a panel cap or a rollout length is given."""
@@ -396,24 +400,58 @@ def grpo_loss_fwd_bwd(H, W, tokens, logq, logp_old, seq_offsets, rewards, group_
     return GrpoResult(loss, logprob, adv, dH, dW, ws)
 
 
-def _heads(t: torch.Tensor, name: str, shape, like: torch.Tensor) -> Heads:
-    """The oapl_heads of a tensor [tokens, heads, channels] whose channels lie side by side."""
-    if t.device != like.device:
-        raise ValueError(f"{name} must live on {like.device}")
-    if t.dtype != like.dtype:
-        raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
-    if t.dim() != 3 or tuple(t.shape) != tuple(shape):
+def _heads(t: torch.Tensor, name: str, shape, dtype: torch.dtype, index: int) -> Heads:
+    """The oapl_heads of a tensor [tokens, heads, channels] on GPU `index` whose channels lie side by side."""
+    if t.get_device() != index:
+        raise ValueError(f"{name} must live on cuda:{index}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
         raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.stride(2) != 1 and t.numel() > 0:
+    token, head, channel = t.stride()
+    if channel != 1 and t.numel() > 0:
         raise ValueError(f"the channels of {name} must lie side by side")
-    return Heads(t.data_ptr(), t.stride(0), t.stride(1))
+    return Heads(t.data_ptr(), token, head)
 
 
-def _qk_shapes(q: torch.Tensor, k: torch.Tensor):
-    _check_device(q)
-    _dtype_code(q)
+def _flat(t: Optional[torch.Tensor], dtype: torch.dtype, name: str, index: int) -> Optional[int]:
+    """As _dev, for calls where its microseconds count."""
+    if t is None:
+        return None
+    if t.get_device() != index:
+        raise ValueError(f"{name} must live on cuda:{index}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _scratch(nbytes: int, like: torch.Tensor, workspace: Optional[torch.Tensor], where: str) -> torch.Tensor:
+    if nbytes == 0:
+        raise OaplError(2, where)
+    if workspace is None:
+        return like.new_empty(nbytes, dtype=torch.uint8)
+    return _workspace(nbytes, like.device, workspace)
+
+
+def _qk_setup(q: torch.Tensor, k: torch.Tensor):
+    """(tokens, heads, channels of q, heads of k, dtype code, GPU)."""
+    index = q.get_device()
+    if index < 0 or index != torch.cuda.current_device():
+        _check_device(q)
+    dt = _dtype_code(q)
     if q.dim() != 3 or k.dim() != 3 or q.shape[2] != k.shape[2]:
         raise ValueError("q and k must be [tokens, heads, channels] with the same channels")
+    T, hq, D = q.shape
+    return T, hq, D, k.shape[1], dt, index
+
+
+def _check_rope(T, D, positions, cos_sin, q_gain, k_gain):
+    if positions.shape != (T,) or cos_sin.dim() != 2:
+        raise ValueError("shape mismatch between q, positions and cos_sin")
+    if (q_gain is None) != (k_gain is None) or (q_gain is not None and (q_gain.shape != (D,) or k_gain.shape != (D,))):
+        raise ValueError("q_gain and k_gain come as a pair, one value a channel")
 
 
 class NormRopeResult(NamedTuple):
@@ -432,24 +470,24 @@ def qk_norm_rope_fwd(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, 
     q, k (and v) may be views into one projection's output.  With `rows`, keys (and values) go to those rows of the caches
     k_out (and v_out); without, k_out defaults to a new tensor.
     """
-    _qk_shapes(q, k)
-    (T, hq, D), hk, dev = q.shape, k.shape[1], q.device
-    if positions.shape != (T,) or cos_sin.dim() != 2 or (rows is not None and rows.shape != (T,)):
-        raise ValueError("shape mismatch between q, positions, cos_sin and rows")
-    if (q_gain is None) != (k_gain is None) or (q_gain is not None and (q_gain.shape != (D,) or k_gain.shape != (D,))):
-        raise ValueError("q_gain and k_gain come as a pair, one value a channel")
+    T, hq, D, hk, dt, gpu = _qk_setup(q, k)
+    _check_rope(T, D, positions, cos_sin, q_gain, k_gain)
+    if rows is not None and rows.shape != (T,):
+        raise ValueError("rows must have one entry a token")
     if (v is None) != (v_out is None) or (rows is not None and k_out is None):
         raise ValueError("rows need a cache k_out, values a cache v_out")
-    q_out = torch.empty((T, hq, D), dtype=q.dtype, device=dev) if q_out is None else q_out
-    k_out = torch.empty((T, hk, D), dtype=q.dtype, device=dev) if k_out is None else k_out
+    kind, q_shape, k_shape = q.dtype, q.shape, (T, hk, D)
+    q_out = q.new_empty(q_shape) if q_out is None else q_out
+    k_out = q.new_empty(k_shape) if k_out is None else k_out
     n_rows = T if rows is None else k_out.shape[0]
+    out_shape = (n_rows, hk, D)
     rc = lib().oapl_qk_norm_rope_fwd(
-        _heads(q, "q", (T, hq, D), q), _heads(k, "k", (T, hk, D), q), None if v is None else _heads(v, "v", (T, hk, D), q),
-        _dev(positions, torch.int32, "positions", dev), _dev(cos_sin, torch.float32, "cos_sin", dev),
-        _dev(q_gain, q.dtype, "q_gain", dev), _dev(k_gain, q.dtype, "k_gain", dev), _dev(rows, torch.int64, "rows", dev),
-        T, hq, hk, D, cos_sin.shape[1], cos_sin.shape[0], n_rows, _dtype_code(q), float(eps),
-        _heads(q_out, "q_out", (T, hq, D), q), _heads(k_out, "k_out", (n_rows, hk, D), q),
-        None if v is None else _heads(v_out, "v_out", (n_rows, hk, D), q), _stream(dev))
+        _heads(q, "q", q_shape, kind, gpu), _heads(k, "k", k_shape, kind, gpu),
+        None if v is None else _heads(v, "v", k_shape, kind, gpu), _flat(positions, torch.int32, "positions", gpu),
+        _flat(cos_sin, torch.float32, "cos_sin", gpu), _flat(q_gain, kind, "q_gain", gpu), _flat(k_gain, kind, "k_gain", gpu),
+        _flat(rows, torch.int64, "rows", gpu), T, hq, hk, D, cos_sin.shape[1], cos_sin.shape[0], n_rows, dt, eps,
+        _heads(q_out, "q_out", q_shape, kind, gpu), _heads(k_out, "k_out", out_shape, kind, gpu),
+        None if v is None else _heads(v_out, "v_out", out_shape, kind, gpu), _raw_stream(gpu))
     if rc != 0:
         raise OaplError(rc, "oapl_qk_norm_rope_fwd")
     return NormRopeResult(q_out, k_out, v_out)
@@ -468,32 +506,26 @@ def qk_norm_rope_bwd(q: torch.Tensor, k: torch.Tensor, dq_out: torch.Tensor, dk_
                      eps: float = 1e-6, dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
                      workspace: Optional[torch.Tensor] = None) -> NormRopeGrads:
     """oapl_qk_norm_rope_bwd: gradients of the inputs (q, k) and of the gains, from those of the outputs."""
-    _qk_shapes(q, k)
-    (T, hq, D), hk, dev = q.shape, k.shape[1], q.device
-    if positions.shape != (T,) or cos_sin.dim() != 2:
-        raise ValueError("shape mismatch between q, positions and cos_sin")
-    if (q_gain is None) != (k_gain is None) or (q_gain is not None and (q_gain.shape != (D,) or k_gain.shape != (D,))):
-        raise ValueError("q_gain and k_gain come as a pair, one value a channel")
-    dq = torch.empty((T, hq, D), dtype=q.dtype, device=dev) if dq is None else dq
-    dk = torch.empty((T, hk, D), dtype=q.dtype, device=dev) if dk is None else dk
-    gains = ws = None
+    T, hq, D, hk, dt, gpu = _qk_setup(q, k)
+    _check_rope(T, D, positions, cos_sin, q_gain, k_gain)
+    kind, q_shape, k_shape = q.dtype, q.shape, (T, hk, D)
+    dq = q.new_empty(q_shape) if dq is None else dq
+    dk = q.new_empty(k_shape) if dk is None else dk
+    gains, ws, at = (None, None), None, 0
     if q_gain is not None:
-        nbytes = lib().oapl_qk_norm_rope_workspace_bytes(T, hq, hk, D)
-        if nbytes == 0:
-            raise OaplError(2, "oapl_qk_norm_rope_workspace_bytes")
-        ws = _workspace(nbytes, dev, workspace)
-        gains = torch.empty((2, D), dtype=torch.float32, device=dev)
+        ws = _scratch(lib().oapl_qk_norm_rope_workspace_bytes(T, hq, hk, D), q, workspace, "oapl_qk_norm_rope_workspace_bytes")
+        both = q.new_empty((2, D), dtype=torch.float32)
+        gains, at = both.unbind(), both.data_ptr()
     rc = lib().oapl_qk_norm_rope_bwd(
-        _heads(q, "q", (T, hq, D), q), _heads(k, "k", (T, hk, D), q), _heads(dq_out, "dq_out", (T, hq, D), q),
-        _heads(dk_out, "dk_out", (T, hk, D), q), _dev(positions, torch.int32, "positions", dev),
-        _dev(cos_sin, torch.float32, "cos_sin", dev), _dev(q_gain, q.dtype, "q_gain", dev), _dev(k_gain, q.dtype, "k_gain", dev),
-        T, hq, hk, D, cos_sin.shape[1], cos_sin.shape[0], _dtype_code(q), float(eps), _heads(dq, "dq", (T, hq, D), q),
-        _heads(dk, "dk", (T, hk, D), q), None if gains is None else gains[0].data_ptr(),
-        None if gains is None else gains[1].data_ptr(), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
-        _stream(dev))
+        _heads(q, "q", q_shape, kind, gpu), _heads(k, "k", k_shape, kind, gpu), _heads(dq_out, "dq_out", q_shape, kind, gpu),
+        _heads(dk_out, "dk_out", k_shape, kind, gpu), _flat(positions, torch.int32, "positions", gpu),
+        _flat(cos_sin, torch.float32, "cos_sin", gpu), _flat(q_gain, kind, "q_gain", gpu), _flat(k_gain, kind, "k_gain", gpu),
+        T, hq, hk, D, cos_sin.shape[1], cos_sin.shape[0], dt, eps, _heads(dq, "dq", q_shape, kind, gpu),
+        _heads(dk, "dk", k_shape, kind, gpu), at or None, at + 4 * D if at else None, None if ws is None else ws.data_ptr(),
+        0 if ws is None else ws.numel(), _raw_stream(gpu))
     if rc != 0:
         raise OaplError(rc, "oapl_qk_norm_rope_bwd")
-    return NormRopeGrads(dq, dk, None if gains is None else gains[0], None if gains is None else gains[1], ws)
+    return NormRopeGrads(dq, dk, gains[0], gains[1], ws)
 
 
 def attention_workspace_bytes(Tq: int, Tk: int, n_seq: int, n_q_heads: int, n_k_heads: int, head_dim: int, dtype: int,
@@ -504,20 +536,16 @@ def attention_workspace_bytes(Tq: int, Tk: int, n_seq: int, n_q_heads: int, n_k_
 
 
 def _attention_setup(q, k, v, q_offsets, k_offsets, scale, with_backward, workspace):
-    _qk_shapes(q, k)
-    (Tq, hq, D), (Tk, hk, _) = q.shape, k.shape
+    """What both attention calls check and pass on: heads, offsets, sizes, the scale, the workspace, the GPU."""
+    Tq, hq, D, hk, dt, gpu = _qk_setup(q, k)
     k_offsets = q_offsets if k_offsets is None else k_offsets
     if q_offsets.dim() != 1 or q_offsets.shape[0] < 1 or k_offsets.shape != q_offsets.shape:
         raise ValueError("q_offsets and k_offsets must have one entry more than there are sequences")
-    n_seq = q_offsets.shape[0] - 1
-    nbytes = attention_workspace_bytes(Tq, Tk, n_seq, hq, hk, D, _dtype_code(q), with_backward)
-    if nbytes == 0:
-        raise OaplError(2, "oapl_attention_workspace_bytes")
-    ws = _workspace(nbytes, q.device, workspace)
-    heads = [_heads(q, "q", (Tq, hq, D), q), _heads(k, "k", (Tk, hk, D), q), _heads(v, "v", (Tk, hk, D), q)]
-    offsets = [_dev(q_offsets, torch.int64, "q_offsets", q.device), _dev(k_offsets, torch.int64, "k_offsets", q.device)]
-    sizes = [Tq, Tk, n_seq, hq, hk, D, _dtype_code(q)]
-    return heads, offsets, sizes, float(D ** -0.5 if scale is None else scale), ws
+    sizes = (Tq, k.shape[0], q_offsets.shape[0] - 1, hq, hk, D, dt)
+    ws = _scratch(lib().oapl_attention_workspace_bytes(*sizes, with_backward), q, workspace, "oapl_attention_workspace_bytes")
+    heads = (_heads(q, "q", q.shape, q.dtype, gpu), _heads(k, "k", k.shape, q.dtype, gpu), _heads(v, "v", k.shape, q.dtype, gpu))
+    offsets = (_flat(q_offsets, torch.int64, "q_offsets", gpu), _flat(k_offsets, torch.int64, "k_offsets", gpu))
+    return heads, offsets, sizes, D ** -0.5 if scale is None else scale, ws, gpu
 
 
 class AttentionResult(NamedTuple):
@@ -534,14 +562,14 @@ def attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: 
 
     k_offsets defaults to q_offsets, scale to 1 / sqrt(D).
     """
-    heads, offsets, sizes, scale, ws = _attention_setup(q, k, v, q_offsets, k_offsets, scale, False, workspace)
+    heads, offsets, sizes, scale, ws, gpu = _attention_setup(q, k, v, q_offsets, k_offsets, scale, 0, workspace)
     if k_used is not None and k_used.shape != (sizes[2],):
         raise ValueError("k_used must have one entry a sequence")
-    out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
-    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
-    rc = lib().oapl_attention_fwd(*heads, *offsets, _dev(k_used, torch.int64, "k_used", q.device), *sizes, 1 if causal else 0,
-                                  scale, _heads(out, "out", q.shape, q), None if lse is None else lse.data_ptr(), ws.data_ptr(),
-                                  ws.numel(), _stream(q.device))
+    out = q.new_empty(q.shape) if out is None else out
+    lse = q.new_empty(q.shape[:2], dtype=torch.float32) if want_lse else None
+    rc = lib().oapl_attention_fwd(*heads, *offsets, _flat(k_used, torch.int64, "k_used", gpu), *sizes, 1 if causal else 0, scale,
+                                  _heads(out, "out", q.shape, q.dtype, gpu), None if lse is None else lse.data_ptr(),
+                                  ws.data_ptr(), ws.numel(), _raw_stream(gpu))
     if rc != 0:
         raise OaplError(rc, "oapl_attention_fwd")
     return AttentionResult(out, lse, ws)
@@ -559,15 +587,17 @@ def attention_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.
                   scale: Optional[float] = None, dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
                   dv: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> AttentionGrads:
     """oapl_attention_bwd: gradients of q, k and v from attention_fwd's output and log-sum-exp and the output's gradient."""
-    heads, offsets, sizes, scale, ws = _attention_setup(q, k, v, q_offsets, k_offsets, scale, True, workspace)
-    dq, dk, dv = (torch.empty(x.shape, dtype=x.dtype, device=x.device) if g is None else g
-                  for x, g in ((q, dq), (k, dk), (v, dv)))
-    if lse.shape != q.shape[:2]:
+    heads, offsets, sizes, scale, ws, gpu = _attention_setup(q, k, v, q_offsets, k_offsets, scale, 1, workspace)
+    kind, q_shape, k_shape = q.dtype, q.shape, k.shape
+    dq = q.new_empty(q_shape) if dq is None else dq
+    dk = q.new_empty(k_shape) if dk is None else dk
+    dv = q.new_empty(k_shape) if dv is None else dv
+    if lse.shape != q_shape[:2]:
         raise ValueError("lse must be [tokens, heads] of q")
-    rc = lib().oapl_attention_bwd(*heads, _heads(out, "out", q.shape, q), _dev(lse, torch.float32, "lse", q.device),
-                                  _heads(dout, "dout", q.shape, q), *offsets, *sizes, 1 if causal else 0, scale,
-                                  _heads(dq, "dq", q.shape, q), _heads(dk, "dk", k.shape, q), _heads(dv, "dv", k.shape, q),
-                                  ws.data_ptr(), ws.numel(), _stream(q.device))
+    rc = lib().oapl_attention_bwd(*heads, _heads(out, "out", q_shape, kind, gpu), _flat(lse, torch.float32, "lse", gpu),
+                                  _heads(dout, "dout", q_shape, kind, gpu), *offsets, *sizes, 1 if causal else 0, scale,
+                                  _heads(dq, "dq", q_shape, kind, gpu), _heads(dk, "dk", k_shape, kind, gpu),
+                                  _heads(dv, "dv", k_shape, kind, gpu), ws.data_ptr(), ws.numel(), _raw_stream(gpu))
     if rc != 0:
         raise OaplError(rc, "oapl_attention_bwd")
     return AttentionGrads(dq, dk, dv, ws)
