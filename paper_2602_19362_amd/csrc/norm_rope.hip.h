@@ -33,10 +33,12 @@ struct NormRopeArgs {
   float eps;
 };
 
-// Sum over the 16 lanes of a group, in every lane.
+// Sum over the 16 lanes of a group, in every lane: rotations by 8, 4, 2 and 1 of a row of lanes.
 __device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-  for (int o = 8; o > 0; o >>= 1) v += __shfl_xor(v, o, 16);
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xf, 0xf, false));
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x124, 0xf, 0xf, false));
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x122, 0xf, 0xf, false));
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x121, 0xf, 0xf, false));
   return v;
 }
 __device__ __forceinline__ float dot4(f32x4 a, f32x4 b) { return a[0] * b[0] + a[1] * b[1] + a[2] * b[2] + a[3] * b[3]; }
@@ -68,6 +70,10 @@ __device__ __forceinline__ void token_angles(const NormRopeArgs& p, const Pieces
   }
 }
 
+// Heads that a group of lanes has under way together: more bytes in flight.  16411 tokens of 32 + 8 heads of 128 in bf16, 1 / 2 / 3:
+// backwards 113 / 108 / 139 us, forward 71 / 73 / 72.
+constexpr int kRopeHeads = 2;
+
 template <class T>
 __global__ __launch_bounds__(256) void k_qk_norm_rope_fwd(const NormRopeArgs p) {
   const int lane = threadIdx.x & 63, group = lane >> 4;
@@ -85,23 +91,31 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope_fwd(const NormRopeArgs p) 
     gq[0] = load4((const T*)p.q_gain + at.a), gq[1] = load4((const T*)p.q_gain + at.b);
     gk[0] = load4((const T*)p.k_gain + at.a), gk[1] = load4((const T*)p.k_gain + at.b);
   }
-  for (int h = (int)(unit % p.parts) * 4 + group; h < heads; h += p.parts * 4) {
-    const bool query = h < p.hq, value = h >= p.hq + p.hk;
-    const T* x = (const T*)(query ? p.q.row(t, h) : value ? p.v.row(t, h - p.hq - p.hk) : p.k.row(t, h - p.hq));
-    T* y = (T*)(query ? p.q_out.row(t, h) : value ? p.v_out.row(to, h - p.hq - p.hk) : p.k_out.row(to, h - p.hq));
-    f32x4 a = {}, b = {};
-    if (at.any) a = load4(x + at.a), b = load4(x + at.b);
-    if (!value) {
-      if (p.q_gain) {
-        const float r = rsqrtf(group_sum(dot4(a, a) + dot4(b, b)) / (float)p.D + p.eps);
-        a = a * r * (query ? gq[0] : gk[0]);
-        b = b * r * (query ? gq[1] : gk[1]);
-      }
-      const f32x4 turned = a * cos - b * sin;
-      b = b * cos + a * sin;
-      a = turned;
+  const int step = p.parts * 4;
+  for (int h0 = (int)(unit % p.parts) * 4 + group; h0 < heads; h0 += step * kRopeHeads) {
+    f32x4 a[kRopeHeads], b[kRopeHeads];
+#pragma unroll
+    for (int i = 0; i < kRopeHeads; ++i) {
+      const int h = h0 + i * step;
+      a[i] = b[i] = f32x4{};
+      if (h >= heads || !at.any) continue;
+      const T* x = (const T*)(h < p.hq ? p.q.row(t, h) : h < p.hq + p.hk ? p.k.row(t, h - p.hq) : p.v.row(t, h - p.hq - p.hk));
+      a[i] = load4(x + at.a), b[i] = load4(x + at.b);
     }
-    if (at.any && (query || kept)) store4(y + at.a, a), store4(y + at.b, b);
+#pragma unroll
+    for (int i = 0; i < kRopeHeads; ++i) {
+      const int h = h0 + i * step;
+      const bool query = h < p.hq, value = h >= p.hq + p.hk;
+      if (p.q_gain && !value) {
+        const float r = rsqrtf(group_sum(dot4(a[i], a[i]) + dot4(b[i], b[i])) / (float)p.D + p.eps);
+        a[i] = a[i] * r * (query ? gq[0] : gk[0]);
+        b[i] = b[i] * r * (query ? gq[1] : gk[1]);
+      }
+      const f32x4 x = value ? a[i] : a[i] * cos - b[i] * sin, y = value ? b[i] : b[i] * cos + a[i] * sin;
+      if (h >= heads || !at.any || !(query || kept)) continue;
+      T* z = (T*)(query ? p.q_out.row(t, h) : value ? p.v_out.row(to, h - p.hq - p.hk) : p.k_out.row(to, h - p.hq));
+      store4(z + at.a, x), store4(z + at.b, y);
+    }
   }
 }
 
@@ -114,31 +128,42 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope_bwd(const NormRopeArgs p) 
     gq[0] = load4((const T*)p.q_gain + at.a), gq[1] = load4((const T*)p.q_gain + at.b);
     gk[0] = load4((const T*)p.k_gain + at.a), gk[1] = load4((const T*)p.k_gain + at.b);
   }
-  const int heads = p.hq + p.hk;
+  const int heads = p.hq + p.hk, step = p.parts * 4;
   for (int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); unit < p.T * p.parts; unit += (int64_t)gridDim.x * 4) {
     const int64_t t = unit / p.parts;
     f32x4 cos, sin;
     token_angles(p, at, t, cos, sin);
-    for (int h = (int)(unit % p.parts) * 4 + group; h < heads; h += p.parts * 4) {
-      const bool query = h < p.hq;
-      const T* x = (const T*)(query ? p.q.row(t, h) : p.k.row(t, h - p.hq));
-      const T* dy = (const T*)(query ? p.q_out.row(t, h) : p.k_out.row(t, h - p.hq));
-      T* dx = (T*)(query ? p.dq.row(t, h) : p.dk.row(t, h - p.hq));
-      f32x4 a = {}, b = {}, da = {}, db = {};
-      if (at.any) a = load4(x + at.a), b = load4(x + at.b), da = load4(dy + at.a), db = load4(dy + at.b);
-      f32x4 ua = da * cos + db * sin, ub = db * cos - da * sin;
-      if (p.q_gain) {
-        const float r = rsqrtf(group_sum(dot4(a, a) + dot4(b, b)) / (float)p.D + p.eps);
-        const f32x4 xa = a * r, xb = b * r;
-        if (query) sum_q[0] += ua * xa, sum_q[1] += ub * xb;
-        else sum_k[0] += ua * xa, sum_k[1] += ub * xb;
-        ua = ua * (query ? gq[0] : gk[0]);
-        ub = ub * (query ? gq[1] : gk[1]);
-        const float m = group_sum(dot4(ua, xa) + dot4(ub, xb)) / (float)p.D;
-        ua = (ua - xa * m) * r;
-        ub = (ub - xb * m) * r;
+    for (int h0 = (int)(unit % p.parts) * 4 + group; h0 < heads; h0 += step * kRopeHeads) {
+      f32x4 a[kRopeHeads], b[kRopeHeads], da[kRopeHeads], db[kRopeHeads];
+#pragma unroll
+      for (int i = 0; i < kRopeHeads; ++i) {
+        const int h = h0 + i * step;
+        a[i] = b[i] = da[i] = db[i] = f32x4{};
+        if (h >= heads || !at.any) continue;
+        const T* x = (const T*)(h < p.hq ? p.q.row(t, h) : p.k.row(t, h - p.hq));
+        const T* dy = (const T*)(h < p.hq ? p.q_out.row(t, h) : p.k_out.row(t, h - p.hq));
+        a[i] = load4(x + at.a), b[i] = load4(x + at.b), da[i] = load4(dy + at.a), db[i] = load4(dy + at.b);
       }
-      if (at.any) store4(dx + at.a, ua), store4(dx + at.b, ub);
+#pragma unroll
+      for (int i = 0; i < kRopeHeads; ++i) {
+        const int h = h0 + i * step;
+        const bool query = h < p.hq;
+        f32x4 ua = da[i] * cos + db[i] * sin, ub = db[i] * cos - da[i] * sin;
+        if (p.q_gain) {
+          const float r = rsqrtf(group_sum(dot4(a[i], a[i]) + dot4(b[i], b[i])) / (float)p.D + p.eps);
+          const f32x4 xa = a[i] * r, xb = b[i] * r;
+          if (query) sum_q[0] += ua * xa, sum_q[1] += ub * xb;
+          else sum_k[0] += ua * xa, sum_k[1] += ub * xb;      // of a head behind the last: zeros
+          ua = ua * (query ? gq[0] : gk[0]);
+          ub = ub * (query ? gq[1] : gk[1]);
+          const float m = group_sum(dot4(ua, xa) + dot4(ub, xb)) / (float)p.D;
+          ua = (ua - xa * m) * r;
+          ub = (ub - xb * m) * r;
+        }
+        if (h >= heads || !at.any) continue;
+        T* dx = (T*)(query ? p.dq.row(t, h) : p.dk.row(t, h - p.hq));
+        store4(dx + at.a, ua), store4(dx + at.b, ub);
+      }
     }
   }
   if (!p.partials) return;
@@ -159,14 +184,23 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope_bwd(const NormRopeArgs p) 
   }
 }
 
-// The gains' gradients from the workgroups' sums, in a fixed order, in 64 bits: one workgroup for each channel of each gain.
-__global__ __launch_bounds__(64) void k_gain_grads(const float* __restrict__ partials, int n, int D, float* __restrict__ dq_gain,
-                                                   float* __restrict__ dk_gain) {
-  const int which = blockIdx.x / D, c = blockIdx.x % D;
+// The gains' gradients from the workgroups' sums, in a fixed order: a workgroup for 16 channels, 64 slices of the workgroups, whose
+// sums are added in 64 bits.
+__global__ __launch_bounds__(1024) void k_gain_grads(const float* __restrict__ partials, int n, int D, float* __restrict__ dq_gain,
+                                                     float* __restrict__ dk_gain) {
+  __shared__ double all[64][17];
+  const int at = blockIdx.x * 16 + (threadIdx.x & 15), slice = threadIdx.x >> 4;
   double v = 0.0;
-  for (int i = threadIdx.x; i < n; i += 64) v += partials[((int64_t)i * 2 + which) * D + c];
-  v = wave_sum(v);
-  if (threadIdx.x == 0) (which ? dk_gain : dq_gain)[c] = (float)v;
+  if (at < 2 * D)
+#pragma unroll 8
+    for (int i = slice; i < n; i += 64) v += partials[(int64_t)i * 2 * D + at];
+  all[slice][threadIdx.x & 15] = v;
+  __syncthreads();
+  if (slice > 0 || at >= 2 * D) return;
+  v = 0.0;
+#pragma unroll 8
+  for (int i = 0; i < 64; ++i) v += all[i][threadIdx.x & 15];
+  (at < D ? dq_gain : dk_gain)[at < D ? at : at - D] = (float)v;
 }
 
 }  // namespace oapl
