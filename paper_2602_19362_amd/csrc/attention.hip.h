@@ -49,18 +49,6 @@ struct SeqTile {
   int first;        // the tile's first row (key), counted in the sequence
 };
 
-// Offsets start at 0, do not fall, and end at the number of tokens; cached lengths lie within their sequences' room.  Every
-// wavefront looks for itself, so nothing has to be launched before the kernel that computes.
-__device__ __forceinline__ bool sequences_ok(const AttnArgs& p) {
-  bool bad = false;
-  for (int i = threadIdx.x & 63; i < p.n_seq; i += 64) {
-    const int64_t a = p.q_offsets[i], b = p.q_offsets[i + 1], c = p.k_offsets[i], d = p.k_offsets[i + 1];
-    bad |= (i == 0 && (a != 0 || c != 0)) || b < a || d < c || (i == p.n_seq - 1 && (b != p.Tq || d != p.Tk));
-    if (p.k_used) bad |= p.k_used[i] < 0 || p.k_used[i] > d - c;
-  }
-  return __ballot(bad) == 0;
-}
-
 // A number that all lanes hold alike, for the scalar unit.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ int64_t uniform(int64_t x) {
@@ -81,7 +69,23 @@ __device__ __forceinline__ SeqTile tile_of(const AttnArgs& p, int seq, TileOf wh
   return t;
 }
 
-// The tile with this id, by a search over the first ids of the sequences, 64 at a time.  Only after sequences_ok.
+// Offsets start at 0, do not fall, and end at the number of tokens; cached lengths lie within their sequences' room.  Every
+// wavefront looks for itself, so nothing has to be launched before the kernel that computes.
+struct SeqEnds {
+  int64_t q0, q1, k0, k1, used;      // of one sequence; zeros behind the last
+  __device__ __forceinline__ SeqEnds(const AttnArgs& p, int i) {
+    q0 = q1 = k0 = k1 = used = 0;
+    if (i >= p.n_seq) return;
+    q0 = p.q_offsets[i], q1 = p.q_offsets[i + 1], k0 = p.k_offsets[i], k1 = p.k_offsets[i + 1];
+    used = p.k_used ? p.k_used[i] : k1 - k0;
+  }
+  __device__ __forceinline__ bool bad(const AttnArgs& p, int i) const {
+    return (i == 0 && (q0 != 0 || k0 != 0)) || q1 < q0 || k1 < k0 || (i == p.n_seq - 1 && (q1 != p.Tq || k1 != p.Tk)) || used < 0 ||
+           used > k1 - k0;
+  }
+};
+
+// The tile with this id, by a search over the first ids of (well-formed) sequences, 64 at a time.
 template <int B>
 __device__ __forceinline__ SeqTile find_tile(const AttnArgs& p, TileOf what, int64_t id) {
   const int64_t* __restrict__ off = what == kOfRows ? p.q_offsets : p.k_offsets;
@@ -114,28 +118,30 @@ __device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readla
 // The tile that stands `rank`-th when all are ordered by how far they reach, longest first (in 256 levels): what a tile of rows costs is
 // the keys that its last row sees, a tile of keys the queries that see its first key, and either is a closed form of the tile's
 // number, so that every workgroup finds its own by a search over levels.  Long tiles that start last are what the chip
-// waits for in the end.  False: there are not so many.  More than 64 sequences go in the order of their ids.
+// waits for in the end.  More than 64 sequences go in the order of their ids.
+enum Found { kMalformed, kNoTile, kTile };
+
 template <int B>
-__device__ __forceinline__ bool pick_tile(const AttnArgs& p, TileOf what, int rank, SeqTile& t) {
+__device__ __forceinline__ Found pick_tile(const AttnArgs& p, TileOf what, int rank, SeqTile& t) {
+  const int lane = threadIdx.x & 63;
+  const SeqEnds ends(p, lane);
+  bool bad = lane < p.n_seq && ends.bad(p, lane);
+  for (int i = lane + 64; i < p.n_seq; i += 64) bad |= SeqEnds(p, i).bad(p, i);
+  if (__ballot(bad) != 0) return kMalformed;
   if (p.n_seq > 64) {
     const int64_t last = what == kOfRows ? tile_ids<B>(p.Tq * p.g, p.n_seq) - 1 : 0;
     t = find_tile<B>(p, what, what == kOfRows ? last - rank : rank);
-    return t.first < (what == kOfRows ? t.nq * p.g : t.nk);
+    return t.first < (what == kOfRows ? t.nq * p.g : t.nk) ? kTile : kNoTile;
   }
-  const int lane = threadIdx.x & 63;
-  int nq = 0, nk = 0;
-  if (lane < p.n_seq) {
-    nq = (int)(p.q_offsets[lane + 1] - p.q_offsets[lane]);
-    nk = (int)(p.k_used ? p.k_used[lane] : p.k_offsets[lane + 1] - p.k_offsets[lane]);
-  }
-  const int tiles = what == kOfRows ? (int)(((int64_t)nq * p.g + B - 1) / B) : (nk + B - 1) / B, reach = what == kOfRows ? nk : nq;
+  const int nq = (int)(ends.q1 - ends.q0), nk = (int)ends.used;
+  const int tiles = ((what == kOfRows ? nq * p.g : nk) + B - 1) / (unsigned)B, reach = what == kOfRows ? nk : nq;
   // the sequence's tiles that reach beyond x >= 0
   const auto beyond = [&](int x) {
     if (x >= reach) return 0;
     if (!p.causal) return tiles;
-    if (what == kOfKeys) return min(tiles, (nk - x + B - 1) / B);
+    if (what == kOfKeys) return min(tiles, (int)((nk - x + B - 1) / (unsigned)B));
     const int token = x - (nk - nq);       // the first that sees more than x
-    return tiles - (token > 0 ? (int)((int64_t)token * p.g / B) : 0);
+    return tiles - (token > 0 ? (int)(token * p.g / (unsigned)B) : 0);
   };
   int most = reach;
 #pragma unroll
@@ -149,11 +155,17 @@ __device__ __forceinline__ bool pick_tile(const AttnArgs& p, TileOf what, int ra
   }
   const int above = beyond(hi * unit), mine = (lo < 0 ? tiles : beyond(lo * unit)) - above;
   const int to = prefix_sum(mine), left = rank - last_lane(prefix_sum(above));
-  if (left >= last_lane(to)) return false;
+  if (left >= last_lane(to)) return kNoTile;
   const int seq = __ffsll((unsigned long long)__ballot(to > left)) - 1;
   const int nth = __builtin_amdgcn_readlane(above + left - (to - mine), seq);    // among the sequence's, longest first
-  t = tile_of(p, seq, what, (int64_t)(what == kOfRows ? __builtin_amdgcn_readlane(tiles, seq) - 1 - nth : nth) * B);
-  return true;
+  const auto of = [&](int64_t x) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), seq) << 32 |
+                     (uint32_t)__builtin_amdgcn_readlane((int)x, seq));
+  };
+  t.q0 = of(ends.q0), t.k0 = of(ends.k0);
+  t.nq = __builtin_amdgcn_readlane(nq, seq), t.nk = __builtin_amdgcn_readlane(nk, seq);
+  t.first = (what == kOfRows ? __builtin_amdgcn_readlane(tiles, seq) - 1 - nth : nth) * B;
+  return kTile;
 }
 
 // Malformed sequences: the outputs are NaN.  Workgroups share the tokens.
@@ -180,16 +192,17 @@ template <> struct FragOf<float> { typedef FragF32 type; };
 // sum.  What it then does not keep are the wait states around an MFMA: results are looked at behind settle(), and operands that
 // vector instructions made go through ready().
 __device__ __forceinline__ void mma(f32x4& c, bf16x8 a, bf16x8 b) { asm("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b)); }
+// (fp32 operands may be copied between registers just before: its wait states go with every multiplication, behind the one before.)
 __device__ __forceinline__ void mma(f32x4& c, const FragF32& a, const FragF32& b) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) asm("v_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+v"(c) : "v"(a.x[j >> 2][j & 3]), "v"(b.x[j >> 2][j & 3]));
+  for (int j = 0; j < 8; ++j) asm("s_nop 1\n\tv_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+v"(c) : "v"(a.x[j >> 2][j & 3]), "v"(b.x[j >> 2][j & 3]));
 }
 // ... the first of a sum.
 __device__ __forceinline__ void mma0(f32x4& c, bf16x8 a, bf16x8 b) { asm("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=&v"(c) : "v"(a), "v"(b)); }
 __device__ __forceinline__ void mma0(f32x4& c, const FragF32& a, const FragF32& b) {
-  asm("v_mfma_f32_16x16x4_f32 %0, %1, %2, 0" : "=&v"(c) : "v"(a.x[0][0]), "v"(b.x[0][0]));
+  asm("s_nop 1\n\tv_mfma_f32_16x16x4_f32 %0, %1, %2, 0" : "=&v"(c) : "v"(a.x[0][0]), "v"(b.x[0][0]));
 #pragma unroll
-  for (int j = 1; j < 8; ++j) asm("v_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+v"(c) : "v"(a.x[j >> 2][j & 3]), "v"(b.x[j >> 2][j & 3]));
+  for (int j = 1; j < 8; ++j) asm("s_nop 1\n\tv_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+v"(c) : "v"(a.x[j >> 2][j & 3]), "v"(b.x[j >> 2][j & 3]));
 }
 // The wait states of the slower of the two shapes: one statement that all results go into and come out of.
 template <int N>
@@ -228,14 +241,17 @@ __device__ __forceinline__ void pack(f32x4 a, f32x4 b, bf16x8& f) {
 }
 __device__ __forceinline__ void pack(f32x4 a, f32x4 b, FragF32& f) { f.x[0] = a, f.x[1] = b; }
 
-// A row's channels of one k-step from memory (nullptr: zeros).
-__device__ __forceinline__ void load_frag(const char* row, int c, int D, bf16x8& f) {
-  f = bf16x8{};
-  if (row && c < D) f = *(const bf16x8*)(row + c * 2);
-}
-__device__ __forceinline__ void load_frag(const char* row, int c, int D, FragF32& f) {
-  f = FragF32{};
-  if (row && c < D) f.x[0] = *(const f32x4*)(row + c * 4), f.x[1] = *(const f32x4*)(row + c * 4 + 16);
+// A lane's eighths of a row of D channels, in steps of 32; zeros behind channel D.
+__device__ __forceinline__ void load_frag(const char* at, bf16x8& f) { f = *(const bf16x8*)at; }
+__device__ __forceinline__ void load_frag(const char* at, FragF32& f) { f.x[0] = *(const f32x4*)at, f.x[1] = *(const f32x4*)(at + 16); }
+template <class T, int KS, class Frag>
+__device__ __forceinline__ void load_row(const char* row, int D, Frag (&f)[KS]) {
+#pragma unroll
+  for (int kk = 0; kk < KS; ++kk) {
+    const int c = (threadIdx.x >> 4 & 3) * 8 + kk * 32;
+    load_frag(row + (c < D ? c : 0) * sizeof(T), f[kk]);
+    if (c >= D) f[kk] = Frag{};
+  }
 }
 __device__ __forceinline__ float dot(const bf16x8& a, const bf16x8& b) {
   float s = 0.f;
@@ -300,8 +316,8 @@ struct Tile {
   static constexpr int kRowBits = 16 * 2 * (int)sizeof(T), kColumnBits = 16 * (int)sizeof(T);   // of a step of 32 (16) channels
 
   // Rows lane % 16 of the 16 rows `off` bytes into the tile, contracted over 32 channels.
-  __device__ static __forceinline__ int rows_place(lds_char_ptr lds) {
-    const int lane = threadIdx.x & 63;
+  __device__ static __forceinline__ int rows_place(lds_char_ptr lds, int thread) {
+    const int lane = thread & 63;
     return lds_place(lds) + (lane & 15) * kPitch + (((lane >> 4) * ((int)sizeof(T) / 2) ^ swizzle(lane & 15)) << 4);
   }
   __device__ static __forceinline__ void rows(int place, int off, bf16x8& f) {
@@ -314,8 +330,8 @@ struct Tile {
 
   // Channels lane % 16 of 16, contracted over 32 rows in the order in which the results of two blocks of 16 rows hold them.  bf16: of the 16 lanes of a group, lane 4e + a points at four channels of row e, and lane i receives channel i of four
   // rows.
-  __device__ static __forceinline__ int columns_place(lds_char_ptr lds) {
-    const int lane = threadIdx.x & 63;
+  __device__ static __forceinline__ int columns_place(lds_char_ptr lds, int thread) {
+    const int lane = thread & 63;
     if (sizeof(T) == 2) {
       const int r = (lane >> 4) * 4 + (lane >> 2 & 3);
       return lds_place(lds) + r * kPitch + (((lane >> 1 & 1) ^ swizzle(r)) << 4) + ((lane & 1) << 3);
@@ -384,14 +400,17 @@ __device__ __forceinline__ void staged_barrier() {
   __builtin_amdgcn_s_barrier();
 }
 
+// Quotients by the group size of numbers below 2^31: (x * mul) >> shift.
+__device__ __forceinline__ int by_group(const AttnArgs& p, int x) { return (int)((uint64_t)(uint32_t)x * p.g_mul >> p.g_shift); }
+
 // What a lane of the forward and dq kernels knows of its row.
 struct Row {
   int token, head;   // head in the group
   int sees;          // keys that it sees; 0 behind the sequence's end
   __device__ __forceinline__ Row(const AttnArgs& p, const SeqTile& t, int row) {
     const bool any = row < t.nq * p.g;
-    token = any ? row / p.g : 0;
-    head = any ? row % p.g : 0;
+    token = any ? by_group(p, row) : 0;      // what reads a row that does not exist reads the sequence's first
+    head = any ? row - token * p.g : 0;
     const int n = p.causal ? token + 1 + t.nk - t.nq : t.nk;
     sees = !any ? 0 : n < 0 ? 0 : n < t.nk ? n : t.nk;
     exists = any;
@@ -404,7 +423,7 @@ template <int B>
 __device__ __forceinline__ int tile_sees(const AttnArgs& p, const SeqTile& t) {
   if (!p.causal) return t.nk;
   const int rows = t.nq * p.g, last = (t.first + B < rows ? t.first + B : rows) - 1;
-  const int n = last / p.g + 1 + t.nk - t.nq;
+  const int n = uniform(by_group(p, last)) + 1 + t.nk - t.nq;
   return n < 0 ? 0 : n < t.nk ? n : t.nk;
 }
 
@@ -427,11 +446,14 @@ __device__ __forceinline__ void negate(FragF32& f) { f.x[0] = -f.x[0], f.x[1] = 
 
 template <class T, int DB>
 __device__ __forceinline__ void store_columns(char* row, const f32x4 (&acc)[DB], float factor, int D) {
-  const int group = threadIdx.x >> 4 & 3;
+  const int c0 = (threadIdx.x >> 4 & 3) * 4;
+  if (D == DB * 16) {
 #pragma unroll
-  for (int b = 0; b < DB; ++b) {
-    const int c = b * 16 + group * 4;
-    if (c < D) store4((T*)row + c, acc[b] * factor);
+    for (int b = 0; b < DB; ++b) store4((T*)row + c0 + b * 16, acc[b] * factor);
+  } else {
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+      if (c0 + b * 16 < D) store4((T*)row + c0 + b * 16, acc[b] * factor);
   }
 }
 
@@ -586,16 +608,15 @@ __global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k
   typedef FwdLds<T, DP, WK> Size;
   constexpr int B = 128 / WK, KS = DW / 32, DB = DW / 16, SIZE = Size::kTile;
   extern __shared__ char smem[];
-  const bool ok = sequences_ok(p);
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = ok ? 0 : kErrOffsets;
-  if (!ok) {
-    poison<T>(p.o, p.Tq, p.hq, p.D);
-    if (p.lse) poison(p.lse, p.Tq * p.hq);
-    return;
-  }
   const int kh = blockIdx.x % p.hk;
   SeqTile t;
-  if (!pick_tile<B>(p, kOfRows, blockIdx.x / p.hk, t)) return;
+  const Found found = pick_tile<B>(p, kOfRows, blockIdx.x / p.hk, t);
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = found == kMalformed ? kErrOffsets : 0;
+  if (found == kMalformed) {
+    poison<T>(p.o, p.Tq, p.hq, p.D);
+    if (p.lse) poison(p.lse, p.Tq * p.hq);
+  }
+  if (found != kTile) return;
   const int wave = uniform((int)threadIdx.x >> 6);
   const lds_char_ptr lds = (lds_char_ptr)smem + (WK == 1 ? 0 : wave * Size::kWave);     // slots of keys and values
   const Part part(tile_sees<B>(p, t), p.splits, blockIdx.y, kFwdKeys * WK);
@@ -607,7 +628,6 @@ __global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k
   };
   if (Size::kSlots == 2 && j0 < part.end) stage(0, j0);
   const int group = threadIdx.x >> 4 & 3, row0 = t.first + (WK == 1 ? wave * 32 : 0) + (threadIdx.x & 15);
-  const bool flip = p.scale < 0.f;                 // then products are taken with -q, and with zeros if it is 0
   const float scale2 = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;
   int row_sees[2];
   Frag q[2][KS];
@@ -617,11 +637,13 @@ __global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     const Row row(p, t, row0 + n * 16);
-    const char* x = row.exists && p.scale != 0.f ? p.q.row(t.q0 + row.token, kh * p.g + row.head) : nullptr;
+    load_row<T>(p.q.row(t.q0 + row.token, kh * p.g + row.head), p.D, q[n]);
+    if (p.scale <= 0.f) {      // products are taken with -q, or with zeros
 #pragma unroll
-    for (int kk = 0; kk < KS; ++kk) {
-      load_frag(x, kk * 32 + group * 8, p.D, q[n][kk]);
-      if (flip) negate(q[n][kk]);
+      for (int kk = 0; kk < KS; ++kk) {
+        negate(q[n][kk]);
+        if (p.scale == 0.f) q[n][kk] = Frag{};
+      }
     }
 #pragma unroll
     for (int d = 0; d < DB; ++d) zero(o[n][d]);
@@ -641,7 +663,7 @@ __global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k
     if (WK == 1) staged_barrier();
     else staged();
     if (Size::kSlots == 2 && j0 + kFwdKeys * WK < part.end) stage(slot ^ 2 * SIZE, j0 + kFwdKeys * WK);
-    const int k_rows = Lds::rows_place(lds + slot), v_columns = Lds::columns_place(lds + slot + SIZE);
+    const int k_rows = Lds::rows_place(lds + slot, threadIdx.x), v_columns = Lds::columns_place(lds + slot + SIZE, threadIdx.x);
     f32x4 s[2][2];     // [rows][keys]
     scores<Lds, KS>(s, k_rows, 0, q, [](int) {});
     if (j0 + kFwdKeys > all_see) {
@@ -829,12 +851,12 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
   constexpr int B = 128, KS = DW / 32, DB = DW / 16, SIZE = kKeys * Lds::kPitch;
   extern __shared__ char smem[];
   const lds_char_ptr lds = (lds_char_ptr)smem;
-  const bool ok = sequences_ok(p);
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = ok ? 0 : kErrOffsets;
-  if (!ok) return poison<T>(p.dq, p.Tq, p.hq, p.D);
   const int kh = blockIdx.x % p.hk;
   SeqTile t;
-  if (!pick_tile<B>(p, kOfRows, blockIdx.x / p.hk, t)) return;
+  const Found found = pick_tile<B>(p, kOfRows, blockIdx.x / p.hk, t);
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = found == kMalformed ? kErrOffsets : 0;
+  if (found == kMalformed) poison<T>(p.dq, p.Tq, p.hq, p.D);
+  if (found != kTile) return;
   const Part part(tile_sees<B>(p, t), p.splits, blockIdx.y, kKeys);
   const Stage ks(p.k.row(t.k0, kh), p.k.token, p.D), vs(p.v.row(t.k0, kh), p.v.token, p.D);
   if (part.begin < part.end) ks.start(lds, part.begin, t.nk), vs.start(lds + SIZE, part.begin, t.nk);
@@ -853,14 +875,12 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
 #pragma unroll
     for (int d = 0; d < DB; ++d) zero(dq[n][d]);
     delta[n] = 0.f;
+    Frag o[KS];
+    load_row<T>(p.q.row(token, head), p.D, q[n]);
+    load_row<T>(p.dout.row(token, head), p.D, dout[n]);
+    load_row<T>(p.o.row(token, head), p.D, o);
 #pragma unroll
-    for (int kk = 0; kk < KS; ++kk) {
-      Frag o;
-      load_frag(row.exists ? p.q.row(token, head) : nullptr, kk * 32 + group * 8, p.D, q[n][kk]);
-      load_frag(row.exists ? p.dout.row(token, head) : nullptr, kk * 32 + group * 8, p.D, dout[n][kk]);
-      load_frag(row.exists ? p.o.row(token, head) : nullptr, kk * 32 + group * 8, p.D, o);
-      delta[n] += dot(o, dout[n][kk]);
-    }
+    for (int kk = 0; kk < KS; ++kk) delta[n] += dot(o[kk], dout[n][kk]);
     delta[n] = row_sum(delta[n]);
     lse2[n] = row.exists ? p.lse[token * p.hq + head] * kLog2e : 0.f;
     if (row.exists && group == 0 && blockIdx.y == 0) {
@@ -885,7 +905,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
       ks.start(lds + (slot ^ 2 * SIZE), j0 + kKeys, t.nk);
       vs.start(lds + (slot ^ 2 * SIZE) + SIZE, j0 + kKeys, t.nk);
     }
-    const int k_rows = Lds::rows_place(lds + slot), k_columns = Lds::columns_place(lds + slot);
+    const int k_rows = Lds::rows_place(lds + slot, threadIdx.x), k_columns = Lds::columns_place(lds + slot, threadIdx.x);
     f32x4 s[2][2][2], dp[2][2][2];     // [half][rows][keys]
     Frag w[2][2];
     const auto finish = [&](int c, int i) {
@@ -928,9 +948,6 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
   }
 }
 
-// Quotients by the group size of numbers below 2^31: (x * mul) >> shift.
-__device__ __forceinline__ int by_group(const AttnArgs& p, int x) { return (int)((uint64_t)(uint32_t)x * p.g_mul >> p.g_shift); }
-
 constexpr int kRows = 64;    // rows staged at a time
 
 // Rows of two operands (queries and the output's gradient) and the rows' two numbers on their way to LDS, as Stager; what lies
@@ -941,28 +958,22 @@ struct RowStager {
   static constexpr int kRowsPerLoad = 64 / Lds::kChunks, kLoads = kRows / (4 * kRowsPerLoad), SIZE = kRows * Lds::kPitch;
   static constexpr int kBytes = 2 * SIZE + 2 * kRows * 4;
   static constexpr uint32_t kOutside = 0x80000000u;
-  // Where the heads in a group divide the rows that lie between two loads of a wavefront, a lane is at the same place of a token's heads
-  // with every load, and only the (scalar) token moves.
-  bool alike;
-  uint32_t whole_q, whole_d;
-  __device__ __forceinline__ RowStager(const AttnArgs& p) {
-    const int lane = threadIdx.x & 63, r = uniform((int)threadIdx.x >> 6) * kRowsPerLoad + lane / Lds::kChunks;
-    const int c = ((lane % Lds::kChunks) ^ Lds::swizzle(r)) * 16;
-    alike = 4 * kRowsPerLoad % 16 == 0 && 4 * kRowsPerLoad % p.g == 0;
-    const int token = by_group(p, r), head = r - token * p.g;
-    const bool any = c < p.D * (int)sizeof(T);
-    whole_q = any ? (uint32_t)(token * (int)p.q.token + head * (int)p.q.head + c) : kOutside;
-    whole_d = any ? (uint32_t)(token * (int)p.dout.token + head * (int)p.dout.head + c) : kOutside;
-  }
   // Starts the loads of rows [first, first + 64); `first` is a multiple of 64.
-  __device__ __forceinline__ void start(const AttnArgs& p, const SeqTile& t, int kh, lds_char_ptr lds, int first) const {
+  __device__ static __forceinline__ void start(const AttnArgs& p, const SeqTile& t, int kh, lds_char_ptr lds, int first) {
     const int wave = uniform((int)threadIdx.x >> 6), rows = t.nq * p.g, token0 = uniform(by_group(p, first));
     const __amdgpu_buffer_rsrc_t q =
         __builtin_amdgcn_make_buffer_rsrc((void*)p.q.row(t.q0 + token0, kh * p.g), 0, kOutside, 0x00020000);
     const __amdgpu_buffer_rsrc_t d =
         __builtin_amdgcn_make_buffer_rsrc((void*)p.dout.row(t.q0 + token0, kh * p.g), 0, kOutside, 0x00020000);
-    if (alike && first + kRows <= rows) {
-      const int tokens = by_group(p, 4 * kRowsPerLoad);
+    const int lane = fresh(threadIdx.x) & 63;      // what follows is made here, not kept: registers are short
+    // Where the heads in a group divide the rows that lie between two loads of a wavefront, a lane is at the same place of a token's
+    // heads with every load, and only the (scalar) token moves.
+    if (4 * kRowsPerLoad % 16 == 0 && p.g <= 4 * kRowsPerLoad && (p.g & (p.g - 1)) == 0 && first + kRows <= rows) {
+      const int tokens = by_group(p, 4 * kRowsPerLoad), r = wave * kRowsPerLoad + lane / Lds::kChunks, token = by_group(p, r);
+      const int c = ((lane % Lds::kChunks) ^ Lds::swizzle(r)) * 16, head = r - token * p.g;
+      const bool any = c < p.D * (int)sizeof(T);
+      const uint32_t whole_q = any ? (uint32_t)(token * (int)p.q.token + head * (int)p.q.head + c) : kOutside;
+      const uint32_t whole_d = any ? (uint32_t)(token * (int)p.dout.token + head * (int)p.dout.head + c) : kOutside;
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) {
         __builtin_amdgcn_raw_ptr_buffer_load_lds(q, (lds_void_ptr)(lds + (j * 4 + wave) * 1024), 16, whole_q,
@@ -971,7 +982,6 @@ struct RowStager {
                                                  j * tokens * (int)p.dout.token, 0, 0);
       }
     } else {
-      const int lane = fresh(threadIdx.x) & 63;
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) {
         const int r = (j * 4 + wave) * kRowsPerLoad + lane / Lds::kChunks, x = first + r;
@@ -988,7 +998,7 @@ struct RowStager {
       const int left = rows - first < kRows ? rows - first : kRows;
       const __amdgpu_buffer_rsrc_t n =
           __builtin_amdgcn_make_buffer_rsrc((void*)((wave ? p.delta : p.lse2) + packed_row(p, t, kh, first)), 0, left * 4, 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(n, (lds_void_ptr)(lds + 2 * SIZE + wave * kRows * 4), 4, (threadIdx.x & 63) * 4, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(n, (lds_void_ptr)(lds + 2 * SIZE + wave * kRows * 4), 4, lane * 4, 0, 0, 0);
     }
   }
 };
@@ -1003,19 +1013,19 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   constexpr int B = 128, KS = DW / 32, DB = DW / 16;
   extern __shared__ char smem[];
   const lds_char_ptr lds = (lds_char_ptr)smem;
-  if (!sequences_ok(p)) {
-    poison<T>(p.dk, p.Tk, p.hk, p.D);
-    return poison<T>(p.dv, p.Tk, p.hk, p.D);
-  }
   const int kh = blockIdx.x % p.hk;
   SeqTile t;
-  if (!pick_tile<B>(p, kOfKeys, blockIdx.x / p.hk, t)) return;
+  const Found found = pick_tile<B>(p, kOfKeys, blockIdx.x / p.hk, t);
+  if (found == kMalformed) {
+    poison<T>(p.dk, p.Tk, p.hk, p.D);
+    poison<T>(p.dv, p.Tk, p.hk, p.D);
+  }
+  if (found != kTile) return;
   const int rows = t.nq * p.g, ahead = t.nk - t.nq;
   // the first row that sees the tile's first key, and whole tiles of rows
   const int from = p.causal && t.first > ahead ? (t.first - ahead) * p.g / kRows * kRows : 0;
-  const Stage stage(p);
   const Part part(rows > from ? rows - from : 0, p.splits, blockIdx.y, kRows);
-  if (part.begin < part.end) stage.start(p, t, kh, lds, from + part.begin);
+  if (part.begin < part.end) Stage::start(p, t, kh, lds, from + part.begin);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Frag k[2][KS], v[2][KS];
   f32x4 dk[2][DB], dv[2][DB];
@@ -1023,15 +1033,11 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   int all_from = 0;     // rows from here on see every key of the wavefront
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
-    const int key = t.first + wave * 32 + n * 16 + (threadIdx.x & 15), group = threadIdx.x >> 4 & 3;
-    const bool exists = key < t.nk;
+    const int key = t.first + wave * 32 + n * 16 + (threadIdx.x & 15), at = key < t.nk ? key : t.nk - 1;
 #pragma unroll
     for (int d = 0; d < DB; ++d) zero(dk[n][d]), zero(dv[n][d]);
-#pragma unroll
-    for (int kk = 0; kk < KS; ++kk) {
-      load_frag(exists ? p.k.row(t.k0 + key, kh) : nullptr, kk * 32 + group * 8, p.D, k[n][kk]);
-      load_frag(exists ? p.v.row(t.k0 + key, kh) : nullptr, kk * 32 + group * 8, p.D, v[n][kk]);
-    }
+    load_row<T>(p.k.row(t.k0 + at, kh), p.D, k[n]);
+    load_row<T>(p.v.row(t.k0 + at, kh), p.D, v[n]);
     all_from = first_row(key) > all_from ? first_row(key) : all_from;
   }
 #pragma unroll
@@ -1044,9 +1050,11 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   int slot = 0;
   for (int r0 = from + part.begin; r0 < from + part.end; r0 += kRows, slot ^= 1) {
     staged_barrier();
-    if (r0 + kRows < from + part.end) stage.start(p, t, kh, lds + (slot ^ 1) * Stage::kBytes, r0 + kRows);
+    if (r0 + kRows < from + part.end) Stage::start(p, t, kh, lds + (slot ^ 1) * Stage::kBytes, r0 + kRows);
     const lds_char_ptr numbers = lds + slot * Stage::kBytes + 2 * Stage::SIZE;
-    const int places = Lds::rows_place(lds + slot * Stage::kBytes), column_places = Lds::columns_place(lds + slot * Stage::kBytes);
+    const int thread = fresh(threadIdx.x);      // places are made here, not kept
+    const int places = Lds::rows_place(lds + slot * Stage::kBytes, thread);
+    const int column_places = Lds::columns_place(lds + slot * Stage::kBytes, thread);
 #pragma unroll 1
     for (int c = 0; c < kRows / 32; ++c) {
       typedef __attribute__((address_space(3))) f32x4* ptr;
