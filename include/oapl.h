@@ -441,8 +441,9 @@ size_t oapl_attention_workspace_bytes(int64_t Tq, int64_t Tk, int32_t n_seq, int
  * Query head h attends to key head h / (n_q_heads / n_k_heads).  Sums and the
  * soft-max in 32 bits; OAPL_BF16 rounds the probabilities (before they are
  * normalised) once for the product with the values.
- * A NaN or infinity among the keys or values of a sequence may reach any row of that sequence,
- * also rows that do not see it; it reaches no other sequence.
+ * What is not finite reaches only who sees it: a NaN or infinity in a key or value no row that does
+ * not see that key, one in a row of queries (or of dout, below) no key that the row does not
+ * see.  Rows that see one may be NaN in every channel.
  *   q_offsets, k_offsets  [n_seq + 1] int64 from 0 to Tq and Tk, non-decreasing
  *                         (may be the same array; sequences may be empty)
  *   k_used      NULL, or [n_seq] int64

@@ -394,12 +394,6 @@ struct Stager {
 
 // Everything that this wavefront started has arrived ...
 __device__ __forceinline__ void staged() { __builtin_amdgcn_s_waitcnt(vmcnt_imm(0) & ~0x0F00); }      // vmcnt(0) lgkmcnt(0)
-// ... and so has what the others of the workgroup started.
-__device__ __forceinline__ void staged_barrier() {
-  staged();
-  __builtin_amdgcn_s_barrier();
-}
-
 // Quotients by the group size of numbers below 2^31: (x * mul) >> shift.
 __device__ __forceinline__ int by_group(const AttnArgs& p, int x) { return (int)((uint64_t)(uint32_t)x * p.g_mul >> p.g_shift); }
 
@@ -424,6 +418,13 @@ __device__ __forceinline__ int tile_sees(const AttnArgs& p, const SeqTile& t) {
   if (!p.causal) return t.nk;
   const int rows = t.nq * p.g, last = (t.first + B < rows ? t.first + B : rows) - 1;
   const int n = uniform(by_group(p, last)) + 1 + t.nk - t.nq;
+  return n < 0 ? 0 : n < t.nk ? n : t.nk;
+}
+
+// Keys that every row of a tile sees.
+__device__ __forceinline__ int all_rows_see(const AttnArgs& p, const SeqTile& t) {
+  if (!p.causal) return t.nk;
+  const int n = uniform(by_group(p, t.first)) + 1 + t.nk - t.nq;
   return n < 0 ? 0 : n < t.nk ? n : t.nk;
 }
 
@@ -467,6 +468,96 @@ __device__ __forceinline__ float over_row(float v, F f) {
 }
 __device__ __forceinline__ float row_max(float v) { return over_row(v, [](float a, float b) { return max3(a, a, b); }); }
 __device__ __forceinline__ float row_sum(float v) { return over_row(v, [](float a, float b) { return a + b; }); }
+
+// What is not finite in a tile's masked places.  A masked probability is 0, and 0 times a NaN or an infinity would be NaN in rows that
+// do not see it.  Where a step masks anything, what is not finite becomes 0 in the tile before it is used, and the
+// probabilities of those rows are made NaN for whoever sees them (mark_odd).
+//
+// Whether this wavefront has staged any such number: its pieces of a tile (j W + wave, of 1 KiB), before the others have to be there.
+template <class T, int LOADS, int W>
+__device__ __forceinline__ bool staged_odd(lds_char_ptr tile) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  const int wave = W == 1 ? 0 : uniform((int)threadIdx.x >> 6);
+  uint32_t top = 0;      // the largest magnitude (of either half), as an integer
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const u32x4 x = *(__attribute__((address_space(3))) u32x4*)(tile + (i * W + wave) * 1024 + (threadIdx.x & 63) * 16);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (sizeof(T) == 4) top = max(top, x[j] & 0x7fffffffu);
+      else top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top), __builtin_bit_cast(u16x2, x[j] & 0x7fff7fffu)));
+    }
+  }
+  return __any(top >= 0x7f800000u || (sizeof(T) == 2 && (top & 0xffffu) >= 0x7f80u));
+}
+// ... and whether anybody of four has, in words that alternate from step to step (the slower ones may still be reading).
+__device__ __forceinline__ void tell_odd(lds_char_ptr words, int parity, bool odd) {
+  if ((threadIdx.x & 63) == 0) ((__attribute__((address_space(3))) uint32_t*)words)[parity * 4 + (threadIdx.x >> 6)] = odd;
+}
+__device__ __forceinline__ bool told_odd(lds_char_ptr words, int parity) {
+  const u32x4 x = *(__attribute__((address_space(3))) u32x4*)(words + parity * 16);
+  return uniform((int)(x[0] | x[1] | x[2] | x[3])) != 0;
+}
+
+// The rows of a tile of ROWS (and of the one SIZE bytes behind it, with TILES = 2) that hold any, as bits.  W wavefronts share a tile:
+// all of them come here, and `words` are W words of LDS for what each has found.
+template <class T, int DP, int ROWS, int W, int TILES = 1, int SIZE = 0>
+__device__ __forceinline__ uint64_t clean_tile(lds_char_ptr tile, lds_char_ptr words) {
+  typedef Tile<T, DP> Lds;
+  typedef __attribute__((address_space(3))) u32x4* lds_u32x4;
+  typedef __attribute__((address_space(3))) uint32_t* lds_u32;
+  constexpr int kAtOnce = 64 / Lds::kChunks, kMine = ROWS / W;      // rows that 64 lanes cover at a time; of a wavefront
+  const int wave = W == 1 ? 0 : uniform((int)threadIdx.x >> 6);
+  const lds_char_ptr mine = tile + wave * kMine * Lds::kPitch + (threadIdx.x & 63) * 16;
+  uint64_t odd = 0;
+  const auto pieces = [&](auto&& f) {
+#pragma unroll 1
+    for (int i = 0; i < TILES * kMine / kAtOnce; ++i)
+      f(i % (kMine / kAtOnce) * kAtOnce, (lds_u32x4)(mine + i / (kMine / kAtOnce) * SIZE + i % (kMine / kAtOnce) * 1024));
+  };
+  pieces([&](int row, lds_u32x4 at) {
+    const u32x4 x = *at;
+    bool any = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) any |= (x[j] & 0x7f800000u) == 0x7f800000u || (sizeof(T) == 2 && (x[j] & 0x7f80u) == 0x7f80u);
+    const uint64_t lanes = __ballot(any);
+#pragma unroll
+    for (int r = 0; r < kAtOnce; ++r)
+      if (lanes >> (r * Lds::kChunks) & ((1ull << Lds::kChunks) - 1)) odd |= 1ull << (row + r);
+  });
+  if (W > 1) {
+    static_assert(W == 1 || kMine <= 32, "a word holds a wavefront's rows");
+    if ((threadIdx.x & 63) == 0) ((lds_u32)words)[wave] = (uint32_t)odd;
+    lds_barrier();
+    odd = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) odd |= (uint64_t)(uint32_t)uniform((int)((lds_u32)words)[w]) << (w * kMine);
+  }
+  if (odd == 0) return 0;
+  pieces([&](int, lds_u32x4 at) {
+    u32x4 x = *at;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (sizeof(T) == 4) {
+        if ((x[j] & 0x7f800000u) == 0x7f800000u) x[j] = 0;
+      } else {
+        if ((x[j] & 0x7f80u) == 0x7f80u) x[j] &= 0xffff0000u;
+        if ((x[j] & 0x7f800000u) == 0x7f800000u) x[j] &= 0xffffu;
+      }
+    }
+    *at = x;
+  });
+  if (W > 1) lds_barrier();
+  return odd;
+}
+__device__ __forceinline__ void mark_odd(f32x4 (&s)[2][2], uint32_t odd) {
+  const int group = fresh(threadIdx.x) >> 4 & 3;
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int x = 0; x < 8; ++x)
+      if (odd >> (group * 4 + (x >> 2) * 16 + (x & 3)) & 1) s[n][x >> 2][x & 3] = quiet_nan();
+}
 
 // Scores of two blocks of 16 rows of a tile in LDS (keys, or rows) with the wavefront's 32 rows (keys): s[n][b] is the tile's block b,
 // `off` bytes into it, by the wavefront's block n.  Operands are fetched three ahead of their multiplications, and after each pair of
@@ -572,7 +663,7 @@ struct FwdLds {
   static constexpr int kTile = kFwdKeys * Tile<T, DP>::kPitch, kSlots = WK == 4 && sizeof(T) == 4 ? 1 : 2;
   static constexpr int kStages = 2 * kSlots * kTile, kResults = 32 * (DP * 4 + 16);
   static constexpr int kWave = WK == 1 || kStages > kResults ? kStages : (kResults + 511) / 512 * 512;
-  static constexpr int kBytes = WK * kWave;
+  static constexpr int kWords = WK * kWave, kBytes = kWords + 48;      // words: tell_odd's, clean_tile's
   static_assert(kBytes <= 160 * 1024, "LDS of one CU");
 };
 
@@ -622,6 +713,10 @@ __global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k
   const Part part(tile_sees<B>(p, t), p.splits, blockIdx.y, kFwdKeys * WK);
   const Stage ks(p.k.row(t.k0, kh), p.k.token, p.D), vs(p.v.row(t.k0, kh), p.v.token, p.D);
   int j0 = part.begin + (WK == 1 ? 0 : wave * kFwdKeys), slot = 0;
+  const lds_char_ptr words = (lds_char_ptr)smem + Size::kWords;
+  // whether a step has keys that some rows of the tile see and others do not
+  const int first_sees = all_rows_see(p, t), last_sees = tile_sees<B>(p, t);
+  const auto masks = [&](int from) { return first_sees < last_sees && from + kFwdKeys > first_sees; };
   const auto stage = [&](int at, int first) {
     ks.start(lds + at, first, t.nk);
     vs.start(lds + at + SIZE, first, t.nk);
@@ -648,7 +743,7 @@ __global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k
 #pragma unroll
     for (int d = 0; d < DB; ++d) zero(o[n][d]);
     row_sees[n] = row.sees;
-    if (row.exists || WK == 1) all_see = row.sees < all_see ? row.sees : all_see;
+    if (row.exists) all_see = row.sees < all_see ? row.sees : all_see;
     m[n] = kNegHuge;
     l[n] = 0.f;
   }
@@ -660,18 +755,26 @@ __global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k
   all_see = __builtin_amdgcn_readfirstlane(all_see);
   for (; j0 < part.end; j0 += kFwdKeys * WK, slot ^= Size::kSlots == 2 ? 2 * SIZE : 0) {
     if (Size::kSlots == 1) stage(0, j0);
-    if (WK == 1) staged_barrier();
-    else staged();
+    staged();
+    bool odd = masks(j0) && staged_odd<T, Stage::kLoads, 4 / WK>(lds + slot + SIZE);
+    if (WK == 1) {
+      if (masks(j0)) tell_odd(words, slot != 0, odd);
+      lds_barrier();
+      odd = masks(j0) && told_odd(words, slot != 0);
+    }
     if (Size::kSlots == 2 && j0 + kFwdKeys * WK < part.end) stage(slot ^ 2 * SIZE, j0 + kFwdKeys * WK);
     const int k_rows = Lds::rows_place(lds + slot, threadIdx.x), v_columns = Lds::columns_place(lds + slot + SIZE, threadIdx.x);
     f32x4 s[2][2];     // [rows][keys]
     scores<Lds, KS>(s, k_rows, 0, q, [](int) {});
+    if (odd) mark_odd(s, (uint32_t)clean_tile<T, DP, kFwdKeys, 4 / WK>(lds + slot + SIZE, words + 32));
     if (j0 + kFwdKeys > all_see) {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int x = 0; x < 8; ++x)
-          if (j0 + (x >> 2) * 16 + group * 4 + (x & 3) >= row_sees[n]) s[n][x >> 2][x & 3] = -__builtin_inff();
+        for (int x = 0; x < 8; ++x) {
+          const int key = (x >> 2) * 16 + group * 4 + (x & 3);
+          if (j0 + key >= row_sees[n]) s[n][x >> 2][x & 3] = -__builtin_inff();
+        }
     }
     // The maximum that the exponentials are taken from follows only when it falls behind by 2^8: until then they stay below 2^8, and
     // what is rounded is rounded as well as below 1.
@@ -857,7 +960,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = found == kMalformed ? kErrOffsets : 0;
   if (found == kMalformed) poison<T>(p.dq, p.Tq, p.hq, p.D);
   if (found != kTile) return;
-  const Part part(tile_sees<B>(p, t), p.splits, blockIdx.y, kKeys);
+  const int first_sees = all_rows_see(p, t), last_sees = tile_sees<B>(p, t);
+  const Part part(last_sees, p.splits, blockIdx.y, kKeys);
   const Stage ks(p.k.row(t.k0, kh), p.k.token, p.D), vs(p.v.row(t.k0, kh), p.v.token, p.D);
   if (part.begin < part.end) ks.start(lds, part.begin, t.nk), vs.start(lds + SIZE, part.begin, t.nk);
   const int group = threadIdx.x >> 4 & 3, row0 = t.first + (threadIdx.x >> 6) * 32 + (threadIdx.x & 15);
@@ -890,7 +994,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
       p.lse2[at] = lse2[n] == -__builtin_inff() ? __builtin_inff() : lse2[n];
     }
     row_sees[n] = row.sees;
-    all_see = row.sees < all_see ? row.sees : all_see;
+    if (row.exists) all_see = row.sees < all_see ? row.sees : all_see;
   }
 #pragma unroll
   for (int x = 8; x > 0; x >>= 1) {
@@ -900,12 +1004,17 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
   all_see = __builtin_amdgcn_readfirstlane(all_see);
   int slot = 0;
   for (int j0 = part.begin; j0 < part.end; j0 += kKeys, slot ^= 2 * SIZE) {
-    staged_barrier();
+    const bool masks = first_sees < last_sees && j0 + kKeys > first_sees;
+    const lds_char_ptr words = lds + 4 * SIZE;
+    staged();
+    if (masks) tell_odd(words, slot != 0, staged_odd<T, Stage::kLoads, 4>(lds + slot));
+    lds_barrier();
     if (j0 + kKeys < part.end) {
       ks.start(lds + (slot ^ 2 * SIZE), j0 + kKeys, t.nk);
       vs.start(lds + (slot ^ 2 * SIZE) + SIZE, j0 + kKeys, t.nk);
     }
     const int k_rows = Lds::rows_place(lds + slot, threadIdx.x), k_columns = Lds::columns_place(lds + slot, threadIdx.x);
+    const uint64_t odd = masks && told_odd(words, slot != 0) ? clean_tile<T, DP, kKeys, 4>(lds + slot, words + 32) : 0;
     f32x4 s[2][2][2], dp[2][2][2];     // [half][rows][keys]
     Frag w[2][2];
     const auto finish = [&](int c, int i) {
@@ -913,12 +1022,15 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
       s[c][n][x >> 2][x & 3] = __builtin_amdgcn_exp2f(fmaf(s[c][n][x >> 2][x & 3], scale2, -lse2[n])) * (dp[c][n][x >> 2][x & 3] - delta[n]);
     };
     const auto mask = [&](int c) {
+      if (odd) mark_odd(s[c], (uint32_t)(odd >> (c * 32)));
       if (j0 + c * 32 + 32 > all_see) {
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
-          for (int x = 0; x < 8; ++x)
-            if (j0 + c * 32 + (x >> 2) * 16 + group * 4 + (x & 3) >= row_sees[n]) s[c][n][x >> 2][x & 3] = 0.f;
+          for (int x = 0; x < 8; ++x) {
+            const int key = (x >> 2) * 16 + group * 4 + (x & 3);
+            if (j0 + c * 32 + key >= row_sees[n]) s[c][n][x >> 2][x & 3] = 0.f;
+          }
       }
 #pragma unroll
       for (int n = 0; n < 2; ++n) pack(s[c][n][0], s[c][n][1], w[c][n]);
@@ -1047,20 +1159,30 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   }
   all_from = __builtin_amdgcn_readfirstlane(all_from);
   const float scale2 = p.scale * kLog2e;
+  const int masked_to = first_row((t.first + B < t.nk ? t.first + B : t.nk) - 1);      // rows from here on see every key of the workgroup
   int slot = 0;
   for (int r0 = from + part.begin; r0 < from + part.end; r0 += kRows, slot ^= 1) {
-    staged_barrier();
+    const lds_char_ptr words = lds + 2 * Stage::kBytes;
+    staged();
+    if (r0 < masked_to)
+      tell_odd(words, slot, staged_odd<T, Stage::kLoads, 4>(lds + slot * Stage::kBytes) ||
+                                staged_odd<T, Stage::kLoads, 4>(lds + slot * Stage::kBytes + Stage::SIZE));
+    lds_barrier();
     if (r0 + kRows < from + part.end) Stage::start(p, t, kh, lds + (slot ^ 1) * Stage::kBytes, r0 + kRows);
     const lds_char_ptr numbers = lds + slot * Stage::kBytes + 2 * Stage::SIZE;
-    const int thread = fresh(threadIdx.x);      // places are made here, not kept
-    const int places = Lds::rows_place(lds + slot * Stage::kBytes, thread);
-    const int column_places = Lds::columns_place(lds + slot * Stage::kBytes, thread);
+    if (r0 < masked_to && told_odd(words, slot)) {      // a row's probabilities are NaN where its log-sum-exp is
+      typedef __attribute__((address_space(3))) float* lds_f32;
+      const uint64_t odd = clean_tile<T, DP, kRows, 4, 2, Stage::SIZE>(lds + slot * Stage::kBytes, words + 32);
+      if (threadIdx.x < kRows && (odd >> threadIdx.x & 1)) ((lds_f32)numbers)[threadIdx.x] = quiet_nan();
+      lds_barrier();
+    }
 #pragma unroll 1
     for (int c = 0; c < kRows / 32; ++c) {
       typedef __attribute__((address_space(3))) f32x4* ptr;
+      const lds_char_ptr tile = lds + slot * Stage::kBytes + c * 32 * Lds::kPitch;
       Frag w[2], wd[2];      // probabilities and dS of 32 rows, keys in columns
       f32x4 s[2][2], dp[2][2];     // [keys][rows]
-      scores2<Lds, KS, Stage::SIZE>(s, dp, places + c * 32 * Lds::kPitch, k, v);
+      scores2<Lds, KS, Stage::SIZE>(s, dp, Lds::rows_place(tile, fresh(threadIdx.x)), k, v);      // places are not kept: registers are short
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const lds_char_ptr at = numbers + (fresh(threadIdx.x) >> 4 & 3) * 16 + (c * 32 + b * 16) * 4;
@@ -1078,15 +1200,16 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
-          for (int x = 0; x < 8; ++x)
-            if (r0 + c * 32 + (x >> 2) * 16 + (lane >> 4) * 4 + (x & 3) < first_row(key0 + n * 16))
-              s[n][x >> 2][x & 3] = dp[n][x >> 2][x & 3] = 0.f;
+          for (int x = 0; x < 8; ++x) {
+            const int row = (x >> 2) * 16 + (lane >> 4) * 4 + (x & 3);
+            if (r0 + c * 32 + row < first_row(key0 + n * 16)) s[n][x >> 2][x & 3] = dp[n][x >> 2][x & 3] = 0.f;
+          }
       }
 #pragma unroll
       for (int n = 0; n < 2; ++n) pack(s[n][0], s[n][1], w[n]), pack(dp[n][0], dp[n][1], wd[n]);
       ready(w);
       ready(wd);
-      add_columns2<Lds, DB, Stage::SIZE>(dk, dv, column_places + c * 32 * Lds::kPitch, wd, w);
+      add_columns2<Lds, DB, Stage::SIZE>(dk, dv, Lds::columns_place(tile, fresh(threadIdx.x)), wd, w);
     }
   }
   settle(dk);

@@ -191,7 +191,7 @@ template <class T, int DW>
 static int launch_attn_bwd(AttnArgs a, const AttnPlan& p, hipStream_t st) {
   constexpr int DP = padded(DW);
   a.splits = p.dq;
-  if (int rc = launch_attn<k_attn_dq<T, DW>, 4 * kKeys * Tile<T, DP>::kPitch>(tile_ids<128>(a.Tq * a.g, a.n_seq) * a.hk, p.dq, a, st))
+  if (int rc = launch_attn<k_attn_dq<T, DW>, 4 * kKeys * Tile<T, DP>::kPitch + 48>(tile_ids<128>(a.Tq * a.g, a.n_seq) * a.hk, p.dq, a, st))
     return rc;
   if (p.dq > 1 && a.Tq > 0) {
     const GradSum dq{a.dq, a.partials, a.scale};
@@ -199,7 +199,7 @@ static int launch_attn_bwd(AttnArgs a, const AttnPlan& p, hipStream_t st) {
     OAPL_LAUNCH_CHECK();
   }
   a.splits = p.dkdv;
-  if (int rc = launch_attn<k_attn_dkdv<T, DW>, 2 * RowStager<T, DP>::kBytes>(tile_ids<128>(a.Tk, a.n_seq) * a.hk, p.dkdv, a, st)) return rc;
+  if (int rc = launch_attn<k_attn_dkdv<T, DW>, 2 * RowStager<T, DP>::kBytes + 48>(tile_ids<128>(a.Tk, a.n_seq) * a.hk, p.dkdv, a, st)) return rc;
   if (p.dkdv > 1 && a.Tk > 0) {
     const int64_t one = a.Tk * a.hk * a.D;
     const GradSum dk{a.dk, a.partials, a.scale}, dv{a.dv, a.partials + one, 1.f};

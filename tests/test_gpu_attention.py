@@ -302,3 +302,68 @@ def test_refusals_of_the_binding():
         oapl.attention_fwd(q, k, v, o, out=torch.empty(9, 1, 64, device=DEV, dtype=q.dtype).expand(9, 4, 64))
     with pytest.raises(oapl.OaplError):
         oapl.attention_fwd(q, k, v, o, workspace=torch.empty(0, dtype=torch.uint8, device=DEV))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("n, hq, D", [(150, 4, 64), (9, 8, 128), (700, 2, 80)])
+def test_what_is_not_finite_reaches_only_who_sees_it(dtype, bad, n, hq, D):
+    """Causal: a key's or value's NaN stays out of the rows before it, a query's or gradient's out of the keys behind it."""
+    at, hk = 2 * n // 3, 2
+    o = _offsets([n])
+    before, behind = torch.arange(at, device=DEV), torch.arange(at + 1, n, device=DEV)
+    for which in range(4):
+        q, k, v = _qkv(dtype, [n], [n], hq, hk, D, seed=160)
+        dout = _normal(q.shape, q.dtype, 163)
+        want = oapl.attention_fwd(q, k, v, o)
+        grads = oapl.attention_bwd(q, k, v, want.out, want.lse, dout, o)
+        (q, k, v, dout)[which][at] = bad
+        got = oapl.attention_fwd(q, k, v, o)
+        assert torch.equal(got.out[before], want.out[before]) and torch.equal(got.lse[before], want.lse[before])
+        assert which == 3 or not bool(got.out[at].isfinite().all())
+        b = oapl.attention_bwd(q, k, v, got.out, got.lse, dout, o)
+        assert torch.equal(b.dq[before], grads.dq[before])
+        if which in (0, 3):      # row `at` alone is touched: keys behind it do not see it
+            assert torch.equal(b.dk[behind], grads.dk[behind]) and torch.equal(b.dv[behind], grads.dv[behind])
+            assert not bool(b.dv[at].isfinite().all())
+
+
+@pytest.mark.parametrize("nq, nk, hq, hk", [([300], [300], 32, 8), ([2500], [2500], 8, 1), ([64] * 16, [2000] * 16, 8, 8), ([1] * 3, [3000, 5, 900], 16, 8),
+                                            ([1000], [1000], 6, 6)])
+def test_cuts_give_the_same_in_fixed_order(nq, nk, hq, hk):
+    """Sizes whose keys or rows are split over workgroups: within the bounds, and the same bits again."""
+    _check("bf16", nq, nk, hq, hk, 128, True, seed=170)
+    q, k, v = _qkv("bf16", nq, nk, hq, hk, 128, seed=174)
+    qo, ko, dout = _offsets(nq), _offsets(nk), _normal(q.shape, q.dtype, 177)
+    a, b = (oapl.attention_fwd(q, k, v, qo, ko) for _ in range(2))
+    assert torch.equal(a.out, b.out) and torch.equal(a.lse, b.lse)
+    x, y = (oapl.attention_bwd(q, k, v, a.out, a.lse, dout, qo, ko) for _ in range(2))
+    assert all(torch.equal(s, t) for s, t in zip(x[:3], y[:3]))
+
+
+def test_in_a_graph_with_other_values():
+    """A decode step and a training step replayed: new values and cached lengths, eager work between the replays."""
+    nq, room, hq, hk, D = [1, 1, 1], 400, 8, 2, 128
+    q, k, v = _qkv("bf16", nq, [room] * 3, hq, hk, D, seed=180)
+    qo, ko, used = _offsets(nq), _offsets([room] * 3), torch.tensor([5, 400, 131], device=DEV)
+    n = [70, 200]
+    tq, tk, tv = _qkv("bf16", n, n, hq, hk, D, seed=184)
+    to, dout = _offsets(n), _normal(tq.shape, tq.dtype, 187)
+
+    def step():
+        a = oapl.attention_fwd(q, k, v, qo, ko, k_used=used)
+        b = oapl.attention_fwd(tq, tk, tv, to)
+        return [a.out, a.lse, b.out, b.lse, *oapl.attention_bwd(tq, tk, tv, b.out, b.lse, dout, to)[:3]]
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for i in range(4):
+        for j, x in enumerate((q, k, v, tq, tk, tv, dout)):
+            x.copy_(_normal(x.shape, x.dtype, 200 + 10 * i + j))
+        used.copy_(torch.tensor([i, 400 - i, 64 * (i + 1)], device=DEV))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, step()))
