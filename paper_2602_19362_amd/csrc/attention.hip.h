@@ -139,7 +139,7 @@ __device__ __forceinline__ Found pick_tile(const AttnArgs& p, TileOf what, int r
   const auto beyond = [&](int x) {
     if (x >= reach) return 0;
     if (!p.causal) return tiles;
-    if (what == kOfKeys) return min(tiles, (int)((nk - x + B - 1) / (unsigned)B));
+    if (what == kOfKeys) return min(tiles, (int)((max(nk - x, 0) + B - 1) / (unsigned)B));      // (more queries than keys: x may pass nk)
     const int token = x - (nk - nq);       // the first that sees more than x
     return tiles - (token > 0 ? (int)(token * p.g / (unsigned)B) : 0);
   };

@@ -69,6 +69,13 @@ def test_lengths(dtype, causal, nq, nk):
     _check(dtype, nq, nk, 4, 2, 64, causal)
 
 
+# Many more queries than keys beside sequences with several tiles of keys: every tile of keys has its gradients written, once.
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq, nk", [([9, 400, 300], [200, 3, 90]), ([300, 500, 30], [20, 300, 30]), ([150, 9, 600], [140, 5, 3])])
+def test_sequences_that_outgrow_their_keys(dtype, nq, nk):
+    _check(dtype, nq, nk, 4, 2, 64, True)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("hq, hk, D", [(1, 1, 8), (3, 3, 16), (5, 1, 24), (8, 2, 40), (6, 3, 72), (14, 2, 80), (2, 1, 96), (16, 2, 104),
                                        (7, 1, 120), (12, 3, 128), (48, 1, 64), (130, 1, 32)])
