@@ -657,13 +657,14 @@ __device__ __forceinline__ int64_t packed_row(const AttnArgs& p, const SeqTile& 
   return (kh * p.Tq + t.q0) * p.g + row;
 }
 
-// LDS of a forward workgroup: slots of a tile of keys and one of values, and (WK = 4) the same for every wavefront, later its results.
-template <class T, int DP, int WK>
-struct FwdLds {
-  static constexpr int kTile = kFwdKeys * Tile<T, DP>::kPitch, kSlots = WK == 4 && sizeof(T) == 4 ? 1 : 2;
+// LDS of a workgroup that walks over keys: slots of a tile of keys and one of values, and (WK = 4) the same for every wavefront, later
+// its results; words of tell_odd and clean_tile.
+template <class T, int DP, int WK, int KEYS>
+struct KeyLds {
+  static constexpr int kTile = KEYS * Tile<T, DP>::kPitch, kSlots = WK == 4 && sizeof(T) == 4 ? 1 : 2;
   static constexpr int kStages = 2 * kSlots * kTile, kResults = 32 * (DP * 4 + 16);
   static constexpr int kWave = WK == 1 || kStages > kResults ? kStages : (kResults + 511) / 512 * 512;
-  static constexpr int kWords = WK * kWave, kBytes = kWords + 48;      // words: tell_odd's, clean_tile's
+  static constexpr int kWords = WK * kWave, kBytes = kWords + 48;
   static_assert(kBytes <= 160 * 1024, "LDS of one CU");
 };
 
@@ -696,7 +697,7 @@ __global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k
   typedef typename FragOf<T>::type Frag;
   typedef Tile<T, DP> Lds;
   typedef Stager<T, DP, kFwdKeys, 4 / WK> Stage;
-  typedef FwdLds<T, DP, WK> Size;
+  typedef KeyLds<T, DP, WK, kFwdKeys> Size;
   constexpr int B = 128 / WK, KS = DW / 32, DB = DW / 16, SIZE = Size::kTile;
   extern __shared__ char smem[];
   const int kh = blockIdx.x % p.hk;
@@ -944,16 +945,47 @@ __global__ __launch_bounds__(256) void k_attn_add(const AttnArgs p, GradSum firs
 }
 
 // ---------------------------------------------------------------------------------------------------------------- backward
-// dq, and what the other kernel needs of a row: its log-sum-exp in base 2 and D_i.  A workgroup has 128 rows, as forward.
-template <class T, int DW>
+// Adds up what four wavefronts have of the same 32 rows (keys), in their order, in LDS of `each` bytes a wavefront: eight threads a row
+// get a share(row, first channel, sums) each.
+template <int DW, class F>
+__device__ __forceinline__ void add_wavefronts(const f32x4 (&acc)[2][DW / 16], lds_char_ptr lds, int each, F&& share) {
+  constexpr int PITCH = padded(DW) * 4 + 16;
+  typedef __attribute__((address_space(3))) f32x4* lds_f32x4;
+  __syncthreads();      // everybody is done with what was there
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int d = 0; d < DW / 16; ++d)
+      *(lds_f32x4)(lds + (threadIdx.x >> 6) * each + (n * 16 + (threadIdx.x & 15)) * PITCH + d * 64 + (threadIdx.x >> 4 & 3) * 16) = acc[n][d];
+  __syncthreads();
+  const int r = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * (DW / 8);
+  f32x4 x[DW / 32] = {};
+#pragma unroll
+  for (int w = 0; w < 4; ++w)
+#pragma unroll
+    for (int c = 0; c < DW / 32; ++c) x[c] += *(lds_f32x4)(lds + w * each + r * PITCH + (c0 + c * 4) * 4);
+  share(r, c0, x);
+}
+template <class T, int N>
+__device__ __forceinline__ void store_share(char* row, int c0, const f32x4 (&x)[N], float factor, int D) {
+#pragma unroll
+  for (int c = 0; c < N; ++c)
+    if (c0 + c * 4 < D) store4((T*)row + c0 + c * 4, x[c] * factor);
+}
+
+// dq, and what the other kernel needs of a row: its log-sum-exp in base 2 and D_i.  A workgroup has 128 rows over steps of 64 keys or,
+// where tiles are few (WK = 4), 32 rows over steps of 32 keys that the wavefronts take in turn, as forward.
+template <class T, int DW, int WK>
 __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
-  constexpr int DP = padded(DW);
+  constexpr int DP = padded(DW), KEYS = kKeys / (WK == 1 ? 1 : 2);
   typedef typename FragOf<T>::type Frag;
   typedef Tile<T, DP> Lds;
-  typedef Stager<T, DP, kKeys, 4> Stage;
-  constexpr int B = 128, KS = DW / 32, DB = DW / 16, SIZE = kKeys * Lds::kPitch;
+  typedef Stager<T, DP, KEYS, 4 / WK> Stage;
+  typedef KeyLds<T, DP, WK, KEYS> Size;
+  constexpr int B = 128 / WK, KS = DW / 32, DB = DW / 16, SIZE = Size::kTile;
   extern __shared__ char smem[];
-  const lds_char_ptr lds = (lds_char_ptr)smem;
+  const int wave = uniform((int)threadIdx.x >> 6);
+  const lds_char_ptr lds = (lds_char_ptr)smem + (WK == 1 ? 0 : wave * Size::kWave), words = (lds_char_ptr)smem + Size::kWords;
   const int kh = blockIdx.x % p.hk;
   SeqTile t;
   const Found found = pick_tile<B>(p, kOfRows, blockIdx.x / p.hk, t);
@@ -961,10 +993,15 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
   if (found == kMalformed) poison<T>(p.dq, p.Tq, p.hq, p.D);
   if (found != kTile) return;
   const int first_sees = all_rows_see(p, t), last_sees = tile_sees<B>(p, t);
-  const Part part(last_sees, p.splits, blockIdx.y, kKeys);
+  const Part part(last_sees, p.splits, blockIdx.y, KEYS * WK);
   const Stage ks(p.k.row(t.k0, kh), p.k.token, p.D), vs(p.v.row(t.k0, kh), p.v.token, p.D);
-  if (part.begin < part.end) ks.start(lds, part.begin, t.nk), vs.start(lds + SIZE, part.begin, t.nk);
-  const int group = threadIdx.x >> 4 & 3, row0 = t.first + (threadIdx.x >> 6) * 32 + (threadIdx.x & 15);
+  int j0 = part.begin + (WK == 1 ? 0 : wave * KEYS), slot = 0;
+  const auto stage = [&](int at, int first) {
+    ks.start(lds + at, first, t.nk);
+    vs.start(lds + at + SIZE, first, t.nk);
+  };
+  if (Size::kSlots == 2 && j0 < part.end) stage(0, j0);
+  const int group = threadIdx.x >> 4 & 3, row0 = t.first + (WK == 1 ? wave * 32 : 0) + (threadIdx.x & 15);
   const float scale2 = p.scale * kLog2e;
   int row_sees[2];
   Frag q[2][KS], dout[2][KS];
@@ -987,7 +1024,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
     for (int kk = 0; kk < KS; ++kk) delta[n] += dot(o[kk], dout[n][kk]);
     delta[n] = row_sum(delta[n]);
     lse2[n] = row.exists ? p.lse[token * p.hq + head] * kLog2e : 0.f;
-    if (row.exists && group == 0 && blockIdx.y == 0) {
+    if (row.exists && group == 0 && blockIdx.y == 0 && (WK == 1 || wave == 0)) {
       const int64_t at = packed_row(p, t, kh, row0 + n * 16);
       p.delta[at] = delta[n];
       // of a row that sees nothing: every probability comes out as 0
@@ -1002,19 +1039,19 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
     all_see = y < all_see ? y : all_see;
   }
   all_see = __builtin_amdgcn_readfirstlane(all_see);
-  int slot = 0;
-  for (int j0 = part.begin; j0 < part.end; j0 += kKeys, slot ^= 2 * SIZE) {
-    const bool masks = first_sees < last_sees && j0 + kKeys > first_sees;
-    const lds_char_ptr words = lds + 4 * SIZE;
+  for (; j0 < part.end; j0 += KEYS * WK, slot ^= Size::kSlots == 2 ? 2 * SIZE : 0) {
+    const bool masks = first_sees < last_sees && j0 + KEYS > first_sees;
+    if (Size::kSlots == 1) stage(0, j0);
     staged();
-    if (masks) tell_odd(words, slot != 0, staged_odd<T, Stage::kLoads, 4>(lds + slot));
-    lds_barrier();
-    if (j0 + kKeys < part.end) {
-      ks.start(lds + (slot ^ 2 * SIZE), j0 + kKeys, t.nk);
-      vs.start(lds + (slot ^ 2 * SIZE) + SIZE, j0 + kKeys, t.nk);
+    bool found_odd = masks && staged_odd<T, Stage::kLoads, 4 / WK>(lds + slot);
+    if (WK == 1) {
+      if (masks) tell_odd(words, slot != 0, found_odd);
+      lds_barrier();
+      found_odd = masks && told_odd(words, slot != 0);
     }
+    if (Size::kSlots == 2 && j0 + KEYS * WK < part.end) stage(slot ^ 2 * SIZE, j0 + KEYS * WK);
     const int k_rows = Lds::rows_place(lds + slot, threadIdx.x), k_columns = Lds::columns_place(lds + slot, threadIdx.x);
-    const uint64_t odd = masks && told_odd(words, slot != 0) ? clean_tile<T, DP, kKeys, 4>(lds + slot, words + 32) : 0;
+    const uint64_t odd = found_odd ? clean_tile<T, DP, KEYS, 4 / WK>(lds + slot, words + 32) : 0;
     f32x4 s[2][2][2], dp[2][2][2];     // [half][rows][keys]
     Frag w[2][2];
     const auto finish = [&](int c, int i) {
@@ -1043,36 +1080,51 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
     };
     scores<Lds, KS>(s[0], k_rows, 0, q, [](int) {});
     scores<Lds, KS>(dp[0], k_rows, SIZE, dout, [](int) {});
-    scores<Lds, KS>(s[1], k_rows, 32 * Lds::kPitch, q, [&](int i) { share(0, 0, 8, i, 2 * KS); });
-    scores<Lds, KS>(dp[1], k_rows, SIZE + 32 * Lds::kPitch, dout, [&](int i) { share(0, 8, 16, i, 2 * KS); });
+    if constexpr (KEYS == 64) {
+      scores<Lds, KS>(s[1], k_rows, 32 * Lds::kPitch, q, [&](int i) { share(0, 0, 8, i, 2 * KS); });
+      scores<Lds, KS>(dp[1], k_rows, SIZE + 32 * Lds::kPitch, dout, [&](int i) { share(0, 8, 16, i, 2 * KS); });
+    } else {
+      share(0, 0, 16, 0, 1);
+    }
     mask(0);
-    add_columns<Lds, DB>(dq, k_columns, 0, w[0], [&](int i) { share(1, 0, 16, i, DB); });
-    mask(1);
-    add_columns<Lds, DB>(dq, k_columns, 32 * Lds::kPitch, w[1], [](int) {});
+    add_columns<Lds, DB>(dq, k_columns, 0, w[0], [&](int i) {
+      if (KEYS == 64) share(1, 0, 16, i, DB);
+    });
+    if constexpr (KEYS == 64) {
+      mask(1);
+      add_columns<Lds, DB>(dq, k_columns, 32 * Lds::kPitch, w[1], [](int) {});
+    }
   }
   settle(dq);
+  if constexpr (WK == 1) {
 #pragma unroll
-  for (int n = 0; n < 2; ++n) {
-    const Row row(p, t, row0 + n * 16);
-    if (!row.exists) continue;
-    if (p.splits > 1) store_columns<float>((char*)partial_row(p, p.Tq * p.hq, packed_row(p, t, kh, row0 + n * 16)), dq[n], 1.f, p.D);
-    else store_columns<T>(p.dq.row(t.q0 + row.token, kh * p.g + row.head), dq[n], p.scale, p.D);
+    for (int n = 0; n < 2; ++n) {
+      const Row row(p, t, row0 + n * 16);
+      if (!row.exists) continue;
+      if (p.splits > 1) store_columns<float>((char*)partial_row(p, p.Tq * p.hq, packed_row(p, t, kh, row0 + n * 16)), dq[n], 1.f, p.D);
+      else store_columns<T>(p.dq.row(t.q0 + row.token, kh * p.g + row.head), dq[n], p.scale, p.D);
+    }
+  } else {
+    add_wavefronts<DW>(dq, (lds_char_ptr)smem, Size::kWave, [&](int r, int c0, const auto& x) {
+      const Row row(p, t, t.first + r);
+      if (!row.exists) return;
+      if (p.splits > 1) store_share<float>((char*)partial_row(p, p.Tq * p.hq, packed_row(p, t, kh, t.first + r)), c0, x, 1.f, p.D);
+      else store_share<T>(p.dq.row(t.q0 + row.token, kh * p.g + row.head), c0, x, p.scale, p.D);
+    });
   }
 }
 
-constexpr int kRows = 64;    // rows staged at a time
-
 // Rows of two operands (queries and the output's gradient) and the rows' two numbers on their way to LDS, as Stager; what lies
 // behind the sequence's last row or channel D reads as zeros.
-template <class T, int DP>
+template <class T, int DP, int R, int W>
 struct RowStager {
   typedef Tile<T, DP> Lds;
-  static constexpr int kRowsPerLoad = 64 / Lds::kChunks, kLoads = kRows / (4 * kRowsPerLoad), SIZE = kRows * Lds::kPitch;
-  static constexpr int kBytes = 2 * SIZE + 2 * kRows * 4;
+  static constexpr int kRowsPerLoad = 64 / Lds::kChunks, kLoads = R / (W * kRowsPerLoad), SIZE = R * Lds::kPitch;
+  static constexpr int kBytes = 2 * SIZE + 2 * 64 * 4;      // a load of numbers has 64
   static constexpr uint32_t kOutside = 0x80000000u;
-  // Starts the loads of rows [first, first + 64); `first` is a multiple of 64.
+  // Starts the loads of rows [first, first + R); `first` is a multiple of R.
   __device__ static __forceinline__ void start(const AttnArgs& p, const SeqTile& t, int kh, lds_char_ptr lds, int first) {
-    const int wave = uniform((int)threadIdx.x >> 6), rows = t.nq * p.g, token0 = uniform(by_group(p, first));
+    const int wave = W == 1 ? 0 : uniform((int)threadIdx.x >> 6), rows = t.nq * p.g, token0 = uniform(by_group(p, first));
     const __amdgpu_buffer_rsrc_t q =
         __builtin_amdgcn_make_buffer_rsrc((void*)p.q.row(t.q0 + token0, kh * p.g), 0, kOutside, 0x00020000);
     const __amdgpu_buffer_rsrc_t d =
@@ -1080,51 +1132,67 @@ struct RowStager {
     const int lane = fresh(threadIdx.x) & 63;      // what follows is made here, not kept: registers are short
     // Where the heads in a group divide the rows that lie between two loads of a wavefront, a lane is at the same place of a token's
     // heads with every load, and only the (scalar) token moves.
-    if (4 * kRowsPerLoad % 16 == 0 && p.g <= 4 * kRowsPerLoad && (p.g & (p.g - 1)) == 0 && first + kRows <= rows) {
-      const int tokens = by_group(p, 4 * kRowsPerLoad), r = wave * kRowsPerLoad + lane / Lds::kChunks, token = by_group(p, r);
+    if (W * kRowsPerLoad % 16 == 0 && p.g <= W * kRowsPerLoad && (p.g & (p.g - 1)) == 0 && first + R <= rows) {
+      const int tokens = by_group(p, W * kRowsPerLoad), r = wave * kRowsPerLoad + lane / Lds::kChunks, token = by_group(p, r);
       const int c = ((lane % Lds::kChunks) ^ Lds::swizzle(r)) * 16, head = r - token * p.g;
       const bool any = c < p.D * (int)sizeof(T);
       const uint32_t whole_q = any ? (uint32_t)(token * (int)p.q.token + head * (int)p.q.head + c) : kOutside;
       const uint32_t whole_d = any ? (uint32_t)(token * (int)p.dout.token + head * (int)p.dout.head + c) : kOutside;
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) {
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(q, (lds_void_ptr)(lds + (j * 4 + wave) * 1024), 16, whole_q,
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(q, (lds_void_ptr)(lds + (j * W + wave) * 1024), 16, whole_q,
                                                  j * tokens * (int)p.q.token, 0, 0);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(d, (lds_void_ptr)(lds + SIZE + (j * 4 + wave) * 1024), 16, whole_d,
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(d, (lds_void_ptr)(lds + SIZE + (j * W + wave) * 1024), 16, whole_d,
                                                  j * tokens * (int)p.dout.token, 0, 0);
       }
     } else {
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) {
-        const int r = (j * 4 + wave) * kRowsPerLoad + lane / Lds::kChunks, x = first + r;
+        const int r = (j * W + wave) * kRowsPerLoad + lane / Lds::kChunks, x = first + r;
         const int c = ((lane % Lds::kChunks) ^ Lds::swizzle(r)) * 16;
         const int token = by_group(p, x), head = x - token * p.g;
         const bool any = x < rows && c < p.D * (int)sizeof(T);
         const uint32_t vq = (uint32_t)((token - token0) * (int)p.q.token + head * (int)p.q.head + c);
         const uint32_t vd = (uint32_t)((token - token0) * (int)p.dout.token + head * (int)p.dout.head + c);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(q, (lds_void_ptr)(lds + (j * 4 + wave) * 1024), 16, any ? vq : kOutside, 0, 0, 0);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(d, (lds_void_ptr)(lds + SIZE + (j * 4 + wave) * 1024), 16, any ? vd : kOutside, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(q, (lds_void_ptr)(lds + (j * W + wave) * 1024), 16, any ? vq : kOutside, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(d, (lds_void_ptr)(lds + SIZE + (j * W + wave) * 1024), 16, any ? vd : kOutside, 0, 0, 0);
       }
     }
-    if (wave < 2) {
-      const int left = rows - first < kRows ? rows - first : kRows;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      if (W > 1 && wave != which) continue;
+      const int left = rows - first < R ? rows - first : R;
       const __amdgpu_buffer_rsrc_t n =
-          __builtin_amdgcn_make_buffer_rsrc((void*)((wave ? p.delta : p.lse2) + packed_row(p, t, kh, first)), 0, left * 4, 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(n, (lds_void_ptr)(lds + 2 * SIZE + wave * kRows * 4), 4, lane * 4, 0, 0, 0);
+          __builtin_amdgcn_make_buffer_rsrc((void*)((which ? p.delta : p.lse2) + packed_row(p, t, kh, first)), 0, left * 4, 0x00020000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(n, (lds_void_ptr)(lds + 2 * SIZE + which * 256), 4, lane * 4, 0, 0, 0);
     }
   }
 };
 
-// dk and dv: a workgroup has 128 keys, 32 a wavefront, over all rows that see any of them, 64 at a time.
-template <class T, int DW>
+// LDS of a workgroup for dk and dv, as KeyLds.
+template <class T, int DP, int WK>
+struct RowLds {
+  static constexpr int kRows = WK == 1 ? 64 : 32, kSlots = WK == 4 && sizeof(T) == 4 ? 1 : 2;
+  typedef RowStager<T, DP, kRows, 4 / WK> Stage;
+  static constexpr int kStages = kSlots * Stage::kBytes, kResults = 32 * (DP * 4 + 16);
+  static constexpr int kWave = WK == 1 || kStages > kResults ? kStages : (kResults + 511) / 512 * 512;
+  static constexpr int kWords = WK * kWave, kBytes = kWords + 48;
+  static_assert(kBytes <= 160 * 1024, "LDS of one CU");
+};
+
+// dk and dv: a workgroup has 128 keys, 32 a wavefront, over all rows that see any of them, 64 at a time; or (WK = 4) 32 keys, over
+// steps of 32 rows that the wavefronts take in turn.
+template <class T, int DW, int WK>
 __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   constexpr int DP = padded(DW);
   typedef typename FragOf<T>::type Frag;
   typedef Tile<T, DP> Lds;
-  typedef RowStager<T, DP> Stage;
-  constexpr int B = 128, KS = DW / 32, DB = DW / 16;
+  typedef RowLds<T, DP, WK> Size;
+  typedef typename Size::Stage Stage;
+  constexpr int B = 128 / WK, KS = DW / 32, DB = DW / 16, kRows = Size::kRows;
   extern __shared__ char smem[];
-  const lds_char_ptr lds = (lds_char_ptr)smem;
+  const int wave = uniform((int)threadIdx.x >> 6), tile_wave = WK == 1 ? wave : 0;
+  const lds_char_ptr lds = (lds_char_ptr)smem + (WK == 1 ? 0 : wave * Size::kWave), words = (lds_char_ptr)smem + Size::kWords;
   const int kh = blockIdx.x % p.hk;
   SeqTile t;
   const Found found = pick_tile<B>(p, kOfKeys, blockIdx.x / p.hk, t);
@@ -1136,16 +1204,17 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   const int rows = t.nq * p.g, ahead = t.nk - t.nq;
   // the first row that sees the tile's first key, and whole tiles of rows
   const int from = p.causal && t.first > ahead ? (t.first - ahead) * p.g / kRows * kRows : 0;
-  const Part part(rows > from ? rows - from : 0, p.splits, blockIdx.y, kRows);
-  if (part.begin < part.end) Stage::start(p, t, kh, lds, from + part.begin);
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Part part(rows > from ? rows - from : 0, p.splits, blockIdx.y, kRows * WK);
+  const int end = from + part.end;
+  int r0 = from + part.begin + (WK == 1 ? 0 : wave * kRows), slot = 0;
+  if (Size::kSlots == 2 && r0 < end) Stage::start(p, t, kh, lds, r0);
   Frag k[2][KS], v[2][KS];
   f32x4 dk[2][DB], dv[2][DB];
   const auto first_row = [&](int key) { return p.causal && key < t.nk && key > ahead ? (key - ahead) * p.g : 0; };   // that sees it
   int all_from = 0;     // rows from here on see every key of the wavefront
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
-    const int key = t.first + wave * 32 + n * 16 + (threadIdx.x & 15), at = key < t.nk ? key : t.nk - 1;
+    const int key = t.first + tile_wave * 32 + n * 16 + (threadIdx.x & 15), at = key < t.nk ? key : t.nk - 1;
 #pragma unroll
     for (int d = 0; d < DB; ++d) zero(dk[n][d]), zero(dv[n][d]);
     load_row<T>(p.k.row(t.k0 + at, kh), p.D, k[n]);
@@ -1160,33 +1229,35 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   all_from = __builtin_amdgcn_readfirstlane(all_from);
   const float scale2 = p.scale * kLog2e;
   const int masked_to = first_row((t.first + B < t.nk ? t.first + B : t.nk) - 1);      // rows from here on see every key of the workgroup
-  int slot = 0;
-  for (int r0 = from + part.begin; r0 < from + part.end; r0 += kRows, slot ^= 1) {
-    const lds_char_ptr words = lds + 2 * Stage::kBytes;
+  for (; r0 < end; r0 += kRows * WK, slot ^= Size::kSlots == 2) {
+    const lds_char_ptr tiles = lds + slot * Stage::kBytes, numbers = tiles + 2 * Stage::SIZE;
+    if (Size::kSlots == 1) Stage::start(p, t, kh, lds, r0);
     staged();
-    if (r0 < masked_to)
-      tell_odd(words, slot, staged_odd<T, Stage::kLoads, 4>(lds + slot * Stage::kBytes) ||
-                                staged_odd<T, Stage::kLoads, 4>(lds + slot * Stage::kBytes + Stage::SIZE));
-    lds_barrier();
-    if (r0 + kRows < from + part.end) Stage::start(p, t, kh, lds + (slot ^ 1) * Stage::kBytes, r0 + kRows);
-    const lds_char_ptr numbers = lds + slot * Stage::kBytes + 2 * Stage::SIZE;
-    if (r0 < masked_to && told_odd(words, slot)) {      // a row's probabilities are NaN where its log-sum-exp is
-      typedef __attribute__((address_space(3))) float* lds_f32;
-      const uint64_t odd = clean_tile<T, DP, kRows, 4, 2, Stage::SIZE>(lds + slot * Stage::kBytes, words + 32);
-      if (threadIdx.x < kRows && (odd >> threadIdx.x & 1)) ((lds_f32)numbers)[threadIdx.x] = quiet_nan();
+    bool odd = r0 < masked_to && (staged_odd<T, Stage::kLoads, 4 / WK>(tiles) || staged_odd<T, Stage::kLoads, 4 / WK>(tiles + Stage::SIZE));
+    if (WK == 1) {
+      if (r0 < masked_to) tell_odd(words, slot, odd);
       lds_barrier();
+      odd = r0 < masked_to && told_odd(words, slot);
+    }
+    if (Size::kSlots == 2 && r0 + kRows * WK < end) Stage::start(p, t, kh, lds + (slot ^ 1) * Stage::kBytes, r0 + kRows * WK);
+    if (odd) {      // a row's probabilities are NaN where its log-sum-exp is
+      typedef __attribute__((address_space(3))) float* lds_f32;
+      const uint64_t which = clean_tile<T, DP, kRows, 4 / WK, 2, Stage::SIZE>(tiles, words + 32);
+      const int x = WK == 1 ? threadIdx.x : threadIdx.x & 63;
+      if (x < kRows && (which >> x & 1)) ((lds_f32)numbers)[x] = quiet_nan();
+      if (WK == 1) lds_barrier();
     }
 #pragma unroll 1
     for (int c = 0; c < kRows / 32; ++c) {
       typedef __attribute__((address_space(3))) f32x4* ptr;
-      const lds_char_ptr tile = lds + slot * Stage::kBytes + c * 32 * Lds::kPitch;
+      const lds_char_ptr tile = tiles + c * 32 * Lds::kPitch;
       Frag w[2], wd[2];      // probabilities and dS of 32 rows, keys in columns
       f32x4 s[2][2], dp[2][2];     // [keys][rows]
       scores2<Lds, KS, Stage::SIZE>(s, dp, Lds::rows_place(tile, fresh(threadIdx.x)), k, v);      // places are not kept: registers are short
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const lds_char_ptr at = numbers + (fresh(threadIdx.x) >> 4 & 3) * 16 + (c * 32 + b * 16) * 4;
-        const f32x4 lse2 = *(ptr)at, delta = *(ptr)(at + kRows * 4);
+        const f32x4 lse2 = *(ptr)at, delta = *(ptr)(at + 256);
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -1196,7 +1267,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
           }
       }
       if (r0 + c * 32 < all_from) {
-        const int lane = fresh(threadIdx.x) & 63, key0 = t.first + wave * 32 + (lane & 15);
+        const int lane = fresh(threadIdx.x) & 63, key0 = t.first + tile_wave * 32 + (lane & 15);
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -1214,18 +1285,31 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   }
   settle(dk);
   settle(dv);
+  if constexpr (WK == 1) {
 #pragma unroll
-  for (int n = 0; n < 2; ++n) {
-    const int key = t.first + wave * 32 + n * 16 + (threadIdx.x & 15);
-    if (key >= t.nk) continue;
-    if (p.splits > 1) {
-      float* to = partial_row(p, 2 * p.Tk * p.hk, kh * p.Tk + t.k0 + key);
-      store_columns<float>((char*)to, dk[n], 1.f, p.D);
-      store_columns<float>((char*)(to + p.Tk * p.hk * p.D), dv[n], 1.f, p.D);
-      continue;
+    for (int n = 0; n < 2; ++n) {
+      const int key = t.first + wave * 32 + n * 16 + (threadIdx.x & 15);
+      if (key >= t.nk) continue;
+      if (p.splits > 1) {
+        float* to = partial_row(p, 2 * p.Tk * p.hk, kh * p.Tk + t.k0 + key);
+        store_columns<float>((char*)to, dk[n], 1.f, p.D);
+        store_columns<float>((char*)(to + p.Tk * p.hk * p.D), dv[n], 1.f, p.D);
+        continue;
+      }
+      store_columns<T>(p.dk.row(t.k0 + key, kh), dk[n], p.scale, p.D);
+      store_columns<T>(p.dv.row(t.k0 + key, kh), dv[n], 1.f, p.D);
     }
-    store_columns<T>(p.dk.row(t.k0 + key, kh), dk[n], p.scale, p.D);
-    store_columns<T>(p.dv.row(t.k0 + key, kh), dv[n], 1.f, p.D);
+  } else {
+    const auto share = [&](const Heads& out, int64_t behind, float factor) {
+      return [&p, &t, &out, kh, behind, factor](int r, int c0, const auto& x) {
+        const int key = t.first + r;
+        if (key >= t.nk) return;
+        if (p.splits > 1) store_share<float>((char*)(partial_row(p, 2 * p.Tk * p.hk, kh * p.Tk + t.k0 + key) + behind), c0, x, 1.f, p.D);
+        else store_share<T>(out.row(t.k0 + key, kh), c0, x, factor, p.D);
+      };
+    };
+    add_wavefronts<DW>(dk, (lds_char_ptr)smem, Size::kWave, share(p.dk, 0, p.scale));
+    add_wavefronts<DW>(dv, (lds_char_ptr)smem, Size::kWave, share(p.dv, p.Tk * p.hk * p.D, 1.f));
   }
 }
 

@@ -75,7 +75,7 @@ static int rope_args(NormRopeArgs& a, const oapl_heads* q, const oapl_heads* k, 
 // What a call of average sequences is cut into; nothing more is known here of them.  Microseconds below: bf16, 128 channels, equal lengths,
 // as replayed graphs on one MI355X.
 struct AttnPlan {
-  bool few = false;                    // tiles of 32 rows whose wavefronts share the keys
+  bool few = false, few_dq = false, few_dkdv = false;      // tiles of 32 rows (keys) whose wavefronts share the steps
   int fwd = 1, dq = 1, dkdv = 1;       // workgroups that share a tile's steps
   size_t off_lse2 = 0, off_delta = 0, off_sums = 0, off_partials = 0, total = 0;
 };
@@ -99,12 +99,21 @@ static void attn_cut(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int g, int 
   // tokens, 32 on 8 (256 of 31), 1 part 35, 2 41.
   p.fwd = p.few ? attn_splits(256 / tiles(rows, 32), Tk / seqs / (4 * kFwdKeys), 3)
                 : attn_splits(1024 / tiles(rows, 128), Tk / seqs / kFwdKeys, 32);
-  // dq: parts of keys are rarely worth their sums.  One sequence of 1000 tokens, 6 heads (48 tiles of 15 steps), 1 part 59, 3 50 with
-  // dk, dv; 300 tokens, 32 on 8 (80 of 4), 1 part 70, 2 74.
-  p.dq = attn_splits(192 / tiles(rows, 128), Tk / seqs / kKeys, 4);
-  // dk, dv: two workgroups a compute unit, walks over the rows of all heads of a group.  300 tokens, 32 on 8 (24 tiles of 18 steps), 1
-  // part 70, 4 50, 8 49; 2500 (160 of 156), 1 part 424, 4 231, 8 247; 4000, 8 on one (32 of 500), 1 part 1151, 8 261, 16 224.
-  p.dkdv = attn_splits((511 + tiles(Tk, 128)) / tiles(Tk, 128), rows / seqs / kRows, 4);
+  // dq: tiles of 32 rows where those are one round.  1000 tokens, 6 heads (192 small tiles) with dk, dv, 32 rows 49, 128 rows 55 (at its
+  // best split); 300, 32 on 8 (304) 78 / 78; 4 of 300, 8 heads (320) 43 / 41; 1000, 32 on 8 (1000) 213 / 199.
+  p.few_dq = tiles(rows, 32) <= 256;
+  p.dq = p.few_dq ? attn_splits(256 / tiles(rows, 32), Tk / seqs / (2 * kKeys), 4)
+                  : attn_splits(192 / tiles(rows, 128), Tk / seqs / kKeys, 4);
+  // dk, dv: tiles of 32 keys up to a work of 64 rows x 64 steps a compute unit (their wavefronts have a SIMD each, which costs rate and
+  // saves time where work is short).  32 keys / 128 keys a tile, each at its best split: 300 tokens, 32 on 8 (80 small tiles of 18 steps)
+  // 40 / 49; 4 of 300, 32 on 8 (320 of 18) 49 / 65; 1000, 6 heads (192 of 15) 42 / 51; 1000, 32 on 8 (256 of 62) 89 / 96; 4000, 8 on
+  // one (125 of 500) 299 / 243; 2500, 32 on 8 (632 of 156) 282 / 243.
+  p.few_dkdv = tiles(Tk, 32) * std::max<int64_t>(1, rows / seqs / 64) <= 256 * 64;
+  // ... in parts of the rows.  Small tiles: 300 tokens, 4 on one (10 of 18), 1 part 43, 4 35, 8 33; 80 of 18, 1 part 42, 2 40, 4 44; 320 of
+  // 18, 1 part 49, 2 67.  Large ones, two workgroups a compute unit: 2500, 32 on 8 (160 of 156), 1 part 462, 4 243, 8 258; 4000, 8 on one (32
+  // of 500), 1 part 1271, 8 290, 16 243.
+  p.dkdv = p.few_dkdv ? attn_splits(256 / tiles(Tk, 32), rows / seqs / 128, 1)
+                      : attn_splits((511 + tiles(Tk, 128)) / tiles(Tk, 128), rows / seqs / 64, 4);
 }
 
 static bool attn_plan(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int hq, int hk, int D, int dtype, bool bwd) {
@@ -179,8 +188,8 @@ static int launch_attn_fwd(AttnArgs a, const AttnPlan& p, hipStream_t st) {
   a.splits = p.fwd;
   const int64_t rows = a.Tq * a.g;
   constexpr int DP = padded(DW);
-  const int rc = p.few ? launch_attn<k_attn_fwd<T, DW, 4>, FwdLds<T, DP, 4>::kBytes>(tile_ids<32>(rows, a.n_seq) * a.hk, p.fwd, a, st)
-                       : launch_attn<k_attn_fwd<T, DW, 1>, FwdLds<T, DP, 1>::kBytes>(tile_ids<128>(rows, a.n_seq) * a.hk, p.fwd, a, st);
+  const int rc = p.few ? launch_attn<k_attn_fwd<T, DW, 4>, KeyLds<T, DP, 4, kFwdKeys>::kBytes>(tile_ids<32>(rows, a.n_seq) * a.hk, p.fwd, a, st)
+                       : launch_attn<k_attn_fwd<T, DW, 1>, KeyLds<T, DP, 1, kFwdKeys>::kBytes>(tile_ids<128>(rows, a.n_seq) * a.hk, p.fwd, a, st);
   if (rc != OAPL_OK || p.fwd == 1 || a.Tq == 0) return rc;
   k_attn_join<T><<<grid1d(a.Tq * a.hq, 8), 256, 0, st>>>(a);
   OAPL_LAUNCH_CHECK();
@@ -191,15 +200,19 @@ template <class T, int DW>
 static int launch_attn_bwd(AttnArgs a, const AttnPlan& p, hipStream_t st) {
   constexpr int DP = padded(DW);
   a.splits = p.dq;
-  if (int rc = launch_attn<k_attn_dq<T, DW>, 4 * kKeys * Tile<T, DP>::kPitch + 48>(tile_ids<128>(a.Tq * a.g, a.n_seq) * a.hk, p.dq, a, st))
-    return rc;
+  const int64_t rows = a.Tq * a.g;
+  int rc = p.few_dq ? launch_attn<k_attn_dq<T, DW, 4>, KeyLds<T, DP, 4, kKeys / 2>::kBytes>(tile_ids<32>(rows, a.n_seq) * a.hk, p.dq, a, st)
+                    : launch_attn<k_attn_dq<T, DW, 1>, KeyLds<T, DP, 1, kKeys>::kBytes>(tile_ids<128>(rows, a.n_seq) * a.hk, p.dq, a, st);
+  if (rc != OAPL_OK) return rc;
   if (p.dq > 1 && a.Tq > 0) {
     const GradSum dq{a.dq, a.partials, a.scale};
     k_attn_add<T><<<grid1d(a.Tq * a.hq, 8), 256, 0, st>>>(a, dq, dq, a.Tq * a.hq * a.D, a.Tq, a.g);
     OAPL_LAUNCH_CHECK();
   }
   a.splits = p.dkdv;
-  if (int rc = launch_attn<k_attn_dkdv<T, DW>, 2 * RowStager<T, DP>::kBytes + 48>(tile_ids<128>(a.Tk, a.n_seq) * a.hk, p.dkdv, a, st)) return rc;
+  rc = p.few_dkdv ? launch_attn<k_attn_dkdv<T, DW, 4>, RowLds<T, DP, 4>::kBytes>(tile_ids<32>(a.Tk, a.n_seq) * a.hk, p.dkdv, a, st)
+                  : launch_attn<k_attn_dkdv<T, DW, 1>, RowLds<T, DP, 1>::kBytes>(tile_ids<128>(a.Tk, a.n_seq) * a.hk, p.dkdv, a, st);
+  if (rc != OAPL_OK) return rc;
   if (p.dkdv > 1 && a.Tk > 0) {
     const int64_t one = a.Tk * a.hk * a.D;
     const GradSum dk{a.dk, a.partials, a.scale}, dv{a.dv, a.partials + one, 1.f};
