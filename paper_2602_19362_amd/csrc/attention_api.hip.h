@@ -85,13 +85,15 @@ static int attn_splits(int64_t want, int64_t steps, int64_t least) {
   return (int)std::max<int64_t>(1, std::min<int64_t>({want, steps / least, 64}));
 }
 
-static void attn_cut(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int g, int hk) {
+static void attn_cut(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int g, int hk, bool f32) {
   const int64_t seqs = std::max(n_seq, 1), rows = Tq * g;
   const auto tiles = [&](int64_t n, int64_t b) { return std::max<int64_t>(1, (n + seqs * b - 1) / (seqs * b)) * seqs * hk; };
   // Tiles of 32 rows: for few rows, and where they are one round of workgroups (160 KB of LDS: one a compute unit) however many.
   // 32 rows / 128 rows a tile: 16 sequences of 64 rows over 2000 keys, 8 key heads (256 small tiles) 29 / 34 (at its best split), of 96 rows
   // (384) 51 / 42; one sequence of 1000 tokens, 8 heads on one (250) 11 / 19, 6 on 6 (192) 11 / 17, 32 on 8 (1000) 42 / 35.
-  p.few = rows <= seqs * 32 || tiles(rows, 32) <= 256;
+  // fp32 products take nine times as long, and all small tiles cost is hidden behind them for longer: 4 of 400 tokens, 6 heads on 2 (304)
+  // 24 / 50; 2 of 1000, 16 on 8 (1008) 57 / 85; 4 of 2000, 8 on 2 (2000) 353 / 381; 4 of 4000, 8 heads (4000) 1248 / 1109.
+  p.few = rows <= seqs * 32 || tiles(rows, 32) <= (f32 ? 2048 : 256);
   // ... their keys in parts that fill that round: one token over 4096 / 32768 keys, 8 key heads, in 1 part 33 / 216, 8 parts 14 / 38, 16
   // parts 13 / 31; 8 over 32768, 1 part 388, 4 181, 8 185; 24 over 4096 (192 tiles), 1 part 85, 2 96.  Short parts cost more to
   // put together than they save: 4 x 32 rows over 2000 keys, 4 parts 16, 8 parts (of two steps) 21.
@@ -99,20 +101,27 @@ static void attn_cut(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int g, int 
   // tokens, 32 on 8 (256 of 31), 1 part 35, 2 41.
   p.fwd = p.few ? attn_splits(256 / tiles(rows, 32), Tk / seqs / (4 * kFwdKeys), 3)
                 : attn_splits(1024 / tiles(rows, 128), Tk / seqs / kFwdKeys, 32);
-  // dq: tiles of 32 rows where those are one round.  1000 tokens, 6 heads (192 small tiles) with dk, dv, 32 rows 49, 128 rows 55 (at its
-  // best split); 300, 32 on 8 (304) 78 / 78; 4 of 300, 8 heads (320) 43 / 41; 1000, 32 on 8 (1000) 213 / 199.
-  p.few_dq = tiles(rows, 32) <= 256;
+  // dq: tiles of 32 rows up to two rounds.  With dk, dv, 32 rows / 128 rows a tile, each at its best split: 1000 tokens, 6 heads (192
+  // small tiles) 49 / 55; 1200, 8 heads (304) 62 / 68; 300, 32 on 8 (304) 78 / 78; 4 of 1000, 4 on one (500) 187 / 192; 4800, 8 on 2
+  // (1200) 280 / 250; 1000, 32 on 8 (1000) 213 / 199.  fp32, one part: 4 of 400, 6 on 2 (304) 290 / 338; 2 of 1000, 16 on 8 (1008) 361 / 401;
+  // 8 of 600, 8 on 2 (1200) 981 / 942.
+  p.few_dq = tiles(rows, 32) <= (f32 ? 1024 : 512);
+  // ... in parts of the keys.  Small tiles: 16 rows over 4096 keys (2 of 32 steps), 1 part 50, 4 30, 8 25; 64 rows over 1024 (8 of 8), 1
+  // part 28, 2 27; 2000 tokens, one head (63 of 15), 1 part 56, 2 52; 192 of 7, 1 part 49, 2 52.  Large ones: 9000, 4 on one (282 of 140), 1
+  // part 473, 2 416, 3 392; 1000, 32 on 8 (256 of 15), 1 part 199, 2 205; 2500, 32 on 8 (632 of 39), 1 part 461, 2 486.
   p.dq = p.few_dq ? attn_splits(256 / tiles(rows, 32), Tk / seqs / (2 * kKeys), 4)
-                  : attn_splits(192 / tiles(rows, 128), Tk / seqs / kKeys, 4);
+                  : attn_splits(900 / tiles(rows, 128), Tk / seqs / kKeys, 24);
   // dk, dv: tiles of 32 keys up to a work of 64 rows x 64 steps a compute unit (their wavefronts have a SIMD each, which costs rate and
   // saves time where work is short).  32 keys / 128 keys a tile, each at its best split: 300 tokens, 32 on 8 (80 small tiles of 18 steps)
   // 40 / 49; 4 of 300, 32 on 8 (320 of 18) 49 / 65; 1000, 6 heads (192 of 15) 42 / 51; 1000, 32 on 8 (256 of 62) 89 / 96; 4000, 8 on
   // one (125 of 500) 299 / 243; 2500, 32 on 8 (632 of 156) 282 / 243.
-  p.few_dkdv = tiles(Tk, 32) * std::max<int64_t>(1, rows / seqs / 64) <= 256 * 64;
+  // fp32: 4 of 400, 6 on 2 (104 of 18) 135 / 151; 4 of 2000, 8 on 2 (504 of 125) 1640 / 1723; 8000, 8 on 2 (500 of 500) 3580 / 3800; 8 of
+  // 1000, 8 heads (2048 of 15) 340 / 359; 4 of 4000, 8 heads (4000 of 62) 6189 / 5873.
+  p.few_dkdv = f32 ? tiles(Tk, 32) <= 2048 : tiles(Tk, 32) * std::max<int64_t>(1, rows / seqs / 64) <= 256 * 64;
   // ... in parts of the rows.  Small tiles: 300 tokens, 4 on one (10 of 18), 1 part 43, 4 35, 8 33; 80 of 18, 1 part 42, 2 40, 4 44; 320 of
-  // 18, 1 part 49, 2 67.  Large ones, two workgroups a compute unit: 2500, 32 on 8 (160 of 156), 1 part 462, 4 243, 8 258; 4000, 8 on one (32
+  // 18, 1 part 49, 2 67; fp32, 160 of 14, 1 part 87, 2 82, 4 78; 304 of 37, 1 part 455, 2 422, 4 455.  Large ones, two workgroups a compute unit: 2500, 32 on 8 (160 of 156), 1 part 462, 4 243, 8 258; 4000, 8 on one (32
   // of 500), 1 part 1271, 8 290, 16 243.
-  p.dkdv = p.few_dkdv ? attn_splits(256 / tiles(Tk, 32), rows / seqs / 128, 1)
+  p.dkdv = p.few_dkdv ? attn_splits(f32 ? 512 / tiles(Tk, 32) : 256 / tiles(Tk, 32), rows / seqs / 128, 1)
                       : attn_splits((511 + tiles(Tk, 128)) / tiles(Tk, 128), rows / seqs / 64, 4);
 }
 
@@ -124,7 +133,7 @@ static bool attn_plan(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int hq, in
   // every grid in 31 bits
   const int g = hq / hk;
   if ((tile_ids<32>(Tq * g, n_seq) + tile_ids<32>(Tk, n_seq)) * hk > kMaxTileRows) return false;
-  attn_cut(p, Tq, Tk, n_seq, g, hk);
+  attn_cut(p, Tq, Tk, n_seq, g, hk, dtype == OAPL_F32);
   size_t at = kStatusWords * sizeof(int);
   const auto take = [&](int64_t floats) {
     const size_t was = at;

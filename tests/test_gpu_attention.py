@@ -374,3 +374,41 @@ def test_in_a_graph_with_other_values():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(held, step()))
+
+
+# Enough tiles that every wavefront has 32 rows (keys) of its own, in all three kernels.
+MANY = [("bf16", [1100, 70], [1100, 333], 48, 8), ("bf16", [1500], [1500], 32, 8), ("bf16", [5000], [5000], 8, 2),
+        ("f32", [1000, 37, 600, 901, 300, 700, 650, 612], [1000, 37, 600, 901, 400, 600, 650, 612], 16, 16)]
+
+
+@pytest.mark.parametrize("D", [16, 64, 80, 128])
+@pytest.mark.parametrize("dtype, nq, nk, hq, hk", MANY)
+def test_many_tiles(dtype, nq, nk, hq, hk, D):
+    _check(dtype, nq, nk, hq, hk, D, True, seed=210)
+
+
+def test_many_tiles_of_many_sequences():
+    nq = [(7 * i * i + i) % 61 for i in range(300)]
+    nk = [(5 * i * i + 3 * i) % 67 for i in range(300)]
+    _check("f32", nq, nk, 16, 8, 64, True, seed=220)
+    _check("bf16", nq, nk, 16, 8, 64, False, seed=223)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("dtype, n, hq, hk, D", [("bf16", 1500, 32, 8, 128), ("f32", 2100, 32, 32, 64)])
+def test_what_is_not_finite_among_many_tiles(dtype, bad, n, hq, hk, D):
+    at, o = 2 * n // 3 + 5, _offsets([n])
+    for which in range(4):
+        q, k, v = _qkv(dtype, [n], [n], hq, hk, D, seed=230)
+        dout = _normal(q.shape, q.dtype, 233)
+        want = oapl.attention_fwd(q, k, v, o)
+        grads = oapl.attention_bwd(q, k, v, want.out, want.lse, dout, o)
+        (q, k, v, dout)[which][at] = bad
+        got = oapl.attention_fwd(q, k, v, o)
+        assert torch.equal(got.out[:at], want.out[:at]) and torch.equal(got.lse[:at], want.lse[:at])
+        assert which == 3 or not bool(got.out[at].isfinite().all())
+        b = oapl.attention_bwd(q, k, v, got.out, got.lse, dout, o)
+        assert torch.equal(b.dq[:at], grads.dq[:at])
+        if which in (0, 3):
+            assert torch.equal(b.dk[at + 1:], grads.dk[at + 1:]) and torch.equal(b.dv[at + 1:], grads.dv[at + 1:])
+            assert not bool(b.dv[at].isfinite().all())
