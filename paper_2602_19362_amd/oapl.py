@@ -138,6 +138,7 @@ def _stream(device) -> int:
 
 # The same number without a stream object around it, where this torch has it (2 us less on calls that take 10).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: _stream(torch.device("cuda", index)))
+_current_gpu = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device      # of a process that has a GPU tensor
 
 
 def workspace_bytes(T: int, d: int, V: int, n_seq: int, n_groups: int, dtype: int, with_backward: bool,
@@ -404,7 +405,7 @@ def _heads(t: torch.Tensor, name: str, shape, dtype: torch.dtype, index: int) ->
     """The oapl_heads of a tensor [tokens, heads, channels] on GPU `index` whose channels lie side by side."""
     if t.get_device() != index:
         raise ValueError(f"{name} must live on cuda:{index}")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
@@ -420,7 +421,7 @@ def _flat(t: Optional[torch.Tensor], dtype: torch.dtype, name: str, index: int) 
         return None
     if t.get_device() != index:
         raise ValueError(f"{name} must live on cuda:{index}")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
@@ -438,7 +439,7 @@ def _scratch(nbytes: int, like: torch.Tensor, workspace: Optional[torch.Tensor],
 def _qk_setup(q: torch.Tensor, k: torch.Tensor):
     """(tokens, heads, channels of q, heads of k, dtype code, GPU)."""
     index = q.get_device()
-    if index < 0 or index != torch.cuda.current_device():
+    if index < 0 or index != _current_gpu():
         _check_device(q)
     dt = _dtype_code(q)
     if q.dim() != 3 or k.dim() != 3 or q.shape[2] != k.shape[2]:
