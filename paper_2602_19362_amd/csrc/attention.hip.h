@@ -678,19 +678,31 @@ struct Part {
   }
 };
 
+// What a workgroup does: the part of a tile's walk, the key head, the tile's rank.  Parts come first: XCDs take workgroups in turn, so one
+// XCD's workgroups walk over the same part, which its L2 then holds.
+struct Job {
+  int part, kh, rank;
+  __device__ __forceinline__ explicit Job(const AttnArgs& p) {
+    const unsigned id = blockIdx.x / (unsigned)p.splits;
+    part = uniform((int)(blockIdx.x - id * p.splits));
+    rank = uniform((int)(id / (unsigned)p.hk));
+    kh = uniform((int)id - rank * p.hk);
+  }
+};
+
 // A result of one split, unnormalised: partial[split][packed row][D], and its maximum (in base 2) and sum.
-__device__ __forceinline__ void store_sums(const AttnArgs& p, int64_t row, float m2, float l) {
-  *(float2*)(p.part_sums + (blockIdx.y * p.Tq * p.hq + row) * 2) = make_float2(m2, l);
+__device__ __forceinline__ void store_sums(const AttnArgs& p, int part, int64_t row, float m2, float l) {
+  *(float2*)(p.part_sums + (part * p.Tq * p.hq + row) * 2) = make_float2(m2, l);
 }
-__device__ __forceinline__ float* partial_row(const AttnArgs& p, int64_t rows, int64_t row) {
-  return p.partials + (blockIdx.y * rows + row) * p.D;
+__device__ __forceinline__ float* partial_row(const AttnArgs& p, int part, int64_t rows, int64_t row) {
+  return p.partials + (part * rows + row) * p.D;
 }
 
 // WK = 1: a workgroup has 128 rows, 32 a wavefront, over all keys that they see, 32 at a time.  Three wavefronts a SIMD: one's exponentials
 // run beside another's products.
 // WK = 4, for few rows: the wavefronts have the same 32 rows and take the steps of 32 keys in turn, each through LDS of its own, and
 // join at the end.  That is bound by reading the keys and values.
-// Where tiles are few, their keys are split over workgroups (blockIdx.y) whose results k_attn_join puts together.
+// Where tiles are few, their keys are split over workgroups whose results k_attn_join puts together.
 template <class T, int DW, int WK>
 __global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k_attn_fwd(const AttnArgs p) {
   constexpr int DP = padded(DW);
@@ -700,10 +712,11 @@ __global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k
   typedef KeyLds<T, DP, WK, kFwdKeys> Size;
   constexpr int B = 128 / WK, KS = DW / 32, DB = DW / 16, SIZE = Size::kTile;
   extern __shared__ char smem[];
-  const int kh = blockIdx.x % p.hk;
+  const Job job(p);
+  const int kh = job.kh;
   SeqTile t;
-  const Found found = pick_tile<B>(p, kOfRows, blockIdx.x / p.hk, t);
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = found == kMalformed ? kErrOffsets : 0;
+  const Found found = pick_tile<B>(p, kOfRows, job.rank, t);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = found == kMalformed ? kErrOffsets : 0;
   if (found == kMalformed) {
     poison<T>(p.o, p.Tq, p.hq, p.D);
     if (p.lse) poison(p.lse, p.Tq * p.hq);
@@ -711,7 +724,7 @@ __global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k
   if (found != kTile) return;
   const int wave = uniform((int)threadIdx.x >> 6);
   const lds_char_ptr lds = (lds_char_ptr)smem + (WK == 1 ? 0 : wave * Size::kWave);     // slots of keys and values
-  const Part part(tile_sees<B>(p, t), p.splits, blockIdx.y, kFwdKeys * WK);
+  const Part part(tile_sees<B>(p, t), p.splits, job.part, kFwdKeys * WK);
   const Stage ks(p.k.row(t.k0, kh), p.k.token, p.D), vs(p.v.row(t.k0, kh), p.v.token, p.D);
   int j0 = part.begin + (WK == 1 ? 0 : wave * kFwdKeys), slot = 0;
   const lds_char_ptr words = (lds_char_ptr)smem + Size::kWords;
@@ -824,8 +837,8 @@ __global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k
       const int head = kh * p.g + row.head;
       if (p.splits > 1) {
         const int64_t at = packed_row(p, t, kh, row0 + n * 16);
-        store_columns<float>((char*)partial_row(p, p.Tq * p.hq, at), o[n], 1.f, p.D);
-        if (group == 0) store_sums(p, at, m[n] * scale2, l[n]);
+        store_columns<float>((char*)partial_row(p, job.part, p.Tq * p.hq, at), o[n], 1.f, p.D);
+        if (group == 0) store_sums(p, job.part, at, m[n] * scale2, l[n]);
         continue;
       }
       store_columns<T>(p.o.row(t.q0 + row.token, head), o[n], inverse(l[n]), p.D);
@@ -869,8 +882,8 @@ __global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k
       const int64_t at = packed_row(p, t, kh, t.first + r);
 #pragma unroll
       for (int c = 0; c < DW / 32; ++c)
-        if (c0 + c * 4 < p.D) store4(partial_row(p, p.Tq * p.hq, at) + c0 + c * 4, x[c]);
-      if (c0 == 0) store_sums(p, at, top, sum);
+        if (c0 + c * 4 < p.D) store4(partial_row(p, job.part, p.Tq * p.hq, at) + c0 + c * 4, x[c]);
+      if (c0 == 0) store_sums(p, job.part, at, top, sum);
       return;
     }
     T* to = (T*)p.o.row(t.q0 + row.token, head);
@@ -986,14 +999,15 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
   extern __shared__ char smem[];
   const int wave = uniform((int)threadIdx.x >> 6);
   const lds_char_ptr lds = (lds_char_ptr)smem + (WK == 1 ? 0 : wave * Size::kWave), words = (lds_char_ptr)smem + Size::kWords;
-  const int kh = blockIdx.x % p.hk;
+  const Job job(p);
+  const int kh = job.kh;
   SeqTile t;
-  const Found found = pick_tile<B>(p, kOfRows, blockIdx.x / p.hk, t);
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = found == kMalformed ? kErrOffsets : 0;
+  const Found found = pick_tile<B>(p, kOfRows, job.rank, t);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = found == kMalformed ? kErrOffsets : 0;
   if (found == kMalformed) poison<T>(p.dq, p.Tq, p.hq, p.D);
   if (found != kTile) return;
   const int first_sees = all_rows_see(p, t), last_sees = tile_sees<B>(p, t);
-  const Part part(last_sees, p.splits, blockIdx.y, KEYS * WK);
+  const Part part(last_sees, p.splits, job.part, KEYS * WK);
   const Stage ks(p.k.row(t.k0, kh), p.k.token, p.D), vs(p.v.row(t.k0, kh), p.v.token, p.D);
   int j0 = part.begin + (WK == 1 ? 0 : wave * KEYS), slot = 0;
   const auto stage = [&](int at, int first) {
@@ -1024,7 +1038,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
     for (int kk = 0; kk < KS; ++kk) delta[n] += dot(o[kk], dout[n][kk]);
     delta[n] = row_sum(delta[n]);
     lse2[n] = row.exists ? p.lse[token * p.hq + head] * kLog2e : 0.f;
-    if (row.exists && group == 0 && blockIdx.y == 0 && (WK == 1 || wave == 0)) {
+    if (row.exists && group == 0 && job.part == 0 && (WK == 1 || wave == 0)) {
       const int64_t at = packed_row(p, t, kh, row0 + n * 16);
       p.delta[at] = delta[n];
       // of a row that sees nothing: every probability comes out as 0
@@ -1101,14 +1115,14 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
     for (int n = 0; n < 2; ++n) {
       const Row row(p, t, row0 + n * 16);
       if (!row.exists) continue;
-      if (p.splits > 1) store_columns<float>((char*)partial_row(p, p.Tq * p.hq, packed_row(p, t, kh, row0 + n * 16)), dq[n], 1.f, p.D);
+      if (p.splits > 1) store_columns<float>((char*)partial_row(p, job.part, p.Tq * p.hq, packed_row(p, t, kh, row0 + n * 16)), dq[n], 1.f, p.D);
       else store_columns<T>(p.dq.row(t.q0 + row.token, kh * p.g + row.head), dq[n], p.scale, p.D);
     }
   } else {
     add_wavefronts<DW>(dq, (lds_char_ptr)smem, Size::kWave, [&](int r, int c0, const auto& x) {
       const Row row(p, t, t.first + r);
       if (!row.exists) return;
-      if (p.splits > 1) store_share<float>((char*)partial_row(p, p.Tq * p.hq, packed_row(p, t, kh, t.first + r)), c0, x, 1.f, p.D);
+      if (p.splits > 1) store_share<float>((char*)partial_row(p, job.part, p.Tq * p.hq, packed_row(p, t, kh, t.first + r)), c0, x, 1.f, p.D);
       else store_share<T>(p.dq.row(t.q0 + row.token, kh * p.g + row.head), c0, x, p.scale, p.D);
     });
   }
@@ -1193,9 +1207,10 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   extern __shared__ char smem[];
   const int wave = uniform((int)threadIdx.x >> 6), tile_wave = WK == 1 ? wave : 0;
   const lds_char_ptr lds = (lds_char_ptr)smem + (WK == 1 ? 0 : wave * Size::kWave), words = (lds_char_ptr)smem + Size::kWords;
-  const int kh = blockIdx.x % p.hk;
+  const Job job(p);
+  const int kh = job.kh;
   SeqTile t;
-  const Found found = pick_tile<B>(p, kOfKeys, blockIdx.x / p.hk, t);
+  const Found found = pick_tile<B>(p, kOfKeys, job.rank, t);
   if (found == kMalformed) {
     poison<T>(p.dk, p.Tk, p.hk, p.D);
     poison<T>(p.dv, p.Tk, p.hk, p.D);
@@ -1204,7 +1219,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   const int rows = t.nq * p.g, ahead = t.nk - t.nq;
   // the first row that sees the tile's first key, and whole tiles of rows
   const int from = p.causal && t.first > ahead ? (t.first - ahead) * p.g / kRows * kRows : 0;
-  const Part part(rows > from ? rows - from : 0, p.splits, blockIdx.y, kRows * WK);
+  const Part part(rows > from ? rows - from : 0, p.splits, job.part, kRows * WK);
   const int end = from + part.end;
   int r0 = from + part.begin + (WK == 1 ? 0 : wave * kRows), slot = 0;
   if (Size::kSlots == 2 && r0 < end) Stage::start(p, t, kh, lds, r0);
@@ -1291,7 +1306,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
       const int key = t.first + wave * 32 + n * 16 + (threadIdx.x & 15);
       if (key >= t.nk) continue;
       if (p.splits > 1) {
-        float* to = partial_row(p, 2 * p.Tk * p.hk, kh * p.Tk + t.k0 + key);
+        float* to = partial_row(p, job.part, 2 * p.Tk * p.hk, kh * p.Tk + t.k0 + key);
         store_columns<float>((char*)to, dk[n], 1.f, p.D);
         store_columns<float>((char*)(to + p.Tk * p.hk * p.D), dv[n], 1.f, p.D);
         continue;
@@ -1301,10 +1316,10 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
     }
   } else {
     const auto share = [&](const Heads& out, int64_t behind, float factor) {
-      return [&p, &t, &out, kh, behind, factor](int r, int c0, const auto& x) {
+      return [&p, &t, &out, &job, kh, behind, factor](int r, int c0, const auto& x) {
         const int key = t.first + r;
         if (key >= t.nk) return;
-        if (p.splits > 1) store_share<float>((char*)(partial_row(p, 2 * p.Tk * p.hk, kh * p.Tk + t.k0 + key) + behind), c0, x, 1.f, p.D);
+        if (p.splits > 1) store_share<float>((char*)(partial_row(p, job.part, 2 * p.Tk * p.hk, kh * p.Tk + t.k0 + key) + behind), c0, x, 1.f, p.D);
         else store_share<T>(out.row(t.k0 + key, kh), c0, x, factor, p.D);
       };
     };

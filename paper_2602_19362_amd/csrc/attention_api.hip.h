@@ -184,10 +184,10 @@ static int by_type(int dtype, int D, F&& launch) {
 }
 
 template <auto kernel, int lds>
-static int launch_attn(int64_t tiles, int splits, const AttnArgs& a, hipStream_t st) {
+static int launch_attn(int64_t tiles, const AttnArgs& a, hipStream_t st) {
   static const bool ready = allow_big_lds(kernel, lds);
   if (!ready) return OAPL_ERR_HIP;
-  kernel<<<dim3((unsigned)tiles, (unsigned)splits), 256, lds, st>>>(a);
+  kernel<<<(unsigned)(tiles * a.splits), 256, lds, st>>>(a);
   OAPL_LAUNCH_CHECK();
   return OAPL_OK;
 }
@@ -197,8 +197,8 @@ static int launch_attn_fwd(AttnArgs a, const AttnPlan& p, hipStream_t st) {
   a.splits = p.fwd;
   const int64_t rows = a.Tq * a.g;
   constexpr int DP = padded(DW);
-  const int rc = p.few ? launch_attn<k_attn_fwd<T, DW, 4>, KeyLds<T, DP, 4, kFwdKeys>::kBytes>(tile_ids<32>(rows, a.n_seq) * a.hk, p.fwd, a, st)
-                       : launch_attn<k_attn_fwd<T, DW, 1>, KeyLds<T, DP, 1, kFwdKeys>::kBytes>(tile_ids<128>(rows, a.n_seq) * a.hk, p.fwd, a, st);
+  const int rc = p.few ? launch_attn<k_attn_fwd<T, DW, 4>, KeyLds<T, DP, 4, kFwdKeys>::kBytes>(tile_ids<32>(rows, a.n_seq) * a.hk, a, st)
+                       : launch_attn<k_attn_fwd<T, DW, 1>, KeyLds<T, DP, 1, kFwdKeys>::kBytes>(tile_ids<128>(rows, a.n_seq) * a.hk, a, st);
   if (rc != OAPL_OK || p.fwd == 1 || a.Tq == 0) return rc;
   k_attn_join<T><<<grid1d(a.Tq * a.hq, 8), 256, 0, st>>>(a);
   OAPL_LAUNCH_CHECK();
@@ -210,8 +210,8 @@ static int launch_attn_bwd(AttnArgs a, const AttnPlan& p, hipStream_t st) {
   constexpr int DP = padded(DW);
   a.splits = p.dq;
   const int64_t rows = a.Tq * a.g;
-  int rc = p.few_dq ? launch_attn<k_attn_dq<T, DW, 4>, KeyLds<T, DP, 4, kKeys / 2>::kBytes>(tile_ids<32>(rows, a.n_seq) * a.hk, p.dq, a, st)
-                    : launch_attn<k_attn_dq<T, DW, 1>, KeyLds<T, DP, 1, kKeys>::kBytes>(tile_ids<128>(rows, a.n_seq) * a.hk, p.dq, a, st);
+  int rc = p.few_dq ? launch_attn<k_attn_dq<T, DW, 4>, KeyLds<T, DP, 4, kKeys / 2>::kBytes>(tile_ids<32>(rows, a.n_seq) * a.hk, a, st)
+                    : launch_attn<k_attn_dq<T, DW, 1>, KeyLds<T, DP, 1, kKeys>::kBytes>(tile_ids<128>(rows, a.n_seq) * a.hk, a, st);
   if (rc != OAPL_OK) return rc;
   if (p.dq > 1 && a.Tq > 0) {
     const GradSum dq{a.dq, a.partials, a.scale};
@@ -219,8 +219,8 @@ static int launch_attn_bwd(AttnArgs a, const AttnPlan& p, hipStream_t st) {
     OAPL_LAUNCH_CHECK();
   }
   a.splits = p.dkdv;
-  rc = p.few_dkdv ? launch_attn<k_attn_dkdv<T, DW, 4>, RowLds<T, DP, 4>::kBytes>(tile_ids<32>(a.Tk, a.n_seq) * a.hk, p.dkdv, a, st)
-                  : launch_attn<k_attn_dkdv<T, DW, 1>, RowLds<T, DP, 1>::kBytes>(tile_ids<128>(a.Tk, a.n_seq) * a.hk, p.dkdv, a, st);
+  rc = p.few_dkdv ? launch_attn<k_attn_dkdv<T, DW, 4>, RowLds<T, DP, 4>::kBytes>(tile_ids<32>(a.Tk, a.n_seq) * a.hk, a, st)
+                  : launch_attn<k_attn_dkdv<T, DW, 1>, RowLds<T, DP, 1>::kBytes>(tile_ids<128>(a.Tk, a.n_seq) * a.hk, a, st);
   if (rc != OAPL_OK) return rc;
   if (p.dkdv > 1 && a.Tk > 0) {
     const int64_t one = a.Tk * a.hk * a.D;
