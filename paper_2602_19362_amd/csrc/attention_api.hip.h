@@ -72,8 +72,8 @@ static int rope_args(NormRopeArgs& a, const oapl_heads* q, const oapl_heads* k, 
 }
 
 // ---------------------------------------------------------------------------------------------------------------- attention
-// What a call of average sequences is cut into; nothing more is known here of them.  Microseconds below: bf16, 128 channels, equal lengths,
-// as replayed graphs on one MI355X.
+// What a call of average sequences is cut into; nothing more is known here of them.  Microseconds below: equal lengths, causal, bf16 and 128
+// channels where nothing else is said, as replayed graphs on one MI355X; of backward, both kernels together with the other one's cut fixed.
 struct AttnPlan {
   bool few = false, few_dq = false, few_dkdv = false;      // tiles of 32 rows (keys) whose wavefronts share the steps
   int fwd = 1, dq = 1, dkdv = 1;       // workgroups that share a tile's steps
@@ -88,40 +88,41 @@ static int attn_splits(int64_t want, int64_t steps, int64_t least) {
 static void attn_cut(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int g, int hk, bool f32) {
   const int64_t seqs = std::max(n_seq, 1), rows = Tq * g;
   const auto tiles = [&](int64_t n, int64_t b) { return std::max<int64_t>(1, (n + seqs * b - 1) / (seqs * b)) * seqs * hk; };
-  // Tiles of 32 rows: for few rows, and where they are one round of workgroups (160 KB of LDS: one a compute unit) however many.
-  // 32 rows / 128 rows a tile: 16 sequences of 64 rows over 2000 keys, 8 key heads (256 small tiles) 29 / 34 (at its best split), of 96 rows
-  // (384) 51 / 42; one sequence of 1000 tokens, 8 heads on one (250) 11 / 19, 6 on 6 (192) 11 / 17, 32 on 8 (1000) 42 / 35.
-  // fp32 products take nine times as long, and all small tiles cost is hidden behind them for longer: 4 of 400 tokens, 6 heads on 2 (304)
-  // 24 / 50; 2 of 1000, 16 on 8 (1008) 57 / 85; 4 of 2000, 8 on 2 (2000) 353 / 381; 4 of 4000, 8 heads (4000) 1248 / 1109.
+  // Forward: tiles of 32 rows for few rows, and where they are one round of workgroups (up to 133 KB of LDS: one a compute unit) however
+  // many.  32 rows / 128 rows a tile, each at its best split: 16 sequences of 64 rows over 2000 keys, 8 key heads (256 small tiles) 29 / 34, of
+  // 96 rows (384) 52 / 38; 64 channels, 1000 tokens, 8 heads on one (250) 11 / 19, 6 heads (192) 11 / 19; 1000 tokens, 32 on 8 (1000) 41 / 35.
+  // fp32 products take nine times as long, and what small tiles cost is hidden behind them for longer: 80 channels, 4 of 400 tokens, 6 on 2
+  // (304) 25 / 50; 64 channels, 2 of 1000, 16 on 8 (1008) 57 / 85; 4 of 2000, 8 on 2 (2000) 353 / 382; 4 of 4000, 8 heads (4000) 1255 / 1113.
   p.few = rows <= seqs * 32 || tiles(rows, 32) <= (f32 ? 2048 : 256);
-  // ... their keys in parts that fill that round: one token over 4096 / 32768 keys, 8 key heads, in 1 part 33 / 216, 8 parts 14 / 38, 16
-  // parts 13 / 31; 8 over 32768, 1 part 388, 4 181, 8 185; 24 over 4096 (192 tiles), 1 part 85, 2 96.  Short parts cost more to
-  // put together than they save: 4 x 32 rows over 2000 keys, 4 parts 16, 8 parts (of two steps) 21.
-  // Tiles of 128 rows: where few tiles have long walks.  8000 tokens, 4 heads on one (250 tiles of 250 steps), 1 part 190, 4 110; 1000
-  // tokens, 32 on 8 (256 of 31), 1 part 35, 2 41.
+  // ... in parts of the keys.  Small tiles, parts that fill the round: one token over 4096 / 32768 keys, 8 key heads, 1 part 35 / 236, 8
+  // parts 13 / 40, 16 parts 12 / 31; 8 over 32768, 1 part 389, 4 189, 8 199; 24 over 4096 (192 tiles), 1 part 83, 2 94.  Short parts cost more
+  // to put together than they save: 4 x 32 rows over 2000 keys, 4 parts 16, 8 parts (of two steps) 19.
+  // Large ones where few tiles have long walks: 8000 tokens, 4 heads on one (250 tiles of 250 steps), 1 part 217, 4 90; 1000 tokens, 32 on 8
+  // (256 of 31), 1 part 35.5, 2 37.5.
   p.fwd = p.few ? attn_splits(256 / tiles(rows, 32), Tk / seqs / (4 * kFwdKeys), 3)
                 : attn_splits(1024 / tiles(rows, 128), Tk / seqs / kFwdKeys, 32);
-  // dq: tiles of 32 rows up to two rounds.  With dk, dv, 32 rows / 128 rows a tile, each at its best split: 1000 tokens, 6 heads (192
-  // small tiles) 49 / 55; 1200, 8 heads (304) 62 / 68; 300, 32 on 8 (304) 78 / 78; 4 of 1000, 4 on one (500) 187 / 192; 4800, 8 on 2
-  // (1200) 280 / 250; 1000, 32 on 8 (1000) 213 / 199.  fp32, one part: 4 of 400, 6 on 2 (304) 290 / 338; 2 of 1000, 16 on 8 (1008) 361 / 401;
-  // 8 of 600, 8 on 2 (1200) 981 / 942.
+  // dq: tiles of 32 rows up to two rounds.  32 rows / 128 rows, each at its best split: 64 channels, 1000 tokens, 6 heads (192 small tiles)
+  // 48 / 55; 1200, 8 heads (304) 46 / 52; 300, 32 on 8 (304) 79 / 78; 4 of 1000, 4 on one (500) 187 / 193; 4800, 8 on 2 (1200) 278 / 241;
+  // 1000, 32 on 8 (1000) 213 / 199.  fp32: 80 channels, 4 of 400, 6 on 2 (304) 291 / 301; 64 channels, 2 of 1000, 16 on 8 (1008) 362 / 401; 8
+  // of 600, 8 on 2 (1200) 983 / 943.
   p.few_dq = tiles(rows, 32) <= (f32 ? 1024 : 512);
   // ... in parts of the keys.  Small tiles: 16 rows over 4096 keys (2 of 32 steps), 1 part 50, 4 30, 8 25; 64 rows over 1024 (8 of 8), 1
-  // part 28, 2 27; 2000 tokens, one head (63 of 15), 1 part 56, 2 52; 192 of 7, 1 part 49, 2 52.  Large ones: 9000, 4 on one (282 of 140), 1
-  // part 473, 2 416, 3 392; 1000, 32 on 8 (256 of 15), 1 part 199, 2 205; 2500, 32 on 8 (632 of 39), 1 part 461, 2 486.
+  // part 28, 2 27; 2000 tokens, one head (63 of 15), 1 part 57, 2 52; 192 of 7, 1 part 48, 2 51.  Large ones: 9000, 4 on one (282 of 140), 1
+  // part 456, 2 373, 3 355; 1000, 32 on 8 (256 of 15), 1 part 199, 2 200; 2500, 32 on 8 (632 of 39), 1 part 460, 2 491.
   p.dq = p.few_dq ? attn_splits(256 / tiles(rows, 32), Tk / seqs / (2 * kKeys), 4)
                   : attn_splits(900 / tiles(rows, 128), Tk / seqs / kKeys, 24);
-  // dk, dv: tiles of 32 keys up to a work of 64 rows x 64 steps a compute unit (their wavefronts have a SIMD each, which costs rate and
-  // saves time where work is short).  32 keys / 128 keys a tile, each at its best split: 300 tokens, 32 on 8 (80 small tiles of 18 steps)
-  // 40 / 49; 4 of 300, 32 on 8 (320 of 18) 49 / 65; 1000, 6 heads (192 of 15) 42 / 51; 1000, 32 on 8 (256 of 62) 89 / 96; 4000, 8 on
-  // one (125 of 500) 299 / 243; 2500, 32 on 8 (632 of 156) 282 / 243.
-  // fp32: 4 of 400, 6 on 2 (104 of 18) 135 / 151; 4 of 2000, 8 on 2 (504 of 125) 1640 / 1723; 8000, 8 on 2 (500 of 500) 3580 / 3800; 8 of
-  // 1000, 8 heads (2048 of 15) 340 / 359; 4 of 4000, 8 heads (4000 of 62) 6189 / 5873.
-  p.few_dkdv = f32 ? tiles(Tk, 32) <= 2048 : tiles(Tk, 32) * std::max<int64_t>(1, rows / seqs / 64) <= 256 * 64;
-  // ... in parts of the rows.  Small tiles: 300 tokens, 4 on one (10 of 18), 1 part 43, 4 35, 8 33; 80 of 18, 1 part 42, 2 40, 4 44; 320 of
-  // 18, 1 part 49, 2 67; fp32, 160 of 14, 1 part 87, 2 82, 4 78; 304 of 37, 1 part 455, 2 422, 4 455.  Large ones, two workgroups a compute unit: 2500, 32 on 8 (160 of 156), 1 part 462, 4 243, 8 258; 4000, 8 on one (32
-  // of 500), 1 part 1271, 8 290, 16 243.
-  p.dkdv = p.few_dkdv ? attn_splits(f32 ? 512 / tiles(Tk, 32) : 256 / tiles(Tk, 32), rows / seqs / 128, 1)
+  // dk, dv: tiles of 32 keys up to a work of 64 (fp32: 128) steps of 64 rows a compute unit; their wavefronts have a SIMD each, which costs
+  // rate and saves time where work is short.  32 keys / 128 keys, each at its best split: 300 tokens, 32 on 8 (80 small tiles of 18
+  // steps) 39 / 47; 4 of 300, 32 on 8 (320 of 18) 49 / 64; 64 channels, 1000, 6 heads (192 of 15) 42 / 50; 1000, 32 on 8 (256 of 62) 90 / 94;
+  // 4000, 8 on one (125 of 500) 259 / 230; 2500, 32 on 8 (632 of 156) 280 / 232.  fp32: 80 channels, 4 of 400, 6 on 2 (104 of 18) 138 / 150; 64
+  // channels, 8 of 1000, 8 heads (2048 of 15) 338 / 358; 4 of 2000, 8 on 2 (504 of 125) 1634 / 1590; 96 channels, 8000, 8 on 2 (500 of 500)
+  // 3530 / 3353; 4 of 4000, 8 heads (4000 of 62) 6267 / 5964.
+  const int64_t work = tiles(Tk, 32) * std::max<int64_t>(1, rows / seqs / 64);
+  p.few_dkdv = work <= 256 * (f32 ? 128 : 64);
+  // ... in parts of the rows.  Small tiles: 300 tokens, 4 on one (10 of 18), 1 part 43, 4 34, 8 32; 80 of 18, 1 part 42, 2 39, 4 44; 320 of
+  // 18, 1 part 49, 2 71; fp32, 304 of 37, 1 part 453, 2 431, 4 471.  Large ones, two workgroups a compute unit: 2500, 32 on 8 (160 of 156), 1
+  // part 459, 4 232, 8 262; 4000, 8 on one (32 of 500), 1 part 1270, 8 289, 16 230.
+  p.dkdv = p.few_dkdv ? attn_splits((f32 ? 512 : 256) / tiles(Tk, 32), rows / seqs / 128, 1)
                       : attn_splits((511 + tiles(Tk, 128)) / tiles(Tk, 128), rows / seqs / 64, 4);
 }
 

@@ -412,3 +412,12 @@ def test_what_is_not_finite_among_many_tiles(dtype, bad, n, hq, hk, D):
         if which in (0, 3):
             assert torch.equal(b.dk[at + 1:], grads.dk[at + 1:]) and torch.equal(b.dv[at + 1:], grads.dv[at + 1:])
             assert not bool(b.dv[at].isfinite().all())
+
+
+def test_large_tiles_of_many_sequences_and_in_fp32():
+    """Long enough walks that tiles of 128 keys are taken, found by either search."""
+    nq = [(7 * i * i + i) % 61 for i in range(300)]
+    nk = [(5 * i * i + 3 * i) % 67 for i in range(300)]
+    _check("bf16", nq, nk, 128, 8, 64, True, seed=240)
+    _check("f32", [2500], [2500], 32, 8, 64, True, seed=243)
+    _check("f32", [1700, 800], [1700, 800], 32, 16, 128, True, seed=246)
