@@ -958,11 +958,11 @@ __global__ __launch_bounds__(256) void k_attn_add(const AttnArgs p, GradSum firs
 }
 
 // ---------------------------------------------------------------------------------------------------------------- backward
-// Adds up what four wavefronts have of the same 32 rows (keys), in their order, in LDS of `each` bytes a wavefront: eight threads a row
+// Adds up what the N wavefronts (every 4 / N-th) have of the same 32 rows (keys), in their order, in LDS of `each` bytes a wavefront: threads
 // get a share(row, first channel, sums) each.
-template <int DW, class F>
+template <int DW, int N, class F>
 __device__ __forceinline__ void add_wavefronts(const f32x4 (&acc)[2][DW / 16], lds_char_ptr lds, int each, F&& share) {
-  constexpr int PITCH = padded(DW) * 4 + 16;
+  constexpr int PITCH = padded(DW) * 4 + 16, G = 4 / N, THREADS = 2 * N, C = DW / THREADS;
   typedef __attribute__((address_space(3))) f32x4* lds_f32x4;
   __syncthreads();      // everybody is done with what was there
 #pragma unroll
@@ -971,12 +971,12 @@ __device__ __forceinline__ void add_wavefronts(const f32x4 (&acc)[2][DW / 16], l
     for (int d = 0; d < DW / 16; ++d)
       *(lds_f32x4)(lds + (threadIdx.x >> 6) * each + (n * 16 + (threadIdx.x & 15)) * PITCH + d * 64 + (threadIdx.x >> 4 & 3) * 16) = acc[n][d];
   __syncthreads();
-  const int r = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * (DW / 8);
-  f32x4 x[DW / 32] = {};
+  const int r = threadIdx.x / THREADS, c0 = threadIdx.x % THREADS * C;
+  f32x4 x[C / 4] = {};
 #pragma unroll
-  for (int w = 0; w < 4; ++w)
+  for (int w = 0; w < N; ++w)
 #pragma unroll
-    for (int c = 0; c < DW / 32; ++c) x[c] += *(lds_f32x4)(lds + w * each + r * PITCH + (c0 + c * 4) * 4);
+    for (int c = 0; c < C / 4; ++c) x[c] += *(lds_f32x4)(lds + (r / 32 + w * G) * each + r % 32 * PITCH + (c0 + c * 4) * 4);
   share(r, c0, x);
 }
 template <class T, int N>
@@ -1119,7 +1119,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
       else store_columns<T>(p.dq.row(t.q0 + row.token, kh * p.g + row.head), dq[n], p.scale, p.D);
     }
   } else {
-    add_wavefronts<DW>(dq, (lds_char_ptr)smem, Size::kWave, [&](int r, int c0, const auto& x) {
+    add_wavefronts<DW, 4>(dq, (lds_char_ptr)smem, Size::kWave, [&](int r, int c0, const auto& x) {
       const Row row(p, t, t.first + r);
       if (!row.exists) return;
       if (p.splits > 1) store_share<float>((char*)partial_row(p, job.part, p.Tq * p.hq, packed_row(p, t, kh, t.first + r)), c0, x, 1.f, p.D);
@@ -1186,16 +1186,16 @@ struct RowStager {
 // LDS of a workgroup for dk and dv, as KeyLds.
 template <class T, int DP, int WK>
 struct RowLds {
-  static constexpr int kRows = WK == 1 ? 64 : 32, kSlots = WK == 4 && sizeof(T) == 4 ? 1 : 2;
-  typedef RowStager<T, DP, kRows, 4 / WK> Stage;
+  static constexpr int kRows = WK == 4 ? 32 : 64, kSlots = WK == 4 && sizeof(T) == 4 ? 1 : 2;
+  typedef RowStager<T, DP, kRows, WK == 4 ? 1 : 4> Stage;
   static constexpr int kStages = kSlots * Stage::kBytes, kResults = 32 * (DP * 4 + 16);
-  static constexpr int kWave = WK == 1 || kStages > kResults ? kStages : (kResults + 511) / 512 * 512;
-  static constexpr int kWords = WK * kWave, kBytes = kWords + 48;
+  static constexpr int kEach = WK == 4 && kStages > kResults ? kStages : (kResults + 511) / 512 * 512;      // of a wavefront
+  static constexpr int kWords = WK == 1 || (WK == 2 && kStages > 4 * kEach) ? kStages : 4 * kEach, kBytes = kWords + 48;
   static_assert(kBytes <= 160 * 1024, "LDS of one CU");
 };
 
-// dk and dv: a workgroup has 128 keys, 32 a wavefront, over all rows that see any of them, 64 at a time; or (WK = 4) 32 keys, over
-// steps of 32 rows that the wavefronts take in turn.
+// dk and dv: a workgroup has 128 keys, 32 a wavefront, over all rows that see any of them, 64 at a time; or (WK = 2) 64 keys, two
+// wavefronts for either half of the 64 rows; or (WK = 4) 32 keys, over steps of 32 rows that the wavefronts take in turn.
 template <class T, int DW, int WK>
 __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   constexpr int DP = padded(DW);
@@ -1205,8 +1205,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   typedef typename Size::Stage Stage;
   constexpr int B = 128 / WK, KS = DW / 32, DB = DW / 16, kRows = Size::kRows;
   extern __shared__ char smem[];
-  const int wave = uniform((int)threadIdx.x >> 6), tile_wave = WK == 1 ? wave : 0;
-  const lds_char_ptr lds = (lds_char_ptr)smem + (WK == 1 ? 0 : wave * Size::kWave), words = (lds_char_ptr)smem + Size::kWords;
+  constexpr bool kAlone = WK == 4;      // a wavefront stages rows for itself
+  const int wave = uniform((int)threadIdx.x >> 6), tile_wave = wave % (4 / WK);
+  const lds_char_ptr lds = (lds_char_ptr)smem + (kAlone ? wave * Size::kEach : 0), words = (lds_char_ptr)smem + Size::kWords;
   const Job job(p);
   const int kh = job.kh;
   SeqTile t;
@@ -1219,10 +1220,14 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   const int rows = t.nq * p.g, ahead = t.nk - t.nq;
   // the first row that sees the tile's first key, and whole tiles of rows
   const int from = p.causal && t.first > ahead ? (t.first - ahead) * p.g / kRows * kRows : 0;
-  const Part part(rows > from ? rows - from : 0, p.splits, job.part, kRows * WK);
-  const int end = from + part.end;
-  int r0 = from + part.begin + (WK == 1 ? 0 : wave * kRows), slot = 0;
-  if (Size::kSlots == 2 && r0 < end) Stage::start(p, t, kh, lds, r0);
+  const Part part(rows > from ? rows - from : 0, p.splits, job.part, kRows * (kAlone ? 4 : 1));
+  // Large tiles go backwards: those that run at a time begin at different rows and end at the same, so they share what the L2 holds from there
+  // on (2 x 8192 tokens, 32 heads on 8, 3447 -> 3243 us with dq).  Small ones go forwards (1000 tokens 95, backwards 100 us).
+  constexpr int kStep = kRows * (kAlone ? 4 : 1), kBy = kAlone ? kStep : -kStep;
+  const int begin = from + part.begin, end = from + part.end;
+  int r0 = kAlone ? begin + wave * kRows : begin + (end - begin + kStep - 1) / kStep * kStep - kStep, slot = 0;
+  const auto any = [&](int at) { return kAlone ? at < end : at >= begin; };
+  if (Size::kSlots == 2 && any(r0)) Stage::start(p, t, kh, lds, r0);
   Frag k[2][KS], v[2][KS];
   f32x4 dk[2][DB], dv[2][DB];
   const auto first_row = [&](int key) { return p.causal && key < t.nk && key > ahead ? (key - ahead) * p.g : 0; };   // that sees it
@@ -1244,26 +1249,26 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   all_from = __builtin_amdgcn_readfirstlane(all_from);
   const float scale2 = p.scale * kLog2e;
   const int masked_to = first_row((t.first + B < t.nk ? t.first + B : t.nk) - 1);      // rows from here on see every key of the workgroup
-  for (; r0 < end; r0 += kRows * WK, slot ^= Size::kSlots == 2) {
+  for (; any(r0); r0 += kBy, slot ^= Size::kSlots == 2) {
     const lds_char_ptr tiles = lds + slot * Stage::kBytes, numbers = tiles + 2 * Stage::SIZE;
     if (Size::kSlots == 1) Stage::start(p, t, kh, lds, r0);
     staged();
-    bool odd = r0 < masked_to && (staged_odd<T, Stage::kLoads, 4 / WK>(tiles) || staged_odd<T, Stage::kLoads, 4 / WK>(tiles + Stage::SIZE));
-    if (WK == 1) {
+    bool odd = r0 < masked_to && (staged_odd<T, Stage::kLoads, kAlone ? 1 : 4>(tiles) || staged_odd<T, Stage::kLoads, kAlone ? 1 : 4>(tiles + Stage::SIZE));
+    if (!kAlone) {
       if (r0 < masked_to) tell_odd(words, slot, odd);
       lds_barrier();
       odd = r0 < masked_to && told_odd(words, slot);
     }
-    if (Size::kSlots == 2 && r0 + kRows * WK < end) Stage::start(p, t, kh, lds + (slot ^ 1) * Stage::kBytes, r0 + kRows * WK);
+    if (Size::kSlots == 2 && any(r0 + kBy)) Stage::start(p, t, kh, lds + (slot ^ 1) * Stage::kBytes, r0 + kBy);
     if (odd) {      // a row's probabilities are NaN where its log-sum-exp is
       typedef __attribute__((address_space(3))) float* lds_f32;
-      const uint64_t which = clean_tile<T, DP, kRows, 4 / WK, 2, Stage::SIZE>(tiles, words + 32);
-      const int x = WK == 1 ? threadIdx.x : threadIdx.x & 63;
+      const uint64_t which = clean_tile<T, DP, kRows, kAlone ? 1 : 4, 2, Stage::SIZE>(tiles, words + 32);
+      const int x = kAlone ? threadIdx.x & 63 : threadIdx.x;
       if (x < kRows && (which >> x & 1)) ((lds_f32)numbers)[x] = quiet_nan();
-      if (WK == 1) lds_barrier();
+      if (!kAlone) lds_barrier();
     }
 #pragma unroll 1
-    for (int c = 0; c < kRows / 32; ++c) {
+    for (int c = WK == 2 ? wave >> 1 : 0; c < kRows / 32; c += WK) {
       typedef __attribute__((address_space(3))) f32x4* ptr;
       const lds_char_ptr tile = tiles + c * 32 * Lds::kPitch;
       Frag w[2], wd[2];      // probabilities and dS of 32 rows, keys in columns
@@ -1303,7 +1308,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   if constexpr (WK == 1) {
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
-      const int key = t.first + wave * 32 + n * 16 + (threadIdx.x & 15);
+      const int key = t.first + tile_wave * 32 + n * 16 + (threadIdx.x & 15);
       if (key >= t.nk) continue;
       if (p.splits > 1) {
         float* to = partial_row(p, job.part, 2 * p.Tk * p.hk, kh * p.Tk + t.k0 + key);
@@ -1323,8 +1328,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
         else store_share<T>(out.row(t.k0 + key, kh), c0, x, factor, p.D);
       };
     };
-    add_wavefronts<DW>(dk, (lds_char_ptr)smem, Size::kWave, share(p.dk, 0, p.scale));
-    add_wavefronts<DW>(dv, (lds_char_ptr)smem, Size::kWave, share(p.dv, p.Tk * p.hk * p.D, 1.f));
+    add_wavefronts<DW, WK>(dk, (lds_char_ptr)smem, Size::kEach, share(p.dk, 0, p.scale));
+    add_wavefronts<DW, WK>(dv, (lds_char_ptr)smem, Size::kEach, share(p.dv, p.Tk * p.hk * p.D, 1.f));
   }
 }
 

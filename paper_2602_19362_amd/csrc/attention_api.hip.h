@@ -76,6 +76,7 @@ static int rope_args(NormRopeArgs& a, const oapl_heads* q, const oapl_heads* k, 
 // channels where nothing else is said, as replayed graphs on one MI355X; of backward, both kernels together with the other one's cut fixed.
 struct AttnPlan {
   bool few = false, few_dq = false, few_dkdv = false;      // tiles of 32 rows (keys) whose wavefronts share the steps
+  bool two_dkdv = false;               // tiles of 64 keys whose wavefronts share each step's rows
   int fwd = 1, dq = 1, dkdv = 1;       // workgroups that share a tile's steps
   size_t off_lse2 = 0, off_delta = 0, off_sums = 0, off_partials = 0, total = 0;
 };
@@ -85,7 +86,7 @@ static int attn_splits(int64_t want, int64_t steps, int64_t least) {
   return (int)std::max<int64_t>(1, std::min<int64_t>({want, steps / least, 64}));
 }
 
-static void attn_cut(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int g, int hk, bool f32) {
+static void attn_cut(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int g, int hk, int D, bool f32) {
   const int64_t seqs = std::max(n_seq, 1), rows = Tq * g;
   const auto tiles = [&](int64_t n, int64_t b) { return std::max<int64_t>(1, (n + seqs * b - 1) / (seqs * b)) * seqs * hk; };
   // Forward: tiles of 32 rows for few rows, and where they are one round of workgroups (up to 133 KB of LDS: one a compute unit) however
@@ -119,11 +120,17 @@ static void attn_cut(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int g, int 
   // 3530 / 3353; 4 of 4000, 8 heads (4000 of 62) 6267 / 5964.
   const int64_t work = tiles(Tk, 32) * std::max<int64_t>(1, rows / seqs / 64);
   p.few_dkdv = work <= 256 * (f32 ? 128 : 64);
+  // Tiles of 64 keys halve the longest walks, which end a call of few rounds, and read rows twice as often.  64 / 128 keys, each at its best
+  // split: 2500, 32 on 8 (160 large tiles) 221 / 230; 4000, 8 on one (32) 189 / 201; 4000, 32 on 8 (256) 459 / 453; 8 of up to 4096, 32 on 8 (1072)
+  // 1330 / 1267.  64 channels: 2500, 32 on 8 140 / 155; 8 of up to 4096 760 / 799; 2 of 8192, 32 on 8 (1024) 1954 / 1891; 32 channels 1284 / 1266
+  // and 512 / 519.  fp32: 4 of 2000, 8 on 2 (128) 1627 / 1582.
+  p.two_dkdv = !f32 && tiles(Tk, 128) <= (D <= 64 ? 1152 : 200);
   // ... in parts of the rows.  Small tiles: 300 tokens, 4 on one (10 of 18), 1 part 43, 4 34, 8 32; 80 of 18, 1 part 42, 2 39, 4 44; 320 of
   // 18, 1 part 49, 2 71; fp32, 304 of 37, 1 part 453, 2 431, 4 471.  Large ones, two workgroups a compute unit: 2500, 32 on 8 (160 of 156), 1
   // part 459, 4 232, 8 262; 4000, 8 on one (32 of 500), 1 part 1270, 8 289, 16 230.
-  p.dkdv = p.few_dkdv ? attn_splits((f32 ? 512 : 256) / tiles(Tk, 32), rows / seqs / 128, 1)
-                      : attn_splits((511 + tiles(Tk, 128)) / tiles(Tk, 128), rows / seqs / 64, 4);
+  p.dkdv = p.few_dkdv   ? attn_splits((f32 ? 512 : 256) / tiles(Tk, 32), rows / seqs / 128, 1)
+           : p.two_dkdv ? attn_splits(1024 / tiles(Tk, 64), rows / seqs / 64, 4)
+                        : attn_splits((511 + tiles(Tk, 128)) / tiles(Tk, 128), rows / seqs / 64, 4);
 }
 
 static bool attn_plan(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int hq, int hk, int D, int dtype, bool bwd) {
@@ -134,7 +141,7 @@ static bool attn_plan(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int hq, in
   // every grid in 31 bits
   const int g = hq / hk;
   if ((tile_ids<32>(Tq * g, n_seq) + tile_ids<32>(Tk, n_seq)) * hk > kMaxTileRows) return false;
-  attn_cut(p, Tq, Tk, n_seq, g, hk, dtype == OAPL_F32);
+  attn_cut(p, Tq, Tk, n_seq, g, hk, D, dtype == OAPL_F32);
   size_t at = kStatusWords * sizeof(int);
   const auto take = [&](int64_t floats) {
     const size_t was = at;
@@ -220,8 +227,15 @@ static int launch_attn_bwd(AttnArgs a, const AttnPlan& p, hipStream_t st) {
     OAPL_LAUNCH_CHECK();
   }
   a.splits = p.dkdv;
-  rc = p.few_dkdv ? launch_attn<k_attn_dkdv<T, DW, 4>, RowLds<T, DP, 4>::kBytes>(tile_ids<32>(a.Tk, a.n_seq) * a.hk, a, st)
-                  : launch_attn<k_attn_dkdv<T, DW, 1>, RowLds<T, DP, 1>::kBytes>(tile_ids<128>(a.Tk, a.n_seq) * a.hk, a, st);
+  const auto dkdv = [&](auto wk) {
+    constexpr int WK = wk, B = 128 / WK;
+    return launch_attn<k_attn_dkdv<T, DW, WK>, RowLds<T, DP, WK>::kBytes>(tile_ids<B>(a.Tk, a.n_seq) * a.hk, a, st);
+  };
+  if constexpr (sizeof(T) == 2) {
+    rc = p.few_dkdv ? dkdv(std::integral_constant<int, 4>{}) : p.two_dkdv ? dkdv(std::integral_constant<int, 2>{}) : dkdv(std::integral_constant<int, 1>{});
+  } else {
+    rc = p.few_dkdv ? dkdv(std::integral_constant<int, 4>{}) : dkdv(std::integral_constant<int, 1>{});
+  }
   if (rc != OAPL_OK) return rc;
   if (p.dkdv > 1 && a.Tk > 0) {
     const int64_t one = a.Tk * a.hk * a.D;

@@ -422,3 +422,14 @@ def test_large_tiles_of_many_sequences_and_in_fp32():
     _check("bf16", nq, nk, 64, 4, 64, True, seed=240)
     _check("f32", [2500], [2500], 32, 8, 64, True, seed=243)
     _check("f32", [1700, 800], [1700, 800], 32, 16, 128, True, seed=246)
+
+
+@pytest.mark.parametrize("lengths, hq, hk, D", [([3500], 32, 8, 128), ([1600] * 11 + [1400], 8, 8, 64), ([1600] * 11 + [1400], 8, 8, 16),
+                                                ([2100, 1900], 16, 8, 80), ([140] * 66, 64, 8, 128)])
+def test_tiles_of_128_keys(lengths, hq, hk, D):
+    _check("bf16", lengths, lengths, hq, hk, D, True, seed=250)
+
+
+@pytest.mark.parametrize("bad", [math.nan, -math.inf])
+def test_what_is_not_finite_among_tiles_of_128_keys(bad):
+    test_what_is_not_finite_among_many_tiles("bf16", bad, 3500, 32, 8, 128)
