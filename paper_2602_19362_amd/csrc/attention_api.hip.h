@@ -121,13 +121,14 @@ static void attn_cut(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int g, int 
   const int64_t work = tiles(Tk, 32) * std::max<int64_t>(1, rows / seqs / 64);
   p.few_dkdv = work <= 256 * (f32 ? 128 : 64);
   // Tiles of 64 keys halve the longest walks, which end a call of few rounds, and read rows twice as often.  64 / 128 keys, each at its best
-  // split: 2500, 32 on 8 (160 large tiles) 221 / 230; 4000, 8 on one (32) 189 / 201; 4000, 32 on 8 (256) 459 / 453; 8 of up to 4096, 32 on 8 (1072)
-  // 1330 / 1267.  64 channels: 2500, 32 on 8 140 / 155; 8 of up to 4096 760 / 799; 2 of 8192, 32 on 8 (1024) 1954 / 1891; 32 channels 1284 / 1266
-  // and 512 / 519.  fp32: 4 of 2000, 8 on 2 (128) 1627 / 1582.
-  p.two_dkdv = !f32 && tiles(Tk, 128) <= (D <= 64 ? 1152 : 200);
+  // split: 2500, 32 on 8 (160 large tiles) 226 / 233; 4000, 8 on one (32) 189 / 201; 4000, 32 on 8 (256) 492 / 486; 3 of 2500 (480) 561 / 600;
+  // 8192 (512) 1779 / 1766; 12000 (752) 3737 / 3640; 8 of up to 4096 (1072) 1330 / 1267.  64 channels: 2500, 32 on 8 142 / 157; 8 of up to 4096
+  // 760 / 799; 2 of 8192, 32 on 8 (1024) 1954 / 1891; 32 channels 1284 / 1266 and 512 / 519.  fp32: 4 of 2000, 8 on 2 (128) 1627 / 1582.
+  p.two_dkdv = !f32 && tiles(Tk, 128) <= (D <= 64 ? 1152 : 512);
   // ... in parts of the rows.  Small tiles: 300 tokens, 4 on one (10 of 18), 1 part 43, 4 34, 8 32; 80 of 18, 1 part 42, 2 39, 4 44; 320 of
-  // 18, 1 part 49, 2 71; fp32, 304 of 37, 1 part 453, 2 431, 4 471.  Large ones, two workgroups a compute unit: 2500, 32 on 8 (160 of 156), 1
-  // part 459, 4 232, 8 262; 4000, 8 on one (32 of 500), 1 part 1270, 8 289, 16 230.
+  // 18, 1 part 49, 2 71; fp32, 304 of 37, 1 part 453, 2 431, 4 471.  64 keys, two workgroups a compute unit: 2500, 32 on 8 (320 small tiles), 1
+  // part 318, 3 226, 4 242; 4000, 8 on one (63), 1 part 776, 8 198, 16 189; 3 of 2500 (960), 1 part 561, 2 622.  128 keys in fp32: 4 of 2000, 8 on
+  // 2 (128 of 125), 1 part 3126, 4 1581, 8 1626.
   p.dkdv = p.few_dkdv   ? attn_splits((f32 ? 512 : 256) / tiles(Tk, 32), rows / seqs / 128, 1)
            : p.two_dkdv ? attn_splits(1024 / tiles(Tk, 64), rows / seqs / 64, 4)
                         : attn_splits((511 + tiles(Tk, 128)) / tiles(Tk, 128), rows / seqs / 64, 4);

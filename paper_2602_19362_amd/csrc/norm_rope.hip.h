@@ -74,6 +74,7 @@ __device__ __forceinline__ void token_angles(const NormRopeArgs& p, const Pieces
 // backwards 113 / 108 / 139 us, forward 71 / 73 / 72.
 constexpr int kRopeHeads = 2;
 
+// 16411 tokens of 32 + 8 heads of 128 in bf16: 336 MB in 67 us, 5.0 TB/s; a large copy reaches 5.07.  8 tokens 3.3 us, the launch.
 template <class T>
 __global__ __launch_bounds__(256) void k_qk_norm_rope_fwd(const NormRopeArgs p) {
   const int lane = threadIdx.x & 63, group = lane >> 4;
@@ -119,6 +120,7 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope_fwd(const NormRopeArgs p) 
   }
 }
 
+// The same tokens: 504 MB in 100 us, 5.1 TB/s, with the workgroups' sums for the gains.
 template <class T>
 __global__ __launch_bounds__(256) void k_qk_norm_rope_bwd(const NormRopeArgs p) {
   const int lane = threadIdx.x & 63, group = lane >> 4;
@@ -185,7 +187,7 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope_bwd(const NormRopeArgs p) 
 }
 
 // The gains' gradients from the workgroups' sums, in a fixed order: a workgroup for 16 channels, 64 slices of the workgroups, whose
-// sums are added in 64 bits.
+// sums are added in 64 bits.  Bound by its launch and a chain of loads: 4 us behind the call above.
 __global__ __launch_bounds__(1024) void k_gain_grads(const float* __restrict__ partials, int n, int D, float* __restrict__ dq_gain,
                                                      float* __restrict__ dk_gain) {
   __shared__ double all[64][17];

@@ -433,3 +433,12 @@ def test_tiles_of_128_keys(lengths, hq, hk, D):
 @pytest.mark.parametrize("bad", [math.nan, -math.inf])
 def test_what_is_not_finite_among_tiles_of_128_keys(bad):
     test_what_is_not_finite_among_many_tiles("bf16", bad, 3500, 32, 8, 128)
+
+
+@pytest.mark.parametrize("D", [80, 128])
+def test_tiles_of_128_keys_of_wide_heads(D):
+    _check("bf16", [2100, 2000, 1900, 2400], [2100, 2000, 1900, 2400], 16, 8, D, True, seed=260)
+
+
+def test_what_is_not_finite_among_tiles_of_128_keys_of_wide_heads():
+    test_what_is_not_finite_among_many_tiles("bf16", math.nan, 2100, 32, 32, 128)
