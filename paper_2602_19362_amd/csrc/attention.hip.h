@@ -433,7 +433,8 @@ __device__ __forceinline__ int all_rows_see(const AttnArgs& p, const SeqTile& t)
   return n < 0 ? 0 : n < t.nk ? n : t.nk;
 }
 
-constexpr int kFwdKeys = 32, kKeys = 64;   // keys staged at a time: forward, for dq
+template <int WK> constexpr int fwd_keys = WK == 2 ? 64 : 32;   // keys staged at a time: forward
+constexpr int kKeys = 64;                                        // ... for dq
 
 // ---------------------------------------------------------------------------------------------------------------- forward
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -668,8 +669,8 @@ template <class T, int DP, int WK, int KEYS>
 struct KeyLds {
   static constexpr int kTile = KEYS * Tile<T, DP>::kPitch, kSlots = WK == 4 && sizeof(T) == 4 ? 1 : 2;
   static constexpr int kStages = 2 * kSlots * kTile, kResults = 32 * (DP * 4 + 16);
-  static constexpr int kWave = WK == 1 || kStages > kResults ? kStages : (kResults + 511) / 512 * 512;
-  static constexpr int kWords = WK * kWave, kBytes = kWords + 48;
+  static constexpr int kEach = WK == 4 && kStages > kResults ? kStages : (kResults + 511) / 512 * 512;      // of a wavefront
+  static constexpr int kWords = WK == 1 || (WK == 2 && kStages > 4 * kEach) ? kStages : 4 * kEach, kBytes = kWords + 48;
   static_assert(kBytes <= 160 * 1024, "LDS of one CU");
 };
 
@@ -707,17 +708,19 @@ __device__ __forceinline__ float* partial_row(const AttnArgs& p, int part, int64
 // run beside another's products.  Bound by the matrix cores at the clock that the power limit leaves, and by the exponentials' issue
 // between them: 4 x 8192 tokens, 32 heads on 8 of 128 channels, no mask, 1066 ... 1156 TFLOP/s by box (a 16384^3 product of the vendor's library
 // 1353), matrix cores busy 0.53 of the time at 1.7 GHz.  64 keys at a time by two wavefronts a SIMD: 5 % less.
+// WK = 2, for few rounds of tiles: 64 rows, two wavefronts for either half of 64 keys; they join at the end.
 // WK = 4, for few rows: the wavefronts have the same 32 rows and take the steps of 32 keys in turn, each through LDS of its own, and
 // join at the end.  That is bound by reading the keys and values: 64 single tokens over up to 4096 each, 8 key heads, 599 MB in 109 us,
 // 5.5 TB/s; 8 over 32768 in parts, 1.07 GB in 181 us, 5.9 TB/s (a large read reaches 5.95).
 // Where tiles are few, their keys are split over workgroups whose results k_attn_join puts together.
 template <class T, int DW, int WK>
-__global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k_attn_fwd(const AttnArgs p) {
-  constexpr int DP = padded(DW);
+__global__ __launch_bounds__(256, WK == 4 ? 1 : WK == 2 && DW > 64 ? 2 : sizeof(T) == 2 ? 3 : 2) void k_attn_fwd(const AttnArgs p) {
+  constexpr bool kAlone = WK == 4;      // a wavefront stages keys for itself
+  constexpr int DP = padded(DW), KEYS = fwd_keys<WK>, W = kAlone ? 1 : 4, STEP = KEYS * 4 / W;
   typedef typename FragOf<T>::type Frag;
   typedef Tile<T, DP> Lds;
-  typedef Stager<T, DP, kFwdKeys, 4 / WK> Stage;
-  typedef KeyLds<T, DP, WK, kFwdKeys> Size;
+  typedef Stager<T, DP, KEYS, W> Stage;
+  typedef KeyLds<T, DP, WK, KEYS> Size;
   constexpr int B = 128 / WK, KS = DW / 32, DB = DW / 16, SIZE = Size::kTile;
   extern __shared__ char smem[];
   const Job job(p);
@@ -730,21 +733,21 @@ __global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k
     if (p.lse) poison(p.lse, p.Tq * p.hq);
   }
   if (found != kTile) return;
-  const int wave = uniform((int)threadIdx.x >> 6);
-  const lds_char_ptr lds = (lds_char_ptr)smem + (WK == 1 ? 0 : wave * Size::kWave);     // slots of keys and values
-  const Part part(tile_sees<B>(p, t), p.splits, job.part, kFwdKeys * WK);
+  const int wave = uniform((int)threadIdx.x >> 6), half = WK == 2 ? (wave >> 1) * 32 : 0;      // of the staged keys, this wavefront's
+  const lds_char_ptr lds = (lds_char_ptr)smem + (kAlone ? wave * Size::kEach : 0);     // slots of keys and values
+  const Part part(tile_sees<B>(p, t), p.splits, job.part, STEP);
   const Stage ks(p.k.row(t.k0, kh), p.k.token, p.D), vs(p.v.row(t.k0, kh), p.v.token, p.D);
-  int j0 = part.begin + (WK == 1 ? 0 : wave * kFwdKeys), slot = 0;
+  int j0 = part.begin + (kAlone ? wave * KEYS : 0), slot = 0;
   const lds_char_ptr words = (lds_char_ptr)smem + Size::kWords;
   // whether a step has keys that some rows of the tile see and others do not
   const int first_sees = all_rows_see(p, t), last_sees = tile_sees<B>(p, t);
-  const auto masks = [&](int from) { return first_sees < last_sees && from + kFwdKeys > first_sees; };
+  const auto masks = [&](int from) { return first_sees < last_sees && from + KEYS > first_sees; };
   const auto stage = [&](int at, int first) {
     ks.start(lds + at, first, t.nk);
     vs.start(lds + at + SIZE, first, t.nk);
   };
   if (Size::kSlots == 2 && j0 < part.end) stage(0, j0);
-  const int group = threadIdx.x >> 4 & 3, row0 = t.first + (WK == 1 ? wave * 32 : 0) + (threadIdx.x & 15);
+  const int group = threadIdx.x >> 4 & 3, row0 = t.first + wave % (4 / WK) * 32 + (threadIdx.x & 15);
   const float scale2 = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;
   int row_sees[2];
   Frag q[2][KS];
@@ -775,27 +778,28 @@ __global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k
     all_see = y < all_see ? y : all_see;
   }
   all_see = __builtin_amdgcn_readfirstlane(all_see);
-  for (; j0 < part.end; j0 += kFwdKeys * WK, slot ^= Size::kSlots == 2 ? 2 * SIZE : 0) {
+  for (; j0 < part.end; j0 += STEP, slot ^= Size::kSlots == 2 ? 2 * SIZE : 0) {
     if (Size::kSlots == 1) stage(0, j0);
     staged();
-    bool odd = masks(j0) && staged_odd<T, Stage::kLoads, 4 / WK>(lds + slot + SIZE);
-    if (WK == 1) {
+    bool odd = masks(j0) && staged_odd<T, Stage::kLoads, W>(lds + slot + SIZE);
+    if (!kAlone) {
       if (masks(j0)) tell_odd(words, slot != 0, odd);
       lds_barrier();
       odd = masks(j0) && told_odd(words, slot != 0);
     }
-    if (Size::kSlots == 2 && j0 + kFwdKeys * WK < part.end) stage(slot ^ 2 * SIZE, j0 + kFwdKeys * WK);
-    const int k_rows = Lds::rows_place(lds + slot, threadIdx.x), v_columns = Lds::columns_place(lds + slot + SIZE, threadIdx.x);
+    if (Size::kSlots == 2 && j0 + STEP < part.end) stage(slot ^ 2 * SIZE, j0 + STEP);
+    const lds_char_ptr own = lds + slot + half * Lds::kPitch;
+    const int k_rows = Lds::rows_place(own, threadIdx.x), v_columns = Lds::columns_place(own + SIZE, threadIdx.x);
     f32x4 s[2][2];     // [rows][keys]
     scores<Lds, KS>(s, k_rows, 0, q, [](int) {});
-    if (odd) mark_odd(s, (uint32_t)clean_tile<T, DP, kFwdKeys, 4 / WK>(lds + slot + SIZE, words + 32));
-    if (j0 + kFwdKeys > all_see) {
+    if (odd) mark_odd(s, (uint32_t)(clean_tile<T, DP, KEYS, W>(lds + slot + SIZE, words + 32) >> half));
+    if (j0 + half + 32 > all_see) {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
           const int key = (x >> 2) * 16 + group * 4 + (x & 3);
-          if (j0 + key >= row_sees[n]) s[n][x >> 2][x & 3] = -__builtin_inff();
+          if (j0 + half + key >= row_sees[n]) s[n][x >> 2][x & 3] = -__builtin_inff();
         }
     }
     // The maximum that the exponentials are taken from follows only when it falls behind by 2^8: until then they stay below 2^8, and
@@ -853,15 +857,15 @@ __global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k
       if (p.lse && group == 0) p.lse[(t.q0 + row.token) * p.hq + head] = finish(m[n] * scale2, l[n]);
     }
   } else {
-    // The wavefronts' results in LDS, then eight threads a row.
-    constexpr int PITCH = DP * 4 + 16;
+    // The wavefronts' results in LDS, then two threads a row for each wavefront that had it.
+    constexpr int PITCH = DP * 4 + 16, G = 4 / WK, C = DW / (2 * WK);
     typedef __attribute__((address_space(3))) float* lds_f32;
     typedef __attribute__((address_space(3))) f32x4* lds_f32x4;
     __syncthreads();      // everybody has read its last tile
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       l[n] = row_sum(l[n]);
-      const lds_char_ptr to = lds + (n * 16 + (threadIdx.x & 15)) * PITCH;
+      const lds_char_ptr to = (lds_char_ptr)smem + wave * Size::kEach + (n * 16 + (threadIdx.x & 15)) * PITCH;
 #pragma unroll
       for (int d = 0; d < DB; ++d) *(lds_f32x4)(to + d * 64 + group * 16) = o[n][d];
       if (group == 0) {
@@ -870,33 +874,33 @@ __global__ __launch_bounds__(256, WK == 1 ? (sizeof(T) == 2 ? 3 : 2) : 1) void k
       }
     }
     __syncthreads();
-    const int r = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * (DW / 8);
+    const int r = threadIdx.x / (2 * WK), c0 = threadIdx.x % (2 * WK) * C;
     const Row row(p, t, t.first + r);
-    const lds_char_ptr from = (lds_char_ptr)smem + r * PITCH;
+    const lds_char_ptr from = (lds_char_ptr)smem + r / 32 * Size::kEach + r % 32 * PITCH;
     float top = kNegHuge, sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, *(lds_f32)(from + w * Size::kWave + DP * 4));
-    f32x4 x[DW / 32] = {};
+    for (int w = 0; w < WK; ++w) top = fmaxf(top, *(lds_f32)(from + w * G * Size::kEach + DP * 4));
+    f32x4 x[C / 4] = {};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float by = __builtin_amdgcn_exp2f(*(lds_f32)(from + w * Size::kWave + DP * 4) - top);
-      sum = fmaf(*(lds_f32)(from + w * Size::kWave + DP * 4 + 4), by, sum);
+    for (int w = 0; w < WK; ++w) {
+      const float by = __builtin_amdgcn_exp2f(*(lds_f32)(from + w * G * Size::kEach + DP * 4) - top);
+      sum = fmaf(*(lds_f32)(from + w * G * Size::kEach + DP * 4 + 4), by, sum);
 #pragma unroll
-      for (int c = 0; c < DW / 32; ++c) x[c] += *(lds_f32x4)(from + w * Size::kWave + (c0 + c * 4) * 4) * by;
+      for (int c = 0; c < C / 4; ++c) x[c] += *(lds_f32x4)(from + w * G * Size::kEach + (c0 + c * 4) * 4) * by;
     }
     if (!row.exists) return;
     const int head = kh * p.g + row.head;
     if (p.splits > 1) {
       const int64_t at = packed_row(p, t, kh, t.first + r);
 #pragma unroll
-      for (int c = 0; c < DW / 32; ++c)
+      for (int c = 0; c < C / 4; ++c)
         if (c0 + c * 4 < p.D) store4(partial_row(p, job.part, p.Tq * p.hq, at) + c0 + c * 4, x[c]);
       if (c0 == 0) store_sums(p, job.part, at, top, sum);
       return;
     }
     T* to = (T*)p.o.row(t.q0 + row.token, head);
 #pragma unroll
-    for (int c = 0; c < DW / 32; ++c)
+    for (int c = 0; c < C / 4; ++c)
       if (c0 + c * 4 < p.D) store4(to + c0 + c * 4, x[c] * inverse(sum));
     if (p.lse && c0 == 0) p.lse[(t.q0 + row.token) * p.hq + head] = finish(top, sum);
   }
@@ -1012,7 +1016,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
   constexpr int B = 128 / WK, KS = DW / 32, DB = DW / 16, SIZE = Size::kTile;
   extern __shared__ char smem[];
   const int wave = uniform((int)threadIdx.x >> 6);
-  const lds_char_ptr lds = (lds_char_ptr)smem + (WK == 1 ? 0 : wave * Size::kWave), words = (lds_char_ptr)smem + Size::kWords;
+  const lds_char_ptr lds = (lds_char_ptr)smem + (WK == 1 ? 0 : wave * Size::kEach), words = (lds_char_ptr)smem + Size::kWords;
   const Job job(p);
   const int kh = job.kh;
   SeqTile t;
@@ -1133,7 +1137,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
       else store_columns<T>(p.dq.row(t.q0 + row.token, kh * p.g + row.head), dq[n], p.scale, p.D);
     }
   } else {
-    add_wavefronts<DW, 4>(dq, (lds_char_ptr)smem, Size::kWave, [&](int r, int c0, const auto& x) {
+    add_wavefronts<DW, 4>(dq, (lds_char_ptr)smem, Size::kEach, [&](int r, int c0, const auto& x) {
       const Row row(p, t, t.first + r);
       if (!row.exists) return;
       if (p.splits > 1) store_share<float>((char*)partial_row(p, job.part, p.Tq * p.hq, packed_row(p, t, kh, t.first + r)), c0, x, 1.f, p.D);

@@ -76,7 +76,7 @@ static int rope_args(NormRopeArgs& a, const oapl_heads* q, const oapl_heads* k, 
 // channels where nothing else is said, as replayed graphs on one MI355X; of backward, both kernels together with the other one's cut fixed.
 struct AttnPlan {
   bool few = false, few_dq = false, few_dkdv = false;      // tiles of 32 rows (keys) whose wavefronts share the steps
-  bool two_dkdv = false;               // tiles of 64 keys whose wavefronts share each step's rows
+  bool two = false, two_dkdv = false;  // tiles of 64 rows (keys) whose wavefronts share each step's keys (rows)
   int fwd = 1, dq = 1, dkdv = 1;       // workgroups that share a tile's steps
   size_t off_lse2 = 0, off_delta = 0, off_sums = 0, off_partials = 0, total = 0;
 };
@@ -100,8 +100,12 @@ static void attn_cut(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int g, int 
   // to put together than they save: 4 x 32 rows over 2000 keys, 4 parts 16, 8 parts (of two steps) 19.
   // Large ones where few tiles have long walks: 8000 tokens, 4 heads on one (250 tiles of 250 steps), 1 part 217, 4 90; 1000 tokens, 32 on 8
   // (256 of 31), 1 part 35.5, 2 37.5.
-  p.fwd = p.few ? attn_splits(256 / tiles(rows, 32), Tk / seqs / (4 * kFwdKeys), 3)
-                : attn_splits(1024 / tiles(rows, 128), Tk / seqs / kFwdKeys, 32);
+  p.fwd = p.few ? attn_splits(256 / tiles(rows, 32), Tk / seqs / 128, 3)
+                : attn_splits(1024 / tiles(rows, 128), Tk / seqs / 32, 32);
+  // Tiles of 64 rows halve a walk: where large ones would be few rounds, their keys are not split, and walks are long enough for what starting
+  // twice as many costs.  64 / 128 rows: 1000 tokens, 32 on 8 (256 large tiles of 31 steps) 26 / 36; 1500 (376 of 46) 40 / 51; 2500 (632) 85 / 81; 4
+  // of 300 (320 of 9) 24 / 18; 4 of 1000, 16 on 8 (512) 43 / 40.  64 channels: 2500 (632) 46 / 57; 4 of 1000 (512) 21 / 28; 4000 (1000) 95 / 95.
+  p.two = !f32 && !p.few && p.fwd == 1 && Tk / seqs / 32 >= 24 && tiles(rows, 128) <= (D <= 64 ? 768 : 400);
   // dq: tiles of 32 rows up to two rounds.  32 rows / 128 rows, each at its best split: 64 channels, 1000 tokens, 6 heads (192 small tiles)
   // 48 / 55; 1200, 8 heads (304) 46 / 52; 300, 32 on 8 (304) 79 / 78; 4 of 1000, 4 on one (500) 187 / 193; 4800, 8 on 2 (1200) 278 / 241;
   // 1000, 32 on 8 (1000) 213 / 199.  fp32: 80 channels, 4 of 400, 6 on 2 (304) 291 / 301; 64 channels, 2 of 1000, 16 on 8 (1008) 362 / 401; 8
@@ -206,8 +210,16 @@ static int launch_attn_fwd(AttnArgs a, const AttnPlan& p, hipStream_t st) {
   a.splits = p.fwd;
   const int64_t rows = a.Tq * a.g;
   constexpr int DP = padded(DW);
-  const int rc = p.few ? launch_attn<k_attn_fwd<T, DW, 4>, KeyLds<T, DP, 4, kFwdKeys>::kBytes>(tile_ids<32>(rows, a.n_seq) * a.hk, a, st)
-                       : launch_attn<k_attn_fwd<T, DW, 1>, KeyLds<T, DP, 1, kFwdKeys>::kBytes>(tile_ids<128>(rows, a.n_seq) * a.hk, a, st);
+  const auto fwd = [&](auto wk) {
+    constexpr int WK = wk, B = 128 / WK;
+    return launch_attn<k_attn_fwd<T, DW, WK>, KeyLds<T, DP, WK, fwd_keys<WK>>::kBytes>(tile_ids<B>(rows, a.n_seq) * a.hk, a, st);
+  };
+  int rc;
+  if constexpr (sizeof(T) == 2) {
+    rc = p.few ? fwd(std::integral_constant<int, 4>{}) : p.two ? fwd(std::integral_constant<int, 2>{}) : fwd(std::integral_constant<int, 1>{});
+  } else {
+    rc = p.few ? fwd(std::integral_constant<int, 4>{}) : fwd(std::integral_constant<int, 1>{});
+  }
   if (rc != OAPL_OK || p.fwd == 1 || a.Tq == 0) return rc;
   k_attn_join<T><<<grid1d(a.Tq * a.hq, 8), 256, 0, st>>>(a);
   OAPL_LAUNCH_CHECK();

@@ -442,3 +442,10 @@ def test_tiles_of_128_keys_of_wide_heads(D):
 
 def test_what_is_not_finite_among_tiles_of_128_keys_of_wide_heads():
     test_what_is_not_finite_among_many_tiles("bf16", math.nan, 2100, 32, 32, 128)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("D", [24, 64, 96, 128])
+def test_tiles_of_64_rows(D, causal):
+    _check("bf16", [1300, 900, 50], [1300, 1000, 700], 16, 8, D, causal, seed=270)
+    _check("bf16", [1100, 0, 1200], [900, 700, 1200], 16, 8, D, causal, seed=273)
