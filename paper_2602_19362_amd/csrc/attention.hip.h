@@ -434,7 +434,7 @@ __device__ __forceinline__ int all_rows_see(const AttnArgs& p, const SeqTile& t)
 }
 
 template <int WK> constexpr int fwd_keys = WK == 2 ? 64 : 32;   // keys staged at a time: forward
-constexpr int kKeys = 64;                                        // ... for dq
+template <int WK> constexpr int dq_keys = WK == 4 ? 32 : 64;    // ... for dq
 
 // ---------------------------------------------------------------------------------------------------------------- forward
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -1001,22 +1001,24 @@ __device__ __forceinline__ void store_share(char* row, int c0, const f32x4 (&x)[
 }
 
 // dq, and what the other kernel needs of a row: its log-sum-exp in base 2 and D_i.  A workgroup has 128 rows over steps of 64 keys or,
-// where tiles are few (WK = 4), 32 rows over steps of 32 keys that the wavefronts take in turn, as forward.
+// where tiles are few, 64 rows, two wavefronts for either half of the keys (WK = 2), or 32 rows over steps of 32 keys that the wavefronts take in
+// turn (WK = 4), as forward.
 // dq is summed here and dk, dv in the other kernel, which computes z and dP again (seven products, not five): one kernel would add to dq in
 // memory from all tiles of keys, by atomics in an order that changes, or through sums of (keys / 128) x dq's size.
 // Bound by the matrix cores at the power limit: 2 x 8192 tokens, 32 heads on 8 of 128 channels, no mask, three products in 2.78 ms, 1186
 // TFLOP/s, matrix cores busy 0.59 at 1.87 GHz.
 template <class T, int DW, int WK>
 __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
-  constexpr int DP = padded(DW), KEYS = kKeys / (WK == 1 ? 1 : 2);
+  constexpr bool kAlone = WK == 4;      // a wavefront stages keys for itself
+  constexpr int DP = padded(DW), KEYS = dq_keys<WK>, W = kAlone ? 1 : 4, STEP = KEYS * 4 / W, PER = WK == 1 ? KEYS : 32;      // PER: a wavefront's
   typedef typename FragOf<T>::type Frag;
   typedef Tile<T, DP> Lds;
-  typedef Stager<T, DP, KEYS, 4 / WK> Stage;
+  typedef Stager<T, DP, KEYS, W> Stage;
   typedef KeyLds<T, DP, WK, KEYS> Size;
   constexpr int B = 128 / WK, KS = DW / 32, DB = DW / 16, SIZE = Size::kTile;
   extern __shared__ char smem[];
-  const int wave = uniform((int)threadIdx.x >> 6);
-  const lds_char_ptr lds = (lds_char_ptr)smem + (WK == 1 ? 0 : wave * Size::kEach), words = (lds_char_ptr)smem + Size::kWords;
+  const int wave = uniform((int)threadIdx.x >> 6), half = WK == 2 ? (wave >> 1) * 32 : 0;      // of the staged keys, this wavefront's
+  const lds_char_ptr lds = (lds_char_ptr)smem + (kAlone ? wave * Size::kEach : 0), words = (lds_char_ptr)smem + Size::kWords;
   const Job job(p);
   const int kh = job.kh;
   SeqTile t;
@@ -1025,15 +1027,15 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
   if (found == kMalformed) poison<T>(p.dq, p.Tq, p.hq, p.D);
   if (found != kTile) return;
   const int first_sees = all_rows_see(p, t), last_sees = tile_sees<B>(p, t);
-  const Part part(last_sees, p.splits, job.part, KEYS * WK);
+  const Part part(last_sees, p.splits, job.part, STEP);
   const Stage ks(p.k.row(t.k0, kh), p.k.token, p.D), vs(p.v.row(t.k0, kh), p.v.token, p.D);
-  int j0 = part.begin + (WK == 1 ? 0 : wave * KEYS), slot = 0;
+  int j0 = part.begin + (kAlone ? wave * KEYS : 0), slot = 0;
   const auto stage = [&](int at, int first) {
     ks.start(lds + at, first, t.nk);
     vs.start(lds + at + SIZE, first, t.nk);
   };
   if (Size::kSlots == 2 && j0 < part.end) stage(0, j0);
-  const int group = threadIdx.x >> 4 & 3, row0 = t.first + (WK == 1 ? wave * 32 : 0) + (threadIdx.x & 15);
+  const int group = threadIdx.x >> 4 & 3, row0 = t.first + wave % (4 / WK) * 32 + (threadIdx.x & 15);
   const float scale2 = p.scale * kLog2e;
   int row_sees[2];
   Frag q[2][KS], dout[2][KS];
@@ -1056,7 +1058,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
     for (int kk = 0; kk < KS; ++kk) delta[n] += dot(o[kk], dout[n][kk]);
     delta[n] = row_sum(delta[n]);
     lse2[n] = row.exists ? p.lse[token * p.hq + head] * kLog2e : 0.f;
-    if (row.exists && group == 0 && job.part == 0 && (WK == 1 || wave == 0)) {
+    if (row.exists && group == 0 && job.part == 0 && wave < 4 / WK) {
       const int64_t at = packed_row(p, t, kh, row0 + n * 16);
       p.delta[at] = delta[n];
       // of a row that sees nothing: every probability comes out as 0
@@ -1071,20 +1073,21 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
     all_see = y < all_see ? y : all_see;
   }
   all_see = __builtin_amdgcn_readfirstlane(all_see);
-  for (; j0 < part.end; j0 += KEYS * WK, slot ^= Size::kSlots == 2 ? 2 * SIZE : 0) {
+  for (; j0 < part.end; j0 += STEP, slot ^= Size::kSlots == 2 ? 2 * SIZE : 0) {
     const bool masks = first_sees < last_sees && j0 + KEYS > first_sees;
     if (Size::kSlots == 1) stage(0, j0);
     staged();
-    bool found_odd = masks && staged_odd<T, Stage::kLoads, 4 / WK>(lds + slot);
-    if (WK == 1) {
+    bool found_odd = masks && staged_odd<T, Stage::kLoads, W>(lds + slot);
+    if (!kAlone) {
       if (masks) tell_odd(words, slot != 0, found_odd);
       lds_barrier();
       found_odd = masks && told_odd(words, slot != 0);
     }
-    if (Size::kSlots == 2 && j0 + KEYS * WK < part.end) stage(slot ^ 2 * SIZE, j0 + KEYS * WK);
-    const int k_rows = Lds::rows_place(lds + slot, threadIdx.x), k_columns = Lds::columns_place(lds + slot, threadIdx.x);
-    const uint64_t odd = found_odd ? clean_tile<T, DP, KEYS, 4 / WK>(lds + slot, words + 32) : 0;
-    f32x4 s[2][2][2], dp[2][2][2];     // [half][rows][keys]
+    if (Size::kSlots == 2 && j0 + STEP < part.end) stage(slot ^ 2 * SIZE, j0 + STEP);
+    const lds_char_ptr own = lds + slot + half * Lds::kPitch;
+    const int k_rows = Lds::rows_place(own, threadIdx.x), k_columns = Lds::columns_place(own, threadIdx.x);
+    const uint64_t odd = found_odd ? clean_tile<T, DP, KEYS, W>(lds + slot, words + 32) >> half : 0;
+    f32x4 s[2][2][2], dp[2][2][2];     // [32 keys][rows][keys]
     Frag w[2][2];
     const auto finish = [&](int c, int i) {
       const int n = i >> 3, x = i & 7;
@@ -1092,27 +1095,27 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
     };
     const auto mask = [&](int c) {
       if (odd) mark_odd(s[c], (uint32_t)(odd >> (c * 32)));
-      if (j0 + c * 32 + 32 > all_see) {
+      if (j0 + half + c * 32 + 32 > all_see) {
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
           for (int x = 0; x < 8; ++x) {
             const int key = (x >> 2) * 16 + group * 4 + (x & 3);
-            if (j0 + c * 32 + key >= row_sees[n]) s[c][n][x >> 2][x & 3] = 0.f;
+            if (j0 + half + c * 32 + key >= row_sees[n]) s[c][n][x >> 2][x & 3] = 0.f;
           }
       }
 #pragma unroll
       for (int n = 0; n < 2; ++n) pack(s[c][n][0], s[c][n][1], w[c][n]);
       ready(w[c]);
     };
-    // the elements [from, to) of half c that go with one of n pairs of multiplications
+    // the elements [from, to) of 32 keys c that go with one of n pairs of multiplications
     const auto share = [&](int c, int from, int to, int i, int n) {
 #pragma unroll
       for (int x = from + (to - from) * i / n; x < from + (to - from) * (i + 1) / n; ++x) finish(c, x);
     };
     scores<Lds, KS>(s[0], k_rows, 0, q, [](int) {});
     scores<Lds, KS>(dp[0], k_rows, SIZE, dout, [](int) {});
-    if constexpr (KEYS == 64) {
+    if constexpr (PER == 64) {
       scores<Lds, KS>(s[1], k_rows, 32 * Lds::kPitch, q, [&](int i) { share(0, 0, 8, i, 2 * KS); });
       scores<Lds, KS>(dp[1], k_rows, SIZE + 32 * Lds::kPitch, dout, [&](int i) { share(0, 8, 16, i, 2 * KS); });
     } else {
@@ -1120,9 +1123,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
     }
     mask(0);
     add_columns<Lds, DB>(dq, k_columns, 0, w[0], [&](int i) {
-      if (KEYS == 64) share(1, 0, 16, i, DB);
+      if (PER == 64) share(1, 0, 16, i, DB);
     });
-    if constexpr (KEYS == 64) {
+    if constexpr (PER == 64) {
       mask(1);
       add_columns<Lds, DB>(dq, k_columns, 32 * Lds::kPitch, w[1], [](int) {});
     }
@@ -1137,7 +1140,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
       else store_columns<T>(p.dq.row(t.q0 + row.token, kh * p.g + row.head), dq[n], p.scale, p.D);
     }
   } else {
-    add_wavefronts<DW, 4>(dq, (lds_char_ptr)smem, Size::kEach, [&](int r, int c0, const auto& x) {
+    add_wavefronts<DW, WK>(dq, (lds_char_ptr)smem, Size::kEach, [&](int r, int c0, const auto& x) {
       const Row row(p, t, t.first + r);
       if (!row.exists) return;
       if (p.splits > 1) store_share<float>((char*)partial_row(p, job.part, p.Tq * p.hq, packed_row(p, t, kh, t.first + r)), c0, x, 1.f, p.D);

@@ -76,7 +76,7 @@ static int rope_args(NormRopeArgs& a, const oapl_heads* q, const oapl_heads* k, 
 // channels where nothing else is said, as replayed graphs on one MI355X; of backward, both kernels together with the other one's cut fixed.
 struct AttnPlan {
   bool few = false, few_dq = false, few_dkdv = false;      // tiles of 32 rows (keys) whose wavefronts share the steps
-  bool two = false, two_dkdv = false;  // tiles of 64 rows (keys) whose wavefronts share each step's keys (rows)
+  bool two = false, two_dq = false, two_dkdv = false;      // tiles of 64 rows (keys) whose wavefronts share each step's keys (rows)
   int fwd = 1, dq = 1, dkdv = 1;       // workgroups that share a tile's steps
   size_t off_lse2 = 0, off_delta = 0, off_sums = 0, off_partials = 0, total = 0;
 };
@@ -114,8 +114,12 @@ static void attn_cut(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int g, int 
   // ... in parts of the keys.  Small tiles: 16 rows over 4096 keys (2 of 32 steps), 1 part 50, 4 30, 8 25; 64 rows over 1024 (8 of 8), 1
   // part 28, 2 27; 2000 tokens, one head (63 of 15), 1 part 57, 2 52; 192 of 7, 1 part 48, 2 51.  Large ones: 9000, 4 on one (282 of 140), 1
   // part 456, 2 373, 3 355; 1000, 32 on 8 (256 of 15), 1 part 199, 2 200; 2500, 32 on 8 (632 of 39), 1 part 460, 2 491.
-  p.dq = p.few_dq ? attn_splits(256 / tiles(rows, 32), Tk / seqs / (2 * kKeys), 4)
-                  : attn_splits(900 / tiles(rows, 128), Tk / seqs / kKeys, 24);
+  p.dq = p.few_dq ? attn_splits(256 / tiles(rows, 32), Tk / seqs / 128, 4)
+                  : attn_splits(900 / tiles(rows, 128), Tk / seqs / 64, 24);
+  // ... of 64 rows where large ones are few rounds and not cut, as forward.  64 / 128 rows: 600 tokens, 32 on 8 (152 large tiles of 9 steps) 61 / 63;
+  // 1000 (256) 89 / 95; 1500 (376) 123 / 130; 2500 (632) 235 / 223; 4 of 300 (320 of 4) 55 / 48.  64 channels: 13 of up to 400, 14 on 2 (572) 44 / 46;
+  // 4 of 1000, 16 on 8 (512) 80 / 79, 32 channels 52 / 57; 4000, 32 on 8 (1000) 286 / 286.
+  p.two_dq = !f32 && !p.few_dq && p.dq == 1 && tiles(rows, 128) <= (D <= 64 ? 640 : 400) && (D <= 64 || Tk / seqs / 64 >= 8);
   // dk, dv: tiles of 32 keys up to a work of 64 (fp32: 128) steps of 64 rows a compute unit; their wavefronts have a SIMD each, which costs
   // rate and saves time where work is short.  32 keys / 128 keys, each at its best split: 300 tokens, 32 on 8 (80 small tiles of 18
   // steps) 39 / 47; 4 of 300, 32 on 8 (320 of 18) 49 / 64; 64 channels, 1000, 6 heads (192 of 15) 42 / 50; 1000, 32 on 8 (256 of 62) 90 / 94;
@@ -231,12 +235,20 @@ static int launch_attn_bwd(AttnArgs a, const AttnPlan& p, hipStream_t st) {
   constexpr int DP = padded(DW);
   a.splits = p.dq;
   const int64_t rows = a.Tq * a.g;
-  int rc = p.few_dq ? launch_attn<k_attn_dq<T, DW, 4>, KeyLds<T, DP, 4, kKeys / 2>::kBytes>(tile_ids<32>(rows, a.n_seq) * a.hk, a, st)
-                    : launch_attn<k_attn_dq<T, DW, 1>, KeyLds<T, DP, 1, kKeys>::kBytes>(tile_ids<128>(rows, a.n_seq) * a.hk, a, st);
+  const auto dq = [&](auto wk) {
+    constexpr int WK = wk, B = 128 / WK;
+    return launch_attn<k_attn_dq<T, DW, WK>, KeyLds<T, DP, WK, dq_keys<WK>>::kBytes>(tile_ids<B>(rows, a.n_seq) * a.hk, a, st);
+  };
+  int rc;
+  if constexpr (sizeof(T) == 2) {
+    rc = p.few_dq ? dq(std::integral_constant<int, 4>{}) : p.two_dq ? dq(std::integral_constant<int, 2>{}) : dq(std::integral_constant<int, 1>{});
+  } else {
+    rc = p.few_dq ? dq(std::integral_constant<int, 4>{}) : dq(std::integral_constant<int, 1>{});
+  }
   if (rc != OAPL_OK) return rc;
   if (p.dq > 1 && a.Tq > 0) {
-    const GradSum dq{a.dq, a.partials, a.scale};
-    k_attn_add<T><<<grid1d(a.Tq * a.hq, 8), 256, 0, st>>>(a, dq, dq, a.Tq * a.hq * a.D, a.Tq, a.g);
+    const GradSum sum{a.dq, a.partials, a.scale};
+    k_attn_add<T><<<grid1d(a.Tq * a.hq, 8), 256, 0, st>>>(a, sum, sum, a.Tq * a.hq * a.D, a.Tq, a.g);
     OAPL_LAUNCH_CHECK();
   }
   a.splits = p.dkdv;
