@@ -120,25 +120,28 @@ static void attn_cut(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int g, int 
   // 1000 (256) 89 / 95; 1500 (376) 123 / 130; 2500 (632) 235 / 223; 4 of 300 (320 of 4) 55 / 48.  64 channels: 13 of up to 400, 14 on 2 (572) 44 / 46;
   // 4 of 1000, 16 on 8 (512) 80 / 79, 32 channels 52 / 57; 4000, 32 on 8 (1000) 286 / 286.
   p.two_dq = !f32 && !p.few_dq && p.dq == 1 && tiles(rows, 128) <= (D <= 64 ? 640 : 400) && (D <= 64 || Tk / seqs / 64 >= 8);
-  // dk, dv: tiles of 32 keys up to a work of 64 (fp32: 128) steps of 64 rows a compute unit; their wavefronts have a SIMD each, which costs
-  // rate and saves time where work is short.  32 keys / 128 keys, each at its best split: 300 tokens, 32 on 8 (80 small tiles of 18
-  // steps) 39 / 47; 4 of 300, 32 on 8 (320 of 18) 49 / 64; 64 channels, 1000, 6 heads (192 of 15) 42 / 50; 1000, 32 on 8 (256 of 62) 90 / 94;
-  // 4000, 8 on one (125 of 500) 259 / 230; 2500, 32 on 8 (632 of 156) 280 / 232.  fp32: 80 channels, 4 of 400, 6 on 2 (104 of 18) 138 / 150; 64
-  // channels, 8 of 1000, 8 heads (2048 of 15) 338 / 358; 4 of 2000, 8 on 2 (504 of 125) 1634 / 1590; 96 channels, 8000, 8 on 2 (500 of 500)
-  // 3530 / 3353; 4 of 4000, 8 heads (4000 of 62) 6267 / 5964.
-  const int64_t work = tiles(Tk, 32) * std::max<int64_t>(1, rows / seqs / 64);
-  p.few_dkdv = work <= 256 * (f32 ? 128 : 64);
+  // dk, dv: tiles of 32 keys where they are few (a workgroup of 128 channels has a compute unit's LDS for itself, of 64 channels half of it) and
+  // their walks, in steps of 64 rows, short; their wavefronts have a SIMD each, which saves time there and costs rate.  32 / 64 / 128 keys, each at
+  // its best split: 300 tokens, 32 on 8 (80 small tiles of 18 steps) 39 / 44 / 48; 4 of 300 (320 of 18) 48 / 59 / 64; 1000 (256 of 62) 83 / 78 / 87; 1500
+  // (376 of 93) 129 / 119 / 135; 16 of 200, 16 on 8 (896 of 6) 64 / 48 / 54; 4 of 1000, 16 on 8 (1024 of 31) 126 / 102 / 116.  64 channels: 13 of up
+  // to 400, 14 on 2 (338 of 43) 37 / 44 / 47; 4 of 1000, 16 on 8 (1024 of 31) 68 / 75 / 78; 64 of up to 120, 8 heads (2048 of one) 32 / 24 / 25.
+  // fp32, 32 / 128: 80 channels, 4 of 400, 6 on 2 (104 of 18) 138 / 150; 64 channels, 8 of 1000, 8 heads (2048 of 15) 338 / 358; 4 of 2000, 8 on 2
+  // (504 of 125) 1634 / 1590; 96 channels, 8000, 8 on 2 (500 of 500) 3530 / 3353; 4 of 4000, 8 heads (4000 of 62) 6267 / 5964.
+  const int64_t small = tiles(Tk, 32), work = small * std::max<int64_t>(1, rows / seqs / 64);
+  p.few_dkdv = f32 ? work <= 256 * 128 : D <= 64 ? small <= 1024 && work <= 256 * 128 : small <= 400 && work <= 256 * 64;
   // Tiles of 64 keys halve the longest walks, which end a call of few rounds, and read rows twice as often.  64 / 128 keys, each at its best
   // split: 2500, 32 on 8 (160 large tiles) 226 / 233; 4000, 8 on one (32) 189 / 201; 4000, 32 on 8 (256) 492 / 486; 3 of 2500 (480) 561 / 600;
   // 8192 (512) 1779 / 1766; 12000 (752) 3737 / 3640; 8 of up to 4096 (1072) 1330 / 1267.  64 channels: 2500, 32 on 8 142 / 157; 8 of up to 4096
   // 760 / 799; 2 of 8192, 32 on 8 (1024) 1954 / 1891; 32 channels 1284 / 1266 and 512 / 519.  fp32: 4 of 2000, 8 on 2 (128) 1627 / 1582.
   p.two_dkdv = !f32 && tiles(Tk, 128) <= (D <= 64 ? 1152 : 512);
-  // ... in parts of the rows.  Small tiles: 300 tokens, 4 on one (10 of 18), 1 part 43, 4 34, 8 32; 80 of 18, 1 part 42, 2 39, 4 44; 320 of
-  // 18, 1 part 49, 2 71; fp32, 304 of 37, 1 part 453, 2 431, 4 471.  64 keys, two workgroups a compute unit: 2500, 32 on 8 (320 small tiles), 1
-  // part 318, 3 226, 4 242; 4000, 8 on one (63), 1 part 776, 8 198, 16 189; 3 of 2500 (960), 1 part 561, 2 622.  128 keys in fp32: 4 of 2000, 8 on
-  // 2 (128 of 125), 1 part 3126, 4 1581, 8 1626.
-  p.dkdv = p.few_dkdv   ? attn_splits((f32 ? 512 : 256) / tiles(Tk, 32), rows / seqs / 128, 1)
-           : p.two_dkdv ? attn_splits(1024 / tiles(Tk, 64), rows / seqs / 64, 4)
+  // ... in parts of the rows.  32 keys: to fill a round, or two with longer parts: 300 tokens, 4 on one (10 of 18), 1 part 43, 4 34, 8 32; 80 of 18,
+  // 1 part 42, 2 39, 4 45; 600, 32 on 8 (152 of 37), 1 part 61, 2 54, 3 57; 1500, 8 on 2 (94 of 93), 1 part 108, 4 64, 8 78; 256 of 62, 1 part
+  // 89, 2 83, 3 90; 320 of 18, 1 part 48, 2 70; fp32, 304 of 37, 1 part 453, 2 431, 4 471.  64 keys, two workgroups a compute unit: 2500, 32 on
+  // 8 (320 small tiles of 156), 1 part 318, 3 226, 4 242; 1500 (188 of 93), 1 part 189, 3 119, 4 123; 4000, 8 on one (63 of 500), 1 part 776, 8
+  // 198, 16 189; 3 of 2500 (960 of 156), 1 part 561, 2 622; 4 of 1000, 16 on 8 (512 of 31), 1 part 102, 2 121.  128 keys in fp32: 4 of 2000, 8 on 2 (128
+  // of 125), 1 part 3126, 4 1581, 8 1626.
+  p.dkdv = p.few_dkdv   ? std::max(attn_splits((f32 ? 512 : 256) / small, rows / seqs / 128, 1), attn_splits(512 / small, rows / seqs / 128, 4))
+           : p.two_dkdv ? attn_splits(1024 / tiles(Tk, 64), rows / seqs / 64, 24)
                         : attn_splits((511 + tiles(Tk, 128)) / tiles(Tk, 128), rows / seqs / 64, 4);
 }
 
