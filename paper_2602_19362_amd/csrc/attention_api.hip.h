@@ -86,40 +86,43 @@ static int attn_splits(int64_t want, int64_t steps, int64_t least) {
   return (int)std::max<int64_t>(1, std::min<int64_t>({want, steps / least, 64}));
 }
 
-static void attn_cut(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int g, int hk, int D, bool f32) {
+static void attn_cut(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int g, int hk, int D, bool f32, bool causal) {
   const int64_t seqs = std::max(n_seq, 1), rows = Tq * g;
   const auto tiles = [&](int64_t n, int64_t b) { return std::max<int64_t>(1, (n + seqs * b - 1) / (seqs * b)) * seqs * hk; };
-  // Forward: tiles of 32 rows for few rows, and where they are one round of workgroups (up to 133 KB of LDS: one a compute unit) however
-  // many.  32 rows / 128 rows a tile, each at its best split: 16 sequences of 64 rows over 2000 keys, 8 key heads (256 small tiles) 29 / 34, of
-  // 96 rows (384) 52 / 38; 64 channels, 1000 tokens, 8 heads on one (250) 11 / 19, 6 heads (192) 11 / 19; 1000 tokens, 32 on 8 (1000) 41 / 35.
+  // Forward: tiles of 32 rows for few rows, and where they are one round of workgroups (up to 133 KB of LDS: one a compute unit, of 64 channels
+  // two) however many; two rounds where walks are long and end apart.  32 / 64 / 128 rows a tile: 300 tokens, 32 on 8 (304 small tiles of 9 steps)
+  // 15 / 13 / 16; 1200, 8 heads (304 of 37) 18 / 25 / 39, without a mask 30 / 25; 2 of 500, 16 on 8 (512 of 15) 19 / 17 / 22; 1000, 16 on 8 (504 of 31) 23 / 24 / 35; 1000, 32 on 8
+  // (1000) 41 / 26 / 35.  64 channels: 300, 32 on 8 (304) 8 / 10 / 12; 2 of 500, 16 on 8 (512) 10 / 13 / 17; 600, 32 on 8 (600) 15 / 14 / 18; 8 of 200, 16
+  // on 8 (832) 14 / 10 / 11.  Equal walks, each at its best split, 32 / 128: 16 sequences of 64 rows over 2000 keys, 8 key heads (256) 29 / 34, of 96
+  // rows (384) 52 / 38.
   // fp32 products take nine times as long, and what small tiles cost is hidden behind them for longer: 80 channels, 4 of 400 tokens, 6 on 2
   // (304) 25 / 50; 64 channels, 2 of 1000, 16 on 8 (1008) 57 / 85; 4 of 2000, 8 on 2 (2000) 353 / 382; 4 of 4000, 8 heads (4000) 1255 / 1113.
-  p.few = rows <= seqs * 32 || tiles(rows, 32) <= (f32 ? 2048 : 256);
+  const int64_t t32 = tiles(rows, 32), t64 = tiles(rows, 64), t128 = tiles(rows, 128), steps = Tk / seqs / 32;
+  p.few = rows <= seqs * 32 || t32 <= (f32 ? 2048 : D <= 64 ? 512 : 256) || (causal && t32 <= 512 && steps >= 30 && 2 * Tq > Tk);
   // ... in parts of the keys.  Small tiles, parts that fill the round: one token over 4096 / 32768 keys, 8 key heads, 1 part 35 / 236, 8
   // parts 13 / 40, 16 parts 12 / 31; 8 over 32768, 1 part 389, 4 189, 8 199; 24 over 4096 (192 tiles), 1 part 83, 2 94.  Short parts cost more
   // to put together than they save: 4 x 32 rows over 2000 keys, 4 parts 16, 8 parts (of two steps) 19.
   // Large ones where few tiles have long walks: 8000 tokens, 4 heads on one (250 tiles of 250 steps), 1 part 217, 4 90; 1000 tokens, 32 on 8
   // (256 of 31), 1 part 35.5, 2 37.5.
-  p.fwd = p.few ? attn_splits(256 / tiles(rows, 32), Tk / seqs / 128, 3)
-                : attn_splits(1024 / tiles(rows, 128), Tk / seqs / 32, 32);
-  // Tiles of 64 rows halve a walk: where large ones would be few rounds, their keys are not split, and walks are long enough for what starting
-  // twice as many costs.  64 / 128 rows: 1000 tokens, 32 on 8 (256 large tiles of 31 steps) 26 / 36; 1500 (376 of 46) 40 / 51; 2500 (632) 85 / 81; 4
-  // of 300 (320 of 9) 24 / 18; 4 of 1000, 16 on 8 (512) 43 / 40.  64 channels: 2500 (632) 46 / 57; 4 of 1000 (512) 21 / 28; 4000 (1000) 95 / 95.
-  p.two = !f32 && !p.few && p.fwd == 1 && Tk / seqs / 32 >= 24 && tiles(rows, 128) <= (D <= 64 ? 768 : 400);
+  p.fwd = p.few ? attn_splits(256 / t32, steps / 4, 3) : attn_splits(1024 / t128, steps, 32);
+  // Tiles of 64 rows halve a walk: where they are one round (two workgroups a compute unit) or large ones few, of long walks, and their keys are
+  // not split.  64 / 128 rows: 600 tokens, 32 on 8 (304 tiles of 64 rows) 19 / 24; 1000 (504) 26 / 36; 1500 (752 of 46 steps) 40 / 51; 2500 (1256)
+  // 85 / 81; 4 of 300 (608 of 9) 24 / 18; 4 of 1000, 16 on 8 (1008) 43 / 40; 64 of 30, 8 heads (512 of either size) 12 / 9.  64 channels: 13 of up to
+  // 400, 14 on 2 (572 large ones) 12 / 15; 2500, 32 on 8 (632) 46 / 57; 64 of 60, 8 heads (512) 8.9 / 9.3; 4000, 32 on 8 (1000) 95 / 95.
+  p.two = !f32 && !p.few && p.fwd == 1 && (D <= 64 ? t128 <= 768 : (t64 <= 512 && t64 > t128) || (t128 <= 400 && steps >= 24));
   // dq: tiles of 32 rows up to two rounds.  32 rows / 128 rows, each at its best split: 64 channels, 1000 tokens, 6 heads (192 small tiles)
   // 48 / 55; 1200, 8 heads (304) 46 / 52; 300, 32 on 8 (304) 79 / 78; 4 of 1000, 4 on one (500) 187 / 193; 4800, 8 on 2 (1200) 278 / 241;
   // 1000, 32 on 8 (1000) 213 / 199.  fp32: 80 channels, 4 of 400, 6 on 2 (304) 291 / 301; 64 channels, 2 of 1000, 16 on 8 (1008) 362 / 401; 8
   // of 600, 8 on 2 (1200) 983 / 943.
-  p.few_dq = tiles(rows, 32) <= (f32 ? 1024 : 512);
+  p.few_dq = t32 <= (f32 ? 1024 : 512);
   // ... in parts of the keys.  Small tiles: 16 rows over 4096 keys (2 of 32 steps), 1 part 50, 4 30, 8 25; 64 rows over 1024 (8 of 8), 1
   // part 28, 2 27; 2000 tokens, one head (63 of 15), 1 part 57, 2 52; 192 of 7, 1 part 48, 2 51.  Large ones: 9000, 4 on one (282 of 140), 1
   // part 456, 2 373, 3 355; 1000, 32 on 8 (256 of 15), 1 part 199, 2 200; 2500, 32 on 8 (632 of 39), 1 part 460, 2 491.
-  p.dq = p.few_dq ? attn_splits(256 / tiles(rows, 32), Tk / seqs / 128, 4)
-                  : attn_splits(900 / tiles(rows, 128), Tk / seqs / 64, 24);
+  p.dq = p.few_dq ? attn_splits(256 / t32, steps / 4, 4) : attn_splits(900 / t128, steps / 2, 24);
   // ... of 64 rows where large ones are few rounds and not cut, as forward.  64 / 128 rows: 600 tokens, 32 on 8 (152 large tiles of 9 steps) 61 / 63;
   // 1000 (256) 89 / 95; 1500 (376) 123 / 130; 2500 (632) 235 / 223; 4 of 300 (320 of 4) 55 / 48.  64 channels: 13 of up to 400, 14 on 2 (572) 44 / 46;
   // 4 of 1000, 16 on 8 (512) 80 / 79, 32 channels 52 / 57; 4000, 32 on 8 (1000) 286 / 286.
-  p.two_dq = !f32 && !p.few_dq && p.dq == 1 && tiles(rows, 128) <= (D <= 64 ? 640 : 400) && (D <= 64 || Tk / seqs / 64 >= 8);
+  p.two_dq = !f32 && !p.few_dq && p.dq == 1 && t128 <= (D <= 64 ? 640 : 400) && (D <= 64 || steps >= 16);
   // dk, dv: tiles of 32 keys where they are few (a workgroup of 128 channels has a compute unit's LDS for itself, of 64 channels half of it) and
   // their walks, in steps of 64 rows, short; their wavefronts have a SIMD each, which saves time there and costs rate.  32 / 64 / 128 keys, each at
   // its best split: 300 tokens, 32 on 8 (80 small tiles of 18 steps) 39 / 44 / 48; 4 of 300 (320 of 18) 48 / 59 / 64; 1000 (256 of 62) 83 / 78 / 87; 1500
@@ -145,7 +148,7 @@ static void attn_cut(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int g, int 
                         : attn_splits((511 + tiles(Tk, 128)) / tiles(Tk, 128), rows / seqs / 64, 4);
 }
 
-static bool attn_plan(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int hq, int hk, int D, int dtype, bool bwd) {
+static bool attn_plan(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int hq, int hk, int D, int dtype, bool causal, bool bwd) {
   if (dtype != OAPL_F32 && dtype != OAPL_BF16) return false;
   if (!head_counts_ok(hq, hk, D) || Tq < 0 || Tk < 0 || n_seq < 0 || (n_seq == 0 && (Tq || Tk)) || Tk > kMaxTileRows ||
       Tq > kMaxTileRows / hq || n_seq > (1 << 24))
@@ -153,7 +156,7 @@ static bool attn_plan(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int hq, in
   // every grid in 31 bits
   const int g = hq / hk;
   if ((tile_ids<32>(Tq * g, n_seq) + tile_ids<32>(Tk, n_seq)) * hk > kMaxTileRows) return false;
-  attn_cut(p, Tq, Tk, n_seq, g, hk, D, dtype == OAPL_F32);
+  attn_cut(p, Tq, Tk, n_seq, g, hk, D, dtype == OAPL_F32, causal);
   size_t at = kStatusWords * sizeof(int);
   const auto take = [&](int64_t floats) {
     const size_t was = at;
@@ -354,8 +357,13 @@ int32_t oapl_qk_norm_rope_bwd(const oapl_heads* q, const oapl_heads* k, const oa
 
 size_t oapl_attention_workspace_bytes(int64_t Tq, int64_t Tk, int32_t n_seq, int32_t n_q_heads, int32_t n_k_heads,
                                       int32_t head_dim, int32_t dtype, int32_t with_backward) {
-  AttnPlan p;
-  return attn_plan(p, Tq, Tk, n_seq, n_q_heads, n_k_heads, head_dim, dtype, with_backward != 0) ? p.total : 0;
+  size_t most = 0;      // of either mask
+  for (const bool causal : {false, true}) {
+    AttnPlan p;
+    if (!attn_plan(p, Tq, Tk, n_seq, n_q_heads, n_k_heads, head_dim, dtype, causal, with_backward != 0)) return 0;
+    most = std::max(most, p.total);
+  }
+  return most;
 }
 
 int32_t oapl_attention_fwd(const oapl_heads* q, const oapl_heads* k, const oapl_heads* v, const int64_t* q_offsets,
@@ -364,7 +372,7 @@ int32_t oapl_attention_fwd(const oapl_heads* q, const oapl_heads* k, const oapl_
                            const oapl_heads* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
   if (dtype != OAPL_F32 && dtype != OAPL_BF16) return OAPL_ERR_DTYPE;
   AttnPlan p;
-  if (!attn_plan(p, Tq, Tk, n_seq, n_q_heads, n_k_heads, head_dim, dtype, false)) return OAPL_ERR_SHAPE;
+  if (!attn_plan(p, Tq, Tk, n_seq, n_q_heads, n_k_heads, head_dim, dtype, causal != 0, false)) return OAPL_ERR_SHAPE;
   AttnArgs a;
   if (int rc = attn_args(a, q, k, v, q_offsets, k_offsets, Tq, Tk, n_seq, n_q_heads, n_k_heads, head_dim, dtype, causal, scale))
     return rc;
@@ -394,7 +402,7 @@ int32_t oapl_attention_bwd(const oapl_heads* q, const oapl_heads* k, const oapl_
                            size_t workspace_bytes, void* stream) {
   if (dtype != OAPL_F32 && dtype != OAPL_BF16) return OAPL_ERR_DTYPE;
   AttnPlan p;
-  if (!attn_plan(p, Tq, Tk, n_seq, n_q_heads, n_k_heads, head_dim, dtype, true)) return OAPL_ERR_SHAPE;
+  if (!attn_plan(p, Tq, Tk, n_seq, n_q_heads, n_k_heads, head_dim, dtype, causal != 0, true)) return OAPL_ERR_SHAPE;
   AttnArgs a;
   if (int rc = attn_args(a, q, k, v, q_offsets, k_offsets, Tq, Tk, n_seq, n_q_heads, n_k_heads, head_dim, dtype, causal, scale))
     return rc;

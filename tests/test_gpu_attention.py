@@ -449,3 +449,10 @@ def test_what_is_not_finite_among_tiles_of_128_keys_of_wide_heads():
 def test_tiles_of_64_rows(D, causal):
     _check("bf16", [1300, 900, 50], [1300, 1000, 700], 16, 8, D, causal, seed=270)
     _check("bf16", [1100, 0, 1200], [900, 700, 1200], 16, 8, D, causal, seed=273)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_one_long_sequence_of_few_tiles(causal):
+    """Cut otherwise with a mask than without one."""
+    _check("bf16", [1200], [1200], 8, 8, 128, causal, seed=280)
+    _check("bf16", [2300], [2300], 6, 3, 128, causal, seed=283)
