@@ -749,6 +749,8 @@ __global__ __launch_bounds__(256, WK == 4 ? 1 : WK == 2 && DW > 64 ? 2 : sizeof(
   if (Size::kSlots == 2 && j0 < part.end) stage(0, j0);
   const int group = threadIdx.x >> 4 & 3, row0 = t.first + wave % (4 / WK) * 32 + (threadIdx.x & 15);
   const float scale2 = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;
+  // Where the running maximum starts: it is scaled before a row has seen any key, and a masked score less an infinite offset would be NaN.
+  const float lowest = kNegHuge / fmaxf(scale2, 1.f);
   int row_sees[2];
   Frag q[2][KS];
   f32x4 o[2][DB];
@@ -769,7 +771,7 @@ __global__ __launch_bounds__(256, WK == 4 ? 1 : WK == 2 && DW > 64 ? 2 : sizeof(
     for (int d = 0; d < DB; ++d) zero(o[n][d]);
     row_sees[n] = row.sees;
     if (row.exists) all_see = row.sees < all_see ? row.sees : all_see;
-    m[n] = kNegHuge;
+    m[n] = lowest;
     l[n] = 0.f;
   }
 #pragma unroll
