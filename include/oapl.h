@@ -449,7 +449,7 @@ size_t oapl_attention_workspace_bytes(int64_t Tq, int64_t Tk, int32_t n_seq, int
  *   k_used      NULL, or [n_seq] int64
  *   lse         [Tq][n_q_heads] float, or NULL if not wanted
  * Malformed offsets or k_used: OAPL_ERR_OFFSETS in the workspace's status, NaN in every output.
- *   scale finite (else OAPL_ERR_BETA)
+ *   scale       |scale| < 2.35e38, so that scale * log2(e) is finite (else OAPL_ERR_BETA)
  */
 int32_t oapl_attention_fwd(const oapl_heads* q, const oapl_heads* k, const oapl_heads* v,
                            const int64_t* q_offsets, const int64_t* k_offsets, const int64_t* k_used,

@@ -176,7 +176,7 @@ static bool attn_plan(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int hq, in
 static int attn_args(AttnArgs& a, const oapl_heads* q, const oapl_heads* k, const oapl_heads* v, const int64_t* q_offsets,
                      const int64_t* k_offsets, int64_t Tq, int64_t Tk, int n_seq, int hq, int hk, int D, int dtype, int causal,
                      float scale) {
-  if (!isfinite(scale)) return OAPL_ERR_BETA;
+  if (!isfinite(scale * kLog2e)) return OAPL_ERR_BETA;      // what the kernels multiply by
   if (n_seq > 0 && (!q_offsets || !k_offsets)) return OAPL_ERR_NULL;
   if (int rc = check_heads(q, Tq, hq, D, dtype, false)) return rc;
   if (int rc = check_heads(k, Tk, hk, D, dtype, false)) return rc;
