@@ -55,6 +55,8 @@ struct Pieces {
     a = turned ? lane16 * 4 : rot + (lane16 - pairs) * 8;
     b = turned ? (rot >> 1) + lane16 * 4 : a + 4;
   }
+  // What the sine of a rotation multiplies: channels that are not rotated have no partner, and what is not finite in one is not the other's.
+  __device__ __forceinline__ f32x4 partner(f32x4 x) const { return turned ? x : f32x4{}; }
 };
 
 // A token's cosines and sines for a lane's pairs; false (and NaN) where its position has none.
@@ -112,7 +114,8 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope_fwd(const NormRopeArgs p) 
         a[i] = a[i] * r * (query ? gq[0] : gk[0]);
         b[i] = b[i] * r * (query ? gq[1] : gk[1]);
       }
-      const f32x4 x = value ? a[i] : a[i] * cos - b[i] * sin, y = value ? b[i] : b[i] * cos + a[i] * sin;
+      const f32x4 ta = at.partner(a[i]), tb = at.partner(b[i]);
+      const f32x4 x = value ? a[i] : a[i] * cos - tb * sin, y = value ? b[i] : b[i] * cos + ta * sin;
       if (h >= heads || !at.any || !(query || kept)) continue;
       T* z = (T*)(query ? p.q_out.row(t, h) : value ? p.v_out.row(to, h - p.hq - p.hk) : p.k_out.row(to, h - p.hq));
       store4(z + at.a, x), store4(z + at.b, y);
@@ -150,7 +153,7 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope_bwd(const NormRopeArgs p) 
       for (int i = 0; i < kRopeHeads; ++i) {
         const int h = h0 + i * step;
         const bool query = h < p.hq;
-        f32x4 ua = da[i] * cos + db[i] * sin, ub = db[i] * cos - da[i] * sin;
+        f32x4 ua = da[i] * cos + at.partner(db[i]) * sin, ub = db[i] * cos - at.partner(da[i]) * sin;
         if (p.q_gain) {
           const float r = rsqrtf(group_sum(dot4(a[i], a[i]) + dot4(b[i], b[i])) / (float)p.D + p.eps);
           const f32x4 xa = a[i] * r, xb = b[i] * r;

@@ -1,4 +1,6 @@
 """Norm and rotation at the ends of what the header allows."""
+import math
+
 import pytest
 import torch
 
@@ -21,3 +23,32 @@ def test_gradients_without_eps(dtype, T, hq, hk):
         want, gain_want, bound, gain_bound = orc.norm_rope_grads(x, dy, gain, pos, table, 0.0)
         _near(dx, want, bound)
         _near(dgain, gain_want, gain_bound)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D, rot", [(24, 8), (80, 40), (16, 0), (128, 64)])
+def test_what_is_not_finite_stays_in_channels_that_are_not_rotated(dtype, bad, D, rot):
+    """Without a norm a channel behind the rotated ones is copied, forward and backward, whatever its neighbours hold."""
+    q, k, _, pos, table, _ = _inputs(dtype, 5, 3, 2, D, rot, False, seed=22)
+    q, k = q.contiguous(), k.contiguous()
+    want = oapl.qk_norm_rope_fwd(q, k, pos, table)
+    for c in (rot, rot + 5, D - 1):
+        x, y = q.clone(), k.clone()
+        x[2, 1, c] = y[3, 0, c] = bad
+        others = torch.arange(D, device=DEV) != c
+        r = oapl.qk_norm_rope_fwd(x, y, pos, table)
+        g = oapl.qk_norm_rope_bwd(q, k, x, y, pos, table)
+        back = oapl.qk_norm_rope_bwd(q, k, q, k, pos, table)
+        for got, plain, given in ((r.q, want.q, x), (r.k, want.k, y), (g.dq, back.dq, x), (g.dk, back.dk, y)):
+            assert torch.equal(got[..., others], plain[..., others])
+            assert torch.equal(got[..., rot:].nan_to_num(7.0, 8.0, 9.0), given[..., rot:].nan_to_num(7.0, 8.0, 9.0))
+
+
+def test_a_position_without_angles_reaches_the_channels_that_are_not_rotated():
+    q, k, _, pos, table, (gq, gk) = _inputs("bf16", 6, 4, 2, 64, 32, True, seed=23)
+    pos[2] = -1
+    got = oapl.qk_norm_rope_fwd(q, k, pos, table, gq, gk)
+    back = oapl.qk_norm_rope_bwd(q, k, q, k, pos, table, gq, gk)
+    for x in (got.q, got.k, back.dq, back.dk):
+        assert bool(x[2].isnan().all()) and bool(x[[0, 1, 3, 4, 5]].isfinite().all())
