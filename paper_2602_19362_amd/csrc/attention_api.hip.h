@@ -44,6 +44,12 @@ static int rope_parts(int64_t T, int heads) {
   return (int)(parts < 1 ? 1 : parts > most ? most : parts);
 }
 
+// Forward: four wavefronts a workgroup, in as many dimensions as it takes: HIP takes fewer than 2^32 threads in one.
+static dim3 rope_fwd_grid(int64_t T, int parts) {
+  const int64_t n = (T * parts + 3) / 4, most = 1 << 22;
+  return n <= most ? dim3((unsigned)n) : dim3((unsigned)most, (unsigned)((n + most - 1) / most));
+}
+
 // Workgroups that walk over the tokens backwards, each with sums of the gains' gradients of its own: three a compute unit.  The batch of
 // kRopeHeads in 512 / 768 / 1024 / 1536: 124 / 105 / 108 / 113 us (504 MB: 4.8 TB/s, the card's copy 5.1).
 static unsigned rope_bwd_grid(int64_t T, int heads) {
@@ -306,7 +312,7 @@ int32_t oapl_qk_norm_rope_fwd(const oapl_heads* q, const oapl_heads* k, const oa
   a.q_out = heads_of(q_out, dtype), a.k_out = heads_of(k_out, dtype), a.v_out = heads_of(v_out, dtype);
   a.rows = rows, a.n_rows = n_rows;
   a.parts = rope_parts(T, n_q_heads + n_k_heads * (v ? 2 : 1));
-  const unsigned grid = (unsigned)((T * a.parts + 3) / 4);
+  const dim3 grid = rope_fwd_grid(T, a.parts);
   if (dtype == OAPL_BF16) k_qk_norm_rope_fwd<bf16_t><<<grid, 256, 0, (hipStream_t)stream>>>(a);
   else k_qk_norm_rope_fwd<float><<<grid, 256, 0, (hipStream_t)stream>>>(a);
   OAPL_LAUNCH_CHECK();

@@ -80,7 +80,7 @@ constexpr int kRopeHeads = 2;
 template <class T>
 __global__ __launch_bounds__(256) void k_qk_norm_rope_fwd(const NormRopeArgs p) {
   const int lane = threadIdx.x & 63, group = lane >> 4;
-  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t unit = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + (threadIdx.x >> 6);
   const int64_t t = unit / p.parts;
   if (t >= p.T) return;
   const Pieces at(lane & 15, p.D, p.rot);

@@ -58,6 +58,12 @@ int main() {
       const dim3 g = f32_grid(T);
       const long long x = (long long)g.x * F32Wide::NT, y = g.y, z = g.z;
       std::printf("tiles=%lld most=%lld rest=%d\n", (long long)g.x * y * z, x > y ? x : y, (int)(g.x % 8));
+    } else if (std::sscanf(line, "rope %lld %d", &T, &n_seq) == 2) {
+      // the norm and rotation of T tokens of n_seq heads in all: wavefronts, tokens times the wavefronts that share one, most threads in a dimension
+      const int parts = rope_parts(T, n_seq);
+      const dim3 g = rope_fwd_grid(T, parts);
+      const long long x = (long long)g.x * 256, y = g.y, z = g.z;
+      std::printf("waves=%lld units=%lld most=%lld\n", (long long)g.x * y * z * 4, T * parts, x > y ? x : y);
     } else if (std::sscanf(line, "finish %lld %d %d", &T, &V, &n_seq) == 3) {
       // an fp32 loss call's log-probs: in the objective's launch?
       Plan p;

@@ -6,7 +6,7 @@ import torch
 
 from oracle import attention_oracle as orc
 from paper_2602_19362_amd import oapl
-from tests.test_gpu_norm_rope import DEV, _gen, _inputs, _near
+from tests.test_gpu_norm_rope import DEV, _gen, _inputs, _near, _table
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +52,20 @@ def test_a_position_without_angles_reaches_the_channels_that_are_not_rotated():
     back = oapl.qk_norm_rope_bwd(q, k, q, k, pos, table, gq, gk)
     for x in (got.q, got.k, back.dq, back.dk):
         assert bool(x[2].isnan().all()) and bool(x[[0, 1, 3, 4, 5]].isfinite().all())
+
+
+def test_more_tokens_than_workgroups_in_one_dimension_of_a_grid():
+    """2^26 tokens and a few: four of them a workgroup, and HIP takes fewer than 2^32 threads in a dimension."""
+    T, D = (1 << 26) + 5, 8
+    q, k = (torch.empty(T, 1, D, dtype=torch.bfloat16, device=DEV).normal_(generator=_gen(s)) for s in (24, 25))
+    pos = torch.randint(0, 100, (T,), generator=_gen(26), device=DEV, dtype=torch.int32)
+    table = _table(100, D)
+    r = oapl.qk_norm_rope_fwd(q, k, pos, table)
+    for at in (slice(0, 1000), slice(T // 2, T // 2 + 1000), slice(T - 1000, T)):
+        part = oapl.qk_norm_rope_fwd(q[at], k[at], pos[at].contiguous(), table)
+        assert torch.equal(r.q[at], part.q) and torch.equal(r.k[at], part.k)
+    # every token was written: the rotation keeps a head's length (to a rounding of each channel)
+    for x, y in ((q, r.q), (k, r.k)):
+        for i in range(0, T, 1 << 24):
+            a, b = (z[i:i + (1 << 24)].float().square().sum((1, 2)) for z in (x, y))
+            assert bool(((a - b).abs() <= 2.0 ** -6 * a).all())
