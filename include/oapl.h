@@ -448,6 +448,8 @@ size_t oapl_attention_workspace_bytes(int64_t Tq, int64_t Tk, int32_t n_seq, int
  *                         (may be the same array; sequences may be empty)
  *   k_used      NULL, or [n_seq] int64
  *   lse         [Tq][n_q_heads] float, or NULL if not wanted
+ * Refused (OAPL_ERR_SHAPE): 2^24 tiles and more, a tile being up to 32, 64 or 128 (as the sizes
+ * have it) rows of one sequence and key head, of keys too backwards; each sequence may take one more.
  * Malformed offsets or k_used: OAPL_ERR_OFFSETS in the workspace's status, NaN in every output.
  *   scale       |scale| < 2.35e38, so that scale * log2(e) is finite (else OAPL_ERR_BETA)
  */

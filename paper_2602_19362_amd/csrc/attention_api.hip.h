@@ -154,15 +154,23 @@ static void attn_cut(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int g, int 
                         : attn_splits((511 + tiles(Tk, 128)) / tiles(Tk, 128), rows / seqs / 64, 4);
 }
 
+// A launch of so many tiles in so many parts has fewer than 2^32 threads, which is what HIP takes in a dimension of a grid.
+static bool attn_launches(const AttnPlan& p, int64_t rows, int64_t Tk, int n_seq, int hk, bool bwd) {
+  const auto fits = [&](int64_t n, bool few, bool two, int parts) {
+    const int64_t tiles = few ? tile_ids<32>(n, n_seq) : two ? tile_ids<64>(n, n_seq) : tile_ids<128>(n, n_seq);
+    return tiles * hk * parts < (int64_t)1 << 24;
+  };
+  return bwd ? fits(rows, p.few_dq, p.two_dq, p.dq) && fits(Tk, p.few_dkdv, p.two_dkdv, p.dkdv) : fits(rows, p.few, p.two, p.fwd);
+}
+
 static bool attn_plan(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int hq, int hk, int D, int dtype, bool causal, bool bwd) {
   if (dtype != OAPL_F32 && dtype != OAPL_BF16) return false;
   if (!head_counts_ok(hq, hk, D) || Tq < 0 || Tk < 0 || n_seq < 0 || (n_seq == 0 && (Tq || Tk)) || Tk > kMaxTileRows ||
       Tq > kMaxTileRows / hq || n_seq > (1 << 24))
     return false;
-  // every grid in 31 bits
   const int g = hq / hk;
-  if ((tile_ids<32>(Tq * g, n_seq) + tile_ids<32>(Tk, n_seq)) * hk > kMaxTileRows) return false;
   attn_cut(p, Tq, Tk, n_seq, g, hk, D, dtype == OAPL_F32, causal);
+  if (!attn_launches(p, Tq * g, Tk, n_seq, hk, bwd)) return false;
   size_t at = kStatusWords * sizeof(int);
   const auto take = [&](int64_t floats) {
     const size_t was = at;
