@@ -430,7 +430,7 @@ int32_t oapl_attention_bwd(const oapl_heads* q, const oapl_heads* k, const oapl_
   hipStream_t st = (hipStream_t)stream;
   a.o = heads_of(out, dtype), a.dout = heads_of(dout, dtype);
   // RowStager's offsets: 64 tokens and the heads of a group within 31 bits
-  if ((a.g - 1) * std::max(a.q.head, a.dout.head) > ((int64_t)1 << 30)) return OAPL_ERR_SHAPE;
+  if (Tq > 0 && a.g > 1 && std::max(a.q.head, a.dout.head) > ((int64_t)1 << 30) / (a.g - 1)) return OAPL_ERR_SHAPE;
   a.dq = heads_of(dq, dtype), a.dk = heads_of(dk, dtype), a.dv = heads_of(dv, dtype);
   a.lse = const_cast<float*>(lse);
   a.lse2 = (float*)((char*)workspace + p.off_lse2);

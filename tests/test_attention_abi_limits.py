@@ -27,3 +27,11 @@ def test_long_caches_and_many_sequences_are_served():
     """A cache's capacity is no part of a forward launch; 2^20 sequences of 8 heads are half of what one takes."""
     assert oapl.attention_workspace_bytes(8, 1 << 27, 8, 64, 64, 128, 1, False) > 0
     assert oapl.attention_workspace_bytes(1 << 20, 1 << 20, 1 << 20, 8, 8, 64, 1, True) > 0
+
+
+@pytest.mark.parametrize("hq, head", [(65536, 1 << 48), (1 << 15, 1 << 48), (3, 1 << 48), (65536, 1 << 47), (2, (1 << 29) + 8)])
+def test_a_group_further_apart_than_32_bit_offsets_reach_is_refused(hq, head):
+    """The span of a group's heads is compared without being multiplied out of 64 bits."""
+    for q, dout in ((H(AT, 128, head), H()), (H(), H(AT, 128, head))):
+        assert oapl.lib().oapl_attention_bwd(q, H(), H(), H(), AT, dout, AT, AT, 4, 4, 1, hq, 1, 64, 1, 1, 0.1, H(), H(), H(), AT, 1 << 40,
+                                             None) == SHAPE
