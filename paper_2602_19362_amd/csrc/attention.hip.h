@@ -433,6 +433,13 @@ __device__ __forceinline__ int all_rows_see(const AttnArgs& p, const SeqTile& t)
   return n < 0 ? 0 : n < t.nk ? n : t.nk;
 }
 
+// Whether keys [from, from + KEYS) hold one that exists and that some row of the tile does not see: one that others see, or one behind the
+// reach of all (which a tile of one token's heads has, too) in the step in which it ends.
+template <int KEYS>
+__device__ __forceinline__ bool hides(const SeqTile& t, int all_see, int from) {
+  return all_see < (from + KEYS < t.nk ? from + KEYS : t.nk);
+}
+
 template <int WK> constexpr int fwd_keys = WK == 2 ? 64 : 32;   // keys staged at a time: forward
 template <int WK> constexpr int dq_keys = WK == 4 ? 32 : 64;    // ... for dq
 
@@ -739,9 +746,8 @@ __global__ __launch_bounds__(256, WK == 4 ? 1 : WK == 2 && DW > 64 ? 2 : sizeof(
   const Stage ks(p.k.row(t.k0, kh), p.k.token, p.D), vs(p.v.row(t.k0, kh), p.v.token, p.D);
   int j0 = part.begin + (kAlone ? wave * KEYS : 0), slot = 0;
   const lds_char_ptr words = (lds_char_ptr)smem + Size::kWords;
-  // whether a step has keys that some rows of the tile see and others do not
-  const int first_sees = all_rows_see(p, t), last_sees = tile_sees<B>(p, t);
-  const auto masks = [&](int from) { return first_sees < last_sees && from + KEYS > first_sees; };
+  const int first_sees = all_rows_see(p, t);
+  const auto masks = [&](int from) { return hides<KEYS>(t, first_sees, from); };
   const auto stage = [&](int at, int first) {
     ks.start(lds + at, first, t.nk);
     vs.start(lds + at + SIZE, first, t.nk);
@@ -1028,8 +1034,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
   if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = found == kMalformed ? kErrOffsets : 0;
   if (found == kMalformed) poison<T>(p.dq, p.Tq, p.hq, p.D);
   if (found != kTile) return;
-  const int first_sees = all_rows_see(p, t), last_sees = tile_sees<B>(p, t);
-  const Part part(last_sees, p.splits, job.part, STEP);
+  const int first_sees = all_rows_see(p, t);
+  const Part part(tile_sees<B>(p, t), p.splits, job.part, STEP);
   const Stage ks(p.k.row(t.k0, kh), p.k.token, p.D), vs(p.v.row(t.k0, kh), p.v.token, p.D);
   int j0 = part.begin + (kAlone ? wave * KEYS : 0), slot = 0;
   const auto stage = [&](int at, int first) {
@@ -1076,7 +1082,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
   }
   all_see = __builtin_amdgcn_readfirstlane(all_see);
   for (; j0 < part.end; j0 += STEP, slot ^= Size::kSlots == 2 ? 2 * SIZE : 0) {
-    const bool masks = first_sees < last_sees && j0 + KEYS > first_sees;
+    const bool masks = hides<KEYS>(t, first_sees, j0);
     if (Size::kSlots == 1) stage(0, j0);
     staged();
     bool found_odd = masks && staged_odd<T, Stage::kLoads, W>(lds + slot);
