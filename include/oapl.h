@@ -443,7 +443,7 @@ size_t oapl_attention_workspace_bytes(int64_t Tq, int64_t Tk, int32_t n_seq, int
  * normalised) once for the product with the values.
  * What is not finite reaches only who sees it: a NaN or infinity in a key or value no row that does
  * not see that key, one in a row of queries (or of dout, below) no key that the row does not
- * see.  Rows that see one may be NaN in every channel.
+ * see.  Rows that see one may be NaN in every channel; lse has no part of the values.
  *   q_offsets, k_offsets  [n_seq + 1] int64 from 0 to Tq and Tk, non-decreasing
  *                         (may be the same array; sequences may be empty)
  *   k_used      NULL, or [n_seq] int64

@@ -483,8 +483,8 @@ __device__ __forceinline__ float row_max(float v) { return over_row(v, [](float 
 __device__ __forceinline__ float row_sum(float v) { return over_row(v, [](float a, float b) { return a + b; }); }
 
 // What is not finite in a tile's masked places.  A masked probability is 0, and 0 times a NaN or an infinity would be NaN in rows that
-// do not see it.  Where a step masks anything, what is not finite becomes 0 in the tile before it is used, and the
-// probabilities of those rows are made NaN for whoever sees them (mark_odd).
+// do not see it.  Where a step masks anything, what is not finite becomes 0 in the tile before it is used.  Whoever sees it is made NaN
+// by hand: forward the output (the log-sum-exp has no part of the values), backwards the probabilities (mark_odd).
 //
 // Whether this wavefront has staged any such number: its pieces of a tile (j W + wave, of 1 KiB), before the others have to be there.
 template <class T, int LOADS, int W>
@@ -800,7 +800,7 @@ __global__ __launch_bounds__(256, WK == 4 ? 1 : WK == 2 && DW > 64 ? 2 : sizeof(
     const int k_rows = Lds::rows_place(own, threadIdx.x), v_columns = Lds::columns_place(own + SIZE, threadIdx.x);
     f32x4 s[2][2];     // [rows][keys]
     scores<Lds, KS>(s, k_rows, 0, q, [](int) {});
-    if (odd) mark_odd(s, (uint32_t)(clean_tile<T, DP, KEYS, W>(lds + slot + SIZE, words + 32) >> half));
+    const uint32_t odd_keys = odd ? (uint32_t)(clean_tile<T, DP, KEYS, W>(lds + slot + SIZE, words + 32) >> half) : 0;
     if (j0 + half + 32 > all_see) {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
@@ -844,6 +844,16 @@ __global__ __launch_bounds__(256, WK == 4 ? 1 : WK == 2 && DW > 64 ? 2 : sizeof(
     }
     ready(w);
     add_columns<Lds, DB>(o, v_columns, 0, w, [](int) {});
+    if (odd_keys) {      // a value is no part of the probabilities' sum
+      settle(o);
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const int first = __ffs(odd_keys) - 1;
+        if (j0 + half + first >= row_sees[n]) continue;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[n][d] = f32x4{} + quiet_nan();
+      }
+    }
   }
   settle(o);
   const auto finish = [&](float m2, float l) { return l == 0.f ? -__builtin_inff() : (m2 + __builtin_amdgcn_logf(l)) * kLn2f; };
