@@ -74,8 +74,8 @@ __device__ __forceinline__ SeqTile tile_of(const AttnArgs& p, int seq, TileOf wh
   return t;
 }
 
-// Offsets start at 0, do not fall, and end at the number of tokens; cached lengths lie within their sequences' room.  Every
-// wavefront looks for itself, so nothing has to be launched before the kernel that computes.
+// Offsets start at 0, do not fall, and end at the number of tokens; cached lengths lie within their sequences' room.  Of up to kLookedAt
+// sequences every wavefront looks for itself, so nothing has to be launched before the kernel that computes.
 struct SeqEnds {
   int64_t q0, q1, k0, k1, used;      // of one sequence; zeros behind the last
   __device__ __forceinline__ SeqEnds(const AttnArgs& p, int i) {
@@ -89,6 +89,18 @@ struct SeqEnds {
            used > k1 - k0;
   }
 };
+
+// Of more, that would be work by the square of their number (all offsets for every sequence's tiles): one workgroup looks first, and
+// the others find in the status word what it saw.  16384 tokens, 8 heads of 64 channels, forward / backward, every wavefront / one workgroup:
+// 128 sequences 32 / 85 and 34 / 82 us; 256, 31 / 83 and 29 / 72; 1024, 181 / 300 and 90 / 177; 4096, 1450 / 2410 and 290 / 600.
+constexpr int kLookedAt = 128;
+__global__ __launch_bounds__(1024) void k_attn_check(const AttnArgs p) {
+  bool bad = false;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < p.n_seq; i += 1024) bad |= SeqEnds(p, i).bad(p, i);
+  const int any = __syncthreads_or(bad);
+  if (threadIdx.x == 0) *p.status = any ? kErrOffsets : 0;
+}
 
 // The tile with this id, by a search over the first ids of (well-formed) sequences, 64 at a time.
 template <int B>
@@ -130,9 +142,13 @@ template <int B>
 __device__ __forceinline__ Found pick_tile(const AttnArgs& p, TileOf what, int rank, SeqTile& t) {
   const int lane = threadIdx.x & 63;
   const SeqEnds ends(p, lane);
-  bool bad = lane < p.n_seq && ends.bad(p, lane);
-  for (int i = lane + 64; i < p.n_seq; i += 64) bad |= SeqEnds(p, i).bad(p, i);
-  if (__ballot(bad) != 0) return kMalformed;
+  if (p.n_seq > kLookedAt) {
+    if (uniform(*p.status) != 0) return kMalformed;
+  } else {
+    bool bad = lane < p.n_seq && ends.bad(p, lane);
+    for (int i = lane + 64; i < p.n_seq; i += 64) bad |= SeqEnds(p, i).bad(p, i);
+    if (__ballot(bad) != 0) return kMalformed;
+  }
   if (p.n_seq > 64) {
     const int64_t last = what == kOfRows ? tile_ids<B>(p.Tq * p.g, p.n_seq) - 1 : 0;
     t = find_tile<B>(p, what, what == kOfRows ? last - rank : rank);

@@ -229,6 +229,15 @@ static int launch_attn(int64_t tiles, const AttnArgs& a, hipStream_t st) {
   return OAPL_OK;
 }
 
+// What goes before either pass: the status of no sequences (nothing else is launched), the offsets of many.
+static int launch_attn_begin(const AttnArgs& a, hipStream_t st) {
+  if (a.n_seq == 0) k_fill_i32<<<1, 64, 0, st>>>(a.status, kStatusWords, 0);
+  else if (a.n_seq > kLookedAt) k_attn_check<<<1, 1024, 0, st>>>(a);
+  else return OAPL_OK;
+  OAPL_LAUNCH_CHECK();
+  return OAPL_OK;
+}
+
 template <class T, int DW>
 static int launch_attn_fwd(AttnArgs a, const AttnPlan& p, hipStream_t st) {
   a.splits = p.fwd;
@@ -399,11 +408,8 @@ int32_t oapl_attention_fwd(const oapl_heads* q, const oapl_heads* k, const oapl_
   a.status = (int*)workspace;
   a.part_sums = (float*)((char*)workspace + p.off_sums);
   a.partials = (float*)((char*)workspace + p.off_partials);
-  if (n_seq == 0) {
-    k_fill_i32<<<1, 64, 0, st>>>(a.status, kStatusWords, 0);
-    OAPL_LAUNCH_CHECK();
-    return OAPL_OK;
-  }
+  if (int rc = launch_attn_begin(a, st)) return rc;
+  if (n_seq == 0) return OAPL_OK;
   return by_type(dtype, head_dim, [&](auto* t, auto dp) {
     return launch_attn_fwd<std::remove_pointer_t<decltype(t)>, decltype(dp)::value>(a, p, st);
   });
@@ -437,11 +443,8 @@ int32_t oapl_attention_bwd(const oapl_heads* q, const oapl_heads* k, const oapl_
   a.delta = (float*)((char*)workspace + p.off_delta);
   a.partials = (float*)((char*)workspace + p.off_partials);
   a.status = (int*)workspace;
-  if (n_seq == 0) {
-    k_fill_i32<<<1, 64, 0, st>>>(a.status, kStatusWords, 0);
-    OAPL_LAUNCH_CHECK();
-    return OAPL_OK;
-  }
+  if (int rc = launch_attn_begin(a, st)) return rc;
+  if (n_seq == 0) return OAPL_OK;
   return by_type(dtype, head_dim, [&](auto* t, auto dp) {
     return launch_attn_bwd<std::remove_pointer_t<decltype(t)>, decltype(dp)::value>(a, p, st);
   });
