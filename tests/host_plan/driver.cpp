@@ -58,6 +58,15 @@ int main() {
       const dim3 g = f32_grid(T);
       const long long x = (long long)g.x * F32Wide::NT, y = g.y, z = g.z;
       std::printf("tiles=%lld most=%lld rest=%d\n", (long long)g.x * y * z, x > y ? x : y, (int)(g.x % 8));
+    } else if (std::sscanf(line, "attention %lld %lld %d %d %d %d %d %d", &T, &cap, &n_seq, &n_groups, &V, &d, &dtype, &bwd) == 8) {
+      // attention of T queries and `cap` keys in n_seq sequences, n_groups heads on V of d channels, `bwd` the mask: rows (keys) of a tile and the
+      // parts that its walk is cut into, of the forward, dq and dk/dv kernels
+      AttnPlan f, b;
+      const bool ok = attn_plan(f, T, cap, n_seq, n_groups, V, d, dtype, bwd != 0, false) &&
+                      attn_plan(b, T, cap, n_seq, n_groups, V, d, dtype, bwd != 0, true);
+      const auto tile = [](bool few, bool two) { return few ? 32 : two ? 64 : 128; };
+      std::printf("ok=%d fwd=%d fwd_parts=%d dq=%d dq_parts=%d dkdv=%d dkdv_parts=%d\n", ok, tile(f.few, f.two), f.fwd, tile(b.few_dq, b.two_dq),
+                  b.dq, tile(b.few_dkdv, b.two_dkdv), b.dkdv);
     } else if (std::sscanf(line, "rope %lld %d", &T, &n_seq) == 2) {
       // the norm and rotation of T tokens of n_seq heads in all: wavefronts, tokens times the wavefronts that share one, most threads in a dimension
       const int parts = rope_parts(T, n_seq);
