@@ -499,8 +499,8 @@ __device__ __forceinline__ float row_max(float v) { return over_row(v, [](float 
 __device__ __forceinline__ float row_sum(float v) { return over_row(v, [](float a, float b) { return a + b; }); }
 
 // What is not finite in a tile's masked places.  A masked probability is 0, and 0 times a NaN or an infinity would be NaN in rows that
-// do not see it.  Where a step masks anything, what is not finite becomes 0 in the tile before it is used.  Whoever sees it is made NaN
-// by hand: forward the output (the log-sum-exp has no part of the values), backwards the probabilities (mark_odd).
+// do not see it.  Where a step masks anything, what is not finite becomes 0 in the tile before it is used.  The
+// probabilities of those rows are made NaN for whoever sees them (mark_odd); forward after they are summed, for the values are no part of that.
 //
 // Whether this wavefront has staged any such number: its pieces of a tile (j W + wave, of 1 KiB), before the others have to be there.
 template <class T, int LOADS, int W>
@@ -586,6 +586,19 @@ __device__ __forceinline__ void mark_odd(f32x4 (&s)[2][2], uint32_t odd) {
 #pragma unroll
     for (int x = 0; x < 8; ++x)
       if (odd >> (group * 4 + (x >> 2) * 16 + (x & 3)) & 1) s[n][x >> 2][x & 3] = quiet_nan();
+}
+
+// ... of probabilities that are operands already, those of the first `sees` keys.
+__device__ __forceinline__ void set_nan(bf16x8& f, int x) { f[x] = (bf16_t)quiet_nan(); }
+__device__ __forceinline__ void set_nan(FragF32& f, int x) { f.x[x >> 2][x & 3] = quiet_nan(); }
+template <class Frag>
+__device__ __forceinline__ void mark_odd(Frag& w, uint32_t odd, int sees) {
+  const int group = fresh(threadIdx.x) >> 4 & 3;
+#pragma unroll
+  for (int x = 0; x < 8; ++x) {
+    const int key = group * 4 + (x >> 2) * 16 + (x & 3);
+    if (key < sees && (odd >> key & 1)) set_nan(w, x);
+  }
 }
 
 // Scores of two blocks of 16 rows of a tile in LDS (keys, or rows) with the wavefront's 32 rows (keys): s[n][b] is the tile's block b,
@@ -858,18 +871,12 @@ __global__ __launch_bounds__(256, WK == 4 ? 1 : WK == 2 && DW > 64 ? 2 : sizeof(
       }
       pack(s[n][0], s[n][1], w[n]);
     }
+    if (odd_keys) {      // behind the sums: a value is no part of them
+#pragma unroll
+      for (int n = 0; n < 2; ++n) mark_odd(w[n], odd_keys, row_sees[n] - j0 - half);
+    }
     ready(w);
     add_columns<Lds, DB>(o, v_columns, 0, w, [](int) {});
-    if (odd_keys) {      // a value is no part of the probabilities' sum
-      settle(o);
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const int first = __ffs(odd_keys) - 1;
-        if (j0 + half + first >= row_sees[n]) continue;
-#pragma unroll
-        for (int d = 0; d < DB; ++d) o[n][d] = f32x4{} + quiet_nan();
-      }
-    }
   }
   settle(o);
   const auto finish = [&](float m2, float l) { return l == 0.f ? -__builtin_inff() : (m2 + __builtin_amdgcn_logf(l)) * kLn2f; };
