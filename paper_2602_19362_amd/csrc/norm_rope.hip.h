@@ -155,11 +155,11 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope_bwd(const NormRopeArgs p) 
         const bool query = h < p.hq;
         f32x4 ua = da[i] * cos + at.partner(db[i]) * sin, ub = db[i] * cos - at.partner(da[i]) * sin;
         if (p.q_gain) {
-          const float r = rsqrtf(group_sum(dot4(a[i], a[i]) + dot4(b[i], b[i])) / (float)p.D + p.eps);
+          // (a head behind the last holds zeros, which without eps have no norm)
+          const float norm = rsqrtf(group_sum(dot4(a[i], a[i]) + dot4(b[i], b[i])) / (float)p.D + p.eps), r = h < heads ? norm : 0.f;
           const f32x4 xa = a[i] * r, xb = b[i] * r;
-          // (a head behind the last is no head of zeros: without eps that has no norm)
           if (query) sum_q[0] += ua * xa, sum_q[1] += ub * xb;
-          else if (h < heads) sum_k[0] += ua * xa, sum_k[1] += ub * xb;
+          else sum_k[0] += ua * xa, sum_k[1] += ub * xb;      // of a head behind the last: zeros
           ua = ua * (query ? gq[0] : gk[0]);
           ub = ub * (query ? gq[1] : gk[1]);
           const float m = group_sum(dot4(ua, xa) + dot4(ub, xb)) / (float)p.D;
