@@ -453,7 +453,7 @@ __device__ __forceinline__ int all_rows_see(const AttnArgs& p, const SeqTile& t)
 // reach of all (which a tile of one token's heads has, too) in the step in which it ends.
 template <int KEYS>
 __device__ __forceinline__ bool hides(const SeqTile& t, int all_see, int from) {
-  return all_see < (from + KEYS < t.nk ? from + KEYS : t.nk);
+  return all_see < t.nk && all_see < from + KEYS;
 }
 
 template <int WK> constexpr int fwd_keys = WK == 2 ? 64 : 32;   // keys staged at a time: forward
@@ -499,8 +499,9 @@ __device__ __forceinline__ float row_max(float v) { return over_row(v, [](float 
 __device__ __forceinline__ float row_sum(float v) { return over_row(v, [](float a, float b) { return a + b; }); }
 
 // What is not finite in a tile's masked places.  A masked probability is 0, and 0 times a NaN or an infinity would be NaN in rows that
-// do not see it.  Where a step masks anything, what is not finite becomes 0 in the tile before it is used.  The
-// probabilities of those rows are made NaN for whoever sees them (mark_odd); forward after they are summed, for the values are no part of that.
+// do not see it.  Where a step masks anything, what is not finite becomes 0 in the tile before it is used.  Forward the
+// rows that see it are remembered and their outputs made NaN in the end (a value is no part of the log-sum-exp); backwards their probabilities are
+// made NaN (mark_odd).
 //
 // Whether this wavefront has staged any such number: its pieces of a tile (j W + wave, of 1 KiB), before the others have to be there.
 template <class T, int LOADS, int W>
@@ -586,19 +587,6 @@ __device__ __forceinline__ void mark_odd(f32x4 (&s)[2][2], uint32_t odd) {
 #pragma unroll
     for (int x = 0; x < 8; ++x)
       if (odd >> (group * 4 + (x >> 2) * 16 + (x & 3)) & 1) s[n][x >> 2][x & 3] = quiet_nan();
-}
-
-// ... of probabilities that are operands already, those of the first `sees` keys.
-__device__ __forceinline__ void set_nan(bf16x8& f, int x) { f[x] = (bf16_t)quiet_nan(); }
-__device__ __forceinline__ void set_nan(FragF32& f, int x) { f.x[x >> 2][x & 3] = quiet_nan(); }
-template <class Frag>
-__device__ __forceinline__ void mark_odd(Frag& w, uint32_t odd, int sees) {
-  const int group = fresh(threadIdx.x) >> 4 & 3;
-#pragma unroll
-  for (int x = 0; x < 8; ++x) {
-    const int key = group * 4 + (x >> 2) * 16 + (x & 3);
-    if (key < sees && (odd >> key & 1)) set_nan(w, x);
-  }
 }
 
 // Scores of two blocks of 16 rows of a tile in LDS (keys, or rows) with the wavefront's 32 rows (keys): s[n][b] is the tile's block b,
@@ -791,6 +779,7 @@ __global__ __launch_bounds__(256, WK == 4 ? 1 : WK == 2 && DW > 64 ? 2 : sizeof(
   f32x4 o[2][DB];
   float m[2], l[2];                                // m: the running maximum before scaling; l: this lane's keys
   int all_see = t.nk;                              // keys that every row of this wavefront sees
+  int sees_odd = 0;                                // rows (bits) that see a value that is not finite
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     const Row row(p, t, row0 + n * 16);
@@ -829,7 +818,12 @@ __global__ __launch_bounds__(256, WK == 4 ? 1 : WK == 2 && DW > 64 ? 2 : sizeof(
     const int k_rows = Lds::rows_place(own, threadIdx.x), v_columns = Lds::columns_place(own + SIZE, threadIdx.x);
     f32x4 s[2][2];     // [rows][keys]
     scores<Lds, KS>(s, k_rows, 0, q, [](int) {});
-    const uint32_t odd_keys = odd ? (uint32_t)(clean_tile<T, DP, KEYS, W>(lds + slot + SIZE, words + 32) >> half) : 0;
+    if (odd) {
+      const int first = __ffs((uint32_t)(clean_tile<T, DP, KEYS, W>(lds + slot + SIZE, words + 32) >> half)) - 1;
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+        if (first >= 0 && j0 + half + first < row_sees[n]) sees_odd |= 1 << n;
+    }
     if (j0 + half + 32 > all_see) {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
@@ -871,14 +865,17 @@ __global__ __launch_bounds__(256, WK == 4 ? 1 : WK == 2 && DW > 64 ? 2 : sizeof(
       }
       pack(s[n][0], s[n][1], w[n]);
     }
-    if (odd_keys) {      // behind the sums: a value is no part of them
-#pragma unroll
-      for (int n = 0; n < 2; ++n) mark_odd(w[n], odd_keys, row_sees[n] - j0 - half);
-    }
     ready(w);
     add_columns<Lds, DB>(o, v_columns, 0, w, [](int) {});
   }
   settle(o);
+  if (__any(sees_odd)) {
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+        if (sees_odd >> n & 1) o[n][d] = f32x4{} + quiet_nan();
+  }
   const auto finish = [&](float m2, float l) { return l == 0.f ? -__builtin_inff() : (m2 + __builtin_amdgcn_logf(l)) * kLn2f; };
   const auto inverse = [&](float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : l; };
   if constexpr (WK == 1) {
