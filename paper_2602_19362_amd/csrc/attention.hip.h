@@ -730,12 +730,13 @@ __device__ __forceinline__ float* partial_row(const AttnArgs& p, int part, int64
 
 // WK = 1: a workgroup has 128 rows, 32 a wavefront, over all keys that they see, 32 at a time.  Three wavefronts a SIMD: one's exponentials
 // run beside another's products.  Bound by the matrix cores at the clock that the power limit leaves, and by the exponentials' issue
-// between them: 4 x 8192 tokens, 32 heads on 8 of 128 channels, no mask, 1066 ... 1156 TFLOP/s by box (a 16384^3 product of the vendor's library
+// between them: 4 x 8192 tokens, 32 heads on 8 of 128 channels, no mask, 1081 ... 1115 TFLOP/s by box, calls in turn (a 16384^3 product of the vendor's library
 // 1353), matrix cores busy 0.53 of the time at 1.7 GHz.  64 keys at a time by two wavefronts a SIMD: 5 % less.
 // WK = 2, for few rounds of tiles: 64 rows, two wavefronts for either half of 64 keys; they join at the end.
 // WK = 4, for few rows: the wavefronts have the same 32 rows and take the steps of 32 keys in turn, each through LDS of its own, and
-// join at the end.  That is bound by reading the keys and values: 64 single tokens over up to 4096 each, 8 key heads, 599 MB in 109 us,
-// 5.5 TB/s; 8 over 32768 in parts, 1.07 GB in 181 us, 5.9 TB/s (a large read reaches 5.95).
+// join at the end.  That is bound by reading the keys and values: 64 single tokens over up to 4096 each, 8 key heads, 599 MB in 112 us,
+// 5.3 TB/s; 8 over 32768 in parts, 1.07 GB in 184 us, 5.8 TB/s (a large read reaches 5.95).  In fp32 a wavefront's LDS holds one step at a time, and
+// loads wait for products: 244 us, 4.9 TB/s, and 392 us, 5.5 TB/s.
 // Where tiles are few, their keys are split over workgroups whose results k_attn_join puts together.
 template <class T, int DW, int WK>
 __global__ __launch_bounds__(256, WK == 4 ? 1 : WK == 2 && DW > 64 ? 2 : sizeof(T) == 2 ? 3 : 2) void k_attn_fwd(const AttnArgs p) {
@@ -1043,8 +1044,9 @@ __device__ __forceinline__ void store_share(char* row, int c0, const f32x4 (&x)[
 // turn (WK = 4), as forward.
 // dq is summed here and dk, dv in the other kernel, which computes z and dP again (seven products, not five): one kernel would add to dq in
 // memory from all tiles of keys, by atomics in an order that changes, or through sums of (keys / 128) x dq's size.
-// Bound by the matrix cores at the power limit: 2 x 8192 tokens, 32 heads on 8 of 128 channels, no mask, three products in 2.78 ms, 1186
-// TFLOP/s, matrix cores busy 0.59 at 1.87 GHz.
+// Bound by the matrix cores at the power limit: 2 x 8192 tokens, 32 heads on 8 of 128 channels, no mask, three products in 2.94 ms, 1123
+// TFLOP/s, matrix cores busy 0.58 at 1.85 GHz (under the profiler; both kernels in turn without it 6.10 ... 6.40 ms, 1202 ... 1262).  fp32 operands are
+// twice as wide for the same registers: at 96 channels 17 to 19 are spilled, at 128 channels 87 (WK = 4) and 165.
 template <class T, int DW, int WK>
 __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs p) {
   constexpr bool kAlone = WK == 4;      // a wavefront stages keys for itself
@@ -1256,8 +1258,9 @@ struct RowLds {
 // dk and dv: a workgroup has 128 keys, 32 a wavefront, over all rows that see any of them, 64 at a time; or (WK = 2) 64 keys, two
 // wavefronts for either half of the 64 rows; or (WK = 4) 32 keys, over steps of 32 rows that the wavefronts take in turn.
 // Two accumulators and two resident operands fill a lane's 256 registers, so where in LDS a step reads is computed anew each time.  Bound by
-// the matrix cores at the power limit: 2 x 8192 tokens, 32 heads on 8 of 128 channels, no mask, four products in 3.70 ms, 1189
-// TFLOP/s, matrix cores busy 0.57 at 1.92 GHz.
+// the matrix cores at the power limit: 2 x 8192 tokens, 32 heads on 8 of 128 channels, no mask, four products in 3.92 ms, 1123
+// TFLOP/s, matrix cores busy 0.56 at 1.89 GHz (under the profiler, as above).  Spilled all the same: at 128 channels 9 registers (WK = 4: 4), in fp32
+// 100; at 96 channels in fp32 11 to 13.
 template <class T, int DW, int WK>
 __global__ __launch_bounds__(256, 2) void k_attn_dkdv(const AttnArgs p) {
   constexpr int DP = padded(DW);

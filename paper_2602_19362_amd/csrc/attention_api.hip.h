@@ -102,7 +102,7 @@ static void attn_cut(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int g, int 
   // on 8 (832) 14 / 10 / 11.  Equal walks, each at its best split, 32 / 128: 16 sequences of 64 rows over 2000 keys, 8 key heads (256) 29 / 34, of 96
   // rows (384) 52 / 38.
   // fp32 products take nine times as long, and what small tiles cost is hidden behind them for longer: 80 channels, 4 of 400 tokens, 6 on 2
-  // (304) 25 / 50; 64 channels, 2 of 1000, 16 on 8 (1008) 57 / 85; 4 of 2000, 8 on 2 (2000) 353 / 382; 4 of 4000, 8 heads (4000) 1255 / 1113.
+  // (304) 25 / 50; 64 channels, 2 of 1000, 16 on 8 (1008) 57 / 85; 4 of 2000, 8 on 2 (2000) 354 / 381; 4 of 4000, 8 heads (4000) 1252 / 1111.
   const int64_t t32 = tiles(rows, 32), t64 = tiles(rows, 64), t128 = tiles(rows, 128), steps = Tk / seqs / 32;
   p.few = rows <= seqs * 32 || t32 <= (f32 ? 2048 : D <= 64 ? 512 : 256) || (causal && t32 <= 512 && steps >= 30 && 2 * Tq > Tk);
   // ... in parts of the keys.  Small tiles, parts that fill the round: one token over 4096 / 32768 keys, 8 key heads, 1 part 35 / 236, 8
@@ -118,8 +118,8 @@ static void attn_cut(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int g, int 
   p.two = !f32 && !p.few && p.fwd == 1 && (D <= 64 ? t128 <= 768 : (t64 <= 512 && t64 > t128) || (t128 <= 400 && steps >= 24));
   // dq: tiles of 32 rows up to two rounds.  32 rows / 128 rows, each at its best split: 64 channels, 1000 tokens, 6 heads (192 small tiles)
   // 48 / 55; 1200, 8 heads (304) 46 / 52; 300, 32 on 8 (304) 79 / 78; 4 of 1000, 4 on one (500) 187 / 193; 4800, 8 on 2 (1200) 278 / 241;
-  // 1000, 32 on 8 (1000) 213 / 199.  fp32: 80 channels, 4 of 400, 6 on 2 (304) 291 / 301; 64 channels, 2 of 1000, 16 on 8 (1008) 362 / 401; 8
-  // of 600, 8 on 2 (1200) 983 / 943.
+  // 1000, 32 on 8 (1000) 213 / 199.  fp32, the other kernel by the rules: 80 channels, 4 of 400, 6 on 2 (304) 85 / 91; 64 channels, 2 of 1000, 16 on 8
+  // (1008) 187 / 204; 8 of 600, 8 on 2 (1200) 491 / 444.
   p.few_dq = t32 <= (f32 ? 1024 : 512);
   // ... in parts of the keys.  Small tiles: 16 rows over 4096 keys (2 of 32 steps), 1 part 50, 4 30, 8 25; 64 rows over 1024 (8 of 8), 1
   // part 28, 2 27; 2000 tokens, one head (63 of 15), 1 part 57, 2 52; 192 of 7, 1 part 48, 2 51.  Large ones: 9000, 4 on one (282 of 140), 1
@@ -134,8 +134,8 @@ static void attn_cut(AttnPlan& p, int64_t Tq, int64_t Tk, int n_seq, int g, int 
   // its best split: 300 tokens, 32 on 8 (80 small tiles of 18 steps) 39 / 44 / 48; 4 of 300 (320 of 18) 48 / 59 / 64; 1000 (256 of 62) 83 / 78 / 87; 1500
   // (376 of 93) 129 / 119 / 135; 16 of 200, 16 on 8 (896 of 6) 64 / 48 / 54; 4 of 1000, 16 on 8 (1024 of 31) 126 / 102 / 116.  64 channels: 13 of up
   // to 400, 14 on 2 (338 of 43) 37 / 44 / 47; 4 of 1000, 16 on 8 (1024 of 31) 68 / 75 / 78; 64 of up to 120, 8 heads (2048 of one) 32 / 24 / 25.
-  // fp32, 32 / 128: 80 channels, 4 of 400, 6 on 2 (104 of 18) 138 / 150; 64 channels, 8 of 1000, 8 heads (2048 of 15) 338 / 358; 4 of 2000, 8 on 2
-  // (504 of 125) 1634 / 1590; 96 channels, 8000, 8 on 2 (500 of 500) 3530 / 3353; 4 of 4000, 8 heads (4000 of 62) 6267 / 5964.
+  // fp32, 32 / 128: 80 channels, 4 of 400, 6 on 2 (104 of 18) 86 / 98; 64 channels, 8 of 1000, 8 heads (2048 of 15) 339 / 356; 4 of 2000, 8 on 2
+  // (504 of 125) 1637 / 1578; 96 channels, 8000, 8 on 2 (500 of 500) 3537 / 3360; 4 of 4000, 8 heads (4000 of 62) 6268 / 5790.
   const int64_t small = tiles(Tk, 32), work = small * std::max<int64_t>(1, rows / seqs / 64);
   p.few_dkdv = f32 ? work <= 256 * 128 : D <= 64 ? small <= 1024 && work <= 256 * 128 : small <= 400 && work <= 256 * 64;
   // Tiles of 64 keys halve the longest walks, which end a call of few rounds, and read rows twice as often.  64 / 128 keys, each at its best

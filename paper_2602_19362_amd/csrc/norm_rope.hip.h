@@ -76,7 +76,8 @@ __device__ __forceinline__ void token_angles(const NormRopeArgs& p, const Pieces
 // backwards 113 / 108 / 139 us, forward 71 / 73 / 72.
 constexpr int kRopeHeads = 2;
 
-// 16411 tokens of 32 + 8 heads of 128 in bf16: 336 MB in 67 us, 5.0 TB/s; a large copy reaches 5.07.  8 tokens 3.3 us, the launch.
+// 16411 tokens of 32 + 8 heads of 128 in bf16: 336 MB in 73 us, 4.6 TB/s (in fp32 671 MB in 134, 5.0); a large copy reaches 5.07.  8 tokens 3.7 us, the
+// launch.
 template <class T>
 __global__ __launch_bounds__(256) void k_qk_norm_rope_fwd(const NormRopeArgs p) {
   const int lane = threadIdx.x & 63, group = lane >> 4;
@@ -123,7 +124,7 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope_fwd(const NormRopeArgs p) 
   }
 }
 
-// The same tokens: 504 MB in 100 us, 5.1 TB/s, with the workgroups' sums for the gains.
+// The same tokens: 504 MB in 102 us, 4.9 TB/s, with the workgroups' sums for the gains.
 template <class T>
 __global__ __launch_bounds__(256) void k_qk_norm_rope_bwd(const NormRopeArgs p) {
   const int lane = threadIdx.x & 63, group = lane >> 4;

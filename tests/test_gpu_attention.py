@@ -376,7 +376,7 @@ def test_in_a_graph_with_other_values():
         assert all(torch.equal(a, b) for a, b in zip(held, step()))
 
 
-# Enough tiles that every wavefront has 32 rows (keys) of its own, in all three kernels.
+# Enough tiles for larger ones in some of the three kernels (which ones is asserted for the cases of test_gpu_attention_forms.py).
 MANY = [("bf16", [1100, 70], [1100, 333], 48, 8), ("bf16", [1500], [1500], 32, 8), ("bf16", [5000], [5000], 8, 2),
         ("f32", [1000, 37, 600, 901, 300, 700, 650, 612], [1000, 37, 600, 901, 400, 600, 650, 612], 16, 16)]
 
