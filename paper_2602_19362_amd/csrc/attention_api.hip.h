@@ -24,10 +24,11 @@ static int check_heads(const oapl_heads* x, int64_t n, int heads, int D, int dty
   return OAPL_OK;
 }
 
-static Heads heads_of(const oapl_heads* x, int dtype) {
-  if (!x) return Heads{nullptr, 0, 0};
+// The operand that check_heads has accepted.  The stride of a single token or head was not looked at, and nothing is multiplied by it.
+static Heads heads_of(const oapl_heads* x, int64_t n, int heads, int dtype) {
+  if (!x || n == 0) return Heads{nullptr, 0, 0};
   const int64_t size = (int64_t)esize(dtype);
-  return Heads{(char*)x->data, x->token_stride * size, x->head_stride * size};
+  return Heads{(char*)x->data, n > 1 ? x->token_stride * size : 0, heads > 1 ? x->head_stride * size : 0};
 }
 
 static bool head_counts_ok(int hq, int hk, int D) {
@@ -71,7 +72,7 @@ static int rope_args(NormRopeArgs& a, const oapl_heads* q, const oapl_heads* k, 
   if (int rc = check_heads(k, T, hk, D, dtype, false)) return rc;
   if ((uintptr_t)cos_sin % 16 || (uintptr_t)q_gain % 16 || (uintptr_t)k_gain % 16) return OAPL_ERR_ALIGN;
   a = NormRopeArgs{};
-  a.q = heads_of(q, dtype), a.k = heads_of(k, dtype);
+  a.q = heads_of(q, T, hq, dtype), a.k = heads_of(k, T, hk, dtype);
   a.positions = positions, a.cos_sin = cos_sin, a.q_gain = q_gain, a.k_gain = k_gain;
   a.T = T, a.n_pos = n_pos, a.hq = hq, a.hk = hk, a.D = D, a.rot = rot, a.eps = eps;
   return OAPL_OK;
@@ -196,7 +197,7 @@ static int attn_args(AttnArgs& a, const oapl_heads* q, const oapl_heads* k, cons
   if (int rc = check_heads(k, Tk, hk, D, dtype, false)) return rc;
   if (int rc = check_heads(v, Tk, hk, D, dtype, false)) return rc;
   a = AttnArgs{};
-  a.q = heads_of(q, dtype), a.k = heads_of(k, dtype), a.v = heads_of(v, dtype);
+  a.q = heads_of(q, Tq, hq, dtype), a.k = heads_of(k, Tk, hk, dtype), a.v = heads_of(v, Tk, hk, dtype);
   a.q_offsets = q_offsets, a.k_offsets = k_offsets;
   a.Tq = Tq, a.Tk = Tk, a.n_seq = n_seq, a.hq = hq, a.hk = hk, a.g = hq / hk, a.D = D, a.causal = causal != 0, a.scale = scale;
   // floor(2^(31 + s) / g) + 1 with 2^s >= g: exact for numbers below 2^31
@@ -325,8 +326,9 @@ int32_t oapl_qk_norm_rope_fwd(const oapl_heads* q, const oapl_heads* k, const oa
     if (int rc = check_heads(v_out, out_rows, n_k_heads, head_dim, dtype, true)) return rc;
   }
   if (T == 0) return OAPL_OK;
-  a.v = heads_of(v, dtype);
-  a.q_out = heads_of(q_out, dtype), a.k_out = heads_of(k_out, dtype), a.v_out = heads_of(v_out, dtype);
+  a.v = heads_of(v, T, n_k_heads, dtype);
+  a.q_out = heads_of(q_out, T, n_q_heads, dtype), a.k_out = heads_of(k_out, out_rows, n_k_heads, dtype);
+  a.v_out = heads_of(v_out, out_rows, n_k_heads, dtype);
   a.rows = rows, a.n_rows = n_rows;
   a.parts = rope_parts(T, n_q_heads + n_k_heads * (v ? 2 : 1));
   const dim3 grid = rope_fwd_grid(T, a.parts);
@@ -360,8 +362,8 @@ int32_t oapl_qk_norm_rope_bwd(const oapl_heads* q, const oapl_heads* k, const oa
   if (q_gain &&
       !workspace_ok(workspace, workspace_bytes, oapl_qk_norm_rope_workspace_bytes(T, n_q_heads, n_k_heads, head_dim)))
     return OAPL_ERR_WORKSPACE;
-  a.q_out = heads_of(dq_out, dtype), a.k_out = heads_of(dk_out, dtype);
-  a.dq = heads_of(dq, dtype), a.dk = heads_of(dk, dtype);
+  a.q_out = heads_of(dq_out, T, n_q_heads, dtype), a.k_out = heads_of(dk_out, T, n_k_heads, dtype);
+  a.dq = heads_of(dq, T, n_q_heads, dtype), a.dk = heads_of(dk, T, n_k_heads, dtype);
   a.partials = q_gain ? (float*)workspace : nullptr;
   a.parts = rope_parts(T, n_q_heads + n_k_heads);
   const unsigned grid = rope_bwd_grid(T, n_q_heads + n_k_heads);
@@ -402,7 +404,7 @@ int32_t oapl_attention_fwd(const oapl_heads* q, const oapl_heads* k, const oapl_
   if (int rc = check_heads(out, Tq, n_q_heads, head_dim, dtype, true)) return rc;
   if (!workspace_ok(workspace, workspace_bytes, p.total)) return OAPL_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)stream;
-  a.o = heads_of(out, dtype);
+  a.o = heads_of(out, Tq, n_q_heads, dtype);
   a.lse = lse;
   a.k_used = k_used;
   a.status = (int*)workspace;
@@ -434,10 +436,10 @@ int32_t oapl_attention_bwd(const oapl_heads* q, const oapl_heads* k, const oapl_
   if (int rc = check_heads(dv, Tk, n_k_heads, head_dim, dtype, true)) return rc;
   if (!workspace_ok(workspace, workspace_bytes, p.total)) return OAPL_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)stream;
-  a.o = heads_of(out, dtype), a.dout = heads_of(dout, dtype);
+  a.o = heads_of(out, Tq, n_q_heads, dtype), a.dout = heads_of(dout, Tq, n_q_heads, dtype);
   // RowStager's offsets: 64 tokens and the heads of a group within 31 bits
-  if (Tq > 0 && a.g > 1 && std::max(a.q.head, a.dout.head) > ((int64_t)1 << 30) / (a.g - 1)) return OAPL_ERR_SHAPE;
-  a.dq = heads_of(dq, dtype), a.dk = heads_of(dk, dtype), a.dv = heads_of(dv, dtype);
+  if (a.g > 1 && std::max(a.q.head, a.dout.head) > ((int64_t)1 << 30) / (a.g - 1)) return OAPL_ERR_SHAPE;
+  a.dq = heads_of(dq, Tq, n_q_heads, dtype), a.dk = heads_of(dk, Tk, n_k_heads, dtype), a.dv = heads_of(dv, Tk, n_k_heads, dtype);
   a.lse = const_cast<float*>(lse);
   a.lse2 = (float*)((char*)workspace + p.off_lse2);
   a.delta = (float*)((char*)workspace + p.off_delta);
