@@ -66,7 +66,7 @@ typedef enum {
   OAPL_ERR_HIP = 8,         /* a HIP launch or runtime call failed */
   OAPL_ERR_TOKEN_RANGE = 9, /* device: sampled token outside [0, V) */
   OAPL_ERR_SCRATCH_LIMIT = 10, /* oapl_loss_fwd_bwd_noalloc: the sizes need more than the static scratch */
-  OAPL_ERR_ALIGN = 11       /* a pointer or stride of heads is not a multiple of 16 bytes */
+  OAPL_ERR_ALIGN = 11       /* a pointer or stride of heads is not a multiple of 16 bytes, another pointer not of an element */
 } oapl_status;
 
 typedef enum {
@@ -478,6 +478,126 @@ int32_t oapl_attention_bwd(const oapl_heads* q, const oapl_heads* k, const oapl_
                            int32_t head_dim, int32_t dtype, int32_t causal, float scale,
                            const oapl_heads* dq, const oapl_heads* dk, const oapl_heads* dv,
                            void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Around the policy's blocks: the embedding, the residual stream with its norms, and the gradients' common norm.
+ *
+ * An operand of rows is [rows][channels] with the channels side by side and any distance between rows (in elements), from any element
+ * on; inputs may have a row stride of 0 (broadcast), rows that are written must not overlap.  The stride of a single row is not
+ * looked at.
+ */
+typedef struct {
+  void* data;
+  int64_t row_stride;
+} oapl_rows;
+
+/*
+ * Rows of the embedding, scaled:   out_t = scale E[tokens_t],   rounded once.
+ *   E        [V][d] in dtype (may be the head's W), from any element on
+ *   tokens   [T] int32 in [0, V); a token outside gets NaN
+ *   out      [T][d] in out_dtype
+ *   0 <= T <= 65535 * 256, 1 <= d, V <= 2^21 (else OAPL_ERR_SHAPE), scale finite (else OAPL_ERR_BETA)
+ * Needs no workspace.
+ */
+int32_t oapl_embed_fwd(const void* E, const int32_t* tokens, int64_t T, int32_t d, int32_t V, int32_t dtype, int32_t out_dtype,
+                       float scale, const oapl_rows* out, void* stream);
+
+/* Bytes of workspace of the next call; 0 for invalid sizes. */
+size_t oapl_embed_workspace_bytes(int64_t T, int32_t d, int32_t V);
+
+/*
+ * Its gradient:   dE[v] = scale sum over t with tokens_t = v of dout_t
+ *
+ * summed in 32 bits and in a fixed order (the same bits every time).
+ *   dout        [T][d] in dtype
+ *   accumulate  0: dE is overwritten, rows without tokens with zeros; otherwise the sums are added to what dE holds (the head's dW, where
+ *               embedding and head share their weights), and rows without tokens stay as they are
+ *   dE          [V][d] float, from any element on
+ * A token outside [0, V) has no part in dE and leaves OAPL_ERR_TOKEN_RANGE in the workspace's status.
+ */
+int32_t oapl_embed_bwd(const oapl_rows* dout, const int32_t* tokens, int64_t T, int32_t d, int32_t V, int32_t dtype, float scale,
+                       int32_t accumulate, float* dE, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A block's output y added to the residual stream x, with a norm behind the block, a gate and a scale, and the norm of the sum for
+ * the next block, in one pass:
+ *
+ *     z = y_gain o y / sqrt(mean_c y_c^2 + eps)   (z = y without y_gain)
+ *     x' = x + scale gate o z                     (without gate: scale z)
+ *     n = gain o x' / sqrt(mean_c x'_c^2 + eps)
+ *
+ * Sums and products in 32 bits, one rounding of x' and one of n (which comes from x' before its rounding).
+ *   x, x_out   [T][d] in x_dtype; x_out may be x
+ *   y          [T][d] in dtype, or NULL (and y_gain, gate, x_out too): n of x alone
+ *   gain, out  [d] and [T][d] in dtype, or both NULL: the sum alone; out may be y where there is an x_out
+ *   gate       NULL; rows [T][d] in dtype (gate_per_token not 0); or [d], the same for all tokens (gate_per_token 0)
+ *   x_dtype    dtype, or OAPL_F32 with blocks in OAPL_BF16 (else OAPL_ERR_DTYPE)
+ *   0 <= T <= 65535 * 256, 1 <= d <= 16384 (else OAPL_ERR_SHAPE); eps >= 0, eps and scale finite (else OAPL_ERR_BETA)
+ * What is not finite in a row stays in that row.  Needs no workspace.
+ */
+int32_t oapl_residual_norm_fwd(const oapl_rows* x, const oapl_rows* y, const void* y_gain, const oapl_rows* gate, int32_t gate_per_token,
+                               const void* gain, int64_t T, int32_t d, int32_t x_dtype, int32_t dtype, float scale, float eps,
+                               const oapl_rows* x_out, const oapl_rows* out, void* stream);
+
+/* Bytes of workspace of the next call; 0 for invalid sizes. */
+size_t oapl_residual_norm_workspace_bytes(int64_t T, int32_t d);
+
+/*
+ * Its gradients.  x: the stream behind the block (x' above; x where there is no y); y, y_gain, gate, gain: as in the forward call;
+ * dx_out, dout: gradients of x' (or NULL: none) and n.  With r, r_y one over the roots above, dX the whole gradient of x':
+ *
+ *     v = r x',  u = gain o dout,  dX = dx_out + r (u - v mean_c(u o v))         dgain = sum_t dout o v
+ *     dx = dX,   dz = scale gate o dX                                           dgate = scale z o dX
+ *     w = r_y y, t = y_gain o dz,  dy = r_y (t - w mean_c(t o w))                dy_gain = sum_t dz o w
+ *
+ * (without y_gain dy = dz).  Norms are taken of x' as it is stored.
+ *   dx, dy         [T][d] in x_dtype and dtype; dx may be dx_out or x, dy may be y or dout
+ *   dgain, dy_gain [d] float, summed over tokens in a fixed order; NULL where there is no such gain
+ *   dgate_rows     rows [T][d] in dtype, may be gate: of a gate for every token; otherwise not looked at
+ *   dgate          [d] float, summed over tokens: of a gate that they share; otherwise not looked at
+ * The workspace is looked at only where there is a sum over tokens.
+ */
+int32_t oapl_residual_norm_bwd(const oapl_rows* x, const oapl_rows* y, const void* y_gain, const oapl_rows* gate, int32_t gate_per_token,
+                               const void* gain, const oapl_rows* dx_out, const oapl_rows* dout, int64_t T, int32_t d, int32_t x_dtype,
+                               int32_t dtype, float scale, float eps, const oapl_rows* dx, const oapl_rows* dy, float* dgain,
+                               float* dy_gain, const oapl_rows* dgate_rows, float* dgate, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
+/*
+ * A dense tensor of n elements, from any element on (device pointers).  The list of tensors itself is host memory, which the calls
+ * below have read when they return.
+ */
+typedef struct {
+  const void* data;
+  void* out;         /* oapl_clip_grads: where the result goes, in the same dtype; may be data */
+  int64_t n;
+  int32_t dtype;
+} oapl_tensor;
+
+/* Bytes of workspace of the next two calls; 0 for invalid counts. */
+size_t oapl_clip_workspace_bytes(int32_t n_tensors);
+
+/*
+ * The norm of all tensors together:   norm = sqrt(sum over tensors and their elements g^2)
+ *
+ * Squares and their sum in 64 bits, in a fixed order; rounded to 32 bits once.
+ *   n_tensors  0 .. 2^20, of less than 2^45 elements in all (else OAPL_ERR_SHAPE); tensors may be empty
+ *   norm       [1] float
+ */
+int32_t oapl_grad_norm(const oapl_tensor* tensors, int32_t n_tensors, float* norm, void* workspace, size_t workspace_bytes,
+                       void* stream);
+
+/*
+ * Tensors scaled to a common norm:   out = g max_norm / norm   where norm is finite and larger than max_norm, otherwise out = g
+ *
+ * so what is not finite is not spread, and shows in norm.  The product is rounded once.
+ *   norm_given  NULL: the norm of these tensors, which is written to norm_out [1] float; or [1] float, the norm to go by (of tensors
+ *               on other GPUs too, say), and norm_out NULL; no workspace is needed then
+ *   max_norm    >= 0 and finite (else OAPL_ERR_BETA)
+ * What is written may overlap nothing but its own input, and that only in place (else OAPL_ERR_SHAPE).
+ */
+int32_t oapl_clip_grads(const oapl_tensor* tensors, int32_t n_tensors, float max_norm, const float* norm_given, float* norm_out,
+                        void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

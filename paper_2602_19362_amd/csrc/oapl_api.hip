@@ -1836,3 +1836,4 @@ int32_t oapl_read_device_status(const void* workspace, void* stream, int32_t* st
 }  // extern "C"
 
 #include "attention_api.hip.h"
+#include "blocks_api.hip.h"

@@ -36,7 +36,20 @@ class Heads(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
+class Rows(ctypes.Structure):
+    """oapl_rows: an operand [rows][channels], the stride in elements."""
+
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64)]
+
+
+class Tensor(ctypes.Structure):
+    """oapl_tensor: a dense tensor and where its result goes."""
+
+    _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
 _H = ctypes.POINTER(Heads)
+_R = ctypes.POINTER(Rows)
 _SIGNATURES = {
     "oapl_status_string": (_c.c_char_p, [_c.c_int32]),
     "oapl_workspace_bytes": (_c.c_size_t, [_c.c_int64, _c.c_int32, _c.c_int32, _c.c_int32, _c.c_int32, _c.c_int32,
@@ -69,6 +82,18 @@ _SIGNATURES = {
                            [_c.c_float, _H] + [_c.c_void_p] * 2 + [_c.c_size_t, _c.c_void_p]),
     "oapl_attention_bwd": (_c.c_int32, [_H] * 4 + [_c.c_void_p, _H] + [_c.c_void_p] * 2 + [_c.c_int64] * 2 + [_c.c_int32] * 6 +
                            [_c.c_float] + [_H] * 3 + [_c.c_void_p, _c.c_size_t, _c.c_void_p]),
+    "oapl_embed_fwd": (_c.c_int32, [_c.c_void_p] * 2 + [_c.c_int64] + [_c.c_int32] * 4 + [_c.c_float, _R, _c.c_void_p]),
+    "oapl_embed_workspace_bytes": (_c.c_size_t, [_c.c_int64] + [_c.c_int32] * 2),
+    "oapl_embed_bwd": (_c.c_int32, [_R, _c.c_void_p, _c.c_int64] + [_c.c_int32] * 3 + [_c.c_float, _c.c_int32] + [_c.c_void_p] * 2 +
+                       [_c.c_size_t, _c.c_void_p]),
+    "oapl_residual_norm_fwd": (_c.c_int32, [_R, _R, _c.c_void_p, _R, _c.c_int32, _c.c_void_p, _c.c_int64] + [_c.c_int32] * 3 +
+                               [_c.c_float] * 2 + [_R, _R, _c.c_void_p]),
+    "oapl_residual_norm_workspace_bytes": (_c.c_size_t, [_c.c_int64, _c.c_int32]),
+    "oapl_residual_norm_bwd": (_c.c_int32, [_R, _R, _c.c_void_p, _R, _c.c_int32, _c.c_void_p, _R, _R, _c.c_int64] + [_c.c_int32] * 3 +
+                               [_c.c_float] * 2 + [_R, _R] + [_c.c_void_p] * 2 + [_R] + [_c.c_void_p] * 2 + [_c.c_size_t, _c.c_void_p]),
+    "oapl_clip_workspace_bytes": (_c.c_size_t, [_c.c_int32]),
+    "oapl_grad_norm": (_c.c_int32, [_c.POINTER(Tensor), _c.c_int32] + [_c.c_void_p] * 2 + [_c.c_size_t, _c.c_void_p]),
+    "oapl_clip_grads": (_c.c_int32, [_c.POINTER(Tensor), _c.c_int32, _c.c_float] + [_c.c_void_p] * 3 + [_c.c_size_t, _c.c_void_p]),
     "oapl_read_device_status": (_c.c_int32, [_c.c_void_p, _c.c_void_p, _c.POINTER(_c.c_int32)]),
     "oapl_read_path_taken": (_c.c_int32, [_c.c_void_p, _c.c_void_p, _c.POINTER(_c.c_int32)]),
     "oapl_timing_enable": (_c.c_int32, [_c.c_int32]),
@@ -602,6 +627,251 @@ def attention_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.
     if rc != 0:
         raise OaplError(rc, "oapl_attention_bwd")
     return AttentionGrads(dq, dk, dv, ws)
+
+
+def _rows(t: torch.Tensor, name: str, shape, dtype: torch.dtype, index: int) -> Rows:
+    """The oapl_rows of a tensor [rows, channels] on GPU `index` whose channels lie side by side."""
+    if t.get_device() != index:
+        raise ValueError(f"{name} must live on cuda:{index}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
+    row, channel = t.stride()
+    if channel != 1 and shape[1] > 1 and shape[0] > 0:
+        raise ValueError(f"the channels of {name} must lie side by side")
+    return Rows(t.data_ptr(), row)
+
+
+def _gpu_of(t: torch.Tensor) -> int:
+    """The index of the current GPU, on which t has to live."""
+    index = t.get_device()
+    if index < 0 or index != _current_gpu():
+        _check_device(t)
+    return index
+
+
+def embed_fwd(E: torch.Tensor, tokens: torch.Tensor, *, scale: float = 1.0, out_dtype: Optional[torch.dtype] = None,
+              out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """oapl_embed_fwd: [T, d], the rows of the embedding E [V, d] at `tokens`, scaled; in E's type or out_dtype (or out's)."""
+    gpu = _gpu_of(E)
+    if E.dim() != 2 or tokens.dim() != 1:
+        raise ValueError("E must be [V, d] and tokens [T]")
+    (V, d), T = E.shape, tokens.shape[0]
+    if out is None:
+        out = E.new_empty((T, d), dtype=out_dtype)
+    elif out_dtype is not None and out.dtype is not out_dtype:
+        raise TypeError(f"out must be {out_dtype}, got {out.dtype}")
+    rc = lib().oapl_embed_fwd(_flat(E, E.dtype, "E", gpu), _flat(tokens, torch.int32, "tokens", gpu), T, d, V, _dtype_code(E),
+                              _dtype_code(out), scale, _rows(out, "out", (T, d), out.dtype, gpu), _raw_stream(gpu))
+    if rc != 0:
+        raise OaplError(rc, "oapl_embed_fwd")
+    return out
+
+
+def embed_workspace_bytes(T: int, d: int, V: int) -> int:
+    """oapl_embed_workspace_bytes."""
+    return int(lib().oapl_embed_workspace_bytes(T, d, V))
+
+
+class EmbedGrads(NamedTuple):
+    dE: torch.Tensor              # [V, d] float32
+    workspace: torch.Tensor
+
+
+def embed_bwd(dout: torch.Tensor, tokens: torch.Tensor, V: Optional[int] = None, *, scale: float = 1.0,
+              dE: Optional[torch.Tensor] = None, accumulate: bool = False, workspace: Optional[torch.Tensor] = None) -> EmbedGrads:
+    """oapl_embed_bwd: the embedding's gradient from that of embed_fwd's output.
+
+    A new tensor of V rows, or into dE: overwritten, or added to it (`accumulate`; the head's dW where the weights are shared).
+    """
+    gpu = _gpu_of(dout)
+    if dout.dim() != 2 or tokens.shape != dout.shape[:1]:
+        raise ValueError("dout must be [T, d] and tokens [T]")
+    T, d = dout.shape
+    if dE is None:
+        if V is None or accumulate:
+            raise ValueError("without dE there is nothing to add to, and V has to be given")
+        dE = dout.new_empty((V, d), dtype=torch.float32)
+    elif dE.dim() != 2 or dE.shape[1] != d or (V is not None and dE.shape[0] != V):
+        raise ValueError("dE must be [V, d]")
+    V = dE.shape[0]
+    ws = _scratch(lib().oapl_embed_workspace_bytes(T, d, V), dout, workspace, "oapl_embed_workspace_bytes")
+    rc = lib().oapl_embed_bwd(_rows(dout, "dout", dout.shape, dout.dtype, gpu), _flat(tokens, torch.int32, "tokens", gpu), T, d, V,
+                              _dtype_code(dout), scale, 1 if accumulate else 0, _flat(dE, torch.float32, "dE", gpu), ws.data_ptr(),
+                              ws.numel(), _raw_stream(gpu))
+    if rc != 0:
+        raise OaplError(rc, "oapl_embed_bwd")
+    return EmbedGrads(dE, ws)
+
+
+def residual_norm_workspace_bytes(T: int, d: int) -> int:
+    """oapl_residual_norm_workspace_bytes."""
+    return int(lib().oapl_residual_norm_workspace_bytes(T, d))
+
+
+def _residual_norm_setup(x, y, gain, y_gain, gate):
+    """(shape, the block's type, whether the gate is one a token, its oapl_rows, GPU)."""
+    gpu = _gpu_of(x)
+    if x.dim() != 2:
+        raise ValueError("x must be [tokens, channels]")
+    if y is None and gain is None:
+        raise ValueError("there is neither a block's output to add nor a norm to take")
+    if y is None and (y_gain is not None or gate is not None):
+        raise ValueError("a gate and y_gain go with a block's output y")
+    kind = (gain if y is None else y).dtype
+    d = x.shape[1]
+    if (gain is not None and gain.shape != (d,)) or (y_gain is not None and y_gain.shape != (d,)):
+        raise ValueError("gains must have one value a channel")
+    if gate is None:
+        return x.shape, kind, 0, None, gpu
+    if gate.dim() == 1:
+        if gate.shape != (d,):
+            raise ValueError("a gate that all tokens share must have one value a channel")
+        return x.shape, kind, 0, Rows(_flat(gate, kind, "gate", gpu), 0), gpu
+    return x.shape, kind, 1, _rows(gate, "gate", x.shape, kind, gpu), gpu
+
+
+class ResidualNormResult(NamedTuple):
+    x: torch.Tensor               # [T, d], the stream behind the block (x itself without one)
+    out: Optional[torch.Tensor]   # [T, d], its norm
+
+
+def residual_norm_fwd(x: torch.Tensor, y: Optional[torch.Tensor] = None, gain: Optional[torch.Tensor] = None, *,
+                      y_gain: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, scale: float = 1.0, eps: float = 1e-6,
+                      x_out: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> ResidualNormResult:
+    """oapl_residual_norm_fwd: a block's output y, normed (y_gain), gated and scaled, added to the residual stream x, and the norm
+    (gain) of the sum.
+
+    x may be float32 where y is bfloat16.  gate: [d], or [T, d] for one a token.  x_out may be x.
+    """
+    shape, kind, per_token, gates, gpu = _residual_norm_setup(x, y, gain, y_gain, gate)
+    T, d = shape
+    if y is not None and x_out is None:
+        x_out = x.new_empty(shape)
+    if gain is not None and out is None:
+        out = x.new_empty(shape, dtype=kind)
+    if (y is None and x_out is not None) or (gain is None and out is not None):
+        raise ValueError("x_out goes with y, out with gain")
+    rc = lib().oapl_residual_norm_fwd(
+        _rows(x, "x", shape, x.dtype, gpu), None if y is None else _rows(y, "y", shape, kind, gpu), _flat(y_gain, kind, "y_gain", gpu),
+        gates, per_token, _flat(gain, kind, "gain", gpu), T, d, _dtype_code(x), _dtype_code(gain if y is None else y), scale, eps,
+        None if y is None else _rows(x_out, "x_out", shape, x.dtype, gpu), None if gain is None else _rows(out, "out", shape, kind, gpu),
+        _raw_stream(gpu))
+    if rc != 0:
+        raise OaplError(rc, "oapl_residual_norm_fwd")
+    return ResidualNormResult(x if y is None else x_out, out)
+
+
+class ResidualNormGrads(NamedTuple):
+    dx: torch.Tensor
+    dy: Optional[torch.Tensor]
+    dgain: Optional[torch.Tensor]     # [d] float32
+    dy_gain: Optional[torch.Tensor]   # [d] float32
+    dgate: Optional[torch.Tensor]     # [d] float32, or [T, d] in the gate's type
+    workspace: Optional[torch.Tensor]
+
+
+def residual_norm_bwd(x: torch.Tensor, y: Optional[torch.Tensor], dx_out: Optional[torch.Tensor], dout: Optional[torch.Tensor],
+                      gain: Optional[torch.Tensor] = None, *, y_gain: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                      scale: float = 1.0, eps: float = 1e-6, dx: Optional[torch.Tensor] = None, dy: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None) -> ResidualNormGrads:
+    """oapl_residual_norm_bwd: gradients of the stream in front of the block, of the block's output, the gains and the gate.
+
+    x is the stream behind the block, residual_norm_fwd's result; dx_out and dout are the gradients of its two results (dx_out may
+    be None, dout goes with gain).
+    """
+    shape, kind, per_token, gates, gpu = _residual_norm_setup(x, y, gain, y_gain, gate)
+    T, d = shape
+    if (gain is None) != (dout is None) or (y is None and dy is not None):
+        raise ValueError("dout goes with gain, dy with y")
+    dx = x.new_empty(shape) if dx is None else dx
+    if y is not None and dy is None:
+        dy = x.new_empty(shape, dtype=kind)
+    dgate = x.new_empty(shape, dtype=kind) if per_token else None
+    sums, ws, at = [None] * 3, None, [None] * 3
+    wanted = (gain is not None, y_gain is not None, gate is not None and not per_token)
+    if any(wanted):
+        ws = _scratch(lib().oapl_residual_norm_workspace_bytes(T, d), x, workspace, "oapl_residual_norm_workspace_bytes")
+        all_sums = x.new_empty((3, d), dtype=torch.float32)
+        base = all_sums.data_ptr()
+        sums = [s if w else None for s, w in zip(all_sums.unbind(), wanted)]
+        at = [base + 4 * d * i if w else None for i, w in enumerate(wanted)]
+    rc = lib().oapl_residual_norm_bwd(
+        _rows(x, "x", shape, x.dtype, gpu), None if y is None else _rows(y, "y", shape, kind, gpu), _flat(y_gain, kind, "y_gain", gpu),
+        gates, per_token, _flat(gain, kind, "gain", gpu), None if dx_out is None else _rows(dx_out, "dx_out", shape, x.dtype, gpu),
+        None if dout is None else _rows(dout, "dout", shape, kind, gpu), T, d, _dtype_code(x), _dtype_code(gain if y is None else y),
+        scale, eps, _rows(dx, "dx", shape, x.dtype, gpu), None if y is None else _rows(dy, "dy", shape, kind, gpu), at[0], at[1],
+        None if dgate is None else _rows(dgate, "dgate", shape, kind, gpu), at[2], None if ws is None else ws.data_ptr(),
+        0 if ws is None else ws.numel(), _raw_stream(gpu))
+    if rc != 0:
+        raise OaplError(rc, "oapl_residual_norm_bwd")
+    return ResidualNormGrads(dx, dy, sums[0], sums[1], sums[2] if dgate is None else dgate, ws)
+
+
+def clip_workspace_bytes(n_tensors: int) -> int:
+    """oapl_clip_workspace_bytes."""
+    return int(lib().oapl_clip_workspace_bytes(n_tensors))
+
+
+def _tensors(grads, out):
+    """The oapl_tensor list of dense tensors on the current GPU, and that GPU."""
+    if len(grads) == 0:
+        raise ValueError("there are no gradients")
+    gpu = _gpu_of(grads[0])
+    into = grads if out is None else out
+    if len(into) != len(grads):
+        raise ValueError("out must have one tensor a gradient")
+    items = (Tensor * len(grads))()
+    for item, g, o in zip(items, grads, into):
+        item.dtype = _dtype_code(g)
+        item.n = g.numel()
+        item.data = at = _flat(g, g.dtype, "a gradient", gpu)
+        if o is not g:
+            if o.shape != g.shape:
+                raise ValueError("out must have the gradients' shapes")
+            at = _flat(o, g.dtype, "out", gpu)
+        item.out = at
+    return items, gpu
+
+
+class GradNorm(NamedTuple):
+    norm: torch.Tensor            # [1] float32
+    workspace: Optional[torch.Tensor]
+
+
+def grad_norm(grads, *, workspace: Optional[torch.Tensor] = None) -> GradNorm:
+    """oapl_grad_norm: the norm of all gradients together (a list of contiguous tensors, float32 and bfloat16 mixed as they come)."""
+    items, gpu = _tensors(grads, None)
+    ws = _scratch(lib().oapl_clip_workspace_bytes(len(items)), grads[0], workspace, "oapl_clip_workspace_bytes")
+    norm = grads[0].new_empty(1, dtype=torch.float32)
+    rc = lib().oapl_grad_norm(items, len(items), norm.data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(gpu))
+    if rc != 0:
+        raise OaplError(rc, "oapl_grad_norm")
+    return GradNorm(norm, ws)
+
+
+def clip_grads(grads, max_norm: float, *, norm: Optional[torch.Tensor] = None, out=None,
+               workspace: Optional[torch.Tensor] = None) -> GradNorm:
+    """oapl_clip_grads: gradients scaled to max_norm where their common norm is larger (and finite), in place or into `out`.
+
+    Returns their norm before that.  `norm`: a norm to go by instead, [1] float32 (of gradients that are spread over GPUs, say).
+    """
+    items, gpu = _tensors(grads, out)
+    ws, given, made = None, None, None
+    if norm is None:
+        ws = _scratch(lib().oapl_clip_workspace_bytes(len(items)), grads[0], workspace, "oapl_clip_workspace_bytes")
+        norm = grads[0].new_empty(1, dtype=torch.float32)
+        made = norm.data_ptr()
+    else:
+        if norm.numel() != 1:
+            raise ValueError("norm must be one number")
+        given = _flat(norm, torch.float32, "norm", gpu)
+    rc = lib().oapl_clip_grads(items, len(items), max_norm, given, made, None if ws is None else ws.data_ptr(),
+                               0 if ws is None else ws.numel(), _raw_stream(gpu))
+    if rc != 0:
+        raise OaplError(rc, "oapl_clip_grads")
+    return GradNorm(norm, ws)
 
 
 def segmented_sum_f32(x: torch.Tensor, seq_offsets: torch.Tensor) -> torch.Tensor:

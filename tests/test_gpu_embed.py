@@ -1,0 +1,187 @@
+"""Embedding lookup and its gradient against the 64-bit oracle within its error bounds."""
+import pytest
+import torch
+
+from oracle import blocks_oracle as orc
+from paper_2602_19362_amd import oapl
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def _gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def _tokens(kind, T, V, seed=0):
+    """even: any; zipf: few very frequent ones; one: the same; each: all different as far as there are (shuffled); ends: the two last rows."""
+    g = _gen(seed)
+    if kind == "even":
+        return torch.randint(0, V, (T,), generator=g, device=DEV, dtype=torch.int32)
+    if kind == "zipf":
+        return (V * torch.rand(T, generator=g, device=DEV, dtype=torch.float64) ** 12).to(torch.int32).clamp_(max=V - 1)
+    if kind == "one":
+        return torch.full((T,), V // 2, device=DEV, dtype=torch.int32)
+    if kind == "ends":
+        return (V - 1 - torch.randint(0, min(2, V), (T,), generator=g, device=DEV)).to(torch.int32)
+    return (torch.randperm(T, generator=g, device=DEV) % V).to(torch.int32)
+
+
+def near(got, want, bound):
+    assert got.shape == want.shape
+    off = (got.to(torch.float64) - want).abs()
+    assert bool((off <= bound + 1e-300).all()), float((off / (bound + 1e-300)).max())
+
+
+@pytest.mark.parametrize("dtype, out, T, d, V, scale", [
+    ("bf16", "bf16", 1, 8, 1, 1.0), ("bf16", "bf16", 64, 4096, 1000, 1.0), ("bf16", "f32", 37, 520, 300, 22.6), ("f32", "f32", 5, 7, 3, -0.3),
+    ("f32", "bf16", 333, 65, 50, 3.0), ("bf16", "bf16", 3001, 1, 9, 0.1), ("f32", "f32", 70001, 12, 2000, 1.7), ("bf16", "bf16", 3, 8200, 5, 0.0)])
+def test_lookup(dtype, out, T, d, V, scale):
+    E = torch.randn(V, d, generator=_gen(1), device=DEV).to(DTYPES[dtype])
+    tokens = _tokens("even", T, V)
+    got = oapl.embed_fwd(E, tokens, scale=scale, out_dtype=DTYPES[out])
+    assert got.dtype == DTYPES[out]
+    near(got, *orc.embed(E, tokens, scale, DTYPES[out]))
+
+
+def test_lookup_from_and_into_parts_of_buffers():
+    """An embedding that starts at any element, rows of the output further apart than their channels and not aligned either."""
+    for dtype in DTYPES.values():
+        E = torch.randn(1 + 40 * 72, generator=_gen(2), device=DEV).to(dtype)[1:].view(40, 72)
+        tokens = _tokens("even", 29, 40)
+        wide = torch.full((29, 101), 7.0, device=DEV, dtype=dtype)
+        got = oapl.embed_fwd(E, tokens, scale=1.5, out=wide[:, 3:75])
+        assert got.data_ptr() == wide.data_ptr() + 3 * wide.element_size()
+        near(got, *orc.embed(E, tokens, 1.5, dtype))
+        assert bool((wide[:, :3] == 7).all()) and bool((wide[:, 75:] == 7).all())
+
+
+def test_lookup_outside_the_embedding_is_nan():
+    E = torch.randn(10, 24, generator=_gen(3), device=DEV)
+    tokens = torch.tensor([3, 10, -1, 9, 2 ** 31 - 1, -2 ** 31, 0], device=DEV, dtype=torch.int32)
+    got = oapl.embed_fwd(E, tokens)
+    assert got.isnan().all(1).tolist() == [False, True, True, False, True, True, False]
+    assert torch.equal(got[[0, 3, 6]], E[[3, 9, 0]])
+
+
+def test_lookup_without_tokens():
+    assert oapl.embed_fwd(torch.zeros(3, 4, device=DEV), torch.zeros(0, device=DEV, dtype=torch.int32)).shape == (0, 4)
+
+
+CASES = [("bf16", 1, 8, 1, "one"), ("bf16", 5, 64, 100, "even"), ("f32", 63, 20, 17, "zipf"), ("f32", 64, 20, 17, "one"), ("bf16", 65, 7, 64, "one"),
+         ("bf16", 1000, 264, 1544, "zipf"), ("f32", 1501, 768, 8192, "even"), ("bf16", 2048, 40, 2047, "each"), ("bf16", 2049, 9, 2048, "ends"),
+         ("f32", 5000, 33, 3000, "zipf"), ("bf16", 4097, 1024, 151936, "each"), ("bf16", 20000, 520, 700, "zipf"), ("f32", 20011, 8, 5, "even"),
+         ("bf16", 30000, 2056, 32000, "one"), ("f32", 300001, 4, 70000, "zipf"), ("bf16", 262145, 3, 1 << 21, "even"), ("f32", 9000, 1, 1 << 21, "ends")]
+
+
+@pytest.mark.parametrize("dtype, T, d, V, kind", CASES)
+def test_gradient(dtype, T, d, V, kind):
+    tokens = _tokens(kind, T, V)
+    dout = torch.randn(T, d, generator=_gen(4), device=DEV).to(DTYPES[dtype])
+    r = oapl.embed_bwd(dout, tokens, V, scale=0.7)
+    assert r.dE.dtype == torch.float32
+    want, bound = orc.embed_grads(dout, tokens, V, 0.7)
+    near(r.dE, want, bound)
+    assert oapl.read_device_status(r.workspace) == 0
+    # added to what is there
+    old = torch.randn(V, d, generator=_gen(5), device=DEV)
+    into = old.clone()
+    again = oapl.embed_bwd(dout, tokens, scale=0.7, dE=into, accumulate=True, workspace=r.workspace)
+    assert again.dE is into
+    want, bound = orc.embed_grads(dout, tokens, V, 0.7, old=old)
+    near(into, want, bound)
+    absent = torch.ones(V, dtype=torch.bool, device=DEV)
+    absent[tokens.long()] = False
+    assert torch.equal(into[absent], old[absent])
+    # the same bits again, on a workspace and a result that held something else
+    r.workspace.fill_(255)
+    third = oapl.embed_bwd(dout, tokens, scale=0.7, dE=torch.full_like(r.dE, torch.nan), workspace=r.workspace)
+    assert torch.equal(third.dE, r.dE)
+
+
+@pytest.mark.parametrize("T", [6, 3000])
+def test_gradient_of_tokens_outside_the_embedding(T):
+    tokens = _tokens("even", T, 50)
+    tokens[::3] = torch.tensor([50, -1, 2 ** 31 - 1, -2 ** 31], device=DEV, dtype=torch.int32).repeat(T)[:len(tokens[::3])]
+    dout = torch.randn(T, 24, generator=_gen(6), device=DEV)
+    dout[::3] = torch.nan
+    r = oapl.embed_bwd(dout, tokens, 50)
+    near(r.dE, *orc.embed_grads(dout, tokens, 50, 1.0))
+    assert oapl.read_device_status(r.workspace) == 9
+    r = oapl.embed_bwd(dout, tokens.clamp(0, 49), 50, workspace=r.workspace)
+    assert oapl.read_device_status(r.workspace) == 0
+
+
+@pytest.mark.parametrize("T", [7, 2500])
+def test_gradient_from_and_into_parts_of_buffers(T):
+    for dtype in DTYPES.values():
+        wide = torch.randn(T, 91, generator=_gen(7), device=DEV).to(dtype)
+        tokens = _tokens("zipf", T, 60)
+        flat = torch.full((2 + 60 * 73,), 5.0, device=DEV)
+        r = oapl.embed_bwd(wide[:, 5:78], tokens, dE=flat[1:-1].view(60, 73))
+        near(r.dE, *orc.embed_grads(wide[:, 5:78], tokens, 60, 1.0))
+        assert flat[0] == 5 and flat[-1] == 5
+        # one row for all tokens
+        row = wide[:1, 5:78].expand(T, 73)
+        near(oapl.embed_bwd(row, tokens, 60).dE, *orc.embed_grads(row, tokens, 60, 1.0))
+
+
+def test_what_is_not_finite_stays_in_its_row():
+    tokens = _tokens("zipf", 4000, 500)
+    dout = torch.randn(4000, 16, generator=_gen(8), device=DEV)
+    dout[17, 3], dout[1234, 9] = torch.inf, torch.nan
+    got = oapl.embed_bwd(dout, tokens, 500).dE
+    want = torch.ones_like(got, dtype=torch.bool)
+    want[tokens[17], 3], want[tokens[1234], 9] = False, False
+    assert torch.equal(got.isfinite(), want)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_gradient_without_tokens(accumulate):
+    dE = torch.full((30, 12), 3.0, device=DEV)
+    oapl.embed_bwd(torch.zeros(0, 12, device=DEV), torch.zeros(0, device=DEV, dtype=torch.int32), dE=dE, accumulate=accumulate)
+    assert bool((dE == (3 if accumulate else 0)).all())
+
+
+def test_the_same_weights_at_both_ends():
+    """A tied embedding's gradient: the head's dW with the lookup's rows added to it."""
+    W = (torch.randn(600, 64, generator=_gen(9), device=DEV) / 8).bfloat16()
+    tokens = _tokens("zipf", 200, 600)
+    H = torch.randn(200, 64, generator=_gen(10), device=DEV).bfloat16()
+    offsets = torch.tensor([0, 120, 200], device=DEV)
+    r = oapl.loss_fwd_bwd(H, W, tokens, torch.full((200,), -6.0, device=DEV), offsets, torch.tensor([1.0, 0.0], device=DEV),
+                          torch.zeros(2, dtype=torch.int32, device=DEV), 1, 0.5)
+    before = r.dW.clone()
+    oapl.embed_bwd(r.dH, tokens, dE=r.dW, accumulate=True)
+    near(r.dW, *orc.embed_grads(r.dH, tokens, 600, 1.0, old=before))
+
+
+def test_refusals():
+    E, t = torch.zeros(5, 8, device=DEV), torch.zeros(3, device=DEV, dtype=torch.int32)
+    with pytest.raises(TypeError):
+        oapl.embed_fwd(E, t.long())
+    with pytest.raises(TypeError):
+        oapl.embed_fwd(E.half(), t)
+    with pytest.raises(ValueError):
+        oapl.embed_fwd(E[:, ::2], t)
+    with pytest.raises(ValueError):
+        oapl.embed_fwd(E, t, out=torch.zeros(3, 9, device=DEV))
+    with pytest.raises(TypeError):
+        oapl.embed_fwd(E, t, out=torch.zeros(3, 8, device=DEV), out_dtype=torch.bfloat16)
+    with pytest.raises(oapl.OaplError):
+        oapl.embed_fwd(E, t, scale=float("inf"))
+    with pytest.raises(oapl.OaplError):
+        oapl.embed_fwd(E, t, out=torch.zeros(1, 8, device=DEV).expand(3, 8))
+    with pytest.raises(ValueError):
+        oapl.embed_bwd(E, t, 5)
+    with pytest.raises(ValueError):
+        oapl.embed_bwd(E[:3], t)
+    with pytest.raises(ValueError):
+        oapl.embed_bwd(E[:3], t, 5, accumulate=True)
+    with pytest.raises(ValueError):
+        oapl.embed_bwd(E[:3], t, 5, dE=torch.zeros(6, 8, device=DEV))
+    with pytest.raises(TypeError):
+        oapl.embed_bwd(E[:3], t, dE=torch.zeros(5, 8, device=DEV).bfloat16())
+    with pytest.raises(oapl.OaplError):
+        oapl.embed_bwd(E[:3], t, 5, workspace=torch.zeros(256, device=DEV, dtype=torch.uint8))
