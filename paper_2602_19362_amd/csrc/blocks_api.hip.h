@@ -12,6 +12,7 @@
 namespace oapl {
 
 constexpr int64_t kMaxRows = 65535 * 256;              // the head's limit
+constexpr int64_t kMaxElements = (int64_t)1 << 42;     // of all tensors of a call: 2^31 chunks
 constexpr int kMaxNormWidth = 16384;                   // 1024 lanes with two pieces of a row each
 
 // A rows argument of n rows of d channels.  The stride of a single row is not looked at.  `written` rows must not overlap.
@@ -32,6 +33,7 @@ static bool element_aligned(const void* p, int dtype) { return (uintptr_t)p % es
 
 // ---------------------------------------------------------------------------------------------------------------- embedding
 struct EmbedPlan {
+  bool few = false;
   int bits = 1, items = 1, blocks = 1, tile = 1, tiles = 0;
   size_t off_keys[2], off_places[2], off_counts[2], off_present = 0, off_partials = 0, total = 0;
 };
@@ -42,53 +44,92 @@ static bool embed_sizes_ok(int64_t T, int d, int V) {
 
 static bool embed_plan(EmbedPlan& p, int64_t T, int d, int V) {
   if (!embed_sizes_ok(T, d, V)) return false;
+  p.total = kStatusWords * sizeof(int);
+  const auto take = [&](int64_t bytes) {
+    const size_t was = p.total;
+    p.total += (size_t)round_up(bytes, 256);
+    return was;
+  };
+  p.off_keys[1] = take(T * 4), p.off_places[1] = take(T * 4);
+  p.few = T <= kFewTokens;
+  if (p.few) return true;
   while (((int64_t)1 << (2 * p.bits)) <= V) ++p.bits;      // ids 0 .. V
   p.items = T <= 128 * kSortThreads * 2 ? 2 : 8;
   p.blocks = (int)std::max<int64_t>(1, (T + (int64_t)kSortThreads * p.items - 1) / (kSortThreads * p.items));
-  p.tile = 64;
+  // 32 / 64 / 128 rows a tile, us for the whole call in bf16: d = 4096, V = 1544: 5000 tokens 44 / 55 / 77, 10000 56 / 69 / 96, 20000 87 / 83 / 113, 80000 211 / 206 /
+  // 229; d = 1024 20000 46 / 56 / 77, 40000 58 / 68 / 87, 80000 95 / 92 / 119; d = 4096, V = 151936 140897 785 / 772 / 788.
+  p.tile = T * ((d + 1023) / 1024) <= 1 << 16 ? 32 : 64;
   p.tiles = (int)((T + p.tile - 1) / p.tile);
-  size_t at = kStatusWords * sizeof(int);
-  const auto take = [&](int64_t bytes) {
-    const size_t was = at;
-    at += (size_t)round_up(bytes, 256);
-    return was;
-  };
-  for (int i = 0; i < 2; ++i) {
-    p.off_keys[i] = take(T * 4), p.off_places[i] = take(T * 4);
-    p.off_counts[i] = take(((int64_t)p.blocks << p.bits) * 4);
-  }
+  p.off_keys[0] = take(T * 4), p.off_places[0] = take(T * 4);
+  for (int i = 0; i < 2; ++i) p.off_counts[i] = take(((int64_t)p.blocks << p.bits) * 4);
   p.off_present = take(V);
   p.off_partials = take((int64_t)p.tiles * 2 * d * 4);
-  p.total = at;
   return true;
+}
+
+// So many workgroups, and what is missing to whole rows of `most`: HIP takes fewer than 2^32 threads in a dimension.
+static dim3 wide_grid(int64_t n, int64_t most) {
+  return dim3((unsigned)std::min(n, most), (unsigned)((n + most - 1) / most));
+}
+
+// Accesses of so many bytes go past the caches: the memory-side one holds 256 MiB.
+static bool past_caches(int64_t bytes) { return bytes > (int64_t)256 << 20; }
+
+template <class TE, class T>
+static int launch_embed_fwd(EmbedArgs a, hipStream_t st) {
+  constexpr int W = sizeof(TE) + sizeof(T) == 4 ? 8 : 4;
+  const auto launch = [&](auto pieces, auto once) {
+    constexpr int PIECES = pieces;
+    constexpr bool ONCE = once;
+    a.slices = grid1d(a.d, 64 * W * PIECES);
+    k_embed_fwd<TE, T, W, PIECES, ONCE><<<wide_grid((a.T * a.slices + 3) / 4, 1 << 23), 256, 0, st>>>(a);
+  };
+  if (a.T * grid1d(a.d, 64 * W) >= (int64_t)1 << 31) return OAPL_ERR_SHAPE;      // 2 TB and more
+  const auto by_size = [&](auto once) {
+    // 140000 rows of 256 channels in bf16, one piece a wavefront / two: 27 / 35 us; 20000 of 520 9.5 / 9.1
+    if (a.d <= 64 * W) launch(std::integral_constant<int, 1>{}, once);
+    else launch(std::integral_constant<int, 2>{}, once);
+  };
+  if (past_caches(a.T * a.d * (int64_t)sizeof(T))) by_size(std::true_type{});
+  else by_size(std::false_type{});
+  OAPL_LAUNCH_CHECK();
+  return OAPL_OK;
 }
 
 template <int ITEMS>
 static int launch_embed_sort(const SortArgs& a, hipStream_t st) {
-  const int bins = 1 << a.bits, bytes = kSortThreads / 64 * bins * 4;
+  const int bins = 1 << a.bits, bytes = (kSortThreads / 64 + 2) * bins * 4;
   if (bytes > 48 * 1024 && (!allow_big_lds(k_embed_place<0, ITEMS>, bytes) || !allow_big_lds(k_embed_place<1, ITEMS>, bytes)))
     return OAPL_ERR_HIP;
   k_embed_count<ITEMS><<<a.blocks, kSortThreads, bins * 4, st>>>(a);
   OAPL_LAUNCH_CHECK();
   k_embed_place<0, ITEMS><<<a.blocks, kSortThreads, bytes, st>>>(a);
   OAPL_LAUNCH_CHECK();
-  k_embed_place<1, ITEMS><<<a.blocks, kSortThreads, bytes, st>>>(a);
+  const int64_t clear = a.dE ? (int64_t)grid1d(a.V, kSortThreads / 64) * grid1d(a.d, 1024) : 0;
+  k_embed_place<1, ITEMS><<<wide_grid(a.blocks + clear, 1 << 21), kSortThreads, bytes, st>>>(a);
   OAPL_LAUNCH_CHECK();
   return OAPL_OK;
 }
 
 // ---------------------------------------------------------------------------------------------------------------- residual stream
-// How the lanes of a workgroup divide rows of d channels; f(threads of a row, pieces of eight channels a thread).
-template <class F>
-static int by_width(int d, F f) {
-  if (d <= 512) return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
-  if (d <= 1024) return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
-  if (d <= 2048) return f(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
-  if (d <= 4096) return f(std::integral_constant<int, 256>{}, std::integral_constant<int, 2>{});
-  if (d <= 8192) return f(std::integral_constant<int, 512>{}, std::integral_constant<int, 2>{});
-  return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
+// How many lanes hold a row of d channels, W in a piece: f(lanes, pieces a lane).  Eight channels a lane, 16 where there are no more lanes:
+// 16411 rows of 4096 in bf16 with 8 / 16 / 32 / 64 forward 92 / 97 / 107 / 158 us (workgroups that take row after row 101 .. 111), 3000 of 8192
+// 36 / 40 / 47 / 66, 8000 of 4096 in fp32 97 / 102 / 121 / 164.
+template <int W, class F>
+static void by_width(int d, F f) {
+  constexpr std::integral_constant<int, 8 / W> eight{};
+  if (d <= 16 * 8) return f(std::integral_constant<int, 16>{}, eight);
+  if (d <= 64 * 8) return f(std::integral_constant<int, 64>{}, eight);
+  if (d <= 128 * 8) return f(std::integral_constant<int, 128>{}, eight);
+  if (d <= 256 * 8) return f(std::integral_constant<int, 256>{}, eight);
+  if (d <= 512 * 8) return f(std::integral_constant<int, 512>{}, eight);
+  if (d <= 1024 * 8) return f(std::integral_constant<int, 1024>{}, eight);
+  return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 16 / W>{});
 }
-static int norm_rows_of_a_workgroup(int d) { return d <= 1024 ? 4 : 1; }
+// Lanes of a workgroup, and the rows they hold.
+static int norm_lanes(int d) { return d <= 512 || (d > 1024 && d <= 2048) ? 256 : d <= 1024 ? 128 : d <= 4096 ? 512 : 1024; }
+static int norm_rows(int d) { return d <= 128 ? 16 : d <= 512 ? 4 : 1; }
+static int64_t norm_workgroups(int64_t T, int d) { return (T + norm_rows(d) - 1) / norm_rows(d); }
 
 // f(null pointer to the residual stream's type, ... to the block's).
 template <class F>
@@ -98,12 +139,10 @@ static int by_types(int x_dtype, int dtype, F f) {
   return f((float*)nullptr, (float*)nullptr);
 }
 
-static unsigned norm_fwd_grid(int64_t T, int d) {
-  return (unsigned)std::min<int64_t>((T + norm_rows_of_a_workgroup(d) - 1) / norm_rows_of_a_workgroup(d), 1 << 16);
-}
-// Backwards every workgroup has sums of its own.
+// Backwards every workgroup has sums of its own, and as many rows as any other.  Workgroups of 512 / 768 / 1024 lanes a compute unit, 16411 rows in
+// bf16: d = 4096 154 / 174 / 165 us, 2048 81 / 87 / 89 (256 lanes: 124), 1024 45.8 / 46.7 / 47.0 (70), 512 23.2 / 23.5 / 23.8 (31).
 static unsigned norm_bwd_grid(int64_t T, int d) {
-  return (unsigned)std::min<int64_t>((T + norm_rows_of_a_workgroup(d) - 1) / norm_rows_of_a_workgroup(d), 512);
+  return (unsigned)std::min<int64_t>(norm_workgroups(T, d), std::max(256, 256 * 512 / norm_lanes(d)));
 }
 
 static int residual_norm_args(ResidualNormArgs& a, const oapl_rows* x, const oapl_rows* y, const void* y_gain, const oapl_rows* gate,
@@ -136,7 +175,12 @@ static int take_rows(Rows& to, const oapl_rows* x, int64_t T, int d, int dtype, 
 }
 
 // ---------------------------------------------------------------------------------------------------------------- clipping
-static int clip_launches(int64_t n) { return (int)((n + kClipTensors - 1) / kClipTensors); }
+struct ClipPlan {
+  int chunk = 0, launches = 0;
+  int64_t elements = 0;
+  bool large = false;              // a launch for the norm between
+  bool load_once = false, store_once = false;
+};
 
 // The tensors' memory: what is written overlaps nothing but what it is the result of.
 static int check_overlaps(const oapl_tensor* tensors, int n) {
@@ -159,46 +203,62 @@ static int check_overlaps(const oapl_tensor* tensors, int n) {
   return OAPL_OK;
 }
 
-static int check_tensors(const oapl_tensor* tensors, int n, bool written) {
+static int clip_plan(ClipPlan& p, const oapl_tensor* tensors, int n, bool written) {
   if (n < 0 || n > (1 << 20)) return OAPL_ERR_SHAPE;
   if (n > 0 && !tensors) return OAPL_ERR_NULL;
-  int64_t chunks = 0;
+  int64_t read = 0, apart = 0;
   for (int i = 0; i < n; ++i) {
     const oapl_tensor& t = tensors[i];
     if (!dtype_ok(t.dtype)) return OAPL_ERR_DTYPE;
-    if (t.n < 0 || t.n > (int64_t)1 << 44) return OAPL_ERR_SHAPE;
-    chunks += (t.n + kClipChunk - 1) / kClipChunk;
-    if (chunks >= (int64_t)1 << 31) return OAPL_ERR_SHAPE;
+    if (t.n < 0 || t.n > kMaxElements - p.elements) return OAPL_ERR_SHAPE;
+    p.elements += t.n;
+    read += t.n * (int64_t)esize(t.dtype);
+    if (t.out != t.data) apart += t.n * (int64_t)esize(t.dtype);
     if (t.n == 0) continue;
     if (!t.data || (written && !t.out)) return OAPL_ERR_NULL;
     if (!element_aligned(t.data, t.dtype) || (written && !element_aligned(t.out, t.dtype))) return OAPL_ERR_ALIGN;
   }
+  // Small sets are a launch for the squares and one for the scaling, whose workgroups all add up the sums; of larger ones a workgroup has one
+  // chunk, so that memory sees them in order, and the norm is a launch of its own.  Chunks of 2048 / 4096 / 8192 / 16384 elements: 98 tensors of 6.3 GB 3351 /
+  // 3352 / 3412 / 3462 us (workgroups that take chunk after chunk 3906), of 1.9 GB 1347 / 1253 / 1285 / 1316.
+  p.large = p.elements > ((int64_t)16 << 20);
+  p.chunk = p.large ? 4096 : 2048;
+  // What the caches cannot hold goes past them: 6.3 GB 3352 -> 3247 us with loads and stores of the scaling, 3239 with the loads for the squares; 135 MB into
+  // other tensors 191 -> 162 with the stores.
+  p.load_once = past_caches(read), p.store_once = past_caches(read + (written ? apart : 0));
+  p.launches = (n + kClipTensors - 1) / kClipTensors;
   return OAPL_OK;
 }
 
-// One launch for every kClipTensors tensors; f(arguments, workgroups).
+// One launch for every kClipTensors tensors, the last ones first where `back`: f(arguments).
 template <class F>
-static int clip_batches(const oapl_tensor* tensors, int n, ClipArgs& a, F f) {
-  for (int at = 0; at < n; at += kClipTensors) {
+static int clip_batches(const ClipPlan& p, const oapl_tensor* tensors, int n, bool back, ClipArgs& a, F f) {
+  a.chunk = p.chunk;
+  for (int k = 0; k < p.launches; ++k) {
+    const int batch = back ? p.launches - 1 - k : k, at = batch * kClipTensors;
     a.count = std::min(kClipTensors, n - at);
-    int64_t chunks = 0;
+    a.mine = batch * kClipGrid;
+    a.chunks = 0;
     for (int i = 0; i < a.count; ++i) {
       const oapl_tensor& t = tensors[at + i];
-      a.t[i] = ClipTensor{t.data, t.out, t.n, (uint32_t)chunks, t.dtype};
-      chunks += (t.n + kClipChunk - 1) / kClipChunk;
+      a.t[i] = ClipTensor{t.data, t.out, t.n, a.chunks, t.dtype == OAPL_BF16};
+      a.chunks += (uint32_t)((t.n + p.chunk - 1) / p.chunk);
     }
-    a.chunks = (uint32_t)chunks;
-    a.mine = at / kClipTensors * kClipGrid;
-    if (int rc = f(a, kClipGrid)) return rc;
+    f(a);
+    OAPL_LAUNCH_CHECK();
   }
   return OAPL_OK;
 }
 
-static int clip_squares(const oapl_tensor* tensors, int n, ClipArgs& a, hipStream_t st) {
-  return clip_batches(tensors, n, a, [&](const ClipArgs& b, int grid) -> int {
-    k_grad_squares<<<grid, 256, 0, st>>>(b);
-    OAPL_LAUNCH_CHECK();
-    return OAPL_OK;
+static int clip_squares(const ClipPlan& p, const oapl_tensor* tensors, int n, void* workspace, ClipArgs& a, hipStream_t st) {
+  a.sum = (double*)workspace;
+  // one launch: as many sums as workgroups; more of them: as many each as there may be
+  a.sums = p.launches * kClipGrid;
+  return clip_batches(p, tensors, n, false, a, [&](ClipArgs& b) {
+    if (p.launches == 1) b.sums = (int)std::min<int64_t>(kClipGrid, std::max(b.chunks, 1u));
+    const int grid = p.launches == 1 ? b.sums : kClipGrid;
+    if (p.load_once) k_grad_squares<true><<<grid, 256, 0, st>>>(b);
+    else k_grad_squares<false><<<grid, 256, 0, st>>>(b);
   });
 }
 
@@ -218,14 +278,11 @@ int32_t oapl_embed_fwd(const void* E, const int32_t* tokens, int64_t T, int32_t 
   EmbedArgs a{E, tokens, {}, T, d, V, scale};
   if (int rc = take_rows(a.out, out, T, d, out_dtype, true)) return rc;
   if (T == 0) return OAPL_OK;
-  const dim3 grid((unsigned)std::min<int64_t>((T + 3) / 4, 1 << 16), grid1d(d, 512));
   hipStream_t st = (hipStream_t)stream;
-  if (dtype == OAPL_BF16 && out_dtype == OAPL_BF16) k_embed_fwd<bf16_t, bf16_t><<<grid, 256, 0, st>>>(a);
-  else if (dtype == OAPL_BF16) k_embed_fwd<bf16_t, float><<<grid, 256, 0, st>>>(a);
-  else if (out_dtype == OAPL_BF16) k_embed_fwd<float, bf16_t><<<grid, 256, 0, st>>>(a);
-  else k_embed_fwd<float, float><<<grid, 256, 0, st>>>(a);
-  OAPL_LAUNCH_CHECK();
-  return OAPL_OK;
+  if (dtype == OAPL_BF16 && out_dtype == OAPL_BF16) return launch_embed_fwd<bf16_t, bf16_t>(a, st);
+  if (dtype == OAPL_BF16) return launch_embed_fwd<bf16_t, float>(a, st);
+  if (out_dtype == OAPL_BF16) return launch_embed_fwd<float, bf16_t>(a, st);
+  return launch_embed_fwd<float, float>(a, st);
 }
 
 size_t oapl_embed_workspace_bytes(int64_t T, int32_t d, int32_t V) {
@@ -246,29 +303,42 @@ int32_t oapl_embed_bwd(const oapl_rows* dout, const int32_t* tokens, int64_t T, 
   if (!workspace_ok(workspace, workspace_bytes, p.total)) return OAPL_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)stream;
   char* ws = (char*)workspace;
+  a.dE = dE, a.T = T, a.d = d, a.V = V, a.scale = scale, a.add = accumulate != 0;
+  int32_t* const keys = (int32_t*)(ws + p.off_keys[1]), * const places = (int32_t*)(ws + p.off_places[1]);
+  a.keys = keys, a.places = places;
+  if (p.few) {
+    const int sorters = (int)std::max<int64_t>(1, (T + kRankTokens - 1) / kRankTokens);
+    const int64_t clear = accumulate ? 0 : ((int64_t)V * d + 1023) / 1024;
+    k_embed_rank<<<wide_grid(sorters + clear, 1 << 23), 256, 0, st>>>(a, tokens, keys, places, (int*)ws, sorters);
+    OAPL_LAUNCH_CHECK();
+    if (T == 0) return OAPL_OK;
+    const dim3 runs(grid1d(T, 32), grid1d(d, 256));
+    if (dtype == OAPL_BF16) k_embed_runs<bf16_t><<<runs, 256, 0, st>>>(a);
+    else k_embed_runs<float><<<runs, 256, 0, st>>>(a);
+    OAPL_LAUNCH_CHECK();
+    return OAPL_OK;
+  }
   SortArgs s = {};
   s.tokens = tokens;
-  for (int i = 0; i < 2; ++i) {
-    s.keys[i] = (int32_t*)(ws + p.off_keys[i]), s.places[i] = (int32_t*)(ws + p.off_places[i]);
-    s.counts[i] = (int32_t*)(ws + p.off_counts[i]);
-  }
+  s.keys[0] = (int32_t*)(ws + p.off_keys[0]), s.places[0] = (int32_t*)(ws + p.off_places[0]);
+  s.keys[1] = keys, s.places[1] = places;
+  for (int i = 0; i < 2; ++i) s.counts[i] = (int32_t*)(ws + p.off_counts[i]);
   s.present = (uint8_t*)(ws + p.off_present), s.status = (int*)ws;
-  s.T = T, s.V = V, s.bits = p.bits, s.blocks = p.blocks;
+  s.dE = accumulate ? nullptr : dE;
+  s.T = T, s.V = V, s.d = d, s.bits = p.bits, s.blocks = p.blocks;
   if (int rc = p.items == 2 ? launch_embed_sort<2>(s, st) : launch_embed_sort<8>(s, st)) return rc;
-  a.keys = s.keys[1], a.places = s.places[1], a.present = s.present;
-  a.dE = dE, a.partials = (float*)(ws + p.off_partials);
-  a.T = T, a.d = d, a.V = V, a.tile = p.tile, a.tiles = p.tiles, a.scale = scale, a.add = accumulate != 0;
-  const unsigned fill = accumulate ? 0 : (unsigned)std::min(V, 4096);
-  if (p.tiles + fill > 0) {
-    const dim3 grid(p.tiles + fill, grid1d(d, 2048));
-    if (dtype == OAPL_BF16) k_embed_sum<bf16_t><<<grid, 256, 0, st>>>(a);
-    else k_embed_sum<float><<<grid, 256, 0, st>>>(a);
-    OAPL_LAUNCH_CHECK();
-  }
-  if (p.tiles > 1) {
-    k_embed_join<<<dim3(p.tiles, grid1d(d, 256)), 256, 0, st>>>(a);
-    OAPL_LAUNCH_CHECK();
-  }
+  a.partials = (float*)(ws + p.off_partials);
+  a.tile = p.tile, a.tiles = p.tiles, a.slices = (int)grid1d(d, 1024);
+  const unsigned grid = (unsigned)p.tiles * a.slices;
+  // Rows that the caches do not hold go past them: 140897 tokens, d = 4096 (1.15 GB) 785 -> 771 us; 4096 at V = 1544 (34 MB) 46 -> 60.
+  const bool once = past_caches(T * d * (int64_t)esize(dtype));
+  if (dtype == OAPL_BF16 && once) k_embed_sum<bf16_t, true><<<grid, 256, 0, st>>>(a);
+  else if (dtype == OAPL_BF16) k_embed_sum<bf16_t, false><<<grid, 256, 0, st>>>(a);
+  else if (once) k_embed_sum<float, true><<<grid, 256, 0, st>>>(a);
+  else k_embed_sum<float, false><<<grid, 256, 0, st>>>(a);
+  OAPL_LAUNCH_CHECK();
+  k_embed_join<<<dim3(grid1d(p.tiles, kJoinTiles), grid1d(d, 256)), 64 * kJoinParts, 0, st>>>(a);
+  OAPL_LAUNCH_CHECK();
   return OAPL_OK;
 }
 
@@ -282,12 +352,14 @@ int32_t oapl_residual_norm_fwd(const oapl_rows* x, const oapl_rows* y, const voi
   if (int rc = out ? take_rows(a.out, out, T, d, dtype, true) : OAPL_OK) return rc;
   if (T == 0) return OAPL_OK;
   by_types(x_dtype, dtype, [&](auto* tx, auto* t) {
-    return by_width(d, [&](auto threads, auto pieces) {
+    typedef std::remove_pointer_t<decltype(tx)> TX;
+    typedef std::remove_pointer_t<decltype(t)> TY;
+    constexpr int W = sizeof(TX) == 2 ? 8 : 4;
+    by_width<W>(d, [&](auto threads, auto pieces) {
       constexpr int THREADS = threads, PIECES = pieces;
-      k_residual_norm_fwd<std::remove_pointer_t<decltype(tx)>, std::remove_pointer_t<decltype(t)>, THREADS, PIECES>
-          <<<norm_fwd_grid(T, d), std::max(256, THREADS), 0, (hipStream_t)stream>>>(a);
-      return 0;
+      k_residual_norm_fwd<TX, TY, W, THREADS, PIECES><<<(unsigned)norm_workgroups(T, d), norm_lanes(d), 0, (hipStream_t)stream>>>(a);
     });
+    return 0;
   });
   OAPL_LAUNCH_CHECK();
   return OAPL_OK;
@@ -295,7 +367,7 @@ int32_t oapl_residual_norm_fwd(const oapl_rows* x, const oapl_rows* y, const voi
 
 size_t oapl_residual_norm_workspace_bytes(int64_t T, int32_t d) {
   if (T < 0 || T > kMaxRows || d < 1 || d > kMaxNormWidth) return 0;
-  return (size_t)round_up((int64_t)norm_bwd_grid(T, d) * norm_rows_of_a_workgroup(d) * 2 * d * (int64_t)sizeof(float) + 1, 256);
+  return (size_t)round_up((int64_t)norm_bwd_grid(T, d) * 2 * d * (int64_t)sizeof(float) + 1, 256);
 }
 
 int32_t oapl_residual_norm_bwd(const oapl_rows* x, const oapl_rows* y, const void* y_gain, const oapl_rows* gate, int32_t gate_per_token,
@@ -323,15 +395,15 @@ int32_t oapl_residual_norm_bwd(const oapl_rows* x, const oapl_rows* y, const voi
     typedef std::remove_pointer_t<decltype(tx)> TX;
     typedef std::remove_pointer_t<decltype(t)> TY;
     if (T > 0) {
-      by_width(d, [&](auto threads, auto pieces) {
+      constexpr int W = sizeof(TX) == 2 ? 8 : 4;
+      by_width<W>(d, [&](auto threads, auto pieces) {
         constexpr int THREADS = threads, PIECES = pieces;
-        k_residual_norm_bwd<TX, TY, THREADS, PIECES><<<grid, std::max(256, THREADS), 0, st>>>(a);
-        return 0;
+        k_residual_norm_bwd<TX, TY, W, THREADS, PIECES><<<grid, norm_lanes(d), 0, st>>>(a);
       });
       OAPL_LAUNCH_CHECK();
     }
     if (sums) {
-      k_norm_gain_grads<TY><<<grid1d(2 * d, 16), 1024, 0, st>>>(a.partials, (int)grid * norm_rows_of_a_workgroup(d), d,
+      k_norm_gain_grads<TY><<<grid1d(2 * d, 16), 1024, 0, st>>>(a.partials, (int)grid, d,
                                                                shared ? (const TY*)gate->data : nullptr, (const TY*)y_gain,
                                                                gain ? dgain : nullptr, y_gain ? dy_gain : nullptr, shared ? dgate : nullptr);
       OAPL_LAUNCH_CHECK();
@@ -342,19 +414,19 @@ int32_t oapl_residual_norm_bwd(const oapl_rows* x, const oapl_rows* y, const voi
 
 size_t oapl_clip_workspace_bytes(int32_t n_tensors) {
   if (n_tensors < 0 || n_tensors > (1 << 20)) return 0;
-  return (size_t)std::max(1, clip_launches(n_tensors)) * kClipGrid * sizeof(double);
+  return (size_t)std::max(1, (n_tensors + kClipTensors - 1) / kClipTensors) * kClipGrid * sizeof(double);
 }
 
 int32_t oapl_grad_norm(const oapl_tensor* tensors, int32_t n_tensors, float* norm, void* workspace, size_t workspace_bytes,
                        void* stream) {
-  if (int rc = check_tensors(tensors, n_tensors, false)) return rc;
+  ClipPlan p;
+  if (int rc = clip_plan(p, tensors, n_tensors, false)) return rc;
   if (!norm) return OAPL_ERR_NULL;
   if (!element_aligned(norm, OAPL_F32)) return OAPL_ERR_ALIGN;
   if (!workspace_ok(workspace, workspace_bytes, oapl_clip_workspace_bytes(n_tensors))) return OAPL_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)stream;
   ClipArgs a = {};
-  a.sum = (double*)workspace, a.sums = clip_launches(n_tensors) * kClipGrid;
-  if (int rc = clip_squares(tensors, n_tensors, a, st)) return rc;
+  if (int rc = clip_squares(p, tensors, n_tensors, workspace, a, st)) return rc;
   a.norm_out = norm;
   k_grad_norm<<<1, 256, 0, st>>>(a);
   OAPL_LAUNCH_CHECK();
@@ -363,7 +435,8 @@ int32_t oapl_grad_norm(const oapl_tensor* tensors, int32_t n_tensors, float* nor
 
 int32_t oapl_clip_grads(const oapl_tensor* tensors, int32_t n_tensors, float max_norm, const float* norm_given, float* norm_out,
                         void* workspace, size_t workspace_bytes, void* stream) {
-  if (int rc = check_tensors(tensors, n_tensors, true)) return rc;
+  ClipPlan p;
+  if (int rc = clip_plan(p, tensors, n_tensors, true)) return rc;
   if (!(max_norm >= 0.f) || !isfinite(max_norm)) return OAPL_ERR_BETA;
   if ((norm_given == nullptr) == (norm_out == nullptr)) return OAPL_ERR_NULL;
   if (!element_aligned(norm_given, OAPL_F32) || !element_aligned(norm_out, OAPL_F32)) return OAPL_ERR_ALIGN;
@@ -373,15 +446,21 @@ int32_t oapl_clip_grads(const oapl_tensor* tensors, int32_t n_tensors, float max
   ClipArgs a = {};
   a.max_norm = max_norm, a.norm = norm_given;
   if (!norm_given) {
-    if (n_tensors == 0) return oapl_grad_norm(tensors, 0, norm_out, workspace, workspace_bytes, stream);
-    a.sum = (double*)workspace, a.sums = clip_launches(n_tensors) * kClipGrid;
-    if (int rc = clip_squares(tensors, n_tensors, a, st)) return rc;
+    if (int rc = clip_squares(p, tensors, n_tensors, workspace, a, st)) return rc;
+    a.norm_out = norm_out;
+    if (p.large || p.launches != 1) {
+      // the norm once, for workgroups that have little else to do
+      k_grad_norm<<<1, 256, 0, st>>>(a);
+      OAPL_LAUNCH_CHECK();
+      a.norm = norm_out, a.norm_out = nullptr;
+    }
   }
-  a.norm_out = norm_out;
-  return clip_batches(tensors, n_tensors, a, [&](const ClipArgs& b, int grid) -> int {
-    k_grad_scale<<<grid, 256, 0, st>>>(b);
-    OAPL_LAUNCH_CHECK();
-    return OAPL_OK;
+  return clip_batches(p, tensors, n_tensors, true, a, [&](const ClipArgs& b) {
+    if (b.chunks == 0 && !b.norm_out) return;
+    const dim3 grid = wide_grid(std::max<int64_t>(1, b.chunks), 1 << 23);
+    if (p.load_once) k_grad_scale<true, true><<<grid, 256, 0, st>>>(b);
+    else if (p.store_once) k_grad_scale<false, true><<<grid, 256, 0, st>>>(b);
+    else k_grad_scale<false, false><<<grid, 256, 0, st>>>(b);
   });
 }
 

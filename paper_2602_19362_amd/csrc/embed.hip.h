@@ -2,9 +2,10 @@
 //
 //   out_t = scale E[tok_t],      dE[v] = scale sum over t with tok_t = v of dout_t
 //
-// Bound by memory.  The gradient's sums have a fixed order: tokens are sorted by id (stably, so by position among equals), the sorted
-// positions cut into tiles of equal length, so that a frequent token is shared by many workgroups; what a tile has of a token that
-// reaches over its ends goes into the workspace and is added up by a second launch, tile by tile.
+// Bound by memory.  The gradient's sums have a fixed order.  Few tokens: workgroups that have a share of dE's rows look through all of them.
+// Many: they are sorted by id (stably, so by position among equals), the sorted positions cut into tiles of equal length, so that a frequent
+// token is shared by many workgroups; what a tile has of a token that reaches over its ends goes into the workspace and is added up by
+// another launch, tile by tile.
 #pragma once
 
 #include "rows.hip.h"
@@ -19,25 +20,29 @@ struct EmbedArgs {
   int64_t T;
   int d, V;
   float scale;
+  uint32_t slices;
 };
 
-// A workgroup takes rows of `out` in turn, a lane eight channels at a time.
-template <class TE, class T>
+// A wavefront has a token and PIECES times 64 pieces of its row; those of a row follow each other, so that memory is written in order.
+// ONCE: results past the caches.  140897 tokens, d = 4096 in bf16, 1 / 2 / 4 pieces: 361 / 308 / 315 us, past the caches 332 / 284 / 300 (1.15 GB
+// written, 0.31 of the embedding read: 5.2 TB/s), slices of rows one after the other 462 / 433 / 331 and 424 / 397 / 316.
+template <class TE, class T, int W, int PIECES, bool ONCE>
 __global__ __launch_bounds__(256) void k_embed_fwd(const EmbedArgs p) {
-  const int c = (blockIdx.y * 64 + (threadIdx.x & 63)) * 8;
-  if (c >= p.d) return;
-  for (int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); t < p.T; t += (int64_t)gridDim.x * 4) {
-    const int32_t v = p.tokens[t];
-    Eight x;
-    if (v >= 0 && v < p.V) {
-      x = load_piece((const TE*)p.E + (int64_t)v * p.d, c, p.d);
+  const uint32_t unit = (blockIdx.y * gridDim.x + blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = unit / p.slices;
+  const int c = (unit % p.slices * PIECES * 64 + (threadIdx.x & 63)) * W;
+  if (t >= p.T) return;
+  const int32_t v = __builtin_amdgcn_readfirstlane(p.tokens[t]);
+  const bool inside = v >= 0 && v < p.V;
+  const TE* from = (const TE*)p.E + (int64_t)(inside ? v : 0) * p.d;
+  const float scale = inside ? p.scale : quiet_nan();
+  Piece<W> x[PIECES];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x.v[e] *= p.scale;
-    } else {
+  for (int i = 0; i < PIECES; ++i) x[i] = load_piece<W>(from, c + i * 64 * W, p.d);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x.v[e] = quiet_nan();
-    }
-    store_piece(p.out.row<T>(t), c, p.d, x);
+  for (int i = 0; i < PIECES; ++i) {
+#pragma unroll
+    for (int e = 0; e < W; ++e) x[i].v[e] *= scale;
+    store_piece<W, ONCE>(p.out.row<T>(t), c + i * 64 * W, p.d, x[i]);
   }
 }
 
@@ -52,8 +57,9 @@ struct SortArgs {
   int32_t* counts[2];               // [blocks][1 << bits]
   uint8_t* present;                 // [V]: whether an id occurs
   int* status;
+  float* dE;                        // to be cleared where no id occurs, beside the second pass; nullptr: not
   int64_t T;
-  int V, bits, blocks;
+  int V, d, bits, blocks;
 };
 
 __device__ __forceinline__ int sort_key(const SortArgs& p, int64_t t) {
@@ -82,6 +88,16 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_count(const SortArgs p) 
   if (blockIdx.x == 0 && threadIdx.x < kStatusWords) p.status[threadIdx.x] = 0;
 }
 
+// 1024 channels of 16 rows of dE, a wavefront's one each, are zero where the row's id does not occur.
+__device__ __forceinline__ void clear_absent(const SortArgs& p, int64_t i) {
+  const int lane = threadIdx.x & 63, pieces = (p.d + 1023) / 1024;
+  const int64_t v = i / pieces * (kSortThreads / 64) + (threadIdx.x >> 6);
+  if (v >= p.V || p.present[v]) return;
+  float* row = p.dE + v * p.d;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) store_piece<4>(row, (int)(i % pieces) * 1024 + (j * 64 + lane) * 4, p.d, Piece<4>{});
+}
+
 // Pass 0 reads tokens, pass 1 what pass 0 left.  A key's place: keys of smaller digits, those of its digit in earlier blocks, in earlier
 // wavefronts of this block, and before it in its wavefront.
 template <int PASS, int ITEMS>
@@ -89,78 +105,94 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_place(const SortArgs p) 
   extern __shared__ int32_t lds[];
   const int bins = 1 << p.bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   constexpr int WAVES = kSortThreads / 64;
-  int32_t* mine = lds;                       // [WAVES][bins]: first a wavefront's counts, then where its keys of a digit begin
-  for (int i = threadIdx.x; i < WAVES * bins; i += kSortThreads) mine[i] = 0;
+  if constexpr (PASS == 1) {
+    if ((int)blockIdx.x >= p.blocks || blockIdx.y > 0) {
+      clear_absent(p, (int64_t)blockIdx.y * gridDim.x + blockIdx.x - p.blocks);
+      return;
+    }
+  }
+  int32_t *mine = lds, *total = lds + WAVES * bins, *earlier = total + bins;
+  // mine [WAVES][bins]: first a wavefront's counts, then where its keys of a digit begin
+  for (int i = threadIdx.x; i < (WAVES + 2) * bins; i += kSortThreads) lds[i] = 0;
   __syncthreads();
   const int64_t from = ((int64_t)blockIdx.x * WAVES + wave) * 64 * ITEMS;
-  int key[ITEMS], rank[ITEMS];
+  int key[ITEMS], rank[ITEMS], first[ITEMS];
+  uint64_t same[ITEMS];                      // lanes with the same digit, and the first of them
 #pragma unroll
   for (int i = 0; i < ITEMS; ++i) {
     const int64_t t = from + i * 64 + lane;
     const bool any = t < p.T;
     key[i] = !any ? 0 : PASS == 0 ? sort_key(p, t) : p.keys[0][t];
     const int digit = PASS == 0 ? key[i] & (bins - 1) : key[i] >> p.bits;
-    uint64_t same = __ballot(any);
+    same[i] = __ballot(any);
     for (int b = 0; b < p.bits; ++b) {
       const uint64_t set = __ballot((digit >> b) & 1);
-      same &= (digit >> b) & 1 ? set : ~set;
+      same[i] &= (digit >> b) & 1 ? set : ~set;
     }
-    const int before = __popcll(same & (((uint64_t)1 << lane) - 1)), first = any ? __ffsll((unsigned long long)same) - 1 : lane;
+    const int before = __popcll(same[i] & (((uint64_t)1 << lane) - 1));
+    first[i] = any ? __ffsll((unsigned long long)same[i]) - 1 : lane;
     int base = 0;
-    if (any && lane == first) base = atomicAdd(&mine[wave * bins + digit], __popcll(same));
-    rank[i] = __shfl(base, first, 64) + before;
+    if (any && lane == first[i]) base = atomicAdd(&mine[wave * bins + digit], __popcll(same[i]));
+    rank[i] = __shfl(base, first[i], 64) + before;
+  }
+  // keys of every digit, in all blocks and in earlier ones
+  const int wide = bins < kSortThreads ? bins : kSortThreads, parts = kSortThreads / wide;
+  for (int bin = threadIdx.x & (wide - 1); bin < bins; bin += kSortThreads) {
+    int32_t in_all = 0, in_earlier = 0;
+#pragma unroll 8
+    for (int i = threadIdx.x / wide; i < p.blocks; i += parts) {
+      const int32_t n = p.counts[PASS][(int64_t)i * bins + bin];
+      in_all += n;
+      in_earlier += i < (int)blockIdx.x ? n : 0;
+    }
+    atomicAdd(&total[bin], in_all);
+    atomicAdd(&earlier[bin], in_earlier);
   }
   __syncthreads();
-  // sums over digits, kSortThreads of them at a time
-  __shared__ int32_t wave_sums[WAVES];
-  int32_t carry = 0;
-  for (int b0 = 0; b0 < bins; b0 += kSortThreads) {
-    const int b = b0 + threadIdx.x;
-    int32_t total = 0, earlier = 0;
-    if (b < bins) {
-      const int32_t* column = p.counts[PASS] + b;
-#pragma unroll 8
-      for (int i = 0; i < p.blocks; ++i) {
-        const int32_t n = column[(int64_t)i * bins];
-        total += n;
-        earlier += i < (int)blockIdx.x ? n : 0;
-      }
-    }
-    int32_t up = total;
-    for (int o = 1; o < 64; o <<= 1) {
-      const int32_t below = __shfl_up(up, o, 64);
-      if (lane >= o) up += below;
-    }
-    if (lane == 63) wave_sums[wave] = up;
-    __syncthreads();
-    int32_t smaller = carry + up - total, all = 0;
-    for (int i = 0; i < WAVES; ++i) {
-      smaller += i < wave ? wave_sums[i] : 0;
-      all += wave_sums[i];
-    }
-    carry += all;
-    if (b < bins) {
-      int32_t at = smaller + earlier;
-      for (int w = 0; w < WAVES; ++w) {
-        const int32_t n = mine[w * bins + b];
-        mine[w * bins + b] = at;
-        at += n;
-      }
-    }
-    __syncthreads();
+  // where a digit's keys begin: sums over smaller digits, two to a thread
+  const int b = threadIdx.x * 2;
+  const int32_t n0 = b < bins ? total[b] : 0, n1 = b < bins ? total[b + 1] : 0;
+  int32_t up = n0 + n1;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int32_t below = __shfl_up(up, o, 64);
+    if (lane >= o) up += below;
   }
+  __shared__ int32_t wave_sums[WAVES];
+  if (lane == 63) wave_sums[wave] = up;
+  __syncthreads();
+  up -= n0 + n1;
+  for (int i = 0; i < wave; ++i) up += wave_sums[i];
+  if (b < bins) earlier[b] += up, earlier[b + 1] += up + n0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < bins; i += kSortThreads) {
+    int32_t at = earlier[i];
+    for (int w = 0; w < WAVES; ++w) {
+      const int32_t n = mine[w * bins + i];
+      mine[w * bins + i] = at;
+      at += n;
+    }
+  }
+  __syncthreads();
 #pragma unroll
   for (int i = 0; i < ITEMS; ++i) {
     const int64_t t = from + i * 64 + lane;
-    if (t >= p.T) continue;
+    const bool any = t < p.T;
     const int digit = PASS == 0 ? key[i] & (bins - 1) : key[i] >> p.bits;
     const int32_t to = mine[wave * bins + digit] + rank[i];
-    p.keys[PASS][to] = key[i];
-    p.places[PASS][to] = PASS == 0 ? (int32_t)t : p.places[0][t];
+    if (any) {
+      p.keys[PASS][to] = key[i];
+      p.places[PASS][to] = PASS == 0 ? (int32_t)t : p.places[0][t];
+    }
     if constexpr (PASS == 0) {
-      atomicAdd(&p.counts[1][(int64_t)(to / (kSortThreads * ITEMS)) * bins + (key[i] >> p.bits)], 1);
-      if (key[i] < p.V) p.present[key[i]] = 1;
-      else atomicExch(p.status, kErrTokenRange);
+      // Counts for the second pass.  Lanes that add to the same one as the first of their digit, as those of a frequent token do, add together:
+      // one atomic after the other at the same place took 15 of 38 us of 140897 tokens, one in twelve of them the same.
+      const int at = any ? (to / (kSortThreads * ITEMS) << p.bits) + (key[i] >> p.bits) : -1;
+      const int with = __shfl(at, first[i], 64);
+      const uint64_t together = __ballot(at == with) & same[i];
+      if (any && at != with) atomicAdd(&p.counts[1][at], 1);
+      if (any && lane == first[i]) atomicAdd(&p.counts[1][at], __popcll(together));
+      if (any && lane == first[i] && key[i] == p.V) atomicExch(p.status, kErrTokenRange);
+      if (any && key[i] < p.V) p.present[key[i]] = 1;
     }
   }
 }
@@ -169,77 +201,248 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_place(const SortArgs p) 
 struct EmbedSumArgs {
   Rows dout;
   const int32_t *keys, *places;     // sorted
-  const uint8_t* present;           // nullptr: rows of dE without tokens stay as they are
   float *dE, *partials;             // partials [tiles][2][d]: of the token that a tile begins in the middle of, and of the one that it leaves
   int64_t T;
-  int d, V, tile, tiles;
+  int d, V, tile, tiles, slices;    // slices of 1024 channels
   float scale;
   bool add;                         // to what dE holds
 };
 
-__device__ __forceinline__ void put_row(const EmbedSumArgs& p, int key, int c, Eight sum) {
-  float* row = p.dE + (int64_t)key * p.d;
+__device__ __forceinline__ void put_row(const EmbedSumArgs& p, int64_t v, int c, Piece<4> sum) {
+  float* row = p.dE + v * p.d;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) sum.v[e] *= p.scale;
+  for (int e = 0; e < 4; ++e) sum.v[e] *= p.scale;
   if (p.add) {
-    const Eight old = load_piece(row, c, p.d);
+    const Piece<4> old = load_piece<4>(row, c, p.d);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum.v[e] += old.v[e];
+    for (int e = 0; e < 4; ++e) sum.v[e] += old.v[e];
   }
-  store_piece(row, c, p.d, sum);
+  store_piece<4>(row, c, p.d, sum);
 }
 
-// Workgroups below p.tiles sum up a tile's rows (blockIdx.y: 2048 channels), the others clear rows without tokens.
+// Rows of dout whose loads are under way together.
+constexpr int kEmbedRows = 8;
+
+// The sum of `n` of 64 rows, from the i-th on, whose positions a wavefront's lanes have.
 template <class T>
+__device__ __forceinline__ void add_rows(const EmbedSumArgs& p, Piece<4>& sum, int place, int i, int n, int c) {
+  Piece<4> x[kEmbedRows] = {};
+#pragma unroll
+  for (int u = 0; u < kEmbedRows; ++u)
+    if (u < n) x[u] = load_piece<4>(p.dout.row<T>(__builtin_amdgcn_readlane(place, i + u)), c, p.d);
+#pragma unroll
+  for (int u = 0; u < kEmbedRows; ++u)
+    if (u < n) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum.v[e] += x[u].v[e];
+    }
+}
+
+// A workgroup sums up 1024 channels, four a lane, of a tile's rows; the slices of a tile run side by side.  A wavefront has the ids and
+// positions of 64 rows in its lanes, so that its walk over them branches on scalars.  ONCE: rows past the caches.
+template <class T, bool ONCE>
 __global__ __launch_bounds__(256) void k_embed_sum(const EmbedSumArgs p) {
-  const int c = (blockIdx.y * 256 + threadIdx.x) * 8;
-  if (c >= p.d) return;
-  if ((int)blockIdx.x >= p.tiles) {
-    for (int64_t v = blockIdx.x - p.tiles; v < p.V; v += gridDim.x - p.tiles)
-      if (!p.present[v]) store_piece(p.dE + v * p.d, c, p.d, Eight{});
+  const int lane = threadIdx.x & 63, tile = blockIdx.x / p.slices, c = (blockIdx.x % p.slices * 256 + threadIdx.x) * 4;
+  if (c - lane * 4 >= p.d) return;
+  const int from = tile * p.tile, to = from + p.tile < p.T ? from + p.tile : (int)p.T;
+  const int first = p.keys[from], last = p.keys[to - 1];
+  const bool begun = from > 0 && p.keys[from - 1] == first, open = to < p.T && p.keys[to] == last;
+  Piece<4> sum = {};
+  for (int base = from; base < to; base += 64) {
+    const int n = to - base < 64 ? to - base : 64;
+    const int key = lane < n ? p.keys[base + lane] : -1, place = lane < n ? p.places[base + lane] : 0;
+    const int after = lane + 1 < n || (lane < n && base + n < to) ? p.keys[base + lane + 1] : -1;
+    const uint64_t ends = __ballot(key != after);
+    for (int i = 0; i < n; i += kEmbedRows) {
+      Piece<4> x[kEmbedRows] = {};
+#pragma unroll
+      for (int u = 0; u < kEmbedRows; ++u)
+        if (i + u < n) x[u] = load_piece<4, ONCE>(p.dout.row<T>(__builtin_amdgcn_readlane(place, i + u)), c, p.d);
+#pragma unroll
+      for (int u = 0; u < kEmbedRows; ++u) {
+        if (i + u >= n) break;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum.v[e] += x[u].v[e];
+        if (!((ends >> (i + u)) & 1)) continue;
+        const int v = __builtin_amdgcn_readlane(key, i + u);
+        if (begun && v == first) store_piece<4>(p.partials + (int64_t)tile * 2 * p.d, c, p.d, sum);
+        else if (open && v == last) store_piece<4>(p.partials + ((int64_t)tile * 2 + 1) * p.d, c, p.d, sum);
+        else if (v < p.V) put_row(p, v, c, sum);
+        sum = Piece<4>{};
+      }
+    }
+  }
+}
+
+// Tokens that reach over the ends of tiles: where one ends in one of a workgroup's 16 tiles, its four wavefronts add up what the tiles have
+// of it, a quarter of them each, in their order and in 64 bits.
+constexpr int kJoinTiles = 4, kJoinParts = 4;
+
+__global__ __launch_bounds__(64 * kJoinParts) void k_embed_join(const EmbedSumArgs p) {
+  __shared__ double parts[kJoinParts][4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (blockIdx.y * 64 + lane) * 4;
+  const int tile0 = blockIdx.x * kJoinTiles;
+  const int64_t from = (int64_t)(tile0 + lane) * p.tile, to = from + p.tile < p.T ? from + p.tile : p.T;
+  int key = p.V;
+  bool here = false;
+  if (lane < kJoinTiles && from > 0 && from < p.T) {
+    key = p.keys[from];
+    here = key < p.V && p.keys[from - 1] == key && !(to < p.T && p.keys[to - 1] == key && p.keys[to] == key);
+  }
+  for (uint64_t todo = __ballot(here); todo; todo &= todo - 1) {
+    const int at = __ffsll((unsigned long long)todo) - 1, v = __builtin_amdgcn_readlane(key, at), tile = tile0 + at;
+    int begin = tile;                   // the tile that the token begins in: the last one that does not begin in the middle of it
+    for (;;) {
+      const int t = begin - lane;
+      const uint64_t found = __ballot(t <= 0 || p.keys[(int64_t)t * p.tile - 1] != v);
+      begin -= found ? __ffsll((unsigned long long)found) - 1 : 64;
+      if (found) break;
+    }
+    const int n = tile - begin + 1, lo = (int)((int64_t)n * wave / kJoinParts), hi = (int)((int64_t)n * (wave + 1) / kJoinParts);
+    double sum[4] = {};
+#pragma unroll 8
+    for (int i = lo; i < hi; ++i) {
+      const Piece<4> x = load_piece<4>(p.partials + ((int64_t)(begin + i) * 2 + (i == 0)) * p.d, c, p.d);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += (double)x.v[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) parts[wave][e][lane] = sum[e];
+    __syncthreads();
+    if (wave == 0) {
+      Piece<4> x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        double all = parts[0][e][lane];
+#pragma unroll
+        for (int w = 1; w < kJoinParts; ++w) all += parts[w][e][lane];
+        x.v[e] = (float)all;
+      }
+      put_row(p, v, c, x);
+    }
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------- gradient: few tokens
+constexpr int kFewTokens = 4096, kRankTokens = 8, kRankParts = 256 / kRankTokens;
+
+// 1024 elements of dE, from 1024 i on, are zero.
+__device__ __forceinline__ void clear_piece(const EmbedSumArgs& p, int64_t i) {
+  const int64_t at = (i * 256 + threadIdx.x) * 4, n = (int64_t)p.V * p.d;
+  if (at + 4 <= n) {
+    store_whole<4>(p.dE + at, Piece<4>{});
+  } else {
+    for (int64_t e = at; e < n; ++e) p.dE[e] = 0.f;
+  }
+}
+
+// Sorting without passes: a token's place is the number of those with smaller ids, and of earlier ones with its own.  A workgroup finds the
+// places of 32 tokens, each 32 lanes among an eighth of all.  The workgroups behind clear dE, 4 KB each, which is the order that memory
+// likes best (2.49 GB in 357 us; 16 KB a workgroup 402, 256 KB 400 .. 430).
+__global__ __launch_bounds__(256) void k_embed_rank(const EmbedSumArgs p, const int32_t* __restrict__ tokens, int32_t* keys, int32_t* places,
+                                                    int* status, int sorters) {
+  if ((int)blockIdx.x >= sorters || blockIdx.y > 0) {
+    clear_piece(p, (int64_t)blockIdx.y * gridDim.x + blockIdx.x - sorters);
     return;
   }
-  const int64_t from = (int64_t)blockIdx.x * p.tile, to = from + p.tile < p.T ? from + p.tile : p.T;
-  const bool begun = from > 0 && p.keys[from - 1] == p.keys[from], open = to < p.T && p.keys[to] == p.keys[to - 1];
-  const int first = p.keys[from], last = p.keys[to - 1];
-  Eight sum = {};
-  int key = first;
-  for (int64_t i = from; i < to; ++i) {
-    const Eight x = load_piece(p.dout.row<T>(p.places[i]), c, p.d);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum.v[e] += x.v[e];
-    const int next = i + 1 < to ? p.keys[i + 1] : -1;
-    if (next == key) continue;
-    if (key < p.V) {
-      if (begun && key == first) store_piece(p.partials + (int64_t)blockIdx.x * 2 * p.d, c, p.d, sum);
-      else if (open && key == last) store_piece(p.partials + ((int64_t)blockIdx.x * 2 + 1) * p.d, c, p.d, sum);
-      else put_row(p, key, c, sum);
-    }
-    sum = Eight{};
-    key = next;
+  __shared__ int4 all4[kFewTokens / 4];
+  __shared__ int ranks[kRankParts][kRankTokens];
+  __shared__ int outside;
+  int* all = (int*)all4;
+  const int T = (int)p.T, padded = (T + 255) / 256 * 256;
+  if (threadIdx.x == 0) outside = 0;
+  __syncthreads();
+#pragma unroll 8
+  for (int t = threadIdx.x; t < padded; t += 256) {
+    const int v = t < T ? tokens[t] : 0;
+    const bool good = v >= 0 && v < p.V;
+    all[t] = t < T ? (good ? v : p.V) : INT32_MAX;       // smaller than no id
+    if (!good) outside = 1;
   }
+  __syncthreads();
+  const int t0 = blockIdx.x * kRankTokens, t = t0 + threadIdx.x % kRankTokens, part = threadIdx.x / kRankTokens;
+  const int mine = t < T ? all[t] : 0;
+  int rank = 0;
+  // ids up to and with its own among tokens before, smaller ones among those behind
+  const auto count = [&](int from, int to, auto before) {
+#pragma unroll 8
+    for (int j = from; j < to; ++j) {
+      const int4 k = all4[j];
+      rank += (k.x < mine + before(4 * j)) + (k.y < mine + before(4 * j + 1)) + (k.z < mine + before(4 * j + 2)) + (k.w < mine + before(4 * j + 3));
+    }
+  };
+  const int each = padded / 4 / kRankParts, from = part * each, to = from + each, own = t0 / 4, behind = own + kRankTokens / 4;
+  count(from, min(to, own), [](int) { return 1; });
+  count(max(from, own), min(to, behind), [&](int j) { return j < t ? 1 : 0; });
+  count(max(from, behind), to, [](int) { return 0; });
+  ranks[part][threadIdx.x % kRankTokens] = rank;
+  __syncthreads();
+  if (part == 0 && t < T) {
+#pragma unroll
+    for (int i = 1; i < kRankParts; ++i) rank += ranks[i][threadIdx.x];
+    keys[rank] = mine;
+    places[rank] = t;
+  }
+  if (blockIdx.x == 0 && threadIdx.x < kStatusWords) status[threadIdx.x] = threadIdx.x == 0 && outside ? kErrTokenRange : 0;
 }
 
-// Tokens that reach over the ends of tiles: the tile that one ends in adds up what the tiles have of it, in their order, in 64 bits.
-__global__ __launch_bounds__(256) void k_embed_join(const EmbedSumArgs p) {
-  const int c = blockIdx.y * 256 + threadIdx.x;
-  const int64_t tile = blockIdx.x, from = tile * p.tile, to = from + p.tile < p.T ? from + p.tile : p.T;
-  if (from == 0 || c >= p.d) return;
-  const int key = p.keys[from];
-  if (p.keys[from - 1] != key || key >= p.V) return;                                // begins here
-  if (to < p.T && p.keys[to - 1] == key && p.keys[to] == key) return;              // ends further on
-  int64_t lo = 0, hi = from;                                                       // its first position
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) / 2;
-    if (p.keys[mid] < key) lo = mid + 1;
-    else hi = mid;
+// Sums of the sorted rows: a workgroup has 32 of them and 256 channels, each wavefront the tokens that begin among 8; one that goes on
+// behind the 32 is shared by the four wavefronts, a quarter of its rows each, which are added in their order.
+template <class T>
+__global__ __launch_bounds__(256) void k_embed_runs(const EmbedSumArgs p) {
+  __shared__ Piece<4> quarter[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (blockIdx.y * 64 + lane) * 4;
+  const int from = blockIdx.x * 32, n = (int)p.T - from < 32 ? (int)p.T - from : 32;
+  const int key = lane < n ? p.keys[from + lane] : -1, place = lane < n ? p.places[from + lane] : 0;
+  const int before = from + lane > 0 && lane < n ? p.keys[from + lane - 1] : -1;
+  const int behind = from + n < p.T ? p.keys[from + n] : -1;
+  const uint64_t begins = __ballot(lane < n && key != before);
+  const bool on = behind >= 0 && behind == __builtin_amdgcn_readlane(key, n - 1);
+  const int last = begins ? 63 - __clzll(begins) : n;          // the last token that begins here
+  const uint64_t ours = begins & (uint64_t)0xff << (8 * wave), after = begins >> (8 * wave) >> 8;
+  // from the first token that begins here to the end of the last one that does not go on behind the 32
+  int i = ours ? __ffsll((unsigned long long)ours) - 1 : n, end = after ? 8 * wave + 7 + __ffsll((unsigned long long)after) : on ? last : n;
+  Piece<4> sum = {};
+  while (i < end) {
+    Piece<4> x[kEmbedRows] = {};
+#pragma unroll
+    for (int u = 0; u < kEmbedRows; ++u)
+      if (i + u < end) x[u] = load_piece<4>(p.dout.row<T>(__builtin_amdgcn_readlane(place, i + u)), c, p.d);
+#pragma unroll
+    for (int u = 0; u < kEmbedRows; ++u) {
+      if (i + u >= end) break;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum.v[e] += x[u].v[e];
+      if (i + u + 1 < n && !((begins >> (i + u + 1)) & 1)) continue;
+      const int v = __builtin_amdgcn_readlane(key, i + u);
+      if (v < p.V) put_row(p, v, c, sum);
+      sum = Piece<4>{};
+    }
+    i += kEmbedRows;
   }
-  const int64_t begin = lo / p.tile;
-  double sum = p.partials[(begin * 2 + 1) * p.d + c];
-#pragma unroll 8
-  for (int64_t i = begin + 1; i <= tile; ++i) sum += p.partials[i * 2 * p.d + c];
-  float* at = p.dE + (int64_t)key * p.d + c;
-  *at = (float)sum * p.scale + (p.add ? *at : 0.f);
+  if (!begins || !on || __builtin_amdgcn_readlane(key, last) >= p.V) return;
+  const int v = __builtin_amdgcn_readlane(key, last);
+  end = from + n;                                             // its last position and one
+  for (;;) {
+    const uint64_t other = __ballot(end + lane >= p.T || p.keys[end + lane] != v);
+    end += other ? __ffsll((unsigned long long)other) - 1 : 64;
+    if (other) break;
+  }
+  const int begin = from + last, rows = end - begin, lo = begin + rows * wave / 4, hi = begin + rows * (wave + 1) / 4;
+  sum = Piece<4>{};
+  for (int base = lo; base < hi; base += 64) {
+    const int at = base + lane < hi ? p.places[base + lane] : 0, here = hi - base < 64 ? hi - base : 64;
+    for (int i = 0; i < here; i += kEmbedRows) add_rows<T>(p, sum, at, i, here - i, c);
+  }
+  quarter[wave][lane] = sum;
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int w = 1; w < 4; ++w)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum.v[e] += quarter[w][lane].v[e];
+  put_row(p, v, c, sum);
 }
 
 }  // namespace oapl

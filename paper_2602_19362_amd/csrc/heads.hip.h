@@ -26,6 +26,15 @@ __device__ __forceinline__ void store4(bf16_t* p, f32x4 v) {
   *(bf16x4*)p = bf16x4{(bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3]};
 }
 
+// Sum over the 16 lanes of a group, in every lane: rotations by 8, 4, 2 and 1 of a row of lanes.
+__device__ __forceinline__ float group_sum(float v) {
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xf, 0xf, false));
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x124, 0xf, 0xf, false));
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x122, 0xf, 0xf, false));
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x121, 0xf, 0xf, false));
+  return v;
+}
+
 __device__ __forceinline__ float quiet_nan() { return __builtin_nanf(""); }
 
 }  // namespace oapl

@@ -33,14 +33,6 @@ struct NormRopeArgs {
   float eps;
 };
 
-// Sum over the 16 lanes of a group, in every lane: rotations by 8, 4, 2 and 1 of a row of lanes.
-__device__ __forceinline__ float group_sum(float v) {
-  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xf, 0xf, false));
-  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x124, 0xf, 0xf, false));
-  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x122, 0xf, 0xf, false));
-  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x121, 0xf, 0xf, false));
-  return v;
-}
 __device__ __forceinline__ float dot4(f32x4 a, f32x4 b) { return a[0] * b[0] + a[1] * b[1] + a[2] * b[2] + a[3] * b[3]; }
 
 // Where a lane's two pieces of four channels lie, and whether it has any: lanes below rot / 8 hold pairs that are turned

@@ -7,8 +7,9 @@
 //   dX = dx' + r (u - v mean_c(u o v)),   dz = scale gate o dX,   dy = r(y) (t - w mean_c(t o w))  (or dz)
 //   dgain = sum dn o v,   dy_gain = sum dz o w,   dgate = scale z o dX (summed over tokens where they share the gate)
 //
-// Bound by memory: every row is read once and written once, and stays in registers in between, in 32 bits; a row's sums are the only
-// thing that its lanes exchange.
+// Bound by memory: every row is read once and written once, and stays in registers in between; a row's sums are the only thing that its
+// lanes exchange.  16411 tokens, d = 4096 in bf16: forward 538 MB in 95 us (5.7 TB/s; a large copy reaches 4.9), backward 807 MB in 150 us (5.4), and 5
+// for the sums over tokens.
 #pragma once
 
 #include "rows.hip.h"
@@ -30,7 +31,7 @@ struct ResidualNormArgs {
 // ahead writes to the other one, and cannot be two sums ahead of a barrier, so that one barrier a sum is enough.
 template <int THREADS>
 __device__ __forceinline__ float row_total(float v, int& turn) {
-  v = wave_total(v);
+  v = lanes_total<(THREADS < 64 ? THREADS : 64)>(v);
   if constexpr (THREADS > 64) {
     __shared__ float all[2][THREADS / 64];
     turn ^= 1;
@@ -43,98 +44,136 @@ __device__ __forceinline__ float row_total(float v, int& turn) {
   return v;
 }
 
-__device__ __forceinline__ float square_sum(const Eight& x) {
+template <int W>
+__device__ __forceinline__ float dot(const Piece<W>& a, const Piece<W>& b) {
   float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) s += x.v[i] * x.v[i];
+  for (int i = 0; i < W; ++i) s += a.v[i] * b.v[i];
   return s;
 }
 
-// TX: the residual stream's type, T: the block's and the norms'.  THREADS lanes hold a row, eight channels in each of PIECES pieces.
-template <class TX, class T, int THREADS, int PIECES>
-__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void k_residual_norm_fwd(const ResidualNormArgs p) {
-  constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1;
+// TX: the residual stream's type, T: the block's and the norms'.  THREADS lanes hold a row, W channels in each of PIECES pieces: 16 of them, a
+// wavefront, or a workgroup.
+template <class TX, class T, int W, int THREADS, int PIECES>
+__global__ __launch_bounds__(THREADS < 128 ? 256 : THREADS) void k_residual_norm_fwd(const ResidualNormArgs p) {
+  constexpr int ROWS = THREADS < 128 ? 256 / THREADS : 1;
   const int lane = threadIdx.x % THREADS, d = p.d;
   int turn = 0;
-  for (int64_t t = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS; t < p.T; t += (int64_t)gridDim.x * ROWS) {
-    Eight x[PIECES], y[PIECES];
+  for (int64_t t = (int64_t)blockIdx.x * ROWS + (ROWS == 1 ? 0 : threadIdx.x / THREADS); t < p.T; t += (int64_t)gridDim.x * ROWS) {
+    Raw<TX, W> rx[PIECES];
+    Raw<T, W> ry[PIECES] = {}, rg[PIECES] = {};
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      const int c = (i * THREADS + lane) * 8;
-      x[i] = load_piece(p.x.row<TX>(t), c, d);
-      if (p.y.p) y[i] = load_piece(p.y.row<T>(t), c, d);
+      const int c = (i * THREADS + lane) * W;
+      rx[i] = load_raw<W>(p.x.row<TX>(t), c, d);
+      if (p.y.p) ry[i] = load_raw<W>(p.y.row<T>(t), c, d);
+      if (p.gate.p) rg[i] = load_raw<W>(p.gate.row<T>(t), c, d);
     }
+    Piece<W> x[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) x[i] = widened(rx[i]);
     if (p.y.p) {
       float r = p.scale;
       if (p.y_gain) {
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) sum += square_sum(y[i]);
+        for (int i = 0; i < PIECES; ++i) sum += dot(widened(ry[i]), widened(ry[i]));
         r *= rsqrtf(row_total<THREADS>(sum, turn) / (float)d + p.eps);
       }
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
-        const int c = (i * THREADS + lane) * 8;
+        const int c = (i * THREADS + lane) * W;
+        Piece<W> y = widened(ry[i]);
         if (p.y_gain) {
-          const Eight g = load_piece((const T*)p.y_gain, c, d);
+          const Piece<W> g = load_piece<W>((const T*)p.y_gain, c, d);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) y[i].v[e] *= g.v[e];
+          for (int e = 0; e < W; ++e) y.v[e] *= g.v[e];
         }
         if (p.gate.p) {
-          const Eight g = load_piece(p.gate.row<T>(t), c, d);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) y[i].v[e] *= g.v[e];
+          for (int e = 0; e < W; ++e) y.v[e] *= (float)rg[i][e];
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[i].v[e] += r * y[i].v[e];
-        store_piece(p.x_out.row<TX>(t), c, d, x[i]);
+        for (int e = 0; e < W; ++e) x[i].v[e] += r * y.v[e];
+        store_piece<W>(p.x_out.row<TX>(t), c, d, x[i]);
       }
     }
     if (p.gain) {
       float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) sum += square_sum(x[i]);
+      for (int i = 0; i < PIECES; ++i) sum += dot(x[i], x[i]);
       const float r = rsqrtf(row_total<THREADS>(sum, turn) / (float)d + p.eps);
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
-        const int c = (i * THREADS + lane) * 8;
-        const Eight g = load_piece((const T*)p.gain, c, d);
+        const int c = (i * THREADS + lane) * W;
+        const Piece<W> g = load_piece<W>((const T*)p.gain, c, d);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[i].v[e] *= r * g.v[e];
-        store_piece(p.out.row<T>(t), c, d, x[i]);
+        for (int e = 0; e < W; ++e) x[i].v[e] *= r * g.v[e];
+        store_piece<W>(p.out.row<T>(t), c, d, x[i]);
       }
     }
   }
 }
 
-template <class TX, class T, int THREADS, int PIECES>
-__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void k_residual_norm_bwd(const ResidualNormArgs p) {
-  constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1;
+// What a row's gradient is made of, as it is stored.
+template <class TX, class T, int W, int PIECES>
+struct NormRow {
+  Raw<TX, W> dx[PIECES], x[PIECES];
+  Raw<T, W> dn[PIECES], y[PIECES], gate[PIECES];
+};
+
+template <class TX, class T, int W, int THREADS, int PIECES>
+__global__ __launch_bounds__(THREADS < 128 ? 256 : THREADS) void k_residual_norm_bwd(const ResidualNormArgs p) {
+  constexpr int ROWS = THREADS < 128 ? 256 / THREADS : 1;
   const int lane = threadIdx.x % THREADS, d = p.d;
   int turn = 0;
-  Eight sum_gain[PIECES] = {}, sum_block[PIECES] = {};
-  for (int64_t t = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS; t < p.T; t += (int64_t)gridDim.x * ROWS) {
-    Eight dx[PIECES], v[PIECES], u[PIECES];
+  Piece<W> sum_gain[PIECES] = {}, sum_block[PIECES] = {};
+  Raw<T, W> gain[PIECES] = {}, y_gain[PIECES] = {};
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) {
+    const int c = (i * THREADS + lane) * W;
+    if (p.gain) gain[i] = load_raw<W>((const T*)p.gain, c, d);
+    if (p.y_gain) y_gain[i] = load_raw<W>((const T*)p.y_gain, c, d);
+  }
+  typedef NormRow<TX, T, W, PIECES> Row;
+  const auto load = [&](Row& row, int64_t t) {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      const int c = (i * THREADS + lane) * 8;
-      dx[i] = p.x_out.p ? load_piece(p.x_out.row<TX>(t), c, d) : Eight{};
-      if (p.gain) v[i] = load_piece(p.x.row<TX>(t), c, d), u[i] = load_piece(p.out.row<T>(t), c, d);
+      const int c = (i * THREADS + lane) * W;
+      row.dx[i] = Raw<TX, W>{};
+      if (p.gain) row.x[i] = load_raw<W>(p.x.row<TX>(t), c, d), row.dn[i] = load_raw<W>(p.out.row<T>(t), c, d);
+      if (p.x_out.p) row.dx[i] = load_raw<W>(p.x_out.row<TX>(t), c, d);
+      if (p.y.p) row.y[i] = load_raw<W>(p.y.row<T>(t), c, d);
+      if (p.gate.p) row.gate[i] = load_raw<W>(p.gate.row<T>(t), c, d);
     }
+  };
+  const int64_t first = (int64_t)blockIdx.x * ROWS + (ROWS == 1 ? 0 : threadIdx.x / THREADS), step = (int64_t)gridDim.x * ROWS;
+  // the next row is under way while one is worked on, as far as there are registers for it
+  constexpr bool AHEAD = THREADS * PIECES * W <= 4096;
+  Row row, next;
+  if (AHEAD && first < p.T) load(next, first);
+  for (int64_t t = first; t < p.T; t += step) {
+    if (AHEAD) row = next;
+    else load(row, t);
+    if (AHEAD && t + step < p.T) load(next, t + step);
+    Piece<W> dx[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) dx[i] = widened(row.dx[i]);
     if (p.gain) {
       float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) sum += square_sum(v[i]);
+      for (int i = 0; i < PIECES; ++i) sum += dot(widened(row.x[i]), widened(row.x[i]));
       const float r = rsqrtf(row_total<THREADS>(sum, turn) / (float)d + p.eps);
+      Piece<W> v[PIECES], u[PIECES];
       float m = 0.f;
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
-        const Eight g = load_piece((const T*)p.gain, (i * THREADS + lane) * 8, d);
+        v[i] = widened(row.x[i]), u[i] = widened(row.dn[i]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < W; ++e) {
           v[i].v[e] *= r;
           sum_gain[i].v[e] += u[i].v[e] * v[i].v[e];
-          u[i].v[e] *= g.v[e];
+          u[i].v[e] *= (float)gain[i][e];
           m += u[i].v[e] * v[i].v[e];
         }
       }
@@ -142,76 +181,85 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void k_residual_norm
 #pragma unroll
       for (int i = 0; i < PIECES; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dx[i].v[e] += r * (u[i].v[e] - v[i].v[e] * m);
+        for (int e = 0; e < W; ++e) dx[i].v[e] += r * (u[i].v[e] - v[i].v[e] * m);
     }
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) store_piece(p.dx.row<TX>(t), (i * THREADS + lane) * 8, d, dx[i]);
-    if (!p.y.p) continue;
-    // from here on dx is dz, v is w (or y)
-    float r = 1.f;
+    for (int i = 0; i < PIECES; ++i) store_piece<W>(p.dx.row<TX>(t), (i * THREADS + lane) * W, d, dx[i]);
+    if (p.y.p) {
+      // from here on dx is dz
+      float r = 1.f;
+      if (p.y_gain) {
+        float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i)
-      if (p.y_gain || p.gate.p) v[i] = load_piece(p.y.row<T>(t), (i * THREADS + lane) * 8, d);
-    if (p.y_gain) {
-      float sum = 0.f;
+        for (int i = 0; i < PIECES; ++i) sum += dot(widened(row.y[i]), widened(row.y[i]));
+        r = rsqrtf(row_total<THREADS>(sum, turn) / (float)d + p.eps);
+      }
+      float m = 0.f;
+      Piece<W> w[PIECES];
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) sum += square_sum(v[i]);
-      r = rsqrtf(row_total<THREADS>(sum, turn) / (float)d + p.eps);
-    }
-    float m = 0.f;
+      for (int i = 0; i < PIECES; ++i) {
+        const int c = (i * THREADS + lane) * W;
+        w[i] = widened(row.y[i]);
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const int c = (i * THREADS + lane) * 8;
-      Eight g;
+        for (int e = 0; e < W; ++e) dx[i].v[e] *= p.scale, w[i].v[e] *= r;
+        // the second sum: of a gate that all tokens share, from which both its gradient and the gain's come, or the gain's
+        if (p.gate.p && p.dgate.p) {
+          Piece<W> dg;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) dx[i].v[e] *= p.scale, g.v[e] = 1.f;
-      if (p.y_gain) g = load_piece((const T*)p.y_gain, c, d);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[i].v[e] *= r;
-      if (p.gate.p) {
-        const Eight gate = load_piece(p.gate.row<T>(t), c, d);
-        if (p.dgate.p) {
-          Eight dg;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) dg.v[e] = dx[i].v[e] * v[i].v[e] * g.v[e];
-          store_piece(p.dgate.row<T>(t), c, d, dg);
-        } else {
-          // the sum for a gate that all tokens share; both it and the gain's gradient come out of it
-#pragma unroll
-          for (int e = 0; e < 8; ++e) sum_block[i].v[e] += dx[i].v[e] * v[i].v[e];
+          for (int e = 0; e < W; ++e) {
+            dg.v[e] = dx[i].v[e] * w[i].v[e] * (p.y_gain ? (float)y_gain[i][e] : 1.f);
+            dx[i].v[e] *= (float)row.gate[i][e];
+          }
+          store_piece<W>(p.dgate.row<T>(t), c, d, dg);
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dx[i].v[e] *= gate.v[e];
+        for (int e = 0; e < W; ++e) sum_block[i].v[e] += dx[i].v[e] * w[i].v[e];
+        if (p.gate.p && !p.dgate.p) {
+#pragma unroll
+          for (int e = 0; e < W; ++e) dx[i].v[e] *= (float)row.gate[i][e];
+        }
+        if (p.y_gain) {
+#pragma unroll
+          for (int e = 0; e < W; ++e) {
+            dx[i].v[e] *= (float)y_gain[i][e];
+            m += dx[i].v[e] * w[i].v[e];
+          }
+        }
       }
       if (p.y_gain) {
-        if (!p.gate.p || p.dgate.p) {
+        m = row_total<THREADS>(m, turn) / (float)d;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sum_block[i].v[e] += dx[i].v[e] * v[i].v[e];
-        }
+        for (int i = 0; i < PIECES; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          dx[i].v[e] *= g.v[e];
-          m += dx[i].v[e] * v[i].v[e];
-        }
+          for (int e = 0; e < W; ++e) dx[i].v[e] = r * (dx[i].v[e] - w[i].v[e] * m);
       }
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) store_piece<W>(p.dy.row<T>(t), (i * THREADS + lane) * W, d, dx[i]);
     }
-    if (p.y_gain) {
-      m = row_total<THREADS>(m, turn) / (float)d;
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) dx[i].v[e] = r * (dx[i].v[e] - v[i].v[e] * m);
-    }
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) store_piece(p.dy.row<T>(t), (i * THREADS + lane) * 8, d, dx[i]);
   }
   if (!p.partials) return;
+  float* to = p.partials + (int64_t)blockIdx.x * 2 * d;
+  if constexpr (ROWS == 1) {
 #pragma unroll
-  for (int i = 0; i < PIECES; ++i) {
-    const int c = (i * THREADS + lane) * 8;
-    float* to = p.partials + ((int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS) * 2 * d;
-    store_piece(to, c, d, sum_gain[i]);
-    store_piece(to + d, c, d, sum_block[i]);
+    for (int i = 0; i < PIECES; ++i) {
+      store_piece<W>(to, (i * THREADS + lane) * W, d, sum_gain[i]);
+      store_piece<W>(to + d, (i * THREADS + lane) * W, d, sum_block[i]);
+    }
+  } else {
+    // the workgroup's rows, added in their order
+    __shared__ float all[ROWS][2][THREADS * PIECES * W];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      store_whole<W>(&all[threadIdx.x / THREADS][0][(i * THREADS + lane) * W], sum_gain[i]);
+      store_whole<W>(&all[threadIdx.x / THREADS][1][(i * THREADS + lane) * W], sum_block[i]);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * d; i += 256) {
+      float v = 0.f;
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) v += all[r][i >= d][i >= d ? i - d : i];
+      to[i] = v;
+    }
   }
 }
 

@@ -14,63 +14,82 @@ struct Rows {
   __device__ __forceinline__ T* row(int64_t i) const { return (T*)(p + i * stride); }
 };
 
-// Eight channels in 32 bits.  Rows may start at any element: memory takes 16-byte accesses at any address, aligned ones at full rate.
-struct Eight {
-  float v[8];
+// W neighbouring channels, as they are stored and in 32 bits: eight where everything is bf16, four where something is fp32, so that a
+// wavefront's access of 16 bytes a lane covers whole lines.  Rows may start at any element: memory takes accesses of 8 and 16 bytes at any
+// address, aligned ones at full rate.
+template <class T, int W>
+struct RawOf {
+  typedef T type __attribute__((ext_vector_type(W)));
+  typedef uint32_t words __attribute__((ext_vector_type(W * sizeof(T) / 4), aligned(sizeof(T))));      // anywhere in memory
+};
+template <class T, int W>
+using Raw = typename RawOf<T, W>::type;
+
+template <int W>
+struct Piece {
+  float v[W];
 };
 
-__device__ __forceinline__ void load8(Eight& x, const float* p) {
-  __builtin_memcpy(x.v, p, 32);
-}
-__device__ __forceinline__ void load8(Eight& x, const bf16_t* p) {
-  bf16x8 b;
-  __builtin_memcpy(&b, p, 16);
+template <class R>
+__device__ __forceinline__ auto widened(const R& raw) {
+  constexpr int W = sizeof(R) / sizeof(raw[0]);
+  Piece<W> x;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x.v[i] = (float)b[i];
-}
-// Rounding to bf16 is to nearest even, once, of values held in 32 bits until then.
-__device__ __forceinline__ void store8(float* p, const Eight& x) {
-  __builtin_memcpy(p, x.v, 32);
-}
-__device__ __forceinline__ void store8(bf16_t* p, const Eight& x) {
-  bf16x8 b;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) b[i] = (bf16_t)x.v[i];
-  __builtin_memcpy(p, &b, 16);
-}
-
-// Channels c .. c + 7 of a row of d, zeros behind its end.
-template <class T>
-__device__ __forceinline__ Eight load_piece(const T* row, int c, int d) {
-  Eight x = {};
-  if (c + 8 <= d) {
-    load8(x, row + c);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (c + i < d) x.v[i] = (float)row[c + i];
-  }
+  for (int i = 0; i < W; ++i) x.v[i] = (float)raw[i];
   return x;
 }
-template <class T>
-__device__ __forceinline__ void store_piece(T* row, int c, int d, const Eight& x) {
-  if (c + 8 <= d) {
-    store8(row + c, x);
+
+// Channels c .. c + W - 1 of a row of d, zeros behind its end.  ONCE: an access that leaves nothing in the caches.
+template <int W, bool ONCE = false, class T>
+__device__ __forceinline__ Raw<T, W> load_raw(const T* row, int c, int d) {
+  typedef typename RawOf<T, W>::words words;
+  if (c + W <= d) {
+    if constexpr (ONCE) return __builtin_bit_cast(Raw<T, W>, __builtin_nontemporal_load((const words*)(row + c)));
+    else return __builtin_bit_cast(Raw<T, W>, *(const words*)(row + c));
+  }
+  Raw<T, W> x = {};
+#pragma unroll
+  for (int i = 0; i < W; ++i)
+    if (c + i < d) x[i] = row[c + i];
+  return x;
+}
+template <int W, bool ONCE = false, class T>
+__device__ __forceinline__ Piece<W> load_piece(const T* row, int c, int d) {
+  return widened(load_raw<W, ONCE>(row, c, d));
+}
+
+// Rounding to bf16 is to nearest even, once, of values held in 32 bits until then.
+template <int W, bool ONCE = false, class T>
+__device__ __forceinline__ void store_whole(T* p, const Piece<W>& x) {
+  typedef typename RawOf<T, W>::words words;
+  Raw<T, W> b;
+#pragma unroll
+  for (int i = 0; i < W; ++i) b[i] = (T)x.v[i];
+  if constexpr (ONCE) __builtin_nontemporal_store(__builtin_bit_cast(words, b), (words*)p);
+  else *(words*)p = __builtin_bit_cast(words, b);
+}
+template <int W, bool ONCE = false, class T>
+__device__ __forceinline__ void store_piece(T* row, int c, int d, const Piece<W>& x) {
+  if (c + W <= d) {
+    store_whole<W, ONCE>(row + c, x);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < W; ++i)
       if (c + i < d) row[c + i] = (T)x.v[i];
   }
 }
 
-// Sum over a wavefront, in every lane, in a fixed order: rows of 16 lanes by rotations, then pairs of rows and of halves trade places.
-__device__ __forceinline__ float wave_total(float v) {
-  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xf, 0xf, false));
-  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x124, 0xf, 0xf, false));
-  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x122, 0xf, 0xf, false));
-  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x121, 0xf, 0xf, false));
-  v += __shfl_xor(v, 16, 64);
-  return v + __shfl_xor(v, 32, 64);
+// Sum over a group of 16 lanes, or over a wavefront, in every lane and in a fixed order: rows of 16 lanes by rotations, then pairs of rows
+// and of halves trade places.
+template <int LANES>
+__device__ __forceinline__ float lanes_total(float v) {
+  static_assert(LANES == 16 || LANES == 64, "a row of lanes, or a wavefront");
+  v = group_sum(v);
+  if constexpr (LANES == 64) {
+    v += __shfl_xor(v, 16, 64);
+    v += __shfl_xor(v, 32, 64);
+  }
+  return v;
 }
 
 }  // namespace oapl

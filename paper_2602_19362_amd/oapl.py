@@ -7,6 +7,7 @@ the calls raise.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 from typing import NamedTuple, Optional
@@ -92,8 +93,8 @@ _SIGNATURES = {
     "oapl_residual_norm_bwd": (_c.c_int32, [_R, _R, _c.c_void_p, _R, _c.c_int32, _c.c_void_p, _R, _R, _c.c_int64] + [_c.c_int32] * 3 +
                                [_c.c_float] * 2 + [_R, _R] + [_c.c_void_p] * 2 + [_R] + [_c.c_void_p] * 2 + [_c.c_size_t, _c.c_void_p]),
     "oapl_clip_workspace_bytes": (_c.c_size_t, [_c.c_int32]),
-    "oapl_grad_norm": (_c.c_int32, [_c.POINTER(Tensor), _c.c_int32] + [_c.c_void_p] * 2 + [_c.c_size_t, _c.c_void_p]),
-    "oapl_clip_grads": (_c.c_int32, [_c.POINTER(Tensor), _c.c_int32, _c.c_float] + [_c.c_void_p] * 3 + [_c.c_size_t, _c.c_void_p]),
+    "oapl_grad_norm": (_c.c_int32, [_c.c_void_p, _c.c_int32] + [_c.c_void_p] * 2 + [_c.c_size_t, _c.c_void_p]),
+    "oapl_clip_grads": (_c.c_int32, [_c.c_void_p, _c.c_int32, _c.c_float] + [_c.c_void_p] * 3 + [_c.c_size_t, _c.c_void_p]),
     "oapl_read_device_status": (_c.c_int32, [_c.c_void_p, _c.c_void_p, _c.POINTER(_c.c_int32)]),
     "oapl_read_path_taken": (_c.c_int32, [_c.c_void_p, _c.c_void_p, _c.POINTER(_c.c_int32)]),
     "oapl_timing_enable": (_c.c_int32, [_c.c_int32]),
@@ -135,6 +136,9 @@ def lib():
             fn.argtypes = args
         _lib = handle
     return _lib
+
+
+_CODES = {torch.float32: OAPL_F32, torch.bfloat16: OAPL_BF16}
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -631,16 +635,16 @@ def attention_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.
 
 def _rows(t: torch.Tensor, name: str, shape, dtype: torch.dtype, index: int) -> Rows:
     """The oapl_rows of a tensor [rows, channels] on GPU `index` whose channels lie side by side."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == index:
+        row, channel = t.stride()
+        if channel == 1 or shape[1] <= 1 or shape[0] == 0:
+            return Rows(t.data_ptr(), row)
+        raise ValueError(f"the channels of {name} must lie side by side")
     if t.get_device() != index:
         raise ValueError(f"{name} must live on cuda:{index}")
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
-    row, channel = t.stride()
-    if channel != 1 and shape[1] > 1 and shape[0] > 0:
-        raise ValueError(f"the channels of {name} must lie side by side")
-    return Rows(t.data_ptr(), row)
+    raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
 def _gpu_of(t: torch.Tensor) -> int:
@@ -789,24 +793,23 @@ def residual_norm_bwd(x: torch.Tensor, y: Optional[torch.Tensor], dx_out: Option
     if y is not None and dy is None:
         dy = x.new_empty(shape, dtype=kind)
     dgate = x.new_empty(shape, dtype=kind) if per_token else None
-    sums, ws, at = [None] * 3, None, [None] * 3
-    wanted = (gain is not None, y_gain is not None, gate is not None and not per_token)
-    if any(wanted):
+    dgain = None if gain is None else x.new_empty(d, dtype=torch.float32)
+    dy_gain = None if y_gain is None else x.new_empty(d, dtype=torch.float32)
+    shared = None if gate is None or per_token else x.new_empty(d, dtype=torch.float32)
+    ws = None
+    if dgain is not None or dy_gain is not None or shared is not None:
         ws = _scratch(lib().oapl_residual_norm_workspace_bytes(T, d), x, workspace, "oapl_residual_norm_workspace_bytes")
-        all_sums = x.new_empty((3, d), dtype=torch.float32)
-        base = all_sums.data_ptr()
-        sums = [s if w else None for s, w in zip(all_sums.unbind(), wanted)]
-        at = [base + 4 * d * i if w else None for i, w in enumerate(wanted)]
     rc = lib().oapl_residual_norm_bwd(
         _rows(x, "x", shape, x.dtype, gpu), None if y is None else _rows(y, "y", shape, kind, gpu), _flat(y_gain, kind, "y_gain", gpu),
         gates, per_token, _flat(gain, kind, "gain", gpu), None if dx_out is None else _rows(dx_out, "dx_out", shape, x.dtype, gpu),
         None if dout is None else _rows(dout, "dout", shape, kind, gpu), T, d, _dtype_code(x), _dtype_code(gain if y is None else y),
-        scale, eps, _rows(dx, "dx", shape, x.dtype, gpu), None if y is None else _rows(dy, "dy", shape, kind, gpu), at[0], at[1],
-        None if dgate is None else _rows(dgate, "dgate", shape, kind, gpu), at[2], None if ws is None else ws.data_ptr(),
+        scale, eps, _rows(dx, "dx", shape, x.dtype, gpu), None if y is None else _rows(dy, "dy", shape, kind, gpu),
+        None if dgain is None else dgain.data_ptr(), None if dy_gain is None else dy_gain.data_ptr(),
+        None if dgate is None else _rows(dgate, "dgate", shape, kind, gpu), None if shared is None else shared.data_ptr(), None if ws is None else ws.data_ptr(),
         0 if ws is None else ws.numel(), _raw_stream(gpu))
     if rc != 0:
         raise OaplError(rc, "oapl_residual_norm_bwd")
-    return ResidualNormGrads(dx, dy, sums[0], sums[1], sums[2] if dgate is None else dgate, ws)
+    return ResidualNormGrads(dx, dy, dgain, dy_gain, shared if dgate is None else dgate, ws)
 
 
 def clip_workspace_bytes(n_tensors: int) -> int:
@@ -815,24 +818,27 @@ def clip_workspace_bytes(n_tensors: int) -> int:
 
 
 def _tensors(grads, out):
-    """The oapl_tensor list of dense tensors on the current GPU, and that GPU."""
+    """The oapl_tensor list of dense tensors on the current GPU, their number, and that GPU."""
     if len(grads) == 0:
         raise ValueError("there are no gradients")
     gpu = _gpu_of(grads[0])
-    into = grads if out is None else out
-    if len(into) != len(grads):
+    if out is not None and len(out) != len(grads):
         raise ValueError("out must have one tensor a gradient")
-    items = (Tensor * len(grads))()
-    for item, g, o in zip(items, grads, into):
-        item.dtype = _dtype_code(g)
-        item.n = g.numel()
-        item.data = at = _flat(g, g.dtype, "a gradient", gpu)
+    # four words a tensor: its address, the result's, how many elements, the type (whose other half is padding)
+    words = []
+    for g, o in zip(grads, grads if out is None else out):
+        kind, code = g.dtype, _CODES.get(g.dtype)
+        if code is None or not (g.is_contiguous() and g.get_device() == gpu):
+            _flat(g, kind, "a gradient", gpu)
+            _dtype_code(g)
+        at = to = g.data_ptr()
         if o is not g:
             if o.shape != g.shape:
                 raise ValueError("out must have the gradients' shapes")
-            at = _flat(o, g.dtype, "out", gpu)
-        item.out = at
-    return items, gpu
+            to = _flat(o, kind, "out", gpu)
+        words += (at, to, g.numel(), code)
+    words = array.array("q", words)
+    return words, len(grads), gpu
 
 
 class GradNorm(NamedTuple):
@@ -842,10 +848,10 @@ class GradNorm(NamedTuple):
 
 def grad_norm(grads, *, workspace: Optional[torch.Tensor] = None) -> GradNorm:
     """oapl_grad_norm: the norm of all gradients together (a list of contiguous tensors, float32 and bfloat16 mixed as they come)."""
-    items, gpu = _tensors(grads, None)
-    ws = _scratch(lib().oapl_clip_workspace_bytes(len(items)), grads[0], workspace, "oapl_clip_workspace_bytes")
+    words, n, gpu = _tensors(grads, None)
+    ws = _scratch(lib().oapl_clip_workspace_bytes(n), grads[0], workspace, "oapl_clip_workspace_bytes")
     norm = grads[0].new_empty(1, dtype=torch.float32)
-    rc = lib().oapl_grad_norm(items, len(items), norm.data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(gpu))
+    rc = lib().oapl_grad_norm(words.buffer_info()[0], n, norm.data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(gpu))
     if rc != 0:
         raise OaplError(rc, "oapl_grad_norm")
     return GradNorm(norm, ws)
@@ -857,17 +863,17 @@ def clip_grads(grads, max_norm: float, *, norm: Optional[torch.Tensor] = None, o
 
     Returns their norm before that.  `norm`: a norm to go by instead, [1] float32 (of gradients that are spread over GPUs, say).
     """
-    items, gpu = _tensors(grads, out)
+    words, n, gpu = _tensors(grads, out)
     ws, given, made = None, None, None
     if norm is None:
-        ws = _scratch(lib().oapl_clip_workspace_bytes(len(items)), grads[0], workspace, "oapl_clip_workspace_bytes")
+        ws = _scratch(lib().oapl_clip_workspace_bytes(n), grads[0], workspace, "oapl_clip_workspace_bytes")
         norm = grads[0].new_empty(1, dtype=torch.float32)
         made = norm.data_ptr()
     else:
         if norm.numel() != 1:
             raise ValueError("norm must be one number")
         given = _flat(norm, torch.float32, "norm", gpu)
-    rc = lib().oapl_clip_grads(items, len(items), max_norm, given, made, None if ws is None else ws.data_ptr(),
+    rc = lib().oapl_clip_grads(words.buffer_info()[0], n, max_norm, given, made, None if ws is None else ws.data_ptr(),
                                0 if ws is None else ws.numel(), _raw_stream(gpu))
     if rc != 0:
         raise OaplError(rc, "oapl_clip_grads")

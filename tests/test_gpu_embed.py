@@ -184,4 +184,4 @@ def test_refusals():
     with pytest.raises(TypeError):
         oapl.embed_bwd(E[:3], t, dE=torch.zeros(5, 8, device=DEV).bfloat16())
     with pytest.raises(oapl.OaplError):
-        oapl.embed_bwd(E[:3], t, 5, workspace=torch.zeros(256, device=DEV, dtype=torch.uint8))
+        oapl.embed_bwd(E[:3], t, 5, workspace=torch.zeros(255, device=DEV, dtype=torch.uint8))
