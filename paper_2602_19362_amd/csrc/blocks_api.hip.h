@@ -51,7 +51,9 @@ static bool embed_plan(EmbedPlan& p, int64_t T, int d, int V) {
     return was;
   };
   p.off_keys[1] = take(T * 4), p.off_places[1] = take(T * 4);
-  p.few = T <= kFewTokens;
+  // Counting / sorting, us for the whole call: fp32, d = 64, V = 1000: 6000 tokens 23 / 39, 8192 31 / 39, 12000 59 / 40; bf16, V = 1000, 8192 tokens: d = 1024 47 / 44, 4096 92 /
+  // 49 (a frequent token's rows are read by one workgroup a slice); 4096 at d = 4096, V = 1544 40 / 44.
+  p.few = T <= (d <= 512 ? kFewTokens : kFewTokens / 2);
   if (p.few) return true;
   while (((int64_t)1 << (2 * p.bits)) <= V) ++p.bits;      // ids 0 .. V
   p.items = T <= 128 * kSortThreads * 2 ? 2 : 8;
@@ -101,12 +103,13 @@ static int launch_embed_sort(const SortArgs& a, hipStream_t st) {
   const int bins = 1 << a.bits, bytes = (kSortThreads / 64 + 2) * bins * 4;
   if (bytes > 48 * 1024 && (!allow_big_lds(k_embed_place<0, ITEMS>, bytes) || !allow_big_lds(k_embed_place<1, ITEMS>, bytes)))
     return OAPL_ERR_HIP;
-  k_embed_count<ITEMS><<<a.blocks, kSortThreads, bins * 4, st>>>(a);
+  const int64_t all = a.dE && !a.clear_absent ? ((int64_t)a.V * a.d + 1023) / 1024 : 0;
+  k_embed_count<<<wide_grid(a.blocks + all, 1 << 23), 256, std::max(bins * 4, kClearLds), st>>>(a);
   OAPL_LAUNCH_CHECK();
   k_embed_place<0, ITEMS><<<a.blocks, kSortThreads, bytes, st>>>(a);
   OAPL_LAUNCH_CHECK();
-  const int64_t clear = a.dE ? (int64_t)grid1d(a.V, kSortThreads / 64) * grid1d(a.d, 1024) : 0;
-  k_embed_place<1, ITEMS><<<wide_grid(a.blocks + clear, 1 << 21), kSortThreads, bytes, st>>>(a);
+  const int64_t absent = a.dE && a.clear_absent ? (int64_t)grid1d(a.V, kSortThreads / 64) * grid1d(a.d, 1024) : 0;
+  k_embed_place<1, ITEMS><<<wide_grid(a.blocks + absent, 1 << 21), kSortThreads, bytes, st>>>(a);
   OAPL_LAUNCH_CHECK();
   return OAPL_OK;
 }
@@ -313,8 +316,8 @@ int32_t oapl_embed_bwd(const oapl_rows* dout, const int32_t* tokens, int64_t T, 
     OAPL_LAUNCH_CHECK();
     if (T == 0) return OAPL_OK;
     const dim3 runs(grid1d(T, 32), grid1d(d, 256));
-    if (dtype == OAPL_BF16) k_embed_runs<bf16_t><<<runs, 256, 0, st>>>(a);
-    else k_embed_runs<float><<<runs, 256, 0, st>>>(a);
+    if (dtype == OAPL_BF16) k_embed_runs<bf16_t><<<runs, 64 * kRunWaves, 0, st>>>(a);
+    else k_embed_runs<float><<<runs, 64 * kRunWaves, 0, st>>>(a);
     OAPL_LAUNCH_CHECK();
     return OAPL_OK;
   }
@@ -325,12 +328,16 @@ int32_t oapl_embed_bwd(const oapl_rows* dout, const int32_t* tokens, int64_t T, 
   for (int i = 0; i < 2; ++i) s.counts[i] = (int32_t*)(ws + p.off_counts[i]);
   s.present = (uint8_t*)(ws + p.off_present), s.status = (int*)ws;
   s.dE = accumulate ? nullptr : dE;
-  s.T = T, s.V = V, s.d = d, s.bits = p.bits, s.blocks = p.blocks;
+  s.T = T, s.V = V, s.d = d, s.bits = p.bits, s.block = kSortThreads * p.items, s.blocks = p.blocks;
+  // Rows without tokens alone are cleared where that leaves out enough: 140897 tokens, d = 4096, V = 151936 774 us, all rows 833; 50000, d = 1024 176, 182; 16000, d = 4096
+  // 482, 472; d = 256 (rows of 1 KB) 50000 92, 73.
+  s.clear_absent = d >= 1024 && 8 * T >= V;
   if (int rc = p.items == 2 ? launch_embed_sort<2>(s, st) : launch_embed_sort<8>(s, st)) return rc;
   a.partials = (float*)(ws + p.off_partials);
   a.tile = p.tile, a.tiles = p.tiles, a.slices = (int)grid1d(d, 1024);
   const unsigned grid = (unsigned)p.tiles * a.slices;
-  // Rows that the caches do not hold go past them: 140897 tokens, d = 4096 (1.15 GB) 785 -> 771 us; 4096 at V = 1544 (34 MB) 46 -> 60.
+  // Rows that the caches do not hold go past them: 140897 tokens, d = 4096 (1.15 GB) 785 -> 771 us, with rows of dE past them too 739;
+  // 4096 at V = 1544 (34 MB) 46 -> 60.  (Eight channels a lane and four rows under way: T = 140000, V = 1000 320 -> 282 us, this one 739 -> 781.)
   const bool once = past_caches(T * d * (int64_t)esize(dtype));
   if (dtype == OAPL_BF16 && once) k_embed_sum<bf16_t, true><<<grid, 256, 0, st>>>(a);
   else if (dtype == OAPL_BF16) k_embed_sum<bf16_t, false><<<grid, 256, 0, st>>>(a);

@@ -57,9 +57,10 @@ struct SortArgs {
   int32_t* counts[2];               // [blocks][1 << bits]
   uint8_t* present;                 // [V]: whether an id occurs
   int* status;
-  float* dE;                        // to be cleared where no id occurs, beside the second pass; nullptr: not
+  float* dE;                        // to be cleared: beside the counting, or only where no id occurs, beside the second pass
+  bool clear_absent;
   int64_t T;
-  int V, d, bits, blocks;
+  int V, d, bits, block, blocks;    // keys of a block, and how many of them
 };
 
 __device__ __forceinline__ int sort_key(const SortArgs& p, int64_t t) {
@@ -67,24 +68,39 @@ __device__ __forceinline__ int sort_key(const SortArgs& p, int64_t t) {
   return v >= 0 && v < p.V ? v : p.V;
 }
 
-// First pass's counts; the second's, and `present`, start at zero.
-template <int ITEMS>
-__global__ __launch_bounds__(kSortThreads) void k_embed_count(const SortArgs p) {
-  extern __shared__ int32_t count[];
-  const int bins = 1 << p.bits;
-  for (int i = threadIdx.x; i < bins; i += kSortThreads) count[i] = 0;
-  __syncthreads();
-  const int64_t from = (int64_t)blockIdx.x * kSortThreads * ITEMS;
-  for (int i = 0; i < ITEMS; ++i) {
-    const int64_t t = from + i * kSortThreads + threadIdx.x;
-    if (t < p.T) atomicAdd(&count[sort_key(p, t) & (bins - 1)], 1);
+// 1024 elements of dE, from 1024 i on, are zero: 4 KB a workgroup, and four workgroups a compute unit, which kClearLds bytes of LDS see to, is the
+// order that memory likes best (2.49 GB in 357 us, 6.98 TB/s; 16 KB a workgroup 402, 256 KB 400 .. 430; beside the counting of 6000 tokens, eight
+// workgroups 431, six 425, four 409).
+constexpr int kClearLds = 33 * 1024;
+__device__ __forceinline__ void clear_piece(float* dE, int64_t n, int64_t i) {
+  const int64_t at = (i * 256 + threadIdx.x) * 4;
+  if (at + 4 <= n) {
+    store_whole<4>(dE + at, Piece<4>{});
+  } else {
+    for (int64_t e = at; e < n; ++e) dE[e] = 0.f;
   }
+}
+
+// First pass's counts; the second's, and `present`, start at zero.  The workgroups behind clear dE.
+__global__ __launch_bounds__(256) void k_embed_count(const SortArgs p) {
+  extern __shared__ int32_t count[];
+  if ((int)blockIdx.x >= p.blocks || blockIdx.y > 0) {
+    clear_piece(p.dE, (int64_t)p.V * p.d, (int64_t)blockIdx.y * gridDim.x + blockIdx.x - p.blocks);
+    return;
+  }
+  const int bins = 1 << p.bits;
+  for (int i = threadIdx.x; i < bins; i += 256) count[i] = 0;
   __syncthreads();
-  for (int i = threadIdx.x; i < bins; i += kSortThreads) {
+  const int64_t from = (int64_t)blockIdx.x * p.block, to = from + p.block < p.T ? from + p.block : p.T;
+#pragma unroll 8
+  for (int64_t t = from + threadIdx.x; t < to; t += 256) atomicAdd(&count[sort_key(p, t) & (bins - 1)], 1);
+  __syncthreads();
+  for (int i = threadIdx.x; i < bins; i += 256) {
     p.counts[0][(int64_t)blockIdx.x * bins + i] = count[i];
     p.counts[1][(int64_t)blockIdx.x * bins + i] = 0;
   }
-  for (int64_t i = (int64_t)blockIdx.x * kSortThreads + threadIdx.x; i < p.V; i += (int64_t)gridDim.x * kSortThreads) p.present[i] = 0;
+  if (p.clear_absent)
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.V; i += (int64_t)p.blocks * 256) p.present[i] = 0;
   if (blockIdx.x == 0 && threadIdx.x < kStatusWords) p.status[threadIdx.x] = 0;
 }
 
@@ -192,7 +208,7 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_place(const SortArgs p) 
       if (any && at != with) atomicAdd(&p.counts[1][at], 1);
       if (any && lane == first[i]) atomicAdd(&p.counts[1][at], __popcll(together));
       if (any && lane == first[i] && key[i] == p.V) atomicExch(p.status, kErrTokenRange);
-      if (any && key[i] < p.V) p.present[key[i]] = 1;
+      if (p.clear_absent && any && key[i] < p.V) p.present[key[i]] = 1;
     }
   }
 }
@@ -208,6 +224,8 @@ struct EmbedSumArgs {
   bool add;                         // to what dE holds
 };
 
+// A row's sum into dE.  ONCE: past the caches.
+template <bool ONCE = false>
 __device__ __forceinline__ void put_row(const EmbedSumArgs& p, int64_t v, int c, Piece<4> sum) {
   float* row = p.dE + v * p.d;
 #pragma unroll
@@ -217,21 +235,21 @@ __device__ __forceinline__ void put_row(const EmbedSumArgs& p, int64_t v, int c,
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum.v[e] += old.v[e];
   }
-  store_piece<4>(row, c, p.d, sum);
+  store_piece<4, ONCE>(row, c, p.d, sum);
 }
 
 // Rows of dout whose loads are under way together.
 constexpr int kEmbedRows = 8;
 
 // The sum of `n` of 64 rows, from the i-th on, whose positions a wavefront's lanes have.
-template <class T>
+template <class T, int ROWS>
 __device__ __forceinline__ void add_rows(const EmbedSumArgs& p, Piece<4>& sum, int place, int i, int n, int c) {
-  Piece<4> x[kEmbedRows] = {};
+  Piece<4> x[ROWS] = {};
 #pragma unroll
-  for (int u = 0; u < kEmbedRows; ++u)
+  for (int u = 0; u < ROWS; ++u)
     if (u < n) x[u] = load_piece<4>(p.dout.row<T>(__builtin_amdgcn_readlane(place, i + u)), c, p.d);
 #pragma unroll
-  for (int u = 0; u < kEmbedRows; ++u)
+  for (int u = 0; u < ROWS; ++u)
     if (u < n) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum.v[e] += x[u].v[e];
@@ -239,7 +257,7 @@ __device__ __forceinline__ void add_rows(const EmbedSumArgs& p, Piece<4>& sum, i
 }
 
 // A workgroup sums up 1024 channels, four a lane, of a tile's rows; the slices of a tile run side by side.  A wavefront has the ids and
-// positions of 64 rows in its lanes, so that its walk over them branches on scalars.  ONCE: rows past the caches.
+// positions of 64 rows in its lanes, so that its walk over them branches on scalars.  ONCE: rows past the caches, in and out.
 template <class T, bool ONCE>
 __global__ __launch_bounds__(256) void k_embed_sum(const EmbedSumArgs p) {
   const int lane = threadIdx.x & 63, tile = blockIdx.x / p.slices, c = (blockIdx.x % p.slices * 256 + threadIdx.x) * 4;
@@ -267,7 +285,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(const EmbedSumArgs p) {
         const int v = __builtin_amdgcn_readlane(key, i + u);
         if (begun && v == first) store_piece<4>(p.partials + (int64_t)tile * 2 * p.d, c, p.d, sum);
         else if (open && v == last) store_piece<4>(p.partials + ((int64_t)tile * 2 + 1) * p.d, c, p.d, sum);
-        else if (v < p.V) put_row(p, v, c, sum);
+        else if (v < p.V) put_row<ONCE>(p, v, c, sum);
         sum = Piece<4>{};
       }
     }
@@ -325,25 +343,14 @@ __global__ __launch_bounds__(64 * kJoinParts) void k_embed_join(const EmbedSumAr
 }
 
 // ---------------------------------------------------------------------------------------------------------------- gradient: few tokens
-constexpr int kFewTokens = 4096, kRankTokens = 8, kRankParts = 256 / kRankTokens;
-
-// 1024 elements of dE, from 1024 i on, are zero.
-__device__ __forceinline__ void clear_piece(const EmbedSumArgs& p, int64_t i) {
-  const int64_t at = (i * 256 + threadIdx.x) * 4, n = (int64_t)p.V * p.d;
-  if (at + 4 <= n) {
-    store_whole<4>(p.dE + at, Piece<4>{});
-  } else {
-    for (int64_t e = at; e < n; ++e) p.dE[e] = 0.f;
-  }
-}
+constexpr int kFewTokens = 8192, kRankTokens = 8, kRankParts = 256 / kRankTokens;
 
 // Sorting without passes: a token's place is the number of those with smaller ids, and of earlier ones with its own.  A workgroup finds the
-// places of 32 tokens, each 32 lanes among an eighth of all.  The workgroups behind clear dE, 4 KB each, which is the order that memory
-// likes best (2.49 GB in 357 us; 16 KB a workgroup 402, 256 KB 400 .. 430).
+// places of 32 tokens, each 32 lanes among an eighth of all.  The workgroups behind clear dE.
 __global__ __launch_bounds__(256) void k_embed_rank(const EmbedSumArgs p, const int32_t* __restrict__ tokens, int32_t* keys, int32_t* places,
                                                     int* status, int sorters) {
   if ((int)blockIdx.x >= sorters || blockIdx.y > 0) {
-    clear_piece(p, (int64_t)blockIdx.y * gridDim.x + blockIdx.x - sorters);
+    clear_piece(p.dE, (int64_t)p.V * p.d, (int64_t)blockIdx.y * gridDim.x + blockIdx.x - sorters);
     return;
   }
   __shared__ int4 all4[kFewTokens / 4];
@@ -354,11 +361,22 @@ __global__ __launch_bounds__(256) void k_embed_rank(const EmbedSumArgs p, const 
   if (threadIdx.x == 0) outside = 0;
   __syncthreads();
 #pragma unroll 8
-  for (int t = threadIdx.x; t < padded; t += 256) {
-    const int v = t < T ? tokens[t] : 0;
-    const bool good = v >= 0 && v < p.V;
-    all[t] = t < T ? (good ? v : p.V) : INT32_MAX;       // smaller than no id
-    if (!good) outside = 1;
+  for (int t = threadIdx.x * 4; t < padded; t += 1024) {
+    int4 k = {-1, -1, -1, -1};
+    if (t + 4 <= T) {
+      __builtin_memcpy(&k, tokens + t, 16);
+    } else {
+      if (t < T) k.x = tokens[t];
+      if (t + 1 < T) k.y = tokens[t + 1];
+      if (t + 2 < T) k.z = tokens[t + 2];
+    }
+    const auto key = [&](int v, int at) {
+      if (at >= T) return INT32_MAX;                       // smaller than no id
+      if (v >= 0 && v < p.V) return v;
+      outside = 1;
+      return p.V;
+    };
+    all4[t / 4] = int4{key(k.x, t), key(k.y, t + 1), key(k.z, t + 2), key(k.w, t + 3)};
   }
   __syncthreads();
   const int t0 = blockIdx.x * kRankTokens, t = t0 + threadIdx.x % kRankTokens, part = threadIdx.x / kRankTokens;
@@ -387,11 +405,13 @@ __global__ __launch_bounds__(256) void k_embed_rank(const EmbedSumArgs p, const 
   if (blockIdx.x == 0 && threadIdx.x < kStatusWords) status[threadIdx.x] = threadIdx.x == 0 && outside ? kErrTokenRange : 0;
 }
 
-// Sums of the sorted rows: a workgroup has 32 of them and 256 channels, each wavefront the tokens that begin among 8; one that goes on
-// behind the 32 is shared by the four wavefronts, a quarter of its rows each, which are added in their order.
+// Sums of the sorted rows: a workgroup has 32 of them and 256 channels, each wavefront the tokens that begin among a few; one that goes on
+// behind the 32 is shared by the wavefronts, equal parts of its rows each, which are added in their order.
+constexpr int kRunWaves = 8, kRunRows = 32 / kRunWaves;
+
 template <class T>
-__global__ __launch_bounds__(256) void k_embed_runs(const EmbedSumArgs p) {
-  __shared__ Piece<4> quarter[4][64];
+__global__ __launch_bounds__(64 * kRunWaves) void k_embed_runs(const EmbedSumArgs p) {
+  __shared__ Piece<4> parts[kRunWaves][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (blockIdx.y * 64 + lane) * 4;
   const int from = blockIdx.x * 32, n = (int)p.T - from < 32 ? (int)p.T - from : 32;
   const int key = lane < n ? p.keys[from + lane] : -1, place = lane < n ? p.places[from + lane] : 0;
@@ -400,9 +420,9 @@ __global__ __launch_bounds__(256) void k_embed_runs(const EmbedSumArgs p) {
   const uint64_t begins = __ballot(lane < n && key != before);
   const bool on = behind >= 0 && behind == __builtin_amdgcn_readlane(key, n - 1);
   const int last = begins ? 63 - __clzll(begins) : n;          // the last token that begins here
-  const uint64_t ours = begins & (uint64_t)0xff << (8 * wave), after = begins >> (8 * wave) >> 8;
+  const uint64_t ours = begins & (((uint64_t)1 << kRunRows) - 1) << (kRunRows * wave), after = begins >> (kRunRows * wave) >> kRunRows;
   // from the first token that begins here to the end of the last one that does not go on behind the 32
-  int i = ours ? __ffsll((unsigned long long)ours) - 1 : n, end = after ? 8 * wave + 7 + __ffsll((unsigned long long)after) : on ? last : n;
+  int i = ours ? __ffsll((unsigned long long)ours) - 1 : n, end = after ? kRunRows * (wave + 1) - 1 + __ffsll((unsigned long long)after) : on ? last : n;
   Piece<4> sum = {};
   while (i < end) {
     Piece<4> x[kEmbedRows] = {};
@@ -429,19 +449,19 @@ __global__ __launch_bounds__(256) void k_embed_runs(const EmbedSumArgs p) {
     end += other ? __ffsll((unsigned long long)other) - 1 : 64;
     if (other) break;
   }
-  const int begin = from + last, rows = end - begin, lo = begin + rows * wave / 4, hi = begin + rows * (wave + 1) / 4;
+  const int begin = from + last, rows = end - begin, lo = begin + rows * wave / kRunWaves, hi = begin + rows * (wave + 1) / kRunWaves;
   sum = Piece<4>{};
   for (int base = lo; base < hi; base += 64) {
     const int at = base + lane < hi ? p.places[base + lane] : 0, here = hi - base < 64 ? hi - base : 64;
-    for (int i = 0; i < here; i += kEmbedRows) add_rows<T>(p, sum, at, i, here - i, c);
+    for (int i = 0; i < here; i += 2 * kEmbedRows) add_rows<T, 2 * kEmbedRows>(p, sum, at, i, here - i, c);
   }
-  quarter[wave][lane] = sum;
+  parts[wave][lane] = sum;
   __syncthreads();
   if (wave > 0) return;
 #pragma unroll
-  for (int w = 1; w < 4; ++w)
+  for (int w = 1; w < kRunWaves; ++w)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum.v[e] += quarter[w][lane].v[e];
+    for (int e = 0; e < 4; ++e) sum.v[e] += parts[w][lane].v[e];
   put_row(p, v, c, sum);
 }
 
