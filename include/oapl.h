@@ -496,7 +496,7 @@ typedef struct {
  *   E        [V][d] in dtype (may be the head's W), from any element on
  *   tokens   [T] int32 in [0, V); a token outside gets NaN
  *   out      [T][d] in out_dtype
- *   0 <= T <= 65535 * 256, 1 <= d, V <= 2^21 (else OAPL_ERR_SHAPE), scale finite (else OAPL_ERR_BETA)
+ *   0 <= T <= 65535 * 256, 1 <= d, V <= 2^21, T d <= 2^40 (else OAPL_ERR_SHAPE), scale finite (else OAPL_ERR_BETA)
  * Needs no workspace.
  */
 int32_t oapl_embed_fwd(const void* E, const int32_t* tokens, int64_t T, int32_t d, int32_t V, int32_t dtype, int32_t out_dtype,
@@ -533,7 +533,8 @@ int32_t oapl_embed_bwd(const oapl_rows* dout, const int32_t* tokens, int64_t T, 
  *   gate       NULL; rows [T][d] in dtype (gate_per_token not 0); or [d], the same for all tokens (gate_per_token 0)
  *   x_dtype    dtype, or OAPL_F32 with blocks in OAPL_BF16 (else OAPL_ERR_DTYPE)
  *   0 <= T <= 65535 * 256, 1 <= d <= 16384 (else OAPL_ERR_SHAPE); eps >= 0, eps and scale finite (else OAPL_ERR_BETA)
- * What is not finite in a row stays in that row.  Needs no workspace.
+ * A row's squares are summed in 32 bits: the sum has to stay below 3.4e38.  What is not finite in a row stays in that row.  Needs no
+ * workspace.
  */
 int32_t oapl_residual_norm_fwd(const oapl_rows* x, const oapl_rows* y, const void* y_gain, const oapl_rows* gate, int32_t gate_per_token,
                                const void* gain, int64_t T, int32_t d, int32_t x_dtype, int32_t dtype, float scale, float eps,
@@ -581,7 +582,7 @@ size_t oapl_clip_workspace_bytes(int32_t n_tensors);
  * The norm of all tensors together:   norm = sqrt(sum over tensors and their elements g^2)
  *
  * Squares and their sum in 64 bits, in a fixed order; rounded to 32 bits once.
- *   n_tensors  0 .. 2^20, of less than 2^45 elements in all (else OAPL_ERR_SHAPE); tensors may be empty
+ *   n_tensors  0 .. 2^20, of at most 2^42 elements in all (else OAPL_ERR_SHAPE); tensors may be empty
  *   norm       [1] float
  */
 int32_t oapl_grad_norm(const oapl_tensor* tensors, int32_t n_tensors, float* norm, void* workspace, size_t workspace_bytes,

@@ -39,7 +39,7 @@ struct EmbedPlan {
 };
 
 static bool embed_sizes_ok(int64_t T, int d, int V) {
-  return T >= 0 && T <= kMaxRows && d >= 1 && d <= (1 << 21) && V >= 1 && V <= (1 << 21);
+  return T >= 0 && T <= kMaxRows && d >= 1 && d <= (1 << 21) && V >= 1 && V <= (1 << 21) && T * d <= (int64_t)1 << 40;
 }
 
 static bool embed_plan(EmbedPlan& p, int64_t T, int d, int V) {
@@ -86,7 +86,6 @@ static int launch_embed_fwd(EmbedArgs a, hipStream_t st) {
     a.slices = grid1d(a.d, 64 * W * PIECES);
     k_embed_fwd<TE, T, W, PIECES, ONCE><<<wide_grid((a.T * a.slices + 3) / 4, 1 << 23), 256, 0, st>>>(a);
   };
-  if (a.T * grid1d(a.d, 64 * W) >= (int64_t)1 << 31) return OAPL_ERR_SHAPE;      // 2 TB and more
   const auto by_size = [&](auto once) {
     // 140000 rows of 256 channels in bf16, one piece a wavefront / two: 27 / 35 us; 20000 of 520 9.5 / 9.1
     if (a.d <= 64 * W) launch(std::integral_constant<int, 1>{}, once);

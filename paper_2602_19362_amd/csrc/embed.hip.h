@@ -2,10 +2,14 @@
 //
 //   out_t = scale E[tok_t],      dE[v] = scale sum over t with tok_t = v of dout_t
 //
-// Bound by memory.  The gradient's sums have a fixed order.  Few tokens: workgroups that have a share of dE's rows look through all of them.
-// Many: they are sorted by id (stably, so by position among equals), the sorted positions cut into tiles of equal length, so that a frequent
-// token is shared by many workgroups; what a tile has of a token that reaches over its ends goes into the workspace and is added up by
-// another launch, tile by tile.
+// Bound by memory.  The gradient's sums have a fixed order: tokens are sorted by id, stably, so by position among equals.  Few of them are sorted
+// by counting (k_embed_rank) and summed by the workgroup that a token's rows begin in (k_embed_runs): two launches.  Many are sorted in two
+// passes (k_embed_count, k_embed_place twice), and their sorted positions cut into tiles of equal length, so that a frequent token is shared by
+// many workgroups (k_embed_sum); what a tile has of a token that reaches over its ends goes into the workspace and is added up by another
+// launch, tile by tile (k_embed_join).  dE is cleared beside the sorting, not between reads: memory takes 6 TB/s of either alone and 4.9 of both.
+//
+// 140897 tokens that follow Zipf's law, d = 4096 in bf16, V = 151936 (3.6 GB): counting 6 us, first pass 26, second pass and 1.9 GB of zeros 308, sums
+// 380 (1.15 GB in, 0.65 out: 4.8 TB/s), tokens over tiles 23.  1003 of them: places and 2.49 GB of zeros 350, sums 10.
 #pragma once
 
 #include "rows.hip.h"
@@ -292,8 +296,9 @@ __global__ __launch_bounds__(256) void k_embed_sum(const EmbedSumArgs p) {
   }
 }
 
-// Tokens that reach over the ends of tiles: where one ends in one of a workgroup's 16 tiles, its four wavefronts add up what the tiles have
-// of it, a quarter of them each, in their order and in 64 bits.
+// Tokens that reach over the ends of tiles: where one ends in one of a workgroup's tiles, its wavefronts add up what the tiles have of it,
+// equal parts of them each, in their order and in 64 bits.  Tiles and wavefronts of a workgroup 4 and 4 / 4 and 8 / 16 and 8 / 16 and 16, whole call of
+// 140897 tokens: 783 / 807 / 804 / 885 us.
 constexpr int kJoinTiles = 4, kJoinParts = 4;
 
 __global__ __launch_bounds__(64 * kJoinParts) void k_embed_join(const EmbedSumArgs p) {
@@ -346,7 +351,8 @@ __global__ __launch_bounds__(64 * kJoinParts) void k_embed_join(const EmbedSumAr
 constexpr int kFewTokens = 8192, kRankTokens = 8, kRankParts = 256 / kRankTokens;
 
 // Sorting without passes: a token's place is the number of those with smaller ids, and of earlier ones with its own.  A workgroup finds the
-// places of 32 tokens, each 32 lanes among an eighth of all.  The workgroups behind clear dE.
+// places of eight tokens, each among 32 parts of all (32 tokens and 8 parts, 16 and 16, 8 and 32, of 4096: 14.8 / 10.7 / 9.0 us, of 1501 7.2 / 5.9 / 5.2).  The
+// workgroups behind clear dE; the LDS of the others' tokens lets four of them run on a compute unit.
 __global__ __launch_bounds__(256) void k_embed_rank(const EmbedSumArgs p, const int32_t* __restrict__ tokens, int32_t* keys, int32_t* places,
                                                     int* status, int sorters) {
   if ((int)blockIdx.x >= sorters || blockIdx.y > 0) {
@@ -406,7 +412,8 @@ __global__ __launch_bounds__(256) void k_embed_rank(const EmbedSumArgs p, const 
 }
 
 // Sums of the sorted rows: a workgroup has 32 of them and 256 channels, each wavefront the tokens that begin among a few; one that goes on
-// behind the 32 is shared by the wavefronts, equal parts of its rows each, which are added in their order.
+// behind the 32 is shared by the wavefronts, equal parts of its rows each, which are added in their order.  Eight wavefronts / four: 4096 tokens, d = 64,
+// V = 1000 17.7 / 22.3 us for the whole call.
 constexpr int kRunWaves = 8, kRunRows = 32 / kRunWaves;
 
 template <class T>

@@ -27,7 +27,9 @@ def tensors(sizes, types="mixed", seed=0):
     return [(torch.randn(n, generator=g, device=DEV) * 10.0 ** (i % 5 - 3)).to(kinds[i % len(kinds)]) for i, n in enumerate(sizes)]
 
 
-SIZES = [[1], [7], [0], [0, 5, 0], [16384], [16383, 16385, 1, 32768], [100003, 12, 3], [256] * 97, [33, 8, 1] * 131, [3000001, 5, 70000]]
+SIZES = [[1], [7], [0], [0, 5, 0], [16384], [16383, 16385, 1, 32768], [100003, 12, 3], [256] * 97, [33, 8, 1] * 131, [3000001, 5, 70000],
+         # the norm in a launch of its own, from one list and from two; what does not fit the caches
+         [17000000, 3], [150001] * 113, [70000001, 2049], [40000000] * 3]
 
 
 @pytest.mark.parametrize("types", ["f32", "bf16", "mixed"])
@@ -112,6 +114,15 @@ def test_the_list_may_go_when_the_call_returns():
         wants.append((oapl.grad_norm(mine).norm, orc.grad_norm(mine)))
     for got, (want, bound) in wants:
         near(got, want, bound)
+
+
+@pytest.mark.parametrize("count", [1, 112, 113, 300])
+def test_nothing_beside_the_workspace_is_touched(count):
+    n = oapl.clip_workspace_bytes(count)
+    room = torch.full((n + 512,), 0x5a, dtype=torch.uint8, device=DEV)
+    grads = tensors([3000] * count)
+    near(oapl.clip_grads(grads, 1e-3, workspace=room[256:256 + n]).norm, *orc.grad_norm(tensors([3000] * count)))
+    assert bool((room[:256] == 0x5a).all()) and bool((room[256 + n:] == 0x5a).all())
 
 
 def test_refusals():

@@ -36,7 +36,9 @@ def near(got, want, bound):
 
 @pytest.mark.parametrize("dtype, out, T, d, V, scale", [
     ("bf16", "bf16", 1, 8, 1, 1.0), ("bf16", "bf16", 64, 4096, 1000, 1.0), ("bf16", "f32", 37, 520, 300, 22.6), ("f32", "f32", 5, 7, 3, -0.3),
-    ("f32", "bf16", 333, 65, 50, 3.0), ("bf16", "bf16", 3001, 1, 9, 0.1), ("f32", "f32", 70001, 12, 2000, 1.7), ("bf16", "bf16", 3, 8200, 5, 0.0)])
+    ("f32", "bf16", 333, 65, 50, 3.0), ("bf16", "bf16", 3001, 1, 9, 0.1), ("f32", "f32", 70001, 12, 2000, 1.7), ("bf16", "bf16", 3, 8200, 5, 0.0),
+    # results past the caches
+    ("bf16", "bf16", 140000, 1000, 3000, 1.1), ("f32", "f32", 70000, 1001, 3000, 0.9), ("bf16", "f32", 300000, 250, 300, 1.0)])
 def test_lookup(dtype, out, T, d, V, scale):
     E = torch.randn(V, d, generator=_gen(1), device=DEV).to(DTYPES[dtype])
     tokens = _tokens("even", T, V)
@@ -125,6 +127,20 @@ def test_gradient_from_and_into_parts_of_buffers(T):
         # one row for all tokens
         row = wide[:1, 5:78].expand(T, 73)
         near(oapl.embed_bwd(row, tokens, 60).dE, *orc.embed_grads(row, tokens, 60, 1.0))
+
+
+@pytest.mark.parametrize("T, d, V", [(0, 8, 3), (5, 24, 60), (8000, 40, 300), (9000, 72, 3000), (9000, 1024, 3000)])
+def test_nothing_beside_the_buffers_is_touched(T, d, V):
+    """A workspace of the bytes that the call asks for, and dE, inside larger buffers."""
+    n = oapl.embed_workspace_bytes(T, d, V)
+    room = torch.full((n + 512,), 0x5a, dtype=torch.uint8, device=DEV)
+    flat = torch.full((V * d + 64,), 7.0, device=DEV)
+    tokens = _tokens("zipf", T, V)
+    dout = torch.randn(T, d, generator=_gen(11), device=DEV)
+    oapl.embed_bwd(dout, tokens, dE=flat[32:-32].view(V, d), workspace=room[256:256 + n])
+    near(flat[32:-32].view(V, d), *orc.embed_grads(dout, tokens, V, 1.0))
+    assert bool((room[:256] == 0x5a).all()) and bool((room[256 + n:] == 0x5a).all())
+    assert bool((flat[:32] == 7).all()) and bool((flat[-32:] == 7).all())
 
 
 def test_what_is_not_finite_stays_in_its_row():

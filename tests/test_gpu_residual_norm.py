@@ -63,7 +63,9 @@ PARTS = ["pre", "block", "pre block", "pre block post", "block post", "pre block
          "pre block post token", "block post channel"]
 # widths: a wavefront and four rows a workgroup, a workgroup a row, ends inside a piece of eight channels, more lanes than channels
 SHAPES = [(1, 8), (5, 64), (3, 100), (9, 512), (4, 513), (6, 1000), (2, 1024), (3, 1025), (5, 2048), (2, 2056), (3, 4096), (2, 5120), (1, 8192),
-          (2, 8201), (3, 16384), (700, 72), (2100, 40), (5, 1), (1, 7), (3, 3000)]
+          (2, 8201), (3, 16384), (700, 72), (2100, 40), (5, 1), (1, 7), (3, 3000),
+          # more rows than workgroups have room for at once
+          (9001, 24), (2500, 300), (1300, 700), (600, 2000), (300, 3000), (300, 8000), (270, 10000)]
 
 
 @pytest.mark.parametrize("types", list(TYPES))
@@ -153,6 +155,15 @@ def test_rows_of_zeros_and_of_large_and_small_numbers(types):
     check_forward(v, 1.0)
     check_backward(v, dx_out, dout, 1.0)
     check_forward(v, 1.0, eps=0.01)
+
+
+@pytest.mark.parametrize("T, d", [(1, 40), (9000, 100), (300, 4096), (260, 9000)])
+def test_nothing_beside_the_workspace_is_touched(T, d):
+    n = oapl.residual_norm_workspace_bytes(T, d)
+    room = torch.full((n + 512,), 0x5a, dtype=torch.uint8, device=DEV)
+    v, dx_out, dout = inputs("mixed", T, d, ["pre", "block", "post", "channel"])
+    check_backward(v, dx_out, dout, 1.0, workspace=room[256:256 + n])
+    assert bool((room[:256] == 0x5a).all()) and bool((room[256 + n:] == 0x5a).all())
 
 
 def test_no_tokens():
