@@ -74,25 +74,32 @@ static dim3 wide_grid(int64_t n, int64_t most) {
   return dim3((unsigned)std::min(n, most), (unsigned)((n + most - 1) / most));
 }
 
+// f(true or false as a type).
+template <class F>
+static void by_truth(bool x, F f) {
+  if (x) f(std::true_type{});
+  else f(std::false_type{});
+}
+
 // Accesses of so many bytes go past the caches: the memory-side one holds 256 MiB.
 static bool past_caches(int64_t bytes) { return bytes > (int64_t)256 << 20; }
 
 template <class TE, class T>
 static int launch_embed_fwd(EmbedArgs a, hipStream_t st) {
   constexpr int W = sizeof(TE) + sizeof(T) == 4 ? 8 : 4;
-  const auto launch = [&](auto pieces, auto once) {
+  const auto launch = [&](auto pieces, auto whole, auto once) {
     constexpr int PIECES = pieces;
-    constexpr bool ONCE = once;
+    constexpr bool WHOLE = whole, ONCE = once;
     a.slices = grid1d(a.d, 64 * W * PIECES);
-    k_embed_fwd<TE, T, W, PIECES, ONCE><<<wide_grid((a.T * a.slices + 3) / 4, 1 << 23), 256, 0, st>>>(a);
+    k_embed_fwd<TE, T, W, PIECES, WHOLE, ONCE><<<wide_grid((a.T * a.slices + 3) / 4, 1 << 23), 256, 0, st>>>(a);
   };
-  const auto by_size = [&](auto once) {
-    // 140000 rows of 256 channels in bf16, one piece a wavefront / two: 27 / 35 us; 20000 of 520 9.5 / 9.1
-    if (a.d <= 64 * W) launch(std::integral_constant<int, 1>{}, once);
-    else launch(std::integral_constant<int, 2>{}, once);
-  };
-  if (past_caches(a.T * a.d * (int64_t)sizeof(T))) by_size(std::true_type{});
-  else by_size(std::false_type{});
+  by_truth(a.d % W == 0, [&](auto whole) {
+    by_truth(past_caches(a.T * a.d * (int64_t)sizeof(T)), [&](auto once) {
+      // 140000 rows of 256 channels in bf16, one piece a wavefront / two: 27 / 35 us; 20000 of 520 9.5 / 9.1
+      if (a.d <= 64 * W) launch(std::integral_constant<int, 1>{}, whole, once);
+      else launch(std::integral_constant<int, 2>{}, whole, once);
+    });
+  });
   OAPL_LAUNCH_CHECK();
   return OAPL_OK;
 }
@@ -114,22 +121,23 @@ static int launch_embed_sort(const SortArgs& a, hipStream_t st) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------- residual stream
-// How many lanes hold a row of d channels, W in a piece: f(lanes, pieces a lane).  Eight channels a lane, 16 where there are no more lanes:
+// How a row of d channels is held, W in a piece: f(lanes of a row, or 0 for a workgroup's; lanes of a workgroup at most; pieces a lane).  Eight channels a
+// lane, 16 where there are no more lanes:
 // 16411 rows of 4096 in bf16 with 8 / 16 / 32 / 64 forward 92 / 97 / 107 / 158 us (workgroups that take row after row 101 .. 111), 3000 of 8192
 // 36 / 40 / 47 / 66, 8000 of 4096 in fp32 97 / 102 / 121 / 164.
 template <int W, class F>
 static void by_width(int d, F f) {
   constexpr std::integral_constant<int, 8 / W> eight{};
-  if (d <= 16 * 8) return f(std::integral_constant<int, 16>{}, eight);
-  if (d <= 64 * 8) return f(std::integral_constant<int, 64>{}, eight);
-  if (d <= 128 * 8) return f(std::integral_constant<int, 128>{}, eight);
-  if (d <= 256 * 8) return f(std::integral_constant<int, 256>{}, eight);
-  if (d <= 512 * 8) return f(std::integral_constant<int, 512>{}, eight);
-  if (d <= 1024 * 8) return f(std::integral_constant<int, 1024>{}, eight);
-  return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 16 / W>{});
+  constexpr std::integral_constant<int, 0> workgroup{};
+  if (d <= 16 * 8) return f(std::integral_constant<int, 16>{}, std::integral_constant<int, 256>{}, eight);
+  if (d <= 64 * 8) return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 256>{}, eight);
+  if (d <= 512 * 8) return f(workgroup, std::integral_constant<int, 512>{}, eight);
+  if (d <= 768 * 8) return f(workgroup, std::integral_constant<int, 768>{}, eight);
+  if (d <= 1024 * 8) return f(workgroup, std::integral_constant<int, 1024>{}, eight);
+  return f(workgroup, std::integral_constant<int, 1024>{}, std::integral_constant<int, 16 / W>{});
 }
 // Lanes of a workgroup, and the rows they hold.
-static int norm_lanes(int d) { return d <= 512 || (d > 1024 && d <= 2048) ? 256 : d <= 1024 ? 128 : d <= 4096 ? 512 : 1024; }
+static int norm_lanes(int d) { return d <= 512 ? 256 : (int)round_up((d + (d <= 8192 ? 8 : 16) - 1) / (d <= 8192 ? 8 : 16), 64); }
 static int norm_rows(int d) { return d <= 128 ? 16 : d <= 512 ? 4 : 1; }
 static int64_t norm_workgroups(int64_t T, int d) { return (T + norm_rows(d) - 1) / norm_rows(d); }
 
@@ -315,8 +323,11 @@ int32_t oapl_embed_bwd(const oapl_rows* dout, const int32_t* tokens, int64_t T, 
     OAPL_LAUNCH_CHECK();
     if (T == 0) return OAPL_OK;
     const dim3 runs(grid1d(T, 32), grid1d(d, 256));
-    if (dtype == OAPL_BF16) k_embed_runs<bf16_t><<<runs, 64 * kRunWaves, 0, st>>>(a);
-    else k_embed_runs<float><<<runs, 64 * kRunWaves, 0, st>>>(a);
+    by_truth(d % 4 == 0, [&](auto whole) {
+      constexpr bool WHOLE = whole;
+      if (dtype == OAPL_BF16) k_embed_runs<bf16_t, WHOLE><<<runs, 64 * kRunWaves, 0, st>>>(a);
+      else k_embed_runs<float, WHOLE><<<runs, 64 * kRunWaves, 0, st>>>(a);
+    });
     OAPL_LAUNCH_CHECK();
     return OAPL_OK;
   }
@@ -338,10 +349,13 @@ int32_t oapl_embed_bwd(const oapl_rows* dout, const int32_t* tokens, int64_t T, 
   // Rows that the caches do not hold go past them: 140897 tokens, d = 4096 (1.15 GB) 785 -> 771 us, with rows of dE past them too 739;
   // 4096 at V = 1544 (34 MB) 46 -> 60.  (Eight channels a lane and four rows under way: T = 140000, V = 1000 320 -> 282 us, this one 739 -> 781.)
   const bool once = past_caches(T * d * (int64_t)esize(dtype));
-  if (dtype == OAPL_BF16 && once) k_embed_sum<bf16_t, true><<<grid, 256, 0, st>>>(a);
-  else if (dtype == OAPL_BF16) k_embed_sum<bf16_t, false><<<grid, 256, 0, st>>>(a);
-  else if (once) k_embed_sum<float, true><<<grid, 256, 0, st>>>(a);
-  else k_embed_sum<float, false><<<grid, 256, 0, st>>>(a);
+  by_truth(d % 4 == 0, [&](auto whole) {
+    by_truth(once, [&](auto past) {
+      constexpr bool WHOLE = whole, ONCE = past;
+      if (dtype == OAPL_BF16) k_embed_sum<bf16_t, WHOLE, ONCE><<<grid, 256, 0, st>>>(a);
+      else k_embed_sum<float, WHOLE, ONCE><<<grid, 256, 0, st>>>(a);
+    });
+  });
   OAPL_LAUNCH_CHECK();
   k_embed_join<<<dim3(grid1d(p.tiles, kJoinTiles), grid1d(d, 256)), 64 * kJoinParts, 0, st>>>(a);
   OAPL_LAUNCH_CHECK();
@@ -361,9 +375,13 @@ int32_t oapl_residual_norm_fwd(const oapl_rows* x, const oapl_rows* y, const voi
     typedef std::remove_pointer_t<decltype(tx)> TX;
     typedef std::remove_pointer_t<decltype(t)> TY;
     constexpr int W = sizeof(TX) == 2 ? 8 : 4;
-    by_width<W>(d, [&](auto threads, auto pieces) {
-      constexpr int THREADS = threads, PIECES = pieces;
-      k_residual_norm_fwd<TX, TY, W, THREADS, PIECES><<<(unsigned)norm_workgroups(T, d), norm_lanes(d), 0, (hipStream_t)stream>>>(a);
+    by_width<W>(d, [&](auto lanes, auto most, auto pieces) {
+      by_truth(d % W == 0, [&](auto whole) {
+        constexpr int LANES = lanes, MOST = most, PIECES = pieces;
+        constexpr bool WHOLE = whole;
+        k_residual_norm_fwd<TX, TY, W, LANES, MOST, PIECES, WHOLE>
+            <<<wide_grid(norm_workgroups(T, d), 1 << 21), norm_lanes(d), 0, (hipStream_t)stream>>>(a);
+      });
     });
     return 0;
   });
@@ -402,9 +420,12 @@ int32_t oapl_residual_norm_bwd(const oapl_rows* x, const oapl_rows* y, const voi
     typedef std::remove_pointer_t<decltype(t)> TY;
     if (T > 0) {
       constexpr int W = sizeof(TX) == 2 ? 8 : 4;
-      by_width<W>(d, [&](auto threads, auto pieces) {
-        constexpr int THREADS = threads, PIECES = pieces;
-        k_residual_norm_bwd<TX, TY, W, THREADS, PIECES><<<grid, norm_lanes(d), 0, st>>>(a);
+      by_width<W>(d, [&](auto lanes, auto most, auto pieces) {
+        by_truth(d % W == 0, [&](auto whole) {
+          constexpr int LANES = lanes, MOST = most, PIECES = pieces;
+          constexpr bool WHOLE = whole;
+          k_residual_norm_bwd<TX, TY, W, LANES, MOST, PIECES, WHOLE><<<grid, norm_lanes(d), 0, st>>>(a);
+        });
       });
       OAPL_LAUNCH_CHECK();
     }

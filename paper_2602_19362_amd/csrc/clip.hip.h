@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256) void k_grad_squares(const ClipArgs p) {
       constexpr int W = 16 / sizeof(*x);
 #pragma unroll 4
       for (int i = threadIdx.x * W; i < n; i += 256 * W) {
-        const Piece<W> v = load_piece<W, ONCE>(x, i, n);
+        const Piece<W> v = load_piece<W, false, ONCE>(x, i, n);
 #pragma unroll
         for (int e = 0; e < W; ++e) sum += (double)v.v[e] * (double)v.v[e];
       }
@@ -105,12 +105,12 @@ __global__ __launch_bounds__(256) void k_grad_scale(const ClipArgs p) {
       constexpr int W = 16 / sizeof(*x);
 #pragma unroll 4
       for (int i = threadIdx.x * W; i < n; i += 256 * W) {
-        Piece<W> v = load_piece<W, LOAD_ONCE>(x, i, n);
+        Piece<W> v = load_piece<W, false, LOAD_ONCE>(x, i, n);
         if (clips) {
 #pragma unroll
           for (int e = 0; e < W; ++e) v.v[e] = (float)((double)v.v[e] * factor);
         }
-        store_piece<W, STORE_ONCE>(y, i, n, v);
+        store_piece<W, false, STORE_ONCE>(y, i, n, v);
       }
     });
 }

@@ -27,19 +27,18 @@ struct ResidualNormArgs {
   float scale, eps;
 };
 
-// Sum over the THREADS lanes of a row, in all of them.  `turn`, kept by the caller, alternates between two places: a wavefront that is
-// ahead writes to the other one, and cannot be two sums ahead of a barrier, so that one barrier a sum is enough.
-template <int THREADS>
+// Sum over the lanes of a row, in all of them: LANES, or the workgroup's (0).  `turn`, kept by the caller, alternates between two places: a
+// wavefront that is ahead writes to the other one, and cannot be two sums ahead of a barrier, so that one barrier a sum is enough.
+template <int LANES>
 __device__ __forceinline__ float row_total(float v, int& turn) {
-  v = lanes_total<(THREADS < 64 ? THREADS : 64)>(v);
-  if constexpr (THREADS > 64) {
-    __shared__ float all[2][THREADS / 64];
+  v = lanes_total<LANES ? LANES : 64>(v);
+  if constexpr (LANES == 0) {
+    __shared__ float all[2][16];
     turn ^= 1;
     if ((threadIdx.x & 63) == 0) all[turn][threadIdx.x >> 6] = v;
     __syncthreads();
-    v = 0.f;
-#pragma unroll
-    for (int i = 0; i < THREADS / 64; ++i) v += all[turn][i];
+    const int wave = threadIdx.x & 15;
+    v = lanes_total<16>(wave < (int)blockDim.x / 64 ? all[turn][wave] : 0.f);
   }
   return v;
 }
@@ -52,22 +51,32 @@ __device__ __forceinline__ float dot(const Piece<W>& a, const Piece<W>& b) {
   return s;
 }
 
-// TX: the residual stream's type, T: the block's and the norms'.  THREADS lanes hold a row, W channels in each of PIECES pieces: 16 of them, a
-// wavefront, or a workgroup.
-template <class TX, class T, int W, int THREADS, int PIECES>
-__global__ __launch_bounds__(THREADS < 128 ? 256 : THREADS) void k_residual_norm_fwd(const ResidualNormArgs p) {
-  constexpr int ROWS = THREADS < 128 ? 256 / THREADS : 1;
-  const int lane = threadIdx.x % THREADS, d = p.d;
+// A row's lanes and where they are: 16 of them, a wavefront, or (LANES == 0) a workgroup, as many as the row has pieces for.
+template <int LANES>
+struct RowLanes {
+  static constexpr int kRows = LANES ? 256 / LANES : 1;      // of a workgroup
+  int lane, lanes, row;
+  __device__ __forceinline__ RowLanes()
+      : lane(LANES ? threadIdx.x % LANES : threadIdx.x), lanes(LANES ? LANES : blockDim.x), row(LANES ? threadIdx.x / LANES : 0) {}
+};
+
+// TX: the residual stream's type, T: the block's and the norms'.  A lane holds W channels in each of PIECES pieces of a row; MOST lanes a workgroup.
+// WHOLE: d is a multiple of W.
+template <class TX, class T, int W, int LANES, int MOST, int PIECES, bool WHOLE>
+__global__ __launch_bounds__(MOST) void k_residual_norm_fwd(const ResidualNormArgs p) {
+  const RowLanes<LANES> at;
+  constexpr int ROWS = at.kRows;
+  const int lane = at.lane, lanes = at.lanes, d = p.d;
   int turn = 0;
-  for (int64_t t = (int64_t)blockIdx.x * ROWS + (ROWS == 1 ? 0 : threadIdx.x / THREADS); t < p.T; t += (int64_t)gridDim.x * ROWS) {
+  if (const int64_t t = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * ROWS + at.row; t < p.T) {
     Raw<TX, W> rx[PIECES];
     Raw<T, W> ry[PIECES] = {}, rg[PIECES] = {};
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      const int c = (i * THREADS + lane) * W;
-      rx[i] = load_raw<W>(p.x.row<TX>(t), c, d);
-      if (p.y.p) ry[i] = load_raw<W>(p.y.row<T>(t), c, d);
-      if (p.gate.p) rg[i] = load_raw<W>(p.gate.row<T>(t), c, d);
+      const int c = (i * lanes + lane) * W;
+      rx[i] = load_raw<W, WHOLE>(p.x.row<TX>(t), c, d);
+      if (p.y.p) ry[i] = load_raw<W, WHOLE>(p.y.row<T>(t), c, d);
+      if (p.gate.p) rg[i] = load_raw<W, WHOLE>(p.gate.row<T>(t), c, d);
     }
     Piece<W> x[PIECES];
 #pragma unroll
@@ -77,15 +86,15 @@ __global__ __launch_bounds__(THREADS < 128 ? 256 : THREADS) void k_residual_norm
       if (p.y_gain) {
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) sum += dot(widened(ry[i]), widened(ry[i]));
-        r *= rsqrtf(row_total<THREADS>(sum, turn) / (float)d + p.eps);
+        for (int i = 0; i < PIECES; ++i) sum += (i * lanes + lane) * W < d ? dot(widened(ry[i]), widened(ry[i])) : 0.f;
+        r *= rsqrtf(row_total<LANES>(sum, turn) / (float)d + p.eps);
       }
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
-        const int c = (i * THREADS + lane) * W;
+        const int c = (i * lanes + lane) * W;
         Piece<W> y = widened(ry[i]);
         if (p.y_gain) {
-          const Piece<W> g = load_piece<W>((const T*)p.y_gain, c, d);
+          const Piece<W> g = load_piece<W, WHOLE>((const T*)p.y_gain, c, d);
 #pragma unroll
           for (int e = 0; e < W; ++e) y.v[e] *= g.v[e];
         }
@@ -95,21 +104,21 @@ __global__ __launch_bounds__(THREADS < 128 ? 256 : THREADS) void k_residual_norm
         }
 #pragma unroll
         for (int e = 0; e < W; ++e) x[i].v[e] += r * y.v[e];
-        store_piece<W>(p.x_out.row<TX>(t), c, d, x[i]);
+        store_piece<W, WHOLE>(p.x_out.row<TX>(t), c, d, x[i]);
       }
     }
     if (p.gain) {
       float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) sum += dot(x[i], x[i]);
-      const float r = rsqrtf(row_total<THREADS>(sum, turn) / (float)d + p.eps);
+      for (int i = 0; i < PIECES; ++i) sum += (i * lanes + lane) * W < d ? dot(x[i], x[i]) : 0.f;
+      const float r = rsqrtf(row_total<LANES>(sum, turn) / (float)d + p.eps);
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
-        const int c = (i * THREADS + lane) * W;
-        const Piece<W> g = load_piece<W>((const T*)p.gain, c, d);
+        const int c = (i * lanes + lane) * W;
+        const Piece<W> g = load_piece<W, WHOLE>((const T*)p.gain, c, d);
 #pragma unroll
         for (int e = 0; e < W; ++e) x[i].v[e] *= r * g.v[e];
-        store_piece<W>(p.out.row<T>(t), c, d, x[i]);
+        store_piece<W, WHOLE>(p.out.row<T>(t), c, d, x[i]);
       }
     }
   }
@@ -122,34 +131,35 @@ struct NormRow {
   Raw<T, W> dn[PIECES], y[PIECES], gate[PIECES];
 };
 
-template <class TX, class T, int W, int THREADS, int PIECES>
-__global__ __launch_bounds__(THREADS < 128 ? 256 : THREADS) void k_residual_norm_bwd(const ResidualNormArgs p) {
-  constexpr int ROWS = THREADS < 128 ? 256 / THREADS : 1;
-  const int lane = threadIdx.x % THREADS, d = p.d;
+template <class TX, class T, int W, int LANES, int MOST, int PIECES, bool WHOLE>
+__global__ __launch_bounds__(MOST) void k_residual_norm_bwd(const ResidualNormArgs p) {
+  const RowLanes<LANES> at;
+  constexpr int ROWS = at.kRows;
+  const int lane = at.lane, lanes = at.lanes, d = p.d;
   int turn = 0;
   Piece<W> sum_gain[PIECES] = {}, sum_block[PIECES] = {};
   Raw<T, W> gain[PIECES] = {}, y_gain[PIECES] = {};
 #pragma unroll
   for (int i = 0; i < PIECES; ++i) {
-    const int c = (i * THREADS + lane) * W;
-    if (p.gain) gain[i] = load_raw<W>((const T*)p.gain, c, d);
-    if (p.y_gain) y_gain[i] = load_raw<W>((const T*)p.y_gain, c, d);
+    const int c = (i * lanes + lane) * W;
+    if (p.gain) gain[i] = load_raw<W, WHOLE>((const T*)p.gain, c, d);
+    if (p.y_gain) y_gain[i] = load_raw<W, WHOLE>((const T*)p.y_gain, c, d);
   }
   typedef NormRow<TX, T, W, PIECES> Row;
   const auto load = [&](Row& row, int64_t t) {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      const int c = (i * THREADS + lane) * W;
+      const int c = (i * lanes + lane) * W;
       row.dx[i] = Raw<TX, W>{};
-      if (p.gain) row.x[i] = load_raw<W>(p.x.row<TX>(t), c, d), row.dn[i] = load_raw<W>(p.out.row<T>(t), c, d);
-      if (p.x_out.p) row.dx[i] = load_raw<W>(p.x_out.row<TX>(t), c, d);
-      if (p.y.p) row.y[i] = load_raw<W>(p.y.row<T>(t), c, d);
-      if (p.gate.p) row.gate[i] = load_raw<W>(p.gate.row<T>(t), c, d);
+      if (p.gain) row.x[i] = load_raw<W, WHOLE>(p.x.row<TX>(t), c, d), row.dn[i] = load_raw<W, WHOLE>(p.out.row<T>(t), c, d);
+      if (p.x_out.p) row.dx[i] = load_raw<W, WHOLE>(p.x_out.row<TX>(t), c, d);
+      if (p.y.p) row.y[i] = load_raw<W, WHOLE>(p.y.row<T>(t), c, d);
+      if (p.gate.p) row.gate[i] = load_raw<W, WHOLE>(p.gate.row<T>(t), c, d);
     }
   };
-  const int64_t first = (int64_t)blockIdx.x * ROWS + (ROWS == 1 ? 0 : threadIdx.x / THREADS), step = (int64_t)gridDim.x * ROWS;
+  const int64_t first = (int64_t)blockIdx.x * ROWS + at.row, step = (int64_t)gridDim.x * ROWS;
   // the next row is under way while one is worked on, as far as there are registers for it
-  constexpr bool AHEAD = THREADS * PIECES * W <= 4096;
+  constexpr bool AHEAD = MOST < 1024 || (W == 8 && PIECES == 1);
   Row row, next;
   if (AHEAD && first < p.T) load(next, first);
   for (int64_t t = first; t < p.T; t += step) {
@@ -162,8 +172,8 @@ __global__ __launch_bounds__(THREADS < 128 ? 256 : THREADS) void k_residual_norm
     if (p.gain) {
       float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) sum += dot(widened(row.x[i]), widened(row.x[i]));
-      const float r = rsqrtf(row_total<THREADS>(sum, turn) / (float)d + p.eps);
+      for (int i = 0; i < PIECES; ++i) sum += (i * lanes + lane) * W < d ? dot(widened(row.x[i]), widened(row.x[i])) : 0.f;
+      const float r = rsqrtf(row_total<LANES>(sum, turn) / (float)d + p.eps);
       Piece<W> v[PIECES], u[PIECES];
       float m = 0.f;
 #pragma unroll
@@ -174,31 +184,31 @@ __global__ __launch_bounds__(THREADS < 128 ? 256 : THREADS) void k_residual_norm
           v[i].v[e] *= r;
           sum_gain[i].v[e] += u[i].v[e] * v[i].v[e];
           u[i].v[e] *= (float)gain[i][e];
-          m += u[i].v[e] * v[i].v[e];
         }
+        m += (i * lanes + lane) * W < d ? dot(u[i], v[i]) : 0.f;
       }
-      m = row_total<THREADS>(m, turn) / (float)d;
+      m = row_total<LANES>(m, turn) / (float)d;
 #pragma unroll
       for (int i = 0; i < PIECES; ++i)
 #pragma unroll
         for (int e = 0; e < W; ++e) dx[i].v[e] += r * (u[i].v[e] - v[i].v[e] * m);
     }
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) store_piece<W>(p.dx.row<TX>(t), (i * THREADS + lane) * W, d, dx[i]);
+    for (int i = 0; i < PIECES; ++i) store_piece<W, WHOLE>(p.dx.row<TX>(t), (i * lanes + lane) * W, d, dx[i]);
     if (p.y.p) {
       // from here on dx is dz
       float r = 1.f;
       if (p.y_gain) {
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) sum += dot(widened(row.y[i]), widened(row.y[i]));
-        r = rsqrtf(row_total<THREADS>(sum, turn) / (float)d + p.eps);
+        for (int i = 0; i < PIECES; ++i) sum += (i * lanes + lane) * W < d ? dot(widened(row.y[i]), widened(row.y[i])) : 0.f;
+        r = rsqrtf(row_total<LANES>(sum, turn) / (float)d + p.eps);
       }
       float m = 0.f;
       Piece<W> w[PIECES];
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
-        const int c = (i * THREADS + lane) * W;
+        const int c = (i * lanes + lane) * W;
         w[i] = widened(row.y[i]);
 #pragma unroll
         for (int e = 0; e < W; ++e) dx[i].v[e] *= p.scale, w[i].v[e] *= r;
@@ -210,7 +220,7 @@ __global__ __launch_bounds__(THREADS < 128 ? 256 : THREADS) void k_residual_norm
             dg.v[e] = dx[i].v[e] * w[i].v[e] * (p.y_gain ? (float)y_gain[i][e] : 1.f);
             dx[i].v[e] *= (float)row.gate[i][e];
           }
-          store_piece<W>(p.dgate.row<T>(t), c, d, dg);
+          store_piece<W, WHOLE>(p.dgate.row<T>(t), c, d, dg);
         }
 #pragma unroll
         for (int e = 0; e < W; ++e) sum_block[i].v[e] += dx[i].v[e] * w[i].v[e];
@@ -220,21 +230,19 @@ __global__ __launch_bounds__(THREADS < 128 ? 256 : THREADS) void k_residual_norm
         }
         if (p.y_gain) {
 #pragma unroll
-          for (int e = 0; e < W; ++e) {
-            dx[i].v[e] *= (float)y_gain[i][e];
-            m += dx[i].v[e] * w[i].v[e];
-          }
+          for (int e = 0; e < W; ++e) dx[i].v[e] *= (float)y_gain[i][e];
+          m += c < d ? dot(dx[i], w[i]) : 0.f;
         }
       }
       if (p.y_gain) {
-        m = row_total<THREADS>(m, turn) / (float)d;
+        m = row_total<LANES>(m, turn) / (float)d;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i)
 #pragma unroll
           for (int e = 0; e < W; ++e) dx[i].v[e] = r * (dx[i].v[e] - w[i].v[e] * m);
       }
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) store_piece<W>(p.dy.row<T>(t), (i * THREADS + lane) * W, d, dx[i]);
+      for (int i = 0; i < PIECES; ++i) store_piece<W, WHOLE>(p.dy.row<T>(t), (i * lanes + lane) * W, d, dx[i]);
     }
   }
   if (!p.partials) return;
@@ -242,16 +250,16 @@ __global__ __launch_bounds__(THREADS < 128 ? 256 : THREADS) void k_residual_norm
   if constexpr (ROWS == 1) {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      store_piece<W>(to, (i * THREADS + lane) * W, d, sum_gain[i]);
-      store_piece<W>(to + d, (i * THREADS + lane) * W, d, sum_block[i]);
+      store_piece<W, WHOLE>(to, (i * lanes + lane) * W, d, sum_gain[i]);
+      store_piece<W, WHOLE>(to + d, (i * lanes + lane) * W, d, sum_block[i]);
     }
   } else {
     // the workgroup's rows, added in their order
-    __shared__ float all[ROWS][2][THREADS * PIECES * W];
+    __shared__ float all[ROWS][2][LANES * PIECES * W];
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      store_whole<W>(&all[threadIdx.x / THREADS][0][(i * THREADS + lane) * W], sum_gain[i]);
-      store_whole<W>(&all[threadIdx.x / THREADS][1][(i * THREADS + lane) * W], sum_block[i]);
+      store_whole<W>(&all[at.row][0][(i * lanes + lane) * W], sum_gain[i]);
+      store_whole<W>(&all[at.row][1][(i * lanes + lane) * W], sum_block[i]);
     }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * d; i += 256) {

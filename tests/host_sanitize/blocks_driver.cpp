@@ -55,7 +55,7 @@ int main() {
       CHECK(good == (bytes > 0) && bytes % 256 == 0);
       ++plans;
       if (!good) continue;
-      CHECK(norm_lanes(d) * 16 >= d && norm_workgroups(T, d) * norm_rows(d) >= T && norm_workgroups(T, d) * norm_lanes(d) < ((int64_t)1 << 35));
+      CHECK(norm_lanes(d) * 16 >= d && norm_workgroups(T, d) * norm_rows(d) >= T && fits(wide_grid(std::max<int64_t>(1, norm_workgroups(T, d)), 1 << 21), norm_lanes(d)));
       CHECK(norm_bwd_grid(T, d) <= 1024 && bytes >= (size_t)norm_bwd_grid(T, d) * 2 * d * 4);
     }
 
