@@ -512,7 +512,7 @@ size_t oapl_embed_workspace_bytes(int64_t T, int32_t d, int32_t V);
  *   dout        [T][d] in dtype
  *   accumulate  0: dE is overwritten, rows without tokens with zeros; otherwise the sums are added to what dE holds (the head's dW, where
  *               embedding and head share their weights), and rows without tokens stay as they are
- *   dE          [V][d] float, from any element on
+ *   dE          [V][d] float, from any element on; it must not overlap dout
  * A token outside [0, V) has no part in dE and leaves OAPL_ERR_TOKEN_RANGE in the workspace's status.
  */
 int32_t oapl_embed_bwd(const oapl_rows* dout, const int32_t* tokens, int64_t T, int32_t d, int32_t V, int32_t dtype, float scale,

@@ -129,7 +129,7 @@ def _same(a, b):
     assert len(a) == len(b) and all(torch.equal(x, y) for x, y in zip(a, b))
 
 
-@pytest.mark.parametrize("T, d, V", [(5, 64, 30), (1500, 256, 1544), (9000, 264, 3000)])
+@pytest.mark.parametrize("T, d, V", [(5, 64, 30), (1500, 256, 1544), (9000, 264, 3000), (9000, 64, 300000)])
 def test_replayed_graphs_give_the_eager_results(T, d, V):
     """Two graphs that share their workspaces, replayed in turn with eager work between, on other inputs in the same buffers."""
     a = Step(T, d, V, 1)
