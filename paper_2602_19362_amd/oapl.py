@@ -647,6 +647,14 @@ def _rows(t: torch.Tensor, name: str, shape, dtype: torch.dtype, index: int) -> 
     raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
+def _result(t: Optional[torch.Tensor], name: str, like: torch.Tensor, shape, dtype: torch.dtype, index: int):
+    """The tensor that a result goes to, t or a new one beside `like`, and its oapl_rows."""
+    if t is not None:
+        return t, _rows(t, name, shape, dtype, index)
+    t = like.new_empty(shape, dtype=dtype)
+    return t, Rows(t.data_ptr(), shape[1])
+
+
 def _gpu_of(t: torch.Tensor) -> int:
     """The index of the current GPU, on which t has to live."""
     index = t.get_device()
@@ -664,10 +672,13 @@ def embed_fwd(E: torch.Tensor, tokens: torch.Tensor, *, scale: float = 1.0, out_
     (V, d), T = E.shape, tokens.shape[0]
     if out is None:
         out = E.new_empty((T, d), dtype=out_dtype)
+        rows = Rows(out.data_ptr(), d)
     elif out_dtype is not None and out.dtype is not out_dtype:
         raise TypeError(f"out must be {out_dtype}, got {out.dtype}")
+    else:
+        rows = _rows(out, "out", (T, d), out.dtype, gpu)
     rc = lib().oapl_embed_fwd(_flat(E, E.dtype, "E", gpu), _flat(tokens, torch.int32, "tokens", gpu), T, d, V, _dtype_code(E),
-                              _dtype_code(out), scale, _rows(out, "out", (T, d), out.dtype, gpu), _raw_stream(gpu))
+                              _dtype_code(out), scale, rows, _raw_stream(gpu))
     if rc != 0:
         raise OaplError(rc, "oapl_embed_fwd")
     return out
@@ -751,17 +762,17 @@ def residual_norm_fwd(x: torch.Tensor, y: Optional[torch.Tensor] = None, gain: O
     """
     shape, kind, per_token, gates, gpu = _residual_norm_setup(x, y, gain, y_gain, gate)
     T, d = shape
-    if y is not None and x_out is None:
-        x_out = x.new_empty(shape)
-    if gain is not None and out is None:
-        out = x.new_empty(shape, dtype=kind)
     if (y is None and x_out is not None) or (gain is None and out is not None):
         raise ValueError("x_out goes with y, out with gain")
+    y_rows = x_out_rows = out_rows = None
+    if y is not None:
+        y_rows = _rows(y, "y", shape, kind, gpu)
+        x_out, x_out_rows = _result(x_out, "x_out", x, shape, x.dtype, gpu)
+    if gain is not None:
+        out, out_rows = _result(out, "out", x, shape, kind, gpu)
     rc = lib().oapl_residual_norm_fwd(
-        _rows(x, "x", shape, x.dtype, gpu), None if y is None else _rows(y, "y", shape, kind, gpu), _flat(y_gain, kind, "y_gain", gpu),
-        gates, per_token, _flat(gain, kind, "gain", gpu), T, d, _dtype_code(x), _dtype_code(gain if y is None else y), scale, eps,
-        None if y is None else _rows(x_out, "x_out", shape, x.dtype, gpu), None if gain is None else _rows(out, "out", shape, kind, gpu),
-        _raw_stream(gpu))
+        _rows(x, "x", shape, x.dtype, gpu), y_rows, _flat(y_gain, kind, "y_gain", gpu), gates, per_token, _flat(gain, kind, "gain", gpu),
+        T, d, _dtype_code(x), _dtype_code(gain if y is None else y), scale, eps, x_out_rows, out_rows, _raw_stream(gpu))
     if rc != 0:
         raise OaplError(rc, "oapl_residual_norm_fwd")
     return ResidualNormResult(x if y is None else x_out, out)
@@ -789,24 +800,28 @@ def residual_norm_bwd(x: torch.Tensor, y: Optional[torch.Tensor], dx_out: Option
     T, d = shape
     if (gain is None) != (dout is None) or (y is None and dy is not None):
         raise ValueError("dout goes with gain, dy with y")
-    dx = x.new_empty(shape) if dx is None else dx
-    if y is not None and dy is None:
-        dy = x.new_empty(shape, dtype=kind)
-    dgate = x.new_empty(shape, dtype=kind) if per_token else None
+    y_rows = dy_rows = dout_rows = dgate_rows = dgate = None
+    dx, dx_rows = _result(dx, "dx", x, shape, x.dtype, gpu)
+    if y is not None:
+        y_rows = _rows(y, "y", shape, kind, gpu)
+        dy, dy_rows = _result(dy, "dy", x, shape, kind, gpu)
+    if dout is not None:
+        dout_rows = _rows(dout, "dout", shape, kind, gpu)
+    if per_token:
+        dgate, dgate_rows = _result(None, "dgate", x, shape, kind, gpu)
     dgain = None if gain is None else x.new_empty(d, dtype=torch.float32)
     dy_gain = None if y_gain is None else x.new_empty(d, dtype=torch.float32)
     shared = None if gate is None or per_token else x.new_empty(d, dtype=torch.float32)
-    ws = None
+    ws, ws_at, ws_bytes = None, None, 0
     if dgain is not None or dy_gain is not None or shared is not None:
         ws = _scratch(lib().oapl_residual_norm_workspace_bytes(T, d), x, workspace, "oapl_residual_norm_workspace_bytes")
+        ws_at, ws_bytes = ws.data_ptr(), ws.numel()
     rc = lib().oapl_residual_norm_bwd(
-        _rows(x, "x", shape, x.dtype, gpu), None if y is None else _rows(y, "y", shape, kind, gpu), _flat(y_gain, kind, "y_gain", gpu),
-        gates, per_token, _flat(gain, kind, "gain", gpu), None if dx_out is None else _rows(dx_out, "dx_out", shape, x.dtype, gpu),
-        None if dout is None else _rows(dout, "dout", shape, kind, gpu), T, d, _dtype_code(x), _dtype_code(gain if y is None else y),
-        scale, eps, _rows(dx, "dx", shape, x.dtype, gpu), None if y is None else _rows(dy, "dy", shape, kind, gpu),
-        None if dgain is None else dgain.data_ptr(), None if dy_gain is None else dy_gain.data_ptr(),
-        None if dgate is None else _rows(dgate, "dgate", shape, kind, gpu), None if shared is None else shared.data_ptr(), None if ws is None else ws.data_ptr(),
-        0 if ws is None else ws.numel(), _raw_stream(gpu))
+        _rows(x, "x", shape, x.dtype, gpu), y_rows, _flat(y_gain, kind, "y_gain", gpu), gates, per_token, _flat(gain, kind, "gain", gpu),
+        None if dx_out is None else _rows(dx_out, "dx_out", shape, x.dtype, gpu), dout_rows, T, d, _dtype_code(x),
+        _dtype_code(gain if y is None else y), scale, eps, dx_rows, dy_rows, None if dgain is None else dgain.data_ptr(),
+        None if dy_gain is None else dy_gain.data_ptr(), dgate_rows, None if shared is None else shared.data_ptr(), ws_at, ws_bytes,
+        _raw_stream(gpu))
     if rc != 0:
         raise OaplError(rc, "oapl_residual_norm_bwd")
     return ResidualNormGrads(dx, dy, dgain, dy_gain, shared if dgate is None else dgate, ws)
