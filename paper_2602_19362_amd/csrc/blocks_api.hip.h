@@ -112,10 +112,10 @@ static int launch_embed_sort(const SortArgs& a, hipStream_t st) {
   const int64_t all = a.dE && !a.clear_absent ? ((int64_t)a.V * a.d + 1023) / 1024 : 0;
   k_embed_count<<<wide_grid(a.blocks + all, 1 << 23), 256, std::max(bins * 4, kClearLds), st>>>(a);
   OAPL_LAUNCH_CHECK();
-  k_embed_place<0, ITEMS><<<a.blocks, kSortThreads, bytes, st>>>(a);
+  const auto clears = [&](int rows) { return a.dE && a.clear_absent ? (int64_t)grid1d(rows, kSortThreads / 64) * grid1d(a.d, 1024) : 0; };
+  k_embed_place<0, ITEMS><<<wide_grid(a.blocks + clears(a.early), 1 << 21), kSortThreads, bytes, st>>>(a);
   OAPL_LAUNCH_CHECK();
-  const int64_t absent = a.dE && a.clear_absent ? (int64_t)grid1d(a.V, kSortThreads / 64) * grid1d(a.d, 1024) : 0;
-  k_embed_place<1, ITEMS><<<wide_grid(a.blocks + absent, 1 << 21), kSortThreads, bytes, st>>>(a);
+  k_embed_place<1, ITEMS><<<wide_grid(a.blocks + clears(a.V - a.early), 1 << 21), kSortThreads, bytes, st>>>(a);
   OAPL_LAUNCH_CHECK();
   return OAPL_OK;
 }
@@ -342,6 +342,9 @@ int32_t oapl_embed_bwd(const oapl_rows* dout, const int32_t* tokens, int64_t T, 
   // Rows without tokens alone are cleared where that leaves out enough: 140897 tokens, d = 4096, V = 151936 774 us, all rows 833; 50000, d = 1024 176, 182; 16000, d = 4096
   // 482, 472; d = 256 (rows of 1 KB) 50000 92, 73.
   s.clear_absent = d >= 1024 && 8 * T >= V;
+  // ... after what the first pass leaves time for: 140897 tokens, d = 4096, V = 151936 with 0 / 64 / 128 / 224 MB of it 742 / 737 / 731 / 725 us, 140000, d = 1024 249 / 245 / 241 / 237;
+  // 12000, d = 4096, V = 8192 (134 MB in all) 73.7, with all of it 76.
+  s.early = (int)std::min<int64_t>(V / 4, 192000000 / (4 * (int64_t)d));
   if (int rc = p.items == 2 ? launch_embed_sort<2>(s, st) : launch_embed_sort<8>(s, st)) return rc;
   a.partials = (float*)(ws + p.off_partials);
   a.tile = p.tile, a.tiles = p.tiles, a.slices = (int)grid1d(d, 1024);

@@ -8,8 +8,8 @@
 // many workgroups (k_embed_sum); what a tile has of a token that reaches over its ends goes into the workspace and is added up by another
 // launch, tile by tile (k_embed_join).  dE is cleared beside the sorting, not between reads: memory takes 6 TB/s of either alone and 4.9 of both.
 //
-// 140897 tokens that follow Zipf's law, d = 4096 in bf16, V = 151936 (3.6 GB): counting 6 us, first pass 26, second pass and 1.9 GB of zeros 308, sums
-// 380 (1.15 GB in, 0.65 out: 4.8 TB/s), tokens over tiles 23.  1003 of them: places and 2.49 GB of zeros 350, sums 10.
+// 140897 tokens that follow Zipf's law, d = 4096 in bf16, V = 151936 (3.6 GB): counting 6 us, first pass and 0.19 GB of zeros 40,
+// second pass and 1.72 GB of zeros 290, sums 368 (1.15 GB in, 0.65 out: 4.9 TB/s), tokens over tiles 23.  1003 of them: places and 2.49 GB of zeros 343, sums 19.
 #pragma once
 
 #include "rows.hip.h"
@@ -61,8 +61,9 @@ struct SortArgs {
   int32_t* counts[2];               // [blocks][1 << bits]
   uint8_t* present;                 // [V]: whether an id occurs
   int* status;
-  float* dE;                        // to be cleared: beside the counting, or only where no id occurs, beside the second pass
-  bool clear_absent;
+  float* dE;                        // to be cleared: all of it beside the counting, or its first rows beside the first pass and, of the others,
+  bool clear_absent;                // those whose id does not occur, beside the second
+  int early;
   int64_t T;
   int V, d, bits, block, blocks;    // keys of a block, and how many of them
 };
@@ -108,11 +109,13 @@ __global__ __launch_bounds__(256) void k_embed_count(const SortArgs p) {
   if (blockIdx.x == 0 && threadIdx.x < kStatusWords) p.status[threadIdx.x] = 0;
 }
 
-// 1024 channels of 16 rows of dE, a wavefront's one each, are zero where the row's id does not occur.
-__device__ __forceinline__ void clear_absent(const SortArgs& p, int64_t i) {
+// 1024 channels of 16 rows of dE, a wavefront's one each, are zero: of the first p.early rows beside the first pass, of the others, where the row's
+// id does not occur, beside the second.
+template <int PASS>
+__device__ __forceinline__ void clear_rows(const SortArgs& p, int64_t i) {
   const int lane = threadIdx.x & 63, pieces = (p.d + 1023) / 1024;
-  const int64_t v = i / pieces * (kSortThreads / 64) + (threadIdx.x >> 6);
-  if (v >= p.V || p.present[v]) return;
+  const int64_t v = i / pieces * (kSortThreads / 64) + (threadIdx.x >> 6) + (PASS == 0 ? 0 : p.early);
+  if (v >= (PASS == 0 ? p.early : p.V) || (PASS == 1 && p.present[v])) return;
   float* row = p.dE + v * p.d;
 #pragma unroll
   for (int j = 0; j < 4; ++j) store_piece<4, false>(row, (int)(i % pieces) * 1024 + (j * 64 + lane) * 4, p.d, Piece<4>{});
@@ -125,11 +128,9 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_place(const SortArgs p) 
   extern __shared__ int32_t lds[];
   const int bins = 1 << p.bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   constexpr int WAVES = kSortThreads / 64;
-  if constexpr (PASS == 1) {
-    if ((int)blockIdx.x >= p.blocks || blockIdx.y > 0) {
-      clear_absent(p, (int64_t)blockIdx.y * gridDim.x + blockIdx.x - p.blocks);
-      return;
-    }
+  if ((int)blockIdx.x >= p.blocks || blockIdx.y > 0) {
+    clear_rows<PASS>(p, (int64_t)blockIdx.y * gridDim.x + blockIdx.x - p.blocks);
+    return;
   }
   int32_t *mine = lds, *total = lds + WAVES * bins, *earlier = total + bins;
   // mine [WAVES][bins]: first a wavefront's counts, then where its keys of a digit begin

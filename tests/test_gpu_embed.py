@@ -173,6 +173,21 @@ def test_the_same_weights_at_both_ends():
     near(r.dW, *orc.embed_grads(r.dH, tokens, 600, 1.0, old=before))
 
 
+@pytest.mark.parametrize("T, d, V", [(300, 40, 77), (9000, 24, 500)])
+def test_the_gradient_is_the_lookups_difference(T, d, V):
+    """The lookup is linear, so a difference along a direction is off by roundings alone: of the two products (2^-24 each), of the moved
+    embedding (2^-24, of what it holds), and of the gradient by the oracle's bound."""
+    F, h = torch.float64, 0.5
+    E, way = (torch.randn(V, d, generator=_gen(i), device=DEV) for i in (12, 13))
+    tokens, dout = _tokens("zipf", T, V), torch.randn(T, d, generator=_gen(14), device=DEV)
+    hi, lo = (oapl.embed_fwd(E + s * h * way, tokens, scale=1.5) for s in (1, -1))
+    quotient = (dout.to(F) * (hi.to(F) - lo.to(F))).sum() / (2 * h)
+    slope = (oapl.embed_bwd(dout, tokens, V, scale=1.5).dE.to(F) * way).sum()
+    bound = (dout.to(F).abs() * (hi.to(F).abs() + lo.to(F).abs())).sum() * 2 * 2.0 ** -24 / (2 * h)
+    bound += (orc.embed_grads(dout, tokens, V, 1.5)[1] * way.abs()).sum()
+    assert abs(quotient - slope) <= bound
+
+
 def test_refusals():
     E, t = torch.zeros(5, 8, device=DEV), torch.zeros(3, device=DEV, dtype=torch.int32)
     with pytest.raises(TypeError):
