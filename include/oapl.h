@@ -483,8 +483,8 @@ int32_t oapl_attention_bwd(const oapl_heads* q, const oapl_heads* k, const oapl_
  * Around the policy's blocks: the embedding, the residual stream with its norms, and the gradients' common norm.
  *
  * An operand of rows is [rows][channels] with the channels side by side and any distance between rows (in elements), from any element
- * on; inputs may have a row stride of 0 (broadcast), rows that are written must not overlap.  The stride of a single row is not
- * looked at.
+ * on (else OAPL_ERR_ALIGN); inputs may have a row stride of 0 (broadcast), rows that are written must not overlap, and rows lie within
+ * 2^46 elements (OAPL_ERR_SHAPE).  The stride of a single row is not looked at.
  */
 typedef struct {
   void* data;

@@ -20,7 +20,7 @@ static int check_rows(const oapl_rows* x, int64_t n, int64_t d, bool written) {
   if (!x) return OAPL_ERR_NULL;
   if (n == 0) return OAPL_OK;
   if (!x->data) return OAPL_ERR_NULL;
-  if (n > 1 && (x->row_stride < (written ? d : 0) || x->row_stride > ((int64_t)1 << 40))) return OAPL_ERR_SHAPE;
+  if (n > 1 && (x->row_stride < (written ? d : 0) || x->row_stride > ((int64_t)1 << 46) / (n - 1))) return OAPL_ERR_SHAPE;
   return OAPL_OK;
 }
 static Rows rows_of(const oapl_rows* x, int64_t n, int dtype) {
@@ -51,15 +51,15 @@ static bool embed_plan(EmbedPlan& p, int64_t T, int d, int V) {
     return was;
   };
   p.off_keys[1] = take(T * 4), p.off_places[1] = take(T * 4);
-  // Counting / sorting, us for the whole call: fp32, d = 64, V = 1000: 6000 tokens 23 / 39, 8192 31 / 39, 12000 59 / 40; bf16, V = 1000, 8192 tokens: d = 1024 47 / 44, 4096 92 /
-  // 49 (a frequent token's rows are read by one workgroup a slice); 4096 at d = 4096, V = 1544 40 / 44.
+  // Counting / sorting, us for the whole call: fp32, d = 64, V = 1000: 6000 tokens 23 / 39, 8192 31 / 39, 12000 59 / 40; bf16, V = 1000, 8192
+  // tokens: d = 1024 47 / 44, 4096 92 / 49 (a frequent token's rows are read by one workgroup a slice); 4096 at d = 4096, V = 1544 40 / 44.
   p.few = T <= (d <= 512 ? kFewTokens : kFewTokens / 2);
   if (p.few) return true;
   while (((int64_t)1 << (2 * p.bits)) <= V) ++p.bits;      // ids 0 .. V
   p.items = T <= 128 * kSortThreads * 2 ? 2 : 8;
   p.blocks = (int)std::max<int64_t>(1, (T + (int64_t)kSortThreads * p.items - 1) / (kSortThreads * p.items));
-  // 32 / 64 / 128 rows a tile, us for the whole call in bf16: d = 4096, V = 1544: 5000 tokens 44 / 55 / 77, 10000 56 / 69 / 96, 20000 87 / 83 / 113, 80000 211 / 206 /
-  // 229; d = 1024 20000 46 / 56 / 77, 40000 58 / 68 / 87, 80000 95 / 92 / 119; d = 4096, V = 151936 140897 785 / 772 / 788.
+  // 32 / 64 / 128 rows a tile, us for the whole call in bf16: d = 4096, V = 1544: 5000 tokens 44 / 55 / 77, 10000 56 / 69 / 96, 20000 87 / 83 / 113,
+  // 80000 211 / 206 / 229; d = 1024 20000 46 / 56 / 77, 40000 58 / 68 / 87, 80000 95 / 92 / 119; d = 4096, V = 151936 140897 785 / 772 / 788.
   p.tile = T * ((d + 1023) / 1024) <= 1 << 16 ? 32 : 64;
   p.tiles = (int)((T + p.tile - 1) / p.tile);
   p.off_keys[0] = take(T * 4), p.off_places[0] = take(T * 4);
@@ -121,10 +121,11 @@ static int launch_embed_sort(const SortArgs& a, hipStream_t st) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------- residual stream
-// How a row of d channels is held, W in a piece: f(lanes of a row, or 0 for a workgroup's; lanes of a workgroup at most; pieces a lane).  Eight channels a
-// lane, 16 where there are no more lanes:
-// 16411 rows of 4096 in bf16 with 8 / 16 / 32 / 64 forward 92 / 97 / 107 / 158 us (workgroups that take row after row 101 .. 111), 3000 of 8192
-// 36 / 40 / 47 / 66, 8000 of 4096 in fp32 97 / 102 / 121 / 164.
+// How a row of d channels is held, W in a piece: f(lanes of a row, or 0 for a workgroup's; lanes of a workgroup at most; pieces a lane).  Eight
+// channels a lane, 16 where there are no more lanes: 16411 rows of 4096 in bf16 with 8 / 16 / 32 / 64 forward 92 / 97 / 107 / 158 us (workgroups
+// that take row after row 101 .. 111), 3000 of 8192 36 / 40 / 47 / 66, 8000 of 4096 in fp32 97 / 102 / 121 / 164.  A workgroup has as many lanes as the
+// row has pieces for, in wavefronts: with 1024 lanes, and branches around the loads, 6007 rows of 5120 took 110 us backwards instead of 83 and 51
+// forward instead of 45 (the two were not timed apart).
 template <int W, class F>
 static void by_width(int d, F f) {
   constexpr std::integral_constant<int, 8 / W> eight{};
@@ -229,12 +230,12 @@ static int clip_plan(ClipPlan& p, const oapl_tensor* tensors, int n, bool writte
     if (!element_aligned(t.data, t.dtype) || (written && !element_aligned(t.out, t.dtype))) return OAPL_ERR_ALIGN;
   }
   // Small sets are a launch for the squares and one for the scaling, whose workgroups all add up the sums; of larger ones a workgroup has one
-  // chunk, so that memory sees them in order, and the norm is a launch of its own.  Chunks of 2048 / 4096 / 8192 / 16384 elements: 98 tensors of 6.3 GB 3351 /
-  // 3352 / 3412 / 3462 us (workgroups that take chunk after chunk 3906), of 1.9 GB 1347 / 1253 / 1285 / 1316.
+  // chunk, so that memory sees them in order, and the norm is a launch of its own.  Chunks of 2048 / 4096 / 8192 / 16384 elements: 98 tensors of
+  // 6.3 GB 3351 / 3352 / 3412 / 3462 us (workgroups that take chunk after chunk 3906), of 1.9 GB 1347 / 1253 / 1285 / 1316.
   p.large = p.elements > ((int64_t)16 << 20);
   p.chunk = p.large ? 4096 : 2048;
-  // What the caches cannot hold goes past them: 6.3 GB 3352 -> 3247 us with loads and stores of the scaling, 3239 with the loads for the squares; 135 MB into
-  // other tensors 191 -> 162 with the stores.
+  // What the caches cannot hold goes past them: 6.3 GB 3352 -> 3247 us with loads and stores of the scaling, 3239 with the loads for the squares,
+  // 3205 with all; 135 MB into other tensors 191 -> 162 with the stores.
   p.load_once = past_caches(read), p.store_once = past_caches(read + (written ? apart : 0));
   p.launches = (n + kClipTensors - 1) / kClipTensors;
   return OAPL_OK;
@@ -284,7 +285,7 @@ int32_t oapl_embed_fwd(const void* E, const int32_t* tokens, int64_t T, int32_t 
   if (!embed_sizes_ok(T, d, V)) return OAPL_ERR_SHAPE;
   if (!isfinite(scale)) return OAPL_ERR_BETA;
   if (T > 0 && (!E || !tokens)) return OAPL_ERR_NULL;
-  if (!element_aligned(E, dtype)) return OAPL_ERR_ALIGN;
+  if (!element_aligned(E, dtype) || (uintptr_t)tokens % sizeof(int32_t)) return OAPL_ERR_ALIGN;
   EmbedArgs a{E, tokens, {}, T, d, V, scale};
   if (int rc = take_rows(a.out, out, T, d, out_dtype, true)) return rc;
   if (T == 0) return OAPL_OK;
@@ -309,7 +310,7 @@ int32_t oapl_embed_bwd(const oapl_rows* dout, const int32_t* tokens, int64_t T, 
   if (!dE || (T > 0 && !tokens)) return OAPL_ERR_NULL;
   EmbedSumArgs a = {};
   if (int rc = take_rows(a.dout, dout, T, d, dtype, false)) return rc;
-  if (!element_aligned(dE, OAPL_F32)) return OAPL_ERR_ALIGN;
+  if (!element_aligned(dE, OAPL_F32) || (uintptr_t)tokens % sizeof(int32_t)) return OAPL_ERR_ALIGN;
   if (!workspace_ok(workspace, workspace_bytes, p.total)) return OAPL_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)stream;
   char* ws = (char*)workspace;
@@ -339,11 +340,11 @@ int32_t oapl_embed_bwd(const oapl_rows* dout, const int32_t* tokens, int64_t T, 
   s.present = (uint8_t*)(ws + p.off_present), s.status = (int*)ws;
   s.dE = accumulate ? nullptr : dE;
   s.T = T, s.V = V, s.d = d, s.bits = p.bits, s.block = kSortThreads * p.items, s.blocks = p.blocks;
-  // Rows without tokens alone are cleared where that leaves out enough: 140897 tokens, d = 4096, V = 151936 774 us, all rows 833; 50000, d = 1024 176, 182; 16000, d = 4096
-  // 482, 472; d = 256 (rows of 1 KB) 50000 92, 73.
+  // Rows without tokens alone are cleared where that leaves out enough: 140897 tokens, d = 4096, V = 151936 774 us, all rows 833; 50000, d = 1024
+  // 176, 182; 16000, d = 4096 482, 472; d = 256 (rows of 1 KB) 50000 92, 73.
   s.clear_absent = d >= 1024 && 8 * T >= V;
-  // ... after what the first pass leaves time for: 140897 tokens, d = 4096, V = 151936 with 0 / 64 / 128 / 224 MB of it 742 / 737 / 731 / 725 us, 140000, d = 1024 249 / 245 / 241 / 237;
-  // 12000, d = 4096, V = 8192 (134 MB in all) 73.7, with all of it 76.
+  // ... after what the first pass leaves time for: 140897 tokens, d = 4096, V = 151936 with 0 / 64 / 128 / 224 MB of it 742 / 737 / 731 / 725 us,
+  // 140000, d = 1024 249 / 245 / 241 / 237; 12000, d = 4096, V = 8192 (134 MB in all) 73.7, with all of it 76.
   s.early = (int)std::min<int64_t>(V / 4, 192000000 / (4 * (int64_t)d));
   if (int rc = p.items == 2 ? launch_embed_sort<2>(s, st) : launch_embed_sort<8>(s, st)) return rc;
   a.partials = (float*)(ws + p.off_partials);

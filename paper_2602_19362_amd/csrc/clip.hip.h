@@ -2,10 +2,9 @@
 //
 //   N = sqrt(sum over tensors of sum_i g_i^2),      g <- g max_norm / N  where N is finite and larger than max_norm
 //
-// Bound by memory: the gradients are read once for the norm and once for the scaling, and written once (98 tensors of 6.3 GB, into others: 19 GB in 3.2
-// ms, 5.9 TB/s).  Squares are taken and added up in
-// 64 bits, so that no gradient's square is too large or too small for its sum; every workgroup has a fixed share of the tensors, and the
-// shares are added in a fixed order.
+// Bound by memory: the gradients are read once for the norm and once for the scaling, and written once (98 tensors of 6.3 GB, into others: 19
+// GB in 3.2 ms, 5.9 TB/s).  Squares are taken and added up in 64 bits, so that no gradient's square is too large or too small for its sum;
+// every workgroup has a fixed share of the tensors, and the shares are added in a fixed order.
 #pragma once
 
 #include "rows.hip.h"
@@ -58,7 +57,7 @@ __device__ __forceinline__ double clip_block_sum(double v) {
   return ((all[0] + all[1]) + all[2]) + all[3];
 }
 
-// A workgroup's sum over every gridDim.x-th chunk.  98 tensors of 6.3 GB: 5.8 TB/s.  ONCE: past the caches.
+// A workgroup's sum over every gridDim.x-th chunk.  98 tensors of 6.3 GB: 6.6 TB/s.  ONCE: past the caches.
 template <bool ONCE>
 __global__ __launch_bounds__(256) void k_grad_squares(const ClipArgs p) {
   double sum = 0.0;
@@ -90,8 +89,9 @@ __global__ __launch_bounds__(256) void k_grad_norm(const ClipArgs p) {
   if (threadIdx.x == 0) *p.norm_out = norm;
 }
 
-// The last chunks first: of what was read for the norm, those are still in the memory-side cache.  The factor is a number of 64 bits, and so is
-// its product with a gradient until that is rounded: 32 bits would hold a factor below 2^-126 in fewer bits.
+// The last chunks first: of what was read for the norm, those are still in the memory-side cache.  The same 98 tensors: 5.7 TB/s.  The factor is
+// a number of 64 bits, and so is its product with a gradient until that is rounded (for bf16 to 32 bits first, which moves the last rounding
+// by 2^-24): 32 bits would hold a factor below 2^-126 in fewer bits.
 template <bool LOAD_ONCE, bool STORE_ONCE>
 __global__ __launch_bounds__(256) void k_grad_scale(const ClipArgs p) {
   const float norm = clip_norm(p);

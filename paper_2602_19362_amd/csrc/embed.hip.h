@@ -206,7 +206,7 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_place(const SortArgs p) 
     }
     if constexpr (PASS == 0) {
       // Counts for the second pass.  Lanes that add to the same one as the first of their digit, as those of a frequent token do, add together:
-      // one atomic after the other at the same place took 15 of 38 us of 140897 tokens, one in twelve of them the same.
+      // 140897 tokens, one in 40 of them the same, V = 151936, each lane for itself / together, us for the whole call: d = 64 94 / 86, 4096 730 / 724.
       const int at = any ? (to / (kSortThreads * ITEMS) << p.bits) + (key[i] >> p.bits) : -1;
       const int with = __shfl(at, first[i], 64);
       const uint64_t together = __ballot(at == with) & same[i];

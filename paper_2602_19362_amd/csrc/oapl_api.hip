@@ -1613,7 +1613,7 @@ const char* oapl_status_string(int32_t status) {
     case OAPL_ERR_HIP: return "HIP launch or runtime call failed";
     case OAPL_ERR_TOKEN_RANGE: return "sampled token outside [0, V)";
     case OAPL_ERR_SCRATCH_LIMIT: return "sizes need more than the library's 64 MiB static scratch";
-    case OAPL_ERR_ALIGN: return "a pointer or stride is not a multiple of 16 bytes";
+    case OAPL_ERR_ALIGN: return "a pointer or stride is not a multiple of 16 bytes, or a pointer not one of an element";
     default: return "unknown status";
   }
 }

@@ -50,7 +50,7 @@ def grad_norm(items=((AT, None, 4, 0),), n=None, norm=AT, ws=AT, have=1 << 24):
     ({"d": (1 << 21) + 1}, SHAPE), ({"V": (1 << 21) + 1}, SHAPE), ({"T": 1 << 23, "d": 1 << 18}, SHAPE), ({"scale": INF}, BETA),
     ({"scale": NAN}, BETA), ({"E": None}, NULL),
     ({"tokens": None}, NULL), ({"out": None}, NULL), ({"out": R(None)}, NULL), ({"out": R(AT, 63)}, SHAPE), ({"out": R(AT, -64)}, SHAPE),
-    ({"E": AT + 1}, ALIGN), ({"out": R(AT + 1)}, ALIGN), ({"dtype": 0, "E": AT + 2}, ALIGN),
+    ({"out": R(AT, 1 << 46)}, SHAPE), ({"tokens": AT + 2}, ALIGN), ({"E": AT + 1}, ALIGN), ({"out": R(AT + 1)}, ALIGN), ({"dtype": 0, "E": AT + 2}, ALIGN),
 ])
 def test_the_lookup_refuses(kw, want):
     assert embed(**kw) == want
@@ -59,7 +59,7 @@ def test_the_lookup_refuses(kw, want):
 @pytest.mark.parametrize("kw, want", [
     ({"dtype": 5}, DTYPE), ({"T": -1}, SHAPE), ({"T": 65535 * 256 + 1}, SHAPE), ({"V": 0}, SHAPE), ({"d": 0}, SHAPE), ({"scale": INF}, BETA),
     ({"dE": None}, NULL), ({"tokens": None}, NULL), ({"dout": None}, NULL), ({"dout": R(None)}, NULL), ({"dout": R(AT, -1)}, SHAPE),
-    ({"dout": R(AT + 1)}, ALIGN), ({"dE": AT + 2}, ALIGN), ({"ws": None}, WORKSPACE), ({"ws": AT + 8}, WORKSPACE), ({"have": 255}, WORKSPACE),
+    ({"dout": R(AT + 1)}, ALIGN), ({"dE": AT + 2}, ALIGN), ({"tokens": AT + 1}, ALIGN), ({"ws": None}, WORKSPACE), ({"ws": AT + 8}, WORKSPACE), ({"have": 255}, WORKSPACE),
 ])
 def test_the_lookups_gradient_refuses(kw, want):
     assert embed_bwd(**kw) == want
