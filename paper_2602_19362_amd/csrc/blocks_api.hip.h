@@ -51,16 +51,17 @@ static bool embed_plan(EmbedPlan& p, int64_t T, int d, int V) {
     return was;
   };
   p.off_keys[1] = take(T * 4), p.off_places[1] = take(T * 4);
-  // Counting / sorting, us for the whole call: fp32, d = 64, V = 1000: 6000 tokens 23 / 39, 8192 31 / 39, 12000 59 / 40; bf16, V = 1000, 8192
-  // tokens: d = 1024 47 / 44, 4096 92 / 49 (a frequent token's rows are read by one workgroup a slice); 4096 at d = 4096, V = 1544 40 / 44.
-  p.few = T <= (d <= 512 ? kFewTokens : kFewTokens / 2);
+  // Counting / sorting, us for the whole call in bf16: d = 512, V = 1000 8000 tokens 28 / 34; d = 1024 30 / 36; d = 2048, V = 8192 41 / 43; d = 4096,
+  // V = 1544 6000 34 / 45, 8000 45 / 44; d = 5120, V = 8192 6000 65 / 65 (a frequent token's rows are read by one workgroup a slice).
+  p.few = T <= (d <= 2048 ? kFewTokens : kFewTokens * 3 / 4);
   if (p.few) return true;
   while (((int64_t)1 << (2 * p.bits)) <= V) ++p.bits;      // ids 0 .. V
   p.items = T <= 128 * kSortThreads * 2 ? 2 : 8;
   p.blocks = (int)std::max<int64_t>(1, (T + (int64_t)kSortThreads * p.items - 1) / (kSortThreads * p.items));
-  // 32 / 64 / 128 rows a tile, us for the whole call in bf16: d = 4096, V = 1544: 5000 tokens 44 / 55 / 77, 10000 56 / 69 / 96, 20000 87 / 83 / 113,
-  // 80000 211 / 206 / 229; d = 1024 20000 46 / 56 / 77, 40000 58 / 68 / 87, 80000 95 / 92 / 119; d = 4096, V = 151936 140897 785 / 772 / 788.
-  p.tile = T * ((d + 1023) / 1024) <= 1 << 16 ? 32 : 64;
+  // By the wavefronts that a row's channels take, all rows together.  16 / 32 / 64 rows a tile, us for the whole call in bf16: d = 4096: V = 1544
+  // 10000 tokens 55 / 51 / 51, 20000 82 / 77 / 75, V = 151936 140897 762 / 731 / 723; d = 1024, V = 8192 40000 62 / 59 / 61, 80000 92 / 88 / 87; d = 64,
+  // V = 151936 50000 47 / 50 / 54, 140000 67 / 65 / 67, V = 8192 400000 144 / 129 / 125.
+  p.tile = T * ((d + 255) / 256) <= 1 << 18 ? 32 : 64;
   p.tiles = (int)((T + p.tile - 1) / p.tile);
   p.off_keys[0] = take(T * 4), p.off_places[0] = take(T * 4);
   for (int i = 0; i < 2; ++i) p.off_counts[i] = take(((int64_t)p.blocks << p.bits) * 4);
@@ -350,9 +351,9 @@ int32_t oapl_embed_bwd(const oapl_rows* dout, const int32_t* tokens, int64_t T, 
   a.partials = (float*)(ws + p.off_partials);
   a.tile = p.tile, a.tiles = p.tiles, a.slices = (int)grid1d(d, 1024);
   const unsigned grid = (unsigned)p.tiles * a.slices;
-  // Rows that the caches do not hold go past them: 140897 tokens, d = 4096 (1.15 GB) 785 -> 771 us, with rows of dE past them too 739;
-  // 4096 at V = 1544 (34 MB) 46 -> 60.  (Eight channels a lane and four rows under way: T = 140000, V = 1000 320 -> 282 us, this one 739 -> 781.)
-  const bool once = past_caches(T * d * (int64_t)esize(dtype));
+  // Beyond 64 MiB rows, in and out, go past the caches, us in bf16: 140897 tokens, d = 4096 (1.15 GB) 758 -> 723, 40000, d = 2048, V = 151936
+  // 300 -> 286; d = 4096: V = 1000 15000 (123 MB) 66 -> 62, V = 1544 10000 (82 MB) 51 -> 52; d = 2048, V = 8192 10000 (41 MB) 46 -> 48.
+  const bool once = T * d * (int64_t)esize(dtype) > (int64_t)64 << 20;
   by_truth(d % 4 == 0, [&](auto whole) {
     by_truth(once, [&](auto past) {
       constexpr bool WHOLE = whole, ONCE = past;
@@ -361,7 +362,10 @@ int32_t oapl_embed_bwd(const oapl_rows* dout, const int32_t* tokens, int64_t T, 
     });
   });
   OAPL_LAUNCH_CHECK();
-  k_embed_join<<<dim3(grid1d(p.tiles, kJoinTiles), grid1d(d, 256)), 64 * kJoinParts, 0, st>>>(a);
+  by_truth(d % 4 == 0, [&](auto whole) {
+    constexpr bool WHOLE = whole;
+    k_embed_join<WHOLE><<<dim3(grid1d(p.tiles, kJoinTiles), grid1d(d, 256)), 64 * kJoinParts, 0, st>>>(a);
+  });
   OAPL_LAUNCH_CHECK();
   return OAPL_OK;
 }

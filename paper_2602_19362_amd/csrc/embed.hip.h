@@ -243,8 +243,10 @@ __device__ __forceinline__ void put_row(const EmbedSumArgs& p, int64_t v, int c,
   store_piece<4, WHOLE, ONCE>(row, c, p.d, sum);
 }
 
-// Rows of dout whose loads are under way together.
-constexpr int kEmbedRows = 8;
+// Rows of dout whose loads are under way together.  Where fewer are left, the last one is loaded again and left out: a branch around a load keeps
+// those after it waiting (140000 tokens, d = 1024, V = 1000 130 us with branches, 102 without; 4000, d = 4096, V = 1544 33 / 26).  Of sorted rows in tiles 16
+// (140897 tokens, d = 4096, V = 151936 4 / 8 / 16: 734 / 728 / 723 us).
+constexpr int kEmbedRows = 8, kSumRows = 16;
 
 // The sum of `n` of 64 rows, from the i-th on, whose positions a wavefront's lanes have.
 template <class T, int ROWS, bool WHOLE>
@@ -252,7 +254,7 @@ __device__ __forceinline__ void add_rows(const EmbedSumArgs& p, Piece<4>& sum, i
   Piece<4> x[ROWS] = {};
 #pragma unroll
   for (int u = 0; u < ROWS; ++u)
-    if (u < n) x[u] = load_piece<4, WHOLE>(p.dout.row<T>(__builtin_amdgcn_readlane(place, i + u)), c, p.d);
+    x[u] = load_piece<4, WHOLE>(p.dout.row<T>(__builtin_amdgcn_readlane(place, i + min(u, n - 1))), c, p.d);
 #pragma unroll
   for (int u = 0; u < ROWS; ++u)
     if (u < n) {
@@ -276,13 +278,13 @@ __global__ __launch_bounds__(256) void k_embed_sum(const EmbedSumArgs p) {
     const int key = lane < n ? p.keys[base + lane] : -1, place = lane < n ? p.places[base + lane] : 0;
     const int after = lane + 1 < n || (lane < n && base + n < to) ? p.keys[base + lane + 1] : -1;
     const uint64_t ends = __ballot(key != after);
-    for (int i = 0; i < n; i += kEmbedRows) {
-      Piece<4> x[kEmbedRows] = {};
+    for (int i = 0; i < n; i += kSumRows) {
+      Piece<4> x[kSumRows] = {};
 #pragma unroll
-      for (int u = 0; u < kEmbedRows; ++u)
-        if (i + u < n) x[u] = load_piece<4, WHOLE, ONCE>(p.dout.row<T>(__builtin_amdgcn_readlane(place, i + u)), c, p.d);
+      for (int u = 0; u < kSumRows; ++u)
+        x[u] = load_piece<4, WHOLE, ONCE>(p.dout.row<T>(__builtin_amdgcn_readlane(place, min(i + u, n - 1))), c, p.d);
 #pragma unroll
-      for (int u = 0; u < kEmbedRows; ++u) {
+      for (int u = 0; u < kSumRows; ++u) {
         if (i + u >= n) break;
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum.v[e] += x[u].v[e];
@@ -300,11 +302,13 @@ __global__ __launch_bounds__(256) void k_embed_sum(const EmbedSumArgs p) {
 // Tokens that reach over the ends of tiles: where one ends in one of a workgroup's tiles, its wavefronts add up what the tiles have of it,
 // equal parts of them each, in their order and in 64 bits.  Tiles and wavefronts of a workgroup 4 and 4 / 4 and 8 / 16 and 8 / 16 and 16, whole call of
 // 140897 tokens: 783 / 807 / 804 / 885 us.
+// Its loads need no branch where rows are whole: 100000 tokens, d = 64, V = 8192, one id, 569 -> 183 us; one in every 21 of V = 1000 75 -> 55.
 constexpr int kJoinTiles = 4, kJoinParts = 4;
 
+template <bool WHOLE>
 __global__ __launch_bounds__(64 * kJoinParts) void k_embed_join(const EmbedSumArgs p) {
   __shared__ double parts[kJoinParts][4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (blockIdx.y * 64 + lane) * 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = (blockIdx.y * 64 + lane) * 4;
   const int tile0 = blockIdx.x * kJoinTiles;
   const int64_t from = (int64_t)(tile0 + lane) * p.tile, to = from + p.tile < p.T ? from + p.tile : p.T;
   int key = p.V;
@@ -326,7 +330,7 @@ __global__ __launch_bounds__(64 * kJoinParts) void k_embed_join(const EmbedSumAr
     double sum[4] = {};
 #pragma unroll 8
     for (int i = lo; i < hi; ++i) {
-      const Piece<4> x = load_piece<4, false>(p.partials + ((int64_t)(begin + i) * 2 + (i == 0)) * p.d, c, p.d);
+      const Piece<4> x = load_piece<4, WHOLE>(p.partials + ((int64_t)(begin + i) * 2 + (i == 0)) * p.d, c, p.d);
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[e] += (double)x.v[e];
     }
@@ -342,7 +346,7 @@ __global__ __launch_bounds__(64 * kJoinParts) void k_embed_join(const EmbedSumAr
         for (int w = 1; w < kJoinParts; ++w) all += parts[w][e][lane];
         x.v[e] = (float)all;
       }
-      put_row<false>(p, v, c, x);
+      put_row<WHOLE>(p, v, c, x);
     }
     __syncthreads();
   }
@@ -436,7 +440,7 @@ __global__ __launch_bounds__(64 * kRunWaves) void k_embed_runs(const EmbedSumArg
     Piece<4> x[kEmbedRows] = {};
 #pragma unroll
     for (int u = 0; u < kEmbedRows; ++u)
-      if (i + u < end) x[u] = load_piece<4, WHOLE>(p.dout.row<T>(__builtin_amdgcn_readlane(place, i + u)), c, p.d);
+      x[u] = load_piece<4, WHOLE>(p.dout.row<T>(__builtin_amdgcn_readlane(place, min(i + u, end - 1))), c, p.d);
 #pragma unroll
     for (int u = 0; u < kEmbedRows; ++u) {
       if (i + u >= end) break;
@@ -461,7 +465,7 @@ __global__ __launch_bounds__(64 * kRunWaves) void k_embed_runs(const EmbedSumArg
   sum = Piece<4>{};
   for (int base = lo; base < hi; base += 64) {
     const int at = base + lane < hi ? p.places[base + lane] : 0, here = hi - base < 64 ? hi - base : 64;
-    for (int i = 0; i < here; i += 2 * kEmbedRows) add_rows<T, 2 * kEmbedRows, WHOLE>(p, sum, at, i, here - i, c);
+    for (int i = 0; i < here; i += kEmbedRows) add_rows<T, kEmbedRows, WHOLE>(p, sum, at, i, here - i, c);
   }
   parts[wave][lane] = sum;
   __syncthreads();

@@ -22,8 +22,8 @@ int main() {
   void* one = (void*)(uintptr_t)256;      // aligned, never dereferenced
   float* f = (float*)one;
   const int32_t* tokens = (const int32_t*)one;
-  const int64_t counts[] = {INT64_MIN, -1, 0, 1, 31, 4096, 4097, 8192, 8193, 262144, 262145, (int64_t)65535 * 256, (int64_t)65535 * 256 + 1, INT64_MAX};
-  const int32_t widths[] = {INT_MIN, -1, 0, 1, 7, 128, 512, 513, 1024, 8192, 16384, 16385, 1 << 21, (1 << 21) + 1, INT_MAX};
+  const int64_t counts[] = {INT64_MIN, -1, 0, 1, 31, 4096, 4097, 6144, 6145, 8192, 8193, 262144, 262145, (int64_t)65535 * 256, (int64_t)65535 * 256 + 1, INT64_MAX};
+  const int32_t widths[] = {INT_MIN, -1, 0, 1, 7, 128, 512, 513, 1024, 2048, 2049, 8192, 16384, 16385, 1 << 21, (1 << 21) + 1, INT_MAX};
   const int64_t strides[] = {INT64_MIN, -8, 0, 8, 16384, (int64_t)1 << 40, ((int64_t)1 << 40) + 1, INT64_MAX};
   long plans = 0, calls = 0;
 
@@ -35,6 +35,8 @@ int main() {
         CHECK(good == (T >= 0 && T <= (int64_t)65535 * 256 && d >= 1 && d <= 1 << 21 && V >= 1 && V <= 1 << 21 && T * d <= (int64_t)1 << 40));
         CHECK(oapl_embed_workspace_bytes(T, d, V) == (good ? p.total : 0) && (!good || p.total % 256 == 0));
         ++plans;
+        // counting holds all ids in a workgroup's LDS
+        CHECK(!good || !p.few || T <= kFewTokens);
         if (!good || p.few) continue;
         // ids 0 .. V have two digits; blocks and tiles hold all tokens; a workgroup's counts fit the LDS
         CHECK(((int64_t)1 << (2 * p.bits)) > V && p.bits <= 11 && (kSortThreads / 64 + 2) * (4 << p.bits) <= 150 * 1024);

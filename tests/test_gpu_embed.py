@@ -77,6 +77,12 @@ CASES = [("bf16", 1, 8, 1, "one"), ("bf16", 5, 64, 100, "even"), ("f32", 63, 20,
          ("bf16", 30000, 2056, 32000, "one"), ("f32", 300001, 4, 70000, "zipf"), ("bf16", 262145, 3, 1 << 21, "even"), ("f32", 9000, 1, 1 << 21, "ends")]
 
 
+# On both sides of the rules: sorting by counting or in passes, tiles of sorted rows, rows past the caches.
+RULES = [("bf16", 8192, 2048, 700, "zipf"), ("bf16", 8193, 2048, 700, "zipf"), ("bf16", 6144, 2052, 900, "one"), ("f32", 6145, 2052, 900, "zipf"),
+         ("bf16", 8192, 2050, 300, "zipf"), ("f32", 262144, 12, 5000, "zipf"), ("f32", 262145, 12, 5000, "zipf"), ("bf16", 8192, 4096, 500, "even"),
+         ("bf16", 8193, 4096, 500, "even"), ("f32", 4097, 4099, 300, "zipf"), ("bf16", 100000, 64, 8192, "one"), ("f32", 20000, 66, 1000, "one")]
+
+
 @pytest.mark.parametrize("dtype, T, d, V, kind", CASES)
 def test_gradient(dtype, T, d, V, kind):
     tokens = _tokens(kind, T, V)
@@ -100,6 +106,27 @@ def test_gradient(dtype, T, d, V, kind):
     r.workspace.fill_(255)
     third = oapl.embed_bwd(dout, tokens, scale=0.7, dE=torch.full_like(r.dE, torch.nan), workspace=r.workspace)
     assert torch.equal(third.dE, r.dE)
+
+
+@pytest.mark.parametrize("dtype, T, d, V, kind", RULES)
+def test_gradient_beside_the_rules(dtype, T, d, V, kind):
+    test_gradient(dtype, T, d, V, kind)
+
+
+@pytest.mark.parametrize("T, d", [(500, 40), (7000, 64), (9001, 64), (9001, 70), (50000, 256)])
+def test_gradient_of_a_padded_batch(T, d):
+    """Half of the tokens are the same one, and tokens outside the embedding lie among them."""
+    V = 1544
+    tokens = _tokens("even", T, V)
+    tokens[1::2] = 7
+    tokens[::97] = V
+    dout = torch.randn(T, d, generator=_gen(6), device=DEV).bfloat16()
+    r = oapl.embed_bwd(dout, tokens, V)
+    assert oapl.read_device_status(r.workspace) != 0
+    inside = tokens < V
+    want, bound = orc.embed_grads(dout[inside], tokens[inside], V, 1.0)
+    near(r.dE, want, bound)
+
 
 
 @pytest.mark.parametrize("T", [6, 3000])
