@@ -9,7 +9,7 @@
 // launch, tile by tile (k_embed_join).  dE is cleared beside the sorting, not between reads: memory takes 6 TB/s of either alone and 4.9 of both.
 //
 // 140897 tokens that follow Zipf's law, d = 4096 in bf16, V = 151936 (3.6 GB): counting 6 us, first pass and 0.19 GB of zeros 40,
-// second pass and 1.72 GB of zeros 290, sums 368 (1.15 GB in, 0.65 out: 4.9 TB/s), tokens over tiles 23.  1003 of them: places and 2.49 GB of zeros 343, sums 19.
+// second pass and 1.72 GB of zeros 290, sums 366 (1.15 GB in, 0.65 out: 4.9 TB/s), tokens over tiles 22.  1003 of them: places and 2.49 GB of zeros 343, sums 12.
 #pragma once
 
 #include "rows.hip.h"
