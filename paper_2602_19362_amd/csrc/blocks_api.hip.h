@@ -82,23 +82,33 @@ static void by_truth(bool x, F f) {
   else f(std::false_type{});
 }
 
+// f(how rows of d channels lie in pieces of W, as a type).  NARROW: d may be smaller than W.
+template <int W, bool NARROW, class F>
+static void by_form(int d, F f) {
+  if (d % W == 0) return f(std::integral_constant<Form, kWhole>{});
+  if constexpr (NARROW)
+    if (d < W) return f(std::integral_constant<Form, kAny>{});
+  f(std::integral_constant<Form, kRagged>{});
+}
+
 // Accesses of so many bytes go past the caches: the memory-side one holds 256 MiB.
 static bool past_caches(int64_t bytes) { return bytes > (int64_t)256 << 20; }
 
 template <class TE, class T>
 static int launch_embed_fwd(EmbedArgs a, hipStream_t st) {
   constexpr int W = sizeof(TE) + sizeof(T) == 4 ? 8 : 4;
-  const auto launch = [&](auto pieces, auto whole, auto once) {
+  const auto launch = [&](auto pieces, auto form, auto once) {
     constexpr int PIECES = pieces;
-    constexpr bool WHOLE = whole, ONCE = once;
+    constexpr Form FORM = form;
+    constexpr bool ONCE = once;
     a.slices = grid1d(a.d, 64 * W * PIECES);
-    k_embed_fwd<TE, T, W, PIECES, WHOLE, ONCE><<<wide_grid((a.T * a.slices + 3) / 4, 1 << 23), 256, 0, st>>>(a);
+    k_embed_fwd<TE, T, W, PIECES, FORM, ONCE><<<wide_grid((a.T * a.slices + 3) / 4, 1 << 23), 256, 0, st>>>(a);
   };
-  by_truth(a.d % W == 0, [&](auto whole) {
+  by_form<W, true>(a.d, [&](auto form) {
     by_truth(past_caches(a.T * a.d * (int64_t)sizeof(T)), [&](auto once) {
       // 140000 rows of 256 channels in bf16, one piece a wavefront / two: 27 / 35 us; 20000 of 520 9.5 / 9.1
-      if (a.d <= 64 * W) launch(std::integral_constant<int, 1>{}, whole, once);
-      else launch(std::integral_constant<int, 2>{}, whole, once);
+      if (a.d <= 64 * W) launch(std::integral_constant<int, 1>{}, form, once);
+      else launch(std::integral_constant<int, 2>{}, form, once);
     });
   });
   OAPL_LAUNCH_CHECK();
@@ -325,10 +335,10 @@ int32_t oapl_embed_bwd(const oapl_rows* dout, const int32_t* tokens, int64_t T, 
     OAPL_LAUNCH_CHECK();
     if (T == 0) return OAPL_OK;
     const dim3 runs(grid1d(T, 32), grid1d(d, 256));
-    by_truth(d % 4 == 0, [&](auto whole) {
-      constexpr bool WHOLE = whole;
-      if (dtype == OAPL_BF16) k_embed_runs<bf16_t, WHOLE><<<runs, 64 * kRunWaves, 0, st>>>(a);
-      else k_embed_runs<float, WHOLE><<<runs, 64 * kRunWaves, 0, st>>>(a);
+    by_form<4, true>(d, [&](auto form) {
+      constexpr Form FORM = form;
+      if (dtype == OAPL_BF16) k_embed_runs<bf16_t, FORM><<<runs, 64 * kRunWaves, 0, st>>>(a);
+      else k_embed_runs<float, FORM><<<runs, 64 * kRunWaves, 0, st>>>(a);
     });
     OAPL_LAUNCH_CHECK();
     return OAPL_OK;
@@ -354,17 +364,18 @@ int32_t oapl_embed_bwd(const oapl_rows* dout, const int32_t* tokens, int64_t T, 
   // Beyond 64 MiB rows, in and out, go past the caches, us in bf16: 140897 tokens, d = 4096 (1.15 GB) 758 -> 723, 40000, d = 2048, V = 151936
   // 300 -> 286; d = 4096: V = 1000 15000 (123 MB) 66 -> 62, V = 1544 10000 (82 MB) 51 -> 52; d = 2048, V = 8192 10000 (41 MB) 46 -> 48.
   const bool once = T * d * (int64_t)esize(dtype) > (int64_t)64 << 20;
-  by_truth(d % 4 == 0, [&](auto whole) {
+  by_form<4, true>(d, [&](auto form) {
     by_truth(once, [&](auto past) {
-      constexpr bool WHOLE = whole, ONCE = past;
-      if (dtype == OAPL_BF16) k_embed_sum<bf16_t, WHOLE, ONCE><<<grid, 256, 0, st>>>(a);
-      else k_embed_sum<float, WHOLE, ONCE><<<grid, 256, 0, st>>>(a);
+      constexpr Form FORM = form;
+      constexpr bool ONCE = past;
+      if (dtype == OAPL_BF16) k_embed_sum<bf16_t, FORM, ONCE><<<grid, 256, 0, st>>>(a);
+      else k_embed_sum<float, FORM, ONCE><<<grid, 256, 0, st>>>(a);
     });
   });
   OAPL_LAUNCH_CHECK();
-  by_truth(d % 4 == 0, [&](auto whole) {
-    constexpr bool WHOLE = whole;
-    k_embed_join<WHOLE><<<dim3(grid1d(p.tiles, kJoinTiles), grid1d(d, 256)), 64 * kJoinParts, 0, st>>>(a);
+  by_form<4, true>(d, [&](auto form) {
+    constexpr Form FORM = form;
+    k_embed_join<FORM><<<dim3(grid1d(p.tiles, kJoinTiles), grid1d(d, 256)), 64 * kJoinParts, 0, st>>>(a);
   });
   OAPL_LAUNCH_CHECK();
   return OAPL_OK;
@@ -384,10 +395,10 @@ int32_t oapl_residual_norm_fwd(const oapl_rows* x, const oapl_rows* y, const voi
     typedef std::remove_pointer_t<decltype(t)> TY;
     constexpr int W = sizeof(TX) == 2 ? 8 : 4;
     by_width<W>(d, [&](auto lanes, auto most, auto pieces) {
-      by_truth(d % W == 0, [&](auto whole) {
+      by_form<W, decltype(lanes)::value == 16>(d, [&](auto form) {
         constexpr int LANES = lanes, MOST = most, PIECES = pieces;
-        constexpr bool WHOLE = whole;
-        k_residual_norm_fwd<TX, TY, W, LANES, MOST, PIECES, WHOLE>
+        constexpr Form FORM = form;
+        k_residual_norm_fwd<TX, TY, W, LANES, MOST, PIECES, FORM>
             <<<wide_grid(norm_workgroups(T, d), 1 << 21), norm_lanes(d), 0, (hipStream_t)stream>>>(a);
       });
     });
@@ -429,10 +440,10 @@ int32_t oapl_residual_norm_bwd(const oapl_rows* x, const oapl_rows* y, const voi
     if (T > 0) {
       constexpr int W = sizeof(TX) == 2 ? 8 : 4;
       by_width<W>(d, [&](auto lanes, auto most, auto pieces) {
-        by_truth(d % W == 0, [&](auto whole) {
+        by_form<W, decltype(lanes)::value == 16>(d, [&](auto form) {
           constexpr int LANES = lanes, MOST = most, PIECES = pieces;
-          constexpr bool WHOLE = whole;
-          k_residual_norm_bwd<TX, TY, W, LANES, MOST, PIECES, WHOLE><<<grid, norm_lanes(d), 0, st>>>(a);
+          constexpr Form FORM = form;
+          k_residual_norm_bwd<TX, TY, W, LANES, MOST, PIECES, FORM><<<grid, norm_lanes(d), 0, st>>>(a);
         });
       });
       OAPL_LAUNCH_CHECK();

@@ -30,7 +30,7 @@ struct EmbedArgs {
 // A wavefront has a token and PIECES times 64 pieces of its row; those of a row follow each other, so that memory is written in order.
 // ONCE: results past the caches.  140897 tokens, d = 4096 in bf16, 1 / 2 / 4 pieces: 361 / 308 / 315 us, past the caches 332 / 284 / 300 (1.15 GB
 // written, 0.31 of the embedding read: 5.2 TB/s), slices of rows one after the other 462 / 433 / 331 and 424 / 397 / 316.
-template <class TE, class T, int W, int PIECES, bool WHOLE, bool ONCE>
+template <class TE, class T, int W, int PIECES, Form FORM, bool ONCE>
 __global__ __launch_bounds__(256) void k_embed_fwd(const EmbedArgs p) {
   const uint32_t unit = (blockIdx.y * gridDim.x + blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = unit / p.slices;
   const int c = (unit % p.slices * PIECES * 64 + (threadIdx.x & 63)) * W;
@@ -41,12 +41,12 @@ __global__ __launch_bounds__(256) void k_embed_fwd(const EmbedArgs p) {
   const float scale = inside ? p.scale : quiet_nan();
   Piece<W> x[PIECES];
 #pragma unroll
-  for (int i = 0; i < PIECES; ++i) x[i] = load_piece<W, WHOLE>(from, c + i * 64 * W, p.d);
+  for (int i = 0; i < PIECES; ++i) x[i] = load_piece<W, FORM>(from, c + i * 64 * W, p.d);
 #pragma unroll
   for (int i = 0; i < PIECES; ++i) {
 #pragma unroll
     for (int e = 0; e < W; ++e) x[i].v[e] *= scale;
-    store_piece<W, WHOLE, ONCE>(p.out.row<T>(t), c + i * 64 * W, p.d, x[i]);
+    store_piece<W, FORM, ONCE>(p.out.row<T>(t), c + i * 64 * W, p.d, x[i]);
   }
 }
 
@@ -118,7 +118,7 @@ __device__ __forceinline__ void clear_rows(const SortArgs& p, int64_t i) {
   if (v >= (PASS == 0 ? p.early : p.V) || (PASS == 1 && p.present[v])) return;
   float* row = p.dE + v * p.d;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) store_piece<4, false>(row, (int)(i % pieces) * 1024 + (j * 64 + lane) * 4, p.d, Piece<4>{});
+  for (int j = 0; j < 4; ++j) store_piece<4, kAny>(row, (int)(i % pieces) * 1024 + (j * 64 + lane) * 4, p.d, Piece<4>{});
 }
 
 // Pass 0 reads tokens, pass 1 what pass 0 left.  A key's place: keys of smaller digits, those of its digit in earlier blocks, in earlier
@@ -230,17 +230,17 @@ struct EmbedSumArgs {
 };
 
 // A row's sum into dE.  ONCE: past the caches.
-template <bool WHOLE, bool ONCE = false>
+template <Form FORM, bool ONCE = false>
 __device__ __forceinline__ void put_row(const EmbedSumArgs& p, int64_t v, int c, Piece<4> sum) {
   float* row = p.dE + v * p.d;
 #pragma unroll
   for (int e = 0; e < 4; ++e) sum.v[e] *= p.scale;
   if (p.add) {
-    const Piece<4> old = load_piece<4, WHOLE>(row, c, p.d);
+    const Piece<4> old = load_piece<4, FORM>(row, c, p.d);
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum.v[e] += old.v[e];
   }
-  store_piece<4, WHOLE, ONCE>(row, c, p.d, sum);
+  store_piece<4, FORM, ONCE>(row, c, p.d, sum);
 }
 
 // Rows of dout whose loads are under way together.  Where fewer are left, the last one is loaded again and left out: a branch around a load keeps
@@ -249,12 +249,12 @@ __device__ __forceinline__ void put_row(const EmbedSumArgs& p, int64_t v, int c,
 constexpr int kEmbedRows = 8, kSumRows = 16;
 
 // The sum of `n` of 64 rows, from the i-th on, whose positions a wavefront's lanes have.
-template <class T, int ROWS, bool WHOLE>
+template <class T, int ROWS, Form FORM>
 __device__ __forceinline__ void add_rows(const EmbedSumArgs& p, Piece<4>& sum, int place, int i, int n, int c) {
   Piece<4> x[ROWS] = {};
 #pragma unroll
   for (int u = 0; u < ROWS; ++u)
-    x[u] = load_piece<4, WHOLE>(p.dout.row<T>(__builtin_amdgcn_readlane(place, i + min(u, n - 1))), c, p.d);
+    x[u] = load_piece<4, FORM>(p.dout.row<T>(__builtin_amdgcn_readlane(place, i + min(u, n - 1))), c, p.d);
 #pragma unroll
   for (int u = 0; u < ROWS; ++u)
     if (u < n) {
@@ -265,7 +265,7 @@ __device__ __forceinline__ void add_rows(const EmbedSumArgs& p, Piece<4>& sum, i
 
 // A workgroup sums up 1024 channels, four a lane, of a tile's rows; the slices of a tile run side by side.  A wavefront has the ids and
 // positions of 64 rows in its lanes, so that its walk over them branches on scalars.  ONCE: rows past the caches, in and out.
-template <class T, bool WHOLE, bool ONCE>
+template <class T, Form FORM, bool ONCE>
 __global__ __launch_bounds__(256) void k_embed_sum(const EmbedSumArgs p) {
   const int lane = threadIdx.x & 63, tile = blockIdx.x / p.slices, c = (blockIdx.x % p.slices * 256 + threadIdx.x) * 4;
   if (c - lane * 4 >= p.d) return;
@@ -282,7 +282,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(const EmbedSumArgs p) {
       Piece<4> x[kSumRows] = {};
 #pragma unroll
       for (int u = 0; u < kSumRows; ++u)
-        x[u] = load_piece<4, WHOLE, ONCE>(p.dout.row<T>(__builtin_amdgcn_readlane(place, min(i + u, n - 1))), c, p.d);
+        x[u] = load_piece<4, FORM, ONCE>(p.dout.row<T>(__builtin_amdgcn_readlane(place, min(i + u, n - 1))), c, p.d);
 #pragma unroll
       for (int u = 0; u < kSumRows; ++u) {
         if (i + u >= n) break;
@@ -290,9 +290,9 @@ __global__ __launch_bounds__(256) void k_embed_sum(const EmbedSumArgs p) {
         for (int e = 0; e < 4; ++e) sum.v[e] += x[u].v[e];
         if (!((ends >> (i + u)) & 1)) continue;
         const int v = __builtin_amdgcn_readlane(key, i + u);
-        if (begun && v == first) store_piece<4, WHOLE>(p.partials + (int64_t)tile * 2 * p.d, c, p.d, sum);
-        else if (open && v == last) store_piece<4, WHOLE>(p.partials + ((int64_t)tile * 2 + 1) * p.d, c, p.d, sum);
-        else if (v < p.V) put_row<WHOLE, ONCE>(p, v, c, sum);
+        if (begun && v == first) store_piece<4, FORM>(p.partials + (int64_t)tile * 2 * p.d, c, p.d, sum);
+        else if (open && v == last) store_piece<4, FORM>(p.partials + ((int64_t)tile * 2 + 1) * p.d, c, p.d, sum);
+        else if (v < p.V) put_row<FORM, ONCE>(p, v, c, sum);
         sum = Piece<4>{};
       }
     }
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(const EmbedSumArgs p) {
 // Its loads need no branch where rows are whole: 100000 tokens, d = 64, V = 8192, one id, 569 -> 183 us; one in every 21 of V = 1000 75 -> 55.
 constexpr int kJoinTiles = 4, kJoinParts = 4;
 
-template <bool WHOLE>
+template <Form FORM>
 __global__ __launch_bounds__(64 * kJoinParts) void k_embed_join(const EmbedSumArgs p) {
   __shared__ double parts[kJoinParts][4][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = (blockIdx.y * 64 + lane) * 4;
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(64 * kJoinParts) void k_embed_join(const EmbedSumAr
     double sum[4] = {};
 #pragma unroll 8
     for (int i = lo; i < hi; ++i) {
-      const Piece<4> x = load_piece<4, WHOLE>(p.partials + ((int64_t)(begin + i) * 2 + (i == 0)) * p.d, c, p.d);
+      const Piece<4> x = load_piece<4, FORM>(p.partials + ((int64_t)(begin + i) * 2 + (i == 0)) * p.d, c, p.d);
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[e] += (double)x.v[e];
     }
@@ -346,7 +346,7 @@ __global__ __launch_bounds__(64 * kJoinParts) void k_embed_join(const EmbedSumAr
         for (int w = 1; w < kJoinParts; ++w) all += parts[w][e][lane];
         x.v[e] = (float)all;
       }
-      put_row<WHOLE>(p, v, c, x);
+      put_row<FORM>(p, v, c, x);
     }
     __syncthreads();
   }
@@ -421,7 +421,7 @@ __global__ __launch_bounds__(256) void k_embed_rank(const EmbedSumArgs p, const 
 // V = 1000 17.7 / 22.3 us for the whole call.
 constexpr int kRunWaves = 8, kRunRows = 32 / kRunWaves;
 
-template <class T, bool WHOLE>
+template <class T, Form FORM>
 __global__ __launch_bounds__(64 * kRunWaves) void k_embed_runs(const EmbedSumArgs p) {
   __shared__ Piece<4> parts[kRunWaves][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (blockIdx.y * 64 + lane) * 4;
@@ -440,7 +440,7 @@ __global__ __launch_bounds__(64 * kRunWaves) void k_embed_runs(const EmbedSumArg
     Piece<4> x[kEmbedRows] = {};
 #pragma unroll
     for (int u = 0; u < kEmbedRows; ++u)
-      x[u] = load_piece<4, WHOLE>(p.dout.row<T>(__builtin_amdgcn_readlane(place, min(i + u, end - 1))), c, p.d);
+      x[u] = load_piece<4, FORM>(p.dout.row<T>(__builtin_amdgcn_readlane(place, min(i + u, end - 1))), c, p.d);
 #pragma unroll
     for (int u = 0; u < kEmbedRows; ++u) {
       if (i + u >= end) break;
@@ -448,7 +448,7 @@ __global__ __launch_bounds__(64 * kRunWaves) void k_embed_runs(const EmbedSumArg
       for (int e = 0; e < 4; ++e) sum.v[e] += x[u].v[e];
       if (i + u + 1 < n && !((begins >> (i + u + 1)) & 1)) continue;
       const int v = __builtin_amdgcn_readlane(key, i + u);
-      if (v < p.V) put_row<WHOLE>(p, v, c, sum);
+      if (v < p.V) put_row<FORM>(p, v, c, sum);
       sum = Piece<4>{};
     }
     i += kEmbedRows;
@@ -465,7 +465,7 @@ __global__ __launch_bounds__(64 * kRunWaves) void k_embed_runs(const EmbedSumArg
   sum = Piece<4>{};
   for (int base = lo; base < hi; base += 64) {
     const int at = base + lane < hi ? p.places[base + lane] : 0, here = hi - base < 64 ? hi - base : 64;
-    for (int i = 0; i < here; i += kEmbedRows) add_rows<T, kEmbedRows, WHOLE>(p, sum, at, i, here - i, c);
+    for (int i = 0; i < here; i += kEmbedRows) add_rows<T, kEmbedRows, FORM>(p, sum, at, i, here - i, c);
   }
   parts[wave][lane] = sum;
   __syncthreads();
@@ -474,7 +474,7 @@ __global__ __launch_bounds__(64 * kRunWaves) void k_embed_runs(const EmbedSumArg
   for (int w = 1; w < kRunWaves; ++w)
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum.v[e] += parts[w][lane].v[e];
-  put_row<WHOLE>(p, v, c, sum);
+  put_row<FORM>(p, v, c, sum);
 }
 
 }  // namespace oapl

@@ -61,8 +61,7 @@ struct RowLanes {
 };
 
 // TX: the residual stream's type, T: the block's and the norms'.  A lane holds W channels in each of PIECES pieces of a row; MOST lanes a workgroup.
-// WHOLE: d is a multiple of W.
-template <class TX, class T, int W, int LANES, int MOST, int PIECES, bool WHOLE>
+template <class TX, class T, int W, int LANES, int MOST, int PIECES, Form FORM>
 __global__ __launch_bounds__(MOST) void k_residual_norm_fwd(const ResidualNormArgs p) {
   const RowLanes<LANES> at;
   constexpr int ROWS = at.kRows;
@@ -74,13 +73,17 @@ __global__ __launch_bounds__(MOST) void k_residual_norm_fwd(const ResidualNormAr
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       const int c = (i * lanes + lane) * W;
-      rx[i] = load_raw<W, WHOLE>(p.x.row<TX>(t), c, d);
-      if (p.y.p) ry[i] = load_raw<W, WHOLE>(p.y.row<T>(t), c, d);
-      if (p.gate.p) rg[i] = load_raw<W, WHOLE>(p.gate.row<T>(t), c, d);
+      rx[i] = load_raw<W, FORM>(p.x.row<TX>(t), c, d);
+      if (p.y.p) ry[i] = load_raw<W, FORM>(p.y.row<T>(t), c, d);
+      if (p.gate.p) rg[i] = load_raw<W, FORM>(p.gate.row<T>(t), c, d);
     }
     Piece<W> x[PIECES];
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) x[i] = widened(rx[i]);
+    for (int i = 0; i < PIECES; ++i) {
+      const int c = (i * lanes + lane) * W;
+      ry[i] = own<FORM>(ry[i], c, d), rg[i] = own<FORM>(rg[i], c, d);
+      x[i] = widened(own<FORM>(rx[i], c, d));
+    }
     if (p.y.p) {
       float r = p.scale;
       if (p.y_gain) {
@@ -94,7 +97,7 @@ __global__ __launch_bounds__(MOST) void k_residual_norm_fwd(const ResidualNormAr
         const int c = (i * lanes + lane) * W;
         Piece<W> y = widened(ry[i]);
         if (p.y_gain) {
-          const Piece<W> g = load_piece<W, WHOLE>((const T*)p.y_gain, c, d);
+          const Piece<W> g = load_piece<W, FORM>((const T*)p.y_gain, c, d);
 #pragma unroll
           for (int e = 0; e < W; ++e) y.v[e] *= g.v[e];
         }
@@ -104,7 +107,7 @@ __global__ __launch_bounds__(MOST) void k_residual_norm_fwd(const ResidualNormAr
         }
 #pragma unroll
         for (int e = 0; e < W; ++e) x[i].v[e] += r * y.v[e];
-        store_piece<W, WHOLE>(p.x_out.row<TX>(t), c, d, x[i]);
+        store_piece<W, FORM>(p.x_out.row<TX>(t), c, d, x[i]);
       }
     }
     if (p.gain) {
@@ -115,10 +118,10 @@ __global__ __launch_bounds__(MOST) void k_residual_norm_fwd(const ResidualNormAr
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
         const int c = (i * lanes + lane) * W;
-        const Piece<W> g = load_piece<W, WHOLE>((const T*)p.gain, c, d);
+        const Piece<W> g = load_piece<W, FORM>((const T*)p.gain, c, d);
 #pragma unroll
         for (int e = 0; e < W; ++e) x[i].v[e] *= r * g.v[e];
-        store_piece<W, WHOLE>(p.out.row<T>(t), c, d, x[i]);
+        store_piece<W, FORM>(p.out.row<T>(t), c, d, x[i]);
       }
     }
   }
@@ -131,7 +134,7 @@ struct NormRow {
   Raw<T, W> dn[PIECES], y[PIECES], gate[PIECES];
 };
 
-template <class TX, class T, int W, int LANES, int MOST, int PIECES, bool WHOLE>
+template <class TX, class T, int W, int LANES, int MOST, int PIECES, Form FORM>
 __global__ __launch_bounds__(MOST) void k_residual_norm_bwd(const ResidualNormArgs p) {
   const RowLanes<LANES> at;
   constexpr int ROWS = at.kRows;
@@ -142,8 +145,8 @@ __global__ __launch_bounds__(MOST) void k_residual_norm_bwd(const ResidualNormAr
 #pragma unroll
   for (int i = 0; i < PIECES; ++i) {
     const int c = (i * lanes + lane) * W;
-    if (p.gain) gain[i] = load_raw<W, WHOLE>((const T*)p.gain, c, d);
-    if (p.y_gain) y_gain[i] = load_raw<W, WHOLE>((const T*)p.y_gain, c, d);
+    if (p.gain) gain[i] = own<FORM>(load_raw<W, FORM>((const T*)p.gain, c, d), c, d);
+    if (p.y_gain) y_gain[i] = own<FORM>(load_raw<W, FORM>((const T*)p.y_gain, c, d), c, d);
   }
   typedef NormRow<TX, T, W, PIECES> Row;
   const auto load = [&](Row& row, int64_t t) {
@@ -151,10 +154,10 @@ __global__ __launch_bounds__(MOST) void k_residual_norm_bwd(const ResidualNormAr
     for (int i = 0; i < PIECES; ++i) {
       const int c = (i * lanes + lane) * W;
       row.dx[i] = Raw<TX, W>{};
-      if (p.gain) row.x[i] = load_raw<W, WHOLE>(p.x.row<TX>(t), c, d), row.dn[i] = load_raw<W, WHOLE>(p.out.row<T>(t), c, d);
-      if (p.x_out.p) row.dx[i] = load_raw<W, WHOLE>(p.x_out.row<TX>(t), c, d);
-      if (p.y.p) row.y[i] = load_raw<W, WHOLE>(p.y.row<T>(t), c, d);
-      if (p.gate.p) row.gate[i] = load_raw<W, WHOLE>(p.gate.row<T>(t), c, d);
+      if (p.gain) row.x[i] = load_raw<W, FORM>(p.x.row<TX>(t), c, d), row.dn[i] = load_raw<W, FORM>(p.out.row<T>(t), c, d);
+      if (p.x_out.p) row.dx[i] = load_raw<W, FORM>(p.x_out.row<TX>(t), c, d);
+      if (p.y.p) row.y[i] = load_raw<W, FORM>(p.y.row<T>(t), c, d);
+      if (p.gate.p) row.gate[i] = load_raw<W, FORM>(p.gate.row<T>(t), c, d);
     }
   };
   const int64_t first = (int64_t)blockIdx.x * ROWS + at.row, step = (int64_t)gridDim.x * ROWS;
@@ -168,7 +171,12 @@ __global__ __launch_bounds__(MOST) void k_residual_norm_bwd(const ResidualNormAr
     if (AHEAD && t + step < p.T) load(next, t + step);
     Piece<W> dx[PIECES];
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) dx[i] = widened(row.dx[i]);
+    for (int i = 0; i < PIECES; ++i) {
+      const int c = (i * lanes + lane) * W;
+      row.x[i] = own<FORM>(row.x[i], c, d), row.dn[i] = own<FORM>(row.dn[i], c, d);
+      row.y[i] = own<FORM>(row.y[i], c, d), row.gate[i] = own<FORM>(row.gate[i], c, d);
+      dx[i] = widened(own<FORM>(row.dx[i], c, d));
+    }
     if (p.gain) {
       float sum = 0.f;
 #pragma unroll
@@ -194,7 +202,7 @@ __global__ __launch_bounds__(MOST) void k_residual_norm_bwd(const ResidualNormAr
         for (int e = 0; e < W; ++e) dx[i].v[e] += r * (u[i].v[e] - v[i].v[e] * m);
     }
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) store_piece<W, WHOLE>(p.dx.row<TX>(t), (i * lanes + lane) * W, d, dx[i]);
+    for (int i = 0; i < PIECES; ++i) store_piece<W, FORM>(p.dx.row<TX>(t), (i * lanes + lane) * W, d, dx[i]);
     if (p.y.p) {
       // from here on dx is dz
       float r = 1.f;
@@ -220,7 +228,7 @@ __global__ __launch_bounds__(MOST) void k_residual_norm_bwd(const ResidualNormAr
             dg.v[e] = dx[i].v[e] * w[i].v[e] * (p.y_gain ? (float)y_gain[i][e] : 1.f);
             dx[i].v[e] *= (float)row.gate[i][e];
           }
-          store_piece<W, WHOLE>(p.dgate.row<T>(t), c, d, dg);
+          store_piece<W, FORM>(p.dgate.row<T>(t), c, d, dg);
         }
 #pragma unroll
         for (int e = 0; e < W; ++e) sum_block[i].v[e] += dx[i].v[e] * w[i].v[e];
@@ -242,7 +250,7 @@ __global__ __launch_bounds__(MOST) void k_residual_norm_bwd(const ResidualNormAr
           for (int e = 0; e < W; ++e) dx[i].v[e] = r * (dx[i].v[e] - w[i].v[e] * m);
       }
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) store_piece<W, WHOLE>(p.dy.row<T>(t), (i * lanes + lane) * W, d, dx[i]);
+      for (int i = 0; i < PIECES; ++i) store_piece<W, FORM>(p.dy.row<T>(t), (i * lanes + lane) * W, d, dx[i]);
     }
   }
   if (!p.partials) return;
@@ -250,8 +258,8 @@ __global__ __launch_bounds__(MOST) void k_residual_norm_bwd(const ResidualNormAr
   if constexpr (ROWS == 1) {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      store_piece<W, WHOLE>(to, (i * lanes + lane) * W, d, sum_gain[i]);
-      store_piece<W, WHOLE>(to + d, (i * lanes + lane) * W, d, sum_block[i]);
+      store_piece<W, FORM>(to, (i * lanes + lane) * W, d, sum_gain[i]);
+      store_piece<W, FORM>(to + d, (i * lanes + lane) * W, d, sum_block[i]);
     }
   } else {
     // the workgroup's rows, added in their order

@@ -39,14 +39,18 @@ __device__ __forceinline__ auto widened(const R& raw) {
   return x;
 }
 
-// Channels c .. c + W - 1 of a row of d.  WHOLE: d is a multiple of W, and lanes behind the row's end repeat its last piece: their loads need no
-// branch, which would keep those after it waiting (16411 rows of 768 bf16 channels in 128 lanes backwards 76 us with branches, 44 without).
-// Otherwise there are zeros behind the end.  ONCE: an access that leaves nothing in the caches.
-template <int W, bool WHOLE, bool ONCE = false, class T>
+// Rows of d channels in pieces of W: d is a multiple of W, has a part of a piece more, or may be anything, fewer than W too.
+enum Form { kWhole, kRagged, kAny };
+
+// Channels c .. c + W - 1 of a row of d.  Loads of whole and ragged rows need no branch, which would keep those after it waiting (16411 rows of
+// 768 bf16 channels in 128 lanes backwards 76 us with branches, 44 without; 16000 of 333 52 and 24): lanes behind the row's last W channels load
+// those.  In ragged rows `own` drops what the lane before holds of them; lanes behind a whole row's end repeat its last piece.  Of rows of any
+// width, the part behind the end is zero.  ONCE: an access that leaves nothing in the caches.
+template <int W, Form FORM, bool ONCE = false, class T>
 __device__ __forceinline__ Raw<T, W> load_raw(const T* row, int c, int d) {
   typedef typename RawOf<T, W>::words words;
-  if (WHOLE || c + W <= d) {
-    const words* at = (const words*)(row + (WHOLE ? min(c, d - W) : c));
+  if (FORM != kAny || c + W <= d) {
+    const words* at = (const words*)(row + (FORM != kAny ? min(c, d - W) : c));
     if constexpr (ONCE) return __builtin_bit_cast(Raw<T, W>, __builtin_nontemporal_load(at));
     else return __builtin_bit_cast(Raw<T, W>, *at);
   }
@@ -56,9 +60,27 @@ __device__ __forceinline__ Raw<T, W> load_raw(const T* row, int c, int d) {
     if (c + i < d) x[i] = row[c + i];
   return x;
 }
-template <int W, bool WHOLE, bool ONCE = false, class T>
+// What was loaded, once it is there: a ragged row's last piece begins at c, with zeros behind the row's end.
+template <Form FORM, class R>
+__device__ __forceinline__ R own(const R& raw, int c, int d) {
+  if constexpr (FORM != kRagged) return raw;
+  constexpr int W = sizeof(R) / sizeof(raw[0]), N = sizeof(R) / 4, PER = W / N;
+  typedef uint32_t words __attribute__((ext_vector_type(N)));
+  words x = __builtin_bit_cast(words, raw);
+  const int before = min(max(c + W - d, 0), W), whole = before / PER;          // channels to drop, and words of them
+#pragma unroll
+  for (int step = 4; step >= 1; step /= 2)
+    if (step <= N)
+#pragma unroll
+      for (int k = 0; k < N; ++k) x[k] = whole & step ? (k + step < N ? x[k + step] : 0u) : x[k];
+  if constexpr (PER == 2)
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = before & 1 ? (k + 1 < N ? x[k + 1] << 16 | x[k] >> 16 : x[k] >> 16) : x[k];
+  return __builtin_bit_cast(R, x);
+}
+template <int W, Form FORM, bool ONCE = false, class T>
 __device__ __forceinline__ Piece<W> load_piece(const T* row, int c, int d) {
-  return widened(load_raw<W, WHOLE, ONCE>(row, c, d));
+  return widened(own<FORM>(load_raw<W, FORM, ONCE>(row, c, d), c, d));
 }
 
 // Rounding to bf16 is to nearest even, once, of values held in 32 bits until then.
@@ -71,11 +93,11 @@ __device__ __forceinline__ void store_whole(T* p, const Piece<W>& x) {
   if constexpr (ONCE) __builtin_nontemporal_store(__builtin_bit_cast(words, b), (words*)p);
   else *(words*)p = __builtin_bit_cast(words, b);
 }
-template <int W, bool WHOLE, bool ONCE = false, class T>
+template <int W, Form FORM, bool ONCE = false, class T>
 __device__ __forceinline__ void store_piece(T* row, int c, int d, const Piece<W>& x) {
   if (c + W <= d) {
     store_whole<W, ONCE>(row + c, x);
-  } else if constexpr (!WHOLE) {
+  } else if constexpr (FORM != kWhole) {
 #pragma unroll
     for (int i = 0; i < W; ++i)
       if (c + i < d) row[c + i] = (T)x.v[i];

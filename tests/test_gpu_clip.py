@@ -57,6 +57,21 @@ def test_norm_and_clipping(types, sizes):
         assert all(torch.equal(k, o) for k, o in zip(kept, out))
 
 
+@pytest.mark.parametrize("n", [2047, 2048, 2049, 2055, 2056, 2057, 4091, 4095, 4096, 4097, 4103, 4104, 6145])
+def test_chunks_that_end_inside_two_pieces(n):
+    """A lane's two pieces of a chunk, and what is left of it, with the norm in one launch and in its own; the same bits in place."""
+    for more in ([], [17000000]):
+        for types in ("f32", "bf16"):
+            grads = tensors([n] + more, types)
+            norm = orc.grad_norm(grads)[0]
+            out = [torch.full_like(g, 5.0) for g in grads]
+            oapl.clip_grads(grads, float(norm) / 3, out=out)
+            for o, (v, b) in zip(out, orc.clipped(grads, float(norm) / 3, norm)):
+                near(o, v, b)
+            oapl.clip_grads(grads, float(norm) / 3)
+            assert all(torch.equal(g, o) for g, o in zip(grads, out))
+
+
 def test_any_element_of_a_buffer():
     """Tensors that start anywhere, results that start anywhere else; nothing beside them is touched."""
     for dtype in (torch.float32, torch.bfloat16):

@@ -243,3 +243,23 @@ def test_refusals():
         oapl.embed_bwd(E[:3], t, dE=torch.zeros(5, 8, device=DEV).bfloat16())
     with pytest.raises(oapl.OaplError):
         oapl.embed_bwd(E[:3], t, 5, workspace=torch.zeros(255, device=DEV, dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("d", [1, 2, 3, 5, 6, 7, 9, 11, 253, 254, 255, 257, 509, 515, 1023, 1029])
+def test_widths_that_end_inside_a_piece(dtype, d):
+    """With NaN on both sides of every row of the gradient, and of the embedding."""
+    for T, V in ((41, 6), (8300, 60)):
+        tokens = _tokens("zipf", T, V)
+        E = torch.full((V * d + 40,), torch.nan, device=DEV, dtype=DTYPES[dtype])
+        E[11:11 + V * d] = torch.randn(V * d, generator=_gen(d), device=DEV)
+        rows = E[11:11 + V * d].view(V, d)
+        assert torch.equal(oapl.embed_fwd(rows, tokens), rows[tokens.long()])
+        wide = torch.full((T, d + 20), torch.nan, device=DEV, dtype=DTYPES[dtype])
+        wide[:, 9:9 + d] = torch.randn(T, d, generator=_gen(d + 1), device=DEV)
+        dout = wide[:, 9:9 + d]
+        into = torch.full((V * d + 40,), 3.0, device=DEV)
+        dE = into[13:13 + V * d].view(V, d)
+        oapl.embed_bwd(dout, tokens, dE=dE)
+        near(dE, *orc.embed_grads(dout, tokens, V, 1.0))
+        assert bool((into[:13] == 3).all()) and bool((into[13 + V * d:] == 3).all())

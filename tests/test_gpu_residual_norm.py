@@ -119,6 +119,35 @@ def test_rows_inside_larger_buffers(types):
 
 
 @pytest.mark.parametrize("types", list(TYPES))
+@pytest.mark.parametrize("d", [2, 3, 4, 5, 9, 10, 11, 12, 13, 14, 15, 125, 131, 509, 515, 777, 1021, 2047, 4099, 6002, 8191, 8193, 16381])
+def test_widths_that_end_inside_a_piece(types, d):
+    """With NaN on both sides of every row, and in place."""
+    T = 37 if d < 2000 else 5
+    v, dx_out, dout = inputs(types, T, d, ["pre", "block", "post", "token"], seed=d)
+
+    def inside(x):
+        wide = torch.full((T, d + 20), torch.nan, device=DEV, dtype=x.dtype)
+        wide[:, 9:9 + d] = x
+        return wide, wide[:, 9:9 + d]
+
+    for n in ("x", "y", "gate"):
+        _, v[n] = inside(v[n])
+    for n in ("gain", "y_gain"):
+        v[n] = torch.cat((v[n] * torch.nan, v[n], v[n] * torch.nan))[d:2 * d]
+    (_, dx_out), (_, dout) = inside(dx_out), inside(dout)
+    plain = check_forward(v, 0.7)
+    want = check_backward(v, dx_out, dout, 0.7)
+    (wx, x), (wy, y), (wdx, dx), (wdy, dy) = (inside(t) for t in (v["x"], v["y"], dx_out, dout))
+    r = oapl.residual_norm_fwd(x, y, v["gain"], y_gain=v["y_gain"], gate=v["gate"], scale=0.7, x_out=x, out=y)
+    assert torch.equal(r.x, plain.x) and torch.equal(r.out, plain.out)
+    got = oapl.residual_norm_bwd(v["x"], v["y"], dx, dy, v["gain"], y_gain=v["y_gain"], gate=v["gate"], scale=0.7, dx=dx, dy=dy)
+    for a, b in zip(got[:5], want[:5]):
+        assert torch.equal(a, b)
+    for wide in (wx, wy, wdx, wdy):
+        assert bool(wide[:, :9].isnan().all()) and bool(wide[:, 9 + d:].isnan().all())
+
+
+@pytest.mark.parametrize("types", list(TYPES))
 def test_in_place(types):
     v, dx_out, dout = inputs(types, 300, 1500, ["pre", "block", "post", "token"])
     plain = check_forward(v, 1.0)
