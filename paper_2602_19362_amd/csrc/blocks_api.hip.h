@@ -51,9 +51,10 @@ static bool embed_plan(EmbedPlan& p, int64_t T, int d, int V) {
     return was;
   };
   p.off_keys[1] = take(T * 4), p.off_places[1] = take(T * 4);
-  // Counting / sorting, us for the whole call in bf16: d = 512, V = 1000 8000 tokens 28 / 34; d = 1024 30 / 36; d = 2048, V = 8192 41 / 43; d = 4096,
-  // V = 1544 6000 34 / 45, 8000 45 / 44; d = 5120, V = 8192 6000 65 / 65 (a frequent token's rows are read by one workgroup a slice).
-  p.few = T <= (d <= 2048 ? kFewTokens : kFewTokens * 3 / 4);
+  // Counting / sorting, us for the whole call in bf16: d = 64, V = 1000 8000 tokens 24 / 33; d = 512 8000 28 / 34; d = 1024 8000 30 / 36; d = 4096,
+  // V = 1544 4000 25 / 40, 6000 34 / 45.  With a token in half of the places, whose rows one workgroup a slice reads: d = 64 4000 37 / 34, 8000 74 / 36;
+  // d = 1024 8000 95 / 42; d = 4096 4000 54 / 40, 6000 82 / 44.
+  p.few = T <= (d <= 512 ? kFewTokens : kFewTokens / 2);
   if (p.few) return true;
   while (((int64_t)1 << (2 * p.bits)) <= V) ++p.bits;      // ids 0 .. V
   p.items = T <= 128 * kSortThreads * 2 ? 2 : 8;

@@ -299,10 +299,29 @@ __global__ __launch_bounds__(256) void k_embed_sum(const EmbedSumArgs p) {
   }
 }
 
+// How many of the numbers before i, i - 1 and on, `f` holds for; it holds for none before the first that it does not hold for, and for fewer than
+// 64^3.  A wavefront asks for 64 of them, and where it holds for all, for every 4096th, every 64th and every one: 8000 equal ids are four
+// loads one after the other, not 125 (d = 64, V = 8192: half of 8000 tokens the same 89 us for the whole call with 125, 74 with four; all of
+// 140897 140 and 117).
+template <class F>
+__device__ __forceinline__ int equal_before(int i, F f) {
+  const int lane = threadIdx.x & 63;
+  const auto steps = [&](int from, int step) {
+    const uint64_t not_held = __ballot(!f(from - (lane + 1) * step));
+    return not_held ? __ffsll((unsigned long long)not_held) - 1 : 64;
+  };
+  int n = steps(i, 1);
+  if (n < 64) return n;
+  n = 0;
+#pragma unroll
+  for (int step = 4096; step >= 1; step /= 64) n += steps(i - n, step) * step;
+  return n;
+}
+
 // Tokens that reach over the ends of tiles: where one ends in one of a workgroup's tiles, its wavefronts add up what the tiles have of it,
 // equal parts of them each, in their order and in 64 bits.  Tiles and wavefronts of a workgroup 4 and 4 / 4 and 8 / 16 and 8 / 16 and 16, whole call of
 // 140897 tokens: 783 / 807 / 804 / 885 us.
-// Its loads need no branch where rows are whole: 100000 tokens, d = 64, V = 8192, one id, 569 -> 183 us; one in every 21 of V = 1000 75 -> 55.
+// Its loads need no branch: 100000 tokens, d = 64, V = 8192, one id, 296 us with branches, 105 without; one in 21 of V = 1000 60 and 51.
 constexpr int kJoinTiles = 4, kJoinParts = 4;
 
 template <Form FORM>
@@ -319,13 +338,8 @@ __global__ __launch_bounds__(64 * kJoinParts) void k_embed_join(const EmbedSumAr
   }
   for (uint64_t todo = __ballot(here); todo; todo &= todo - 1) {
     const int at = __ffsll((unsigned long long)todo) - 1, v = __builtin_amdgcn_readlane(key, at), tile = tile0 + at;
-    int begin = tile;                   // the tile that the token begins in: the last one that does not begin in the middle of it
-    for (;;) {
-      const int t = begin - lane;
-      const uint64_t found = __ballot(t <= 0 || p.keys[(int64_t)t * p.tile - 1] != v);
-      begin -= found ? __ffsll((unsigned long long)found) - 1 : 64;
-      if (found) break;
-    }
+    // the tile that the token begins in: the last one that does not begin in the middle of it, as `tile` does
+    const int begin = tile - equal_before(tile, [&](int t) { return t > 0 && p.keys[(int64_t)t * p.tile - 1] == v; }) - 1;
     const int n = tile - begin + 1, lo = (int)((int64_t)n * wave / kJoinParts), hi = (int)((int64_t)n * (wave + 1) / kJoinParts);
     double sum[4] = {};
 #pragma unroll 8
@@ -455,12 +469,8 @@ __global__ __launch_bounds__(64 * kRunWaves) void k_embed_runs(const EmbedSumArg
   }
   if (!begins || !on || __builtin_amdgcn_readlane(key, last) >= p.V) return;
   const int v = __builtin_amdgcn_readlane(key, last);
-  end = from + n;                                             // its last position and one
-  for (;;) {
-    const uint64_t other = __ballot(end + lane >= p.T || p.keys[end + lane] != v);
-    end += other ? __ffsll((unsigned long long)other) - 1 : 64;
-    if (other) break;
-  }
+  // its last position and one
+  end = from + n + equal_before(0, [&](int i) { return from + n - i <= p.T && p.keys[from + n - i - 1] == v; });
   const int begin = from + last, rows = end - begin, lo = begin + rows * wave / kRunWaves, hi = begin + rows * (wave + 1) / kRunWaves;
   sum = Piece<4>{};
   for (int base = lo; base < hi; base += 64) {

@@ -78,7 +78,7 @@ CASES = [("bf16", 1, 8, 1, "one"), ("bf16", 5, 64, 100, "even"), ("f32", 63, 20,
 
 
 # On both sides of the rules: sorting by counting or in passes, tiles of sorted rows, rows past the caches.
-RULES = [("bf16", 8192, 2048, 700, "zipf"), ("bf16", 8193, 2048, 700, "zipf"), ("bf16", 6144, 2052, 900, "one"), ("f32", 6145, 2052, 900, "zipf"),
+RULES = [("bf16", 8192, 512, 700, "zipf"), ("bf16", 8193, 512, 700, "zipf"), ("bf16", 4096, 516, 900, "one"), ("f32", 4097, 516, 900, "zipf"),
          ("bf16", 8192, 2050, 300, "zipf"), ("f32", 262144, 12, 5000, "zipf"), ("f32", 262145, 12, 5000, "zipf"), ("bf16", 8192, 4096, 500, "even"),
          ("bf16", 8193, 4096, 500, "even"), ("f32", 4097, 4099, 300, "zipf"), ("bf16", 100000, 64, 8192, "one"), ("f32", 20000, 66, 1000, "one")]
 
@@ -108,9 +108,20 @@ def test_gradient(dtype, T, d, V, kind):
     assert torch.equal(third.dE, r.dE)
 
 
+def _want(dout, tokens, V):
+    """The oracle on the CPU, which adds up many rows of one token sooner."""
+    return [x.to(DEV) for x in orc.embed_grads(dout.cpu(), tokens.cpu(), V, 1.0)]
+
+
 @pytest.mark.parametrize("dtype, T, d, V, kind", RULES)
 def test_gradient_beside_the_rules(dtype, T, d, V, kind):
-    test_gradient(dtype, T, d, V, kind)
+    tokens = _tokens(kind, T, V)
+    dout = torch.randn(T, d, generator=_gen(4), device=DEV).to(DTYPES[dtype])
+    r = oapl.embed_bwd(dout, tokens, V)
+    near(r.dE, *_want(dout, tokens, V))
+    r.workspace.fill_(255)
+    again = oapl.embed_bwd(dout, tokens, dE=torch.full_like(r.dE, torch.nan), workspace=r.workspace)
+    assert torch.equal(again.dE, r.dE)
 
 
 @pytest.mark.parametrize("T, d", [(500, 40), (7000, 64), (9001, 64), (9001, 70), (50000, 256)])
@@ -124,8 +135,7 @@ def test_gradient_of_a_padded_batch(T, d):
     r = oapl.embed_bwd(dout, tokens, V)
     assert oapl.read_device_status(r.workspace) != 0
     inside = tokens < V
-    want, bound = orc.embed_grads(dout[inside], tokens[inside], V, 1.0)
-    near(r.dE, want, bound)
+    near(r.dE, *_want(dout[inside], tokens[inside], V))
 
 
 
@@ -263,3 +273,18 @@ def test_widths_that_end_inside_a_piece(dtype, d):
         oapl.embed_bwd(dout, tokens, dE=dE)
         near(dE, *orc.embed_grads(dout, tokens, V, 1.0))
         assert bool((into[:13] == 3).all()) and bool((into[13 + V * d:] == 3).all())
+
+
+@pytest.mark.parametrize("T, run", [(8192, 8192), (8192, 4096), (8192, 4161), (5000, 95), (5000, 96), (5000, 97), (5000, 160), (5000, 4160), (9000, 2048),
+                                    (9000, 2049), (140000, 131072), (140000, 139999), (262144, 200001)])
+def test_one_token_among_others(T, run):
+    """Its sorted rows end, and begin, at steps of the search for where they do, and beside them."""
+    V = 50
+    tokens = _tokens("even", T, V)
+    tokens[torch.randperm(T, generator=_gen(7), device=DEV)[:run]] = 23
+    dout = torch.randn(T, 8, generator=_gen(8), device=DEV)
+    near(oapl.embed_bwd(dout, tokens, V).dE, *_want(dout, tokens, V))
+    tokens = torch.arange(T, device=DEV, dtype=torch.int32).clamp_(max=T - run)         # all others before it, and behind it
+    near(oapl.embed_bwd(dout, tokens, T).dE, *_want(dout, tokens, T))
+    tokens = (tokens - (T - run)).neg_()
+    near(oapl.embed_bwd(dout, tokens, T).dE, *_want(dout, tokens, T))
