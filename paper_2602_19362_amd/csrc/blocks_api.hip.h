@@ -76,6 +76,10 @@ static dim3 wide_grid(int64_t n, int64_t most) {
   return dim3((unsigned)std::min(n, most), (unsigned)((n + most - 1) / most));
 }
 
+// k_embed_sum's: a workgroup for every tile and 1024 channels, which are 2^24 of them and more at the ends of the sizes.  Rows of 2^20, so that
+// calls of 2^36 elements of dout have more than one.
+static dim3 embed_sum_grid(const EmbedPlan& p, int d) { return wide_grid((int64_t)p.tiles * grid1d(d, 1024), 1 << 20); }
+
 // f(true or false as a type).
 template <class F>
 static void by_truth(bool x, F f) {
@@ -361,7 +365,7 @@ int32_t oapl_embed_bwd(const oapl_rows* dout, const int32_t* tokens, int64_t T, 
   if (int rc = p.items == 2 ? launch_embed_sort<2>(s, st) : launch_embed_sort<8>(s, st)) return rc;
   a.partials = (float*)(ws + p.off_partials);
   a.tile = p.tile, a.tiles = p.tiles, a.slices = (int)grid1d(d, 1024);
-  const unsigned grid = (unsigned)p.tiles * a.slices;
+  const dim3 grid = embed_sum_grid(p, d);
   // Beyond 64 MiB rows, in and out, go past the caches, us in bf16: 140897 tokens, d = 4096 (1.15 GB) 758 -> 723, 40000, d = 2048, V = 151936
   // 300 -> 286; d = 4096: V = 1000 15000 (123 MB) 66 -> 62, V = 1544 10000 (82 MB) 51 -> 52; d = 2048, V = 8192 10000 (41 MB) 46 -> 48.
   const bool once = T * d * (int64_t)esize(dtype) > (int64_t)64 << 20;

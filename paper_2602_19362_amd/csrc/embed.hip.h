@@ -267,8 +267,9 @@ __device__ __forceinline__ void add_rows(const EmbedSumArgs& p, Piece<4>& sum, i
 // positions of 64 rows in its lanes, so that its walk over them branches on scalars.  ONCE: rows past the caches, in and out.
 template <class T, Form FORM, bool ONCE>
 __global__ __launch_bounds__(256) void k_embed_sum(const EmbedSumArgs p) {
-  const int lane = threadIdx.x & 63, tile = blockIdx.x / p.slices, c = (blockIdx.x % p.slices * 256 + threadIdx.x) * 4;
-  if (c - lane * 4 >= p.d) return;
+  const uint32_t unit = blockIdx.y * gridDim.x + blockIdx.x;
+  const int lane = threadIdx.x & 63, tile = unit / p.slices, c = (unit % p.slices * 256 + threadIdx.x) * 4;
+  if (tile >= p.tiles || c - lane * 4 >= p.d) return;
   const int from = tile * p.tile, to = from + p.tile < p.T ? from + p.tile : (int)p.T;
   const int first = p.keys[from], last = p.keys[to - 1];
   const bool begun = from > 0 && p.keys[from - 1] == first, open = to < p.T && p.keys[to] == last;

@@ -1,0 +1,29 @@
+"""Launches of the embedding's gradient at the ends of the sizes that it takes, checked on the host under AddressSanitizer and
+UndefinedBehaviorSanitizer; compiled for the host alone and run on the CPU."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def test_launches_at_the_ends_of_the_sizes(tmp_path):
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    if shutil.which(hipcc) is None:
+        pytest.skip("hipcc not found")
+    exe = str(tmp_path / "blocks_limits_driver")
+    # no device pass: the code object that the launch stubs refer to is missing, and nothing is launched
+    cmd = [hipcc, "--offload-arch=gfx950", "--offload-host-only", "-O1", "-g", "-std=c++17", "-x", "hip",
+           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+           "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
+           "-Xarch_host", "-fno-sanitize-recover=all",
+           "-I", os.path.join(ROOT, "include"), os.path.join(ROOT, "tests", "host_sanitize", "blocks_limits_driver.cpp"), "-o", exe,
+           "-Wl,--unresolved-symbols=ignore-all"]
+    build = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=600)
+    assert build.returncode == 0, build.stdout[-4000:]
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:abort_on_error=1", UBSAN_OPTIONS="print_stacktrace=1")
+    run = subprocess.run([exe], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=600, env=env)
+    assert run.returncode == 0, run.stdout[-4000:]
+    assert "all checks passed" in run.stdout
