@@ -62,7 +62,9 @@ static bool embed_plan(EmbedPlan& p, int64_t T, int d, int V) {
   // By the wavefronts that a row's channels take, all rows together.  16 / 32 / 64 rows a tile, us for the whole call in bf16: d = 4096: V = 1544
   // 10000 tokens 55 / 51 / 51, 20000 82 / 77 / 75, V = 151936 140897 762 / 731 / 723; d = 1024, V = 8192 40000 62 / 59 / 61, 80000 92 / 88 / 87; d = 64,
   // V = 151936 50000 47 / 50 / 54, 140000 67 / 65 / 67, V = 8192 400000 144 / 129 / 125.
-  p.tile = T * ((d + 255) / 256) <= 1 << 18 ? 32 : 64;
+  constexpr int64_t small = 1 << 18;
+  p.tile = T * ((d + 255) / 256) <= small ? 32 : 64;
+  static_assert(kMaxRows / 64 < kMostEqual && small / 32 < kMostEqual && kFewTokens < kMostEqual, "a token's rows and tiles are found by equal_before");
   p.tiles = (int)((T + p.tile - 1) / p.tile);
   p.off_keys[0] = take(T * 4), p.off_places[0] = take(T * 4);
   for (int i = 0; i < 2; ++i) p.off_counts[i] = take(((int64_t)p.blocks << p.bits) * 4);

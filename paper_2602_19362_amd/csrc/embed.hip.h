@@ -301,9 +301,10 @@ __global__ __launch_bounds__(256) void k_embed_sum(const EmbedSumArgs p) {
 }
 
 // How many of the numbers before i, i - 1 and on, `f` holds for; it holds for none before the first that it does not hold for, and for fewer than
-// 64^3.  A wavefront asks for 64 of them, and where it holds for all, for every 4096th, every 64th and every one: 8000 equal ids are four
+// kMostEqual.  A wavefront asks for 64 of them, and where it holds for all, for every 4096th, every 64th and every one: 8000 equal ids are four
 // loads one after the other, not 125 (d = 64, V = 8192: half of 8000 tokens the same 89 us for the whole call with 125, 74 with four; all of
 // 140897 140 and 117).
+constexpr int kMostEqual = 64 * 64 * 64;
 template <class F>
 __device__ __forceinline__ int equal_before(int i, F f) {
   const int lane = threadIdx.x & 63;

@@ -37,6 +37,8 @@ int main() {
         CHECK(fits(dim3(grid1d(T, 32), grid1d(d, 256)), 64 * kRunWaves));
         continue;
       }
+      // a token may have all of the tiles, which one search goes through
+      CHECK(p.tiles < kMostEqual);
       const dim3 sum = embed_sum_grid(p, d);
       const int64_t units = (int64_t)p.tiles * grid1d(d, 1024);
       CHECK(fits(sum, 256) && (int64_t)sum.x * sum.y >= units && (int64_t)sum.x * (sum.y - 1) < units);
