@@ -553,9 +553,10 @@ size_t oapl_residual_norm_workspace_bytes(int64_t T, int32_t d);
  *
  * (without y_gain dy = dz).  Norms are taken of x' as it is stored.
  *   dx, dy         [T][d] in x_dtype and dtype; dx may be dx_out or x, dy may be y or dout
- *   dgain, dy_gain [d] float, summed over tokens in a fixed order; NULL where there is no such gain
+ *   dgain, dy_gain [d] float, summed over tokens in a fixed order: at most 1024 rows one after the other in 32 bits, then up to 16 such sums, and
+ *                  all others in 64; NULL where there is no such gain
  *   dgate_rows     rows [T][d] in dtype, may be gate: of a gate for every token; otherwise not looked at
- *   dgate          [d] float, summed over tokens: of a gate that they share; otherwise not looked at
+ *   dgate          [d] float, summed over tokens in the same way: of a gate that they share; otherwise not looked at
  * The workspace is looked at only where there is a sum over tokens.
  */
 int32_t oapl_residual_norm_bwd(const oapl_rows* x, const oapl_rows* y, const void* y_gain, const oapl_rows* gate, int32_t gate_per_token,

@@ -174,6 +174,20 @@ static unsigned norm_bwd_grid(int64_t T, int d) {
   return (unsigned)std::min<int64_t>(norm_workgroups(T, d), std::max(256, 256 * 512 / norm_lanes(d)));
 }
 
+// In 32 bits a workgroup adds up so many rows one after the other and no more: more tokens are several launches, each with sums of its own, which
+// are added in 64 bits.  Equal rows of 129 channels, 8192 of them one after the other: off by up to 2017 roundings.  One launch / several, bf16:
+// 300000 tokens, d = 4096 2837 / 2652 us, 600000 5573 / 5282, 2000000, d = 520 3779 / 3739.
+constexpr int kNormChain = 1024;
+struct NormParts {
+  int n;
+  int64_t rows;      // of one
+};
+static NormParts norm_bwd_parts(int64_t T, int d) {
+  const int64_t workgroups = norm_workgroups(T, d), at_once = std::max<int64_t>(1, (int64_t)norm_bwd_grid(T, d) * kNormChain);
+  const int64_t n = std::max<int64_t>(1, (workgroups + at_once - 1) / at_once);
+  return {(int)n, (workgroups + n - 1) / n * norm_rows(d)};
+}
+
 static int residual_norm_args(ResidualNormArgs& a, const oapl_rows* x, const oapl_rows* y, const void* y_gain, const oapl_rows* gate,
                               int gate_per_token, const void* gain, int64_t T, int d, int x_dtype, int dtype, float scale, float eps) {
   if (!dtype_ok(x_dtype) || !dtype_ok(dtype) || (x_dtype == OAPL_BF16 && dtype == OAPL_F32)) return OAPL_ERR_DTYPE;
@@ -417,7 +431,7 @@ int32_t oapl_residual_norm_fwd(const oapl_rows* x, const oapl_rows* y, const voi
 
 size_t oapl_residual_norm_workspace_bytes(int64_t T, int32_t d) {
   if (T < 0 || T > kMaxRows || d < 1 || d > kMaxNormWidth) return 0;
-  return (size_t)round_up((int64_t)norm_bwd_grid(T, d) * 2 * d * (int64_t)sizeof(float) + 1, 256);
+  return (size_t)round_up((int64_t)norm_bwd_parts(T, d).n * norm_bwd_grid(T, d) * 2 * d * (int64_t)sizeof(float) + 1, 256);
 }
 
 int32_t oapl_residual_norm_bwd(const oapl_rows* x, const oapl_rows* y, const void* y_gain, const oapl_rows* gate, int32_t gate_per_token,
@@ -441,22 +455,28 @@ int32_t oapl_residual_norm_bwd(const oapl_rows* x, const oapl_rows* y, const voi
   a.partials = sums ? (float*)workspace : nullptr;
   hipStream_t st = (hipStream_t)stream;
   const unsigned grid = norm_bwd_grid(T, d);
+  const NormParts parts = sums ? norm_bwd_parts(T, d) : NormParts{1, T};
   return by_types(x_dtype, dtype, [&](auto* tx, auto* t) -> int {
     typedef std::remove_pointer_t<decltype(tx)> TX;
     typedef std::remove_pointer_t<decltype(t)> TY;
-    if (T > 0) {
+    for (int i = 0; i < parts.n && T > 0; ++i) {
+      ResidualNormArgs b = a;
+      for (Rows* rows : {&b.x, &b.y, &b.gate, &b.x_out, &b.out, &b.dx, &b.dy, &b.dgate})
+        if (rows->p) rows->p += i * parts.rows * rows->stride;
+      if (sums) b.partials += (int64_t)i * grid * 2 * d;
+      b.T = std::min(parts.rows, T - i * parts.rows);
       constexpr int W = sizeof(TX) == 2 ? 8 : 4;
       by_width<W>(d, [&](auto lanes, auto most, auto pieces) {
         by_form<W, decltype(lanes)::value == 16>(d, [&](auto form) {
           constexpr int LANES = lanes, MOST = most, PIECES = pieces;
           constexpr Form FORM = form;
-          k_residual_norm_bwd<TX, TY, W, LANES, MOST, PIECES, FORM><<<grid, norm_lanes(d), 0, st>>>(a);
+          k_residual_norm_bwd<TX, TY, W, LANES, MOST, PIECES, FORM><<<grid, norm_lanes(d), 0, st>>>(b);
         });
       });
       OAPL_LAUNCH_CHECK();
     }
     if (sums) {
-      k_norm_gain_grads<TY><<<grid1d(2 * d, 16), 1024, 0, st>>>(a.partials, (int)grid, d,
+      k_norm_gain_grads<TY><<<grid1d(2 * d, 16), 1024, 0, st>>>(a.partials, parts.n * (int)grid, d,
                                                                shared ? (const TY*)gate->data : nullptr, (const TY*)y_gain,
                                                                gain ? dgain : nullptr, y_gain ? dy_gain : nullptr, shared ? dgate : nullptr);
       OAPL_LAUNCH_CHECK();

@@ -1,4 +1,4 @@
-// Launches of the embedding's gradient at the ends of the sizes that it takes, compiled for the host alone with AddressSanitizer and
+// Launches of the gradients of embedding and residual norm at the ends of the sizes that they take, compiled for the host alone with AddressSanitizer and
 // UndefinedBehaviorSanitizer: a dimension of a launch has fewer than 2^32 threads, and the other ones fewer than 2^16 workgroups.  Nothing is launched.
 #include <cstdint>
 #include <cstdio>
@@ -47,6 +47,16 @@ int main() {
       CHECK((int64_t)sum.x * sum.y < (int64_t)1 << 31);
     }
   }
+  for (int64_t T : counts)
+    for (int d : {1, 127, 128, 129, 512, 513, 1024, 4096, 4097, 8192, 8193, 16384}) {
+      const NormParts parts = norm_bwd_parts(T, d);
+      const int64_t grid = norm_bwd_grid(T, d), slots = grid * norm_rows(d);
+      ++plans;
+      // parts hold all rows, none is empty, and a lane has no more than the chain's rows of one
+      CHECK(parts.n >= 1 && parts.n * parts.rows >= T && (T == 0 || (parts.n - 1) * parts.rows < T) && parts.rows % norm_rows(d) == 0);
+      CHECK(parts.rows <= slots * 1024);
+      CHECK(oapl_residual_norm_workspace_bytes(T, d) >= (size_t)(parts.n * grid * 2 * d * 4));
+    }
   std::printf("launches of %ld plans, all checks passed\n", plans);
   return 0;
 }

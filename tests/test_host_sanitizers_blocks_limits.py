@@ -1,4 +1,4 @@
-"""Launches of the embedding's gradient at the ends of the sizes that it takes, checked on the host under AddressSanitizer and
+"""Launches of the gradients of embedding and residual norm at the ends of the sizes that they take, checked on the host under AddressSanitizer and
 UndefinedBehaviorSanitizer; compiled for the host alone and run on the CPU."""
 import os
 import shutil
