@@ -492,7 +492,9 @@ typedef struct {
 } oapl_rows;
 
 /*
- * Rows of the embedding, scaled:   out_t = scale E[tokens_t],   rounded once.
+ * Rows of the embedding, scaled:   out_t = scale E[tokens_t]
+ *
+ * The product is rounded to 32 bits, and from there to out_dtype.
  *   E        [V][d] in dtype (may be the head's W), from any element on
  *   tokens   [T] int32 in [0, V); a token outside gets NaN
  *   out      [T][d] in out_dtype
@@ -508,7 +510,8 @@ size_t oapl_embed_workspace_bytes(int64_t T, int32_t d, int32_t V);
 /*
  * Its gradient:   dE[v] = scale sum over t with tokens_t = v of dout_t
  *
- * summed in 32 bits and in a fixed order (the same bits every time).
+ * summed in a fixed order (the same bits every time): at most 1024 rows one after the other in 32 bits, then at most eight such sums in 32
+ * bits, or any number of them in 64.
  *   dout        [T][d] in dtype
  *   accumulate  0: dE is overwritten, rows without tokens with zeros; otherwise the sums are added to what dE holds (the head's dW, where
  *               embedding and head share their weights), and rows without tokens stay as they are
@@ -592,7 +595,8 @@ int32_t oapl_grad_norm(const oapl_tensor* tensors, int32_t n_tensors, float* nor
 /*
  * Tensors scaled to a common norm:   out = g max_norm / norm   where norm is finite and larger than max_norm, otherwise out = g
  *
- * so what is not finite is not spread, and shows in norm.  The product is rounded once.
+ * so what is not finite is not spread, and shows in norm.  The factor and its product with g are numbers of 64 bits; the product is rounded to
+ * 32 bits, and from there to bf16 where g is.
  *   norm_given  NULL: the norm of these tensors, which is written to norm_out [1] float; or [1] float, the norm to go by (of tensors
  *               on other GPUs too, say), and norm_out NULL; no workspace is needed then
  *   max_norm    >= 0 and finite (else OAPL_ERR_BETA)
