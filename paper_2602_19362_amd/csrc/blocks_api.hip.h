@@ -168,8 +168,11 @@ static int by_types(int x_dtype, int dtype, F f) {
   return f((float*)nullptr, (float*)nullptr);
 }
 
-// Backwards every workgroup has sums of its own, and as many rows as any other.  Workgroups of 512 / 768 / 1024 lanes a compute unit, 16411 rows in
+// Backwards every workgroup has sums of its own, and as many rows as any other or one more.  Workgroups of 512 / 768 / 1024 lanes a compute unit, 16411 rows in
 // bf16: d = 4096 154 / 174 / 165 us, 2048 81 / 87 / 89 (256 lanes: 124), 1024 45.8 / 46.7 / 47.0 (70), 512 23.2 / 23.5 / 23.8 (31).
+// Few rows, the kernels alone (calls in a graph), these / as few as leave the most rows of a workgroup as they are / 512 / 256 workgroups, us: d = 768 in fp32 500
+// rows 12.1 / 12.1 / 12.1 / 10.8, 900 13.6 / 13.6 / 12.8 / 15.0, 1501 15.5 / 14.8 / 15.2 / 19.2, 2000 16.6 / 17.1 / 17.4 / 22.8, 4000 22.2 / 22.9 / 25.8 / 37.6; bf16 2048 700 rows 13.6 / 13.0 /
+// 13.6 / 13.5, 1501 17.1 / 18.2 / 16.8 / 19.3, 4000 27.3 / 27.7 / 26.8 / 35.7, 512 3000 10.5 / 11.4 / 10.4 / 11.2.
 static unsigned norm_bwd_grid(int64_t T, int d) {
   return (unsigned)std::min<int64_t>(norm_workgroups(T, d), std::max(256, 256 * 512 / norm_lanes(d)));
 }

@@ -6,10 +6,11 @@
 // by counting (k_embed_rank) and summed by the workgroup that a token's rows begin in (k_embed_runs): two launches.  Many are sorted in two
 // passes (k_embed_count, k_embed_place twice), and their sorted positions cut into tiles of equal length, so that a frequent token is shared by
 // many workgroups (k_embed_sum); what a tile has of a token that reaches over its ends goes into the workspace and is added up by another
-// launch, tile by tile (k_embed_join).  dE is cleared beside the sorting, not between reads: memory takes 6 TB/s of either alone and 4.9 of both.
+// launch, tile by tile (k_embed_join).  dE is cleared beside the sorting, not between reads: memory takes 6.6 TB/s of reads alone, 7.3 of zeros
+// and 5.3 of the sums' reads and writes.
 //
-// 140897 tokens that follow Zipf's law, d = 4096 in bf16, V = 151936 (3.6 GB): counting 6 us, first pass and 0.19 GB of zeros 40,
-// second pass and 1.72 GB of zeros 290, sums 366 (1.15 GB in, 0.65 out: 4.9 TB/s), tokens over tiles 22.  1003 of them: places and 2.49 GB of zeros 343, sums 12.
+// 140897 tokens that follow Zipf's law, d = 4096 in bf16, V = 151936 (3.6 GB): counting 6 us, first pass and 0.19 GB of zeros 39,
+// second pass and 1.86 GB of zeros 281, sums 343 (1.16 GB in, 0.66 out: 5.3 TB/s), tokens over tiles 23.  1003 of them: places and 2.49 GB of zeros 341, sums 12.
 #pragma once
 
 #include "rows.hip.h"
@@ -74,7 +75,7 @@ __device__ __forceinline__ int sort_key(const SortArgs& p, int64_t t) {
 }
 
 // 1024 elements of dE, from 1024 i on, are zero: 4 KB a workgroup, and four workgroups a compute unit, which kClearLds bytes of LDS see to, is the
-// order that memory likes best (2.49 GB in 357 us, 6.98 TB/s; 16 KB a workgroup 402, 256 KB 400 .. 430; beside the counting of 6000 tokens, eight
+// order that memory likes best (2.49 GB in a launch of its own 357 us, 16 KB a workgroup 402, 256 KB 400 .. 430; beside the places of 1003 tokens 341; beside the counting of 6000 tokens, eight
 // workgroups 431, six 425, four 409).
 constexpr int kClearLds = 33 * 1024;
 __device__ __forceinline__ void clear_piece(float* dE, int64_t n, int64_t i) {
